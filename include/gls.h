@@ -96,6 +96,7 @@ typedef enum {
 
 /* bits OR-ed into *device_status by the kernels */
 #define GLS_DEV_EMPTY_SUPPORT 1u /* some row had no finite logit: its token is -1 */
+#define GLS_DEV_BAD_TOKEN 2u     /* a token given to the calls below was not smaller than V */
 
 typedef enum { GLS_F32 = 0, GLS_BF16 = 1 } gls_dtype_t;
 
@@ -439,6 +440,116 @@ int gls_compress_select(const gls_rows_t* enc_logw, const gls_rows_t* dec_logw, 
                         int32_t* out_enc_index, uint8_t* out_message, int32_t* out_dec_index,
                         uint8_t* out_match, float* out_scores, void* workspace,
                         size_t workspace_bytes, uint32_t* device_status, void* stream);
+
+/*
+ * Log probabilities of given tokens, with the row's entropy and its most likely alternatives (no
+ * counterpart in the paper: what a serving loop reports next to the tokens it sampled, and the loss
+ * a drafter is trained on).  Per row, z = logit * inv_temp over the row's finite logits (-inf, NaN
+ * and +inf are masked, as in the races):
+ *     lse = ln sum_i e^(z_i);  log probability of token t = z_t - lse;  p_i = e^(z_i - lse)
+ *     entropy = -sum_i p_i ln p_i   (nats)
+ *     alternatives: the M largest logits in descending order, ties to the lower index
+ * The row is read once.
+ *
+ *   logits            [B,K,J,V] rows (fp32 or bf16, any alignment of their first elements)
+ *   inv_temp, inv_temp_per_draft_host  as in gls_draft_sample, each within [1e-20, 1e20]
+ *                     (GLS_ERR_UNSUPPORTED outside)
+ *   tokens            int32 [B,K,J,G], 0 <= G <= GLS_MAX_GIVEN; a token below 0 is none (0 is
+ *                     returned), one that is masked or not below V has probability zero (-inf; the
+ *                     latter ORs GLS_DEV_BAD_TOKEN into *device_status)
+ *   M                 alternatives per row, 0 .. 256
+ *   out_logprobs      fp32 [B,K,J,G] (may be NULL when G = 0)
+ *   out_lse           fp32 [B,K,J]
+ *   out_lse_tail      NULL or fp32 [B,K,J]: what rounding lse to fp32 left, for the backward call
+ *   out_entropy       NULL or fp32 [B,K,J]
+ *   out_top_ids       int32 [B,K,J,M], -1 past the row's finite logits, and
+ *   out_top_logprobs  fp32 [B,K,J,M], -inf there (may be NULL when M = 0)
+ *   workspace         gls_token_logprobs_workspace_bytes(B, K, J, V, M) bytes, 16-byte aligned; its
+ *                     contents on entry are ignored
+ * A row without a finite logit: lse -inf, entropy 0, log probabilities -inf, no alternatives, and
+ * GLS_DEV_EMPTY_SUPPORT.
+ */
+#define GLS_MAX_GIVEN 64
+size_t gls_token_logprobs_workspace_bytes(int B, int K, int J, int64_t V, int M);
+int gls_token_logprobs(const gls_rows_t* logits, int B, int K, int J, int64_t V, float inv_temp,
+                       const float* inv_temp_per_draft_host, const int32_t* tokens, int G, int M,
+                       float* out_logprobs, float* out_lse, float* out_lse_tail, float* out_entropy,
+                       int32_t* out_top_ids, float* out_top_logprobs, void* workspace,
+                       size_t workspace_bytes, uint32_t* device_status, void* stream);
+
+/*
+ * The same for the tokens that a verification emitted: position j of sequence b is scored on the
+ * target row (b, k, j) of the lowest-numbered draft k still active there (active drafts share the
+ * accepted prefix, hence the distribution).  Rows that no emitted token needs are not read.
+ *
+ *   target_logits  the rows given to gls_target_sample_verify, J = L + 1 (J = L with GLS_NO_BONUS)
+ *   tokens, accept its out_tokens [B,J] and out_accept [B,K,L] (accept may be NULL when J = 1)
+ *   flags          its GLS_NO_BONUS and GLS_COMBINE_ALL
+ *   outputs        [B,J] (alternatives [B,J,M]); at and beyond tau: 0, alternatives -1 and 0
+ *   workspace      as gls_token_logprobs
+ */
+int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, int64_t V, float inv_temp,
+                         const int32_t* tokens, const uint8_t* accept, uint32_t flags, int M,
+                         float* out_logprobs, float* out_lse, float* out_entropy, int32_t* out_top_ids,
+                         float* out_top_logprobs, void* workspace, size_t workspace_bytes,
+                         uint32_t* device_status, void* stream);
+
+/*
+ * Gradient of the outputs of gls_token_logprobs with respect to the logits.  With g the gradients
+ * given (each may be NULL) and the sums over the tokens and alternatives whose logits are finite,
+ *     d logit_i = inv_temp * [ p_i (g_lse - sum g_logprob - sum g_top - g_entropy (ln p_i + entropy))
+ *                              + sum of g_logprob and g_top at token i ]
+ * and 0 at masked logits and in rows without a finite logit.  A token that occurs several times in
+ * a row adds up.  Each element is rounded once.
+ *
+ *   lse, lse_tail (may be NULL), entropy (only with grad_entropy), top_ids (only with
+ *   grad_top_logprobs)   as returned by gls_token_logprobs for the same rows and temperatures
+ *   grad_logits          [B,K,J,V] rows of the logits' type, written in full; strides that are 0
+ *                        over more than one row and the logits' own memory are refused.  Rows whose
+ *                        first element is as far from a 32-byte boundary as the logits' row is are
+ *                        written by vectors, others element by element.
+ */
+int gls_token_logprobs_backward(const gls_rows_t* logits, int B, int K, int J, int64_t V, float inv_temp,
+                                const float* inv_temp_per_draft_host, const int32_t* tokens, int G,
+                                const int32_t* top_ids, int M, const float* lse, const float* lse_tail,
+                                const float* entropy, const float* grad_logprobs, const float* grad_lse,
+                                const float* grad_entropy, const float* grad_top_logprobs,
+                                const gls_rows_t* grad_logits, void* stream);
+
+/*
+ * Rows of a table by token, scaled: out[n,:] = scale * table[tokens[n],:], rounded once.  The
+ * inputs of the next draft position from the tokens that a call above returned, or the candidates
+ * that gls_compress_select's decoders chose (W_k = U_{X^(k)}, Sec. 5.1).  A token below 0 (behind a
+ * sequence's last token, a decoder without a candidate) gives a row of zeros, and so does one that
+ * is not below V, which also ORs GLS_DEV_BAD_TOKEN into *device_status.
+ *
+ *   table [V,D], out [N,D]: of one type (gls_dtype_t), rows contiguous, strides in elements and
+ *   at least D (table_stride is ignored for V = 1, out_stride for N = 1); N = 0 is legal.
+ *   16-byte aligned rows take vector loads, others are copied element by element.
+ */
+int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t V, int64_t D,
+                     const int32_t* tokens, int64_t N, float scale, void* out, int64_t out_stride,
+                     uint32_t* device_status, void* stream);
+
+/*
+ * Its gradient: grad_table[v,:] = scale * sum over n with tokens[n] == v of grad_out[n,:].  The
+ * tokens are sorted and every sum runs in the order of n in fp32, so equal calls return equal bits.
+ * Tokens outside [0, V) add nothing.  Rows of tokens that do not occur are written as zeros;
+ * with GLS_EMBED_ACCUMULATE the sums are added to what grad_table holds and those rows are neither
+ * read nor written.
+ *
+ *   grad_out [N,D] of type `dtype`; grad_table [V,D] of type `grad_dtype`: the same, or fp32 for
+ *   bf16 grad_out; strides as above
+ *   workspace  gls_embed_tokens_backward_workspace_bytes(N, V, D) bytes, 16-byte aligned; its
+ *              contents on entry are ignored (may be NULL when N = 0)
+ * N < 2^30.
+ */
+#define GLS_EMBED_ACCUMULATE 1u
+size_t gls_embed_tokens_backward_workspace_bytes(int64_t N, int64_t V, int64_t D);
+int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_stride, const int32_t* tokens,
+                              int64_t N, int64_t V, int64_t D, float scale, void* grad_table, int grad_dtype,
+                              int64_t grad_table_stride, uint32_t flags, void* workspace,
+                              size_t workspace_bytes, uint32_t* device_status, void* stream);
 
 #ifdef __cplusplus
 }

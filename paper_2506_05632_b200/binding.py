@@ -16,7 +16,9 @@ VERIFY_ALL_ROWS, VERIFY_ACTIVE_ROWS = 4, 8  # how the dense verify call walks Al
 VERIFY_FIRST_PHASE, VERIFY_REST = 16, 32   # the walk in phases as two calls (rows fetched on demand)
 VERIFY_THREE_PHASES = 64                   # positions 1 and 2 as a phase of their own
 NOISE_SHARED_ACROSS_K = 1
-DEV_EMPTY_SUPPORT = 1
+DEV_EMPTY_SUPPORT, DEV_BAD_TOKEN = 1, 2
+EMBED_ACCUMULATE = 1
+MAX_GIVEN = 64  # tokens per row of token_logprobs
 F32, BF16 = 0, 1
 
 _lock = threading.Lock()
@@ -141,6 +143,33 @@ def load():
             C.POINTER(_Rows), C.POINTER(_Rows), C.c_void_p, C.c_int64, C.c_int, C.c_int,
             C.c_int64, C.POINTER(_Noise), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
             C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.gls_token_logprobs_workspace_bytes.restype = C.c_size_t
+        L.gls_token_logprobs_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int64, C.c_int]
+        L.gls_token_logprobs.restype = C.c_int
+        L.gls_token_logprobs.argtypes = [
+            C.POINTER(_Rows), C.c_int, C.c_int, C.c_int, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
+            C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+            C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.gls_emitted_logprobs.restype = C.c_int
+        L.gls_emitted_logprobs.argtypes = [
+            C.POINTER(_Rows), C.c_int, C.c_int, C.c_int, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
+            C.c_uint32, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+            C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.gls_token_logprobs_backward.restype = C.c_int
+        L.gls_token_logprobs_backward.argtypes = [
+            C.POINTER(_Rows), C.c_int, C.c_int, C.c_int, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
+            C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+            C.c_void_p, C.c_void_p, C.POINTER(_Rows), C.c_void_p]
+        L.gls_embed_tokens.restype = C.c_int
+        L.gls_embed_tokens.argtypes = [
+            C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_float,
+            C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.gls_embed_tokens_backward_workspace_bytes.restype = C.c_size_t
+        L.gls_embed_tokens_backward_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int64]
+        L.gls_embed_tokens_backward.restype = C.c_int
+        L.gls_embed_tokens_backward.argtypes = [
+            C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_float,
+            C.c_void_p, C.c_int, C.c_int64, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
         _lib = L
         return _lib
 
@@ -594,3 +623,228 @@ def compress_gaussian(candidates, source, side_info, bins=None, s2_eta=0.5, s2_z
         _ptr(out.get("recon")), _ptr(out.get("sqerr")), workspace.data_ptr(), workspace.numel(),
         _ptr(status), _stream()))
     return out
+
+
+# ---- operators next to the sampler: log probabilities, embedding lookup, their gradients ----------
+def _vec(t, name, shape, dtype, dev):
+    """Pointer of a contiguous device tensor of this shape and type (None stays None)."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise GlsError("%s must be a contiguous %s device tensor of shape %s" % (name, dtype, tuple(shape)))
+    if t.device != dev:
+        raise GlsError("%s is on %s, the call's other tensors on %s" % (name, t.device, dev))
+    return t.data_ptr()
+
+
+def _space(workspace, need, dev):
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    if not workspace.is_cuda or workspace.device != dev or not workspace.is_contiguous():
+        raise GlsError("workspace must be a contiguous tensor on %s" % dev)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _temps(inv_temp_per_draft, K):
+    if inv_temp_per_draft is None:
+        return None, None
+    v = [float(x) for x in inv_temp_per_draft]
+    if len(v) != K:
+        raise GlsError("inv_temp_per_draft needs one value per draft")
+    a = (C.c_float * K)(*v)
+    return a, C.cast(a, C.c_void_p)
+
+
+def _given(tokens, lead, dev):
+    """(tokens pointer, G, trailing shape) of int32 tokens [*lead] or [*lead, G]."""
+    if tokens is None:
+        return None, 0, (0,)
+    tail = tuple(tokens.shape[len(lead):])
+    if tuple(tokens.shape[:len(lead)]) != tuple(lead) or len(tail) > 1:
+        raise GlsError("tokens must have shape %s or that with one more dimension" % (tuple(lead),))
+    G = tail[0] if tail else 1
+    return _vec(tokens, "tokens", tokens.shape, torch.int32, dev), G, tail
+
+
+def token_logprobs_workspace_bytes(B, K, J, V, top=0):
+    return int(load().gls_token_logprobs_workspace_bytes(int(B), int(K), int(J), int(V), int(top)))
+
+
+def _top(top):
+    if not 0 <= int(top) <= 256:
+        raise GlsError("top must be between 0 and 256")
+    return int(top)
+
+
+def _score_out(out, lead, tail, M, want_entropy, dev):
+    f = dict(dtype=torch.float32, device=dev)
+    if out is None:
+        out = dict(logprobs=torch.empty(tuple(lead) + tail, **f), lse=torch.empty(lead, **f))
+        if want_entropy:
+            out["entropy"] = torch.empty(lead, **f)
+        if M:
+            out["top_ids"] = torch.empty(tuple(lead) + (M,), dtype=torch.int32, device=dev)
+            out["top_logprobs"] = torch.empty(tuple(lead) + (M,), **f)
+    p = [_vec(out["logprobs"], "out['logprobs']", tuple(lead) + tail, torch.float32, dev),
+         _vec(out["lse"], "out['lse']", lead, torch.float32, dev),
+         _vec(out.get("lse_tail"), "out['lse_tail']", lead, torch.float32, dev),
+         _vec(out.get("entropy"), "out['entropy']", lead, torch.float32, dev),
+         _vec(out["top_ids"], "out['top_ids']", tuple(lead) + (M,), torch.int32, dev) if M else None,
+         _vec(out["top_logprobs"], "out['top_logprobs']", tuple(lead) + (M,), torch.float32, dev)
+         if M else None]
+    return out, p
+
+
+def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=None, want_entropy=True,
+                       workspace=None, status=None, out=None):
+    """gls_token_logprobs: logits [B,K,J,V], tokens int32 [B,K,J] or [B,K,J,G] (None: no tokens).
+
+    Returns dict(logprobs, lse [B,K,J], entropy [B,K,J], top_ids and top_logprobs [B,K,J,top]); entropy
+    only if wanted, the alternatives only for top > 0.  Given `out`, its tensors are written (an
+    'lse_tail' among them too).  No autograd: see token_logprobs."""
+    L = load()
+    B, K, J, V = logits.shape
+    dev, M = logits.device, _top(top)
+    rows = _rows(logits, 3)
+    tp, G, tail = _given(tokens, (B, K, J), dev)
+    out, p = _score_out(out, (B, K, J), tail, M, want_entropy, dev)
+    ws, nbytes = _space(workspace, token_logprobs_workspace_bytes(B, K, J, V, M), dev)
+    keep, itk = _temps(inv_temp_per_draft, K)
+    with torch.cuda.device(dev):
+        _check(L.gls_token_logprobs(C.byref(rows), B, K, J, V, float(inv_temp), itk, tp, G, M, *p,
+                                    ws.data_ptr(), nbytes, _vec(status, "status", (1,), torch.int32, dev),
+                                    _stream()))
+    return out
+
+
+def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0, want_entropy=True,
+                     workspace=None, status=None, out=None):
+    """gls_emitted_logprobs: the target rows [B,K,J,V] of a verification with the tokens [B,J] and
+    accept flags [B,K,L] it returned -> token_logprobs' dict over [B,J], zeros (alternatives -1) at and
+    beyond tau."""
+    L_ = load()
+    B, K, J, V = target_logits.shape
+    L = J if (flags & NO_BONUS) else J - 1
+    dev, M = target_logits.device, _top(top)
+    rows = _rows(target_logits, 3)
+    tp = _vec(tokens, "tokens", (B, J), torch.int32, dev)
+    ap = _vec(accept, "accept", (B, K, L), torch.uint8, dev) if L > 0 else None
+    out, p = _score_out(out, (B, J), (), M, want_entropy, dev)
+    ws, nbytes = _space(workspace, token_logprobs_workspace_bytes(B, K, J, V, M), dev)
+    with torch.cuda.device(dev):
+        _check(L_.gls_emitted_logprobs(C.byref(rows), B, K, L, V, float(inv_temp), tp, ap, int(flags), M,
+                                       p[0], p[1], *p[3:], ws.data_ptr(), nbytes,
+                                       _vec(status, "status", (1,), torch.int32, dev), _stream()))
+    return out
+
+
+def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, top_ids=None,
+                            grad_logprobs=None, grad_lse=None, grad_entropy=None,
+                            grad_top_logprobs=None, inv_temp=1.0, inv_temp_per_draft=None,
+                            grad_logits=None):
+    """gls_token_logprobs_backward: the gradient with respect to the logits, [B,K,J,V] in their type,
+    from token_logprobs' inputs and outputs and the gradients of its outputs (each may be None)."""
+    L = load()
+    B, K, J, V = logits.shape
+    dev = logits.device
+    lead = (B, K, J)
+    rows = _rows(logits, 3)
+    tp, G, tail = _given(tokens, lead, dev)
+    M = 0 if top_ids is None else top_ids.shape[-1]
+    if grad_entropy is not None and entropy is None:
+        raise GlsError("grad_entropy needs the forward call's entropy")
+    if grad_top_logprobs is not None and top_ids is None:
+        raise GlsError("grad_top_logprobs needs the forward call's top_ids")
+    if grad_logprobs is not None and tokens is None:
+        raise GlsError("grad_logprobs needs the tokens")
+    if grad_logits is None:
+        grad_logits = torch.empty(lead + (V,), dtype=logits.dtype, device=dev)
+    if tuple(grad_logits.shape) != lead + (V,) or grad_logits.dtype != logits.dtype or grad_logits.device != dev:
+        raise GlsError("grad_logits must have the logits' shape, type and device")
+    grows = _rows(grad_logits, 3)
+    f = torch.float32
+    keep, itk = _temps(inv_temp_per_draft, K)
+    args = [tp, G, _vec(top_ids, "top_ids", lead + (M,), torch.int32, dev), M, _vec(lse, "lse", lead, f, dev),
+            _vec(lse_tail, "lse_tail", lead, f, dev), _vec(entropy, "entropy", lead, f, dev),
+            _vec(grad_logprobs, "grad_logprobs", lead + tail, f, dev),
+            _vec(grad_lse, "grad_lse", lead, f, dev), _vec(grad_entropy, "grad_entropy", lead, f, dev),
+            _vec(grad_top_logprobs, "grad_top_logprobs", lead + (M,), f, dev)]
+    with torch.cuda.device(dev):
+        _check(L.gls_token_logprobs_backward(C.byref(rows), B, K, J, V, float(inv_temp), itk, *args,
+                                             C.byref(grows), _stream()))
+    return grad_logits
+
+
+def _matrix(t, name):
+    """(dtype code, row stride) of a 2-d device tensor with contiguous rows."""
+    if not t.is_cuda:
+        raise GlsError("libgls takes device tensors; there is no CPU path")
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise GlsError("%s must be float32 or bfloat16" % name)
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise GlsError("%s must be a matrix with contiguous rows" % name)
+    return F32 if t.dtype == torch.float32 else BF16, t.stride(0)
+
+
+def embed_tokens_raw(table, tokens, scale=1.0, status=None, out=None):
+    """gls_embed_tokens: scale * table[tokens] for table [V,D] and int32 tokens of any shape ->
+    [*tokens.shape, D]; a token below 0 gives zeros.  No autograd: see embed_tokens."""
+    L = load()
+    dt, stride = _matrix(table, "table")
+    V, D = table.shape
+    dev = table.device
+    tp = _vec(tokens, "tokens", tokens.shape, torch.int32, dev)
+    N = tokens.numel()
+    if out is None:
+        out = torch.empty(tuple(tokens.shape) + (D,), dtype=table.dtype, device=dev)
+    if tuple(out.shape) != tuple(tokens.shape) + (D,) or out.dtype != table.dtype or out.device != dev:
+        raise GlsError("out must have shape [*tokens.shape, D], the table's type and its device")
+    try:
+        flat = out.view(N, D)  # rows a constant stride apart
+    except RuntimeError:
+        raise GlsError("out's rows must be a constant stride apart") from None
+    _, ostride = _matrix(flat, "out")
+    with torch.cuda.device(dev):
+        _check(L.gls_embed_tokens(table.data_ptr(), dt, stride, V, D, tp, N, float(scale), out.data_ptr(),
+                                  ostride, _vec(status, "status", (1,), torch.int32, dev), _stream()))
+    return out
+
+
+def embed_tokens_backward_workspace_bytes(N, V, D):
+    return int(load().gls_embed_tokens_backward_workspace_bytes(int(N), int(V), int(D)))
+
+
+def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accumulate=False,
+                          workspace=None, status=None):
+    """gls_embed_tokens_backward: grad_out [*tokens.shape, D] -> the gradient of the table, [V,D] in
+    grad_out's type unless grad_table (the same type, or float32) is given.  accumulate: added to
+    grad_table, whose other rows are not touched."""
+    L = load()
+    if not grad_out.is_cuda:
+        raise GlsError("libgls takes device tensors; there is no CPU path")
+    N, D = tokens.numel(), grad_out.shape[-1]
+    dev = grad_out.device
+    if tuple(grad_out.shape) != tuple(tokens.shape) + (D,):
+        raise GlsError("grad_out must have shape [*tokens.shape, D]")
+    tp = _vec(tokens, "tokens", tokens.shape, torch.int32, dev)
+    try:
+        flat = grad_out.view(N, D)
+    except RuntimeError:
+        flat = grad_out.reshape(N, D)
+    if N and D > 1 and flat.stride(1) != 1 or N > 1 and flat.stride(0) < D:
+        flat = flat.contiguous()  # an expanded gradient
+    dt, stride = _matrix(flat, "grad_out")
+    if grad_table is None:
+        if accumulate:
+            raise GlsError("accumulate needs a grad_table to add to")
+        grad_table = torch.empty((int(V), D), dtype=grad_out.dtype, device=dev)
+    if tuple(grad_table.shape) != (int(V), D) or grad_table.device != dev:
+        raise GlsError("grad_table must have shape [V, D] and be on grad_out's device")
+    gdt, gstride = _matrix(grad_table, "grad_table")
+    ws, nbytes = _space(workspace, embed_tokens_backward_workspace_bytes(N, V, D), dev)
+    with torch.cuda.device(dev):
+        _check(L.gls_embed_tokens_backward(flat.data_ptr(), dt, stride, tp, N, int(V), D, float(scale),
+                                           grad_table.data_ptr(), gdt, gstride,
+                                           EMBED_ACCUMULATE if accumulate else 0, ws.data_ptr(), nbytes,
+                                           _vec(status, "status", (1,), torch.int32, dev), _stream()))
+    return grad_table

@@ -21,6 +21,8 @@
 
 namespace gls {
 
+int token_ops_bounds(uint32_t out[4]);  // gls_token_ops.cu
+
 // Number of SMs of the current device (grids and slice plans are sized from it); looked up once
 // per device.  148 on B200; that value is also the answer when no device can be queried, so that
 // gls_workspace_bytes() stays callable without one.
@@ -1179,12 +1181,16 @@ using namespace gls;
 
 extern "C" {
 
-int gls_version(void) { return 200; }
+int gls_version(void) { return 210; }
 
 int gls_debug_bounds(uint32_t out_host[4]) {
 #ifdef GLS_DEBUG_BOUNDS
   if (!out_host) return 1;
   if (cudaMemcpyFromSymbol(out_host, g_bounds_fault, 4 * sizeof(uint32_t)) != cudaSuccess) return -1;
+  uint32_t more[4];
+  if (token_ops_bounds(more) != 1) return -1;
+  if (out_host[0] == 0u) std::memcpy(out_host, more, sizeof(more));
+  else out_host[0] += more[0];
   return 1;
 #else
   if (out_host) out_host[0] = out_host[1] = out_host[2] = out_host[3] = 0u;

@@ -1,0 +1,474 @@
+// gls_token_ops.cu -- C ABI of the operators next to the sampler (see include/gls.h): log
+// probabilities of tokens with entropy and alternatives and their gradient, the embedding lookup
+// and its gradient.
+#include <atomic>
+#include <cmath>
+#include <cstring>
+
+#include "../../include/gls.h"
+#include "gls_embed.cuh"
+
+namespace gls {
+
+static_assert(kDevBadToken == GLS_DEV_BAD_TOKEN && kScoreMaxG == GLS_MAX_GIVEN && kMaxK == GLS_MAX_K, "header");
+
+// SMs of the current device, looked up once per device; 148 (B200) when none can be queried
+static int sm_count() {
+  constexpr int kMaxDev = 64;
+  static std::atomic<int> cache[kMaxDev];
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDev) {
+    (void)cudaGetLastError();
+    return 148;
+  }
+  n = cache[dev].load(std::memory_order_relaxed);
+  if (n > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) {
+    (void)cudaGetLastError();
+    return 148;
+  }
+  cache[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+static bool score_sizes_ok(int B, int K, int J, int64_t V) {
+  return B > 0 && K > 0 && K <= GLS_MAX_K && J > 0 && V > 0 && V < (1LL << 31) - 65536 &&
+         (long long)B * K * J < (1LL << 31) / 64;
+}
+static int rows_ok(const gls_rows_t* r) {
+  if (!r || !r->data) return GLS_ERR_INVALID_ARG;
+  if (r->dtype != GLS_F32 && r->dtype != GLS_BF16) return GLS_ERR_UNSUPPORTED;
+  if (((uintptr_t)r->data) % (r->dtype == GLS_F32 ? 4 : 2)) return GLS_ERR_MISALIGNED;
+  return GLS_OK;
+}
+// Temperatures are held to a range in which a difference of logits scaled by one neither vanishes
+// nor overflows before its exponential does.
+static int temps_ok(float inv_temp, const float* per_draft, int K, float* out) {
+  for (int k = 0; k < K; ++k) {
+    const float it = per_draft ? per_draft[k] : inv_temp;
+    if (!std::isfinite(it) || it <= 0.f) return GLS_ERR_INVALID_ARG;
+    if (it < 1e-20f || it > 1e20f) return GLS_ERR_UNSUPPORTED;
+    out[k] = it;
+  }
+  return GLS_OK;
+}
+
+struct ScorePlan {
+  int splits, steps;
+  size_t off_cand, total;
+};
+// Slices per row: the fewest for which the last round of warps wastes at most 15 % of the machine, or
+// that give every resident warp 12 items; slices of four steps and more unless the rows are so few
+// that one step each still leaves warps idle.  `rows` is the number of rows expected to be read.
+static ScorePlan score_plan(long long rows, long long alloc_rows, long long V, int dtype, int M) {
+  ScorePlan p;
+  const int step = dtype == GLS_BF16 ? ScoreCfg<kBF16>::kStep : ScoreCfg<kF32>::kStep;
+  const long long steps = (V + 15 + step - 1) / step;  // a row may start up to 15 elements past a boundary
+  const long long grid = (long long)sm_count() * kScoreCtasPerSM;
+  long long most = (steps + 3) / 4;
+  if (rows * most < 2 * grid) most = steps;
+  if (M > 0 && most > kScoreMaxCand / M) most = kScoreMaxCand / M;
+  long long splits = 1;
+  for (; splits < most; ++splits) {
+    const long long items = rows * splits;
+    if (items >= 12 * grid) break;
+    const long long rounds = (items + grid - 1) / grid;
+    if (items >= grid && (double)(rounds * grid - items) <= 0.15 * (double)(rounds * grid)) break;
+  }
+  p.steps = (int)((steps + splits - 1) / splits);
+  p.splits = (int)((steps + p.steps - 1) / p.steps);
+  p.off_cand = p.splits > 1 ? up256((size_t)alloc_rows * p.splits * sizeof(ScorePart)) : 0;
+  p.total = p.splits > 1 ? p.off_cand + up256((size_t)alloc_rows * p.splits * M * 8) : 0;
+  return p;
+}
+// Rows an emitted call reads: at least one per sequence and at most J; sequences stop early as a
+// rule, so the slices are cut for two each.
+static long long emitted_rows(int B, int J) { return (long long)B * (J < 2 ? J : 2); }
+
+template <int DT, bool ENT>
+static cudaError_t launch_score(const ScoreArgs& A, cudaStream_t st) {
+  const long long items = A.rows * A.splits;
+  const long long cap = (long long)sm_count() * kScoreCtasPerSM;
+  const size_t smem = A.M > 0 ? sizeof(TopmWarpBuf) : 0;
+  score_kernel<DT, ENT><<<(int)(items < cap ? items : cap), 32, smem, st>>>(A);
+  cudaError_t err = cudaGetLastError();
+  if (err != cudaSuccess || A.splits == 1) return err;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  const long long mcap = (long long)sm_count() * 8;
+  cfg.gridDim = dim3((unsigned)(A.rows < mcap ? A.rows : mcap));
+  cfg.blockDim = dim3(kScoreMergeThreads);
+  int p2 = 32;
+  while (p2 < A.splits * A.M) p2 <<= 1;
+  cfg.dynamicSmemBytes = A.M > 0 ? (size_t)p2 * 8 : 0;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, score_merge_kernel<DT>, A);
+}
+
+static int run_score(ScoreArgs& A, const gls_rows_t* rows, const ScorePlan& P, void* workspace,
+                     size_t workspace_bytes, cudaStream_t st) {
+  if (P.total > 0 && (!workspace || workspace_bytes < P.total)) return GLS_ERR_WORKSPACE;
+  if (P.total > 0 && (uintptr_t)workspace % 16) return GLS_ERR_MISALIGNED;
+  A.data = rows->data;
+  A.sb = rows->stride_b;
+  A.sk = rows->stride_k;
+  A.sj = rows->stride_j;
+  A.splits = P.splits;
+  A.steps_per_slice = P.steps;
+  A.parts = (ScorePart*)workspace;
+  A.cand = (unsigned long long*)((char*)workspace + P.off_cand);
+  const bool bf = rows->dtype == GLS_BF16, ent = A.out_ent != nullptr;
+  const cudaError_t err = bf ? (ent ? launch_score<kBF16, true>(A, st) : launch_score<kBF16, false>(A, st))
+                             : (ent ? launch_score<kF32, true>(A, st) : launch_score<kF32, false>(A, st));
+  return err == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
+
+}  // namespace gls
+
+using namespace gls;
+
+namespace gls {
+// the range-check record of this translation unit's kernels (gls_debug_bounds adds it to its own)
+int token_ops_bounds(uint32_t out[4]) {
+#ifdef GLS_DEBUG_BOUNDS
+  return cudaMemcpyFromSymbol(out, g_bounds_fault, 4 * sizeof(uint32_t)) == cudaSuccess ? 1 : -1;
+#else
+  out[0] = out[1] = out[2] = out[3] = 0u;
+  return 0;
+#endif
+}
+}  // namespace gls
+
+extern "C" {
+
+size_t gls_token_logprobs_workspace_bytes(int B, int K, int J, int64_t V, int M) {
+  if (!score_sizes_ok(B, K, J, V) || M < 0 || M > kScoreMaxM) return 0;
+  size_t need = 16;
+  for (int dt = 0; dt < 2; ++dt) {
+    const size_t t = score_plan((long long)B * K * J, (long long)B * K * J, V, dt, M).total;
+    const size_t e = score_plan(emitted_rows(B, J), (long long)B * J, V, dt, M).total;
+    if (t > need) need = t;
+    if (e > need) need = e;
+  }
+  return need;
+}
+
+int gls_token_logprobs(const gls_rows_t* logits, int B, int K, int J, int64_t V, float inv_temp,
+                       const float* inv_temp_per_draft_host, const int32_t* tokens, int G, int M,
+                       float* out_logprobs, float* out_lse, float* out_lse_tail, float* out_entropy,
+                       int32_t* out_top_ids, float* out_top_logprobs, void* workspace,
+                       size_t workspace_bytes, uint32_t* device_status, void* stream) {
+  if (!score_sizes_ok(B, K, J, V) || G < 0 || G > GLS_MAX_GIVEN || M < 0 || M > kScoreMaxM || !out_lse)
+    return GLS_ERR_INVALID_ARG;
+  if ((G > 0 && (!tokens || !out_logprobs)) || (M > 0 && (!out_top_ids || !out_top_logprobs)))
+    return GLS_ERR_INVALID_ARG;
+  int rc = rows_ok(logits);
+  if (rc != GLS_OK) return rc;
+  ScoreArgs A;
+  std::memset(&A, 0, sizeof(A));
+  rc = temps_ok(inv_temp, inv_temp_per_draft_host, K, A.inv_t);
+  if (rc != GLS_OK) return rc;
+  A.K = K;
+  A.J = J;
+  A.V = (int)V;
+  A.M = M;
+  A.G = G;
+  A.rows = (long long)B * K * J;
+  A.tokens = tokens;
+  A.out_lp = out_logprobs;
+  A.out_lse = out_lse;
+  A.out_tail = out_lse_tail;
+  A.out_ent = out_entropy;
+  A.top_ids = out_top_ids;
+  A.top_lp = out_top_logprobs;
+  A.status = device_status;
+  return run_score(A, logits, score_plan(A.rows, A.rows, V, logits->dtype, M), workspace, workspace_bytes,
+                   (cudaStream_t)stream);
+}
+
+int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, int64_t V, float inv_temp,
+                         const int32_t* tokens, const uint8_t* accept, uint32_t flags, int M,
+                         float* out_logprobs, float* out_lse, float* out_entropy, int32_t* out_top_ids,
+                         float* out_top_logprobs, void* workspace, size_t workspace_bytes,
+                         uint32_t* device_status, void* stream) {
+  if (flags & ~(GLS_NO_BONUS | GLS_COMBINE_ALL)) return GLS_ERR_INVALID_ARG;
+  if (L < 0 || L >= (1 << 30)) return GLS_ERR_INVALID_ARG;
+  const int J = L + ((flags & GLS_NO_BONUS) ? 0 : 1);
+  if (!score_sizes_ok(B, K, J, V) || M < 0 || M > kScoreMaxM || !tokens || !out_logprobs || !out_lse)
+    return GLS_ERR_INVALID_ARG;
+  if ((J > 1 && !accept) || (M > 0 && (!out_top_ids || !out_top_logprobs))) return GLS_ERR_INVALID_ARG;
+  int rc = rows_ok(target_logits);
+  if (rc != GLS_OK) return rc;
+  ScoreArgs A;
+  std::memset(&A, 0, sizeof(A));
+  rc = temps_ok(inv_temp, nullptr, K, A.inv_t);
+  if (rc != GLS_OK) return rc;
+  A.K = K;
+  A.J = J;
+  A.V = (int)V;
+  A.M = M;
+  A.G = 1;
+  A.emitted = 1;
+  A.L = L;
+  A.accept = accept;
+  A.rows = (long long)B * J;
+  A.tokens = tokens;
+  A.out_lp = out_logprobs;
+  A.out_lse = out_lse;
+  A.out_ent = out_entropy;
+  A.top_ids = out_top_ids;
+  A.top_lp = out_top_logprobs;
+  A.status = device_status;
+  return run_score(A, target_logits, score_plan(emitted_rows(B, J), A.rows, V, target_logits->dtype, M),
+                   workspace, workspace_bytes, (cudaStream_t)stream);
+}
+
+int gls_token_logprobs_backward(const gls_rows_t* logits, int B, int K, int J, int64_t V, float inv_temp,
+                                const float* inv_temp_per_draft_host, const int32_t* tokens, int G,
+                                const int32_t* top_ids, int M, const float* lse, const float* lse_tail,
+                                const float* entropy, const float* grad_logprobs, const float* grad_lse,
+                                const float* grad_entropy, const float* grad_top_logprobs,
+                                const gls_rows_t* grad_logits, void* stream) {
+  if (!score_sizes_ok(B, K, J, V) || G < 0 || G > GLS_MAX_GIVEN || M < 0 || M > kScoreMaxM || !lse)
+    return GLS_ERR_INVALID_ARG;
+  if ((grad_logprobs && G > 0 && !tokens) || (grad_top_logprobs && M > 0 && !top_ids) || (grad_entropy && !entropy))
+    return GLS_ERR_INVALID_ARG;
+  int rc = rows_ok(logits);
+  if (rc == GLS_OK) rc = rows_ok(grad_logits);
+  if (rc != GLS_OK) return rc;
+  if (logits->dtype != grad_logits->dtype) return GLS_ERR_UNSUPPORTED;
+  // every element of the gradient has a place of its own, and not that of a logit
+  if (grad_logits->data == logits->data || (B > 1 && grad_logits->stride_b == 0) ||
+      (K > 1 && grad_logits->stride_k == 0) || (J > 1 && grad_logits->stride_j == 0))
+    return GLS_ERR_INVALID_ARG;
+  ScoreGradArgs A;
+  std::memset(&A, 0, sizeof(A));
+  rc = temps_ok(inv_temp, inv_temp_per_draft_host, K, A.inv_t);
+  if (rc != GLS_OK) return rc;
+  A.data = logits->data;
+  A.sb = logits->stride_b;
+  A.sk = logits->stride_k;
+  A.sj = logits->stride_j;
+  A.grad = (void*)grad_logits->data;
+  A.gb = grad_logits->stride_b;
+  A.gk = grad_logits->stride_k;
+  A.gj = grad_logits->stride_j;
+  A.K = K;
+  A.J = J;
+  A.V = (int)V;
+  A.M = M;
+  A.G = G;
+  A.rows = (long long)B * K * J;
+  A.tokens = tokens;
+  A.top_ids = top_ids;
+  A.lse = lse;
+  A.tail = lse_tail;
+  A.ent = entropy;
+  A.g_lp = G > 0 ? grad_logprobs : nullptr;
+  A.g_lse = grad_lse;
+  A.g_ent = grad_entropy;
+  A.g_top = M > 0 ? grad_top_logprobs : nullptr;
+  const bool bf = logits->dtype == GLS_BF16;
+  const long long chunk = (long long)kGradThreads * kGradVecs * (bf ? 16 : 8);
+  A.chunks = (int)((V + 15 + chunk - 1) / chunk);
+  const long long items = A.rows * A.chunks;
+  const int grid = (int)(items < (1 << 20) ? items : (1 << 20));
+  cudaStream_t st = (cudaStream_t)stream;
+  if (bf && grad_entropy) score_grad_kernel<kBF16, true><<<grid, kGradThreads, 0, st>>>(A);
+  else if (bf) score_grad_kernel<kBF16, false><<<grid, kGradThreads, 0, st>>>(A);
+  else if (grad_entropy) score_grad_kernel<kF32, true><<<grid, kGradThreads, 0, st>>>(A);
+  else score_grad_kernel<kF32, false><<<grid, kGradThreads, 0, st>>>(A);
+  return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
+
+int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t V, int64_t D,
+                     const int32_t* tokens, int64_t N, float scale, void* out, int64_t out_stride,
+                     uint32_t* device_status, void* stream) {
+  if (V <= 0 || V >= (1LL << 31) || D <= 0 || D >= (1LL << 31) || N < 0 || N >= (1LL << 31) || !std::isfinite(scale))
+    return GLS_ERR_INVALID_ARG;
+  if (dtype != GLS_F32 && dtype != GLS_BF16) return GLS_ERR_UNSUPPORTED;
+  if (N == 0) return GLS_OK;
+  if (!table || !tokens || !out || (V > 1 && table_stride < D) || (N > 1 && out_stride < D)) return GLS_ERR_INVALID_ARG;
+  const int es = dtype == GLS_F32 ? 4 : 2;
+  if ((uintptr_t)table % es || (uintptr_t)out % es) return GLS_ERR_MISALIGNED;
+  EmbedArgs A;
+  A.table = (const char*)table;
+  A.table_stride = table_stride;
+  A.out = (char*)out;
+  A.out_stride = out_stride;
+  A.tokens = tokens;
+  A.N = N;
+  A.V = V;
+  A.D = D;
+  A.scale = scale;
+  A.status = device_status;
+  cudaStream_t st = (cudaStream_t)stream;
+  const bool vec = D * es % 16 == 0 && table_stride * es % 16 == 0 && out_stride * es % 16 == 0 &&
+                   (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0;
+  const long long units = vec ? N * (D * es / 16) : N * D;
+  const long long want = (units + kEmbedThreads - 1) / kEmbedThreads, cap = 1 << 20;
+  const int grid = (int)(want < cap ? want : cap);
+  if (vec) {
+    if (dtype == GLS_BF16) embed_vec_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, (int)(D * es / 16));
+    else embed_vec_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, (int)(D * es / 16));
+  } else {
+    if (dtype == GLS_BF16) embed_any_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A);
+    else embed_any_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A);
+  }
+  return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
+
+}  // extern "C"
+
+namespace gls {
+
+struct EmbedGradPlan {
+  int bits, passes, tiles, per_range, ranges;
+  size_t off_key[2], off_pos[2], off_cnt, off_touched, off_partial, total;
+  size_t zero_from, zero_bytes;  // what has to be zero at the start (counts of later passes, touched)
+};
+static bool embed_grad_sizes_ok(int64_t N, int64_t V, int64_t D) {
+  return N >= 0 && N < (1LL << 30) && V > 0 && V < (1LL << 31) - 1 && D > 0 && D < (1LL << 31);
+}
+static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
+  EmbedGradPlan p;
+  int bits = 1;
+  while (bits < 31 && (V >> bits) != 0) ++bits;  // keys 0 .. V
+  p.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
+  p.bits = (bits + p.passes - 1) / p.passes;
+  p.tiles = (int)((N + kSortTile - 1) / kSortTile);
+  if (p.tiles < 1) p.tiles = 1;
+  p.per_range = 8;
+  while (p.per_range < kEgMaxRange && N / p.per_range > 2048) p.per_range *= 2;
+  p.ranges = (int)((N + p.per_range - 1) / p.per_range);
+  size_t at = 0;
+  for (int i = 0; i < 2; ++i) {
+    p.off_key[i] = at;
+    at += up256((size_t)N * 4);
+    p.off_pos[i] = at;
+    at += up256((size_t)N * 4);
+  }
+  p.off_cnt = at;
+  const size_t first = (size_t)p.tiles * kSortBins * 4;
+  at += up256((size_t)p.passes * first);
+  p.off_touched = at;
+  at += up256((size_t)((V + 31) / 32) * 4);
+  p.zero_from = p.off_cnt + first;
+  p.zero_bytes = at - p.zero_from;
+  p.off_partial = at;
+  at += up256((size_t)p.ranges * 2 * (size_t)D * 4);
+  p.total = at;
+  return p;
+}
+
+template <int DT, int DTO, bool VEC>
+static cudaError_t launch_embed_grad(const EmbedGradArgs& A, int threads, cudaStream_t st) {
+  const long long n_sum = (long long)A.ranges * A.slabs;
+  embed_grad_kernel<DT, DTO, VEC><<<(unsigned)(n_sum + A.zero_ctas), threads, 0, st>>>(A);
+  cudaError_t err = cudaGetLastError();
+  if (err != cudaSuccess || A.ranges < 2) return err;
+  embed_join_kernel<DTO, VEC><<<(unsigned)n_sum, threads, 0, st>>>(A);
+  return cudaGetLastError();
+}
+
+}  // namespace gls
+
+extern "C" {
+
+size_t gls_embed_tokens_backward_workspace_bytes(int64_t N, int64_t V, int64_t D) {
+  return embed_grad_sizes_ok(N, V, D) ? embed_grad_plan(N, V, D).total : 0;
+}
+
+int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_stride, const int32_t* tokens,
+                              int64_t N, int64_t V, int64_t D, float scale, void* grad_table, int grad_dtype,
+                              int64_t grad_table_stride, uint32_t flags, void* workspace, size_t workspace_bytes,
+                              uint32_t* device_status, void* stream) {
+  if (!embed_grad_sizes_ok(N, V, D) || !std::isfinite(scale) || (flags & ~GLS_EMBED_ACCUMULATE) || !grad_table ||
+      (V > 1 && grad_table_stride < D))
+    return GLS_ERR_INVALID_ARG;
+  if ((dtype != GLS_F32 && dtype != GLS_BF16) || (grad_dtype != GLS_F32 && grad_dtype != GLS_BF16) ||
+      (dtype == GLS_F32 && grad_dtype == GLS_BF16))
+    return GLS_ERR_UNSUPPORTED;
+  const bool accumulate = (flags & GLS_EMBED_ACCUMULATE) != 0;
+  if (N > 0 && (!grad_out || !tokens || (N > 1 && grad_out_stride < D))) return GLS_ERR_INVALID_ARG;
+  const int es = dtype == GLS_F32 ? 4 : 2, eso = grad_dtype == GLS_F32 ? 4 : 2;
+  if ((uintptr_t)grad_out % es || (uintptr_t)grad_table % eso) return GLS_ERR_MISALIGNED;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (N == 0) {
+    if (accumulate) return GLS_OK;
+    return cudaMemset2DAsync(grad_table, (size_t)(V > 1 ? grad_table_stride : D) * eso, 0, (size_t)D * eso, (size_t)V, st) ==
+                   cudaSuccess
+               ? GLS_OK
+               : GLS_ERR_CUDA;
+  }
+  const EmbedGradPlan P = embed_grad_plan(N, V, D);
+  if (!workspace || workspace_bytes < P.total) return GLS_ERR_WORKSPACE;
+  if ((uintptr_t)workspace % 16) return GLS_ERR_MISALIGNED;
+  char* ws = (char*)workspace;
+  SortArgs S;
+  S.tokens = tokens;
+  S.N = (int)N;
+  S.V = (int)V;
+  S.bits = P.bits;
+  S.passes = P.passes;
+  S.tiles = P.tiles;
+  S.cnt = (uint32_t*)(ws + P.off_cnt);
+  S.touched = (uint32_t*)(ws + P.off_touched);
+  for (int i = 0; i < 2; ++i) {
+    S.key[i] = (int32_t*)(ws + P.off_key[i]);
+    S.pos[i] = (int32_t*)(ws + P.off_pos[i]);
+  }
+  S.status = device_status;
+  if (P.tiles == 1) {
+    const size_t smem = sizeof(uint16_t) * kSortWarps * kSortBins + (sizeof(int32_t) + sizeof(uint16_t)) * kSortTile;
+    embed_sort_small_kernel<<<1, kSortThreads, smem, st>>>(S);
+  } else {
+    if (cudaMemsetAsync(ws + P.zero_from, 0, P.zero_bytes, st) != cudaSuccess) return GLS_ERR_CUDA;
+    embed_sort_count_kernel<<<P.tiles, kSortThreads, 0, st>>>(S);
+    for (int pass = 0; pass < P.passes; ++pass) embed_sort_pass_kernel<<<P.tiles, kSortThreads, 0, st>>>(S, pass);
+  }
+  if (cudaGetLastError() != cudaSuccess) return GLS_ERR_CUDA;
+  EmbedGradArgs A;
+  A.g = (const char*)grad_out;
+  A.g_stride = grad_out_stride;
+  A.out = (char*)grad_table;
+  A.out_stride = grad_table_stride;
+  A.key = S.key[(P.passes - 1) & 1];
+  A.pos = S.pos[(P.passes - 1) & 1];
+  A.touched = S.touched;
+  A.partial = (float*)(ws + P.off_partial);
+  A.N = (int)N;
+  A.V = (int)V;
+  A.D = D;
+  A.per_range = P.per_range;
+  A.ranges = P.ranges;
+  A.accumulate = accumulate ? 1 : 0;
+  A.scale = scale;
+  const bool vec = D % kEgCols == 0 && grad_out_stride * es % 16 == 0 && grad_table_stride * eso % 16 == 0 &&
+                   (uintptr_t)grad_out % 16 == 0 && (uintptr_t)grad_table % 16 == 0;
+  const long long per_thread = (D + kEgCols - 1) / kEgCols;
+  const int threads = (int)(per_thread < 256 ? (per_thread + 31) / 32 * 32 : 256);
+  const long long slabs = (D + (long long)threads * kEgCols - 1) / ((long long)threads * kEgCols);
+  if (slabs * P.ranges > (1LL << 31) - (1LL << 24)) return GLS_ERR_UNSUPPORTED;
+  A.slabs = (int)slabs;
+  const long long rows_per_cta = 8;
+  long long zc = accumulate ? 0 : (V + rows_per_cta - 1) / rows_per_cta;
+  if (zc > (1 << 20)) zc = 1 << 20;
+  A.zero_ctas = (int)zc;
+  cudaError_t err;
+#define EMBED_GRAD(DT, DTO) \
+  err = vec ? launch_embed_grad<DT, DTO, true>(A, threads, st) : launch_embed_grad<DT, DTO, false>(A, threads, st)
+  if (dtype == GLS_F32) EMBED_GRAD(kF32, kF32);
+  else if (grad_dtype == GLS_F32) EMBED_GRAD(kBF16, kF32);
+  else EMBED_GRAD(kBF16, kBF16);
+#undef EMBED_GRAD
+  return err == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
+
+}  // extern "C"

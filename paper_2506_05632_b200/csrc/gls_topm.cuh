@@ -47,7 +47,7 @@ struct TopmWarpBuf {
 // order of arrival; returns the new count and the code of the M-th largest.  Requires n > M.
 // last_pass: 0 for fp32 logits; 2 for bf16 logits, whose codes differ in their upper 16 bits only
 // (the lower 16 are all zero or all one with the sign), so two of the four radix passes suffice.
-__device__ __noinline__ unsigned long long topm_prune(TopmWarpBuf* wb, int n, int M, int last_pass) {
+static __device__ __noinline__ unsigned long long topm_prune(TopmWarpBuf* wb, int n, int M, int last_pass) {
   const int lane = threadIdx.x & 31;
   const uint32_t lt = (1u << lane) - 1u;
   uint32_t prefix = 0u;
