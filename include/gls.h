@@ -464,18 +464,16 @@ int gls_compress_select(const gls_rows_t* enc_logw, const gls_rows_t* dec_logw, 
  *   out_entropy       NULL or fp32 [B,K,J]
  *   out_top_ids       int32 [B,K,J,M], -1 past the row's finite logits, and
  *   out_top_logprobs  fp32 [B,K,J,M], -inf there (may be NULL when M = 0)
- *   workspace         gls_token_logprobs_workspace_bytes(B, K, J, V, M) bytes, 16-byte aligned; its
- *                     contents on entry are ignored
+ * No workspace is needed.
  * A row without a finite logit: lse -inf, entropy 0, log probabilities -inf, no alternatives, and
  * GLS_DEV_EMPTY_SUPPORT.
  */
 #define GLS_MAX_GIVEN 64
-size_t gls_token_logprobs_workspace_bytes(int B, int K, int J, int64_t V, int M);
 int gls_token_logprobs(const gls_rows_t* logits, int B, int K, int J, int64_t V, float inv_temp,
                        const float* inv_temp_per_draft_host, const int32_t* tokens, int G, int M,
                        float* out_logprobs, float* out_lse, float* out_lse_tail, float* out_entropy,
-                       int32_t* out_top_ids, float* out_top_logprobs, void* workspace,
-                       size_t workspace_bytes, uint32_t* device_status, void* stream);
+                       int32_t* out_top_ids, float* out_top_logprobs, uint32_t* device_status,
+                       void* stream);
 
 /*
  * The same for the tokens that a verification emitted: position j of sequence b is scored on the
@@ -486,13 +484,11 @@ int gls_token_logprobs(const gls_rows_t* logits, int B, int K, int J, int64_t V,
  *   tokens, accept its out_tokens [B,J] and out_accept [B,K,L] (accept may be NULL when J = 1)
  *   flags          its GLS_NO_BONUS and GLS_COMBINE_ALL
  *   outputs        [B,J] (alternatives [B,J,M]); at and beyond tau: 0, alternatives -1 and 0
- *   workspace      as gls_token_logprobs
  */
 int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, int64_t V, float inv_temp,
                          const int32_t* tokens, const uint8_t* accept, uint32_t flags, int M,
                          float* out_logprobs, float* out_lse, float* out_entropy, int32_t* out_top_ids,
-                         float* out_top_logprobs, void* workspace, size_t workspace_bytes,
-                         uint32_t* device_status, void* stream);
+                         float* out_top_logprobs, uint32_t* device_status, void* stream);
 
 /*
  * Gradient of the outputs of gls_token_logprobs with respect to the logits.  With g the gradients

@@ -25,4 +25,4 @@ from .binding import (  # noqa: F401
     draft_sample_topm, draft_verify, draft_verify_workspace_bytes, lib_path, load,
     embed_tokens_backward, embed_tokens_backward_workspace_bytes, emitted_logprobs,
     static_scratch_bytes, status_string, target_sample_verify, target_sample_verify_sparse,
-    target_sample_verify_topm, token_logprobs_backward, token_logprobs_workspace_bytes, topm_workspace_bytes, verify_phases, verify_walk, version, workspace_bytes)
+    target_sample_verify_topm, token_logprobs_backward, topm_workspace_bytes, verify_phases, verify_walk, version, workspace_bytes)

@@ -60,7 +60,7 @@ class _TokenLogprobs(torch.autograd.Function):
 
 
 def token_logprobs(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=None, want_entropy=True,
-                   workspace=None, status=None, out=None):
+                   status=None, out=None):
     """Log probabilities of the tokens (int32 [B,K,J] or [B,K,J,G], -1: none) under the rows of logits
     [B,K,J,V], with the rows' log-sum-exp, entropy and `top` most likely tokens.
 
@@ -68,7 +68,7 @@ def token_logprobs(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=None,
     alternatives only for top > 0; see gls_token_logprobs in include/gls.h.  Differentiable in the
     logits (once; not during a graph capture, and not into given outputs)."""
     kw = dict(inv_temp=inv_temp, inv_temp_per_draft=inv_temp_per_draft, want_entropy=want_entropy,
-              workspace=workspace, status=status)
+              status=status)
     if not (logits.requires_grad and torch.is_grad_enabled()):
         return binding.token_logprobs_raw(logits, tokens, top=top, out=out, **kw)
     if out is not None:

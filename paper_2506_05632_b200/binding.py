@@ -143,18 +143,16 @@ def load():
             C.POINTER(_Rows), C.POINTER(_Rows), C.c_void_p, C.c_int64, C.c_int, C.c_int,
             C.c_int64, C.POINTER(_Noise), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
             C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
-        L.gls_token_logprobs_workspace_bytes.restype = C.c_size_t
-        L.gls_token_logprobs_workspace_bytes.argtypes = [C.c_int, C.c_int, C.c_int, C.c_int64, C.c_int]
         L.gls_token_logprobs.restype = C.c_int
         L.gls_token_logprobs.argtypes = [
             C.POINTER(_Rows), C.c_int, C.c_int, C.c_int, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
             C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-            C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+            C.c_void_p, C.c_void_p]
         L.gls_emitted_logprobs.restype = C.c_int
         L.gls_emitted_logprobs.argtypes = [
             C.POINTER(_Rows), C.c_int, C.c_int, C.c_int, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
             C.c_uint32, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-            C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+            C.c_void_p, C.c_void_p]
         L.gls_token_logprobs_backward.restype = C.c_int
         L.gls_token_logprobs_backward.argtypes = [
             C.POINTER(_Rows), C.c_int, C.c_int, C.c_int, C.c_int64, C.c_float, C.c_void_p, C.c_void_p,
@@ -666,10 +664,6 @@ def _given(tokens, lead, dev):
     return _vec(tokens, "tokens", tokens.shape, torch.int32, dev), G, tail
 
 
-def token_logprobs_workspace_bytes(B, K, J, V, top=0):
-    return int(load().gls_token_logprobs_workspace_bytes(int(B), int(K), int(J), int(V), int(top)))
-
-
 def _top(top):
     if not 0 <= int(top) <= 256:
         raise GlsError("top must be between 0 and 256")
@@ -696,7 +690,7 @@ def _score_out(out, lead, tail, M, want_entropy, dev):
 
 
 def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=None, want_entropy=True,
-                       workspace=None, status=None, out=None):
+                       status=None, out=None):
     """gls_token_logprobs: logits [B,K,J,V], tokens int32 [B,K,J] or [B,K,J,G] (None: no tokens).
 
     Returns dict(logprobs, lse [B,K,J], entropy [B,K,J], top_ids and top_logprobs [B,K,J,top]); entropy
@@ -708,17 +702,15 @@ def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=N
     rows = _rows(logits, 3)
     tp, G, tail = _given(tokens, (B, K, J), dev)
     out, p = _score_out(out, (B, K, J), tail, M, want_entropy, dev)
-    ws, nbytes = _space(workspace, token_logprobs_workspace_bytes(B, K, J, V, M), dev)
     keep, itk = _temps(inv_temp_per_draft, K)
     with torch.cuda.device(dev):
         _check(L.gls_token_logprobs(C.byref(rows), B, K, J, V, float(inv_temp), itk, tp, G, M, *p,
-                                    ws.data_ptr(), nbytes, _vec(status, "status", (1,), torch.int32, dev),
-                                    _stream()))
+                                    _vec(status, "status", (1,), torch.int32, dev), _stream()))
     return out
 
 
 def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0, want_entropy=True,
-                     workspace=None, status=None, out=None):
+                     status=None, out=None):
     """gls_emitted_logprobs: the target rows [B,K,J,V] of a verification with the tokens [B,J] and
     accept flags [B,K,L] it returned -> token_logprobs' dict over [B,J], zeros (alternatives -1) at and
     beyond tau."""
@@ -730,11 +722,9 @@ def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0
     tp = _vec(tokens, "tokens", (B, J), torch.int32, dev)
     ap = _vec(accept, "accept", (B, K, L), torch.uint8, dev) if L > 0 else None
     out, p = _score_out(out, (B, J), (), M, want_entropy, dev)
-    ws, nbytes = _space(workspace, token_logprobs_workspace_bytes(B, K, J, V, M), dev)
     with torch.cuda.device(dev):
         _check(L_.gls_emitted_logprobs(C.byref(rows), B, K, L, V, float(inv_temp), tp, ap, int(flags), M,
-                                       p[0], p[1], *p[3:], ws.data_ptr(), nbytes,
-                                       _vec(status, "status", (1,), torch.int32, dev), _stream()))
+                                       p[0], p[1], *p[3:], _vec(status, "status", (1,), torch.int32, dev), _stream()))
     return out
 
 

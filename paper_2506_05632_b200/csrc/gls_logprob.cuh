@@ -8,22 +8,16 @@
 // for any reference x_m, so one pass over the row yields all of it, and the M largest logits of
 // the same pass (descending, ties to the lower index) are the alternatives.
 #pragma once
-#include "gls_topm.cuh"
+#include <cstddef>
+#include <type_traits>
+
+#include "gls_group16.cuh"
 
 namespace gls {
 
-constexpr int kScoreMaxM = kTopmMaxM;    // alternatives per row
+constexpr int kScoreMaxM = 256;          // alternatives per row
 constexpr int kScoreMaxG = 64;           // given tokens per row
-constexpr int kScoreMaxCand = 4096;      // candidates of all slices of a row that the merge sorts
-constexpr int kScoreCtasPerSM = 16;      // one warp each
 constexpr uint32_t kDevBadToken = 2u;    // GLS_DEV_BAD_TOKEN
-
-// Softmax statistics of one slice of a row: sums relative to the reference logit m.
-// s == 0: the slice has no finite logit.
-struct __align__(16) ScorePart {
-  float m, s, u;
-  int n;  // candidates the slice left
-};
 
 struct ScoreArgs {
   const void* data;       // rows [B][K][J][V]
@@ -33,7 +27,6 @@ struct ScoreArgs {
   int L;
   const uint8_t* accept;  // [B][K][L]
   long long rows;         // B * K * J, or B * J for emitted rows
-  int splits, steps_per_slice;
   const int32_t* tokens;  // [rows][G]
   float inv_t[kMaxK];
   float* out_lp;          // [rows][G]
@@ -42,8 +35,6 @@ struct ScoreArgs {
   float* out_ent;         // NULL or [rows]
   int32_t* top_ids;       // [rows][M]
   float* top_lp;          // [rows][M]
-  ScorePart* parts;       // [rows][splits]
-  unsigned long long* cand;  // [rows][splits][M]: (ordered code << 32) | ~index
   uint32_t* status;
 };
 
@@ -59,9 +50,10 @@ __device__ __forceinline__ ScoreRow score_locate(const ScoreArgs& A, long long r
   const int lane = threadIdx.x & 31;
   int k;
   long long b;
-  const int j = (int)(row % A.J);
+  const uint32_t bk = (uint32_t)row / (uint32_t)A.J;  // rows number fewer than 2^25
+  const int j = (int)((uint32_t)row - bk * (uint32_t)A.J);
   if (A.emitted) {
-    b = row / A.J;
+    b = bk;
     k = 0;
     r.live = __ldg(A.tokens + row) >= 0;
     if (r.live && j > 0) {  // lowest draft whose position j - 1 was accepted
@@ -71,9 +63,8 @@ __device__ __forceinline__ ScoreRow score_locate(const ScoreArgs& A, long long r
       k = lo != 0u ? __ffs(lo) - 1 : hi != 0u ? 31 + __ffs(hi) : 0;
     }
   } else {
-    const long long bk = row / A.J;
-    k = (int)(bk % A.K);
-    b = bk / A.K;
+    b = bk / (uint32_t)A.K;
+    k = (int)(bk - (uint32_t)b * (uint32_t)A.K);
     r.live = true;
   }
   r.inv_t = A.inv_t[k];
@@ -81,91 +72,431 @@ __device__ __forceinline__ ScoreRow score_locate(const ScoreArgs& A, long long r
   return r;
 }
 
+// A row is read in groups of 16 tokens counted from the 32-byte boundary at or below its start, so
+// that a row that starts anywhere is read by aligned 32-byte loads.  `mis`: elements between that
+// boundary and the row's start; `end`: mis + V.  Virtual index v is token v - mis.
 template <int DT>
 struct ScoreCfg {  // one step of a warp: 4 KB of the row
   static constexpr int kGroups = DT == kBF16 ? 4 : 2;  // groups of 16 tokens per lane
   static constexpr int kStep = 512 * kGroups;
 };
 
-__device__ __forceinline__ unsigned long long score_code(uint32_t key, int idx) {
-  return ((unsigned long long)key << 32) | (uint32_t)~idx;
-}
-
-// The largest float below x (x finite).
-__device__ __forceinline__ float just_below(float x) {
-  const uint32_t b = __float_as_uint(x);
-  if (x == 0.f) return __uint_as_float(0x80000001u);
-  return __uint_as_float(x > 0.f ? b - 1u : b + 1u);
-}
-
-// Examines queued groups (indices of 16-token groups counted from the 32-byte boundary at or below
-// the row's start, `mis` elements before it): appends their tokens above thr to the buffer in index
-// order and prunes it past M + 64 entries.  Returns (threshold bits << 32) | new count.
+// A group that sticks out of the row at either end, element by element.  What is outside becomes
+// the lowest finite value: its exponential is exactly 0 and its product with a difference too.
 template <int DT>
-__device__ __noinline__ unsigned long long score_expand(TopmWarpBuf* wb, const int* queue, const char* rowp,
-                                                        int mis, int V, int first, int nb, int n, int M,
-                                                        float thr) {
-  const int lane = threadIdx.x & 31;
-  float a[16];
-  uint32_t m = 0u;
-  int tok = 0;
-  if (lane < nb) {
-    tok = (queue[first + lane] << 4) - mis;
-#pragma unroll
-    for (int t = 0; t < 16; ++t)
-      a[t] = tok + t >= 0 && tok + t < V ? load_logit<DT>(rowp, tok + t) : -CUDART_INF_F;
-#pragma unroll
-    for (int t = 0; t < 16; ++t)
-      if (a[t] > thr && a[t] < CUDART_INF_F) m |= 1u << t;  // false for NaN
-  }
-  const int cnt = __popc(m);
-  int incl = cnt;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int o = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += o;
-  }
-  int pos = n + incl - cnt;
-#pragma unroll
-  for (int t = 0; t < 16; ++t) {
-    if ((m >> t) & 1u) {
-      if (GLS_IN_RANGE(pos, 0, kTopmCap, 60u)) {
-        wb->key[pos] = enc_ordered(a[t] + 0.0f);  // -0 and +0 are the same logit: one code
-        wb->idx[pos] = tok + t;
-      }
-      ++pos;
+__device__ __noinline__ void score_edge(Group16<DT>* g, const char* rowp, int v, int mis, int end) {
+  if constexpr (DT == kBF16) {
+#pragma unroll 1
+    for (int t = 0; t < 8; ++t) {
+      const int a = v + 2 * t;
+      const uint32_t lo = a >= mis && a < end ? (uint32_t)__ldg((const unsigned short*)rowp + (a - mis)) : 0xff7fu;
+      const uint32_t hi = a + 1 >= mis && a + 1 < end ? (uint32_t)__ldg((const unsigned short*)rowp + (a + 1 - mis)) : 0xff7fu;
+      g->a.w[t] = lo | (hi << 16);
+    }
+  } else {
+    uint32_t* const w = (uint32_t*)g;
+#pragma unroll 1
+    for (int t = 0; t < 16; ++t) {
+      const int a = v + t;
+      w[t] = a >= mis && a < end ? __float_as_uint(__ldg((const float*)rowp + (a - mis))) : 0xff7fffffu;
     }
   }
-  n += __shfl_sync(0xffffffffu, incl, 31);
-  __syncwarp();
-  if (n > M + 64) {
-    const unsigned long long r = topm_prune(wb, n, M, DT == kBF16 ? 2 : 0);
-    n = (int)(unsigned)r;
-    thr = dec_ordered((uint32_t)(r >> 32));
+}
+template <int DT>
+__device__ __forceinline__ void score_load(Group16<DT> (&g)[ScoreCfg<DT>::kGroups], const char* rowp, int mis, int end,
+                                           int step) {
+  constexpr int ES = DT == kBF16 ? 2 : 4;
+  constexpr int kStep = ScoreCfg<DT>::kStep;
+  const int s0 = step * kStep;
+  const int v0 = s0 + (threadIdx.x & 31) * 16;
+  const char* const p = rowp + ((long long)v0 - mis) * ES;
+  if (s0 >= mis && s0 + kStep <= end) {
+#pragma unroll
+    for (int q = 0; q < ScoreCfg<DT>::kGroups; ++q) load16_vec(g[q], p + q * 512 * ES);
+  } else {
+#pragma unroll
+    for (int q = 0; q < ScoreCfg<DT>::kGroups; ++q) {
+      const int v = v0 + q * 512;
+      if (v >= mis && v + 16 <= end) {
+        load16_vec(g[q], p + q * 512 * ES);
+      } else {
+        Group16<DT> e;
+        score_edge<DT>(&e, rowp, v, mis, end);
+        g[q] = e;
+      }
+    }
   }
-  return ((unsigned long long)__float_as_uint(thr) << 32) | (unsigned)n;
 }
 
-// Statistics of tokens [t0, t1) of a row with every element checked, two passes, sums in 64 bits:
-// for slices on which the sweep's arithmetic does not hold (NaN or +inf logits, logits beyond 1e30
-// in size, no finite logit at all).  Warp-collective; every lane returns the result.
+// Softmax statistics relative to the reference logit m; s == 0: no finite logit.
+struct ScoreSums {
+  float m, s, u;
+};
+
+// Adds one step of a lane's groups to its sums.  The reference moves only when the step's maximum
+// mx exceeds it by 2^8, so that terms stay within fp32 and the two parts of the entropy small.  A
+// step's terms are added up by themselves first: a lane's chain of additions is 32 + V / (32 step)
+// long.  The difference to the reference is taken before the scale: it is exact, or rounded at
+// 2^-24 of itself, so an exponent is good to 1e-7 of its own size however large the logits are.
+// -inf and NaN make the step's sums NaN (a masked vocabulary tail is common, a masked step in the
+// middle is not); such a step is taken again with both set to the lowest finite value, whose terms
+// are exactly 0.  +inf makes the sums infinite, which the caller finds at the end.
+template <int DT, bool ENT, bool CLAMP>
+__device__ __forceinline__ void score_terms(const Group16<DT> (&g)[ScoreCfg<DT>::kGroups], float lm, float c2,
+                                            float& s, float& u) {
+  const unsigned long long c22 = pack_f32x2(c2, c2), nlm2 = pack_f32x2(-lm, -lm);
+  constexpr int NG = ScoreCfg<DT>::kGroups;
+  unsigned long long s2[NG], u2[NG];  // a chain of additions per group: they overlap
+#pragma unroll
+  for (int q = 0; q < NG; ++q) {
+    s2[q] = u2[q] = 0ull;
+    Group16<DT> h = g[q];
+    if (CLAMP) {
+      if constexpr (DT == kBF16) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) h.a.w[t] = max_bf16x2(h.a.w[t], 0xff7fff7fu);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          h.a.w[t] = __float_as_uint(fmaxf(__uint_as_float(h.a.w[t]), -3.402823466e38f));
+          h.b.w[t] = __float_as_uint(fmaxf(__uint_as_float(h.b.w[t]), -3.402823466e38f));
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 16; t += 2) {
+      const unsigned long long d2 = group16_diff2(h, t, -lm, nlm2);
+      float e0, e1;
+      unpack_f32x2(mul_f32x2(d2, c22), e0, e1);
+      const unsigned long long e2 = pack_f32x2(ex2_approx(e0), ex2_approx(e1));
+      s2[q] = add_f32x2(s2[q], e2);
+      if (ENT) u2[q] = fma_f32x2(e2, d2, u2[q]);
+    }
+  }
+#pragma unroll
+  for (int d = NG / 2; d > 0; d >>= 1) {
+#pragma unroll
+    for (int q = 0; q < d; ++q) {
+      s2[q] = add_f32x2(s2[q], s2[q + d]);
+      if (ENT) u2[q] = add_f32x2(u2[q], u2[q + d]);
+    }
+  }
+  float a0, a1;
+  unpack_f32x2(s2[0], a0, a1);
+  s = a0 + a1;
+  unpack_f32x2(u2[0], a0, a1);
+  u = a0 + a1;
+}
+template <int DT, bool ENT>
+__device__ __forceinline__ void score_step(const Group16<DT> (&g)[ScoreCfg<DT>::kGroups], float mx, float c2,
+                                           ScoreSums& t, bool& masked) {
+  if (fmaf(mx - t.m, c2, -8.0f) > 0.f && mx < CUDART_INF_F) {
+    const float r = ex2_approx((t.m - mx) * c2);
+    if (ENT) t.u = r > 0.f ? r * (t.u + t.s * (t.m - mx)) : 0.f;  // x - mx = (x - m) + (m - mx)
+    t.s *= r;
+    t.m = mx;
+  }
+  float s, u;
+  if (!masked) {
+    score_terms<DT, ENT, false>(g, t.m, c2, s, u);
+    masked = __any_sync(0xffffffffu, ENT ? u != u : s != s);
+  }
+  if (masked) score_terms<DT, ENT, true>(g, t.m, c2, s, u);
+  t.s += s;
+  if (ENT) t.u += u;
+}
+
+// Maximum of a lane's tokens of a step, NaN ignored (NaN if there is nothing else).
 template <int DT>
-__device__ __noinline__ ScorePart score_careful(const char* rowp, int t0, int t1, float c2) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ float score_max(const Group16<DT> (&g)[ScoreCfg<DT>::kGroups]) {
+  if constexpr (DT == kBF16) {
+    uint32_t x = g[0].a.w[0];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        if (q + t > 0) x = max_bf16x2(x, g[q].a.w[t]);
+    return fmaxf(bf16_lo(x), bf16_hi(x));
+  } else {
+    return fmaxf(group16_max(g[0]), group16_max(g[1]));
+  }
+}
+
+// A lower bound on the k-th largest of the warp's 32 N values (ordered codes), exact in its upper
+// 16 bits at least.  0 when fewer than k are above 0.  A few are taken off the top one by one (80
+// cycles each); otherwise the code is found two bits at a time.
+template <int N>
+__device__ __forceinline__ uint32_t warp_kth(const uint32_t (&code)[N], int k) {
+  uint32_t kth = 0u;
+  if (k <= 6) {
+    uint32_t v[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) v[q] = code[q];
+#pragma unroll 1
+    for (int i = 0; i < k; ++i) {
+      uint32_t mine = v[0];
+#pragma unroll
+      for (int q = 1; q < N; ++q) mine = max(mine, v[q]);
+      kth = __reduce_max_sync(0xffffffffu, mine);
+      const unsigned who = __ballot_sync(0xffffffffu, mine == kth);
+      bool drop = (int)(threadIdx.x & 31) == __ffs(who) - 1;
+#pragma unroll
+      for (int q = 0; q < N; ++q) {
+        if (drop && v[q] == kth) {
+          v[q] = 0u;
+          drop = false;
+        }
+      }
+    }
+    return kth;
+  }
+#pragma unroll 1
+  for (int shift = 30; shift >= 16; shift -= 2) {
+    // how many values are at or above each of the three next thresholds: at most 128, ten bits each
+    uint32_t c = 0u;
+#pragma unroll
+    for (int d = 0; d < 3; ++d) {
+      const uint32_t t = kth | ((uint32_t)(d + 1) << shift);
+#pragma unroll
+      for (int q = 0; q < N; ++q) c += code[q] >= t ? 1u << (10 * d) : 0u;
+    }
+    c = __reduce_add_sync(0xffffffffu, c);
+    const uint32_t k_ = (uint32_t)k;
+    kth |= (uint32_t)(((c & 1023u) >= k_) + (((c >> 10) & 1023u) >= k_) + ((c >> 20) >= k_)) << shift;
+  }
+  return kth;
+}
+// ------------------------------------------------------------------------------------------
+// The M largest logits.  The sweep itself only stores, per lane and step, the largest of the lane's
+// tokens ("entry": 64 tokens of bf16, 32 of fp32, or a power of two of steps where there would be
+// too many), rounded down to bf16: two instructions a step.  At the end the M-th largest of a few
+// maxima over entries (distinct tokens) bounds the M-th largest logit T from below; entries that
+// reach T are listed, their tokens read once more, and those that reach T ranked.  Some 1.1 M tokens
+// get that far, so what this costs does not depend on the row's length or order.  (Testing groups
+// against a running threshold in the sweep and examining them in batches took 11 thousand
+// instructions a row of 152064 tokens and M = 20, four tenths of what the sums take.)
+// Rows of which more tokens reach T than the buffers hold (equal logits) go through a radix select.
+// ------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t top_entry_bits(float x, std::integral_constant<int, kBF16>) {
+  return __float_as_uint(x) >> 16;
+}
+// x rounded down to bf16
+__device__ __forceinline__ uint32_t bf16_floor_bits(float x) {
+  uint32_t b = __float_as_uint(x);
+  if (b & 0x80000000u) b += 0xffffu;
+  return b >> 16;
+}
+__device__ __forceinline__ uint32_t top_entry_bits(float x, std::integral_constant<int, kF32>) {
+  return bf16_floor_bits(x);
+}
+// log2 of the steps per entry for at most `most` entries
+__device__ __forceinline__ int entry_shift(int steps, int most) {
+  int k = 0;
+  while (((steps - 1) >> k) >= most) ++k;
+  return k;
+}
+// A lane's column of entries: word w holds entries 2 w and 2 w + 1, words 32 apart.
+struct EntryColumn {
+  uint32_t* col;  // + lane already
+  int n;          // entries
+  __device__ __forceinline__ void put(int e, uint32_t bits) { ((uint16_t*)(col + (e >> 1) * 32))[e & 1] = (uint16_t)bits; }
+  __device__ __forceinline__ int words() const { return (n + 1) >> 1; }
+};
+constexpr uint32_t kNoEntry2 = 0xff80ff80u;  // -inf twice
+
+// Maxima of a lane's entries, 16 of them, as ordered codes (fewer: the others 0).  An entry of +inf is
+// left out: nothing is known about its finite tokens.
+__device__ __forceinline__ void entry_slots(const EntryColumn& c, uint32_t (&code)[16]) {
+  uint32_t acc[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = kNoEntry2;
+  const int W = c.words();
+#pragma unroll 1
+  for (int w0 = 0; w0 < W; w0 += 8) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (w0 + j < W) acc[j] = max_bf16x2(acc[j], c.col[(w0 + j) * 32]);
+  }
+  uint32_t any = acc[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) any = max_bf16x2(any, acc[j]);
+  if ((any & 0xffffu) == 0x7f80u || (any >> 16) == 0x7f80u) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = kNoEntry2;
+    for (int w = 0; w < W; ++w) {
+      uint32_t x = c.col[w * 32];
+      if ((x & 0xffffu) == 0x7f80u) x = (x & 0xffff0000u) | 0xff80u;
+      if ((x >> 16) == 0x7f80u) x = (x & 0xffffu) | 0xff800000u;
+      acc[0] = max_bf16x2(acc[0], x);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float lo = bf16_lo(acc[j]), hi = bf16_hi(acc[j]);
+    code[2 * j] = lo > -CUDART_INF_F ? enc_ordered(lo + 0.0f) : 0u;
+    code[2 * j + 1] = hi > -CUDART_INF_F ? enc_ordered(hi + 0.0f) : 0u;
+  }
+}
+// The warp's bound: at least k of its tokens have this code or more (0: no bound).
+__device__ __forceinline__ uint32_t entry_bound(const EntryColumn& c, int k) {
+  uint32_t code[16];
+  entry_slots(c, code);
+  if (k > 64) return warp_kth<16>(code, k);
+  uint32_t few[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) few[j] = max(max(code[j], code[j + 4]), max(code[j + 8], code[j + 12]));
+  return warp_kth<4>(few, k);
+}
+// What an entry and a token have to exceed to reach the bound.
+struct EntryTest {
+  bool all;       // no bound: every entry
+  uint32_t low2;  // the bf16 below the bound, twice
+  float thr;      // tokens strictly above it
+};
+__device__ __forceinline__ EntryTest entry_test(uint32_t bound) {
+  EntryTest t;
+  const uint32_t o = bound >> 16;
+  t.all = o <= 0x007fu;  // at or below the code of -inf
+  const uint32_t d = o - 1u;
+  uint32_t raw = (d & 0x8000u) ? d & 0x7fffu : ~d & 0xffffu;
+  if (raw == 0x8000u) raw = 0x8001u;  // below +0 comes the largest negative number, not -0
+  t.low2 = raw * 0x10001u;
+  const float f = dec_ordered(o << 16);
+  t.thr = t.all ? -CUDART_INF_F : __uint_as_float(o == 0x8000u ? 0x80000001u : o > 0x8000u ? __float_as_uint(f) - 1u : __float_as_uint(f) + 1u);
+  return t;
+}
+// Lists the lane's entries that pass: ids e * 32 + lane + base.
+__device__ __forceinline__ void entry_list(const EntryColumn& c, const EntryTest& t, uint16_t* list, int cap, int* count,
+                                           int base) {
+  const int W = c.words();
+#pragma unroll 4
+  for (int w = 0; w < W; ++w) {
+    const uint32_t x = max_bf16x2(c.col[w * 32], t.low2) ^ t.low2;
+    if (x != 0u || t.all) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int e = 2 * w + h;
+        if (e < c.n && (t.all || ((x >> (16 * h)) & 0xffffu) != 0u)) {
+          const int at = atomicAdd(count, 1);  // the order does not matter: tokens are ranked
+          if (at < cap) list[at] = (uint16_t)(base + e * 32 + (int)(threadIdx.x & 31));
+        }
+      }
+    }
+  }
+}
+__device__ __forceinline__ unsigned long long score_code(uint32_t key, int idx) {
+  return ((unsigned long long)key << 32) | (uint32_t)~idx;  // orders by value, then by lower index
+}
+// Appends the tokens above thr of the group at virtual index v to the candidates.
+template <int DT>
+__device__ __forceinline__ void group_candidates(const char* rowp, int v, int mis, int end, float thr,
+                                                 unsigned long long* cand, int cap, int* count) {
+  constexpr int ES = DT == kBF16 ? 2 : 4;
+  if (v >= end) return;
+  Group16<DT> g;
+  if (v >= mis && v + 16 <= end)
+    load16_vec(g, rowp + ((long long)v - mis) * ES);
+  else
+    score_edge<DT>(&g, rowp, v, mis, end);
+  uint32_t pass = 0u;
+#pragma unroll
+  for (int t = 0; t < 16; ++t) {
+    const float x = group16_get<DT>(g, t);
+    if (x > thr && x < CUDART_INF_F) pass |= 1u << t;  // false for NaN
+  }
+  if (v < mis) pass &= 0xffffu << (mis - v);  // outside the row
+  if (v + 16 > end) pass &= 0xffffu >> (v + 16 - end);
+  if (pass == 0u) return;
+  int at = atomicAdd(count, __popc(pass));
+#pragma unroll
+  for (int t = 0; t < 16; ++t) {
+    if ((pass >> t) & 1u) {
+      if (at < cap) cand[at] = score_code(enc_ordered(group16_get<DT>(g, t) + 0.0f), v + t - mis);
+      ++at;
+    }
+  }
+}
+
+// The M best tokens among the steps first, first + stride, .. of the caller's warps by a radix select
+// over (value, index) codes, eight bits a pass from the top, each pass reading the steps again; then
+// the tokens at or above the M-th code, at most M, in no order.  THREADS: 32 (a warp) or a whole CTA.
+struct SelectShared {
+  uint32_t hist[256];
+  uint32_t bin, rem, count;
+};
+template <int DT, int THREADS>
+__device__ __noinline__ void score_select(SelectShared& sh, unsigned long long* cand, int* n_cand, const char* rowp,
+                                          int mis, int end, int first, int stride, int M) {
+  constexpr int kStep = ScoreCfg<DT>::kStep;
+  const int tid = THREADS == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x, lane = threadIdx.x & 31;
+  auto sync = [&]() {
+    if (THREADS == 32) __syncwarp();
+    else __syncthreads();
+  };
+  auto for_each = [&](auto&& f) {
+    for (long long s = first; s * kStep < end; s += stride) {
+      for (int t = lane; t < kStep; t += 32) {
+        const long long v = s * kStep + t;
+        if (v < mis || v >= end) continue;
+        const float x = load_logit<DT>(rowp, v - mis);
+        if (fabsf(x) < CUDART_INF_F) f(score_code(enc_ordered(x + 0.0f), (int)(v - mis)));
+      }
+    }
+  };
+  unsigned long long prefix = 0ull;
+  uint32_t remaining = (uint32_t)M;
+  int shift = 56;
+  for (;;) {
+    sync();
+    for (int i = tid; i < 256; i += THREADS) sh.hist[i] = 0u;
+    sync();
+    for_each([&](unsigned long long c) {
+      if (shift == 56 || (c >> (shift + 8)) == prefix) atomicAdd(&sh.hist[(c >> shift) & 255u], 1u);
+    });
+    sync();
+    if (tid == 0) {
+      uint32_t above = 0u;
+      int bin = 255;
+      for (; bin > 0 && above + sh.hist[bin] < remaining; --bin) above += sh.hist[bin];
+      sh.bin = (uint32_t)bin;
+      sh.rem = remaining - above;  // more than the bin's count when there are fewer than M tokens
+      sh.count = sh.hist[bin];
+    }
+    sync();
+    prefix = (prefix << 8) | sh.bin;
+    remaining = sh.rem;
+    if (sh.count <= remaining || shift == 0) break;  // every code with this prefix is wanted
+    shift -= 8;
+  }
+  const unsigned long long from = prefix << shift;
+  sync();
+  if (tid == 0) *n_cand = 0;
+  sync();
+  for_each([&](unsigned long long c) {
+    if (c >= from) {
+      const int at = atomicAdd(n_cand, 1);
+      if (at < M) cand[at] = c;
+    }
+  });
+  sync();
+}
+
+// Statistics of tokens t0, t0 + dt, .. below V (each thread its own) with every element checked, two
+// passes, sums in 64 bits: for rows on which the sweep's arithmetic does not hold (+inf logits,
+// logits beyond 1e30 in size, no finite logit at all).  First the maximum, then the sums.
+template <int DT>
+__device__ __noinline__ float careful_max(const char* rowp, int t0, int dt, int V) {
   float m = -CUDART_INF_F;
-  for (int t = t0 + lane; t < t1; t += 32) {
+  for (long long t = t0; t < V; t += dt) {
     const float x = load_logit<DT>(rowp, t);
     if (fabsf(x) < CUDART_INF_F) m = fmaxf(m, x);
   }
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  ScorePart r;
-  r.m = m;
-  r.s = r.u = 0.f;
-  r.n = 0;
-  if (m == -CUDART_INF_F) return r;
+  return m;
+}
+template <int DT>
+__device__ __noinline__ double2 careful_sums(const char* rowp, int t0, int dt, int V, float m, float c2) {
   double s = 0.0, u = 0.0;
-  for (int t = t0 + lane; t < t1; t += 32) {
+  for (long long t = t0; t < V; t += dt) {
     const float x = load_logit<DT>(rowp, t);
     if (!(fabsf(x) < CUDART_INF_F)) continue;
     const double d = (double)x - (double)m;
@@ -173,20 +504,53 @@ __device__ __noinline__ ScorePart score_careful(const char* rowp, int t0, int t1
     s += e;
     if (e > 0.0) u += e * d;
   }
+  return make_double2(s, u);
+}
+__device__ __forceinline__ double2 warp_sum2(double2 a) {
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) {
-    s += __shfl_xor_sync(0xffffffffu, s, d);
-    u += __shfl_xor_sync(0xffffffffu, u, d);
+    a.x += __shfl_xor_sync(0xffffffffu, a.x, d);
+    a.y += __shfl_xor_sync(0xffffffffu, a.y, d);
   }
-  r.s = (float)s;
-  r.u = (float)u;
+  return a;
+}
+__device__ __forceinline__ float warp_max(float m) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  return m;
+}
+// The lane's sums moved to the reference m; NaN when they are not finite, however far below m.
+__device__ __forceinline__ double2 sums_at(const ScoreSums& t, float m, float c2) {
+  if (!(t.s < CUDART_INF_F)) return make_double2(CUDART_NAN, CUDART_NAN);
+  const float r = ex2_approx((t.m - m) * c2);
+  if (!(r > 0.f)) return make_double2(0.0, 0.0);
+  return make_double2((double)t.s * r, ((double)t.u + (double)t.s * ((double)t.m - (double)m)) * r);
+}
+// Whether the sweep's sums stand: not zero, infinite or NaN, and the reference in the range in which
+// a difference of two logits can not overflow.
+__device__ __forceinline__ bool sums_stand(double2 a, float m) {
+  return a.x > 0.0 && a.x < (double)CUDART_INF_F && fabs(a.y) < (double)CUDART_INF_F && m < 1e30f;
+}
+
+// The given token of this lane and its logit, requested before the row is read.
+struct ScoreGiven {
+  int t;
+  float x;
+};
+template <int DT>
+__device__ __forceinline__ ScoreGiven score_given(const ScoreArgs& A, long long row, const ScoreRow& rl, int g) {
+  ScoreGiven r = {-1, 0.f};
+  if (g < A.G) {
+    r.t = __ldg(A.tokens + row * A.G + g);
+    if (r.t >= 0 && r.t < A.V) r.x = load_logit<DT>(rl.rowp, r.t);
+  }
   return r;
 }
 
 // Outputs of one row except its alternatives, by one warp.  m reference logit, s and u the sums.
 template <int DT>
-__device__ __forceinline__ double score_emit(const ScoreArgs& A, long long row, const ScoreRow& rl, float m,
-                                             double s, double u) {
+__device__ __forceinline__ double score_emit(const ScoreArgs& A, long long row, const ScoreRow& rl, ScoreGiven gv,
+                                             float m, double s, double u) {
   const int lane = threadIdx.x & 31;
   const bool some = s > 0.0;
   const double ls = some ? log(s) : 0.0;
@@ -202,15 +566,14 @@ __device__ __forceinline__ double score_emit(const ScoreArgs& A, long long row, 
     if (!some && A.status != nullptr) atomicOr(A.status, 1u);
   }
   for (int g = lane; g < A.G; g += 32) {
-    const int t = __ldg(A.tokens + row * A.G + g);
+    if (g >= 32) gv = score_given<DT>(A, row, rl, g);
     float lp = 0.f;
-    if (t >= A.V) {
+    if (gv.t >= A.V) {
       lp = -CUDART_INF_F;
       if (A.status != nullptr) atomicOr(A.status, kDevBadToken);
-    } else if (t >= 0) {
-      const float x = load_logit<DT>(rl.rowp, t);
-      lp = some && fabsf(x) < CUDART_INF_F
-               ? (float)(((double)x - (double)m) * (double)rl.inv_t - ls)
+    } else if (gv.t >= 0) {
+      lp = some && fabsf(gv.x) < CUDART_INF_F
+               ? (float)(((double)gv.x - (double)m) * (double)rl.inv_t - ls)
                : -CUDART_INF_F;
     }
     A.out_lp[row * A.G + g] = lp;
@@ -223,13 +586,16 @@ __device__ __forceinline__ void score_emit_top(const ScoreArgs& A, long long row
   A.top_ids[row * A.M + i] = idx;
   A.top_lp[row * A.M + i] = (float)(((double)dec_ordered(key) - (double)m) * (double)inv_t - ls);
 }
+__device__ __forceinline__ void score_emit_no_top(const ScoreArgs& A, long long row, int i) {
+  A.top_ids[row * A.M + i] = -1;
+  A.top_lp[row * A.M + i] = -CUDART_INF_F;
+}
 
 // The row of an emitted position behind the last token.
 __device__ __forceinline__ void score_emit_nothing(const ScoreArgs& A, long long row) {
   const int lane = threadIdx.x & 31;
   if (lane == 0) {
     A.out_lse[row] = 0.f;
-    if (A.out_tail != nullptr) A.out_tail[row] = 0.f;
     if (A.out_ent != nullptr) A.out_ent[row] = 0.f;
     A.out_lp[row] = 0.f;
   }
@@ -239,331 +605,356 @@ __device__ __forceinline__ void score_emit_nothing(const ScoreArgs& A, long long
   }
 }
 
-// One pass over the rows.  A warp takes (row, slice) items in turn.
+// ------------------------------------------------------------------------------------------
+// Many rows: a warp per row.
+// ------------------------------------------------------------------------------------------
+constexpr int kScoreCtasPerSM = 16;  // one warp each
+constexpr int kRowEntries = 80;      // per lane
+constexpr int kRowCap = 512;         // listed entries, candidates
+
+struct RowShared {
+  uint32_t entry[kRowEntries / 2][32];
+  unsigned long long cand[kRowCap];
+  uint16_t list[kRowCap];
+  SelectShared sel;
+  int n_list, n;
+};
+
 template <int DT, bool ENT>
-__global__ void __launch_bounds__(32, kScoreCtasPerSM) score_kernel(const __grid_constant__ ScoreArgs A) {
+__global__ void __launch_bounds__(32, kScoreCtasPerSM) score_rows_kernel(const __grid_constant__ ScoreArgs A) {
   extern __shared__ __align__(16) unsigned char score_smem[];
-  TopmWarpBuf* const wb = (TopmWarpBuf*)score_smem;  // present when M > 0
-  __shared__ int queue[kS4QueueCap];
+  RowShared& sh = *(RowShared*)score_smem;  // present when M > 0
   constexpr int ES = DT == kBF16 ? 2 : 4;
   constexpr int NG = ScoreCfg<DT>::kGroups;
   constexpr int kStep = ScoreCfg<DT>::kStep;
   typedef Group16<DT> Grp;
-  const int lane = threadIdx.x & 31;
-  const uint32_t lt = (1u << lane) - 1u;
-  const long long n_items = A.rows * A.splits;
+  const int lane = threadIdx.x;
 
-  for (long long it = blockIdx.x; it < n_items; it += gridDim.x) {
-    const long long row = it / A.splits;
-    const int split = (int)(it % A.splits);
+  for (long long row = blockIdx.x; row < A.rows; row += gridDim.x) {
     const ScoreRow rl = score_locate<ES>(A, row);
     if (!rl.live) {
-      if (split == 0) score_emit_nothing(A, row);
+      score_emit_nothing(A, row);
       continue;
     }
     const float c2 = rl.inv_t * kLog2e;
-    // the row in groups counted from the 32-byte boundary at or below its start, so that a row
-    // that starts anywhere is read by aligned 32-byte loads; only groups that stick out at either
-    // end are read element by element
     const int mis = (int)((uintptr_t)rl.rowp & 31) / ES;
-    const char* const base = rl.rowp - mis * ES;
     const int end = mis + A.V;
     const int n_steps = (end + kStep - 1) / kStep;
-    const int s_begin = split * A.steps_per_slice;
-    const int s_end = min(n_steps, s_begin + A.steps_per_slice);
+    const int es = entry_shift(n_steps, kRowEntries), in_entry = (1 << es) - 1;
+    EntryColumn col = {&sh.entry[0][lane], ((n_steps - 1) >> es) + 1};
 
-    auto load_step = [&](Grp (&g)[NG], int s) {
-      const int v0 = s * kStep + lane * 16;
-#pragma unroll
-      for (int q = 0; q < NG; ++q) {
-        const int v = v0 + q * 512;
-        if (v >= mis && v + 16 <= end) {
-          load16_vec(g[q], base + (size_t)v * ES);
-        } else {
-          float x[16];
-#pragma unroll
-          for (int t = 0; t < 16; ++t)
-            x[t] = v + t >= mis && v + t < end ? load_logit<DT>(rl.rowp, v + t - mis) : -CUDART_INF_F;
-          if constexpr (DT == kBF16) {
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-              g[q].a.w[t] = (__float_as_uint(x[2 * t]) >> 16) | (__float_as_uint(x[2 * t + 1]) & 0xffff0000u);
-          } else {
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-              g[q].a.w[t] = __float_as_uint(x[t]);
-              g[q].b.w[t] = __float_as_uint(x[8 + t]);
-            }
-          }
-        }
-      }
-    };
-
-    float thr = A.M > 0 ? -CUDART_INF_F : CUDART_INF_F;
-    int n = 0, qn = 0, s = s_begin;
-    float lm = kGroupLseFloor;
-    float s_tot = 0.f, u_tot = 0.f;
     Grp nxt[NG];
-    if (s < s_end) {
-      load_step(nxt, s);
-      // the first step's maximum is the sums' reference; the M-th largest of its group maxima
-      // (distinct tokens) bounds the M-th largest logit of the row from below
-      float gm[NG];
-      float mx = -CUDART_INF_F;
-#pragma unroll
-      for (int q = 0; q < NG; ++q) {
-        gm[q] = group16_max(nxt[q]);
-        if (gm[q] == CUDART_INF_F) gm[q] = -CUDART_INF_F;
-        mx = fmaxf(mx, gm[q]);
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-      lm = fmaxf(lm, mx);
-      if (A.M > 0 && A.M <= 32 * NG) {
-        uint32_t code[NG], kth = 0u;
-#pragma unroll
-        for (int q = 0; q < NG; ++q) code[q] = enc_ordered(gm[q] + 0.0f);
+    score_load<DT>(nxt, rl.rowp, mis, end, 0);
+    const ScoreGiven given = score_given<DT>(A, row, rl, lane);
+    // the first step's maximum is the sums' reference
+    const float mx0 = warp_max(score_max<DT>(nxt));
+    ScoreSums sums = {mx0 < CUDART_INF_F ? fmaxf(mx0, kGroupLseFloor) : kGroupLseFloor, 0.f, 0.f};
+    bool masked = false;
+    float top = -CUDART_INF_F;
 #pragma unroll 1
-        for (uint32_t bit = 0x80000000u; bit != 0u; bit >>= 1) {
-          int c = 0;
+    for (int s = 0; s < n_steps; ++s) {
+      Grp g[NG];
 #pragma unroll
-          for (int q = 0; q < NG; ++q) c += __popc(__ballot_sync(0xffffffffu, code[q] >= (kth | bit)));
-          if (c >= A.M) kth |= bit;
-        }
-        const float f = dec_ordered(kth);
-        if (f > -CUDART_INF_F) thr = just_below(f);
+      for (int q = 0; q < NG; ++q) g[q] = nxt[q];
+      if (s + 1 < n_steps) score_load<DT>(nxt, rl.rowp, mis, end, s + 1);
+      const float mx = score_max<DT>(g);
+      if (A.M > 0) {
+        top = (s & in_entry) != 0 ? fmaxf(top, mx) : mx;
+        col.put(s >> es, top_entry_bits(top, std::integral_constant<int, DT>()));
       }
+      score_step<DT, ENT>(g, mx, c2, sums, masked);
     }
-    __syncwarp();
-    for (;;) {
-#pragma unroll 1
-      for (; s < s_end && qn < 32; ++s) {
-        Grp g[NG];
-#pragma unroll
-        for (int q = 0; q < NG; ++q) g[q] = nxt[q];
-        if (s + 1 < s_end) load_step(nxt, s + 1);
-        unsigned long long s2 = 0ull, u2 = 0ull;  // this step's sums; folded into the totals below
-#pragma unroll
-        for (int q = 0; q < NG; ++q) {
-          const float amax = group16_max(g[q]);
-          const bool hit = amax > thr;  // false for NaN
-          const unsigned bal = __ballot_sync(0xffffffffu, hit);
-          if (bal != 0u) {
-            if (hit && GLS_IN_RANGE(qn + __popc(bal & lt), 0, kS4QueueCap, 61u))
-              queue[qn + __popc(bal & lt)] = ((s * kStep + q * 512) >> 4) + lane;
-            qn += __popc(bal);
-          }
-          // The reference moves only when a maximum exceeds it by 2^8: the terms stay within
-          // fp32 and the two parts of the entropy small.
-          if (fmaf(amax - lm, c2, -8.0f) > 0.f && amax < CUDART_INF_F) {
-            const float r = ex2_approx((lm - amax) * c2);
-            const float dl = lm - amax;  // x - amax = (x - lm) + (lm - amax)
-            float s0, s1, u0, u1;
-            unpack_f32x2(s2, s0, s1);
-            unpack_f32x2(u2, u0, u1);
-            if (ENT) {
-              u2 = pack_f32x2(r > 0.f ? r * (u0 + s0 * dl) : 0.f, r > 0.f ? r * (u1 + s1 * dl) : 0.f);
-              u_tot = r > 0.f ? r * (u_tot + s_tot * dl) : 0.f;
-            }
-            s2 = pack_f32x2(r * s0, r * s1);
-            s_tot *= r;
-            lm = amax;
-          }
-          const unsigned long long c22 = pack_f32x2(c2, c2), nlm2 = pack_f32x2(-lm, -lm);
-          Grp h = g[q];
-          if (ENT) {
-            // -inf and NaN become the lowest finite value: their terms are exactly 0 in both sums
-            if constexpr (DT == kBF16) {
-#pragma unroll
-              for (int t = 0; t < 8; ++t) h.a.w[t] = max_bf16x2(h.a.w[t], 0xff7fff7fu);
-            } else {
-#pragma unroll
-              for (int t = 0; t < 8; ++t) {
-                h.a.w[t] = __float_as_uint(fmaxf(__uint_as_float(h.a.w[t]), -3.402823466e38f));
-                h.b.w[t] = __float_as_uint(fmaxf(__uint_as_float(h.b.w[t]), -3.402823466e38f));
-              }
-            }
-          }
-#pragma unroll
-          for (int t = 0; t < 16; t += 2) {
-            const unsigned long long d2 = group16_diff2(h, t, -lm, nlm2);
-            float e0, e1;
-            unpack_f32x2(mul_f32x2(d2, c22), e0, e1);
-            const unsigned long long e2 = pack_f32x2(ex2_approx(e0), ex2_approx(e1));
-            s2 = add_f32x2(s2, e2);
-            if (ENT) u2 = fma_f32x2(e2, d2, u2);
-          }
-        }
-        float a0, a1;
-        unpack_f32x2(s2, a0, a1);
-        s_tot += a0 + a1;
-        if (ENT) {
-          unpack_f32x2(u2, a0, a1);
-          u_tot += a0 + a1;
-        }
-      }
-      if (qn == 0) break;
-      __syncwarp();
-      for (int first = 0; first < qn; first += 32) {
-        const unsigned long long r =
-            score_expand<DT>(wb, queue, rl.rowp, mis, A.V, first, min(32, qn - first), n, A.M, thr);
-        n = (int)(unsigned)r;
-        thr = __uint_as_float((uint32_t)(r >> 32));
-      }
-      qn = 0;
-      __syncwarp();
-      if (s >= s_end) break;
-    }
-    if (n > A.M) n = (int)(unsigned)topm_prune(wb, n, A.M, DT == kBF16 ? 2 : 0);
-    __syncwarp();
 
     // ---- combine the lanes ---------------------------------------------------------------------
-    float m = lm;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    const float r = ex2_approx((lm - m) * c2);
-    double sd = (double)s_tot * r;
-    double ud = r > 0.f ? ((double)u_tot + (double)s_tot * ((double)lm - (double)m)) * r : 0.0;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      sd += __shfl_xor_sync(0xffffffffu, sd, d);
-      if (ENT) ud += __shfl_xor_sync(0xffffffffu, ud, d);
+    float m = warp_max(sums.m);
+    double2 a = warp_sum2(sums_at(sums, m, c2));
+    if (!sums_stand(a, m)) {
+      m = warp_max(careful_max<DT>(rl.rowp, lane, 32, A.V));
+      a = make_double2(0.0, 0.0);
+      if (m > -CUDART_INF_F) a = warp_sum2(careful_sums<DT>(rl.rowp, lane, 32, A.V, m, c2));
     }
-    // sums that are zero, infinite or NaN, or a reference out of the range in which a difference
-    // of two logits can not overflow
-    if (!(sd > 0.0 && sd < (double)CUDART_INF_F && fabs(ud) < (double)CUDART_INF_F && m < 1e30f)) {
-      const int t0 = max(0, s_begin * kStep - mis);
-      const int t1 = (int)min((long long)A.V, (long long)s_end * kStep - mis);
-      const ScorePart p = score_careful<DT>(rl.rowp, t0, t1, c2);
-      m = p.m;
-      sd = p.s;
-      ud = p.u;
-    }
-    if (A.splits == 1) {
-      const double ls = score_emit<DT>(A, row, rl, m, sd, ud);
-      for (int i = lane; i < A.M; i += 32) {  // rank of entry i: how many come before it
-        int rank = i;
-        int idx = -1;
-        uint32_t key = 0u;
-        if (i < n) {
-          key = wb->key[i];
-          idx = wb->idx[i];
-          rank = 0;
-          const unsigned long long mine = score_code(key, idx);
-          for (int o = 0; o < n; ++o) rank += score_code(wb->key[o], wb->idx[o]) > mine;
-        }
-        if (idx >= 0) {
-          score_emit_top(A, row, rank, key, idx, m, rl.inv_t, ls);
-        } else {
-          A.top_ids[row * A.M + i] = -1;
-          A.top_lp[row * A.M + i] = -CUDART_INF_F;
-        }
+    const double ls = score_emit<DT>(A, row, rl, given, m, a.x, a.y);
+    if (A.M == 0) continue;
+
+    // ---- alternatives ----------------------------------------------------------------------------
+    if (col.n & 1) col.put(col.n, 0xff80u);
+    if (lane == 0) sh.n_list = sh.n = 0;
+    __syncwarp();
+    const EntryTest test = entry_test(entry_bound(col, A.M));
+    entry_list(col, test, sh.list, kRowCap, &sh.n_list, 0);
+    __syncwarp();
+    const int groups = sh.n_list << es;  // per lane slot: NG groups each
+    if (sh.n_list <= kRowCap) {
+      for (int i = lane; i < groups * NG; i += 32) {
+        const int id = sh.list[i / NG >> es];
+        const int step = (id >> 5 << es) + (i / NG & in_entry);
+        if (step < n_steps)
+          group_candidates<DT>(rl.rowp, step * kStep + (i % NG) * 512 + (id & 31) * 16, mis, end, test.thr, sh.cand,
+                               kRowCap, &sh.n);
       }
-    } else {
-      const long long at = row * A.splits + split;
-      if (lane == 0) {
-        ScorePart p;
-        p.m = m;
-        p.s = (float)sd;
-        p.u = (float)ud;
-        p.n = n;
-        A.parts[at] = p;
-      }
-      for (int i = lane; i < n; i += 32) A.cand[at * A.M + i] = score_code(wb->key[i], wb->idx[i]);
     }
-    __syncwarp();  // the buffer is free for the next item
+    __syncwarp();
+    if (sh.n_list > kRowCap || sh.n > kRowCap)
+      score_select<DT, 32>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, 0, 1, A.M);
+    const int n = sh.n;
+    for (int i = lane; i < n; i += 32) {  // the rank of candidate i: how many come before it
+      const unsigned long long mine = sh.cand[i];
+      int rank = 0;
+      for (int o = 0; o < n; ++o) rank += sh.cand[o] > mine;
+      if (rank < A.M) score_emit_top(A, row, rank, (uint32_t)(mine >> 32), (int)~(uint32_t)mine, m, rl.inv_t, ls);
+    }
+    for (int i = n + lane; i < A.M; i += 32) score_emit_no_top(A, row, i);
+    __syncwarp();  // the shared memory is free for the next row
   }
-  asm volatile("griddepcontrol.launch_dependents;");
 }
 
-// Merges the slices of a row: statistics in 64 bits, the slices' candidates sorted in shared memory.
-constexpr int kScoreMergeThreads = 256;
-template <int DT>
-__global__ void __launch_bounds__(kScoreMergeThreads) score_merge_kernel(const __grid_constant__ ScoreArgs A) {
+// ------------------------------------------------------------------------------------------
+// Few rows: a cluster of CTAs per row.  The row's steps are dealt to the cluster's warps in turn; the
+// CTAs' statistics and their M best tokens meet in the first CTA through distributed shared memory.
+// ------------------------------------------------------------------------------------------
+// Four warps a CTA, four CTAs an SM: one CTA's selection runs beside the others' loads (1200 rows of
+// 152064 tokens: 101 us; with eight warps and two CTAs 116 us.  One row: 15.5 us against 14.3).
+constexpr int kClWarps = 4;
+constexpr int kClThreads = 32 * kClWarps;
+constexpr int kClCtasPerSM = 16 / kClWarps;
+constexpr int kClMaxCtas = 8;       // CTAs per cluster
+constexpr int kClEntries = 32;      // per lane
+constexpr int kClList = 256 * kClWarps;       // listed entries of a CTA
+constexpr int kClCand = 1024;       // tokens of a CTA that reach the bound
+static_assert(kClMaxCtas <= 32, "a lane per part");
+
+struct ClusterShared {
+  uint32_t entry[kClWarps][kClEntries / 2][32];
+  unsigned long long cand[kClCand];
+  unsigned long long best[kClMaxCtas][kScoreMaxM];  // the CTAs' M best, in descending order
+  uint16_t list[kClList];
+  SelectShared sel;
+  uint32_t bound[kClWarps];  // at least `share` tokens of the warp have this code or more
+  int all_best[kClMaxCtas];  // per CTA of the cluster, in the first one: codes in best, sums, reference
+  double2 all_part[kClMaxCtas];
+  float all_m[kClMaxCtas];
+  float red[kClWarps];
+  double2 red2[kClWarps];
+  int n_list, n;
+  double ls;
+};
+
+__device__ __forceinline__ uint32_t cluster_map(const void* p, uint32_t rank) {
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void cluster_st64(uint32_t a, unsigned long long v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_st32(uint32_t a, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
+template <int DT, bool ENT>
+__global__ void __launch_bounds__(kClThreads, kClCtasPerSM)
+score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
   extern __shared__ __align__(16) unsigned char score_smem[];
-  unsigned long long* const codes = (unsigned long long*)score_smem;
-  __shared__ int sh_n;
-  __shared__ double sh_ls;
-  __shared__ float sh_m;
+  ClusterShared& sh = *(ClusterShared*)score_smem;
   constexpr int ES = DT == kBF16 ? 2 : 4;
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // the sweep's writes are visible
+  constexpr int NG = ScoreCfg<DT>::kGroups;
+  constexpr int kStep = ScoreCfg<DT>::kStep;
+  typedef Group16<DT> Grp;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  for (long long row = blockIdx.x; row < A.rows; row += gridDim.x) {
-    const ScoreRow rl = score_locate<ES>(A, row);
-    if (!rl.live) continue;  // uniform over the CTA
-    const ScorePart* parts = A.parts + row * A.splits;
-    if (tid == 0) sh_n = 0;
-    __syncthreads();
-    if (warp == 0) {
-      const double c2 = (double)(rl.inv_t * kLog2e);
-      float m = -CUDART_INF_F;
-      for (int i = lane; i < A.splits; i += 32) {
-        const ScorePart p = parts[i];
-        if (p.s > 0.f) m = fmaxf(m, p.m);
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-      double s = 0.0, u = 0.0;
-      for (int i = lane; i < A.splits; i += 32) {
-        const ScorePart p = parts[i];
-        if (p.s > 0.f) {
-          const double dl = (double)p.m - (double)m;
-          const double r = exp2(dl * c2);
-          s += r * (double)p.s;
-          if (r > 0.0) u += r * ((double)p.u + (double)p.s * dl);
-        }
-      }
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, d);
-        u += __shfl_xor_sync(0xffffffffu, u, d);
-      }
-      const double ls = score_emit<DT>(A, row, rl, m, s, u);
-      if (lane == 0) {
-        sh_ls = ls;
-        sh_m = m;
-      }
-    }
-    if (A.M > 0) {
-      for (int i = warp; i < A.splits; i += kScoreMergeThreads / 32) {
-        const int n = parts[i].n;
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&sh_n, n);  // the order does not matter: the codes are sorted
-        at = __shfl_sync(0xffffffffu, at, 0);
-        for (int o = lane; o < n; o += 32)
-          if (GLS_IN_RANGE(at + o, 0, kScoreMaxCand, 62u)) codes[at + o] = A.cand[(row * A.splits + i) * A.M + o];
-      }
-      __syncthreads();
-      const int n = sh_n;
-      int p2 = 32;
-      while (p2 < n) p2 <<= 1;
-      for (int i = n + tid; i < p2; i += kScoreMergeThreads) codes[i] = 0ull;
-      __syncthreads();
-      for (int size = 2; size <= p2; size <<= 1) {  // bitonic sort, descending
-        for (int stride = size >> 1; stride > 0; stride >>= 1) {
-          for (int i = tid; i < p2 / 2; i += kScoreMergeThreads) {
-            const int a = 2 * i - (i & (stride - 1)), b = a + stride;
-            const unsigned long long x = codes[a], y = codes[b];
-            if ((x < y) == ((a & size) == 0)) {
-              codes[a] = y;
-              codes[b] = x;
-            }
-          }
-          __syncthreads();
-        }
-      }
-      for (int i = tid; i < A.M; i += kScoreMergeThreads) {
-        if (i < n) {
-          const unsigned long long c = codes[i];
-          score_emit_top(A, row, i, (uint32_t)(c >> 32), (int)~(uint32_t)c, sh_m, rl.inv_t, sh_ls);
-        } else {
-          A.top_ids[row * A.M + i] = -1;
-          A.top_lp[row * A.M + i] = -CUDART_INF_F;
-        }
-      }
-    }
-    __syncthreads();
+  const int rank = (int)(blockIdx.x % ctas);
+  const long long row = blockIdx.x / ctas;
+  const ScoreRow rl = score_locate<ES>(A, row);
+  if (ctas > 1) cluster_arrive();  // this CTA has started: its shared memory may be written
+  if (!rl.live) {  // the whole cluster
+    if (rank == 0 && warp == 0) score_emit_nothing(A, row);
+    if (ctas > 1) cluster_wait();
+    return;
   }
+  const float c2 = rl.inv_t * kLog2e;
+  const int mis = (int)((uintptr_t)rl.rowp & 31) / ES;
+  const int end = mis + A.V;
+  const int n_steps = (end + kStep - 1) / kStep;
+  const int first = rank * kClWarps + warp, stride = ctas * kClWarps;
+  const int mine = first < n_steps ? (n_steps - 1 - first) / stride + 1 : 0;  // steps of this warp
+  const int es = entry_shift((n_steps - 1) / stride + 1, kClEntries), in_entry = (1 << es) - 1;
+  EntryColumn col = {&sh.entry[warp][0][lane], mine > 0 ? ((mine - 1) >> es) + 1 : 0};
+
+  if (tid == 0) sh.n_list = sh.n = 0;
+  Grp nxt[NG];
+  ScoreSums sums = {kGroupLseFloor, 0.f, 0.f};
+  bool masked = false;
+  float top = -CUDART_INF_F;
+  ScoreGiven given = {-1, 0.f};
+  if (mine > 0) {
+    score_load<DT>(nxt, rl.rowp, mis, end, first);
+    if (rank == 0 && warp == 0) given = score_given<DT>(A, row, rl, lane);  // it has the row's first step
+    const float mx0 = warp_max(score_max<DT>(nxt));
+    if (mx0 < CUDART_INF_F) sums.m = fmaxf(mx0, kGroupLseFloor);
+  }
+#pragma unroll 1
+  for (int i = 0; i < mine; ++i) {
+    Grp g[NG];
+#pragma unroll
+    for (int q = 0; q < NG; ++q) g[q] = nxt[q];
+    if (i + 1 < mine) score_load<DT>(nxt, rl.rowp, mis, end, first + (i + 1) * stride);
+    const float mx = score_max<DT>(g);
+    if (A.M > 0) {
+      top = (i & in_entry) != 0 ? fmaxf(top, mx) : mx;
+      col.put(i >> es, top_entry_bits(top, std::integral_constant<int, DT>()));
+    }
+    score_step<DT, ENT>(g, mx, c2, sums, masked);
+  }
+  // Warps of this CTA that have a step; each vouches for `share` tokens at or above its own bound, so
+  // that M tokens of the row are at or above the smallest of them.
+  const int busy = min(kClWarps, max(0, n_steps - rank * kClWarps));
+  if (A.M > 0 && mine > 0) {
+    if (col.n & 1) col.put(col.n, 0xff80u);
+    const uint32_t b = entry_bound(col, (A.M + busy - 1) / busy);
+    if (lane == 0) sh.bound[warp] = b;
+  }
+  {
+    const float m = warp_max(sums.m);
+    const double2 a = warp_sum2(sums_at(sums, m, c2));
+    if (lane == 0) {
+      sh.red[warp] = m;
+      sh.red2[warp] = a;
+    }
+  }
+  __syncthreads();
+
+  // ---- this CTA's M best and sums go to the cluster's first CTA -----------------------------------
+  uint32_t home = (uint32_t)__cvta_generic_to_shared(&sh);
+  if (ctas > 1) {
+    cluster_wait();
+    home = cluster_map(&sh, 0u);
+  }
+  const uint32_t o_best = (uint32_t)offsetof(ClusterShared, best) + (uint32_t)rank * kScoreMaxM * 8u;
+  if (A.M > 0) {
+    uint32_t bound = 0xffffffffu;
+    for (int w = 0; w < busy; ++w) bound = min(bound, sh.bound[w]);
+    const EntryTest test = entry_test(bound);
+    if (mine > 0) entry_list(col, test, sh.list, kClList, &sh.n_list, warp * (kClEntries * 32));
+    __syncthreads();
+    const int listed = sh.n_list;
+    if (listed <= kClList) {
+      for (int i = tid; i < (listed << es) * NG; i += kClThreads) {
+        const int id = sh.list[i / NG >> es];
+        const int k = ((id >> 5) % kClEntries << es) + (i / NG & in_entry);  // the warp's k-th step
+        const int step = rank * kClWarps + id / (kClEntries * 32) + k * stride;
+        if (step < n_steps)
+          group_candidates<DT>(rl.rowp, step * kStep + (i % NG) * 512 + (id & 31) * 16, mis, end, test.thr, sh.cand,
+                               kClCand, &sh.n);
+      }
+    }
+    __syncthreads();
+    if (listed > kClList || sh.n > kClCand)
+      score_select<DT, kClThreads>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, first, stride, A.M);
+    const int n = sh.n;
+    for (int i = tid; i < n; i += kClThreads) {
+      const unsigned long long mine = sh.cand[i];
+      int r = 0;
+      for (int o = 0; o < n; ++o) r += sh.cand[o] > mine;
+      if (r < A.M) cluster_st64(home + o_best + 8u * r, mine);
+    }
+    if (tid == 0) cluster_st32(home + (uint32_t)offsetof(ClusterShared, all_best) + 4u * rank, (uint32_t)min(n, A.M));
+  }
+  if (warp == 0) {
+    const bool on = lane < kClWarps && sh.red2[lane < kClWarps ? lane : 0].x > 0.0;
+    const float mw = on ? sh.red[lane] : -CUDART_INF_F;
+    // a warp whose sums are NaN spoils the CTA's: the row is then summed again with every check
+    const bool odd = lane < kClWarps && !(sh.red2[lane < kClWarps ? lane : 0].x >= 0.0);
+    const float m = warp_max(mw);
+    double2 a = make_double2(0.0, 0.0);
+    if (on) {
+      const double dl = (double)mw - (double)m, r = exp2(dl * (double)c2);
+      a.x = r * sh.red2[lane].x;
+      a.y = r > 0.0 ? r * (sh.red2[lane].y + sh.red2[lane].x * dl) : 0.0;
+    }
+    a = warp_sum2(a);
+    if (__any_sync(0xffffffffu, odd)) a.x = CUDART_NAN;
+    if (lane == 0) {
+      const uint32_t o_part = (uint32_t)offsetof(ClusterShared, all_part) + 16u * rank;
+      cluster_st64(home + o_part, (unsigned long long)__double_as_longlong(a.x));
+      cluster_st64(home + o_part + 8u, (unsigned long long)__double_as_longlong(a.y));
+      cluster_st32(home + (uint32_t)offsetof(ClusterShared, all_m) + 4u * rank, __float_as_uint(m));
+    }
+  }
+  if (ctas > 1) {
+    cluster_arrive();
+    cluster_wait();
+    if (rank != 0) return;
+  }
+  __syncthreads();
+
+  // ---- the row -----------------------------------------------------------------------------------
+  const float mc = lane < ctas ? sh.all_m[lane] : -CUDART_INF_F;
+  float m = warp_max(mc);  // every warp for itself
+  double2 a = make_double2(0.0, 0.0);
+  if (lane < ctas) {
+    const double dl = (double)mc - (double)m;
+    const double r = mc > -CUDART_INF_F ? exp2(dl * (double)c2) : 0.0;
+    if (!(sh.all_part[lane].x >= 0.0)) {
+      a.x = CUDART_NAN;
+    } else if (r > 0.0) {
+      a.x = r * sh.all_part[lane].x;
+      a.y = r * (sh.all_part[lane].y + sh.all_part[lane].x * dl);
+    }
+  }
+  a = warp_sum2(a);
+  if (!sums_stand(a, m)) {  // uniform over the CTA
+    const float mt = warp_max(careful_max<DT>(rl.rowp, tid, kClThreads, A.V));
+    __syncthreads();
+    if (lane == 0) sh.red[warp] = mt;
+    __syncthreads();
+    m = sh.red[0];
+    for (int w = 1; w < kClWarps; ++w) m = fmaxf(m, sh.red[w]);
+    a = make_double2(0.0, 0.0);
+    if (m > -CUDART_INF_F) {
+      const double2 at = warp_sum2(careful_sums<DT>(rl.rowp, tid, kClThreads, A.V, m, c2));
+      if (lane == 0) sh.red2[warp] = at;
+      __syncthreads();
+      for (int w = 0; w < kClWarps; ++w) {
+        a.x += sh.red2[w].x;
+        a.y += sh.red2[w].y;
+      }
+    }
+  }
+  if (warp == 0) {
+    const double ls = score_emit<DT>(A, row, rl, given, m, a.x, a.y);
+    if (lane == 0) sh.ls = ls;
+  }
+  if (A.M == 0) return;
+  __syncthreads();
+  int total = 0;
+  for (int c = 0; c < ctas; ++c) total += sh.all_best[c];
+  // The lists are in descending order: a code's rank is its place in its own list and where it would
+  // stand in each other one, found in all of them at once.
+  const int half = 1 << (31 - __clz(A.M));  // the largest power of two that is not above M
+  for (int c = warp; c < ctas; c += kClWarps) {
+    for (int i = lane; i < sh.all_best[c]; i += 32) {
+      const unsigned long long mine = sh.best[c][i];
+      int lo[kClMaxCtas], n[kClMaxCtas];
+#pragma unroll
+      for (int o = 0; o < kClMaxCtas; ++o) {
+        lo[o] = 0;
+        n[o] = o < ctas && o != c ? sh.all_best[o] : 0;
+      }
+      for (int bit = ctas > 1 ? half : 0; bit > 0; bit >>= 1) {
+#pragma unroll
+        for (int o = 0; o < kClMaxCtas; ++o) {
+          const int at = lo[o] + bit;
+          const unsigned long long other = sh.best[o][min(at, kScoreMaxM) - 1];
+          lo[o] = (at <= n[o]) & (other > mine) ? at : lo[o];
+        }
+      }
+      int r = i;
+#pragma unroll
+      for (int o = 0; o < kClMaxCtas; ++o) r += lo[o];
+      if (r < A.M) score_emit_top(A, row, r, (uint32_t)(mine >> 32), (int)~(uint32_t)mine, m, rl.inv_t, sh.ls);
+    }
+  }
+  for (int i = total + tid; i < A.M; i += kClThreads) score_emit_no_top(A, row, i);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -612,13 +1003,6 @@ __device__ __forceinline__ void store_elem(char* rowp, long long t, float v) {
   else
     ((unsigned short*)rowp)[t] = (unsigned short)(pack_bf16x2(v, 0.f) & 0xffffu);
 }
-// x rounded down to bf16 (finite x well inside the range)
-__device__ __forceinline__ uint32_t bf16_floor_bits(float x) {
-  uint32_t b = __float_as_uint(x);
-  if (b & 0x80000000u) b += 0xffffu;
-  return b >> 16;
-}
-
 // Constants of a row: the gradient at logit x is p (a + b t) with p = 2^t, t = (x - xr) c2 + k.
 // xr = lse T as a float; the difference x - xr is taken first and k holds what xr rounded away, so
 // that t is good to 2^-23 of its own size however large the logits are.

@@ -55,77 +55,59 @@ static int temps_ok(float inv_temp, const float* per_draft, int K, float* out) {
   return GLS_OK;
 }
 
-struct ScorePlan {
-  int splits, steps;
-  size_t off_cand, total;
-};
-// Slices per row: the fewest for which the last round of warps wastes at most 15 % of the machine, or
-// that give every resident warp 12 items; slices of four steps and more unless the rows are so few
-// that one step each still leaves warps idle.  `rows` is the number of rows expected to be read.
-static ScorePlan score_plan(long long rows, long long alloc_rows, long long V, int dtype, int M) {
-  ScorePlan p;
+// Which kernel scores `rows` rows of V tokens: 0, a warp per row; c > 0, a cluster of c CTAs per row.
+// The times (us) are a fit to both kernels measured over 1 .. 8192 rows of 4000 .. 152064 tokens; a step
+// is 4 KB of a row, read by one warp.  E.g. 1 row of 152064 bf16 tokens: 56 us by a warp, 24 / 19 / 16 /
+// 15 us by 1 / 2 / 4 / 8 CTAs; 600 of 128256: 66 by a warp, 58 / 65 / 86 / 140 by CTAs; 1000 of 8000:
+// 15 by a warp, 28 / 55 / 97 / 182; 8192 of 152064: 437 by a warp, 510 / 714 by 1 / 2 CTAs.
+static int score_ctas(long long rows, long long V, int dtype) {
   const int step = dtype == GLS_BF16 ? ScoreCfg<kBF16>::kStep : ScoreCfg<kF32>::kStep;
-  const long long steps = (V + 15 + step - 1) / step;  // a row may start up to 15 elements past a boundary
-  const long long grid = (long long)sm_count() * kScoreCtasPerSM;
-  long long most = (steps + 3) / 4;
-  if (rows * most < 2 * grid) most = steps;
-  if (M > 0 && most > kScoreMaxCand / M) most = kScoreMaxCand / M;
-  long long splits = 1;
-  for (; splits < most; ++splits) {
-    const long long items = rows * splits;
-    if (items >= 12 * grid) break;
-    const long long rounds = (items + grid - 1) / grid;
-    if (items >= grid && (double)(rounds * grid - items) <= 0.15 * (double)(rounds * grid)) break;
+  const double steps = (double)((V + 15 + step - 1) / step);  // a row may start 15 elements past a boundary
+  const double warps = (double)sm_count() * kScoreCtasPerSM, slots = (double)sm_count() * kClCtasPerSM;
+  const double load = (double)rows / warps;
+  double least = 8.0 + steps * std::fmax(0.72 + std::fmin(load, 1.0), 1.71 * load);
+  int best = 0;
+  for (int c = 1; c <= kClMaxCtas; c *= 2) {
+    const double waves = (double)rows * c / slots, each = std::ceil(steps / (c * kClWarps));
+    const double t = (waves <= 1.0 ? 1.0 : waves + 0.5) * (10.0 + each * (0.55 + 0.9 * std::fmin(waves, 1.0)));
+    if (t < least) {
+      least = t;
+      best = c;
+    }
   }
-  p.steps = (int)((steps + splits - 1) / splits);
-  p.splits = (int)((steps + p.steps - 1) / p.steps);
-  p.off_cand = p.splits > 1 ? up256((size_t)alloc_rows * p.splits * sizeof(ScorePart)) : 0;
-  p.total = p.splits > 1 ? p.off_cand + up256((size_t)alloc_rows * p.splits * M * 8) : 0;
-  return p;
+  return best;
 }
-// Rows an emitted call reads: at least one per sequence and at most J; sequences stop early as a
-// rule, so the slices are cut for two each.
-static long long emitted_rows(int B, int J) { return (long long)B * (J < 2 ? J : 2); }
 
 template <int DT, bool ENT>
-static cudaError_t launch_score(const ScoreArgs& A, cudaStream_t st) {
-  const long long items = A.rows * A.splits;
-  const long long cap = (long long)sm_count() * kScoreCtasPerSM;
-  const size_t smem = A.M > 0 ? sizeof(TopmWarpBuf) : 0;
-  score_kernel<DT, ENT><<<(int)(items < cap ? items : cap), 32, smem, st>>>(A);
-  cudaError_t err = cudaGetLastError();
-  if (err != cudaSuccess || A.splits == 1) return err;
+static cudaError_t launch_score(const ScoreArgs& A, int ctas, cudaStream_t st) {
+  if (ctas == 0) {
+    const long long cap = (long long)sm_count() * kScoreCtasPerSM;
+    const size_t smem = A.M > 0 ? sizeof(RowShared) : 0;
+    score_rows_kernel<DT, ENT><<<(unsigned)(A.rows < cap ? A.rows : cap), 32, smem, st>>>(A);
+    return cudaGetLastError();
+  }
   cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)ctas;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  const long long mcap = (long long)sm_count() * 8;
-  cfg.gridDim = dim3((unsigned)(A.rows < mcap ? A.rows : mcap));
-  cfg.blockDim = dim3(kScoreMergeThreads);
-  int p2 = 32;
-  while (p2 < A.splits * A.M) p2 <<= 1;
-  cfg.dynamicSmemBytes = A.M > 0 ? (size_t)p2 * 8 : 0;
+  cfg.gridDim = dim3((unsigned)(A.rows * ctas));
+  cfg.blockDim = dim3(kClThreads);
+  cfg.dynamicSmemBytes = sizeof(ClusterShared);
   cfg.stream = st;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, score_merge_kernel<DT>, A);
+  return cudaLaunchKernelEx(&cfg, score_cluster_kernel<DT, ENT>, A, ctas);
 }
 
-static int run_score(ScoreArgs& A, const gls_rows_t* rows, const ScorePlan& P, void* workspace,
-                     size_t workspace_bytes, cudaStream_t st) {
-  if (P.total > 0 && (!workspace || workspace_bytes < P.total)) return GLS_ERR_WORKSPACE;
-  if (P.total > 0 && (uintptr_t)workspace % 16) return GLS_ERR_MISALIGNED;
+static int run_score(ScoreArgs& A, const gls_rows_t* rows, int ctas, cudaStream_t st) {
   A.data = rows->data;
   A.sb = rows->stride_b;
   A.sk = rows->stride_k;
   A.sj = rows->stride_j;
-  A.splits = P.splits;
-  A.steps_per_slice = P.steps;
-  A.parts = (ScorePart*)workspace;
-  A.cand = (unsigned long long*)((char*)workspace + P.off_cand);
   const bool bf = rows->dtype == GLS_BF16, ent = A.out_ent != nullptr;
-  const cudaError_t err = bf ? (ent ? launch_score<kBF16, true>(A, st) : launch_score<kBF16, false>(A, st))
-                             : (ent ? launch_score<kF32, true>(A, st) : launch_score<kF32, false>(A, st));
+  const cudaError_t err = bf ? (ent ? launch_score<kBF16, true>(A, ctas, st) : launch_score<kBF16, false>(A, ctas, st))
+                             : (ent ? launch_score<kF32, true>(A, ctas, st) : launch_score<kF32, false>(A, ctas, st));
   return err == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
 }
 
@@ -147,23 +129,11 @@ int token_ops_bounds(uint32_t out[4]) {
 
 extern "C" {
 
-size_t gls_token_logprobs_workspace_bytes(int B, int K, int J, int64_t V, int M) {
-  if (!score_sizes_ok(B, K, J, V) || M < 0 || M > kScoreMaxM) return 0;
-  size_t need = 16;
-  for (int dt = 0; dt < 2; ++dt) {
-    const size_t t = score_plan((long long)B * K * J, (long long)B * K * J, V, dt, M).total;
-    const size_t e = score_plan(emitted_rows(B, J), (long long)B * J, V, dt, M).total;
-    if (t > need) need = t;
-    if (e > need) need = e;
-  }
-  return need;
-}
-
 int gls_token_logprobs(const gls_rows_t* logits, int B, int K, int J, int64_t V, float inv_temp,
                        const float* inv_temp_per_draft_host, const int32_t* tokens, int G, int M,
                        float* out_logprobs, float* out_lse, float* out_lse_tail, float* out_entropy,
-                       int32_t* out_top_ids, float* out_top_logprobs, void* workspace,
-                       size_t workspace_bytes, uint32_t* device_status, void* stream) {
+                       int32_t* out_top_ids, float* out_top_logprobs, uint32_t* device_status,
+                       void* stream) {
   if (!score_sizes_ok(B, K, J, V) || G < 0 || G > GLS_MAX_GIVEN || M < 0 || M > kScoreMaxM || !out_lse)
     return GLS_ERR_INVALID_ARG;
   if ((G > 0 && (!tokens || !out_logprobs)) || (M > 0 && (!out_top_ids || !out_top_logprobs)))
@@ -188,15 +158,13 @@ int gls_token_logprobs(const gls_rows_t* logits, int B, int K, int J, int64_t V,
   A.top_ids = out_top_ids;
   A.top_lp = out_top_logprobs;
   A.status = device_status;
-  return run_score(A, logits, score_plan(A.rows, A.rows, V, logits->dtype, M), workspace, workspace_bytes,
-                   (cudaStream_t)stream);
+  return run_score(A, logits, score_ctas(A.rows, V, logits->dtype), (cudaStream_t)stream);
 }
 
 int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, int64_t V, float inv_temp,
                          const int32_t* tokens, const uint8_t* accept, uint32_t flags, int M,
                          float* out_logprobs, float* out_lse, float* out_entropy, int32_t* out_top_ids,
-                         float* out_top_logprobs, void* workspace, size_t workspace_bytes,
-                         uint32_t* device_status, void* stream) {
+                         float* out_top_logprobs, uint32_t* device_status, void* stream) {
   if (flags & ~(GLS_NO_BONUS | GLS_COMBINE_ALL)) return GLS_ERR_INVALID_ARG;
   if (L < 0 || L >= (1 << 30)) return GLS_ERR_INVALID_ARG;
   const int J = L + ((flags & GLS_NO_BONUS) ? 0 : 1);
@@ -225,8 +193,9 @@ int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, i
   A.top_ids = out_top_ids;
   A.top_lp = out_top_logprobs;
   A.status = device_status;
-  return run_score(A, target_logits, score_plan(emitted_rows(B, J), A.rows, V, target_logits->dtype, M),
-                   workspace, workspace_bytes, (cudaStream_t)stream);
+  // at least one row per sequence is read and at most J; sequences stop early as a rule
+  return run_score(A, target_logits, score_ctas((long long)B * (J < 2 ? J : 2), V, target_logits->dtype),
+                   (cudaStream_t)stream);
 }
 
 int gls_token_logprobs_backward(const gls_rows_t* logits, int B, int K, int J, int64_t V, float inv_temp,

@@ -622,16 +622,14 @@ def test_two_streams_and_a_shared_workspace(gls):
     tk = [_skewed(7000, 900, i) for i in range(4)]
     wantg = [gls.embed_tokens_backward(go[i], tk[i], 900) for i in range(4)]
     torch.cuda.synchronize()
-    n = gls.token_logprobs_workspace_bytes(2, 2, 2, V, M)
     ne = gls.embed_tokens_backward_workspace_bytes(7000, 900, 64)
     streams = [torch.cuda.Stream() for _ in range(2)]
-    ws = [torch.full((n,), 0xA5, dtype=torch.uint8, device="cuda") for _ in range(2)]
     we = [torch.full((ne,), 0xA5, dtype=torch.uint8, device="cuda") for _ in range(2)]
     torch.cuda.synchronize()
     got, gotg = [None] * 4, [None] * 4
     for i in range(4):
         with torch.cuda.stream(streams[i % 2]):
-            got[i] = gls.token_logprobs(x[i], tok, top=M, workspace=ws[i % 2])
+            got[i] = gls.token_logprobs(x[i], tok, top=M)
             gotg[i] = gls.embed_tokens_backward(go[i], tk[i], 900, workspace=we[i % 2])
     torch.cuda.synchronize()
     for i in range(4):
@@ -651,8 +649,8 @@ def test_refusals_of_the_binding(gls):
            lambda: gls.token_logprobs(x.transpose(2, 3), tok),
            lambda: gls.token_logprobs(x, tok.expand(1, 2, 3).transpose(1, 2)),
            lambda: gls.token_logprobs(x, torch.zeros((1, 2, 3, 65), dtype=torch.int32, device="cuda")),
-           lambda: gls.token_logprobs(_logits((1, 1, 1, 90000), BF, 1), tok[:, :1, :1].contiguous(),
-                                      workspace=torch.empty(8, dtype=torch.uint8, device="cuda")),
+           lambda: gls.embed_tokens_backward(x[0, 0], tok.view(6)[:3], 9,
+                                             workspace=torch.empty(8, dtype=torch.uint8, device="cuda")),
            lambda: gls.emitted_logprobs(x, tok[:, 0].contiguous(), None),
            lambda: gls.token_logprobs_backward(x, tok, ok["lse"], grad_entropy=ok["lse"]),
            lambda: gls.token_logprobs_backward(x, tok, ok["lse"], grad_top_logprobs=ok["top_logprobs"]),

@@ -21,11 +21,11 @@ def _rows(dtype=1, data=P, sb=1000, sk=1000, sj=1000):
 
 def _logprobs(**kw):
     a = dict(rows=_rows(), B=2, K=2, J=2, V=1000, it=1.0, per=None, tokens=P, G=1, M=5, lp=P, lse=P, tail=None,
-             ent=P, ids=P, tlp=P, ws=P, n=1 << 30)
+             ent=P, ids=P, tlp=P)
     a.update(kw)
     return gls.load().gls_token_logprobs(C.byref(a["rows"]), a["B"], a["K"], a["J"], a["V"], a["it"], a["per"],
                                          a["tokens"], a["G"], a["M"], a["lp"], a["lse"], a["tail"], a["ent"],
-                                         a["ids"], a["tlp"], a["ws"], a["n"], None, None)
+                                         a["ids"], a["tlp"], None, None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -37,8 +37,6 @@ def _logprobs(**kw):
     (dict(it=float("inf")), INVALID), (dict(it=1e-30), UNSUPPORTED), (dict(it=1e30), UNSUPPORTED),
     (dict(rows=_rows(data=None)), INVALID), (dict(rows=_rows(dtype=2)), UNSUPPORTED),
     (dict(rows=_rows(data=P + 1)), MISALIGNED), (dict(rows=_rows(dtype=0, data=P + 2)), MISALIGNED),
-    (dict(V=100000, ws=None), WORKSPACE), (dict(V=100000, n=64), WORKSPACE),  # rows in several slices
-    (dict(V=100000, ws=P + 4), MISALIGNED),
 ])
 def test_logprobs_refusals(kw, status):
     assert _logprobs(**kw) == status
@@ -51,18 +49,17 @@ def test_logprobs_per_draft_temperatures_are_checked():
 
 def _emitted(**kw):
     a = dict(rows=_rows(), B=2, K=2, L=2, V=1000, it=1.0, tokens=P, accept=P, flags=0, M=5, lp=P, lse=P, ent=P,
-             ids=P, tlp=P, ws=P, n=1 << 30)
+             ids=P, tlp=P)
     a.update(kw)
     return gls.load().gls_emitted_logprobs(C.byref(a["rows"]), a["B"], a["K"], a["L"], a["V"], a["it"], a["tokens"],
                                            a["accept"], a["flags"], a["M"], a["lp"], a["lse"], a["ent"], a["ids"],
-                                           a["tlp"], a["ws"], a["n"], None, None)
+                                           a["tlp"], None, None)
 
 
 @pytest.mark.parametrize("kw,status", [
     (dict(L=-1), INVALID), (dict(L=0, flags=2), INVALID), (dict(tokens=None), INVALID),
     (dict(accept=None), INVALID), (dict(flags=4), INVALID), (dict(flags=64), INVALID), (dict(lp=None), INVALID),
     (dict(M=300), INVALID), (dict(K=65), INVALID), (dict(it=0.0), INVALID),
-    (dict(V=100000, n=16), WORKSPACE),
 ])
 def test_emitted_refusals(kw, status):
     assert _emitted(**kw) == status
@@ -131,10 +128,6 @@ def test_embed_backward_refusals(kw, status):
 
 
 def test_workspace_sizes():
-    assert gls.token_logprobs_workspace_bytes(1, 1, 1, 152064, 20) > 0
-    assert gls.token_logprobs_workspace_bytes(1, 65, 1, 152064, 20) == 0
-    assert gls.token_logprobs_workspace_bytes(1, 1, 1, 152064, 257) == 0
-    assert gls.token_logprobs_workspace_bytes(256, 8, 9, 152064, 256) < (1 << 30)
     small = gls.embed_tokens_backward_workspace_bytes(10, 100, 64)
     assert 0 < small < gls.embed_tokens_backward_workspace_bytes(100000, 100, 64)
     assert gls.embed_tokens_backward_workspace_bytes(10, 0, 64) == 0
