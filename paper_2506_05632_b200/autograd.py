@@ -67,10 +67,10 @@ def token_logprobs(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=None,
     Returns dict(logprobs, lse, entropy, top_ids, top_logprobs), the entropy only if wanted and the
     alternatives only for top > 0; see gls_token_logprobs in include/gls.h.  Differentiable in the
     logits (once; not during a graph capture, and not into given outputs)."""
+    if not (logits.requires_grad and torch.is_grad_enabled()):
+        return binding.token_logprobs_raw(logits, tokens, top, inv_temp, inv_temp_per_draft, want_entropy, status, out)
     kw = dict(inv_temp=inv_temp, inv_temp_per_draft=inv_temp_per_draft, want_entropy=want_entropy,
               status=status)
-    if not (logits.requires_grad and torch.is_grad_enabled()):
-        return binding.token_logprobs_raw(logits, tokens, top=top, out=out, **kw)
     if out is not None:
         raise binding.GlsError("given outputs can not carry a gradient: call under torch.no_grad()")
     names = ("logprobs", "lse", "entropy", "top_ids", "top_logprobs")
@@ -97,7 +97,7 @@ def embed_tokens(table, tokens, scale=1.0, status=None, out=None):
     below 0 gives zeros; see gls_embed_tokens in include/gls.h.  Differentiable in the table (once; not
     during a graph capture, and not into a given output)."""
     if not (table.requires_grad and torch.is_grad_enabled()):
-        return binding.embed_tokens_raw(table, tokens, scale=scale, status=status, out=out)
+        return binding.embed_tokens_raw(table, tokens, scale, status, out)
     if out is not None:
         raise binding.GlsError("a given output can not carry a gradient: call under torch.no_grad()")
     return _EmbedTokens.apply(table, tokens, float(scale), status)

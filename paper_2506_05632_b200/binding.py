@@ -624,23 +624,67 @@ def compress_gaussian(candidates, source, side_info, bins=None, s2_eta=0.5, s2_z
 
 
 # ---- operators next to the sampler: log probabilities, embedding lookup, their gradients ----------
+# A call on a few rows takes the GPU about 10 us, so the wrappers keep the host's share small: one check
+# per tensor, none of those made here, and the stream's handle without a Stream object.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda i: torch.cuda.current_stream(i).cuda_stream)
+_I32, _F32T, _BF16T, _U8 = torch.int32, torch.float32, torch.bfloat16, torch.uint8
+
+
+def _ready():
+    return _lib if _lib is not None else load()
+
+
+def _run(dev, fn, *args):
+    """fn(*args, stream) on device index dev and its current stream; GlsError unless it returns 0."""
+    if torch.cuda.current_device() == dev:
+        rc = fn(*args, _raw_stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, _raw_stream(dev))
+    if rc:
+        raise GlsError(status_string(rc))
+
+
+def _device(t, name):
+    dev = t.get_device()
+    if dev < 0:
+        raise GlsError("libgls takes device tensors; %s is not one" % name)
+    return dev
+
+
 def _vec(t, name, shape, dtype, dev):
-    """Pointer of a contiguous device tensor of this shape and type (None stays None)."""
+    """Pointer of a contiguous tensor of this shape and type on device dev (None stays None)."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise GlsError("%s must be a contiguous %s device tensor of shape %s" % (name, dtype, tuple(shape)))
-    if t.device != dev:
-        raise GlsError("%s is on %s, the call's other tensors on %s" % (name, t.device, dev))
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
+        raise GlsError("%s must be a contiguous %s tensor of shape %s on the device of the call's other "
+                       "tensors (%d)" % (name, dtype, tuple(shape), dev))
     return t.data_ptr()
 
 
-def _space(workspace, need, dev):
+def _rows4(t, name):
+    """gls_rows_t of a [B,K,J,V] tensor with contiguous rows."""
+    if t.dtype is _BF16T:
+        dt = BF16
+    elif t.dtype is _F32T:
+        dt = F32
+    else:
+        raise GlsError("%s must be float32 or bfloat16" % name)
+    st = t.stride()
+    if len(st) != 4 or (st[3] != 1 and t.shape[3] > 1):
+        raise GlsError("%s must be [B,K,J,V] with a contiguous token dimension" % name)
+    return _Rows(t.data_ptr(), dt, st[0], st[1], st[2])
+
+
+def _space(workspace, need, like):
+    """(pointer, bytes) of the workspace, made here if there is none."""
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    if not workspace.is_cuda or workspace.device != dev or not workspace.is_contiguous():
-        raise GlsError("workspace must be a contiguous tensor on %s" % dev)
-    return workspace, workspace.numel() * workspace.element_size()
+        workspace = torch.empty(need, dtype=_U8, device=like.device)
+        return workspace, workspace.data_ptr(), need
+    if workspace.get_device() != like.get_device() or not workspace.is_contiguous():
+        raise GlsError("workspace must be a contiguous tensor on the device of the call's other tensors")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def _temps(inv_temp_per_draft, K):
@@ -654,39 +698,47 @@ def _temps(inv_temp_per_draft, K):
 
 
 def _given(tokens, lead, dev):
-    """(tokens pointer, G, trailing shape) of int32 tokens [*lead] or [*lead, G]."""
+    """(pointer, G, shape) of int32 tokens [*lead] or [*lead, G]; none: shape [*lead, 0]."""
     if tokens is None:
-        return None, 0, (0,)
-    tail = tuple(tokens.shape[len(lead):])
-    if tuple(tokens.shape[:len(lead)]) != tuple(lead) or len(tail) > 1:
-        raise GlsError("tokens must have shape %s or that with one more dimension" % (tuple(lead),))
-    G = tail[0] if tail else 1
-    return _vec(tokens, "tokens", tokens.shape, torch.int32, dev), G, tail
+        return None, 0, lead + (0,)
+    shape = tokens.shape
+    if shape[:3] != lead or len(shape) > 4:
+        raise GlsError("tokens must have shape %s or that with one more dimension" % (lead,))
+    return _vec(tokens, "tokens", shape, _I32, dev), shape[3] if len(shape) == 4 else 1, shape
 
 
 def _top(top):
-    if not 0 <= int(top) <= 256:
+    top = int(top)
+    if not 0 <= top <= 256:
         raise GlsError("top must be between 0 and 256")
-    return int(top)
+    return top
 
 
-def _score_out(out, lead, tail, M, want_entropy, dev):
-    f = dict(dtype=torch.float32, device=dev)
+def _score_out(out, like, lead, given, M, want_entropy, dev):
+    """(outputs, their pointers: log probabilities, lse, lse's tail, entropy, ids, their log probabilities)"""
     if out is None:
-        out = dict(logprobs=torch.empty(tuple(lead) + tail, **f), lse=torch.empty(lead, **f))
+        pe = pi = pt = None
+        if given == lead and want_entropy:  # one allocation for three tensors of one shape
+            lp, lse, ent = torch.empty((3,) + lead, dtype=_F32T, device=like.device).unbind(0)
+        else:
+            lse = torch.empty(lead, dtype=_F32T, device=like.device)
+            lp = lse.new_empty(given)
+            ent = lse.new_empty(lead) if want_entropy else None
+        out = {"logprobs": lp, "lse": lse}
         if want_entropy:
-            out["entropy"] = torch.empty(lead, **f)
+            out["entropy"] = ent
+            pe = ent.data_ptr()
         if M:
-            out["top_ids"] = torch.empty(tuple(lead) + (M,), dtype=torch.int32, device=dev)
-            out["top_logprobs"] = torch.empty(tuple(lead) + (M,), **f)
-    p = [_vec(out["logprobs"], "out['logprobs']", tuple(lead) + tail, torch.float32, dev),
-         _vec(out["lse"], "out['lse']", lead, torch.float32, dev),
-         _vec(out.get("lse_tail"), "out['lse_tail']", lead, torch.float32, dev),
-         _vec(out.get("entropy"), "out['entropy']", lead, torch.float32, dev),
-         _vec(out["top_ids"], "out['top_ids']", tuple(lead) + (M,), torch.int32, dev) if M else None,
-         _vec(out["top_logprobs"], "out['top_logprobs']", tuple(lead) + (M,), torch.float32, dev)
-         if M else None]
-    return out, p
+            out["top_ids"] = ids = torch.empty(lead + (M,), dtype=_I32, device=like.device)
+            out["top_logprobs"] = tlp = lse.new_empty(lead + (M,))
+            pi, pt = ids.data_ptr(), tlp.data_ptr()
+        return out, lp.data_ptr(), lse.data_ptr(), None, pe, pi, pt
+    top = lead + (M,)
+    return (out, _vec(out["logprobs"], "out['logprobs']", given, _F32T, dev), _vec(out["lse"], "out['lse']", lead, _F32T, dev),
+            _vec(out.get("lse_tail"), "out['lse_tail']", lead, _F32T, dev),
+            _vec(out.get("entropy"), "out['entropy']", lead, _F32T, dev),
+            _vec(out["top_ids"], "out['top_ids']", top, _I32, dev) if M else None,
+            _vec(out["top_logprobs"], "out['top_logprobs']", top, _F32T, dev) if M else None)
 
 
 def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=None, want_entropy=True,
@@ -696,16 +748,15 @@ def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=N
     Returns dict(logprobs, lse [B,K,J], entropy [B,K,J], top_ids and top_logprobs [B,K,J,top]); entropy
     only if wanted, the alternatives only for top > 0.  Given `out`, its tensors are written (an
     'lse_tail' among them too).  No autograd: see token_logprobs."""
-    L = load()
+    dev = _device(logits, "logits")
+    rows = _rows4(logits, "logits")
     B, K, J, V = logits.shape
-    dev, M = logits.device, _top(top)
-    rows = _rows(logits, 3)
-    tp, G, tail = _given(tokens, (B, K, J), dev)
-    out, p = _score_out(out, (B, K, J), tail, M, want_entropy, dev)
+    lead, M = (B, K, J), _top(top)
+    tp, G, given = _given(tokens, lead, dev)
+    out, lp, lse, tail, ent, ids, tlp = _score_out(out, logits, lead, given, M, want_entropy, dev)
     keep, itk = _temps(inv_temp_per_draft, K)
-    with torch.cuda.device(dev):
-        _check(L.gls_token_logprobs(C.byref(rows), B, K, J, V, float(inv_temp), itk, tp, G, M, *p,
-                                    _vec(status, "status", (1,), torch.int32, dev), _stream()))
+    _run(dev, _ready().gls_token_logprobs, rows, B, K, J, V, inv_temp, itk, tp, G, M, lp, lse, tail, ent, ids, tlp,
+         _vec(status, "status", (1,), _I32, dev))
     return out
 
 
@@ -714,17 +765,16 @@ def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0
     """gls_emitted_logprobs: the target rows [B,K,J,V] of a verification with the tokens [B,J] and
     accept flags [B,K,L] it returned -> token_logprobs' dict over [B,J], zeros (alternatives -1) at and
     beyond tau."""
-    L_ = load()
+    dev = _device(target_logits, "target_logits")
+    rows = _rows4(target_logits, "target_logits")
     B, K, J, V = target_logits.shape
     L = J if (flags & NO_BONUS) else J - 1
-    dev, M = target_logits.device, _top(top)
-    rows = _rows(target_logits, 3)
-    tp = _vec(tokens, "tokens", (B, J), torch.int32, dev)
-    ap = _vec(accept, "accept", (B, K, L), torch.uint8, dev) if L > 0 else None
-    out, p = _score_out(out, (B, J), (), M, want_entropy, dev)
-    with torch.cuda.device(dev):
-        _check(L_.gls_emitted_logprobs(C.byref(rows), B, K, L, V, float(inv_temp), tp, ap, int(flags), M,
-                                       p[0], p[1], *p[3:], _vec(status, "status", (1,), torch.int32, dev), _stream()))
+    lead, M = (B, J), _top(top)
+    tp = _vec(tokens, "tokens", lead, _I32, dev)
+    ap = _vec(accept, "accept", (B, K, L), _U8, dev) if L > 0 else None
+    out, lp, lse, _, ent, ids, tlp = _score_out(out, target_logits, lead, lead, M, want_entropy, dev)
+    _run(dev, _ready().gls_emitted_logprobs, rows, B, K, L, V, inv_temp, tp, ap, flags, M, lp, lse, ent, ids, tlp,
+         _vec(status, "status", (1,), _I32, dev))
     return out
 
 
@@ -734,13 +784,12 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
                             grad_logits=None):
     """gls_token_logprobs_backward: the gradient with respect to the logits, [B,K,J,V] in their type,
     from token_logprobs' inputs and outputs and the gradients of its outputs (each may be None)."""
-    L = load()
-    B, K, J, V = logits.shape
-    dev = logits.device
+    dev = _device(logits, "logits")
+    rows = _rows4(logits, "logits")
+    shape = logits.shape
+    B, K, J, V = shape
     lead = (B, K, J)
-    rows = _rows(logits, 3)
-    tp, G, tail = _given(tokens, lead, dev)
-    M = 0 if top_ids is None else top_ids.shape[-1]
+    tp, G, given = _given(tokens, lead, dev)
     if grad_entropy is not None and entropy is None:
         raise GlsError("grad_entropy needs the forward call's entropy")
     if grad_top_logprobs is not None and top_ids is None:
@@ -748,60 +797,61 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
     if grad_logprobs is not None and tokens is None:
         raise GlsError("grad_logprobs needs the tokens")
     if grad_logits is None:
-        grad_logits = torch.empty(lead + (V,), dtype=logits.dtype, device=dev)
-    if tuple(grad_logits.shape) != lead + (V,) or grad_logits.dtype != logits.dtype or grad_logits.device != dev:
+        grad_logits = torch.empty(shape, dtype=logits.dtype, device=logits.device)
+    elif grad_logits.shape != shape or grad_logits.dtype is not logits.dtype or grad_logits.get_device() != dev:
         raise GlsError("grad_logits must have the logits' shape, type and device")
-    grows = _rows(grad_logits, 3)
-    f = torch.float32
+    M = 0 if top_ids is None else top_ids.shape[-1]
+    top = lead + (M,)
     keep, itk = _temps(inv_temp_per_draft, K)
-    args = [tp, G, _vec(top_ids, "top_ids", lead + (M,), torch.int32, dev), M, _vec(lse, "lse", lead, f, dev),
-            _vec(lse_tail, "lse_tail", lead, f, dev), _vec(entropy, "entropy", lead, f, dev),
-            _vec(grad_logprobs, "grad_logprobs", lead + tail, f, dev),
-            _vec(grad_lse, "grad_lse", lead, f, dev), _vec(grad_entropy, "grad_entropy", lead, f, dev),
-            _vec(grad_top_logprobs, "grad_top_logprobs", lead + (M,), f, dev)]
-    with torch.cuda.device(dev):
-        _check(L.gls_token_logprobs_backward(C.byref(rows), B, K, J, V, float(inv_temp), itk, *args,
-                                             C.byref(grows), _stream()))
+    _run(dev, _ready().gls_token_logprobs_backward, rows, B, K, J, V, inv_temp, itk, tp, G,
+         _vec(top_ids, "top_ids", top, _I32, dev), M, _vec(lse, "lse", lead, _F32T, dev),
+         _vec(lse_tail, "lse_tail", lead, _F32T, dev), _vec(entropy, "entropy", lead, _F32T, dev),
+         _vec(grad_logprobs, "grad_logprobs", given, _F32T, dev), _vec(grad_lse, "grad_lse", lead, _F32T, dev),
+         _vec(grad_entropy, "grad_entropy", lead, _F32T, dev),
+         _vec(grad_top_logprobs, "grad_top_logprobs", top, _F32T, dev), _rows4(grad_logits, "grad_logits"))
     return grad_logits
 
 
 def _matrix(t, name):
-    """(dtype code, row stride) of a 2-d device tensor with contiguous rows."""
-    if not t.is_cuda:
-        raise GlsError("libgls takes device tensors; there is no CPU path")
-    if t.dtype not in (torch.float32, torch.bfloat16):
+    """(dtype code, row stride) of a 2-d tensor with contiguous rows."""
+    if t.dtype is _BF16T:
+        dt = BF16
+    elif t.dtype is _F32T:
+        dt = F32
+    else:
         raise GlsError("%s must be float32 or bfloat16" % name)
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    st = t.stride()
+    if len(st) != 2 or (st[1] != 1 and t.shape[1] > 1):
         raise GlsError("%s must be a matrix with contiguous rows" % name)
-    return F32 if t.dtype == torch.float32 else BF16, t.stride(0)
+    return dt, st[0]
 
 
 def embed_tokens_raw(table, tokens, scale=1.0, status=None, out=None):
     """gls_embed_tokens: scale * table[tokens] for table [V,D] and int32 tokens of any shape ->
     [*tokens.shape, D]; a token below 0 gives zeros.  No autograd: see embed_tokens."""
-    L = load()
+    dev = _device(table, "table")
     dt, stride = _matrix(table, "table")
     V, D = table.shape
-    dev = table.device
-    tp = _vec(tokens, "tokens", tokens.shape, torch.int32, dev)
-    N = tokens.numel()
+    lead = tokens.shape
+    tp = _vec(tokens, "tokens", lead, _I32, dev)
+    N, ostride = tokens.numel(), D
     if out is None:
-        out = torch.empty(tuple(tokens.shape) + (D,), dtype=table.dtype, device=dev)
-    if tuple(out.shape) != tuple(tokens.shape) + (D,) or out.dtype != table.dtype or out.device != dev:
-        raise GlsError("out must have shape [*tokens.shape, D], the table's type and its device")
-    try:
-        flat = out.view(N, D)  # rows a constant stride apart
-    except RuntimeError:
-        raise GlsError("out's rows must be a constant stride apart") from None
-    _, ostride = _matrix(flat, "out")
-    with torch.cuda.device(dev):
-        _check(L.gls_embed_tokens(table.data_ptr(), dt, stride, V, D, tp, N, float(scale), out.data_ptr(),
-                                  ostride, _vec(status, "status", (1,), torch.int32, dev), _stream()))
+        out = torch.empty(lead + (D,), dtype=table.dtype, device=table.device)
+    else:
+        if out.shape != lead + (D,) or out.dtype is not table.dtype or out.get_device() != dev:
+            raise GlsError("out must have shape [*tokens.shape, D], the table's type and its device")
+        try:
+            flat = out.view(N, D)  # rows a constant stride apart
+        except RuntimeError:
+            raise GlsError("out's rows must be a constant stride apart") from None
+        _, ostride = _matrix(flat, "out")
+    _run(dev, _ready().gls_embed_tokens, table.data_ptr(), dt, stride, V, D, tp, N, scale, out.data_ptr(), ostride,
+         _vec(status, "status", (1,), _I32, dev))
     return out
 
 
 def embed_tokens_backward_workspace_bytes(N, V, D):
-    return int(load().gls_embed_tokens_backward_workspace_bytes(int(N), int(V), int(D)))
+    return int(_ready().gls_embed_tokens_backward_workspace_bytes(N, V, D))
 
 
 def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accumulate=False,
@@ -809,32 +859,24 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
     """gls_embed_tokens_backward: grad_out [*tokens.shape, D] -> the gradient of the table, [V,D] in
     grad_out's type unless grad_table (the same type, or float32) is given.  accumulate: added to
     grad_table, whose other rows are not touched."""
-    L = load()
-    if not grad_out.is_cuda:
-        raise GlsError("libgls takes device tensors; there is no CPU path")
-    N, D = tokens.numel(), grad_out.shape[-1]
-    dev = grad_out.device
-    if tuple(grad_out.shape) != tuple(tokens.shape) + (D,):
+    dev = _device(grad_out, "grad_out")
+    lead, shape = tokens.shape, grad_out.shape
+    N, D = tokens.numel(), shape[-1] if len(shape) else 0
+    if shape != lead + (D,):
         raise GlsError("grad_out must have shape [*tokens.shape, D]")
-    tp = _vec(tokens, "tokens", tokens.shape, torch.int32, dev)
-    try:
-        flat = grad_out.view(N, D)
-    except RuntimeError:
-        flat = grad_out.reshape(N, D)
-    if N and D > 1 and flat.stride(1) != 1 or N > 1 and flat.stride(0) < D:
+    tp = _vec(tokens, "tokens", lead, _I32, dev)
+    flat = grad_out if grad_out.dim() == 2 else grad_out.reshape(N, D)
+    if N and (D > 1 and flat.stride(1) != 1 or N > 1 and flat.stride(0) < D):
         flat = flat.contiguous()  # an expanded gradient
     dt, stride = _matrix(flat, "grad_out")
     if grad_table is None:
         if accumulate:
             raise GlsError("accumulate needs a grad_table to add to")
-        grad_table = torch.empty((int(V), D), dtype=grad_out.dtype, device=dev)
-    if tuple(grad_table.shape) != (int(V), D) or grad_table.device != dev:
+        grad_table = torch.empty((V, D), dtype=grad_out.dtype, device=grad_out.device)
+    elif grad_table.shape != (V, D) or grad_table.get_device() != dev:
         raise GlsError("grad_table must have shape [V, D] and be on grad_out's device")
     gdt, gstride = _matrix(grad_table, "grad_table")
-    ws, nbytes = _space(workspace, embed_tokens_backward_workspace_bytes(N, V, D), dev)
-    with torch.cuda.device(dev):
-        _check(L.gls_embed_tokens_backward(flat.data_ptr(), dt, stride, tp, N, int(V), D, float(scale),
-                                           grad_table.data_ptr(), gdt, gstride,
-                                           EMBED_ACCUMULATE if accumulate else 0, ws.data_ptr(), nbytes,
-                                           _vec(status, "status", (1,), torch.int32, dev), _stream()))
+    keep, ws, nbytes = _space(workspace, embed_tokens_backward_workspace_bytes(N, V, D), grad_out)
+    _run(dev, _ready().gls_embed_tokens_backward, flat.data_ptr(), dt, stride, tp, N, V, D, scale, grad_table.data_ptr(),
+         gdt, gstride, EMBED_ACCUMULATE if accumulate else 0, ws, nbytes, _vec(status, "status", (1,), _I32, dev))
     return grad_table

@@ -39,29 +39,42 @@ __device__ __forceinline__ uint32_t scale_word(uint32_t w, float s) {
 }
 
 constexpr int kEmbedThreads = 256;
-// 16 bytes per unit; rows of `per_row` units
+constexpr int kEmbedUnits = 4;  // per thread, requested together
+// Units of 16 bytes, `per_row` to a row; a CTA takes 1024 in a row.
 template <int DT>
-__global__ void __launch_bounds__(kEmbedThreads) embed_vec_kernel(const __grid_constant__ EmbedArgs A, int per_row) {
+__global__ void __launch_bounds__(kEmbedThreads) embed_vec_kernel(const __grid_constant__ EmbedArgs A, uint32_t per_row) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
   const long long n_units = A.N * per_row;
-  for (long long u = (long long)blockIdx.x * kEmbedThreads + threadIdx.x; u < n_units;
-       u += (long long)gridDim.x * kEmbedThreads) {
-    const long long n = u / per_row;
-    const long long c = (u - n * per_row) * 16;
-    const int t = __ldg(A.tokens + n);
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (t >= 0 && t < A.V) {
-      v = ld_global16(A.table + (long long)t * A.table_stride * ES + c);
-      if (A.scale != 1.0f) {
-        v.x = scale_word<DT>(v.x, A.scale);
-        v.y = scale_word<DT>(v.y, A.scale);
-        v.z = scale_word<DT>(v.z, A.scale);
-        v.w = scale_word<DT>(v.w, A.scale);
-      }
-    } else if (t >= A.V && c == 0 && A.status != nullptr) {
-      atomicOr(A.status, kDevBadToken);
+  for (long long u0 = (long long)blockIdx.x * (kEmbedThreads * kEmbedUnits) + threadIdx.x; u0 < n_units;
+       u0 += (long long)gridDim.x * (kEmbedThreads * kEmbedUnits)) {
+    uint4 v[kEmbedUnits];
+    char* to[kEmbedUnits];
+#pragma unroll
+    for (int j = 0; j < kEmbedUnits; ++j) {
+      const long long u = u0 + j * kEmbedThreads;
+      v[j] = make_uint4(0u, 0u, 0u, 0u);
+      to[j] = nullptr;
+      if (u >= n_units) continue;
+      const long long n = u < (1ll << 32) ? (long long)((uint32_t)u / per_row) : u / per_row;
+      const long long c = (u - n * per_row) * 16;
+      to[j] = A.out + n * A.out_stride * ES + c;
+      const int t = __ldg(A.tokens + n);
+      if (t >= 0 && t < A.V)
+        v[j] = ld_global16(A.table + (long long)t * A.table_stride * ES + c);
+      else if (t >= A.V && c == 0 && A.status != nullptr)
+        atomicOr(A.status, kDevBadToken);
     }
-    *(uint4*)(A.out + n * A.out_stride * ES + c) = v;
+#pragma unroll
+    for (int j = 0; j < kEmbedUnits; ++j) {
+      if (to[j] == nullptr) continue;
+      if (A.scale != 1.0f) {
+        v[j].x = scale_word<DT>(v[j].x, A.scale);
+        v[j].y = scale_word<DT>(v[j].y, A.scale);
+        v[j].z = scale_word<DT>(v[j].z, A.scale);
+        v[j].w = scale_word<DT>(v[j].w, A.scale);
+      }
+      *(uint4*)to[j] = v[j];
+    }
   }
 }
 // any alignment, any D
@@ -84,68 +97,131 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_any_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------------------------------
-// gradient: the sort.  Least significant digit first; a tile of kSortTile positions per CTA.
+// gradient: rows of tokens that do not occur.  For a large table these zeros are most of what the call
+// writes, and they depend on nothing but the tokens, so every launch below carries CTAs that write a
+// share of them while its other CTAs, few and waiting on one another's results, leave the memory
+// system idle.
+// ------------------------------------------------------------------------------------------
+struct ZeroArgs {
+  char* out;              // [V][D]
+  long long out_stride;   // elements
+  int V;
+  long long D;
+  int es, vec;            // bytes per element; 16-byte stores
+  const uint32_t* touched;  // bit per token, or NULL: look through the tokens
+  const int32_t* tokens;
+  int N;
+};
+constexpr int kZeroRows = 4096;  // rows per CTA at most where the tokens are looked through
+
+// Rows [first, last) of tokens that do not occur, by the calling CTA.
+__device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, long long last) {
+  __shared__ uint32_t here[kZeroRows / 32];
+  const bool look = Z.touched == nullptr;
+  if (look) {
+    for (int w = threadIdx.x; w < kZeroRows / 32; w += blockDim.x) here[w] = 0u;
+    __syncthreads();
+    for (int i = threadIdx.x; i < Z.N; i += blockDim.x) {
+      const long long r = (long long)__ldg(Z.tokens + i) - first;
+      if (r >= 0 && r < last - first) atomicOr(&here[r >> 5], 1u << (r & 31));
+    }
+    __syncthreads();
+  }
+  // rows side by side where one does not fill the CTA
+  const long long units = Z.vec ? Z.D * Z.es / 16 : Z.D;
+  const int side = units < blockDim.x ? (int)(blockDim.x / (unsigned)units) : 1;
+  const int mine = units < blockDim.x ? (int)(threadIdx.x / (unsigned)units) : 0;
+  const long long c0 = units < blockDim.x ? (long long)(threadIdx.x % (unsigned)units) : (long long)threadIdx.x;
+  if (mine >= side) return;
+  for (long long v = first + mine; v < last; v += side) {
+    const long long b = look ? v - first : v;
+    if (((look ? here[b >> 5] : __ldg(Z.touched + (b >> 5))) >> (b & 31)) & 1u) continue;
+    char* const row = Z.out + v * Z.out_stride * Z.es;
+    for (long long c = c0; c < units; c += blockDim.x) {
+      if (Z.vec) ((uint4*)row)[c] = make_uint4(0u, 0u, 0u, 0u);
+      else if (Z.es == 2) ((unsigned short*)row)[c] = 0;
+      else ((float*)row)[c] = 0.f;
+    }
+  }
+}
+// A launch's share: rows [first, last) over CTAs `from` and up, `each` rows per CTA.
+struct ZeroShare {
+  long long first, last;
+  int from, each;
+};
+__device__ __forceinline__ bool zero_share(const ZeroArgs& Z, const ZeroShare& h) {
+  if ((int)blockIdx.x < h.from) return false;
+  const long long a = h.first + (long long)(blockIdx.x - h.from) * h.each;
+  zero_rows(Z, a, min(h.last, a + h.each));
+  return true;
+}
+
+// ------------------------------------------------------------------------------------------
+// gradient: the sort.  Least significant digit first; a tile of positions per CTA.
 // cnt[pass][tile][digit] holds the tiles' digit counts of a pass; a pass places its keys from the
 // counts and counts the next pass's digits at the places they went to.  Tokens outside [0, V) get
 // the key V and end up behind the others.
 // ------------------------------------------------------------------------------------------
 constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortRounds = 8;                            // keys per lane
-constexpr int kSortTile = kSortThreads * kSortRounds;     // 4096
 constexpr int kSortMaxBits = 9;
 constexpr int kSortBins = 1 << kSortMaxBits;
+constexpr int kSortSmall = 4096;  // tokens that one CTA sorts by itself (8 keys per thread)
+// Keys per thread of a tile: 4 while the counts that every CTA adds up (tiles x 512) stay small.
+constexpr long long kSortShortTiles = 262144;
 
 struct SortArgs {
   const int32_t* tokens;
   int N, V, bits, passes, tiles;
   uint32_t* cnt;                  // [passes][tiles][kSortBins]
-  uint32_t* touched;              // [(V + 31) / 32] bits
+  uint32_t* touched;              // [(V + 31) / 32] bits, or NULL
   int32_t* key[2];                // ping, pong
   int32_t* pos[2];
   uint32_t* status;
+  ZeroArgs zero;
 };
 
-__device__ __forceinline__ int sort_key(const SortArgs& S, int i) {
-  const int t = __ldg(S.tokens + i);
-  return t >= 0 && t < S.V ? t : S.V;
-}
-
+template <int ROUNDS>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const __grid_constant__ SortArgs S) {
   __shared__ uint32_t h[kSortBins];
   for (int d = threadIdx.x; d < kSortBins; d += kSortThreads) h[d] = 0u;
   __syncthreads();
   const uint32_t mask = (1u << S.bits) - 1u;
-  const int i0 = blockIdx.x * kSortTile;
-  for (int r = 0; r < kSortRounds; ++r) {
+  const int i0 = blockIdx.x * (kSortThreads * ROUNDS);
+  int t[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
     const int i = i0 + r * kSortThreads + threadIdx.x;
-    if (i < S.N) {
-      const int t = __ldg(S.tokens + i);
-      const int key = t >= 0 && t < S.V ? t : S.V;
-      atomicAdd(&h[key & mask], 1u);
-      if (key < S.V) {
-        const uint32_t bit = 1u << (key & 31);
-        if (!(*(volatile uint32_t*)(S.touched + (key >> 5)) & bit)) atomicOr(S.touched + (key >> 5), bit);
-      } else if (t >= S.V && S.status != nullptr) {
-        atomicOr(S.status, kDevBadToken);
-      }
+    t[r] = i < S.N ? __ldg(S.tokens + i) : -1;
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = i0 + r * kSortThreads + threadIdx.x;
+    if (i >= S.N) continue;
+    const int key = t[r] >= 0 && t[r] < S.V ? t[r] : S.V;
+    atomicAdd(&h[key & mask], 1u);
+    if (key < S.V) {
+      if (S.touched != nullptr) atomicOr(S.touched + (key >> 5), 1u << (key & 31));
+    } else if (t[r] >= S.V && S.status != nullptr) {
+      atomicOr(S.status, kDevBadToken);
     }
   }
   __syncthreads();
   for (int d = threadIdx.x; d < kSortBins; d += kSortThreads) S.cnt[(long long)blockIdx.x * kSortBins + d] = h[d];
 }
 
-// Stable ranks of a tile's keys by digit: warp w owns 256 consecutive keys, in rounds of 32.
-// On return wc[w][d] is the number of keys with digit d before warp w in the tile and rank[r] the
-// number before this one in its warp.
-__device__ __forceinline__ void tile_ranks(const uint32_t (&digit)[kSortRounds], const bool (&valid)[kSortRounds],
-                                           int (&rank)[kSortRounds], uint16_t (*wc)[kSortBins]) {
+// Stable ranks of a tile's keys by digit: warp w owns 32 ROUNDS consecutive keys, 32 a round.  On
+// return wc[w][d] is the number of keys with digit d before warp w in the tile and rank[r] the number
+// before this one in its warp.
+template <int ROUNDS>
+__device__ __forceinline__ void tile_ranks(const uint32_t (&digit)[ROUNDS], const bool (&valid)[ROUNDS],
+                                           int (&rank)[ROUNDS], uint16_t (*wc)[kSortBins]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t lt = (1u << lane) - 1u;
-  for (int d = lane; d < kSortBins; d += 32) wc[warp][d] = 0;
+  for (int d = lane; d < kSortBins / 2; d += 32) ((uint32_t*)wc[warp])[d] = 0u;
   __syncwarp();
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     const uint32_t d = valid[r] ? digit[r] : 0xffffffffu;
     const unsigned peers = __match_any_sync(0xffffffffu, d);
     int before = 0;
@@ -194,75 +270,88 @@ __device__ __forceinline__ uint32_t cta_scan(uint32_t x, uint32_t* warp_sums) {
   return r;
 }
 
-__global__ void __launch_bounds__(kSortThreads) embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass) {
-  __shared__ uint16_t wc[kSortWarps][kSortBins];
+template <int ROUNDS>
+__global__ void __launch_bounds__(kSortThreads)
+embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroShare share) {
+  __shared__ __align__(16) uint16_t wc[kSortWarps][kSortBins];
   __shared__ uint32_t base[kSortBins];
   __shared__ uint32_t warp_sums[kSortWarps];
   static_assert(kSortBins == kSortThreads, "a thread per digit");
+  if (zero_share(S.zero, share)) return;
+  constexpr int kTile = kSortThreads * ROUNDS;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t mask = (1u << S.bits) - 1u;
   const int shift = pass * S.bits;
   const uint32_t* cnt = S.cnt + (long long)pass * S.tiles * kSortBins;
+  const int32_t* kin = S.key[(pass + 1) & 1];
+  const int32_t* pin = S.pos[(pass + 1) & 1];
+  int32_t* kout = S.key[pass & 1];
+  int32_t* pout = S.pos[pass & 1];
+  int key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
+  uint32_t digit[ROUNDS];
+  bool valid[ROUNDS];
+  const int i0 = blockIdx.x * kTile + warp * 32 * ROUNDS;
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const int i = i0 + r * 32 + lane;
+    valid[r] = i < S.N;
+    key[r] = pos[r] = 0;
+    if (valid[r]) {
+      if (pass == 0) {
+        const int t = __ldg(S.tokens + i);
+        key[r] = t >= 0 && t < S.V ? t : S.V;
+        pos[r] = i;
+      } else {
+        key[r] = __ldcg(kin + i);
+        pos[r] = __ldcg(pin + i);
+      }
+    }
+    digit[r] = ((uint32_t)key[r] >> shift) & mask;
+  }
   // where this tile's keys of digit d = threadIdx.x start
   uint32_t total = 0u, before = 0u;
+#pragma unroll 8
   for (int t = 0; t < S.tiles; ++t) {
     const uint32_t c = __ldcg(cnt + (long long)t * kSortBins + threadIdx.x);
     if (t < (int)blockIdx.x) before += c;
     total += c;
   }
   base[threadIdx.x] = cta_scan(total, warp_sums) + before;
-
-  const int32_t* kin = S.key[(pass + 1) & 1];
-  const int32_t* pin = S.pos[(pass + 1) & 1];
-  int32_t* kout = S.key[pass & 1];
-  int32_t* pout = S.pos[pass & 1];
-  int key[kSortRounds], pos[kSortRounds], rank[kSortRounds];
-  uint32_t digit[kSortRounds];
-  bool valid[kSortRounds];
-  const int i0 = blockIdx.x * kSortTile + warp * 32 * kSortRounds;
-#pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
-    const int i = i0 + r * 32 + lane;
-    valid[r] = i < S.N;
-    key[r] = pos[r] = 0;
-    if (valid[r]) {
-      key[r] = pass == 0 ? sort_key(S, i) : __ldcg(kin + i);
-      pos[r] = pass == 0 ? i : __ldcg(pin + i);
-    }
-    digit[r] = ((uint32_t)key[r] >> shift) & mask;
-  }
-  tile_ranks(digit, valid, rank, wc);
+  tile_ranks<ROUNDS>(digit, valid, rank, wc);
   uint32_t* next = pass + 1 < S.passes ? S.cnt + (long long)(pass + 1) * S.tiles * kSortBins : nullptr;
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     if (!valid[r]) continue;
     const uint32_t at = base[digit[r]] + wc[warp][digit[r]] + (uint32_t)rank[r];
     if (!GLS_IN_RANGE(at, 0, S.N, 70u)) continue;
     kout[at] = key[r];
     pout[at] = pos[r];
     if (next != nullptr)
-      atomicAdd(next + (long long)(at / kSortTile) * kSortBins + (((uint32_t)key[r] >> (shift + S.bits)) & mask), 1u);
+      atomicAdd(next + (long long)(at / kTile) * kSortBins + (((uint32_t)key[r] >> (shift + S.bits)) & mask), 1u);
   }
 }
 
-// At most kSortTile tokens: the whole sort in one CTA, through shared memory.
-__global__ void __launch_bounds__(kSortThreads) embed_sort_small_kernel(const __grid_constant__ SortArgs S) {
+// At most kSortSmall tokens: the whole sort in the first CTA, through shared memory; the others write
+// zeros.
+__global__ void __launch_bounds__(kSortThreads)
+embed_sort_small_kernel(const __grid_constant__ SortArgs S, int* counters, const ZeroShare share) {
+  constexpr int ROUNDS = kSortSmall / kSortThreads;
+  if (zero_share(S.zero, share)) return;
   extern __shared__ __align__(16) unsigned char score_smem[];
   uint16_t(*wc)[kSortBins] = (uint16_t(*)[kSortBins])score_smem;
   int32_t* skey = (int32_t*)(score_smem + sizeof(uint16_t) * kSortWarps * kSortBins);
-  uint16_t* spos = (uint16_t*)(skey + kSortTile);  // positions are below kSortTile
+  uint16_t* spos = (uint16_t*)(skey + kSortSmall);  // positions are below kSortSmall
   __shared__ uint32_t base[kSortBins];
   __shared__ uint32_t warp_sums[kSortWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t mask = (1u << S.bits) - 1u;
-  for (int w = threadIdx.x; w < (S.V + 31) / 32; w += kSortThreads) S.touched[w] = 0u;
-  __syncthreads();
-  int key[kSortRounds], pos[kSortRounds], rank[kSortRounds];
-  uint32_t digit[kSortRounds];
-  bool valid[kSortRounds];
-  const int i0 = warp * 32 * kSortRounds;
+  if (threadIdx.x < 2) counters[threadIdx.x] = 0;
+  int key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
+  uint32_t digit[ROUNDS];
+  bool valid[ROUNDS];
+  const int i0 = warp * 32 * ROUNDS;
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     const int i = i0 + r * 32 + lane;
     valid[r] = i < S.N;
     key[r] = 0;
@@ -270,40 +359,35 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_small_kernel(const __
     if (valid[r]) {
       const int t = __ldg(S.tokens + i);
       key[r] = t >= 0 && t < S.V ? t : S.V;
-      if (key[r] < S.V)
-        atomicOr(S.touched + (key[r] >> 5), 1u << (key[r] & 31));
-      else if (t >= S.V && S.status != nullptr)
-        atomicOr(S.status, kDevBadToken);
+      if (t >= S.V && S.status != nullptr) atomicOr(S.status, kDevBadToken);
     }
   }
   for (int pass = 0; pass < S.passes; ++pass) {
     const int shift = pass * S.bits;
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) digit[r] = ((uint32_t)key[r] >> shift) & mask;
-    tile_ranks(digit, valid, rank, wc);
-    // keys of each digit in the whole tile: those before the last warp plus the last warp's own
-    uint32_t* const hist = base;
-    hist[threadIdx.x] = 0u;
-    __syncthreads();
+    for (int r = 0; r < ROUNDS; ++r) digit[r] = ((uint32_t)key[r] >> shift) & mask;
+    base[threadIdx.x] = 0u;
+    tile_ranks<ROUNDS>(digit, valid, rank, wc);
+    // keys of each digit in the whole tile
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r)
-      if (valid[r]) atomicAdd(&hist[digit[r]], 1u);
+    for (int r = 0; r < ROUNDS; ++r)
+      if (valid[r]) atomicAdd(&base[digit[r]], 1u);
     __syncthreads();
-    const uint32_t total = hist[threadIdx.x];
+    const uint32_t total = base[threadIdx.x];
     const uint32_t start = cta_scan(total, warp_sums);
     base[threadIdx.x] = start;
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
       if (!valid[r]) continue;
       const uint32_t at = base[digit[r]] + wc[warp][digit[r]] + (uint32_t)rank[r];
-      if (!GLS_IN_RANGE(at, 0, kSortTile, 71u)) continue;
+      if (!GLS_IN_RANGE(at, 0, kSortSmall, 71u)) continue;
       skey[at] = key[r];
       spos[at] = (uint16_t)pos[r];
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < ROUNDS; ++r) {
       const int i = i0 + r * 32 + lane;
       if (valid[r]) {
         key[r] = skey[i];
@@ -315,7 +399,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_small_kernel(const __
   int32_t* kout = S.key[(S.passes - 1) & 1];
   int32_t* pout = S.pos[(S.passes - 1) & 1];
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < ROUNDS; ++r) {
     const int i = i0 + r * 32 + lane;
     if (valid[r]) {
       kout[i] = key[r];
@@ -334,18 +418,21 @@ struct EmbedGradArgs {
   long long out_stride;
   const int32_t* key;      // sorted tokens
   const int32_t* pos;      // their positions
-  const uint32_t* touched;
   float* partial;          // [2 * ranges][D]
+  int* counters;           // [2]: heads that go on for a few ranges, for many
+  int4* heads;             // [2][ranges]: range, token, ranges that go on with it (few)
   int N, V;
   long long D;
   int per_range, ranges, slabs, accumulate;
-  int zero_ctas;           // CTAs that write the rows of tokens that do not occur
   float scale;
+  ZeroArgs zero;
 };
 
+constexpr int kEgThreads = 256;
 constexpr int kEgCols = 8;       // columns per thread
 constexpr int kEgMaxRange = 64;  // sorted positions per range
 constexpr int kEgBatch = 4;      // rows in flight
+constexpr int kEgMany = 32;      // ranges from which a token's partials are shared out among warps
 
 // Columns of thread t in slab s: VEC: 8 neighbouring ones; otherwise every blockDim-th.
 template <bool VEC>
@@ -385,11 +472,18 @@ __device__ __forceinline__ float eg_get(const EgRow<DT, VEC>& r, int i) {
   else
     return __uint_as_float(r.w[i]);
 }
+template <int DTO>
+__device__ __forceinline__ void eg_write1(const EmbedGradArgs& A, int token, long long c, float sum) {
+  char* const row = A.out + (long long)token * A.out_stride * (DTO == kBF16 ? 2 : 4);
+  float v = sum * A.scale;
+  if (A.accumulate) v += DTO == kF32 ? ((const float*)row)[c] : __uint_as_float((uint32_t)((const unsigned short*)row)[c] << 16);
+  store_elem<DTO>(row, c, v);
+}
 template <int DTO, bool VEC>
 __device__ __forceinline__ void eg_store(const EmbedGradArgs& A, int token, int slab, const float (&acc)[kEgCols]) {
   constexpr int ES = DTO == kBF16 ? 2 : 4;
-  char* const row = A.out + (long long)token * A.out_stride * ES;
   if constexpr (VEC) {
+    char* const row = A.out + (long long)token * A.out_stride * ES;
     const long long c = eg_col<true>(slab, 0);
     if (c >= A.D) return;
     float v[kEgCols];
@@ -423,47 +517,34 @@ __device__ __forceinline__ void eg_store(const EmbedGradArgs& A, int token, int 
 #pragma unroll
     for (int i = 0; i < kEgCols; ++i) {
       const long long c = eg_col<false>(slab, i);
-      if (c >= A.D) continue;
-      float v = acc[i] * A.scale;
-      if (A.accumulate) v += DTO == kF32 ? ((const float*)row)[c] : __uint_as_float((uint32_t)((const unsigned short*)row)[c] << 16);
-      store_elem<DTO>(row, c, v);
+      if (c < A.D) eg_write1<DTO>(A, token, c, acc[i]);
     }
   }
 }
 template <bool VEC>
 __device__ __forceinline__ void eg_put(float* p, int slab, long long D, const float (&acc)[kEgCols]) {
+  if constexpr (VEC) {
+    const long long c = eg_col<true>(slab, 0);
+    if (c >= D) return;
+    *(float4*)(p + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    *(float4*)(p + c + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+  } else {
 #pragma unroll
-  for (int i = 0; i < kEgCols; ++i) {
-    const long long c = eg_col<VEC>(slab, i);
-    if (c < D) p[c] = acc[i];
+    for (int i = 0; i < kEgCols; ++i) {
+      const long long c = eg_col<false>(slab, i);
+      if (c < D) p[c] = acc[i];
+    }
   }
 }
 
 // CTAs [0, ranges * slabs): a range of sorted positions and a slab of columns each.  A token whose
 // positions all lie in the range is written; what a range has of a token that began before it goes
-// to the partial 2 r, of one that goes on behind it to 2 r + 1 (one that does both: 2 r).
-// The other CTAs write zeros to the rows of tokens that do not occur.
+// to the partial 2 r, of one that goes on behind it to 2 r + 1 (one that does both: 2 r), and a range
+// in which a token begins that goes on is listed.
 template <int DT, int DTO, bool VEC>
-__global__ void __launch_bounds__(256) embed_grad_kernel(const __grid_constant__ EmbedGradArgs A) {
+__global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_constant__ EmbedGradArgs A, const ZeroShare share) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
-  constexpr int ESO = DTO == kBF16 ? 2 : 4;
-  const long long n_sum = (long long)A.ranges * A.slabs;
-  if (blockIdx.x >= n_sum) {
-    const long long rows_each = ((long long)A.V + A.zero_ctas - 1) / A.zero_ctas;
-    const long long first = ((long long)blockIdx.x - n_sum) * rows_each;
-    const long long last = min((long long)A.V, first + rows_each);
-    for (long long v = first; v < last; ++v) {
-      if ((__ldg(A.touched + (v >> 5)) >> (v & 31)) & 1u) continue;
-      char* const row = A.out + v * A.out_stride * ESO;
-      if constexpr (VEC) {
-        for (long long c = (long long)threadIdx.x * 16; c < A.D * ESO; c += (long long)blockDim.x * 16)
-          *(uint4*)(row + c) = make_uint4(0u, 0u, 0u, 0u);
-      } else {
-        for (long long c = threadIdx.x; c < A.D; c += blockDim.x) store_elem<DTO>(row, c, 0.f);
-      }
-    }
-    return;
-  }
+  if (zero_share(A.zero, share)) return;
   __shared__ int sk[kEgMaxRange + 2], sp[kEgMaxRange];
   const int range = (int)(blockIdx.x / A.slabs), slab = (int)(blockIdx.x % A.slabs);
   const int i0 = range * A.per_range;
@@ -474,6 +555,20 @@ __global__ void __launch_bounds__(256) embed_grad_kernel(const __grid_constant__
     if (i >= 1 && i <= n) sp[i - 1] = __ldg(A.pos + at);
   }
   __syncthreads();
+  if (slab == 0 && sk[n] < A.V && sk[n] == sk[n + 1] && sk[0] != sk[n]) {
+    // how many ranges behind this one start with the token, up to kEgMany + 1
+    int go = 0;
+    for (int t0 = 0; t0 <= kEgMany; t0 += blockDim.x) {
+      const int t = t0 + threadIdx.x;
+      const long long at = (long long)i0 + (long long)(1 + t) * A.per_range;
+      go += __syncthreads_count(t <= kEgMany && at < A.N && __ldg(A.key + at) == sk[n]);
+    }
+    if (threadIdx.x == 0) {
+      const int many = go > kEgMany ? 1 : 0;
+      // in any order: heads do not meet
+      A.heads[(long long)many * A.ranges + atomicAdd(A.counters + many, 1)] = make_int4(range, sk[n], go, 0);
+    }
+  }
   float acc[kEgCols];
 #pragma unroll
   for (int i = 0; i < kEgCols; ++i) acc[i] = 0.f;
@@ -504,32 +599,77 @@ __global__ void __launch_bounds__(256) embed_grad_kernel(const __grid_constant__
   }
 }
 
-// Joins the partials of the token that begins in a range and goes on behind it.
-template <int DTO, bool VEC>
-__global__ void __launch_bounds__(256) embed_join_kernel(const __grid_constant__ EmbedGradArgs A) {
-  const int range = (int)(blockIdx.x / A.slabs), slab = (int)(blockIdx.x % A.slabs);
-  const int i1 = (range + 1) * A.per_range;  // first position behind the range
-  if (i1 >= A.N) return;
-  const int key = __ldg(A.key + i1 - 1);
-  if (key >= A.V || __ldg(A.key + i1) != key) return;
-  const int i0 = range * A.per_range;
-  if (i0 > 0 && __ldg(A.key + i0 - 1) == key) return;  // it began before: an earlier range joins it
-  float acc[kEgCols];
-#pragma unroll
-  for (int i = 0; i < kEgCols; ++i) {
-    const long long c = eg_col<VEC>(slab, i);
-    acc[i] = c < A.D ? A.partial[(2ll * range + 1) * A.D + c] : 0.f;
+// Joins the partials of the tokens that begin in a listed range and go on behind it: partial 2 r + 1
+// of that range, then 2 r of each range after it that starts with the token.  Work items: for heads of
+// a few ranges (head, W columns per thread); for heads of many (head, W columns per lane), whose
+// ranges the CTA's eight warps share out, each adding its own in order.
+template <int W>
+struct EgVec {
+  float v[W];
+};
+template <int W>
+__device__ __forceinline__ EgVec<W> eg_partial(const float* p, bool on) {
+  EgVec<W> r;
+  if constexpr (W == 4) {
+    const float4 x = on ? *(const float4*)p : make_float4(0.f, 0.f, 0.f, 0.f);
+    r.v[0] = x.x, r.v[1] = x.y, r.v[2] = x.z, r.v[3] = x.w;
+  } else {
+    r.v[0] = on ? *p : 0.f;
   }
-  for (int r = range + 1; r < A.ranges; ++r) {
-#pragma unroll
-    for (int i = 0; i < kEgCols; ++i) {
-      const long long c = eg_col<VEC>(slab, i);
-      if (c < A.D) acc[i] += A.partial[2ll * r * A.D + c];
+  return r;
+}
+template <int DTO, int W>
+__global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_constant__ EmbedGradArgs A, const ZeroShare share) {
+  if (zero_share(A.zero, share)) return;
+  __shared__ float sums[kEgThreads][W];
+  constexpr int kWarps = kEgThreads / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t wide = (uint32_t)((A.D + W * kEgThreads - 1) / (W * kEgThreads)), narrow = (uint32_t)((A.D + W * 32 - 1) / (W * 32));
+  const long long n_few = (long long)A.counters[0] * wide, n_items = n_few + (long long)A.counters[1] * narrow;
+  for (long long it = blockIdx.x; it < n_items; it += share.from) {
+    const bool many = it >= n_few;
+    const long long i = many ? it - n_few : it;
+    const uint32_t tiles = many ? narrow : wide;
+    const int head = (int)(i / tiles);
+    const long long c = ((i - (long long)head * tiles) * (many ? 32 : kEgThreads) + (many ? lane : (int)threadIdx.x)) * W;
+    const int4 h = A.heads[(many ? A.ranges : 0) + head];
+    int go = h.z;
+    if (many) {
+      for (;;) {
+        const long long at = ((long long)h.x + 1 + go + threadIdx.x) * A.per_range;
+        const int more = __syncthreads_count(at < A.N && __ldg(A.key + at) == h.y);
+        go += more;
+        if (more < kEgThreads) break;
+      }
     }
-    const int next = (r + 1) * A.per_range;
-    if (next >= A.N || __ldg(A.key + next) != key) break;
+    const bool on = c < A.D;
+    const int from = many ? warp : 0, step = many ? kWarps : 1;
+    EgVec<W> acc = eg_partial<W>(A.partial + (2ll * h.x + 1) * A.D + c, on && from == 0);
+    const float* const p = A.partial + 2ll * (h.x + 1) * A.D + c;
+    for (int r = from; r < go; r += 8 * step) {
+      EgVec<W> x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = eg_partial<W>(p + 2ll * (r + q * step) * A.D, on && r + q * step < go);
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+#pragma unroll
+        for (int e = 0; e < W; ++e) acc.v[e] += x[q].v[e];
+    }
+    if (many) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) sums[threadIdx.x][e] = acc.v[e];
+      __syncthreads();
+      if (warp == 0)
+        for (int w = 1; w < kWarps; ++w)
+#pragma unroll
+          for (int e = 0; e < W; ++e) acc.v[e] += sums[w * 32 + lane][e];
+      __syncthreads();
+    }
+    if (on && (!many || warp == 0)) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) eg_write1<DTO>(A, h.y, c + e, acc.v[e]);
+    }
   }
-  eg_store<DTO, VEC>(A, key, slab, acc);
 }
 
 }  // namespace gls

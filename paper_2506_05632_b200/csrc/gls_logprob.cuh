@@ -969,7 +969,7 @@ struct ScoreGradArgs {
   long long gb, gk, gj;
   int K, J, V, M, G;
   long long rows;
-  int chunks;              // chunks per row
+  int chunks, iters;       // chunks per row; a chunk is iters times 64 bytes per thread
   const int32_t* tokens;   // [rows][G]
   const int32_t* top_ids;  // [rows][M]
   const float* lse;        // [rows]
@@ -979,12 +979,12 @@ struct ScoreGradArgs {
   const float* g_lse;      // NULL or [rows]
   const float* g_ent;      // NULL or [rows]
   const float* g_top;      // NULL or [rows][M]
-  float inv_t[kMaxK];
+  float inv_t[kMaxK], temp[kMaxK];  // 1 / T and T
 };
 
 constexpr int kGradThreads = 256;
-constexpr int kGradVecs = 4;  // 32-byte vectors per thread and chunk
-constexpr int kGradMaxEntries = kScoreMaxG + kScoreMaxM;
+constexpr int kGradVecs = 2;      // 32-byte vectors per thread, requested together
+constexpr int kGradCtasPerSM = 4;
 
 __device__ __forceinline__ void st_stream32(void* p, const Words8& v) {
   asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(v.w[0]),
@@ -1075,128 +1075,155 @@ __device__ __forceinline__ void grad_vec(Words8& w, const GradRow& r, float xlow
   }
 }
 
-// A CTA takes chunks of rows in turn: reads the chunk, forms the row's constants while the loads are
-// in flight, writes the gradients, then writes the given tokens' own elements again with their
+// The given tokens and alternatives of a row, one after the other.
+struct GradEntry {
+  int t;
+  float g;
+};
+__device__ __forceinline__ GradEntry grad_entry(const ScoreGradArgs& A, long long row, int n_lp, int e) {
+  GradEntry r;
+  if (e < n_lp) {
+    r.t = __ldg(A.tokens + row * A.G + e);
+    r.g = __ldg(A.g_lp + row * A.G + e);
+  } else {
+    r.t = __ldg(A.top_ids + row * A.M + (e - n_lp));
+    r.g = __ldg(A.g_top + row * A.M + (e - n_lp));
+  }
+  return r;
+}
+
+// A CTA takes chunks of rows in turn.  Each warp forms the row's constants for itself while its first
+// loads are in flight (no barrier: waiting for one thread's constants took half of the kernel's time),
+// writes its gradients, and the thread that wrote a given token's element writes it again with the
 // extra term (added in fp32 before the one rounding; a token given twice is written once, with the
 // sum taken in the order given).
 template <int DT, bool ENT>
-__global__ void __launch_bounds__(kGradThreads) score_grad_kernel(const __grid_constant__ ScoreGradArgs A) {
+__global__ void __launch_bounds__(kGradThreads, kGradCtasPerSM) score_grad_kernel(const __grid_constant__ ScoreGradArgs A) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
-  constexpr int EV = 32 / ES;                            // elements per vector
-  constexpr int kChunk = kGradThreads * kGradVecs * EV;  // elements per chunk
-  __shared__ int e_tok[kGradMaxEntries];
-  __shared__ float e_g[kGradMaxEntries], e_x[kGradMaxEntries];
-  __shared__ GradRow sh_row;
-  const int tid = threadIdx.x;
+  constexpr int EV = 32 / ES;                           // elements per vector
+  constexpr int kTurn = kGradThreads * kGradVecs * EV;  // elements per turn of the CTA
+  const int tid = threadIdx.x, lane = tid & 31;
   const long long n_items = A.rows * A.chunks;
   const int n_lp = A.g_lp != nullptr ? A.G : 0;
   const int n_e = n_lp + (A.g_top != nullptr ? A.M : 0);
   for (long long it = blockIdx.x; it < n_items; it += gridDim.x) {
-    const long long row = it / A.chunks;
-    const int chunk = (int)(it % A.chunks);
-    const int j = (int)(row % A.J);
-    const long long bk = row / A.J;
-    const int k = (int)(bk % A.K);
-    const long long b = bk / A.K;
-    const char* rowp = (const char*)A.data + (b * A.sb + k * A.sk + j * A.sj) * ES;
-    char* outp = (char*)A.grad + (b * A.gb + k * A.gk + j * A.gj) * ES;
+    const uint32_t row = n_items < (1ll << 32) ? (uint32_t)it / (uint32_t)A.chunks : (uint32_t)(it / A.chunks);
+    const int chunk = (int)(it - (long long)row * A.chunks);
+    const uint32_t bk = row / (uint32_t)A.J, b = bk / (uint32_t)A.K;
+    const int j = (int)(row - bk * (uint32_t)A.J), k = (int)(bk - b * (uint32_t)A.K);
+    const char* const rowp = (const char*)A.data + (b * A.sb + k * A.sk + j * A.sj) * ES;
+    char* const outp = (char*)A.grad + (b * A.gb + k * A.gk + j * A.gj) * ES;
     const int mis = (int)((uintptr_t)rowp & 31) / ES;
     const bool same = ((uintptr_t)rowp & 31) == ((uintptr_t)outp & 31);
     const int end = mis + A.V;
-    const long long v0 = (long long)chunk * kChunk;
+    const long long first = (long long)chunk * A.iters * kTurn + tid * EV;  // this thread's first vector
 
     Words8 w[kGradVecs];
+    auto load = [&](long long v0) {
 #pragma unroll
-    for (int q = 0; q < kGradVecs; ++q) {
-      const long long v = v0 + (q * kGradThreads + tid) * EV;
-      if (v >= mis && v + EV <= end) w[q] = ld_stream32(rowp + (v - mis) * ES);
-    }
-    for (int e = tid; e < n_e; e += kGradThreads) {
-      const int t = e < n_lp ? __ldg(A.tokens + row * A.G + e) : __ldg(A.top_ids + row * A.M + (e - n_lp));
-      e_tok[e] = t;
-      e_g[e] = e < n_lp ? __ldg(A.g_lp + row * A.G + e) : __ldg(A.g_top + row * A.M + (e - n_lp));
-      e_x[e] = t >= 0 && t < A.V ? load_logit<DT>(rowp, t) : -CUDART_INF_F;
-    }
-    __syncthreads();
-    if (tid < 32) {
-      double a = 0.0;
-      for (int e = tid; e < n_e; e += 32)
-        if (fabsf(e_x[e]) < CUDART_INF_F) a -= (double)e_g[e];
+      for (int q = 0; q < kGradVecs; ++q) {
+        const long long v = v0 + q * (kGradThreads * EV);
+        if (v >= mis && v + EV <= end) w[q] = ld_stream32(rowp + (v - mis) * ES);
+      }
+    };
+    load(first);
+
+    // ---- the row's constants -----------------------------------------------------------------------
+    GradRow r;
+    r.inv_t = A.inv_t[k];
+    r.c2 = r.inv_t * kLog2e;
+    {
+      const float lse = __ldg(A.lse + row);
+      const float tail = A.tail != nullptr ? __ldg(A.tail + row) : 0.f;
+      float gh = 0.f, h = 0.f;
+      if (ENT) {
+        gh = __ldg(A.g_ent + row);
+        h = __ldg(A.ent + row);
+      }
+      float a = A.g_lse != nullptr ? __ldg(A.g_lse + row) : 0.f;
+      if (n_e > 0) {
+        double sum = 0.0;
+        for (int e = lane; e < n_e; e += 32) {
+          const GradEntry ge = grad_entry(A, row, n_lp, e);
+          if (ge.t >= 0 && ge.t < A.V && fabsf(load_logit<DT>(rowp, ge.t)) < CUDART_INF_F) sum += (double)ge.g;
+        }
+        if (n_e > 1) {
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
-      if (tid == 0) {
-        const double inv_t = (double)A.inv_t[k];
-        const float lse = __ldg(A.lse + row);
-        const double tail = A.tail != nullptr ? (double)__ldg(A.tail + row) : 0.0;
-        const double kLog2eD = 1.4426950408889634074;
-        GradRow r;
-        r.inv_t = A.inv_t[k];
-        r.c2 = A.inv_t[k] * kLog2e;
-        if (A.g_lse != nullptr) a += (double)__ldg(A.g_lse + row);
-        double gb = 0.0;
-        if (ENT) {
-          const double gh = (double)__ldg(A.g_ent + row);
-          a -= gh * (double)__ldg(A.ent + row);
-          gb = -gh * 0.69314718055994530942;  // ln p = t ln 2
+          for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        } else {
+          sum = __shfl_sync(0xffffffffu, sum, 0);
         }
-        r.a = (float)(a * inv_t);
-        r.b = (float)(gb * inv_t);
-        r.xr = (float)((double)lse / inv_t);
-        if (fabsf(lse) < CUDART_INF_F && fabsf(r.xr) < CUDART_INF_F) {
-          r.k = (float)((((double)r.xr * inv_t - (double)lse) - tail) * kLog2eD);
-          r.careful = fabsf(r.xr) >= 1e30f;
-        } else {  // a row without a finite logit has no gradient
-          r.xr = r.a = r.b = 0.f;
-          r.k = -CUDART_INF_F;
-          r.careful = 2;
-        }
-        sh_row = r;
+        a = (float)((double)a - sum);
+      }
+      if (ENT) a = fmaf(-gh, h, a);
+      r.a = a * r.inv_t;
+      r.b = ENT ? -gh * (0.69314718056f * r.inv_t) : 0.f;  // ln p = t ln 2
+      r.xr = lse * A.temp[k];
+      if (fabsf(lse) < CUDART_INF_F && fabsf(r.xr) < CUDART_INF_F) {
+        r.k = (float)((((double)r.xr * (double)r.inv_t - (double)lse) - (double)tail) * 1.4426950408889634074);
+        r.careful = fabsf(r.xr) >= 1e30f;
+      } else {  // a row without a finite logit has no gradient
+        r.xr = r.a = r.b = 0.f;
+        r.k = -CUDART_INF_F;
+        r.careful = 2;
       }
     }
-    __syncthreads();
-    const GradRow r = sh_row;
     const float xlow = r.xr - 200.0f / r.c2;
+
+    for (int i = 0; i < A.iters; ++i) {
+      const long long v0 = first + (long long)i * kTurn;
+      if (v0 - lane * EV >= end) break;
+      if (i > 0) load(v0);
 #pragma unroll
-    for (int q = 0; q < kGradVecs; ++q) {
-      const long long v = v0 + (q * kGradThreads + tid) * EV;
-      if (v >= mis && v + EV <= end) {
-        grad_vec<DT, ENT>(w[q], r, xlow);
-        char* const o = outp + (v - mis) * ES;
-        if (same) {
-          st_stream32(o, w[q]);
-        } else {
+      for (int q = 0; q < kGradVecs; ++q) {
+        const long long v = v0 + q * (kGradThreads * EV);
+        if (v >= mis && v + EV <= end) {
+          grad_vec<DT, ENT>(w[q], r, xlow);
+          char* const o = outp + (v - mis) * ES;
+          if (same) {
+            st_stream32(o, w[q]);
+          } else {
 #pragma unroll
-          for (int t = 0; t < EV; ++t) {
-            if (DT == kF32)
-              ((float*)o)[t] = __uint_as_float(w[q].w[t % 8]);
-            else
-              ((unsigned short*)o)[t] = (unsigned short)(w[q].w[t / 2] >> (16 * (t & 1)));
+            for (int t = 0; t < EV; ++t) {
+              if (DT == kF32)
+                ((float*)o)[t] = __uint_as_float(w[q].w[t % 8]);
+              else
+                ((unsigned short*)o)[t] = (unsigned short)(w[q].w[t / 2] >> (16 * (t & 1)));
+            }
           }
         }
-      } else if (v + EV > mis && v < end) {  // the vector that holds the row's first or last element
-        for (int t = 0; t < EV; ++t) {
-          const long long i = v + t - mis;
-          if (i >= 0 && i < A.V) store_elem<DT>(outp, i, grad_one<ENT>(r, load_logit<DT>(rowp, i)));
-        }
       }
     }
-    __syncthreads();  // the chunk is written
-    for (int e = tid; e < n_e; e += kGradThreads) {
-      const int t = e_tok[e];
-      const float x = e_x[e];
-      if (!(fabsf(x) < CUDART_INF_F) || r.careful == 2) continue;
-      const long long v = (long long)t + mis;
-      if (v < v0 || v >= v0 + kChunk) continue;
-      bool first = true;
+    // the vectors that stick out of the row at its ends: an element per thread
+    const long long c0 = (long long)chunk * A.iters * kTurn;
+    if (tid < EV) {
+      auto edge = [&](long long v) {
+        if (v >= mis && v < end) store_elem<DT>(outp, v - mis, grad_one<ENT>(r, load_logit<DT>(rowp, v - mis)));
+      };
+      const long long tail = (long long)end / EV * EV;  // starts the last vector when that is not full
+      if (chunk == 0 && (mis > 0 || end < EV)) edge(tid);
+      if (tail < end && tail > 0 && tail >= c0 && tail < c0 + (long long)A.iters * kTurn) edge(tail + tid);
+    }
+
+    // ---- the given tokens' own elements, by the threads that have just written them -----------------
+    for (int e = 0; e < n_e; ++e) {
+      const GradEntry ge = grad_entry(A, row, n_lp, e);
+      const long long v = (long long)ge.t + mis, vec = v / EV * EV;
+      if (ge.t < 0 || ge.t >= A.V || vec < c0 || vec >= c0 + (long long)A.iters * kTurn || r.careful == 2) continue;
+      const bool whole = vec >= mis && vec + EV <= end;
+      if ((whole ? (int)((vec - c0) / EV % kGradThreads) : (int)(v - vec)) != tid) continue;
+      const float x = load_logit<DT>(rowp, ge.t);
+      if (!(fabsf(x) < CUDART_INF_F)) continue;
       double g = 0.0;
+      bool given_before = false;
       for (int o = 0; o < n_e; ++o) {
-        if (e_tok[o] != t) continue;
-        if (o < e) first = false;
-        g += (double)e_g[o];
+        const GradEntry other = grad_entry(A, row, n_lp, o);
+        if (other.t != ge.t) continue;
+        if (o < e) given_before = true;
+        g += (double)other.g;
       }
-      if (first) store_elem<DT>(outp, t, fmaf((float)g, r.inv_t, grad_one<ENT>(r, x)));
+      if (!given_before) store_elem<DT>(outp, ge.t, fmaf((float)g, r.inv_t, grad_one<ENT>(r, x)));
     }
-    __syncthreads();  // the entries are free for the next chunk
   }
 }
 

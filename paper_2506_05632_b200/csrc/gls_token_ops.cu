@@ -244,8 +244,14 @@ int gls_token_logprobs_backward(const gls_rows_t* logits, int B, int K, int J, i
   A.g_ent = grad_entropy;
   A.g_top = M > 0 ? grad_top_logprobs : nullptr;
   const bool bf = logits->dtype == GLS_BF16;
-  const long long chunk = (long long)kGradThreads * kGradVecs * (bf ? 16 : 8);
-  A.chunks = (int)((V + 15 + chunk - 1) / chunk);
+  for (int k = 0; k < K; ++k) A.temp[k] = 1.0f / A.inv_t[k];
+  // chunks of up to 64 KB of a row, shorter where the rows do not fill the machine four times over
+  const long long turn = (long long)kGradThreads * kGradVecs * (bf ? 16 : 8), turns = (V + 15 + turn - 1) / turn;
+  const long long want = (long long)sm_count() * kGradCtasPerSM * 4;
+  long long iters = turns * A.rows / want;
+  iters = iters < 1 ? 1 : iters > 4 ? 4 : iters;
+  A.iters = (int)iters;
+  A.chunks = (int)((turns + iters - 1) / iters);
   const long long items = A.rows * A.chunks;
   const int grid = (int)(items < (1 << 20) ? items : (1 << 20));
   cudaStream_t st = (cudaStream_t)stream;
@@ -281,11 +287,12 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
   const bool vec = D * es % 16 == 0 && table_stride * es % 16 == 0 && out_stride * es % 16 == 0 &&
                    (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0;
   const long long units = vec ? N * (D * es / 16) : N * D;
-  const long long want = (units + kEmbedThreads - 1) / kEmbedThreads, cap = 1 << 20;
+  const long long per_cta = vec ? kEmbedThreads * kEmbedUnits : kEmbedThreads;
+  const long long want = (units + per_cta - 1) / per_cta, cap = 1 << 20;
   const int grid = (int)(want < cap ? want : cap);
   if (vec) {
-    if (dtype == GLS_BF16) embed_vec_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, (int)(D * es / 16));
-    else embed_vec_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, (int)(D * es / 16));
+    if (dtype == GLS_BF16) embed_vec_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, (uint32_t)(D * es / 16));
+    else embed_vec_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, (uint32_t)(D * es / 16));
   } else {
     if (dtype == GLS_BF16) embed_any_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A);
     else embed_any_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A);
@@ -298,21 +305,26 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
 namespace gls {
 
 struct EmbedGradPlan {
-  int bits, passes, tiles, per_range, ranges;
-  size_t off_key[2], off_pos[2], off_cnt, off_touched, off_partial, total;
-  size_t zero_from, zero_bytes;  // what has to be zero at the start (counts of later passes, touched)
+  int bits, passes, rounds, tiles, per_range, ranges;
+  bool small;                  // one CTA sorts, and the CTAs that write zeros look through the tokens
+  size_t off_key[2], off_pos[2], off_heads, off_cnt, off_touched, off_counters, off_partial, total;
+  size_t zero_from, zero_bytes;  // what has to be zero at the start (counts of later passes, touched, counters)
 };
 static bool embed_grad_sizes_ok(int64_t N, int64_t V, int64_t D) {
   return N >= 0 && N < (1LL << 30) && V > 0 && V < (1LL << 31) - 1 && D > 0 && D < (1LL << 31);
 }
+constexpr int kZeroCtas = 1184;  // CTAs that write zeros in a launch of the small sort: eight per SM of a B200
 static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
   EmbedGradPlan p;
   int bits = 1;
   while (bits < 31 && (V >> bits) != 0) ++bits;  // keys 0 .. V
   p.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.tiles = (int)((N + kSortTile - 1) / kSortTile);
+  p.small = N <= kSortSmall && V <= (long long)kZeroCtas * kZeroRows;
+  p.rounds = N <= kSortShortTiles ? 4 : 8;
+  p.tiles = (int)((N + kSortThreads * p.rounds - 1) / (kSortThreads * p.rounds));
   if (p.tiles < 1) p.tiles = 1;
+  // as many ranges as fill the machine a few times over, no more: a range's ends cost a partial each
   p.per_range = 8;
   while (p.per_range < kEgMaxRange && N / p.per_range > 2048) p.per_range *= 2;
   p.ranges = (int)((N + p.per_range - 1) / p.per_range);
@@ -323,11 +335,15 @@ static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
     p.off_pos[i] = at;
     at += up256((size_t)N * 4);
   }
+  p.off_heads = at;
+  at += up256((size_t)p.ranges * 2 * sizeof(int4));
   p.off_cnt = at;
   const size_t first = (size_t)p.tiles * kSortBins * 4;
   at += up256((size_t)p.passes * first);
   p.off_touched = at;
   at += up256((size_t)((V + 31) / 32) * 4);
+  p.off_counters = at;
+  at += 256;
   p.zero_from = p.off_cnt + first;
   p.zero_bytes = at - p.zero_from;
   p.off_partial = at;
@@ -336,13 +352,38 @@ static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
   return p;
 }
 
+// Deals rows of zeros to the launches.
+struct ZeroDeal {
+  long long next, V, row_bytes;
+  ZeroShare take(long long rows, int from, int each) {
+    ZeroShare h;
+    h.from = from;
+    h.each = each;
+    h.first = next;
+    next = rows < V - next ? next + rows : V;
+    h.last = next;
+    return h;
+  }
+  // rows that about `bytes` make up
+  long long worth(double bytes) const { return (long long)(bytes / (double)row_bytes); }
+  static unsigned ctas(const ZeroShare& h) { return (unsigned)(h.from + (h.last - h.first + h.each - 1) / h.each); }
+};
+
 template <int DT, int DTO, bool VEC>
-static cudaError_t launch_embed_grad(const EmbedGradArgs& A, int threads, cudaStream_t st) {
-  const long long n_sum = (long long)A.ranges * A.slabs;
-  embed_grad_kernel<DT, DTO, VEC><<<(unsigned)(n_sum + A.zero_ctas), threads, 0, st>>>(A);
+static cudaError_t launch_embed_grad(const EmbedGradArgs& A, ZeroDeal& deal, int threads, int each, cudaStream_t st) {
+  const int n_sum = A.ranges * A.slabs;
+  // the join takes some 10 us of which little is spent on memory
+  const long long rest = deal.V - deal.next, last = A.ranges > 1 ? (deal.worth(48e6) < rest / 2 ? deal.worth(48e6) : rest / 2) : 0;
+  const ZeroShare h = deal.take(rest - last, n_sum, each);
+  embed_grad_kernel<DT, DTO, VEC><<<ZeroDeal::ctas(h), threads, 0, st>>>(A, h);
   cudaError_t err = cudaGetLastError();
   if (err != cudaSuccess || A.ranges < 2) return err;
-  embed_join_kernel<DTO, VEC><<<(unsigned)n_sum, threads, 0, st>>>(A);
+  const int W = A.D % 4 == 0 ? 4 : 1;
+  const long long tiles = (A.D + W * kEgThreads - 1) / (W * kEgThreads) * A.ranges;
+  const long long cap = (long long)sm_count() * 8;
+  const ZeroShare j = deal.take(deal.V, (int)(tiles < cap ? tiles : cap), each);
+  if (W == 4) embed_join_kernel<DTO, 4><<<ZeroDeal::ctas(j), kEgThreads, 0, st>>>(A, j);
+  else embed_join_kernel<DTO, 1><<<ZeroDeal::ctas(j), kEgThreads, 0, st>>>(A, j);
   return cudaGetLastError();
 }
 
@@ -380,6 +421,28 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   if (!workspace || workspace_bytes < P.total) return GLS_ERR_WORKSPACE;
   if ((uintptr_t)workspace % 16) return GLS_ERR_MISALIGNED;
   char* ws = (char*)workspace;
+  const bool vec = D % kEgCols == 0 && grad_out_stride * es % 16 == 0 && grad_table_stride * eso % 16 == 0 &&
+                   (uintptr_t)grad_out % 16 == 0 && (uintptr_t)grad_table % 16 == 0;
+  const long long per_thread = (D + kEgCols - 1) / kEgCols;
+  const int threads = (int)(per_thread < kEgThreads ? (per_thread + 31) / 32 * 32 : kEgThreads);
+  const long long slabs = (D + (long long)threads * kEgCols - 1) / ((long long)threads * kEgCols);
+  if (slabs * P.ranges > (1LL << 30)) return GLS_ERR_UNSUPPORTED;
+  ZeroArgs Z;
+  Z.out = (char*)grad_table;
+  Z.out_stride = grad_table_stride;
+  Z.V = (int)V;
+  Z.D = D;
+  Z.es = eso;
+  Z.vec = (D * eso % 16 == 0 && grad_table_stride * eso % 16 == 0 && (uintptr_t)grad_table % 16 == 0) ? 1 : 0;
+  Z.touched = P.small ? nullptr : (const uint32_t*)(ws + P.off_touched);
+  Z.tokens = tokens;
+  Z.N = (int)N;
+  ZeroDeal deal = {accumulate ? (long long)V : 0, (long long)V, (long long)D * eso};
+  // rows per CTA that writes zeros: some 64 KB each, and no more than 2^20 CTAs
+  long long each = 65536 / deal.row_bytes;
+  if (each < 1) each = 1;
+  if (each < (V >> 20) + 1) each = (V >> 20) + 1;
+  if (P.small && each > kZeroRows) each = kZeroRows;
   SortArgs S;
   S.tokens = tokens;
   S.N = (int)N;
@@ -388,19 +451,28 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   S.passes = P.passes;
   S.tiles = P.tiles;
   S.cnt = (uint32_t*)(ws + P.off_cnt);
-  S.touched = (uint32_t*)(ws + P.off_touched);
+  S.touched = accumulate ? nullptr : (uint32_t*)(ws + P.off_touched);
   for (int i = 0; i < 2; ++i) {
     S.key[i] = (int32_t*)(ws + P.off_key[i]);
     S.pos[i] = (int32_t*)(ws + P.off_pos[i]);
   }
   S.status = device_status;
-  if (P.tiles == 1) {
-    const size_t smem = sizeof(uint16_t) * kSortWarps * kSortBins + (sizeof(int32_t) + sizeof(uint16_t)) * kSortTile;
-    embed_sort_small_kernel<<<1, kSortThreads, smem, st>>>(S);
+  S.zero = Z;
+  int* const counters = (int*)(ws + P.off_counters);
+  if (P.small) {
+    const size_t smem = sizeof(uint16_t) * kSortWarps * kSortBins + (sizeof(int32_t) + sizeof(uint16_t)) * kSortSmall;
+    // the sort takes some 13 us
+    const ZeroShare h = deal.take(deal.worth(64e6), 1, (int)((V + kZeroCtas - 1) / kZeroCtas));
+    embed_sort_small_kernel<<<ZeroDeal::ctas(h), kSortThreads, smem, st>>>(S, counters, h);
   } else {
     if (cudaMemsetAsync(ws + P.zero_from, 0, P.zero_bytes, st) != cudaSuccess) return GLS_ERR_CUDA;
-    embed_sort_count_kernel<<<P.tiles, kSortThreads, 0, st>>>(S);
-    for (int pass = 0; pass < P.passes; ++pass) embed_sort_pass_kernel<<<P.tiles, kSortThreads, 0, st>>>(S, pass);
+    if (P.rounds == 4) embed_sort_count_kernel<4><<<P.tiles, kSortThreads, 0, st>>>(S);
+    else embed_sort_count_kernel<8><<<P.tiles, kSortThreads, 0, st>>>(S);
+    for (int pass = 0; pass < P.passes; ++pass) {
+      const ZeroShare h = deal.take(deal.worth(64e6), P.tiles, (int)each);  // a pass takes some 10 us
+      if (P.rounds == 4) embed_sort_pass_kernel<4><<<ZeroDeal::ctas(h), kSortThreads, 0, st>>>(S, pass, h);
+      else embed_sort_pass_kernel<8><<<ZeroDeal::ctas(h), kSortThreads, 0, st>>>(S, pass, h);
+    }
   }
   if (cudaGetLastError() != cudaSuccess) return GLS_ERR_CUDA;
   EmbedGradArgs A;
@@ -410,8 +482,9 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   A.out_stride = grad_table_stride;
   A.key = S.key[(P.passes - 1) & 1];
   A.pos = S.pos[(P.passes - 1) & 1];
-  A.touched = S.touched;
   A.partial = (float*)(ws + P.off_partial);
+  A.counters = counters;
+  A.heads = (int4*)(ws + P.off_heads);
   A.N = (int)N;
   A.V = (int)V;
   A.D = D;
@@ -419,20 +492,12 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   A.ranges = P.ranges;
   A.accumulate = accumulate ? 1 : 0;
   A.scale = scale;
-  const bool vec = D % kEgCols == 0 && grad_out_stride * es % 16 == 0 && grad_table_stride * eso % 16 == 0 &&
-                   (uintptr_t)grad_out % 16 == 0 && (uintptr_t)grad_table % 16 == 0;
-  const long long per_thread = (D + kEgCols - 1) / kEgCols;
-  const int threads = (int)(per_thread < 256 ? (per_thread + 31) / 32 * 32 : 256);
-  const long long slabs = (D + (long long)threads * kEgCols - 1) / ((long long)threads * kEgCols);
-  if (slabs * P.ranges > (1LL << 31) - (1LL << 24)) return GLS_ERR_UNSUPPORTED;
   A.slabs = (int)slabs;
-  const long long rows_per_cta = 8;
-  long long zc = accumulate ? 0 : (V + rows_per_cta - 1) / rows_per_cta;
-  if (zc > (1 << 20)) zc = 1 << 20;
-  A.zero_ctas = (int)zc;
+  A.zero = Z;
   cudaError_t err;
 #define EMBED_GRAD(DT, DTO) \
-  err = vec ? launch_embed_grad<DT, DTO, true>(A, threads, st) : launch_embed_grad<DT, DTO, false>(A, threads, st)
+  err = vec ? launch_embed_grad<DT, DTO, true>(A, deal, threads, (int)each, st) \
+            : launch_embed_grad<DT, DTO, false>(A, deal, threads, (int)each, st)
   if (dtype == GLS_F32) EMBED_GRAD(kF32, kF32);
   else if (grad_dtype == GLS_F32) EMBED_GRAD(kBF16, kF32);
   else EMBED_GRAD(kBF16, kBF16);
