@@ -149,7 +149,12 @@ struct ZeroShare {
   long long first, last;
   int from, each;
 };
+// The launches of a call follow one another as programmatic dependents: every CTA lets the next launch
+// start and then waits for the one before, except that CTAs which look through the tokens need nothing
+// of it.  True for a CTA that has written its share.
 __device__ __forceinline__ bool zero_share(const ZeroArgs& Z, const ZeroShare& h) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  if ((int)blockIdx.x < h.from || Z.touched != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");
   if ((int)blockIdx.x < h.from) return false;
   const long long a = h.first + (long long)(blockIdx.x - h.from) * h.each;
   zero_rows(Z, a, min(h.last, a + h.each));
@@ -184,6 +189,7 @@ struct SortArgs {
 template <int ROUNDS>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const __grid_constant__ SortArgs S) {
   __shared__ uint32_t h[kSortBins];
+  asm volatile("griddepcontrol.launch_dependents;");
   for (int d = threadIdx.x; d < kSortBins; d += kSortThreads) h[d] = 0u;
   __syncthreads();
   const uint32_t mask = (1u << S.bits) - 1u;

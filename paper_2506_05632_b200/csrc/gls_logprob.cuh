@@ -304,10 +304,9 @@ struct EntryColumn {
 };
 constexpr uint32_t kNoEntry2 = 0xff80ff80u;  // -inf twice
 
-// Maxima of a lane's entries, 16 of them, as ordered codes (fewer: the others 0).  An entry of +inf is
-// left out: nothing is known about its finite tokens.
-__device__ __forceinline__ void entry_slots(const EntryColumn& c, uint32_t (&code)[16]) {
-  uint32_t acc[8];
+// Maxima of a lane's entries, eight pairs.  An entry of +inf is left out: nothing is known about its
+// finite tokens.
+__device__ __forceinline__ void entry_slots(const EntryColumn& c, uint32_t (&acc)[8]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) acc[j] = kNoEntry2;
   const int W = c.words();
@@ -330,22 +329,28 @@ __device__ __forceinline__ void entry_slots(const EntryColumn& c, uint32_t (&cod
       acc[0] = max_bf16x2(acc[0], x);
     }
   }
+}
+// Ordered codes of N pairs; 0 where there is no finite logit.
+template <int N>
+__device__ __forceinline__ uint32_t slots_kth(const uint32_t (&pair)[N], int k) {
+  uint32_t code[2 * N];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float lo = bf16_lo(acc[j]), hi = bf16_hi(acc[j]);
+  for (int j = 0; j < N; ++j) {
+    const float lo = bf16_lo(pair[j]), hi = bf16_hi(pair[j]);
     code[2 * j] = lo > -CUDART_INF_F ? enc_ordered(lo + 0.0f) : 0u;
     code[2 * j + 1] = hi > -CUDART_INF_F ? enc_ordered(hi + 0.0f) : 0u;
   }
+  return warp_kth<2 * N>(code, k);
 }
-// The warp's bound: at least k of its tokens have this code or more (0: no bound).
+// The warp's bound: at least k of its tokens have this code or more (0: no bound).  512 maxima for many
+// tokens, 128 for few.
 __device__ __forceinline__ uint32_t entry_bound(const EntryColumn& c, int k) {
-  uint32_t code[16];
-  entry_slots(c, code);
-  if (k > 64) return warp_kth<16>(code, k);
-  uint32_t few[4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) few[j] = max(max(code[j], code[j + 4]), max(code[j + 8], code[j + 12]));
-  return warp_kth<4>(few, k);
+  uint32_t acc[8];
+  entry_slots(c, acc);
+  if (k > 64) return slots_kth<8>(acc, k);
+  const uint32_t few[2] = {max_bf16x2(max_bf16x2(acc[0], acc[2]), max_bf16x2(acc[4], acc[6])),
+                           max_bf16x2(max_bf16x2(acc[1], acc[3]), max_bf16x2(acc[5], acc[7]))};
+  return slots_kth<2>(few, k);
 }
 // What an entry and a token have to exceed to reach the bound.
 struct EntryTest {
@@ -519,12 +524,16 @@ __device__ __forceinline__ float warp_max(float m) {
   for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
   return m;
 }
+// Sums relative to the reference from, moved to the reference m.
+__device__ __forceinline__ double2 part_at(double2 a, float from, float m, float c2) {
+  const float r = ex2_approx((from - m) * c2);
+  if (!(r > 0.f)) return make_double2(0.0, 0.0);
+  return make_double2(a.x * (double)r, (a.y + a.x * ((double)from - (double)m)) * (double)r);
+}
 // The lane's sums moved to the reference m; NaN when they are not finite, however far below m.
 __device__ __forceinline__ double2 sums_at(const ScoreSums& t, float m, float c2) {
   if (!(t.s < CUDART_INF_F)) return make_double2(CUDART_NAN, CUDART_NAN);
-  const float r = ex2_approx((t.m - m) * c2);
-  if (!(r > 0.f)) return make_double2(0.0, 0.0);
-  return make_double2((double)t.s * r, ((double)t.u + (double)t.s * ((double)t.m - (double)m)) * r);
+  return part_at(make_double2((double)t.s, (double)t.u), t.m, m, c2);
 }
 // Whether the sweep's sums stand: not zero, infinite or NaN, and the reference in the range in which
 // a difference of two logits can not overflow.
@@ -547,13 +556,13 @@ __device__ __forceinline__ ScoreGiven score_given(const ScoreArgs& A, long long 
   return r;
 }
 
-// Outputs of one row except its alternatives, by one warp.  m reference logit, s and u the sums.
+// Outputs of one row except its alternatives, by one warp.  m reference logit, s and u the sums, ls the
+// logarithm of s (0 without a finite logit).
 template <int DT>
-__device__ __forceinline__ double score_emit(const ScoreArgs& A, long long row, const ScoreRow& rl, ScoreGiven gv,
-                                             float m, double s, double u) {
+__device__ __forceinline__ void score_emit(const ScoreArgs& A, long long row, const ScoreRow& rl, ScoreGiven gv,
+                                           float m, double s, double u, double ls) {
   const int lane = threadIdx.x & 31;
   const bool some = s > 0.0;
-  const double ls = some ? log(s) : 0.0;
   const double lse = (double)m * (double)rl.inv_t + ls;
   if (lane == 0) {
     const float hi = some ? (float)lse : -CUDART_INF_F;
@@ -578,7 +587,6 @@ __device__ __forceinline__ double score_emit(const ScoreArgs& A, long long row, 
     }
     A.out_lp[row * A.G + g] = lp;
   }
-  return ls;
 }
 
 __device__ __forceinline__ void score_emit_top(const ScoreArgs& A, long long row, int i, uint32_t key, int idx,
@@ -673,7 +681,8 @@ __global__ void __launch_bounds__(32, kScoreCtasPerSM) score_rows_kernel(const _
       a = make_double2(0.0, 0.0);
       if (m > -CUDART_INF_F) a = warp_sum2(careful_sums<DT>(rl.rowp, lane, 32, A.V, m, c2));
     }
-    const double ls = score_emit<DT>(A, row, rl, given, m, a.x, a.y);
+    const double ls = a.x > 0.0 ? log(a.x) : 0.0;
+    score_emit<DT>(A, row, rl, given, m, a.x, a.y, ls);
     if (A.M == 0) continue;
 
     // ---- alternatives ----------------------------------------------------------------------------
@@ -736,7 +745,6 @@ struct ClusterShared {
   float red[kClWarps];
   double2 red2[kClWarps];
   int n_list, n;
-  double ls;
 };
 
 __device__ __forceinline__ uint32_t cluster_map(const void* p, uint32_t rank) {
@@ -866,11 +874,7 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
     const bool odd = lane < kClWarps && !(sh.red2[lane < kClWarps ? lane : 0].x >= 0.0);
     const float m = warp_max(mw);
     double2 a = make_double2(0.0, 0.0);
-    if (on) {
-      const double dl = (double)mw - (double)m, r = exp2(dl * (double)c2);
-      a.x = r * sh.red2[lane].x;
-      a.y = r > 0.0 ? r * (sh.red2[lane].y + sh.red2[lane].x * dl) : 0.0;
-    }
+    if (on) a = part_at(sh.red2[lane], mw, m, c2);
     a = warp_sum2(a);
     if (__any_sync(0xffffffffu, odd)) a.x = CUDART_NAN;
     if (lane == 0) {
@@ -892,14 +896,8 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
   float m = warp_max(mc);  // every warp for itself
   double2 a = make_double2(0.0, 0.0);
   if (lane < ctas) {
-    const double dl = (double)mc - (double)m;
-    const double r = mc > -CUDART_INF_F ? exp2(dl * (double)c2) : 0.0;
-    if (!(sh.all_part[lane].x >= 0.0)) {
-      a.x = CUDART_NAN;
-    } else if (r > 0.0) {
-      a.x = r * sh.all_part[lane].x;
-      a.y = r * (sh.all_part[lane].y + sh.all_part[lane].x * dl);
-    }
+    if (!(sh.all_part[lane].x >= 0.0)) a.x = CUDART_NAN;
+    else if (mc > -CUDART_INF_F) a = part_at(sh.all_part[lane], mc, m, c2);
   }
   a = warp_sum2(a);
   if (!sums_stand(a, m)) {  // uniform over the CTA
@@ -920,12 +918,9 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
       }
     }
   }
-  if (warp == 0) {
-    const double ls = score_emit<DT>(A, row, rl, given, m, a.x, a.y);
-    if (lane == 0) sh.ls = ls;
-  }
+  const double ls = a.x > 0.0 ? log(a.x) : 0.0;  // every warp for itself
+  if (warp == 0) score_emit<DT>(A, row, rl, given, m, a.x, a.y, ls);
   if (A.M == 0) return;
-  __syncthreads();
   int total = 0;
   for (int c = 0; c < ctas; ++c) total += sh.all_best[c];
   // The lists are in descending order: a code's rank is its place in its own list and where it would
@@ -951,7 +946,7 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
       int r = i;
 #pragma unroll
       for (int o = 0; o < kClMaxCtas; ++o) r += lo[o];
-      if (r < A.M) score_emit_top(A, row, r, (uint32_t)(mine >> 32), (int)~(uint32_t)mine, m, rl.inv_t, sh.ls);
+      if (r < A.M) score_emit_top(A, row, r, (uint32_t)(mine >> 32), (int)~(uint32_t)mine, m, rl.inv_t, ls);
     }
   }
   for (int i = total + tid; i < A.M; i += kClThreads) score_emit_no_top(A, row, i);
@@ -1119,14 +1114,11 @@ __global__ void __launch_bounds__(kGradThreads, kGradCtasPerSM) score_grad_kerne
     const long long first = (long long)chunk * A.iters * kTurn + tid * EV;  // this thread's first vector
 
     Words8 w[kGradVecs];
-    auto load = [&](long long v0) {
-#pragma unroll
-      for (int q = 0; q < kGradVecs; ++q) {
-        const long long v = v0 + q * (kGradThreads * EV);
-        if (v >= mis && v + EV <= end) w[q] = ld_stream32(rowp + (v - mis) * ES);
-      }
+    auto load = [&](int q, long long v) {
+      if (v >= mis && v + EV <= end) w[q] = ld_stream32(rowp + (v - mis) * ES);
     };
-    load(first);
+#pragma unroll
+    for (int q = 0; q < kGradVecs; ++q) load(q, first + q * (kGradThreads * EV));
 
     // ---- the row's constants -----------------------------------------------------------------------
     GradRow r;
@@ -1173,7 +1165,6 @@ __global__ void __launch_bounds__(kGradThreads, kGradCtasPerSM) score_grad_kerne
     for (int i = 0; i < A.iters; ++i) {
       const long long v0 = first + (long long)i * kTurn;
       if (v0 - lane * EV >= end) break;
-      if (i > 0) load(v0);
 #pragma unroll
       for (int q = 0; q < kGradVecs; ++q) {
         const long long v = v0 + q * (kGradThreads * EV);
@@ -1192,6 +1183,7 @@ __global__ void __launch_bounds__(kGradThreads, kGradCtasPerSM) score_grad_kerne
             }
           }
         }
+        if (i + 1 < A.iters) load(q, v + kTurn);  // the next turn's, as soon as the registers are free
       }
     }
     // the vectors that stick out of the row at its ends: an element per thread

@@ -2,7 +2,9 @@
 
 `spec_step` is what a serving loop calls per speculative-decoding step once both sets of logits
 are on the GPU: draft-side sampling (Algorithm 2, draft loop) followed by target-side sampling and
-verification (Algorithm 2, second half).  `HostStepper` is the same step for logits that live in
+verification (Algorithm 2, second half), and where the buffers ask for it what a serving loop needs of
+the emitted tokens next: their log probabilities with entropy and alternatives, and their rows of an
+embedding table, the inputs of the next step.  `HostStepper` is the same step for logits that live in
 (pinned) host memory: it streams sequence chunks to the device through two staging buffers so
 that the copy of chunk n+1 overlaps the sweep of chunk n, and returns the results to the host.
 Only copies, launches and bookkeeping happen here; all arithmetic is in the CUDA library.
@@ -22,10 +24,24 @@ def shard_sequences(B, rank, world):
 
 
 class StepBuffers:
-    """Preallocated outputs and workspace for `spec_step` on B sequences."""
+    """Preallocated outputs and workspace for `spec_step` on B sequences.
 
-    def __init__(self, B, K, L, V, device="cuda"):
+    top: None, or the number of alternatives to report per emitted token: `answers` then holds
+    emitted_logprobs' outputs.  table: None, or an embedding table [V,D] on the device: `inputs`
+    [B,L+1,D] then holds table_scale * table[emitted tokens], zeros at and beyond tau."""
+
+    def __init__(self, B, K, L, V, device="cuda", top=None, table=None, table_scale=1.0):
         self.shape = (B, K, L, V)
+        self.top, self.table, self.table_scale = top, table, table_scale
+        self.answers = self.inputs = None
+        if top is not None:
+            f32 = dict(dtype=torch.float32, device=device)
+            self.answers = {n: torch.empty((B, L + 1), **f32) for n in ("logprobs", "lse", "entropy")}
+            if top:
+                self.answers["top_ids"] = torch.empty((B, L + 1, top), dtype=torch.int32, device=device)
+                self.answers["top_logprobs"] = torch.empty((B, L + 1, top), **f32)
+        if table is not None:
+            self.inputs = torch.empty((B, L + 1, table.shape[1]), dtype=table.dtype, device=device)
         self.draft_tokens = torch.empty((B, K, max(L, 0)), dtype=torch.int32, device=device)
         self.draft_scores = torch.empty((B, K, max(L, 0)), dtype=torch.float32, device=device)
         self.out = dict(tokens=torch.empty((B, L + 1), dtype=torch.int32, device=device),
@@ -41,18 +57,25 @@ class StepBuffers:
 
 def spec_step(draft_logits, target_logits, buf, inv_temp=1.0, seed=0, seq_base=0, pos_base=0,
               spec=4, rounds=10, fused=False):
-    """draft_logits [B,K,L,V], target_logits [B,K,L+1,V] on the device -> buf.out (device).
+    """draft_logits [B,K,L,V], target_logits [B,K,L+1,V] on the device -> buf.out (device), and
+    buf.answers and buf.inputs where the buffers have them.
     fused: one gls_draft_verify call instead of a draft call followed by a verify call."""
     kw = dict(inv_temp=inv_temp, seed=seed, seq_base=seq_base, pos_base=pos_base, spec=spec,
               rounds=rounds, workspace=buf.workspace, status=buf.status)
     if fused and draft_logits.shape[2] > 0:
         binding.draft_verify(draft_logits, target_logits, out_draft_tokens=buf.draft_tokens,
                              out_draft_scores=buf.draft_scores, out=buf.out, **kw)
-        return buf.out
-    if draft_logits.shape[2] > 0:
-        binding.draft_sample(draft_logits, out_tokens=buf.draft_tokens,
-                             out_scores=buf.draft_scores, **kw)
-    binding.target_sample_verify(target_logits, buf.draft_tokens, out=buf.out, **kw)
+    else:
+        if draft_logits.shape[2] > 0:
+            binding.draft_sample(draft_logits, out_tokens=buf.draft_tokens,
+                                 out_scores=buf.draft_scores, **kw)
+        binding.target_sample_verify(target_logits, buf.draft_tokens, out=buf.out, **kw)
+    if buf.answers is not None:
+        binding.emitted_logprobs(target_logits, buf.out["tokens"], buf.out["accept"], top=buf.top,
+                                 inv_temp=inv_temp, status=buf.status, out=buf.answers)
+    if buf.inputs is not None:
+        binding.embed_tokens_raw(buf.table, buf.out["tokens"], scale=buf.table_scale, status=buf.status,
+                                 out=buf.inputs)
     return buf.out
 
 

@@ -576,6 +576,38 @@ def test_serving_step_with_answers(gls):
         assert torch.equal(want[2], held[2])
 
 
+@pytest.mark.parametrize("fused", [False, True])
+def test_spec_step_reports_on_the_emitted_tokens(gls, fused):
+    """The pipeline's step with answers and next inputs, and as a captured graph on refilled logits."""
+    from paper_2506_05632_b200 import pipeline
+
+    B, K, L, V, D = 5, 3, 2, 4001, 24
+    t = _logits((B, K, L + 1, V), BF, 90)
+    d = (t[:, :, :L].float() + 0.5 * torch.randn((B, K, L, V), generator=_gen(91), device="cuda")).to(BF)
+    table = torch.randn((V, D), generator=_gen(92), device="cuda").to(BF)
+    buf = pipeline.StepBuffers(B, K, L, V, top=6, table=table, table_scale=2.0)
+    plain = pipeline.StepBuffers(B, K, L, V)
+    kw = dict(inv_temp=0.8, seed=7, fused=fused)
+
+    def check():
+        want = pipeline.spec_step(d, t, plain, **kw)
+        for n in want:
+            assert torch.equal(buf.out[n], want[n]), n
+        answers = gls.emitted_logprobs(t, want["tokens"], want["accept"], top=6, inv_temp=0.8)
+        for n in answers:
+            assert torch.equal(buf.answers[n], answers[n]), n
+        live = (want["tokens"] >= 0)[..., None]
+        assert torch.equal(buf.inputs, table[want["tokens"].long().clamp(min=0)] * 2.0 * live)
+    pipeline.spec_step(d, t, buf, **kw)
+    check()
+    graph = pipeline.GraphedStep(d, t, buf, **kw)
+    t.copy_(_logits((B, K, L + 1, V), BF, 95))
+    graph.replay()
+    torch.cuda.synchronize()
+    check()
+    assert int(buf.status.item()) == 0
+
+
 def test_backward_in_a_graph(gls):
     """The binding's backward functions captured while an eager graph of the same leaf is alive; the
     differentiable form refuses the capture."""
