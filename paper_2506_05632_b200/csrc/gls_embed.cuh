@@ -102,28 +102,59 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_any_kernel(const __grid_c
 // share of them while its other CTAs, few and waiting on one another's results, leave the memory
 // system idle.
 // ------------------------------------------------------------------------------------------
+enum : int { kZeroByBits, kZeroByTokens, kZeroByKeys };  // how a CTA learns which of its rows to leave
 struct ZeroArgs {
   char* out;              // [V][D]
   long long out_stride;   // elements
   int V;
   long long D;
   int es, vec;            // bytes per element; 16-byte stores
-  const uint32_t* touched;  // bit per token, or NULL: look through the tokens
-  const int32_t* tokens;
+  int how;
+  const uint32_t* touched;  // by bits: one per token
+  const int32_t* tokens;    // by tokens: the CTA looks through all of them
+  const int32_t* keys;      // by keys: the sorted tokens; the CTA finds its own among them
   int N;
 };
-constexpr int kZeroRows = 4096;  // rows per CTA at most where the tokens are looked through
+constexpr int kZeroRows = 16384;  // rows per CTA at most, except by bits
 
 // Rows [first, last) of tokens that do not occur, by the calling CTA.
 __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, long long last) {
   __shared__ uint32_t here[kZeroRows / 32];
-  const bool look = Z.touched == nullptr;
+  const bool look = Z.how != kZeroByBits;
+  if (first >= last) return;
   if (look) {
-    for (int w = threadIdx.x; w < kZeroRows / 32; w += blockDim.x) here[w] = 0u;
+    for (int w = threadIdx.x; w < (last - first + 31) / 32; w += blockDim.x) here[w] = 0u;
     __syncthreads();
-    for (int i = threadIdx.x; i < Z.N; i += blockDim.x) {
-      const long long r = (long long)__ldg(Z.tokens + i) - first;
-      if (r >= 0 && r < last - first) atomicOr(&here[r >> 5], 1u << (r & 31));
+    if (Z.how == kZeroByTokens) {
+#pragma unroll 1
+      for (int i0 = 0; i0 < Z.N; i0 += 8 * blockDim.x) {
+        int t[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int i = i0 + q * blockDim.x + threadIdx.x;
+          t[q] = i < Z.N ? __ldg(Z.tokens + i) : -1;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const long long r = (long long)t[q] - first;
+          if (r >= 0 && r < last - first) atomicOr(&here[r >> 5], 1u << (r & 31));
+        }
+      }
+    } else {
+      // the first key that is not below `first`: the range is cut by as many threads at a time
+      int lo = 0, n = Z.N;  // it is in [lo, lo + n]
+      while (n > 0) {
+        const int part = (n + (int)blockDim.x) / ((int)blockDim.x + 1);  // 1 .. n
+        const int at = (int)(threadIdx.x + 1) * part - 1;                // the last of this thread's part
+        const int below = __syncthreads_count(at < n && __ldg(Z.keys + lo + at) < first);
+        lo += below * part;
+        n = min(n - below * part, part - 1);
+      }
+      for (int i = lo + threadIdx.x; i < Z.N; i += blockDim.x) {
+        const long long r = (long long)__ldg(Z.keys + i) - first;
+        if (r >= last - first) break;
+        atomicOr(&here[r >> 5], 1u << (r & 31));
+      }
     }
     __syncthreads();
   }
@@ -154,7 +185,7 @@ struct ZeroShare {
 // of it.  True for a CTA that has written its share.
 __device__ __forceinline__ bool zero_share(const ZeroArgs& Z, const ZeroShare& h) {
   asm volatile("griddepcontrol.launch_dependents;");
-  if ((int)blockIdx.x < h.from || Z.touched != nullptr) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if ((int)blockIdx.x < h.from || Z.how != kZeroByTokens) asm volatile("griddepcontrol.wait;" ::: "memory");
   if ((int)blockIdx.x < h.from) return false;
   const long long a = h.first + (long long)(blockIdx.x - h.from) * h.each;
   zero_rows(Z, a, min(h.last, a + h.each));
@@ -171,7 +202,6 @@ constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortMaxBits = 9;
 constexpr int kSortBins = 1 << kSortMaxBits;
-constexpr int kSortSmall = 4096;  // tokens that one CTA sorts by itself (8 keys per thread)
 // Keys per thread of a tile: 4 while the counts that every CTA adds up (tiles x 512) stay small.
 constexpr long long kSortShortTiles = 262144;
 
@@ -217,14 +247,14 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const __
 }
 
 // Stable ranks of a tile's keys by digit: warp w owns 32 ROUNDS consecutive keys, 32 a round.  On
-// return wc[w][d] is the number of keys with digit d before warp w in the tile and rank[r] the number
-// before this one in its warp.
-template <int ROUNDS>
+// return wc[w][d] is the number of keys with digit d before warp w in the tile, total[d] the tile's, and
+// rank[r] the number before this one in its warp.
+template <int ROUNDS, int WARPS, int BINS>
 __device__ __forceinline__ void tile_ranks(const uint32_t (&digit)[ROUNDS], const bool (&valid)[ROUNDS],
-                                           int (&rank)[ROUNDS], uint16_t (*wc)[kSortBins]) {
+                                           int (&rank)[ROUNDS], uint16_t (*wc)[BINS], uint32_t* total, int bins) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t lt = (1u << lane) - 1u;
-  for (int d = lane; d < kSortBins / 2; d += 32) ((uint32_t*)wc[warp])[d] = 0u;
+  for (int d = lane; d < bins / 2; d += 32) ((uint32_t*)wc[warp])[d] = 0u;
   __syncwarp();
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
@@ -238,19 +268,22 @@ __device__ __forceinline__ void tile_ranks(const uint32_t (&digit)[ROUNDS], cons
     __syncwarp();
   }
   __syncthreads();
-  for (int d = threadIdx.x; d < kSortBins; d += kSortThreads) {
-    uint32_t run = 0u;
+  for (int d = threadIdx.x; d < bins; d += 32 * WARPS) {
+    uint32_t c[WARPS], run = 0u;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
-      const uint32_t c = wc[w][d];
+    for (int w = 0; w < WARPS; ++w) c[w] = wc[w][d];
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
       wc[w][d] = (uint16_t)run;
-      run += c;
+      run += c[w];
     }
+    total[d] = run;
   }
   __syncthreads();
 }
 
-// exclusive scan over the CTA's kSortThreads values (one per thread)
+// exclusive scan over the CTA's values (one per thread)
+template <int WARPS>
 __device__ __forceinline__ uint32_t cta_scan(uint32_t x, uint32_t* warp_sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t incl = x;
@@ -262,13 +295,13 @@ __device__ __forceinline__ uint32_t cta_scan(uint32_t x, uint32_t* warp_sums) {
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
   if (warp == 0) {
-    uint32_t s = lane < kSortWarps ? warp_sums[lane] : 0u;
+    uint32_t s = lane < WARPS ? warp_sums[lane] : 0u;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const uint32_t o = __shfl_up_sync(0xffffffffu, s, d);
       if (lane >= d) s += o;
     }
-    if (lane < kSortWarps) warp_sums[lane] = s;
+    if (lane < WARPS) warp_sums[lane] = s;
   }
   __syncthreads();
   const uint32_t r = incl - x + (warp > 0 ? warp_sums[warp - 1] : 0u);
@@ -281,7 +314,7 @@ __global__ void __launch_bounds__(kSortThreads)
 embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroShare share) {
   __shared__ __align__(16) uint16_t wc[kSortWarps][kSortBins];
   __shared__ uint32_t base[kSortBins];
-  __shared__ uint32_t warp_sums[kSortWarps];
+  __shared__ uint32_t warp_sums[kSortWarps], tile_total[kSortBins];
   static_assert(kSortBins == kSortThreads, "a thread per digit");
   if (zero_share(S.zero, share)) return;
   constexpr int kTile = kSortThreads * ROUNDS;
@@ -322,8 +355,8 @@ embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroS
     if (t < (int)blockIdx.x) before += c;
     total += c;
   }
-  base[threadIdx.x] = cta_scan(total, warp_sums) + before;
-  tile_ranks<ROUNDS>(digit, valid, rank, wc);
+  base[threadIdx.x] = cta_scan<kSortWarps>(total, warp_sums) + before;
+  tile_ranks<ROUNDS, kSortWarps, kSortBins>(digit, valid, rank, wc, tile_total, kSortBins);
   uint32_t* next = pass + 1 < S.passes ? S.cnt + (long long)(pass + 1) * S.tiles * kSortBins : nullptr;
 #pragma unroll
   for (int r = 0; r < ROUNDS; ++r) {
@@ -337,79 +370,105 @@ embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroS
   }
 }
 
-// At most kSortSmall tokens: the whole sort in the first CTA, through shared memory; the others write
-// zeros.
-__global__ void __launch_bounds__(kSortThreads)
-embed_sort_small_kernel(const __grid_constant__ SortArgs S, int* counters, const ZeroShare share) {
-  constexpr int ROUNDS = kSortSmall / kSortThreads;
-  if (zero_share(S.zero, share)) return;
+// At most kClSortMost tokens: the whole sort in the first cluster of the launch, in its CTAs' shared
+// memory; the other CTAs write zeros.  A CTA holds 8192 consecutive positions.  Per pass every CTA ranks
+// its keys, the CTAs read one another's digit counts, and each key goes straight to its place in the
+// shared memory of the CTA that holds it next.  (65536 tokens below 2^18: 19 us; by the kernels above,
+// which go through global memory and four launches, 33 us.)
+constexpr int kClSortThreads = 1024;
+constexpr int kClSortWarps = kClSortThreads / 32;
+constexpr int kClSortRounds = 2;
+constexpr int kClSortTile = kClSortThreads * kClSortRounds;  // 2048
+constexpr int kClSortCtas = 8;
+constexpr int kClSortMost = kClSortTile * kClSortCtas;       // 16384
+constexpr int kClSortMaxBits = 10;
+constexpr int kClSortBins = 1 << kClSortMaxBits;
+struct ClSortShared {
+  uint2 item[2][kClSortTile];  // (key, position)
+  uint16_t wc[kClSortWarps][kClSortBins];
+  uint32_t total[2][kClSortBins];
+  uint32_t base[kClSortBins];
+  uint32_t warp_sums[kClSortWarps];
+};
+static_assert(kClSortBins == kClSortThreads, "a thread per digit");
+
+__global__ void __launch_bounds__(kClSortThreads)
+embed_sort_cluster_kernel(const __grid_constant__ SortArgs S, int* counters, int ctas, const ZeroShare share) {
+  if (zero_share(S.zero, share)) return;  // share.from == ctas: whole clusters
   extern __shared__ __align__(16) unsigned char score_smem[];
-  uint16_t(*wc)[kSortBins] = (uint16_t(*)[kSortBins])score_smem;
-  int32_t* skey = (int32_t*)(score_smem + sizeof(uint16_t) * kSortWarps * kSortBins);
-  uint16_t* spos = (uint16_t*)(skey + kSortSmall);  // positions are below kSortSmall
-  __shared__ uint32_t base[kSortBins];
-  __shared__ uint32_t warp_sums[kSortWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  ClSortShared& sh = *(ClSortShared*)score_smem;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int cta = (int)blockIdx.x;
   const uint32_t mask = (1u << S.bits) - 1u;
-  if (threadIdx.x < 2) counters[threadIdx.x] = 0;
-  int key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
-  uint32_t digit[ROUNDS];
-  bool valid[ROUNDS];
-  const int i0 = warp * 32 * ROUNDS;
+  if (cta == 0 && tid < 2) counters[tid] = 0;
+  uint32_t key[kClSortRounds], pos[kClSortRounds], digit[kClSortRounds];
+  int rank[kClSortRounds];
+  bool valid[kClSortRounds];
+  const int i0 = warp * 32 * kClSortRounds + lane;  // within the tile
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
-    const int i = i0 + r * 32 + lane;
+  for (int r = 0; r < kClSortRounds; ++r) {
+    const int i = cta * kClSortTile + i0 + r * 32;
     valid[r] = i < S.N;
-    key[r] = 0;
-    pos[r] = i;
+    key[r] = 0u;
+    pos[r] = (uint32_t)i;
     if (valid[r]) {
       const int t = __ldg(S.tokens + i);
-      key[r] = t >= 0 && t < S.V ? t : S.V;
+      key[r] = t >= 0 && t < S.V ? (uint32_t)t : (uint32_t)S.V;
       if (t >= S.V && S.status != nullptr) atomicOr(S.status, kDevBadToken);
     }
   }
   for (int pass = 0; pass < S.passes; ++pass) {
-    const int shift = pass * S.bits;
+    const int shift = pass * S.bits, half = pass & 1;
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) digit[r] = ((uint32_t)key[r] >> shift) & mask;
-    base[threadIdx.x] = 0u;
-    tile_ranks<ROUNDS>(digit, valid, rank, wc);
-    // keys of each digit in the whole tile
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r)
-      if (valid[r]) atomicAdd(&base[digit[r]], 1u);
-    __syncthreads();
-    const uint32_t total = base[threadIdx.x];
-    const uint32_t start = cta_scan(total, warp_sums);
-    base[threadIdx.x] = start;
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-      if (!valid[r]) continue;
-      const uint32_t at = base[digit[r]] + wc[warp][digit[r]] + (uint32_t)rank[r];
-      if (!GLS_IN_RANGE(at, 0, kSortSmall, 71u)) continue;
-      skey[at] = key[r];
-      spos[at] = (uint16_t)pos[r];
+    for (int r = 0; r < kClSortRounds; ++r) digit[r] = (key[r] >> shift) & mask;
+    tile_ranks<kClSortRounds, kClSortWarps, kClSortBins>(digit, valid, rank, sh.wc, sh.total[half], (int)mask + 1);
+    // all CTAs' counts are there, and all CTAs have read what the last pass left in `item`
+    if (ctas > 1) {
+      cluster_arrive();
+      cluster_wait();
     }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-      const int i = i0 + r * 32 + lane;
-      if (valid[r]) {
-        key[r] = skey[i];
-        pos[r] = spos[i];
+    uint32_t before = 0u, all = 0u;
+    if ((uint32_t)tid <= mask) {
+      for (int c = 0; c < ctas; ++c) {
+        const uint32_t n = cluster_ld32(cluster_map(&sh.total[half][tid], (uint32_t)c));
+        if (c < cta) before += n;
+        all += n;
       }
     }
+    const uint32_t start = cta_scan<kClSortWarps>(all, sh.warp_sums) + before;
+    sh.base[tid] = start;
     __syncthreads();
-  }
-  int32_t* kout = S.key[(S.passes - 1) & 1];
-  int32_t* pout = S.pos[(S.passes - 1) & 1];
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
-    const int i = i0 + r * 32 + lane;
+    for (int r = 0; r < kClSortRounds; ++r) {
+      if (!valid[r]) continue;
+      const uint32_t at = sh.base[digit[r]] + sh.wc[warp][digit[r]] + (uint32_t)rank[r];
+      if (!GLS_IN_RANGE(at, 0, S.N, 71u)) continue;
+      cluster_st64(cluster_map(&sh.item[half][at % kClSortTile], at / kClSortTile),
+                   ((unsigned long long)pos[r] << 32) | key[r]);
+    }
+    if (ctas > 1) {
+      cluster_arrive();
+      cluster_wait();
+    } else {
+      __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < kClSortRounds; ++r) {
+      if (valid[r]) {
+        const uint2 x = sh.item[half][i0 + r * 32];
+        key[r] = x.x;
+        pos[r] = x.y;
+      }
+    }
+  }
+  int32_t* const kout = S.key[(S.passes - 1) & 1];
+  int32_t* const pout = S.pos[(S.passes - 1) & 1];
+#pragma unroll
+  for (int r = 0; r < kClSortRounds; ++r) {
+    const int i = cta * kClSortTile + i0 + r * 32;
     if (valid[r]) {
-      kout[i] = key[r];
-      pout[i] = pos[r];
+      kout[i] = (int32_t)key[r];
+      pout[i] = (int32_t)pos[r];
     }
   }
 }

@@ -250,8 +250,27 @@ __device__ __forceinline__ uint32_t warp_kth(const uint32_t (&code)[N], int k) {
     }
     return kth;
   }
+  // the bits that all values above 0 share need no search
+  uint32_t hi = code[0], lo = code[0] - 1u;
+#pragma unroll
+  for (int q = 1; q < N; ++q) {
+    hi = max(hi, code[q]);
+    lo = min(lo, code[q] - 1u);  // 0 wraps to the top
+  }
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  lo = __reduce_min_sync(0xffffffffu, lo) + 1u;
+  if (hi == 0u) return 0u;
+  const int free_bits = 32 - __clz(hi ^ lo);
+  int shift = free_bits > 16 ? (free_bits - 1) & ~1 : 14;
+  kth = shift >= 30 ? 0u : hi >> (shift + 2) << (shift + 2);
+  {  // fewer than k values above 0: no bound
+    uint32_t c = 0u;
+#pragma unroll
+    for (int q = 0; q < N; ++q) c += code[q] > 0u ? 1u : 0u;
+    if (__reduce_add_sync(0xffffffffu, c) < (uint32_t)k) return 0u;
+  }
 #pragma unroll 1
-  for (int shift = 30; shift >= 16; shift -= 2) {
+  for (; shift >= 16; shift -= 2) {
     // how many values are at or above each of the three next thresholds: at most 128, ten bits each
     uint32_t c = 0u;
 #pragma unroll
@@ -370,39 +389,72 @@ __device__ __forceinline__ EntryTest entry_test(uint32_t bound) {
   t.thr = t.all ? -CUDART_INF_F : __uint_as_float(o == 0x8000u ? 0x80000001u : o > 0x8000u ? __float_as_uint(f) - 1u : __float_as_uint(f) + 1u);
   return t;
 }
-// Lists the lane's entries that pass: ids e * 32 + lane + base.
+// Lists the entries of the warp's lanes that pass, ids e * 32 + lane + base, behind what *count says; the
+// caller's warps may share the list.
+template <int WORDS>
 __device__ __forceinline__ void entry_list(const EntryColumn& c, const EntryTest& t, uint16_t* list, int cap, int* count,
                                            int base) {
-  const int W = c.words();
-#pragma unroll 4
-  for (int w = 0; w < W; ++w) {
-    const uint32_t x = max_bf16x2(c.col[w * 32], t.low2) ^ t.low2;
-    if (x != 0u || t.all) {
+  const int lane = threadIdx.x & 31;
+  constexpr int kMasks = (WORDS + 15) / 16;
+  uint32_t pass[kMasks];  // a bit per entry
+  int n = 0;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int e = 2 * w + h;
-        if (e < c.n && (t.all || ((x >> (16 * h)) & 0xffffu) != 0u)) {
-          const int at = atomicAdd(count, 1);  // the order does not matter: tokens are ranked
-          if (at < cap) list[at] = (uint16_t)(base + e * 32 + (int)(threadIdx.x & 31));
-        }
+  for (int j = 0; j < kMasks; ++j) {
+    pass[j] = 0u;
+    if (16 * j >= c.words()) continue;
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int w = j * 16 + i;
+      if (w < WORDS && w < c.words()) {
+        const uint32_t x = max_bf16x2(c.col[w * 32], t.low2) ^ t.low2;
+        if ((x & 0xffffu) != 0u || t.all) m |= 1u << (2 * i);
+        if ((x >> 16) != 0u || t.all) m |= 2u << (2 * i);
       }
     }
+    const int left = c.n - 32 * j;
+    if (left < 32) m &= (1u << left) - 1u;
+    pass[j] = m;
+    n += __popc(m);
+  }
+  int incl = n;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += o;
+  }
+  int at = 0;
+  if (lane == 31) at = atomicAdd(count, incl);
+  at = __shfl_sync(0xffffffffu, at, 31) + incl - n;
+#pragma unroll
+  for (int j = 0; j < kMasks; ++j) {
+    for (uint32_t m = pass[j]; m != 0u; m &= m - 1u, ++at)
+      if (at < cap) list[at] = (uint16_t)(base + (32 * j + __ffs(m) - 1) * 32 + lane);
   }
 }
 __device__ __forceinline__ unsigned long long score_code(uint32_t key, int idx) {
   return ((unsigned long long)key << 32) | (uint32_t)~idx;  // orders by value, then by lower index
 }
-// Appends the tokens above thr of the group at virtual index v to the candidates.
+__device__ __forceinline__ void copy16_async(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+// Requests the group at virtual index v into shared memory (cp.async.wait_all by the same thread).
 template <int DT>
-__device__ __forceinline__ void group_candidates(const char* rowp, int v, int mis, int end, float thr,
-                                                 unsigned long long* cand, int cap, int* count) {
+__device__ __forceinline__ void group_fetch(Group16<DT>* to, const char* rowp, int v, int mis, int end) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
-  if (v >= end) return;
-  Group16<DT> g;
-  if (v >= mis && v + 16 <= end)
-    load16_vec(g, rowp + ((long long)v - mis) * ES);
-  else
-    score_edge<DT>(&g, rowp, v, mis, end);
+  if (v >= mis && v + 16 <= end) {
+    const char* const p = rowp + ((long long)v - mis) * ES;
+#pragma unroll
+    for (int h = 0; h < 16 * ES / 16; ++h) copy16_async((char*)to + 16 * h, p + 16 * h);
+  } else if (v < end) {
+    score_edge<DT>(to, rowp, v, mis, end);
+  }
+}
+// Appends the tokens above thr of a group in shared memory to the candidates.
+template <int DT>
+__device__ __forceinline__ void group_candidates(const Group16<DT>* from, int v, int mis, int end, float thr,
+                                                 unsigned long long* cand, int cap, int* count) {
+  const Group16<DT> g = *from;
   uint32_t pass = 0u;
 #pragma unroll
   for (int t = 0; t < 16; ++t) {
@@ -620,7 +672,7 @@ constexpr int kScoreCtasPerSM = 16;  // one warp each
 constexpr int kRowEntries = 80;      // per lane
 constexpr int kRowCap = 512;         // listed entries, candidates
 
-struct RowShared {
+struct __align__(16) RowShared {
   uint32_t entry[kRowEntries / 2][32];
   unsigned long long cand[kRowCap];
   uint16_t list[kRowCap];
@@ -690,16 +742,27 @@ __global__ void __launch_bounds__(32, kScoreCtasPerSM) score_rows_kernel(const _
     if (lane == 0) sh.n_list = sh.n = 0;
     __syncwarp();
     const EntryTest test = entry_test(entry_bound(col, A.M));
-    entry_list(col, test, sh.list, kRowCap, &sh.n_list, 0);
+    entry_list<kRowEntries / 2>(col, test, sh.list, kRowCap, &sh.n_list, 0);
     __syncwarp();
-    const int groups = sh.n_list << es;  // per lane slot: NG groups each
     if (sh.n_list <= kRowCap) {
-      for (int i = lane; i < groups * NG; i += 32) {
+      // The listed groups come through shared memory (the entries' place), as many at a time as fit: all
+      // of them are on their way together, and the sweep's registers stay what they are.
+      constexpr int kPer = (int)sizeof(sh.entry) / (32 * (int)sizeof(Grp));  // groups per lane and turn
+      Grp* const stage = (Grp*)&sh.entry[0][0] + lane;
+      const int groups = (sh.n_list << es) * NG;
+      auto where = [&](int i) {
         const int id = sh.list[i / NG >> es];
         const int step = (id >> 5 << es) + (i / NG & in_entry);
-        if (step < n_steps)
-          group_candidates<DT>(rl.rowp, step * kStep + (i % NG) * 512 + (id & 31) * 16, mis, end, test.thr, sh.cand,
-                               kRowCap, &sh.n);
+        return step < n_steps ? step * kStep + (i % NG) * 512 + (id & 31) * 16 : end;
+      };
+      for (int i0 = lane; i0 < groups; i0 += 32 * kPer) {
+        for (int q = 0; q < kPer && i0 + 32 * q < groups; ++q)
+          group_fetch<DT>(stage + 32 * q, rl.rowp, where(i0 + 32 * q), mis, end);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        for (int q = 0; q < kPer && i0 + 32 * q < groups; ++q) {
+          const int v = where(i0 + 32 * q);
+          if (v < end) group_candidates<DT>(stage + 32 * q, v, mis, end, test.thr, sh.cand, kRowCap, &sh.n);
+        }
       }
     }
     __syncwarp();
@@ -732,7 +795,7 @@ constexpr int kClList = 256 * kClWarps;       // listed entries of a CTA
 constexpr int kClCand = 1024;       // tokens of a CTA that reach the bound
 static_assert(kClMaxCtas <= 32, "a lane per part");
 
-struct ClusterShared {
+struct __align__(16) ClusterShared {
   uint32_t entry[kClWarps][kClEntries / 2][32];
   unsigned long long cand[kClCand];
   unsigned long long best[kClMaxCtas][kScoreMaxM];  // the CTAs' M best, in descending order
@@ -751,6 +814,11 @@ __device__ __forceinline__ uint32_t cluster_map(const void* p, uint32_t rank) {
   uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
   return r;
+}
+__device__ __forceinline__ uint32_t cluster_ld32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
 }
 __device__ __forceinline__ void cluster_st64(uint32_t a, unsigned long long v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(a), "l"(v) : "memory");
@@ -842,17 +910,22 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
     uint32_t bound = 0xffffffffu;
     for (int w = 0; w < busy; ++w) bound = min(bound, sh.bound[w]);
     const EntryTest test = entry_test(bound);
-    if (mine > 0) entry_list(col, test, sh.list, kClList, &sh.n_list, warp * (kClEntries * 32));
+    if (mine > 0) entry_list<kClEntries / 2>(col, test, sh.list, kClList, &sh.n_list, warp * (kClEntries * 32));
     __syncthreads();
     const int listed = sh.n_list;
     if (listed <= kClList) {
+      static_assert(sizeof(sh.entry) >= kClThreads * sizeof(Group16<kF32>), "a group per thread");
+      Grp* const stage = (Grp*)&sh.entry[0][0][0] + tid;  // all entries have been listed
       for (int i = tid; i < (listed << es) * NG; i += kClThreads) {
         const int id = sh.list[i / NG >> es];
         const int k = ((id >> 5) % kClEntries << es) + (i / NG & in_entry);  // the warp's k-th step
         const int step = rank * kClWarps + id / (kClEntries * 32) + k * stride;
-        if (step < n_steps)
-          group_candidates<DT>(rl.rowp, step * kStep + (i % NG) * 512 + (id & 31) * 16, mis, end, test.thr, sh.cand,
-                               kClCand, &sh.n);
+        const int v = step * kStep + (i % NG) * 512 + (id & 31) * 16;
+        if (step < n_steps && v < end) {
+          group_fetch<DT>(stage, rl.rowp, v, mis, end);
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          group_candidates<DT>(stage, v, mis, end, test.thr, sh.cand, kClCand, &sh.n);
+        }
       }
     }
     __syncthreads();

@@ -307,23 +307,26 @@ namespace gls {
 
 struct EmbedGradPlan {
   int bits, passes, rounds, tiles, per_range, ranges;
-  bool small;                  // one CTA sorts, and the CTAs that write zeros look through the tokens
+  bool small;                  // a cluster sorts, and the CTAs that write zeros look through the tokens
   size_t off_key[2], off_pos[2], off_heads, off_cnt, off_touched, off_counters, off_partial, total;
   size_t zero_from, zero_bytes;  // what has to be zero at the start (counts of later passes, touched, counters)
 };
 static bool embed_grad_sizes_ok(int64_t N, int64_t V, int64_t D) {
   return N >= 0 && N < (1LL << 30) && V > 0 && V < (1LL << 31) - 1 && D > 0 && D < (1LL << 31);
 }
-constexpr int kZeroCtas = 1184;  // CTAs that write zeros in a launch of the small sort: eight per SM of a B200
+// CTAs that write zeros beside a cluster that sorts (one per SM: the sort takes an SM's shared memory)
+constexpr int kZeroCtas = 140;
 static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
   EmbedGradPlan p;
   int bits = 1;
   while (bits < 31 && (V >> bits) != 0) ++bits;  // keys 0 .. V
-  p.passes = (bits + kSortMaxBits - 1) / kSortMaxBits;
+  p.small = N <= kClSortMost && V <= (long long)kZeroCtas * kZeroRows;
+  const int most = p.small ? kClSortMaxBits : kSortMaxBits;
+  p.passes = (bits + most - 1) / most;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.small = N <= kSortSmall && V <= (long long)kZeroCtas * kZeroRows;
   p.rounds = N <= kSortShortTiles ? 4 : 8;
-  p.tiles = (int)((N + kSortThreads * p.rounds - 1) / (kSortThreads * p.rounds));
+  const int tile = p.small ? kClSortTile : kSortThreads * p.rounds;
+  p.tiles = (int)((N + tile - 1) / tile);
   if (p.tiles < 1) p.tiles = 1;
   // as many ranges as fill the machine a few times over, no more: a range's ends cost a partial each
   p.per_range = 8;
@@ -448,12 +451,18 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   Z.D = D;
   Z.es = eso;
   Z.vec = (D * eso % 16 == 0 && grad_table_stride * eso % 16 == 0 && (uintptr_t)grad_table % 16 == 0) ? 1 : 0;
-  Z.touched = P.small ? nullptr : (const uint32_t*)(ws + P.off_touched);
+  Z.how = P.small ? kZeroByTokens : kZeroByBits;
+  Z.touched = (const uint32_t*)(ws + P.off_touched);
   Z.tokens = tokens;
+  Z.keys = (const int32_t*)(ws + P.off_key[(P.passes - 1) & 1]);
   Z.N = (int)N;
   ZeroDeal deal = {accumulate ? (long long)V : 0, (long long)V, (long long)D * eso};
-  // rows per CTA that writes zeros: some 64 KB each, and no more than 2^20 CTAs
-  long long each = 65536 / deal.row_bytes;
+  // Rows per CTA that writes zeros: some 64 KB each, and no more than 2^20 CTAs.  Behind a cluster that
+  // sorts, a CTA first has to find out which of its rows to leave: among few tokens it looks through all
+  // of them, which lets it start beside the sort (1184 CTAs, eight per SM), among many it waits and finds
+  // its own among the sorted ones (256 KB of rows each).
+  const bool by_tokens = P.small && N <= 8192;
+  long long each = by_tokens ? (V + 1183) / 1184 : (P.small ? 262144 : 65536) / deal.row_bytes;
   if (each < 1) each = 1;
   if (each < (V >> 20) + 1) each = (V >> 20) + 1;
   if (P.small && each > kZeroRows) each = kZeroRows;
@@ -474,10 +483,28 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   S.zero = Z;
   int* const counters = (int*)(ws + P.off_counters);
   if (P.small) {
-    const size_t smem = sizeof(uint16_t) * kSortWarps * kSortBins + (sizeof(int32_t) + sizeof(uint16_t)) * kSortSmall;
-    // the sort takes some 13 us
-    const ZeroShare h = deal.take(deal.worth(64e6), 1, (int)((V + kZeroCtas - 1) / kZeroCtas));
-    embed_sort_small_kernel<<<ZeroDeal::ctas(h), kSortThreads, smem, st>>>(S, counters, h);
+    int ctas = 1;
+    while (ctas < P.tiles) ctas *= 2;
+    // the sort takes 10 us and more
+    ZeroShare h = deal.take(deal.worth(64e6), ctas, 1);
+    h.each = (int)((h.last - h.first + kZeroCtas - 1) / kZeroCtas);
+    if (h.each < 1) h.each = 1;
+    const unsigned grid = (ZeroDeal::ctas(h) + ctas - 1) / ctas * ctas;  // whole clusters
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)ctas;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kClSortThreads);
+    cfg.dynamicSmemBytes = sizeof(ClSortShared);
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(embed_sort_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)sizeof(ClSortShared)) != cudaSuccess ||
+        cudaLaunchKernelEx(&cfg, embed_sort_cluster_kernel, S, counters, ctas, h) != cudaSuccess)
+      return GLS_ERR_CUDA;
   } else {
     if (cudaMemsetAsync(ws + P.zero_from, 0, P.zero_bytes, st) != cudaSuccess) return GLS_ERR_CUDA;
     if (P.rounds == 4) embed_sort_count_kernel<4><<<P.tiles, kSortThreads, 0, st>>>(S);
@@ -509,6 +536,7 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   A.scale = scale;
   A.slabs = (int)slabs;
   A.zero = Z;
+  if (P.small && !by_tokens) A.zero.how = kZeroByKeys;
   cudaError_t err;
 #define EMBED_GRAD(DT, DTO) \
   err = vec ? launch_embed_grad<DT, DTO, true>(A, deal, threads, (int)each, st) \
