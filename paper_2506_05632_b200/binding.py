@@ -755,7 +755,7 @@ def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=N
     tp, G, given = _given(tokens, lead, dev)
     out, lp, lse, tail, ent, ids, tlp = _score_out(out, logits, lead, given, M, want_entropy, dev)
     keep, itk = _temps(inv_temp_per_draft, K)
-    _run(dev, _ready().gls_token_logprobs, rows, B, K, J, V, inv_temp, itk, tp, G, M, lp, lse, tail, ent, ids, tlp,
+    _run(dev, _ready().gls_token_logprobs, rows, B, K, J, V, float(inv_temp), itk, tp, G, M, lp, lse, tail, ent, ids, tlp,
          _vec(status, "status", (1,), _I32, dev))
     return out
 
@@ -773,7 +773,7 @@ def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0
     tp = _vec(tokens, "tokens", lead, _I32, dev)
     ap = _vec(accept, "accept", (B, K, L), _U8, dev) if L > 0 else None
     out, lp, lse, _, ent, ids, tlp = _score_out(out, target_logits, lead, lead, M, want_entropy, dev)
-    _run(dev, _ready().gls_emitted_logprobs, rows, B, K, L, V, inv_temp, tp, ap, flags, M, lp, lse, ent, ids, tlp,
+    _run(dev, _ready().gls_emitted_logprobs, rows, B, K, L, V, float(inv_temp), tp, ap, int(flags), M, lp, lse, ent, ids, tlp,
          _vec(status, "status", (1,), _I32, dev))
     return out
 
@@ -803,7 +803,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
     M = 0 if top_ids is None else top_ids.shape[-1]
     top = lead + (M,)
     keep, itk = _temps(inv_temp_per_draft, K)
-    _run(dev, _ready().gls_token_logprobs_backward, rows, B, K, J, V, inv_temp, itk, tp, G,
+    _run(dev, _ready().gls_token_logprobs_backward, rows, B, K, J, V, float(inv_temp), itk, tp, G,
          _vec(top_ids, "top_ids", top, _I32, dev), M, _vec(lse, "lse", lead, _F32T, dev),
          _vec(lse_tail, "lse_tail", lead, _F32T, dev), _vec(entropy, "entropy", lead, _F32T, dev),
          _vec(grad_logprobs, "grad_logprobs", given, _F32T, dev), _vec(grad_lse, "grad_lse", lead, _F32T, dev),
@@ -845,7 +845,7 @@ def embed_tokens_raw(table, tokens, scale=1.0, status=None, out=None):
         except RuntimeError:
             raise GlsError("out's rows must be a constant stride apart") from None
         _, ostride = _matrix(flat, "out")
-    _run(dev, _ready().gls_embed_tokens, table.data_ptr(), dt, stride, V, D, tp, N, scale, out.data_ptr(), ostride,
+    _run(dev, _ready().gls_embed_tokens, table.data_ptr(), dt, stride, V, D, tp, N, float(scale), out.data_ptr(), ostride,
          _vec(status, "status", (1,), _I32, dev))
     return out
 
@@ -877,6 +877,6 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
         raise GlsError("grad_table must have shape [V, D] and be on grad_out's device")
     gdt, gstride = _matrix(grad_table, "grad_table")
     keep, ws, nbytes = _space(workspace, embed_tokens_backward_workspace_bytes(N, V, D), grad_out)
-    _run(dev, _ready().gls_embed_tokens_backward, flat.data_ptr(), dt, stride, tp, N, V, D, scale, grad_table.data_ptr(),
+    _run(dev, _ready().gls_embed_tokens_backward, flat.data_ptr(), dt, stride, tp, N, V, D, float(scale), grad_table.data_ptr(),
          gdt, gstride, EMBED_ACCUMULATE if accumulate else 0, ws, nbytes, _vec(status, "status", (1,), _I32, dev))
     return grad_table

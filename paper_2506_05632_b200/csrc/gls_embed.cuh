@@ -202,13 +202,17 @@ constexpr int kSortThreads = 512;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortMaxBits = 9;
 constexpr int kSortBins = 1 << kSortMaxBits;
-// Keys per thread of a tile: 4 while the counts that every CTA adds up (tiles x 512) stay small.
-constexpr long long kSortShortTiles = 262144;
+constexpr int kSortRounds = 4;                         // keys per thread
+constexpr int kSortTile = kSortThreads * kSortRounds;  // 2048
+// Tiles up to which every CTA of a pass adds up the others' counts itself; beyond, a launch per pass turns
+// them into places first.
+constexpr int kSortFewTiles = 64;
 
 struct SortArgs {
   const int32_t* tokens;
   int N, V, bits, passes, tiles;
   uint32_t* cnt;                  // [passes][tiles][kSortBins]
+  uint32_t* sum;                  // [passes][kSortBins]: where there are many tiles, the digits' totals
   uint32_t* touched;              // [(V + 31) / 32] bits, or NULL
   int32_t* key[2];                // ping, pong
   int32_t* pos[2];
@@ -216,22 +220,21 @@ struct SortArgs {
   ZeroArgs zero;
 };
 
-template <int ROUNDS>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_count_kernel(const __grid_constant__ SortArgs S) {
   __shared__ uint32_t h[kSortBins];
   asm volatile("griddepcontrol.launch_dependents;");
   for (int d = threadIdx.x; d < kSortBins; d += kSortThreads) h[d] = 0u;
   __syncthreads();
   const uint32_t mask = (1u << S.bits) - 1u;
-  const int i0 = blockIdx.x * (kSortThreads * ROUNDS);
-  int t[ROUNDS];
+  const int i0 = blockIdx.x * kSortTile;
+  int t[kSortRounds];
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
+  for (int r = 0; r < kSortRounds; ++r) {
     const int i = i0 + r * kSortThreads + threadIdx.x;
     t[r] = i < S.N ? __ldg(S.tokens + i) : -1;
   }
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
+  for (int r = 0; r < kSortRounds; ++r) {
     const int i = i0 + r * kSortThreads + threadIdx.x;
     if (i >= S.N) continue;
     const int key = t[r] >= 0 && t[r] < S.V ? t[r] : S.V;
@@ -309,7 +312,34 @@ __device__ __forceinline__ uint32_t cta_scan(uint32_t x, uint32_t* warp_sums) {
   return r;
 }
 
-template <int ROUNDS>
+// Many tiles: the counts of a pass become, per digit, the sums over the tiles before each.  A CTA takes 32
+// digits, its warps the tiles in contiguous parts.
+constexpr int kScanWarps = 16;
+__global__ void __launch_bounds__(32 * kScanWarps) embed_sort_scan_kernel(const __grid_constant__ SortArgs S, int pass) {
+  __shared__ uint32_t part[kScanWarps][32];
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int d = (int)blockIdx.x * 32 + lane;
+  uint32_t* const cnt = S.cnt + (long long)pass * S.tiles * kSortBins + d;
+  const int each = (S.tiles + kScanWarps - 1) / kScanWarps;
+  const int t0 = min(S.tiles, warp * each), t1 = min(S.tiles, t0 + each);
+  uint32_t run = 0u;
+#pragma unroll 8
+  for (int t = t0; t < t1; ++t) run += __ldcg(cnt + (long long)t * kSortBins);
+  part[warp][lane] = run;
+  __syncthreads();
+  run = 0u;
+  for (int w = 0; w < warp; ++w) run += part[w][lane];
+  for (int t = t0; t < t1; ++t) {
+    uint32_t* const p = cnt + (long long)t * kSortBins;
+    const uint32_t c = __ldcg(p);
+    __stcg(p, run);
+    run += c;
+  }
+  if (warp == kScanWarps - 1) S.sum[pass * kSortBins + d] = run;
+}
+
 __global__ void __launch_bounds__(kSortThreads)
 embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroShare share) {
   __shared__ __align__(16) uint16_t wc[kSortWarps][kSortBins];
@@ -317,7 +347,6 @@ embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroS
   __shared__ uint32_t warp_sums[kSortWarps], tile_total[kSortBins];
   static_assert(kSortBins == kSortThreads, "a thread per digit");
   if (zero_share(S.zero, share)) return;
-  constexpr int kTile = kSortThreads * ROUNDS;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t mask = (1u << S.bits) - 1u;
   const int shift = pass * S.bits;
@@ -326,12 +355,12 @@ embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroS
   const int32_t* pin = S.pos[(pass + 1) & 1];
   int32_t* kout = S.key[pass & 1];
   int32_t* pout = S.pos[pass & 1];
-  int key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
-  uint32_t digit[ROUNDS];
-  bool valid[ROUNDS];
-  const int i0 = blockIdx.x * kTile + warp * 32 * ROUNDS;
+  int key[kSortRounds], pos[kSortRounds], rank[kSortRounds];
+  uint32_t digit[kSortRounds];
+  bool valid[kSortRounds];
+  const int i0 = blockIdx.x * kSortTile + warp * 32 * kSortRounds;
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
+  for (int r = 0; r < kSortRounds; ++r) {
     const int i = i0 + r * 32 + lane;
     valid[r] = i < S.N;
     key[r] = pos[r] = 0;
@@ -349,24 +378,29 @@ embed_sort_pass_kernel(const __grid_constant__ SortArgs S, int pass, const ZeroS
   }
   // where this tile's keys of digit d = threadIdx.x start
   uint32_t total = 0u, before = 0u;
+  if (S.tiles <= kSortFewTiles) {
 #pragma unroll 8
-  for (int t = 0; t < S.tiles; ++t) {
-    const uint32_t c = __ldcg(cnt + (long long)t * kSortBins + threadIdx.x);
-    if (t < (int)blockIdx.x) before += c;
-    total += c;
+    for (int t = 0; t < S.tiles; ++t) {
+      const uint32_t c = __ldcg(cnt + (long long)t * kSortBins + threadIdx.x);
+      if (t < (int)blockIdx.x) before += c;
+      total += c;
+    }
+  } else {
+    before = __ldcg(cnt + (long long)blockIdx.x * kSortBins + threadIdx.x);
+    total = __ldcg(S.sum + pass * kSortBins + threadIdx.x);
   }
   base[threadIdx.x] = cta_scan<kSortWarps>(total, warp_sums) + before;
-  tile_ranks<ROUNDS, kSortWarps, kSortBins>(digit, valid, rank, wc, tile_total, kSortBins);
+  tile_ranks<kSortRounds, kSortWarps, kSortBins>(digit, valid, rank, wc, tile_total, kSortBins);
   uint32_t* next = pass + 1 < S.passes ? S.cnt + (long long)(pass + 1) * S.tiles * kSortBins : nullptr;
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
+  for (int r = 0; r < kSortRounds; ++r) {
     if (!valid[r]) continue;
     const uint32_t at = base[digit[r]] + wc[warp][digit[r]] + (uint32_t)rank[r];
     if (!GLS_IN_RANGE(at, 0, S.N, 70u)) continue;
     kout[at] = key[r];
     pout[at] = pos[r];
     if (next != nullptr)
-      atomicAdd(next + (long long)(at / kTile) * kSortBins + (((uint32_t)key[r] >> (shift + S.bits)) & mask), 1u);
+      atomicAdd(next + (long long)(at / kSortTile) * kSortBins + (((uint32_t)key[r] >> (shift + S.bits)) & mask), 1u);
   }
 }
 

@@ -306,9 +306,9 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
 namespace gls {
 
 struct EmbedGradPlan {
-  int bits, passes, rounds, tiles, per_range, ranges;
+  int bits, passes, tiles, per_range, ranges;
   bool small;                  // a cluster sorts, and the CTAs that write zeros look through the tokens
-  size_t off_key[2], off_pos[2], off_heads, off_cnt, off_touched, off_counters, off_partial, total;
+  size_t off_key[2], off_pos[2], off_heads, off_sum, off_cnt, off_touched, off_counters, off_partial, total;
   size_t zero_from, zero_bytes;  // what has to be zero at the start (counts of later passes, touched, counters)
 };
 static bool embed_grad_sizes_ok(int64_t N, int64_t V, int64_t D) {
@@ -324,8 +324,7 @@ static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
   const int most = p.small ? kClSortMaxBits : kSortMaxBits;
   p.passes = (bits + most - 1) / most;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.rounds = N <= kSortShortTiles ? 4 : 8;
-  const int tile = p.small ? kClSortTile : kSortThreads * p.rounds;
+  const int tile = p.small ? kClSortTile : kSortTile;
   p.tiles = (int)((N + tile - 1) / tile);
   if (p.tiles < 1) p.tiles = 1;
   // as many ranges as fill the machine a few times over, no more: a range's ends cost a partial each
@@ -341,6 +340,8 @@ static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
   }
   p.off_heads = at;
   at += up256((size_t)p.ranges * 2 * sizeof(int4));
+  p.off_sum = at;
+  at += up256((size_t)p.passes * kSortBins * 4);
   p.off_cnt = at;
   const size_t first = (size_t)p.tiles * kSortBins * 4;
   at += up256((size_t)p.passes * first);
@@ -474,6 +475,7 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   S.passes = P.passes;
   S.tiles = P.tiles;
   S.cnt = (uint32_t*)(ws + P.off_cnt);
+  S.sum = (uint32_t*)(ws + P.off_sum);
   S.touched = accumulate ? nullptr : (uint32_t*)(ws + P.off_touched);
   for (int i = 0; i < 2; ++i) {
     S.key[i] = (int32_t*)(ws + P.off_key[i]);
@@ -507,12 +509,13 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
       return GLS_ERR_CUDA;
   } else {
     if (cudaMemsetAsync(ws + P.zero_from, 0, P.zero_bytes, st) != cudaSuccess) return GLS_ERR_CUDA;
-    if (P.rounds == 4) embed_sort_count_kernel<4><<<P.tiles, kSortThreads, 0, st>>>(S);
-    else embed_sort_count_kernel<8><<<P.tiles, kSortThreads, 0, st>>>(S);
+    embed_sort_count_kernel<<<P.tiles, kSortThreads, 0, st>>>(S);
     for (int pass = 0; pass < P.passes; ++pass) {
+      if (P.tiles > kSortFewTiles &&
+          launch_after(embed_sort_scan_kernel, kSortBins / 32, 32 * kScanWarps, st, S, pass) != cudaSuccess)
+        return GLS_ERR_CUDA;
       const ZeroShare h = deal.take(deal.worth(64e6), P.tiles, (int)each);  // a pass takes some 10 us
-      if (launch_after(P.rounds == 4 ? embed_sort_pass_kernel<4> : embed_sort_pass_kernel<8>, ZeroDeal::ctas(h),
-                       kSortThreads, st, S, pass, h) != cudaSuccess)
+      if (launch_after(embed_sort_pass_kernel, ZeroDeal::ctas(h), kSortThreads, st, S, pass, h) != cudaSuccess)
         return GLS_ERR_CUDA;
     }
   }

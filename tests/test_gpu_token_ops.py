@@ -177,6 +177,21 @@ def test_logprobs_full_size_row(gls):
             _check(gls, x, _tokens((2, 1, 1), 151000, 4), M, what="152064 M=%d" % M)
 
 
+@pytest.mark.parametrize("dtype,V", [(F, 300007), (BF, 1300003), (F, 1250011), (BF, 2500007)])
+def test_logprobs_long_rows(gls, dtype, V):
+    """Rows so long that an entry of the selection covers several steps of a warp: few rows, and as many
+    (one read again and again) as are scored a warp each."""
+    x = _logits((1, 1, 3, V), dtype, V)
+    x[0, 0, 2] = x[0, 0, 2].float().sort().values.to(dtype)  # ascending
+    tok = _tokens((1, 1, 3), V, 6, none=0.0)
+    few = _check(gls, x, tok, 40, what="long rows V=%d %s" % (V, dtype))
+    many = gls.token_logprobs(x.expand(800, 1, 3, V), tok.expand(800, 1, 3).contiguous(), top=40)
+    for n in ("logprobs", "lse", "entropy", "top_logprobs"):
+        tol = 2 * (ref.ENT if n == "entropy" else ref.LSE)
+        ref.near(many[n], few[n].double().expand(many[n].shape), tol, "many long rows " + n)
+    assert torch.equal(many["top_ids"], few["top_ids"].expand(800, 1, 3, 40))
+
+
 def test_logprobs_elements_past_32_bits(gls):
     """Row offsets beyond 2^32 elements (8.9 GB of bf16 rows, two of them looked at)."""
     V, B = 152064, 29000
@@ -440,7 +455,8 @@ def _embed_grad_ref(g, tok, V, scale):
 @pytest.mark.parametrize("dtype", [F, BF])
 @pytest.mark.parametrize("N,V,D", [(1, 1, 1), (3, 5, 8), (64, 7, 40), (1000, 50, 33), (4096, 30000, 64), (4097, 600, 24),
                                    (9000, 152064, 16), (20000, 300, 264), (50000, 1 << 20, 8), (5000, 3, 1032),
-                                   (300, 2000, 4104)])
+                                   (300, 2000, 4104), (16384, 700, 16), (16385, 70000, 16), (150000, 5000, 16),
+                                   (400000, 200, 8), (70000, 3000000, 8)])
 def test_embedding_gradient(gls, dtype, N, V, D):
     g = torch.randn((N, D), generator=_gen(N), device="cuda").to(dtype)
     tok = _skewed(N, V, N)
