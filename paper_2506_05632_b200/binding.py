@@ -718,19 +718,15 @@ def _score_out(out, like, lead, given, M, want_entropy, dev):
     """(outputs, their pointers: log probabilities, lse, lse's tail, entropy, ids, their log probabilities)"""
     if out is None:
         pe = pi = pt = None
-        if given == lead and want_entropy:  # one allocation for three tensors of one shape
-            lp, lse, ent = torch.empty((3,) + lead, dtype=_F32T, device=like.device).unbind(0)
-        else:
-            lse = torch.empty(lead, dtype=_F32T, device=like.device)
-            lp = lse.new_empty(given)
-            ent = lse.new_empty(lead) if want_entropy else None
+        lse = torch.empty(lead, dtype=_F32T, device=like.device)
+        lp = torch.empty_like(lse) if given == lead else lse.new_empty(given)
         out = {"logprobs": lp, "lse": lse}
         if want_entropy:
-            out["entropy"] = ent
+            out["entropy"] = ent = torch.empty_like(lse)
             pe = ent.data_ptr()
         if M:
-            out["top_ids"] = ids = torch.empty(lead + (M,), dtype=_I32, device=like.device)
             out["top_logprobs"] = tlp = lse.new_empty(lead + (M,))
+            out["top_ids"] = ids = tlp.new_empty(lead + (M,), dtype=_I32)
             pi, pt = ids.data_ptr(), tlp.data_ptr()
         return out, lp.data_ptr(), lse.data_ptr(), None, pe, pi, pt
     top = lead + (M,)

@@ -287,15 +287,21 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
   cudaStream_t st = (cudaStream_t)stream;
   const bool vec = D * es % 16 == 0 && table_stride * es % 16 == 0 && out_stride * es % 16 == 0 &&
                    (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0;
-  const long long units = vec ? N * (D * es / 16) : N * D;
-  const long long per_cta = vec ? kEmbedThreads * kEmbedUnits : kEmbedThreads;
+  const uint32_t per_row = (uint32_t)(D * es / 16);
+  const bool rows_long = vec && per_row >= kEmbedLongRow;
+  const long long per_cta = rows_long ? kEmbedThreads / 32 : vec ? kEmbedThreads * kEmbedUnits : kEmbedThreads;
+  const long long units = rows_long ? N * ((per_row + 32 * kEmbedUnits - 1) / (32 * kEmbedUnits)) : vec ? N * per_row : N * D;
   const long long want = (units + per_cta - 1) / per_cta, cap = 1 << 20;
   const int grid = (int)(want < cap ? want : cap);
-  if (vec) {
-    if (dtype == GLS_BF16) embed_vec_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, (uint32_t)(D * es / 16));
-    else embed_vec_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, (uint32_t)(D * es / 16));
+  const bool bf = dtype == GLS_BF16;
+  if (rows_long) {
+    if (bf) embed_long_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
+    else embed_long_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
+  } else if (vec) {
+    if (bf) embed_vec_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
+    else embed_vec_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
   } else {
-    if (dtype == GLS_BF16) embed_any_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A);
+    if (bf) embed_any_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A);
     else embed_any_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A);
   }
   return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;

@@ -401,7 +401,8 @@ def test_autograd_of_logprobs(gls):
 # ---- embedding ----------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [F, BF])
 @pytest.mark.parametrize("V,D,N", [(1, 1, 1), (5, 8, 3), (100, 16, 1000), (37, 33, 70), (3000, 1024, 17),
-                                   (500, 4096, 300), (20, 8200, 9), (1000, 7, 4097)])
+                                   (500, 4096, 300), (20, 8200, 9), (1000, 7, 4097), (300, 504, 77), (300, 512, 77),
+                                   (300, 520, 77), (300, 1016, 50)])
 def test_embedding(gls, dtype, V, D, N):
     table = torch.randn((V, D), generator=_gen(V), device="cuda").to(dtype)
     tok = _tokens((N,), V, N)
