@@ -378,6 +378,25 @@ static cudaError_t launch_after(void (*kernel)(P...), unsigned grid, int block, 
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+static cudaError_t launch_cluster_sort(const SortArgs& S, int* counters, int ctas, unsigned grid, const ZeroShare& h,
+                                       cudaStream_t st) {
+  const int smem = (int)sizeof(ClSortShared);
+  const cudaError_t err = cudaFuncSetAttribute(embed_sort_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err != cudaSuccess) return err;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)ctas;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kClSortThreads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, embed_sort_cluster_kernel, S, counters, ctas, h);
+}
+
 // Deals rows of zeros to the launches.
 struct ZeroDeal {
   long long next, V, row_bytes;
@@ -498,21 +517,7 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
     h.each = (int)((h.last - h.first + kZeroCtas - 1) / kZeroCtas);
     if (h.each < 1) h.each = 1;
     const unsigned grid = (ZeroDeal::ctas(h) + ctas - 1) / ctas * ctas;  // whole clusters
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)ctas;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(kClSortThreads);
-    cfg.dynamicSmemBytes = sizeof(ClSortShared);
-    cfg.stream = st;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (cudaFuncSetAttribute(embed_sort_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)sizeof(ClSortShared)) != cudaSuccess ||
-        cudaLaunchKernelEx(&cfg, embed_sort_cluster_kernel, S, counters, ctas, h) != cudaSuccess)
-      return GLS_ERR_CUDA;
+    if (launch_cluster_sort(S, counters, ctas, grid, h, st) != cudaSuccess) return GLS_ERR_CUDA;
   } else {
     if (cudaMemsetAsync(ws + P.zero_from, 0, P.zero_bytes, st) != cudaSuccess) return GLS_ERR_CUDA;
     embed_sort_count_kernel<<<P.tiles, kSortThreads, 0, st>>>(S);

@@ -456,7 +456,8 @@ def _embed_grad_ref(g, tok, V, scale):
 @pytest.mark.parametrize("dtype", [F, BF])
 @pytest.mark.parametrize("N,V,D", [(1, 1, 1), (3, 5, 8), (64, 7, 40), (1000, 50, 33), (4096, 30000, 64), (4097, 600, 24),
                                    (9000, 152064, 16), (20000, 300, 264), (50000, 1 << 20, 8), (5000, 3, 1032),
-                                   (300, 2000, 4104), (16384, 700, 16), (16385, 70000, 16), (150000, 5000, 16),
+                                   (300, 2000, 4104), (16384, 700, 16), (16385, 70000, 16), (20000, 40000, 1024),
+                                   (32768, 900, 8), (32769, 900, 8), (150000, 5000, 16),
                                    (400000, 200, 8), (70000, 3000000, 8)])
 def test_embedding_gradient(gls, dtype, N, V, D):
     g = torch.randn((N, D), generator=_gen(N), device="cuda").to(dtype)
