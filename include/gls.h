@@ -495,13 +495,14 @@ int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, i
  * given (each may be NULL) and the sums over the tokens and alternatives whose logits are finite,
  *     d logit_i = inv_temp * [ p_i (g_lse - sum g_logprob - sum g_top - g_entropy (ln p_i + entropy))
  *                              + sum of g_logprob and g_top at token i ]
- * and 0 at masked logits and in rows without a finite logit.  A token that occurs several times in
- * a row adds up.  Each element is rounded once.
+ * and 0 at masked logits, in rows without a finite logit and in rows whose lse is beyond fp32.  A
+ * token that occurs several times in a row adds up.  Each element is rounded once.
  *
  *   lse, lse_tail (may be NULL), entropy (only with grad_entropy), top_ids (only with
  *   grad_top_logprobs)   as returned by gls_token_logprobs for the same rows and temperatures
  *   grad_logits          [B,K,J,V] rows of the logits' type, written in full; strides that are 0
- *                        over more than one row and the logits' own memory are refused.  Rows whose
+ *                        over more than one row and the logits' own memory are refused, and no row
+ *                        may overlap another or a logit row.  Rows whose
  *                        first element is as far from a 32-byte boundary as the logits' row is are
  *                        written by vectors, others element by element.
  */

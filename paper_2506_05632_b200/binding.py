@@ -857,6 +857,7 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
     grad_table, whose other rows are not touched."""
     dev = _device(grad_out, "grad_out")
     lead, shape = tokens.shape, grad_out.shape
+    V = int(V)
     N, D = tokens.numel(), shape[-1] if len(shape) else 0
     if shape != lead + (D,):
         raise GlsError("grad_out must have shape [*tokens.shape, D]")

@@ -140,7 +140,7 @@ struct ScoreSums {
 // 2^-24 of itself, so an exponent is good to 1e-7 of its own size however large the logits are.
 // -inf and NaN make the step's sums NaN (a masked vocabulary tail is common, a masked step in the
 // middle is not); such a step is taken again with both set to the lowest finite value, whose terms
-// are exactly 0.  +inf makes the sums infinite, which the caller finds at the end.
+// are exactly 0, and the row's further steps are taken that way at once.  +inf makes the sums infinite, which the caller finds at the end.
 template <int DT, bool ENT, bool CLAMP>
 __device__ __forceinline__ void score_terms(const Group16<DT> (&g)[ScoreCfg<DT>::kGroups], float lm, float c2,
                                             float& s, float& u) {
@@ -271,7 +271,7 @@ __device__ __forceinline__ uint32_t warp_kth(const uint32_t (&code)[N], int k) {
   }
 #pragma unroll 1
   for (; shift >= 16; shift -= 2) {
-    // how many values are at or above each of the three next thresholds: at most 128, ten bits each
+    // how many values are at or above each of the three next thresholds: at most 512, ten bits each
     uint32_t c = 0u;
 #pragma unroll
     for (int d = 0; d < 3; ++d) {
@@ -290,8 +290,8 @@ __device__ __forceinline__ uint32_t warp_kth(const uint32_t (&code)[N], int k) {
 // tokens ("entry": 64 tokens of bf16, 32 of fp32, or a power of two of steps where there would be
 // too many), rounded down to bf16: two instructions a step.  At the end the M-th largest of a few
 // maxima over entries (distinct tokens) bounds the M-th largest logit T from below; entries that
-// reach T are listed, their tokens read once more, and those that reach T ranked.  Some 1.1 M tokens
-// get that far, so what this costs does not depend on the row's length or order.  (Testing groups
+// reach T are listed, their tokens read once more, and those that reach T ranked.  About a tenth more
+// than M tokens get that far, so what this costs does not depend on the row's length or order.  (Testing groups
 // against a running threshold in the sweep and examining them in batches took 11 thousand
 // instructions a row of 152064 tokens and M = 20, four tenths of what the sums take.)
 // Rows of which more tokens reach T than the buffers hold (equal logits) go through a radix select.
@@ -1076,7 +1076,7 @@ __device__ __forceinline__ void store_elem(char* rowp, long long t, float v) {
 // that t is good to 2^-23 of its own size however large the logits are.
 struct GradRow {
   float xr, c2, k, a, b, inv_t;
-  int careful;  // the row's logits are beyond 1e30 in size: every element is checked by itself
+  int careful;  // every element is checked by itself (see where it is set); 2: the gradient is 0
 };
 template <bool ENT>
 __device__ __forceinline__ float grad_one(const GradRow& r, float x) {
@@ -1226,7 +1226,8 @@ __global__ void __launch_bounds__(kGradThreads, kGradCtasPerSM) score_grad_kerne
       r.xr = lse * A.temp[k];
       if (fabsf(lse) < CUDART_INF_F && fabsf(r.xr) < CUDART_INF_F) {
         r.k = (float)((((double)r.xr * (double)r.inv_t - (double)lse) - (double)tail) * 1.4426950408889634074);
-        r.careful = fabsf(r.xr) >= 1e30f;
+        // logits beyond 1e30 in size, or a temperature so low that xr - 200 / c2 could round to xr
+        r.careful = fabsf(r.xr) >= 1e30f || fabsf(r.xr) * r.c2 > 1e8f;
       } else {  // a row without a finite logit has no gradient
         r.xr = r.a = r.b = 0.f;
         r.k = -CUDART_INF_F;

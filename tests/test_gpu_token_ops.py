@@ -346,6 +346,19 @@ def test_gradient_special_rows(gls, dtype, V):
         _check_grad(gls, x, tok, 20, which, what="special V=%d %s" % (V, which))
 
 
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("inv_temp", [1e-20, 1e-6, 3e3, 1e9, 1e20])
+def test_extreme_temperatures(gls, dtype, inv_temp):
+    """From a uniform law to one token that takes all, forward and backward."""
+    x = _logits((2, 1, 2, 3001), dtype, 14) + (0 if dtype == BF else 40.0)
+    x[1, 0, 1, 7:9] = -INF
+    tok = _tokens((2, 1, 2), 3001, 15, none=0.0)
+    tok[0, 0, 0] = int(x[0, 0, 0].float().argmax())
+    _check(gls, x, tok, 5, inv_temp, what="inv_temp %g %s" % (inv_temp, dtype))
+    for which in (("g_lp",), ALL):
+        _check_grad(gls, x, tok, 5, which, inv_temp, what="inv_temp %g %s" % (inv_temp, dtype))
+
+
 def test_gradient_against_differences(gls):
     """Central differences of the 64-bit formula, in a random direction."""
     B, K, J, V = 2, 1, 2, 200
