@@ -55,13 +55,14 @@ __device__ __forceinline__ ScoreRow score_locate(const ScoreArgs& A, long long r
   if (A.emitted) {
     b = bk;
     k = 0;
-    r.live = __ldg(A.tokens + row) >= 0;
-    if (r.live && j > 0) {  // lowest draft whose position j - 1 was accepted
+    const int t = __ldg(A.tokens + row);
+    if (j > 0) {  // lowest draft whose position j - 1 was accepted; read beside the token
       const uint8_t* a = A.accept + b * A.K * A.L + (j - 1);
-      const unsigned lo = __ballot_sync(0xffffffffu, lane < A.K && a[(long long)lane * A.L] != 0);
-      const unsigned hi = __ballot_sync(0xffffffffu, lane + 32 < A.K && a[(long long)(lane + 32) * A.L] != 0);
+      const unsigned lo = __ballot_sync(0xffffffffu, lane < A.K && __ldg(a + (long long)lane * A.L) != 0);
+      const unsigned hi = A.K > 32 ? __ballot_sync(0xffffffffu, lane + 32 < A.K && __ldg(a + (long long)(lane + 32) * A.L) != 0) : 0u;
       k = lo != 0u ? __ffs(lo) - 1 : hi != 0u ? 31 + __ffs(hi) : 0;
     }
+    r.live = t >= 0;
   } else {
     b = bk / (uint32_t)A.K;
     k = (int)(bk - (uint32_t)b * (uint32_t)A.K);
@@ -465,12 +466,38 @@ __device__ __forceinline__ void group_candidates(const Group16<DT>* from, int v,
   if (v + 16 > end) pass &= 0xffffu >> (v + 16 - end);
   if (pass == 0u) return;
   int at = atomicAdd(count, __popc(pass));
+  for (; pass != 0u; pass &= pass - 1u, ++at) {
+    const int t = __ffs(pass) - 1;
+    const float x = DT == kF32 ? ((const float*)from)[t] : __uint_as_float((uint32_t)((const uint16_t*)from)[t] << 16);
+    if (at < cap) cand[at] = score_code(enc_ordered(x + 0.0f), v + t - mis);
+  }
+}
+
+// The rank of each of n candidates, by counting those before it; a thread takes every `stride`-th from
+// `first`, four at a time where there are many.
+template <class F>
+__device__ __forceinline__ void rank_candidates(const unsigned long long* cand, int n, int first, int stride, F&& put) {
+  int i = first;
+  for (; i + stride < n; i += 4 * stride) {
+    unsigned long long c[4];
+    int r[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int t = 0; t < 16; ++t) {
-    if ((pass >> t) & 1u) {
-      if (at < cap) cand[at] = score_code(enc_ordered(group16_get<DT>(g, t) + 0.0f), v + t - mis);
-      ++at;
+    for (int q = 0; q < 4; ++q) c[q] = i + q * stride < n ? cand[i + q * stride] : 0ull;
+#pragma unroll 2
+    for (int o = 0; o < n; ++o) {
+      const unsigned long long x = cand[o];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) r[q] += x > c[q];
     }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (i + q * stride < n) put(r[q], c[q]);
+  }
+  if (i < n) {
+    const unsigned long long c = cand[i];
+    int r = 0;
+    for (int o = 0; o < n; ++o) r += cand[o] > c;
+    put(r, c);
   }
 }
 
@@ -769,12 +796,9 @@ __global__ void __launch_bounds__(32, kScoreCtasPerSM) score_rows_kernel(const _
     if (sh.n_list > kRowCap || sh.n > kRowCap)
       score_select<DT, 32>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, 0, 1, A.M);
     const int n = sh.n;
-    for (int i = lane; i < n; i += 32) {  // the rank of candidate i: how many come before it
-      const unsigned long long mine = sh.cand[i];
-      int rank = 0;
-      for (int o = 0; o < n; ++o) rank += sh.cand[o] > mine;
-      if (rank < A.M) score_emit_top(A, row, rank, (uint32_t)(mine >> 32), (int)~(uint32_t)mine, m, rl.inv_t, ls);
-    }
+    rank_candidates(sh.cand, n, lane, 32, [&](int rank, unsigned long long c) {
+      if (rank < A.M) score_emit_top(A, row, rank, (uint32_t)(c >> 32), (int)~(uint32_t)c, m, rl.inv_t, ls);
+    });
     for (int i = n + lane; i < A.M; i += 32) score_emit_no_top(A, row, i);
     __syncwarp();  // the shared memory is free for the next row
   }
@@ -862,9 +886,11 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
   bool masked = false;
   float top = -CUDART_INF_F;
   ScoreGiven given = {-1, 0.f};
+  // the last warp merges the sums and writes the row's outputs while the others rank
+  constexpr int kLast = kClWarps - 1;
+  if (rank == 0 && warp == kLast) given = score_given<DT>(A, row, rl, lane);
   if (mine > 0) {
     score_load<DT>(nxt, rl.rowp, mis, end, first);
-    if (rank == 0 && warp == 0) given = score_given<DT>(A, row, rl, lane);  // it has the row's first step
     const float mx0 = warp_max(score_max<DT>(nxt));
     if (mx0 < CUDART_INF_F) sums.m = fmaxf(mx0, kGroupLseFloor);
   }
@@ -932,15 +958,12 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
     if (listed > kClList || sh.n > kClCand)
       score_select<DT, kClThreads>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, first, stride, A.M);
     const int n = sh.n;
-    for (int i = tid; i < n; i += kClThreads) {
-      const unsigned long long mine = sh.cand[i];
-      int r = 0;
-      for (int o = 0; o < n; ++o) r += sh.cand[o] > mine;
-      if (r < A.M) cluster_st64(home + o_best + 8u * r, mine);
-    }
+    rank_candidates(sh.cand, n, tid, kClThreads, [&](int r, unsigned long long c) {
+      if (r < A.M) cluster_st64(home + o_best + 8u * r, c);
+    });
     if (tid == 0) cluster_st32(home + (uint32_t)offsetof(ClusterShared, all_best) + 4u * rank, (uint32_t)min(n, A.M));
   }
-  if (warp == 0) {
+  if (warp == kLast) {
     const bool on = lane < kClWarps && sh.red2[lane < kClWarps ? lane : 0].x > 0.0;
     const float mw = on ? sh.red[lane] : -CUDART_INF_F;
     // a warp whose sums are NaN spoils the CTA's: the row is then summed again with every check
@@ -992,16 +1015,16 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
     }
   }
   const double ls = a.x > 0.0 ? log(a.x) : 0.0;  // every warp for itself
-  if (warp == 0) score_emit<DT>(A, row, rl, given, m, a.x, a.y, ls);
+  if (warp == kLast) score_emit<DT>(A, row, rl, given, m, a.x, a.y, ls);
   if (A.M == 0) return;
   int total = 0;
   for (int c = 0; c < ctas; ++c) total += sh.all_best[c];
-  // The lists are in descending order: a code's rank is its place in its own list and where it would
-  // stand in each other one, found in all of them at once.
   const int half = 1 << (31 - __clz(A.M));  // the largest power of two that is not above M
   for (int c = warp; c < ctas; c += kClWarps) {
     for (int i = lane; i < sh.all_best[c]; i += 32) {
       const unsigned long long mine = sh.best[c][i];
+      // the lists are in descending order: a code's rank is its place in its own list and where it
+      // would stand in each other one, found in all of them at once
       int lo[kClMaxCtas], n[kClMaxCtas];
 #pragma unroll
       for (int o = 0; o < kClMaxCtas; ++o) {

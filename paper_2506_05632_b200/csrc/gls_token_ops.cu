@@ -56,20 +56,23 @@ static int temps_ok(float inv_temp, const float* per_draft, int K, float* out) {
 }
 
 // Which kernel scores `rows` rows of V tokens: 0, a warp per row; c > 0, a cluster of c CTAs per row.
-// The times (us) are a fit to both kernels measured over 1 .. 8192 rows of 4000 .. 152064 tokens; a step
-// is 4 KB of a row, read by one warp.  E.g. 1 row of 152064 bf16 tokens: 56 us by a warp, 24 / 19 / 16 /
-// 15 us by 1 / 2 / 4 / 8 CTAs; 600 of 128256: 66 by a warp, 58 / 65 / 86 / 140 by CTAs; 1000 of 8000:
-// 15 by a warp, 28 / 55 / 97 / 182; 8192 of 152064: 437 by a warp, 510 / 714 by 1 / 2 CTAs.
-static int score_ctas(long long rows, long long V, int dtype) {
+// The times (us) are a fit to both kernels over 1 .. 8192 rows of 1000 .. 152064 tokens; a step is 4 KB of a
+// row, read by one warp.  Measured, by a warp / by 1, 2, 4, 8 CTAs per row: 1 row of 152064 bf16 tokens
+// 54 / 19, 14, 12, 11; 224 of 128256 53 / 23, 21, 28, 39; 1200 of 152064 96 / 86, 97, 131, 213; 2400 of 152064
+// 168 / 146, 177, ..; 8192 of 152064 423 / 455, ..; 1000 of 8000 14 / 20, 40, ..
+static int score_ctas(long long rows, long long V, int M, int dtype) {
   const int step = dtype == GLS_BF16 ? ScoreCfg<kBF16>::kStep : ScoreCfg<kF32>::kStep;
   const double steps = (double)((V + 15 + step - 1) / step);  // a row may start 15 elements past a boundary
   const double warps = (double)sm_count() * kScoreCtasPerSM, slots = (double)sm_count() * kClCtasPerSM;
   const double load = (double)rows / warps;
-  double least = 8.0 + steps * std::fmax(0.72 + std::fmin(load, 1.0), 1.71 * load);
+  double least = 8.0 + steps * (load <= 1.0 ? 0.62 + load : 0.8 + 1.4 * load);
   int best = 0;
   for (int c = 1; c <= kClMaxCtas; c *= 2) {
+    // a CTA's bound on the M-th logit comes from 32 maxima per step: with fewer than 2 M of them so many
+    // tokens reach it that the buffers overflow (4 rows of 152064, M = 256: 234 us by 8 CTAs each)
+    if (c > 1 && 16.0 * steps < (double)c * M) break;
     const double waves = (double)rows * c / slots, each = std::ceil(steps / (c * kClWarps));
-    const double t = (waves <= 1.0 ? 1.0 : waves + 0.5) * (10.0 + each * (0.55 + 0.9 * std::fmin(waves, 1.0)));
+    const double t = 9.0 + (waves <= 1.0 ? each * (0.5 + 1.2 * waves) : (waves + 0.35) * (4.0 + 1.5 * each));
     if (t < least) {
       least = t;
       best = c;
@@ -158,7 +161,7 @@ int gls_token_logprobs(const gls_rows_t* logits, int B, int K, int J, int64_t V,
   A.top_ids = out_top_ids;
   A.top_lp = out_top_logprobs;
   A.status = device_status;
-  return run_score(A, logits, score_ctas(A.rows, V, logits->dtype), (cudaStream_t)stream);
+  return run_score(A, logits, score_ctas(A.rows, V, M, logits->dtype), (cudaStream_t)stream);
 }
 
 int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, int64_t V, float inv_temp,
@@ -194,7 +197,7 @@ int gls_emitted_logprobs(const gls_rows_t* target_logits, int B, int K, int L, i
   A.top_lp = out_top_logprobs;
   A.status = device_status;
   // between one row per sequence and J are read
-  return run_score(A, target_logits, score_ctas((long long)B * (J + 1) / 2, V, target_logits->dtype),
+  return run_score(A, target_logits, score_ctas((long long)B * (J + 1) / 2, V, M, target_logits->dtype),
                    (cudaStream_t)stream);
 }
 
