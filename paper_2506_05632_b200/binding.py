@@ -1,7 +1,10 @@
 """ctypes binding of libgls.so (C ABI in include/gls.h).  Argument marshalling only."""
 import ctypes as C
+import importlib.util
 import os
+import shutil
 import subprocess
+import sysconfig
 import threading
 
 import torch
@@ -10,6 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 _SRC_DIR = os.path.join(_HERE, "csrc")
 _LIB = os.path.join(_HERE, "libgls.so")
+_CALLS_LIB = os.path.join(_HERE, "gls_torch_calls.so")
 
 COMBINE_ACTIVE, COMBINE_ALL, NO_BONUS = 0, 1, 2
 VERIFY_ALL_ROWS, VERIFY_ACTIVE_ROWS = 4, 8  # how the dense verify call walks Algorithm 2
@@ -23,6 +27,7 @@ F32, BF16 = 0, 1
 
 _lock = threading.Lock()
 _lib = None
+_calls = None
 
 
 class GlsError(RuntimeError):
@@ -38,8 +43,29 @@ def _sources():
                   if f.endswith((".cu", ".cuh"))) + [os.path.join(_ROOT, "include", "gls.h")]
 
 
+def _build_calls(force):
+    """Compile csrc/torch_calls.cpp, a Python module over torch's headers, with the host compiler."""
+    srcs = [os.path.join(_SRC_DIR, "torch_calls.cpp"), os.path.join(_ROOT, "include", "gls.h")]
+    if (not force and os.path.exists(_CALLS_LIB)
+            and os.path.getmtime(_CALLS_LIB) >= max(os.path.getmtime(s) for s in srcs)):
+        return
+    at = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc")))
+    tmp = _CALLS_LIB + ".tmp%d" % os.getpid()
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+                    "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+                    "-I" + os.path.join(at, "include"),
+                    "-I" + os.path.join(at, "include", "torch", "csrc", "api", "include"),
+                    "-I" + os.path.join(cuda, "include"), "-I" + sysconfig.get_paths()["include"], "-o", tmp, srcs[0],
+                    "-L" + os.path.join(at, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch",
+                    "-ltorch_python"], check=True)
+    os.replace(tmp, _CALLS_LIB)
+
+
 def build(force=False, verbose=False, debug_bounds=False):
-    """Compile csrc/*.cu into libgls.so for sm_100a with nvcc (cross-compiles without a GPU)."""
+    """Compile csrc/*.cu into libgls.so for sm_100a with nvcc (cross-compiles without a GPU), and
+    csrc/torch_calls.cpp beside it."""
+    _build_calls(force)
     srcs = _sources()
     if (not force and os.path.exists(_LIB)
             and os.path.getmtime(_LIB) >= max(os.path.getmtime(s) for s in srcs)):
@@ -75,11 +101,11 @@ class _Noise(C.Structure):
 
 def load():
     """Load libgls.so (building it if the sources are newer and nvcc is present)."""
-    global _lib
+    global _lib, _calls
     with _lock:
         if _lib is not None:
             return _lib
-        if not os.path.exists(_LIB):
+        if not os.path.exists(_LIB) or not os.path.exists(_CALLS_LIB):
             build()
         L = C.CDLL(_LIB)
         L.gls_version.restype = C.c_int
@@ -168,6 +194,12 @@ def load():
         L.gls_embed_tokens_backward.argtypes = [
             C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_float,
             C.c_void_p, C.c_int, C.c_int64, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        spec = importlib.util.spec_from_file_location("gls_torch_calls", _CALLS_LIB)
+        calls = importlib.util.module_from_spec(spec)
+        calls.entry_points(*(C.cast(getattr(L, "gls_" + n), C.c_void_p).value for n in (
+            "token_logprobs", "emitted_logprobs", "token_logprobs_backward", "embed_tokens",
+            "embed_tokens_backward_workspace_bytes", "embed_tokens_backward")))
+        _calls = calls
         _lib = L
         return _lib
 
@@ -624,8 +656,9 @@ def compress_gaussian(candidates, source, side_info, bins=None, s2_eta=0.5, s2_z
 
 
 # ---- operators next to the sampler: log probabilities, embedding lookup, their gradients ----------
-# A call on a few rows takes the GPU about 10 us, so the wrappers keep the host's share small: one check
-# per tensor, none of those made here, and the stream's handle without a Stream object.
+# A call on a few rows takes the GPU about 10 us, so the host's share counts.  The usual call (tensors on
+# the current device, results made by the call) is made by the compiled module of csrc/torch_calls.cpp;
+# what that does not take, wrong arguments among it, comes back as None and goes the general way below it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda i: torch.cuda.current_stream(i).cuda_stream)
 _I32, _F32T, _BF16T, _U8 = torch.int32, torch.float32, torch.bfloat16, torch.uint8
@@ -633,6 +666,19 @@ _I32, _F32T, _BF16T, _U8 = torch.int32, torch.float32, torch.bfloat16, torch.uin
 
 def _ready():
     return _lib if _lib is not None else load()
+
+
+def _fast():
+    if _calls is None:
+        load()
+    return _calls
+
+
+def _done(r):
+    """The compiled module's answer: results, or a status code."""
+    if r.__class__ is int:
+        raise GlsError(status_string(r))
+    return r
 
 
 def _run(dev, fn, *args):
@@ -674,6 +720,8 @@ def _rows4(t, name):
     st = t.stride()
     if len(st) != 4 or (st[3] != 1 and t.shape[3] > 1):
         raise GlsError("%s must be [B,K,J,V] with a contiguous token dimension" % name)
+    if max(t.shape[:3]) > 0x7fffffff:  # possible with strides of 0; the library's counts have 32 bits
+        raise GlsError("%s has a dimension beyond 32 bits" % name)
     return _Rows(t.data_ptr(), dt, st[0], st[1], st[2])
 
 
@@ -704,6 +752,8 @@ def _given(tokens, lead, dev):
     shape = tokens.shape
     if shape[:3] != lead or len(shape) > 4:
         raise GlsError("tokens must have shape %s or that with one more dimension" % (lead,))
+    if len(shape) == 4 and shape[3] > MAX_GIVEN:
+        raise GlsError("at most %d tokens a row" % MAX_GIVEN)
     return _vec(tokens, "tokens", shape, _I32, dev), shape[3] if len(shape) == 4 else 1, shape
 
 
@@ -744,6 +794,10 @@ def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=N
     Returns dict(logprobs, lse [B,K,J], entropy [B,K,J], top_ids and top_logprobs [B,K,J,top]); entropy
     only if wanted, the alternatives only for top > 0.  Given `out`, its tensors are written (an
     'lse_tail' among them too).  No autograd: see token_logprobs."""
+    if out is None and inv_temp_per_draft is None:
+        r = (_calls or _fast()).token_logprobs(logits, tokens, top, inv_temp, want_entropy, status)
+        if r is not None:
+            return _done(r)
     dev = _device(logits, "logits")
     rows = _rows4(logits, "logits")
     B, K, J, V = logits.shape
@@ -761,6 +815,10 @@ def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0
     """gls_emitted_logprobs: the target rows [B,K,J,V] of a verification with the tokens [B,J] and
     accept flags [B,K,L] it returned -> token_logprobs' dict over [B,J], zeros (alternatives -1) at and
     beyond tau."""
+    if out is None:
+        r = (_calls or _fast()).emitted_logprobs(target_logits, tokens, accept, top, inv_temp, flags, want_entropy, status)
+        if r is not None:
+            return _done(r)
     dev = _device(target_logits, "target_logits")
     rows = _rows4(target_logits, "target_logits")
     B, K, J, V = target_logits.shape
@@ -780,6 +838,11 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
                             grad_logits=None):
     """gls_token_logprobs_backward: the gradient with respect to the logits, [B,K,J,V] in their type,
     from token_logprobs' inputs and outputs and the gradients of its outputs (each may be None)."""
+    if grad_logits is None and inv_temp_per_draft is None:
+        r = (_calls or _fast()).token_logprobs_backward(logits, tokens, lse, entropy, lse_tail, top_ids, grad_logprobs,
+                                                        grad_lse, grad_entropy, grad_top_logprobs, inv_temp)
+        if r is not None:
+            return _done(r)
     dev = _device(logits, "logits")
     rows = _rows4(logits, "logits")
     shape = logits.shape
@@ -796,7 +859,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
         grad_logits = torch.empty(shape, dtype=logits.dtype, device=logits.device)
     elif grad_logits.shape != shape or grad_logits.dtype is not logits.dtype or grad_logits.get_device() != dev:
         raise GlsError("grad_logits must have the logits' shape, type and device")
-    M = 0 if top_ids is None else top_ids.shape[-1]
+    M = 0 if top_ids is None else _top(top_ids.shape[-1])
     top = lead + (M,)
     keep, itk = _temps(inv_temp_per_draft, K)
     _run(dev, _ready().gls_token_logprobs_backward, rows, B, K, J, V, float(inv_temp), itk, tp, G,
@@ -825,6 +888,10 @@ def _matrix(t, name):
 def embed_tokens_raw(table, tokens, scale=1.0, status=None, out=None):
     """gls_embed_tokens: scale * table[tokens] for table [V,D] and int32 tokens of any shape ->
     [*tokens.shape, D]; a token below 0 gives zeros.  No autograd: see embed_tokens."""
+    if out is None:
+        r = (_calls or _fast()).embed_tokens(table, tokens, scale, status)
+        if r is not None:
+            return _done(r)
     dev = _device(table, "table")
     dt, stride = _matrix(table, "table")
     V, D = table.shape
@@ -855,6 +922,10 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
     """gls_embed_tokens_backward: grad_out [*tokens.shape, D] -> the gradient of the table, [V,D] in
     grad_out's type unless grad_table (the same type, or float32) is given.  accumulate: added to
     grad_table, whose other rows are not touched."""
+    if grad_table is None and workspace is None and not accumulate:
+        r = (_calls or _fast()).embed_tokens_backward(grad_out, tokens, V, scale, status)
+        if r is not None:
+            return _done(r)
     dev = _device(grad_out, "grad_out")
     lead, shape = tokens.shape, grad_out.shape
     V = int(V)

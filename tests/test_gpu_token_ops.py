@@ -731,3 +731,112 @@ def test_refusals_of_the_binding(gls):
         with pytest.raises(gls.GlsError):
             f()
             raise AssertionError("call %d was accepted" % n)
+
+
+class _Declines:
+    """Stands in for the compiled module: every call goes the general way."""
+
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+def _same(a, b):
+    if isinstance(a, dict):
+        assert set(a) == set(b)
+        for n in a:
+            _same(a[n], b[n])
+        return
+    assert a.dtype == b.dtype and a.shape == b.shape and a.is_contiguous()
+    assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_both_ways_of_a_call(gls, dtype, monkeypatch):
+    """The compiled module and the binding's own path: the same tensors, the same errors."""
+    x = _logits((2, 3, 4, 1030), dtype, 1)[..., :1021]  # rows that start off a 16-byte boundary
+    tok, many = _tokens((2, 3, 4), 1021, 2), _tokens((2, 3, 4, 5), 1021, 3)
+    bad = _tokens((2, 3, 4), 2000, 4)
+    d = _tokens((2, 3, 3), 1021, 5, none=0)
+    v = gls.target_sample_verify(x, d, inv_temp=1.25, seed=7)
+    table = torch.randn(77, 24, generator=_gen(6), device="cuda").to(dtype)
+    g = torch.randn(2, 3, 4, 24, generator=_gen(7), device="cuda").to(dtype)
+    gl = torch.randn(2, 3, 4, generator=_gen(8), device="cuda")
+
+    def all_calls():
+        status = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(4)]
+        f = gls.token_logprobs(x, tok, top=7, inv_temp=2, status=status[0])
+        out = [f, gls.token_logprobs(x, many, 0, 0.5, None, False), gls.token_logprobs(x, bad, 300 - 44, status=status[1]),
+               gls.token_logprobs(x, many[..., :0].contiguous()), gls.token_logprobs(x, None, 3),
+               gls.emitted_logprobs(x, v["tokens"], v["accept"], top=4, inv_temp=1.25, status=status[2]),
+               gls.token_logprobs_backward(x, tok, f["lse"], entropy=f["entropy"], top_ids=f["top_ids"], grad_logprobs=gl,
+                                           grad_entropy=gl, grad_top_logprobs=f["top_logprobs"], inv_temp=2),
+               gls.embed_tokens(table, bad % 90, 3, status=status[3]), gls.embed_tokens(table[:, :7], tok % 77, 1.5),
+               gls.embed_tokens(table, tok[:0]), gls.embed_tokens_backward(g, tok % 77, 77, 1.5),
+               gls.embed_tokens_backward(g[:0], tok[:0], 77), gls.embed_tokens_backward(g[..., :1], tok % 77, 77)]
+        return out + status
+
+    def errors():
+        z = torch.zeros
+        calls = [lambda: gls.token_logprobs(x, tok, inv_temp=0.0), lambda: gls.token_logprobs(x, tok, inv_temp=float("nan")),
+                 lambda: gls.token_logprobs(x, tok, inv_temp=1 << 2000), lambda: gls.token_logprobs(x, tok, top=-1),
+                 lambda: gls.token_logprobs(x, tok, top=1 << 70), lambda: gls.token_logprobs(x, tok.long()),
+                 lambda: gls.token_logprobs(x, tok.cpu()), lambda: gls.token_logprobs(x, tok[:1]),
+                 lambda: gls.token_logprobs(x[..., ::2], tok), lambda: gls.token_logprobs(x.half(), tok),
+                 lambda: gls.token_logprobs(x[0], tok), lambda: gls.token_logprobs(x[..., :0], tok),
+                 lambda: gls.token_logprobs(x[:0], tok[:0]), lambda: gls.token_logprobs(x, tok, status=z(2).int().cuda()),
+                 lambda: gls.token_logprobs(x, tok[..., None].expand(2, 3, 4, 65).contiguous()),
+                 lambda: gls.token_logprobs(x[:1, :1, :1].expand(2 ** 31, 1, 1, 1021), tok),
+                 lambda: gls.emitted_logprobs(x, v["tokens"], v["accept"][:, :, :2]),
+                 lambda: gls.emitted_logprobs(x, v["tokens"].t(), v["accept"]),
+                 lambda: gls.emitted_logprobs(x, v["tokens"], v["accept"], flags=64),
+                 lambda: gls.token_logprobs_backward(x, tok, gl, grad_entropy=gl),
+                 lambda: gls.token_logprobs_backward(x, tok, None, grad_logprobs=gl),
+                 lambda: gls.token_logprobs_backward(x, tok, gl, grad_logprobs=gl.double()),
+                 lambda: gls.embed_tokens(table, tok, scale=float("inf")), lambda: gls.embed_tokens(table.t(), tok),
+                 lambda: gls.embed_tokens(table.cpu(), tok), lambda: gls.embed_tokens(table, tok.cpu()),
+                 lambda: gls.embed_tokens_backward(g, tok[:1], 77), lambda: gls.embed_tokens_backward(g, tok, 0),
+                 lambda: gls.embed_tokens_backward(g, tok, 77, scale=float("nan"))]
+        names = []
+        for i, c in enumerate(calls):
+            with pytest.raises(Exception) as e:
+                c()
+                pytest.fail("call %d was not refused" % i)
+            names.append((e.type, str(e.value)))
+        return names
+
+    got, bad_calls = all_calls(), errors()
+    monkeypatch.setattr(gls.binding, "_calls", _Declines())
+    want, same_calls = all_calls(), errors()
+    for a, b in zip(got, want):
+        _same(a, b)
+    assert bad_calls == same_calls
+
+
+def test_calls_from_two_threads(gls):
+    """Each thread on its own stream: the calls let other threads run, and keep to their stream."""
+    import threading
+
+    x = _logits((4, 2, 3, 5000), BF, 1)
+    tok = [_tokens((4, 2, 3), 5000, s) for s in (2, 3)]
+    want = [gls.token_logprobs(x, t, top=5) for t in tok]
+    torch.cuda.synchronize()
+    got, fail = [[], []], []
+
+    def work(i):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                for _ in range(50):
+                    got[i].append(gls.token_logprobs(x, tok[i], top=5))
+            s.synchronize()
+        except Exception as e:  # pragma: no cover
+            fail.append(e)
+
+    ts = [threading.Thread(target=work, args=(i,)) for i in (0, 1)]
+    [t.start() for t in ts]
+    [t.join() for t in ts]
+    assert not fail
+    for i in (0, 1):
+        assert len(got[i]) == 50
+        for r in got[i]:
+            _same(r, want[i])
