@@ -223,6 +223,18 @@ __device__ __forceinline__ float score_max(const Group16<DT> (&g)[ScoreCfg<DT>::
   }
 }
 
+template <int DT>
+__device__ __forceinline__ float score_group_max(const Group16<DT>& g) {
+  if constexpr (DT == kBF16) {
+    uint32_t x = g.a.w[0];
+#pragma unroll
+    for (int t = 1; t < 8; ++t) x = max_bf16x2(x, g.a.w[t]);
+    return fmaxf(bf16_lo(x), bf16_hi(x));
+  } else {
+    return group16_max(g);
+  }
+}
+
 // A lower bound on the k-th largest of the warp's 32 N values (ordered codes), exact in its upper
 // 16 bits at least.  0 when fewer than k are above 0.  A few are taken off the top one by one (80
 // cycles each); otherwise the code is found two bits at a time.
@@ -501,17 +513,19 @@ __device__ __forceinline__ void rank_candidates(const unsigned long long* cand, 
   }
 }
 
-// The M best tokens among the steps first, first + stride, .. of the caller's warps by a radix select
-// over (value, index) codes, eight bits a pass from the top, each pass reading the steps again; then
-// the tokens at or above the M-th code, at most M, in no order.  THREADS: 32 (a warp) or a whole CTA.
+// The M best tokens among the steps first, first + stride, .. of the caller's warps, and perhaps more, `cap`
+// in all: a radix select over (value, index) codes, eight bits a pass from the top, each pass reading the
+// steps again, until what is at or above the M-th code's bits fits; then these tokens, in no order.
+// THREADS: 32 (a warp) or a whole CTA.
 struct SelectShared {
   uint32_t hist[256];
   uint32_t bin, rem, count;
 };
 template <int DT, int THREADS>
 __device__ __noinline__ void score_select(SelectShared& sh, unsigned long long* cand, int* n_cand, const char* rowp,
-                                          int mis, int end, int first, int stride, int M) {
+                                          int mis, int end, int first, int stride, int M, int cap) {
   constexpr int kStep = ScoreCfg<DT>::kStep;
+  constexpr int kAhead = 8;
   const int tid = THREADS == 32 ? (int)(threadIdx.x & 31) : (int)threadIdx.x, lane = threadIdx.x & 31;
   auto sync = [&]() {
     if (THREADS == 32) __syncwarp();
@@ -519,11 +533,15 @@ __device__ __noinline__ void score_select(SelectShared& sh, unsigned long long* 
   };
   auto for_each = [&](auto&& f) {
     for (long long s = first; s * kStep < end; s += stride) {
-      for (int t = lane; t < kStep; t += 32) {
+      for (int t = lane; t < kStep; t += 32 * kAhead) {
         const long long v = s * kStep + t;
-        if (v < mis || v >= end) continue;
-        const float x = load_logit<DT>(rowp, v - mis);
-        if (fabsf(x) < CUDART_INF_F) f(score_code(enc_ordered(x + 0.0f), (int)(v - mis)));
+        float x[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+          x[q] = v + 32 * q >= mis && v + 32 * q < end ? load_logit<DT>(rowp, v + 32 * q - mis) : CUDART_INF_F;
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+          if (fabsf(x[q]) < CUDART_INF_F) f(score_code(enc_ordered(x[q] + 0.0f), (int)(v + 32 * q - mis)));
       }
     }
   };
@@ -538,18 +556,31 @@ __device__ __noinline__ void score_select(SelectShared& sh, unsigned long long* 
       if (shift == 56 || (c >> (shift + 8)) == prefix) atomicAdd(&sh.hist[(c >> shift) & 255u], 1u);
     });
     sync();
-    if (tid == 0) {
-      uint32_t above = 0u;
-      int bin = 255;
-      for (; bin > 0 && above + sh.hist[bin] < remaining; --bin) above += sh.hist[bin];
-      sh.bin = (uint32_t)bin;
-      sh.rem = remaining - above;  // more than the bin's count when there are fewer than M tokens
-      sh.count = sh.hist[bin];
+    if (tid < 32) {  // eight bins a lane, from the top
+      int bin = 255 - 8 * lane;
+      uint32_t mine = 0u;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) mine += sh.hist[bin - b];
+      uint32_t incl = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
+      }
+      uint32_t above = incl - mine;
+      if (above < remaining && (incl >= remaining || lane == 31)) {
+        const int last = bin - 7;
+        for (; bin > last && above + sh.hist[bin] < remaining; --bin) above += sh.hist[bin];
+        sh.bin = (uint32_t)bin;
+        sh.rem = remaining - above;  // more than the bin's count when there are fewer than M tokens
+        sh.count = sh.hist[bin];
+      }
     }
     sync();
     prefix = (prefix << 8) | sh.bin;
     remaining = sh.rem;
-    if (sh.count <= remaining || shift == 0) break;  // every code with this prefix is wanted
+    // every code with this prefix is wanted, or can be had with those above it
+    if (sh.count <= remaining || (uint32_t)M - remaining + sh.count <= (uint32_t)cap || shift == 0) break;
     shift -= 8;
   }
   const unsigned long long from = prefix << shift;
@@ -559,7 +590,7 @@ __device__ __noinline__ void score_select(SelectShared& sh, unsigned long long* 
   for_each([&](unsigned long long c) {
     if (c >= from) {
       const int at = atomicAdd(n_cand, 1);
-      if (at < M) cand[at] = c;
+      if (at < cap) cand[at] = c;
     }
   });
   sync();
@@ -698,6 +729,10 @@ __device__ __forceinline__ void score_emit_nothing(const ScoreArgs& A, long long
 constexpr int kScoreCtasPerSM = 16;  // one warp each
 constexpr int kRowEntries = 80;      // per lane
 constexpr int kRowCap = 512;         // listed entries, candidates
+// Alternatives per step beyond which a row's entries are groups: an entry per lane and step gives no bound
+// beyond 32 of them (280 rows of 1945 bf16, M = 50: 108 -> 13 us, 4000 of 2000, M = 28: 31 -> 25); with
+// fewer the second look at the row does not pay (M = 20: 25 us either way).
+constexpr int kFineTop = 24;
 
 struct __align__(16) RowShared {
   uint32_t entry[kRowEntries / 2][32];
@@ -765,6 +800,19 @@ __global__ void __launch_bounds__(32, kScoreCtasPerSM) score_rows_kernel(const _
     if (A.M == 0) continue;
 
     // ---- alternatives ----------------------------------------------------------------------------
+    int lg = es + (NG == 4 ? 2 : 1);  // log2 of the groups per entry
+    if (A.M > kFineTop * n_steps) {
+      // few entries, the bound would be loose or none: the short row again, an entry per group
+      static_assert((kScoreMaxM / kFineTop + 1) * 4 <= kRowEntries, "the groups' entries fit");
+      lg = 0;
+      col.n = n_steps * NG;
+      for (int s = 0; s < n_steps; ++s) {
+        score_load<DT>(nxt, rl.rowp, mis, end, s);
+#pragma unroll
+        for (int q = 0; q < NG; ++q)
+          col.put(s * NG + q, top_entry_bits(score_group_max<DT>(nxt[q]), std::integral_constant<int, DT>()));
+      }
+    }
     if (col.n & 1) col.put(col.n, 0xff80u);
     if (lane == 0) sh.n_list = sh.n = 0;
     __syncwarp();
@@ -776,11 +824,11 @@ __global__ void __launch_bounds__(32, kScoreCtasPerSM) score_rows_kernel(const _
       // of them are on their way together, and the sweep's registers stay what they are.
       constexpr int kPer = (int)sizeof(sh.entry) / (32 * (int)sizeof(Grp));  // groups per lane and turn
       Grp* const stage = (Grp*)&sh.entry[0][0] + lane;
-      const int groups = (sh.n_list << es) * NG;
+      const int groups = sh.n_list << lg;
       auto where = [&](int i) {
-        const int id = sh.list[i / NG >> es];
-        const int step = (id >> 5 << es) + (i / NG & in_entry);
-        return step < n_steps ? step * kStep + (i % NG) * 512 + (id & 31) * 16 : end;
+        const int id = sh.list[i >> lg];
+        const int g = ((id >> 5) << lg) + (i & ((1 << lg) - 1));
+        return g < n_steps * NG ? g * 512 + (id & 31) * 16 : end;
       };
       for (int i0 = lane; i0 < groups; i0 += 32 * kPer) {
         for (int q = 0; q < kPer && i0 + 32 * q < groups; ++q)
@@ -794,7 +842,7 @@ __global__ void __launch_bounds__(32, kScoreCtasPerSM) score_rows_kernel(const _
     }
     __syncwarp();
     if (sh.n_list > kRowCap || sh.n > kRowCap)
-      score_select<DT, 32>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, 0, 1, A.M);
+      score_select<DT, 32>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, 0, 1, A.M, kRowCap);
     const int n = sh.n;
     rank_candidates(sh.cand, n, lane, 32, [&](int rank, unsigned long long c) {
       if (rank < A.M) score_emit_top(A, row, rank, (uint32_t)(c >> 32), (int)~(uint32_t)c, m, rl.inv_t, ls);
@@ -956,7 +1004,7 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
     }
     __syncthreads();
     if (listed > kClList || sh.n > kClCand)
-      score_select<DT, kClThreads>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, first, stride, A.M);
+      score_select<DT, kClThreads>(sh.sel, sh.cand, &sh.n, rl.rowp, mis, end, first, stride, A.M, kClCand);
     const int n = sh.n;
     rank_candidates(sh.cand, n, tid, kClThreads, [&](int r, unsigned long long c) {
       if (r < A.M) cluster_st64(home + o_best + 8u * r, c);

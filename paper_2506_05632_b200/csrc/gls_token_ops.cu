@@ -65,6 +65,7 @@ static int score_ctas(long long rows, long long V, int M, int dtype) {
   const double steps = (double)((V + 15 + step - 1) / step);  // a row may start 15 elements past a boundary
   const double warps = (double)sm_count() * kScoreCtasPerSM, slots = (double)sm_count() * kClCtasPerSM;
   const double load = (double)rows / warps;
+  if (M > kFineTop * steps) return 0;  // the rows kernel has a bound for these
   double least = 8.0 + steps * (load <= 1.0 ? 0.62 + load : 0.8 + 1.4 * load);
   int best = 0;
   for (int c = 1; c <= kClMaxCtas; c *= 2) {

@@ -52,6 +52,29 @@ def test_logprobs_sizes(gls, dtype, V):
 
 
 @pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("V", [300, 513, 700, 1000, 1025, 1817, 2049, 4500, 9000, 17000])
+def test_logprobs_many_alternatives_of_short_rows(gls, dtype, V):
+    for M in (24, 25, 50, 129, 256):
+        x = _logits((5, 2, 3, V + 5), dtype, V + M)[..., 2:V + 2]
+        x[0, 0, 0, :V - M // 2] = -INF       # fewer alternatives than asked for
+        x[0, 0, 1] = 0.25                    # all equal: the lowest indices
+        x[0, 0, 2, ::7] = float("-inf")
+        x[0, 1, 0, 3::5] = float("nan")    
+        x[0, 1, 1, 5] = INF
+        x[0, 1, 2] = x[0, 1, 2].round()      # many equal values
+        x = x.clone() if M == 25 else x
+        got = gls.token_logprobs(x, _tokens((5, 2, 3), V, M), top=M, inv_temp=1.25)
+        live = x.float().masked_fill(~torch.isfinite(x), -INF).view(-1, V)
+        order = torch.sort(live, dim=-1, descending=True, stable=True)
+        n = min(M, V)
+        ids = torch.where(order.values[:, :n] > -INF, order.indices[:, :n], -1)
+        assert torch.equal(got["top_ids"].view(-1, M)[:, :n].long(), ids), (V, M)
+        assert (got["top_ids"].view(-1, M)[:, n:] == -1).all()
+        rest = x[1:].contiguous()
+        _check(gls, rest, _tokens((4, 2, 3), V, M), M, 1.25, what="V=%d M=%d %s" % (V, M, dtype))
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
 @pytest.mark.parametrize("M", [20, 64, 65, 128, 129, 256])
 def test_logprobs_alternatives(gls, dtype, M):
     for B, K, J, V in [(1, 1, 1, 152064), (1, 2, 1, 200), (3, 1, 2, 20000)]:
