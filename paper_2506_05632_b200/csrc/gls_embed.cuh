@@ -38,6 +38,62 @@ __device__ __forceinline__ uint32_t scale_word(uint32_t w, float s) {
   return pack_bf16x2(bf16_lo(w) * s, bf16_hi(w) * s);
 }
 
+// ---- rows at any alignment -------------------------------------------------------------------
+// Rows of an odd size start anywhere.  What is written is cut at 16-byte boundaries of the output; the 16
+// bytes for one store are taken from the two aligned words of the source that hold them.  A word may reach
+// into the row's neighbours, whose elements are not used, but not out of the tensor [lo, hi).
+template <int ES>
+__device__ __noinline__ uint4 span_edge(uintptr_t at, uintptr_t lo, uintptr_t hi) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uintptr_t p = at + 4 * i;
+    if constexpr (ES == 4) {
+      w[i] = p >= lo && p < hi ? __float_as_uint(__ldg((const float*)p)) : 0u;
+    } else {
+      const uint32_t a = p >= lo && p < hi ? (uint32_t)__ldg((const unsigned short*)p) : 0u;
+      const uint32_t b = p + 2 >= lo && p + 2 < hi ? (uint32_t)__ldg((const unsigned short*)(p + 2)) : 0u;
+      w[i] = a | (b << 16);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int ES>
+__device__ __forceinline__ uint4 span_word(uintptr_t at, uintptr_t lo, uintptr_t hi) {
+  if (at >= lo && at + 16 <= hi) return ld_global16((const void*)at);
+  if (at + 16 <= lo || at >= hi) return make_uint4(0u, 0u, 0u, 0u);
+  return span_edge<ES>(at, lo, hi);
+}
+// N 4-byte words that begin `by` bytes (0 .. 15, even) into N + 4 of them
+template <int N>
+__device__ __forceinline__ void shift_words(const uint32_t (&w)[N + 4], int by, uint32_t (&o)[N]) {
+  uint32_t a[N + 2], b[N + 1];
+#pragma unroll
+  for (int i = 0; i < N + 2; ++i) a[i] = (by & 8) ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < N + 1; ++i) b[i] = (by & 4) ? a[i + 1] : a[i];
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = __funnelshift_r(b[i], b[i + 1], (by & 2) * 8);
+}
+// 16 bytes at offset `o` (which may stick out at either end) of a row of `len` bytes
+template <int ES>
+__device__ __forceinline__ void row_put16(char* row, long long o, long long len, uint4 v) {
+  if (o >= 0 && o + 16 <= len) {
+    *(uint4*)(row + o) = v;
+    return;
+  }
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 16 / ES; ++e) {
+    const long long at = o + e * ES;
+    if (at < 0 || at >= len) continue;
+    if constexpr (ES == 4) *(uint32_t*)(row + at) = w[e];
+    else *(unsigned short*)(row + at) = (unsigned short)(w[e >> 1] >> (16 * (e & 1)));
+  }
+}
+// 16-byte pieces that a row of `len` bytes can touch
+__host__ __device__ __forceinline__ long long row_pieces(long long len, int es) { return (len + 16 - es + 15) / 16; }
+
 constexpr int kEmbedThreads = 256;
 constexpr int kEmbedUnits = 4;  // per thread, requested together
 // Units of 16 bytes, `per_row` to a row; a CTA takes 1024 in a row.
@@ -116,22 +172,65 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_long_kernel(const __grid_
     }
   }
 }
-// any alignment, any D
-template <int DT>
-__global__ void __launch_bounds__(kEmbedThreads) embed_any_kernel(const __grid_constant__ EmbedArgs A) {
+// Any alignment, any D: a unit is one of the `per_row` 16-byte pieces that an output row can touch.  Units are
+// dealt as in the two kernels above (LONG: to warps within a row).  One element a thread instead took
+// 535 us for 97450 rows of 1002 fp32.
+template <int DT, bool LONG>
+__global__ void __launch_bounds__(kEmbedThreads) embed_shift_kernel(const __grid_constant__ EmbedArgs A, uint32_t per_row) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
-  const long long n_units = A.N * A.D;
-  for (long long u = (long long)blockIdx.x * kEmbedThreads + threadIdx.x; u < n_units;
-       u += (long long)gridDim.x * kEmbedThreads) {
-    const long long n = u / A.D;
-    const long long c = u - n * A.D;
-    const int t = __ldg(A.tokens + n);
-    float x = 0.f;
-    if (t >= 0 && t < A.V)
-      x = load_logit<DT>(A.table + (long long)t * A.table_stride * ES, c) * A.scale;
-    else if (t >= A.V && c == 0 && A.status != nullptr)
-      atomicOr(A.status, kDevBadToken);
-    store_elem<DT>(A.out + n * A.out_stride * ES, c, x);
+  const int lane = threadIdx.x & 31;
+  const long long len = A.D * ES;
+  const uintptr_t lo = (uintptr_t)A.table, hi = lo + ((A.V - 1) * A.table_stride + A.D) * ES;
+  const uint32_t pieces = LONG ? (per_row + 32 * kEmbedUnits - 1) / (32 * kEmbedUnits) : per_row;
+  const long long n_items = A.N * pieces;
+  const long long per_cta = LONG ? kEmbedThreads / 32 : kEmbedThreads * kEmbedUnits;
+  for (long long i0 = (long long)blockIdx.x * per_cta + (LONG ? threadIdx.x >> 5 : threadIdx.x); i0 < n_items;
+       i0 += (long long)gridDim.x * per_cta) {
+    uint32_t w[kEmbedUnits][8];
+    long long o[kEmbedUnits];
+    char* to[kEmbedUnits];
+    int by[kEmbedUnits];
+#pragma unroll
+    for (int j = 0; j < kEmbedUnits; ++j) {
+      const long long it = LONG ? i0 : i0 + j * kEmbedThreads;
+      to[j] = nullptr;
+      by[j] = -1;  // zeros
+      o[j] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[j][i] = 0u;
+      if (it >= n_items) continue;
+      const long long n = it < (1ll << 32) ? (long long)((uint32_t)it / pieces) : it / pieces;
+      const uint32_t p = (uint32_t)(it - n * pieces);
+      const uint32_t u = LONG ? p * (32 * kEmbedUnits) + 32 * j + lane : p;
+      char* const row = A.out + n * A.out_stride * ES;
+      o[j] = (long long)u * 16 - (long long)((uintptr_t)row & 15);
+      if (o[j] >= len) continue;
+      to[j] = row;
+      const int t = __ldg(A.tokens + n);
+      if (t >= 0 && t < A.V) {
+        const uintptr_t q = lo + (uintptr_t)((long long)t * A.table_stride * ES + o[j]);
+        by[j] = (int)(q & 15);
+        const uint4 x = span_word<ES>(q - by[j], lo, hi);
+        w[j][0] = x.x, w[j][1] = x.y, w[j][2] = x.z, w[j][3] = x.w;
+        if (by[j] != 0) {
+          const uint4 y = span_word<ES>(q - by[j] + 16, lo, hi);
+          w[j][4] = y.x, w[j][5] = y.y, w[j][6] = y.z, w[j][7] = y.w;
+        }
+      } else if (t >= A.V && u == 0 && A.status != nullptr) {
+        atomicOr(A.status, kDevBadToken);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kEmbedUnits; ++j) {
+      if (to[j] == nullptr) continue;
+      uint32_t v[4];
+      shift_words<4>(w[j], max(by[j], 0), v);
+      if (by[j] >= 0 && A.scale != 1.0f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = scale_word<DT>(v[i], A.scale);
+      }
+      row_put16<ES>(to[j], o[j], len, make_uint4(v[0], v[1], v[2], v[3]));
+    }
   }
 }
 
@@ -147,7 +246,8 @@ struct ZeroArgs {
   long long out_stride;   // elements
   int V;
   long long D;
-  int es, vec;            // bytes per element; 16-byte stores
+  int es;                 // bytes per element
+  long long units;        // 16-byte pieces that a row can touch
   int how;
   const uint32_t* touched;  // by bits: one per token
   const int32_t* tokens;    // by tokens: the CTA looks through all of them
@@ -198,7 +298,7 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, lo
     __syncthreads();
   }
   // rows side by side where one does not fill the CTA
-  const long long units = Z.vec ? Z.D * Z.es / 16 : Z.D;
+  const long long units = Z.units, len = Z.D * Z.es;
   const int side = units < blockDim.x ? (int)(blockDim.x / (unsigned)units) : 1;
   const int mine = units < blockDim.x ? (int)(threadIdx.x / (unsigned)units) : 0;
   const long long c0 = units < blockDim.x ? (long long)(threadIdx.x % (unsigned)units) : (long long)threadIdx.x;
@@ -207,10 +307,16 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, lo
     const long long b = look ? v - first : v;
     if (((look ? here[b >> 5] : __ldg(Z.touched + (b >> 5))) >> (b & 31)) & 1u) continue;
     char* const row = Z.out + v * Z.out_stride * Z.es;
-    for (long long c = c0; c < units; c += blockDim.x) {
-      if (Z.vec) ((uint4*)row)[c] = make_uint4(0u, 0u, 0u, 0u);
-      else if (Z.es == 2) ((unsigned short*)row)[c] = 0;
-      else ((float*)row)[c] = 0.f;
+    const long long off = (long long)((uintptr_t)row & 15);
+    for (long long o = c0 * 16 - off; o < len; o += 16ll * blockDim.x) {
+      if (o >= 0 && o + 16 <= len) {
+        *(uint4*)(row + o) = make_uint4(0u, 0u, 0u, 0u);
+      } else {
+        for (long long e = o < 0 ? 0 : o; e < len && e < o + 16; e += Z.es) {
+          if (Z.es == 2) *(unsigned short*)(row + e) = 0;
+          else *(float*)(row + e) = 0.f;
+        }
+      }
     }
   }
 }
@@ -557,7 +663,8 @@ struct EmbedGradArgs {
   long long out_stride;
   const int32_t* key;      // sorted tokens
   const int32_t* pos;      // their positions
-  float* partial;          // [2 * ranges][D]
+  float* partial;          // [2 * ranges][partial_stride]: columns as they lie in the token's row, see eg_first
+  long long partial_stride;
   int* counters;           // [2]: heads that go on for a few ranges, for many
   int4* heads;             // [2][ranges]: range, token, ranges that go on with it (few)
   int N, V;
@@ -573,43 +680,51 @@ constexpr int kEgMaxRange = 64;  // sorted positions per range
 constexpr int kEgBatch = 4;      // rows in flight
 constexpr int kEgMany = 32;      // ranges from which a token's partials are shared out among warps
 
-// Columns of thread t in slab s: VEC: 8 neighbouring ones; otherwise every blockDim-th.
-template <bool VEC>
-__device__ __forceinline__ long long eg_col(int slab, int i) {
-  const long long c0 = (long long)slab * blockDim.x * kEgCols;
-  return VEC ? c0 + (long long)threadIdx.x * kEgCols + i : c0 + (long long)i * blockDim.x + threadIdx.x;
+// A thread has eight neighbouring columns.  VEC: rows of a multiple of eight columns on 16-byte boundaries.
+// Otherwise the columns are cut at the 16-byte boundaries of the token's row in the table, which begins
+// eg_first columns behind one: what is written is aligned and what is read is shifted into place.
+template <int DTO>
+__device__ __forceinline__ int eg_first(const EmbedGradArgs& A, int token) {
+  constexpr int ES = DTO == kBF16 ? 2 : 4;
+  return (int)(((uintptr_t)A.out + (uintptr_t)((long long)token * A.out_stride * ES)) & 15) / ES;
 }
+__device__ __forceinline__ long long eg_place(int slab) { return ((long long)slab * blockDim.x + threadIdx.x) * kEgCols; }
 template <int DT, bool VEC>
 struct EgRow {
-  uint32_t w[VEC && DT == kBF16 ? 4 : 8];
+  static constexpr int kWords = DT == kBF16 ? 4 : 8;
+  uint32_t w[kWords + (VEC ? 0 : 4)];
+  int by;  // bytes that the columns begin behind w
 };
+// columns from c of the row at `row` into r; the tensor is [lo, hi)
 template <int DT, bool VEC>
-__device__ __forceinline__ void eg_load(EgRow<DT, VEC>& r, const char* row, int slab, long long D) {
+__device__ __forceinline__ void eg_load(EgRow<DT, VEC>& r, const char* row, long long c, long long D, uintptr_t lo, uintptr_t hi) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
-  if constexpr (VEC) {
-    const long long c = eg_col<true>(slab, 0);
-    if (c < D) {
-      const uint4 a = ld_global16(row + c * ES);
-      r.w[0] = a.x, r.w[1] = a.y, r.w[2] = a.z, r.w[3] = a.w;
-      if constexpr (DT == kF32) {
-        const uint4 b = ld_global16(row + c * ES + 16);
-        r.w[4] = b.x, r.w[5] = b.y, r.w[6] = b.z, r.w[7] = b.w;
-      }
-    }
-  } else {
+  constexpr int kLoads = (int)sizeof(r.w) / 16;
+  if (c >= D || c + kEgCols <= 0) return;
+  const uintptr_t q = (uintptr_t)row + (uintptr_t)(c * ES);
+  r.by = VEC ? 0 : (int)(q & 15);
 #pragma unroll
-    for (int i = 0; i < kEgCols; ++i) {
-      const long long c = eg_col<false>(slab, i);
-      r.w[i] = c < D ? __float_as_uint(load_logit<DT>(row, c)) : 0u;
-    }
+  for (int k = 0; k < kLoads; ++k) {
+    if (!VEC && k == kLoads - 1 && r.by == 0) continue;
+    const uint4 a = VEC ? ld_global16((const void*)(q + 16 * k)) : span_word<ES>(q - r.by + 16 * k, lo, hi);
+    r.w[4 * k] = a.x, r.w[4 * k + 1] = a.y, r.w[4 * k + 2] = a.z, r.w[4 * k + 3] = a.w;
   }
 }
 template <int DT, bool VEC>
-__device__ __forceinline__ float eg_get(const EgRow<DT, VEC>& r, int i) {
-  if constexpr (VEC && DT == kBF16)
-    return (i & 1) ? bf16_hi(r.w[i >> 1]) : bf16_lo(r.w[i >> 1]);
-  else
-    return __uint_as_float(r.w[i]);
+__device__ __forceinline__ void eg_add(float (&acc)[kEgCols], const EgRow<DT, VEC>& r) {
+  constexpr int kWords = EgRow<DT, VEC>::kWords;
+  uint32_t v[kWords];
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) v[i] = r.w[i];
+  } else {
+    shift_words<kWords>(r.w, r.by, v);
+  }
+#pragma unroll
+  for (int i = 0; i < kEgCols; ++i) {
+    if constexpr (DT == kBF16) acc[i] += (i & 1) ? bf16_hi(v[i >> 1]) : bf16_lo(v[i >> 1]);
+    else acc[i] += __uint_as_float(v[i]);
+  }
 }
 template <int DTO>
 __device__ __forceinline__ void eg_write1(const EmbedGradArgs& A, int token, long long c, float sum) {
@@ -619,59 +734,41 @@ __device__ __forceinline__ void eg_write1(const EmbedGradArgs& A, int token, lon
   store_elem<DTO>(row, c, v);
 }
 template <int DTO, bool VEC>
-__device__ __forceinline__ void eg_store(const EmbedGradArgs& A, int token, int slab, const float (&acc)[kEgCols]) {
+__device__ __forceinline__ void eg_store(const EmbedGradArgs& A, int token, long long c, const float (&acc)[kEgCols]) {
   constexpr int ES = DTO == kBF16 ? 2 : 4;
-  if constexpr (VEC) {
-    char* const row = A.out + (long long)token * A.out_stride * ES;
-    const long long c = eg_col<true>(slab, 0);
-    if (c >= A.D) return;
-    float v[kEgCols];
+  if (c >= A.D || c + kEgCols <= 0) return;
+  if (!VEC && (c < 0 || c + kEgCols > A.D)) {
 #pragma unroll
-    for (int i = 0; i < kEgCols; ++i) v[i] = acc[i] * A.scale;
-    uint4* const o = (uint4*)(row + c * ES);
-    if constexpr (DTO == kBF16) {
-      if (A.accumulate) {
-        const uint4 x = *o;
-        const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[2 * i] += bf16_lo(xw[i]);
-          v[2 * i + 1] += bf16_hi(xw[i]);
-        }
-      }
-      *o = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float4* const of = (float4*)o + h;
-        float4 x = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
-        if (A.accumulate) {
-          const float4 y = *of;
-          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
-        }
-        *of = x;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kEgCols; ++i) {
-      const long long c = eg_col<false>(slab, i);
-      if (c < A.D) eg_write1<DTO>(A, token, c, acc[i]);
-    }
+    for (int i = 0; i < kEgCols; ++i)
+      if (c + i >= 0 && c + i < A.D) eg_write1<DTO>(A, token, c + i, acc[i]);
+    return;
   }
-}
-template <bool VEC>
-__device__ __forceinline__ void eg_put(float* p, int slab, long long D, const float (&acc)[kEgCols]) {
-  if constexpr (VEC) {
-    const long long c = eg_col<true>(slab, 0);
-    if (c >= D) return;
-    *(float4*)(p + c) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    *(float4*)(p + c + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+  char* const row = A.out + (long long)token * A.out_stride * ES;
+  float v[kEgCols];
+#pragma unroll
+  for (int i = 0; i < kEgCols; ++i) v[i] = acc[i] * A.scale;
+  uint4* const o = (uint4*)(row + c * ES);
+  if constexpr (DTO == kBF16) {
+    if (A.accumulate) {
+      const uint4 x = *o;
+      const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[2 * i] += bf16_lo(xw[i]);
+        v[2 * i + 1] += bf16_hi(xw[i]);
+      }
+    }
+    *o = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
   } else {
 #pragma unroll
-    for (int i = 0; i < kEgCols; ++i) {
-      const long long c = eg_col<false>(slab, i);
-      if (c < D) p[c] = acc[i];
+    for (int h = 0; h < 2; ++h) {
+      float4* const of = (float4*)o + h;
+      float4 x = make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]);
+      if (A.accumulate) {
+        const float4 y = *of;
+        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+      }
+      *of = x;
     }
   }
 }
@@ -708,6 +805,8 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
       A.heads[(long long)many * A.ranges + atomicAdd(A.counters + many, 1)] = make_int4(range, sk[n], go, 0);
     }
   }
+  const long long place = eg_place(slab);
+  const uintptr_t lo = (uintptr_t)A.g, hi = lo + ((A.N - 1ll) * A.g_stride + A.D) * ES;
   float acc[kEgCols];
 #pragma unroll
   for (int i = 0; i < kEgCols; ++i) acc[i] = 0.f;
@@ -716,20 +815,24 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     EgRow<DT, VEC> rows[kEgBatch];
 #pragma unroll
     for (int q = 0; q < kEgBatch; ++q)
-      if (i + q < n && sk[i + q + 1] < A.V) eg_load<DT, VEC>(rows[q], A.g + (long long)sp[i + q] * A.g_stride * ES, slab, A.D);
+      if (i + q < n && sk[i + q + 1] < A.V)
+        eg_load<DT, VEC>(rows[q], A.g + (long long)sp[i + q] * A.g_stride * ES,
+                         place - (VEC ? 0 : eg_first<DTO>(A, sk[i + q + 1])), A.D, lo, hi);
 #pragma unroll
     for (int q = 0; q < kEgBatch; ++q) {
       if (i + q >= n) break;
       const int key = sk[i + q + 1];
       if (key >= A.V) return;  // only tokens outside the table from here on
-#pragma unroll
-      for (int c = 0; c < kEgCols; ++c) acc[c] += eg_get<DT, VEC>(rows[q], c);
+      eg_add<DT, VEC>(acc, rows[q]);
       if (sk[i + q + 2] != key || i + q + 1 == n) {  // the token's last position here
         const bool goes_on = sk[i + q + 2] == key;
-        if (from_before || goes_on)
-          eg_put<VEC>(A.partial + (2ll * range + (from_before ? 0 : 1)) * A.D, slab, A.D, acc);
-        else
-          eg_store<DTO, VEC>(A, key, slab, acc);
+        if (!from_before && !goes_on) {
+          eg_store<DTO, VEC>(A, key, place - (VEC ? 0 : eg_first<DTO>(A, key)), acc);
+        } else if (place < A.partial_stride) {
+          float* const p = A.partial + (2ll * range + (from_before ? 0 : 1)) * A.partial_stride + place;
+          *(float4*)p = make_float4(acc[0], acc[1], acc[2], acc[3]);
+          *(float4*)(p + 4) = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        }
         from_before = false;
 #pragma unroll
         for (int c = 0; c < kEgCols; ++c) acc[c] = 0.f;
@@ -740,30 +843,24 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
 
 // Joins the partials of the tokens that begin in a listed range and go on behind it: partial 2 r + 1
 // of that range, then 2 r of each range after it that starts with the token.  Work items: for heads of
-// a few ranges (head, W columns per thread); for heads of many (head, W columns per lane), whose
+// a few ranges (head, four columns per thread); for heads of many (head, four columns per lane), whose
 // ranges the CTA's eight warps share out, each adding its own in order.
-template <int W>
 struct EgVec {
-  float v[W];
+  float v[4];
 };
-template <int W>
-__device__ __forceinline__ EgVec<W> eg_partial(const float* p, bool on) {
-  EgVec<W> r;
-  if constexpr (W == 4) {
-    const float4 x = on ? *(const float4*)p : make_float4(0.f, 0.f, 0.f, 0.f);
-    r.v[0] = x.x, r.v[1] = x.y, r.v[2] = x.z, r.v[3] = x.w;
-  } else {
-    r.v[0] = on ? *p : 0.f;
-  }
-  return r;
+__device__ __forceinline__ EgVec eg_partial(const float* p, bool on) {
+  const float4 x = on ? *(const float4*)p : make_float4(0.f, 0.f, 0.f, 0.f);
+  return {{x.x, x.y, x.z, x.w}};
 }
-template <int DTO, int W>
+template <int DTO>
 __global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_constant__ EmbedGradArgs A, const ZeroShare share) {
   if (zero_share(A.zero, share)) return;
+  constexpr int W = 4;
   __shared__ float sums[kEgThreads][W];
   constexpr int kWarps = kEgThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t wide = (uint32_t)((A.D + W * kEgThreads - 1) / (W * kEgThreads)), narrow = (uint32_t)((A.D + W * 32 - 1) / (W * 32));
+  const long long places = A.partial_stride;
+  const uint32_t wide = (uint32_t)((places + W * kEgThreads - 1) / (W * kEgThreads)), narrow = (uint32_t)((places + W * 32 - 1) / (W * 32));
   const long long n_few = (long long)A.counters[0] * wide, n_items = n_few + (long long)A.counters[1] * narrow;
   for (long long it = blockIdx.x; it < n_items; it += share.from) {
     const bool many = it >= n_few;
@@ -781,14 +878,15 @@ __global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_con
         if (more < kEgThreads) break;
       }
     }
-    const bool on = c < A.D;
+    const int skip = eg_first<DTO>(A, h.y);  // place c is column c - skip
+    const bool on = c < places;
     const int from = many ? warp : 0, step = many ? kWarps : 1;
-    EgVec<W> acc = eg_partial<W>(A.partial + (2ll * h.x + 1) * A.D + c, on && from == 0);
-    const float* const p = A.partial + 2ll * (h.x + 1) * A.D + c;
+    EgVec acc = eg_partial(A.partial + (2ll * h.x + 1) * places + c, on && from == 0);
+    const float* const p = A.partial + 2ll * (h.x + 1) * places + c;
     for (int r = from; r < go; r += 8 * step) {
-      EgVec<W> x[8];
+      EgVec x[8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) x[q] = eg_partial<W>(p + 2ll * (r + q * step) * A.D, on && r + q * step < go);
+      for (int q = 0; q < 8; ++q) x[q] = eg_partial(p + 2ll * (r + q * step) * places, on && r + q * step < go);
 #pragma unroll
       for (int q = 0; q < 8; ++q)
 #pragma unroll
@@ -806,7 +904,8 @@ __global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_con
     }
     if (on && (!many || warp == 0)) {
 #pragma unroll
-      for (int e = 0; e < W; ++e) eg_write1<DTO>(A, h.y, c + e, acc.v[e]);
+      for (int e = 0; e < W; ++e)
+        if (c + e >= skip && c + e - skip < A.D) eg_write1<DTO>(A, h.y, c + e - skip, acc.v[e]);
     }
   }
 }

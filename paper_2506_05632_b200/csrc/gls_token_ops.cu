@@ -291,23 +291,23 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
   cudaStream_t st = (cudaStream_t)stream;
   const bool vec = D * es % 16 == 0 && table_stride * es % 16 == 0 && out_stride * es % 16 == 0 &&
                    (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0;
-  const uint32_t per_row = (uint32_t)(D * es / 16);
-  const bool rows_long = vec && per_row >= kEmbedLongRow;
-  const long long per_cta = rows_long ? kEmbedThreads / 32 : vec ? kEmbedThreads * kEmbedUnits : kEmbedThreads;
-  const long long units = rows_long ? N * ((per_row + 32 * kEmbedUnits - 1) / (32 * kEmbedUnits)) : vec ? N * per_row : N * D;
+  const uint32_t per_row = (uint32_t)(vec ? D * es / 16 : row_pieces(D * es, es));
+  const bool rows_long = per_row >= kEmbedLongRow;
+  const long long per_cta = rows_long ? kEmbedThreads / 32 : kEmbedThreads * kEmbedUnits;
+  const long long units = rows_long ? N * ((per_row + 32 * kEmbedUnits - 1) / (32 * kEmbedUnits)) : N * per_row;
   const long long want = (units + per_cta - 1) / per_cta, cap = 1 << 20;
   const int grid = (int)(want < cap ? want : cap);
-  const bool bf = dtype == GLS_BF16;
-  if (rows_long) {
-    if (bf) embed_long_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
-    else embed_long_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
-  } else if (vec) {
-    if (bf) embed_vec_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
-    else embed_vec_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A, per_row);
+#define EMBED(DT)                                                                               \
+  if (vec && rows_long) embed_long_kernel<DT><<<grid, kEmbedThreads, 0, st>>>(A, per_row);      \
+  else if (vec) embed_vec_kernel<DT><<<grid, kEmbedThreads, 0, st>>>(A, per_row);               \
+  else if (rows_long) embed_shift_kernel<DT, true><<<grid, kEmbedThreads, 0, st>>>(A, per_row); \
+  else embed_shift_kernel<DT, false><<<grid, kEmbedThreads, 0, st>>>(A, per_row)
+  if (dtype == GLS_BF16) {
+    EMBED(kBF16);
   } else {
-    if (bf) embed_any_kernel<kBF16><<<grid, kEmbedThreads, 0, st>>>(A);
-    else embed_any_kernel<kF32><<<grid, kEmbedThreads, 0, st>>>(A);
+    EMBED(kF32);
   }
+#undef EMBED
   return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
 }
 
@@ -326,6 +326,8 @@ static bool embed_grad_sizes_ok(int64_t N, int64_t V, int64_t D) {
 }
 // CTAs that write zeros beside a cluster that sorts (one per SM: the sort takes an SM's shared memory)
 constexpr int kZeroCtas = 140;
+// places of a partial: the columns, and up to seven before them where rows start off 16-byte boundaries
+static long long partial_places(int64_t D, bool vec) { return vec ? D : (D + 7 + kEgCols - 1) / kEgCols * kEgCols; }
 static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
   EmbedGradPlan p;
   int bits = 1;
@@ -362,7 +364,7 @@ static EmbedGradPlan embed_grad_plan(int64_t N, int64_t V, int64_t D) {
   p.zero_from = p.off_cnt + first;
   p.zero_bytes = at - p.zero_from;
   p.off_partial = at;
-  at += up256((size_t)p.ranges * 2 * (size_t)D * 4);
+  at += up256((size_t)p.ranges * 2 * (size_t)partial_places(D, false) * 4);
   p.total = at;
   return p;
 }
@@ -426,12 +428,10 @@ static cudaError_t launch_embed_grad(const EmbedGradArgs& A, ZeroDeal& deal, int
   const ZeroShare h = deal.take(rest - last, n_sum, each);
   cudaError_t err = launch_after(embed_grad_kernel<DT, DTO, VEC>, ZeroDeal::ctas(h), threads, st, A, h);
   if (err != cudaSuccess || A.ranges < 2) return err;
-  const int W = A.D % 4 == 0 ? 4 : 1;
-  const long long tiles = (A.D + W * kEgThreads - 1) / (W * kEgThreads) * A.ranges;
+  const long long tiles = (A.partial_stride + 4 * kEgThreads - 1) / (4 * kEgThreads) * A.ranges;
   const long long cap = (long long)sm_count() * 8;
   const ZeroShare j = deal.take(deal.V, (int)(tiles < cap ? tiles : cap), each);
-  return W == 4 ? launch_after(embed_join_kernel<DTO, 4>, ZeroDeal::ctas(j), kEgThreads, st, A, j)
-                : launch_after(embed_join_kernel<DTO, 1>, ZeroDeal::ctas(j), kEgThreads, st, A, j);
+  return launch_after(embed_join_kernel<DTO>, ZeroDeal::ctas(j), kEgThreads, st, A, j);
 }
 
 }  // namespace gls
@@ -470,9 +470,9 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   char* ws = (char*)workspace;
   const bool vec = D % kEgCols == 0 && grad_out_stride * es % 16 == 0 && grad_table_stride * eso % 16 == 0 &&
                    (uintptr_t)grad_out % 16 == 0 && (uintptr_t)grad_table % 16 == 0;
-  const long long per_thread = (D + kEgCols - 1) / kEgCols;
+  const long long places = partial_places(D, vec), per_thread = places / kEgCols;
   const int threads = (int)(per_thread < kEgThreads ? (per_thread + 31) / 32 * 32 : kEgThreads);
-  const long long slabs = (D + (long long)threads * kEgCols - 1) / ((long long)threads * kEgCols);
+  const long long slabs = (places + (long long)threads * kEgCols - 1) / ((long long)threads * kEgCols);
   if (slabs * P.ranges > (1LL << 30)) return GLS_ERR_UNSUPPORTED;
   ZeroArgs Z;
   Z.out = (char*)grad_table;
@@ -480,7 +480,8 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   Z.V = (int)V;
   Z.D = D;
   Z.es = eso;
-  Z.vec = (D * eso % 16 == 0 && grad_table_stride * eso % 16 == 0 && (uintptr_t)grad_table % 16 == 0) ? 1 : 0;
+  const bool even = D * eso % 16 == 0 && grad_table_stride * eso % 16 == 0 && (uintptr_t)grad_table % 16 == 0;
+  Z.units = even ? D * eso / 16 : row_pieces(D * eso, eso);
   Z.how = P.small ? kZeroByTokens : kZeroByBits;
   Z.touched = (const uint32_t*)(ws + P.off_touched);
   Z.tokens = tokens;
@@ -553,6 +554,7 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   A.accumulate = accumulate ? 1 : 0;
   A.scale = scale;
   A.slabs = (int)slabs;
+  A.partial_stride = places;
   A.zero = Z;
   if (P.small && !by_tokens) A.zero.how = kZeroByKeys;
   cudaError_t err;

@@ -513,6 +513,62 @@ def test_embedding_gradient(gls, dtype, N, V, D):
     ref.check_gradient(acc, before.double() + want, scale + ref.U * want.abs(), "accumulated")
 
 
+def _odd(rows, D, off, pad, dtype, fill):
+    """(buffer, its rows [rows, D]: `off` elements in, `pad` between them, nothing behind the last)"""
+    buf = torch.full((off + rows * (D + pad) - pad,), fill, dtype=dtype, device="cuda")
+    return buf, buf.as_strided((rows, D), (D + pad, 1), off)
+
+
+def _outside(buf, view):
+    out = torch.ones_like(buf, dtype=torch.bool)
+    out.as_strided(view.shape, view.stride(), view.storage_offset())[:] = False
+    return buf[out]
+
+
+ODD = [1, 2, 3, 5, 7, 8, 9, 15, 17, 31, 40, 63, 65, 129, 511, 515, 1002, 2051, 2283, 4101]
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("D", ODD)
+def test_embedding_of_odd_rows(gls, dtype, D):
+    V, N = 37, 301
+    tok = _tokens((N,), V, D)
+    tok[0], tok[1], tok[2], tok[N - 1] = V - 1, 0, -1, V - 1
+    for n, (off, pad, ooff, opad) in enumerate([(0, 0, 0, 0), (1, 0, 0, 0), (0, 0, 1, 0), (3, 1, 5, 2), (7, 8, 2, 0), (8, 0, 3, 5)]):
+        buf, table = _odd(V, D, off, pad, dtype, float("nan"))  # what lies between the rows is not used
+        table.copy_(torch.randn((V, D), generator=_gen(D + n), device="cuda"))
+        obuf, out = _odd(N, D, ooff, opad, dtype, 3.0)
+        for scale in (1.0, -0.3):
+            gls.embed_tokens(table, tok, scale=scale, out=out)
+            want = table.double()[tok.long().clamp(min=0)] * ref.f32(scale) * (tok >= 0).double()[:, None]
+            ref.near(out, want, (ref.HALF[dtype] + 2 * ref.U) * want.abs() * (scale != 1.0), "D=%d %d" % (D, n))
+            assert bool((_outside(obuf, out) == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(F, F), (BF, BF), (BF, F)])
+@pytest.mark.parametrize("D", ODD)
+def test_embedding_gradient_of_odd_rows(gls, dtype, out_dtype, D):
+    for n, (N, V, off, pad, ooff, opad) in enumerate([(300, 40, 0, 0, 0, 0), (700, 900, 1, 0, 3, 0), (3000, 5, 3, 2, 1, 1),
+                                                      (20000, 70, 0, 1, 2, 0), (40, 3000, 5, 0, 0, 7)]):
+        if N * D > 1 << 23:
+            continue
+        _, g = _odd(N, D, off, pad, dtype, float("nan"))
+        g.copy_(torch.randn((N, D), generator=_gen(D + n), device="cuda"))
+        tok = _skewed(N, V, D + n)
+        want, scale = _embed_grad_ref(g, tok, V, 0.3)
+        buf, out = _odd(V, D, ooff, opad, out_dtype, 3.0)
+        gls.embed_tokens_backward(g, tok, V, scale=0.3, grad_table=out)
+        ref.check_gradient(out, want, scale, "D=%d %d" % (D, n))
+        assert bool((_outside(buf, out) == 3.0).all())
+        first = out.clone()
+        gls.embed_tokens_backward(g, tok, V, scale=0.3, grad_table=out, accumulate=True)
+        # the sum is rounded to the output's type, which check_gradient counts
+        ref.check_gradient(out, first.double() + want, scale + ref.U * (first.double().abs() + want.abs()), "accumulated %d" % n)
+        touched = torch.zeros(V, dtype=torch.bool, device="cuda")
+        touched[tok.long()[tok >= 0]] = True
+        assert torch.equal(out[~touched], first[~touched]) and bool((_outside(buf, out) == 3.0).all())
+
+
 @pytest.mark.parametrize("dtype", [F, BF])
 def test_embedding_gradient_special(gls, dtype):
     V, D = 100, 48
