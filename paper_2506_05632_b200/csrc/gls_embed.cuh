@@ -256,6 +256,19 @@ struct ZeroArgs {
 };
 constexpr int kZeroRows = 16384;  // rows per CTA at most, except by bits
 
+// `len` bytes from `p`, by the calling warp
+__device__ __forceinline__ void zero_span(char* p, long long len, int es) {
+  for (long long o = (long long)(threadIdx.x & 31) * 16 - (long long)((uintptr_t)p & 15); o < len; o += 512) {
+    if (o >= 0 && o + 16 <= len) {
+      *(uint4*)(p + o) = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+      for (long long e = o < 0 ? 0 : o; e < len && e < o + 16; e += es) {
+        if (es == 2) *(unsigned short*)(p + e) = 0;
+        else *(float*)(p + e) = 0.f;
+      }
+    }
+  }
+}
 // Rows [first, last) of tokens that do not occur, by the calling CTA.
 __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, long long last) {
   __shared__ uint32_t here[kZeroRows / 32];
@@ -296,6 +309,32 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, lo
       }
     }
     __syncthreads();
+  }
+  const int warps = (int)(blockDim.x >> 5);
+  if (Z.out_stride == Z.D && last - first >= 4 * warps) {
+    // Rows without gaps between them: each warp writes its rows' runs, whatever a row's size and alignment.
+    const long long part = (last - first + warps - 1) / warps, base = look ? first : 0ll, row = Z.D * Z.es;
+    const long long a = first + (threadIdx.x >> 5) * part, b = min(last, a + part);
+    auto bits = [&](long long v) { return look ? here[(v - base) >> 5] : __ldg(Z.touched + (v >> 5)); };
+    for (long long v = a; v < b;) {
+      const int at = (int)((v - base) & 31);
+      const uint32_t w = bits(v) >> at;
+      if (w & 1u) {  // rows that occur
+        v += min(~w != 0u ? __ffs(~w) - 1 : 32, 32 - at);
+        continue;
+      }
+      long long e = v + (w != 0u ? __ffs(w) - 1 : 32 - at);
+      while (w == 0u && e < b) {
+        const uint32_t x = bits(e);
+        e += x != 0u ? __ffs(x) - 1 : 32;
+        if (x != 0u) break;
+      }
+      e = min(e, b);
+      char* const from = Z.out + v * row;
+      zero_span(from, (e - v) * row, Z.es);
+      v = e;
+    }
+    return;
   }
   // rows side by side where one does not fill the CTA
   const long long units = Z.units, len = Z.D * Z.es;
@@ -695,19 +734,27 @@ struct EgRow {
   uint32_t w[kWords + (VEC ? 0 : 4)];
   int by;  // bytes that the columns begin behind w
 };
-// columns from c of the row at `row` into r; the tensor is [lo, hi)
+// The words that hold the columns at `at[q]`; the tensor is [lo, hi).  All loads are on their way together.
 template <int DT, bool VEC>
-__device__ __forceinline__ void eg_load(EgRow<DT, VEC>& r, const char* row, long long c, long long D, uintptr_t lo, uintptr_t hi) {
-  constexpr int ES = DT == kBF16 ? 2 : 4;
-  constexpr int kLoads = (int)sizeof(r.w) / 16;
-  if (c >= D || c + kEgCols <= 0) return;
-  const uintptr_t q = (uintptr_t)row + (uintptr_t)(c * ES);
-  r.by = VEC ? 0 : (int)(q & 15);
+__device__ __forceinline__ void eg_load(EgRow<DT, VEC> (&r)[kEgBatch], const uintptr_t (&at)[kEgBatch], uintptr_t lo, uintptr_t hi) {
+  constexpr int kLoads = (int)sizeof(r[0].w) / 16;
+  bool inside = true;
 #pragma unroll
-  for (int k = 0; k < kLoads; ++k) {
-    if (!VEC && k == kLoads - 1 && r.by == 0) continue;
-    const uint4 a = VEC ? ld_global16((const void*)(q + 16 * k)) : span_word<ES>(q - r.by + 16 * k, lo, hi);
-    r.w[4 * k] = a.x, r.w[4 * k + 1] = a.y, r.w[4 * k + 2] = a.z, r.w[4 * k + 3] = a.w;
+  for (int q = 0; q < kEgBatch; ++q) {
+    r[q].by = VEC ? 0 : (int)(at[q] & 15);
+    inside = inside && at[q] - r[q].by >= lo && at[q] - r[q].by + 16 * kLoads <= hi;
+  }
+  auto put = [&](int q, int k, uint4 a) { r[q].w[4 * k] = a.x, r[q].w[4 * k + 1] = a.y, r[q].w[4 * k + 2] = a.z, r[q].w[4 * k + 3] = a.w; };
+  if (VEC || inside) {
+#pragma unroll
+    for (int q = 0; q < kEgBatch; ++q)
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) put(q, k, ld_global16((const void*)(at[q] - r[q].by + 16 * k)));
+  } else {
+#pragma unroll
+    for (int q = 0; q < kEgBatch; ++q)
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) put(q, k, span_word<DT == kBF16 ? 2 : 4>(at[q] - r[q].by + 16 * k, lo, hi));
   }
 }
 template <int DT, bool VEC>
@@ -806,6 +853,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     }
   }
   const long long place = eg_place(slab);
+  if (place >= A.partial_stride || sk[1] >= A.V) return;  // no column, only tokens outside the table
   const uintptr_t lo = (uintptr_t)A.g, hi = lo + ((A.N - 1ll) * A.g_stride + A.D) * ES;
   float acc[kEgCols];
 #pragma unroll
@@ -813,11 +861,15 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
   bool from_before = sk[1] == sk[0];
   for (int i = 0; i < n; i += kEgBatch) {
     EgRow<DT, VEC> rows[kEgBatch];
+    uintptr_t at[kEgBatch];
 #pragma unroll
-    for (int q = 0; q < kEgBatch; ++q)
-      if (i + q < n && sk[i + q + 1] < A.V)
-        eg_load<DT, VEC>(rows[q], A.g + (long long)sp[i + q] * A.g_stride * ES,
-                         place - (VEC ? 0 : eg_first<DTO>(A, sk[i + q + 1])), A.D, lo, hi);
+    for (int q = 0; q < kEgBatch; ++q) {
+      const int p = min(i + q, n - 1);  // behind the range and outside the table: any row, not used
+      long long c = place - (VEC ? 0 : eg_first<DTO>(A, sk[p + 1]));
+      if (!VEC && (c >= A.D || c + kEgCols <= 0)) c = 0;  // no column of this token: not used
+      at[q] = lo + (uintptr_t)(((long long)sp[p] * A.g_stride + c) * ES);
+    }
+    eg_load<DT, VEC>(rows, at, lo, hi);
 #pragma unroll
     for (int q = 0; q < kEgBatch; ++q) {
       if (i + q >= n) break;
@@ -848,9 +900,10 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
 struct EgVec {
   float v[4];
 };
-__device__ __forceinline__ EgVec eg_partial(const float* p, bool on) {
-  const float4 x = on ? *(const float4*)p : make_float4(0.f, 0.f, 0.f, 0.f);
-  return {{x.x, x.y, x.z, x.w}};
+__device__ __forceinline__ EgVec eg_partial(const float* p) {
+  EgVec x;
+  asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x.v[0]), "=f"(x.v[1]), "=f"(x.v[2]), "=f"(x.v[3]) : "l"(p));
+  return x;
 }
 template <int DTO>
 __global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_constant__ EmbedGradArgs A, const ZeroShare share) {
@@ -881,16 +934,18 @@ __global__ void __launch_bounds__(kEgThreads) embed_join_kernel(const __grid_con
     const int skip = eg_first<DTO>(A, h.y);  // place c is column c - skip
     const bool on = c < places;
     const int from = many ? warp : 0, step = many ? kWarps : 1;
-    EgVec acc = eg_partial(A.partial + (2ll * h.x + 1) * places + c, on && from == 0);
-    const float* const p = A.partial + 2ll * (h.x + 1) * places + c;
+    const long long cc = on ? c : 0;
+    EgVec acc = eg_partial(A.partial + (2ll * h.x + 1) * places + cc);
+    if (from != 0) acc = {{0.f, 0.f, 0.f, 0.f}};
+    const float* const p = A.partial + 2ll * (h.x + 1) * places + cc;
     for (int r = from; r < go; r += 8 * step) {
       EgVec x[8];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) x[q] = eg_partial(p + 2ll * (r + q * step) * places, on && r + q * step < go);
+      for (int q = 0; q < 8; ++q) x[q] = eg_partial(p + 2ll * min(r + q * step, go - 1) * places);
 #pragma unroll
       for (int q = 0; q < 8; ++q)
 #pragma unroll
-        for (int e = 0; e < W; ++e) acc.v[e] += x[q].v[e];
+        for (int e = 0; e < W; ++e) acc.v[e] += r + q * step < go ? x[q].v[e] : 0.f;
     }
     if (many) {
 #pragma unroll
