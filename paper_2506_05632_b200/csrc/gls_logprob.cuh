@@ -923,7 +923,12 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
   const int mis = (int)((uintptr_t)rl.rowp & 31) / ES;
   const int end = mis + A.V;
   const int n_steps = (end + kStep - 1) / kStep;
-  const int first = rank * kClWarps + warp, stride = ctas * kClWarps;
+  // Many steps: a CTA's warps take neighbouring ones (600 rows of 128256: 52 us, 55 dealt the other way); few:
+  // they go to the CTAs in turn, so that the CTAs' shares differ by one at most.
+  const int stride = ctas * kClWarps;
+  const bool few = n_steps < 2 * stride;
+  const int per_warp = few ? ctas : 1, per_rank = few ? 1 : kClWarps;
+  const int first = warp * per_warp + rank * per_rank;
   const int mine = first < n_steps ? (n_steps - 1 - first) / stride + 1 : 0;  // steps of this warp
   const int es = entry_shift((n_steps - 1) / stride + 1, kClEntries), in_entry = (1 << es) - 1;
   EntryColumn col = {&sh.entry[warp][0][lane], mine > 0 ? ((mine - 1) >> es) + 1 : 0};
@@ -955,11 +960,15 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
     }
     score_step<DT, ENT>(g, mx, c2, sums, masked);
   }
-  // Warps of this CTA that have a step; each vouches for `share` tokens at or above its own bound, so
-  // that M tokens of the row are at or above the smallest of them.
-  const int busy = min(kClWarps, max(0, n_steps - rank * kClWarps));
+  // Warps of this CTA that have a step, a whole one if any has; each vouches for `share` tokens at or above
+  // its own bound, so that M tokens of the row are at or above the smallest of them.  (The row's last step
+  // may hold fewer groups than a share: 90 rows of 12420, M = 50, 31 -> 15 us.)
+  const int whole = few ? min(kClWarps, (max(0, end / kStep - rank) + ctas - 1) / ctas) : kClWarps;
+  const int busy = whole > 0 ? whole : min(kClWarps, (max(0, n_steps - rank) + ctas - 1) / ctas);
   if (A.M > 0 && mine > 0) {
     if (col.n & 1) col.put(col.n, 0xff80u);
+  }
+  if (A.M > 0 && warp < busy) {
     const uint32_t b = entry_bound(col, (A.M + busy - 1) / busy);
     if (lane == 0) sh.bound[warp] = b;
   }
@@ -993,7 +1002,7 @@ score_cluster_kernel(const __grid_constant__ ScoreArgs A, int ctas) {
       for (int i = tid; i < (listed << es) * NG; i += kClThreads) {
         const int id = sh.list[i / NG >> es];
         const int k = ((id >> 5) % kClEntries << es) + (i / NG & in_entry);  // the warp's k-th step
-        const int step = rank * kClWarps + id / (kClEntries * 32) + k * stride;
+        const int step = id / (kClEntries * 32) * per_warp + rank * per_rank + k * stride;
         const int v = step * kStep + (i % NG) * 512 + (id & 31) * 16;
         if (step < n_steps && v < end) {
           group_fetch<DT>(stage, rl.rowp, v, mis, end);

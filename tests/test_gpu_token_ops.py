@@ -75,6 +75,15 @@ def test_logprobs_many_alternatives_of_short_rows(gls, dtype, V):
 
 
 @pytest.mark.parametrize("dtype", [F, BF])
+@pytest.mark.parametrize("V", [6150, 10189, 12420, 16385, 33000, 61898])
+def test_logprobs_short_last_step(gls, dtype, V):
+    for B, M in [(1, 33), (7, 50), (90, 50), (3, 256)]:
+        x = _logits((B, 1, 1, V), dtype, V + M)
+        x[0, 0, 0, -100:] += 20  # the last step has the best
+        _check(gls, x, _tokens((B, 1, 1), V, M), M, 1.25, what="V=%d M=%d %s" % (V, M, dtype))
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
 @pytest.mark.parametrize("M", [20, 64, 65, 128, 129, 256])
 def test_logprobs_alternatives(gls, dtype, M):
     for B, K, J, V in [(1, 1, 1, 152064), (1, 2, 1, 200), (3, 1, 2, 20000)]:
