@@ -522,7 +522,9 @@ int gls_token_logprobs_backward(const gls_rows_t* logits, int B, int K, int J, i
  *
  *   table [V,D], out [N,D]: of one type (gls_dtype_t), rows contiguous, strides in elements and
  *   at least D (table_stride is ignored for V = 1, out_stride for N = 1); N = 0 is legal.
- *   16-byte aligned rows take vector loads, others are copied element by element.
+ *   Rows may start at any element and have any size.  They are read in aligned 16-byte words, which may
+ *   hold elements beside or between the rows (not used), but nothing in front of the table's first
+ *   element or behind its last.  Nothing but the N rows is written.
  */
 int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t V, int64_t D,
                      const int32_t* tokens, int64_t N, float scale, void* out, int64_t out_stride,
@@ -536,7 +538,7 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
  * read nor written.
  *
  *   grad_out [N,D] of type `dtype`; grad_table [V,D] of type `grad_dtype`: the same, or fp32 for
- *   bf16 grad_out; strides as above
+ *   bf16 grad_out; strides, sizes and alignment as above
  *   workspace  gls_embed_tokens_backward_workspace_bytes(N, V, D) bytes, 16-byte aligned; its
  *              contents on entry are ignored (may be NULL when N = 0)
  * N < 2^30.

@@ -70,7 +70,7 @@ static int score_ctas(long long rows, long long V, int M, int dtype) {
   int best = 0;
   for (int c = 1; c <= kClMaxCtas; c *= 2) {
     // a CTA's bound on the M-th logit comes from 32 maxima per step: with fewer than 2 M of them so many
-    // tokens reach it that the buffers overflow (4 rows of 152064, M = 256: 234 us by 8 CTAs each)
+    // tokens reach it that the buffers overflow and the radix selection has to read the row again
     if (c > 1 && 16.0 * steps < (double)c * M) break;
     const double waves = (double)rows * c / slots, each = std::ceil(steps / (c * kClWarps));
     const double t = 9.0 + (waves <= 1.0 ? each * (0.5 + 1.2 * waves) : (waves + 0.35) * (4.0 + 1.5 * each));
