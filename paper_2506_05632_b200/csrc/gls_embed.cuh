@@ -172,64 +172,114 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_long_kernel(const __grid_
     }
   }
 }
-// Any alignment, any D: a unit is one of the `per_row` 16-byte pieces that an output row can touch.  Units are
-// dealt as in the two kernels above (LONG: to warps within a row).  One element a thread instead took
-// 535 us for 97450 rows of 1002 fp32.
-template <int DT, bool LONG>
+// Any alignment, any D: a unit is one of the `per_row` 16-byte pieces that an output row can touch.  One
+// element a thread instead took 535 us for 97450 rows of 1002 fp32.
+template <int DT>
+__device__ __forceinline__ uint4 embed_shifted(const uint32_t (&w)[8], int by, float scale, bool scaled) {
+  uint32_t v[4];
+  shift_words<4>(w, by, v);
+  if (scaled) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = scale_word<DT>(v[i], scale);
+  }
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+template <int DT>
 __global__ void __launch_bounds__(kEmbedThreads) embed_shift_kernel(const __grid_constant__ EmbedArgs A, uint32_t per_row) {
+  constexpr int ES = DT == kBF16 ? 2 : 4;
+  const long long len = A.D * ES;
+  const uintptr_t lo = (uintptr_t)A.table, hi = lo + ((A.V - 1) * A.table_stride + A.D) * ES;
+  const long long n_units = A.N * per_row;
+  constexpr int kUnits = 2;  // in flight: 48 registers (300000 rows of 37 fp32 24 us; four of them, 76: 28)
+  for (long long u0 = (long long)blockIdx.x * (kEmbedThreads * kEmbedUnits) + threadIdx.x; u0 < n_units;
+       u0 += (long long)gridDim.x * (kEmbedThreads * kEmbedUnits)) {
+#pragma unroll 1
+    for (int half = 0; half < kEmbedUnits; half += kUnits) {
+      uint32_t w[kUnits][8];
+      long long o[kUnits];
+      char* to[kUnits];
+      int by[kUnits];
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j) {
+        const long long it = u0 + (half + j) * kEmbedThreads;
+        to[j] = nullptr;
+        by[j] = -1;  // zeros
+        o[j] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[j][i] = 0u;
+        if (it >= n_units) continue;
+        const long long n = it < (1ll << 32) ? (long long)((uint32_t)it / per_row) : it / per_row;
+        const uint32_t u = (uint32_t)(it - n * per_row);
+        char* const row = A.out + n * A.out_stride * ES;
+        o[j] = (long long)u * 16 - (long long)((uintptr_t)row & 15);
+        if (o[j] >= len) continue;
+        to[j] = row;
+        const int t = __ldg(A.tokens + n);
+        if (t >= 0 && t < A.V) {
+          const uintptr_t q = lo + (uintptr_t)((long long)t * A.table_stride * ES + o[j]);
+          by[j] = (int)(q & 15);
+          const uint4 x = span_word<ES>(q - by[j], lo, hi);
+          w[j][0] = x.x, w[j][1] = x.y, w[j][2] = x.z, w[j][3] = x.w;
+          if (by[j] != 0) {
+            const uint4 y = span_word<ES>(q - by[j] + 16, lo, hi);
+            w[j][4] = y.x, w[j][5] = y.y, w[j][6] = y.z, w[j][7] = y.w;
+          }
+        } else if (t >= A.V && u == 0 && A.status != nullptr) {
+          atomicOr(A.status, kDevBadToken);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j)
+        if (to[j] != nullptr)
+          row_put16<ES>(to[j], o[j], len, embed_shifted<DT>(w[j], max(by[j], 0), A.scale, by[j] >= 0 && A.scale != 1.0f));
+    }
+  }
+}
+// Long rows: a warp takes up to 128 units of one row, whose shift is the same for all of them (97450 rows of
+// 1002 fp32 111 us; 65536 of 2283 bf16 148, and 192 with a row, an offset and a shift per unit).
+template <int DT>
+__global__ void __launch_bounds__(kEmbedThreads) embed_shift_long_kernel(const __grid_constant__ EmbedArgs A, uint32_t per_row) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
   const int lane = threadIdx.x & 31;
   const long long len = A.D * ES;
   const uintptr_t lo = (uintptr_t)A.table, hi = lo + ((A.V - 1) * A.table_stride + A.D) * ES;
-  const uint32_t pieces = LONG ? (per_row + 32 * kEmbedUnits - 1) / (32 * kEmbedUnits) : per_row;
+  const uint32_t pieces = (per_row + 32 * kEmbedUnits - 1) / (32 * kEmbedUnits);
   const long long n_items = A.N * pieces;
-  const long long per_cta = LONG ? kEmbedThreads / 32 : kEmbedThreads * kEmbedUnits;
-  for (long long i0 = (long long)blockIdx.x * per_cta + (LONG ? threadIdx.x >> 5 : threadIdx.x); i0 < n_items;
-       i0 += (long long)gridDim.x * per_cta) {
-    uint32_t w[kEmbedUnits][8];
-    long long o[kEmbedUnits];
-    char* to[kEmbedUnits];
-    int by[kEmbedUnits];
+  for (long long it = (long long)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5); it < n_items;
+       it += (long long)gridDim.x * (kEmbedThreads / 32)) {
+    const long long n = it < (1ll << 32) ? (long long)((uint32_t)it / pieces) : it / pieces;
+    const uint32_t u0 = (uint32_t)(it - n * pieces) * (32 * kEmbedUnits) + lane;
+    char* const row = A.out + n * A.out_stride * ES;
+    const long long o = (long long)u0 * 16 - (long long)((uintptr_t)row & 15);
+    const int t = __ldg(A.tokens + n);
+    const bool in = t >= 0 && t < A.V;
+    if (t >= A.V && u0 == 0 && A.status != nullptr) atomicOr(A.status, kDevBadToken);
+    const uintptr_t q = lo + (uintptr_t)((in ? (long long)t * A.table_stride * ES : 0ll) + o);
+    const int by = (int)(q & 15);
+    const bool scaled = in && A.scale != 1.0f;
+    const uintptr_t from = q - by;
+    constexpr long long kLast = 512 * (kEmbedUnits - 1);
+    if (in && o >= 0 && o + kLast + 16 <= len && from >= lo && from + kLast + 32 <= hi) {
+      uint32_t w[kEmbedUnits][8];
 #pragma unroll
-    for (int j = 0; j < kEmbedUnits; ++j) {
-      const long long it = LONG ? i0 : i0 + j * kEmbedThreads;
-      to[j] = nullptr;
-      by[j] = -1;  // zeros
-      o[j] = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[j][i] = 0u;
-      if (it >= n_items) continue;
-      const long long n = it < (1ll << 32) ? (long long)((uint32_t)it / pieces) : it / pieces;
-      const uint32_t p = (uint32_t)(it - n * pieces);
-      const uint32_t u = LONG ? p * (32 * kEmbedUnits) + 32 * j + lane : p;
-      char* const row = A.out + n * A.out_stride * ES;
-      o[j] = (long long)u * 16 - (long long)((uintptr_t)row & 15);
-      if (o[j] >= len) continue;
-      to[j] = row;
-      const int t = __ldg(A.tokens + n);
-      if (t >= 0 && t < A.V) {
-        const uintptr_t q = lo + (uintptr_t)((long long)t * A.table_stride * ES + o[j]);
-        by[j] = (int)(q & 15);
-        const uint4 x = span_word<ES>(q - by[j], lo, hi);
+      for (int j = 0; j < kEmbedUnits; ++j) {
+        const uint4 x = ld_global16((const void*)(from + 512 * j)), y = ld_global16((const void*)(from + 512 * j + 16));
         w[j][0] = x.x, w[j][1] = x.y, w[j][2] = x.z, w[j][3] = x.w;
-        if (by[j] != 0) {
-          const uint4 y = span_word<ES>(q - by[j] + 16, lo, hi);
-          w[j][4] = y.x, w[j][5] = y.y, w[j][6] = y.z, w[j][7] = y.w;
+        w[j][4] = y.x, w[j][5] = y.y, w[j][6] = y.z, w[j][7] = y.w;
+      }
+#pragma unroll
+      for (int j = 0; j < kEmbedUnits; ++j) *(uint4*)(row + o + 512 * j) = embed_shifted<DT>(w[j], by, A.scale, scaled);
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < kEmbedUnits; ++j) {
+        if (o + 512 * j >= len) break;
+        uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+        if (in) {
+          const uint4 x = span_word<ES>(from + 512 * j, lo, hi), y = span_word<ES>(from + 512 * j + 16, lo, hi);
+          w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w, w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
         }
-      } else if (t >= A.V && u == 0 && A.status != nullptr) {
-        atomicOr(A.status, kDevBadToken);
+        row_put16<ES>(row, o + 512 * j, len, embed_shifted<DT>(w, by, A.scale, scaled));
       }
-    }
-#pragma unroll
-    for (int j = 0; j < kEmbedUnits; ++j) {
-      if (to[j] == nullptr) continue;
-      uint32_t v[4];
-      shift_words<4>(w[j], max(by[j], 0), v);
-      if (by[j] >= 0 && A.scale != 1.0f) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = scale_word<DT>(v[i], A.scale);
-      }
-      row_put16<ES>(to[j], o[j], len, make_uint4(v[0], v[1], v[2], v[3]));
     }
   }
 }

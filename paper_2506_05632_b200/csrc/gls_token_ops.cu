@@ -300,8 +300,8 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
 #define EMBED(DT)                                                                               \
   if (vec && rows_long) embed_long_kernel<DT><<<grid, kEmbedThreads, 0, st>>>(A, per_row);      \
   else if (vec) embed_vec_kernel<DT><<<grid, kEmbedThreads, 0, st>>>(A, per_row);               \
-  else if (rows_long) embed_shift_kernel<DT, true><<<grid, kEmbedThreads, 0, st>>>(A, per_row); \
-  else embed_shift_kernel<DT, false><<<grid, kEmbedThreads, 0, st>>>(A, per_row)
+  else if (rows_long) embed_shift_long_kernel<DT><<<grid, kEmbedThreads, 0, st>>>(A, per_row);  \
+  else embed_shift_kernel<DT><<<grid, kEmbedThreads, 0, st>>>(A, per_row)
   if (dtype == GLS_BF16) {
     EMBED(kBF16);
   } else {
