@@ -6,6 +6,7 @@ import shutil
 import subprocess
 import sysconfig
 import threading
+import warnings
 
 import torch
 
@@ -13,7 +14,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 _SRC_DIR = os.path.join(_HERE, "csrc")
 _LIB = os.path.join(_HERE, "libgls.so")
-_CALLS_LIB = os.path.join(_HERE, "gls_torch_calls.so")
+# The compiled calls use the layout of this Python's and this torch's objects: a module made for others has
+# another name and is not loaded.
+_CALLS_LIB = os.path.join(_HERE, "gls_torch_calls.%s-torch%s-cuda%s.so" % (
+    sysconfig.get_config_var("SOABI"), torch.__version__, torch.version.cuda))
 
 COMBINE_ACTIVE, COMBINE_ALL, NO_BONUS = 0, 1, 2
 VERIFY_ALL_ROWS, VERIFY_ACTIVE_ROWS = 4, 8  # how the dense verify call walks Algorithm 2
@@ -64,23 +68,57 @@ def _build_calls(force):
 
 def build(force=False, verbose=False, debug_bounds=False):
     """Compile csrc/*.cu into libgls.so for sm_100a with nvcc (cross-compiles without a GPU), and
-    csrc/torch_calls.cpp beside it."""
-    _build_calls(force)
+    csrc/torch_calls.cpp beside it; warns when the latter can not be compiled (see _GeneralWay)."""
     srcs = _sources()
-    if (not force and os.path.exists(_LIB)
-            and os.path.getmtime(_LIB) >= max(os.path.getmtime(s) for s in srcs)):
-        return _LIB
-    cus = [s for s in srcs if s.endswith(".cu")]
-    tmp = _LIB + ".tmp%d" % os.getpid()
-    cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", tmp] + cus
-    if debug_bounds or os.environ.get("GLS_DEBUG_BOUNDS") == "1":
-        cmd.insert(1, "-DGLS_DEBUG_BOUNDS")  # range checks of the kernels' own indices
-    if verbose:
-        cmd.insert(1, "-Xptxas=-v")
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, _LIB)
+    if force or not os.path.exists(_LIB) or os.path.getmtime(_LIB) < max(os.path.getmtime(s) for s in srcs):
+        cus = [s for s in srcs if s.endswith(".cu")]
+        tmp = _LIB + ".tmp%d" % os.getpid()
+        cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+               "-shared", "-Xcompiler", "-fPIC", "-o", tmp] + cus
+        if debug_bounds or os.environ.get("GLS_DEBUG_BOUNDS") == "1":
+            cmd.insert(1, "-DGLS_DEBUG_BOUNDS")  # range checks of the kernels' own indices
+        if verbose:
+            cmd.insert(1, "-Xptxas=-v")
+        subprocess.run(cmd, check=True)
+        os.replace(tmp, _LIB)
+    try:
+        _build_calls(force)
+    except (OSError, subprocess.CalledProcessError) as e:
+        _without_calls(e)
     return _LIB
+
+
+class _GeneralWay:
+    """Stands in for the compiled calls where they can not be had: declines every call, which binding.py
+    then makes through ctypes, with the same kernels and results and 10 us more of host time."""
+
+    def __getattr__(self, name):
+        return self._decline
+
+    @staticmethod
+    def _decline(*args):
+        return None
+
+
+def _without_calls(error):
+    warnings.warn("%s can not be used (%s): the calls that it shortens are made through ctypes"
+                  % (os.path.basename(_CALLS_LIB), error), RuntimeWarning, stacklevel=3)
+
+
+def _load_calls(L):
+    """The compiled calls with the entry points of the library L."""
+    try:
+        if not os.path.exists(_CALLS_LIB):
+            _build_calls(False)
+        spec = importlib.util.spec_from_file_location("gls_torch_calls", _CALLS_LIB)
+        calls = importlib.util.module_from_spec(spec)
+        calls.entry_points(*(C.cast(getattr(L, "gls_" + n), C.c_void_p).value for n in (
+            "token_logprobs", "emitted_logprobs", "token_logprobs_backward", "embed_tokens",
+            "embed_tokens_backward_workspace_bytes", "embed_tokens_backward")))
+        return calls
+    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        _without_calls(e)
+        return _GeneralWay()
 
 
 class _Rows(C.Structure):
@@ -100,12 +138,12 @@ class _Noise(C.Structure):
 
 
 def load():
-    """Load libgls.so (building it if the sources are newer and nvcc is present)."""
+    """Load libgls.so (building it if it is not there), and the compiled calls beside it where they can be had."""
     global _lib, _calls
     with _lock:
         if _lib is not None:
             return _lib
-        if not os.path.exists(_LIB) or not os.path.exists(_CALLS_LIB):
+        if not os.path.exists(_LIB):
             build()
         L = C.CDLL(_LIB)
         L.gls_version.restype = C.c_int
@@ -194,12 +232,7 @@ def load():
         L.gls_embed_tokens_backward.argtypes = [
             C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_float,
             C.c_void_p, C.c_int, C.c_int64, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
-        spec = importlib.util.spec_from_file_location("gls_torch_calls", _CALLS_LIB)
-        calls = importlib.util.module_from_spec(spec)
-        calls.entry_points(*(C.cast(getattr(L, "gls_" + n), C.c_void_p).value for n in (
-            "token_logprobs", "emitted_logprobs", "token_logprobs_backward", "embed_tokens",
-            "embed_tokens_backward_workspace_bytes", "embed_tokens_backward")))
-        _calls = calls
+        _calls = _load_calls(L)
         _lib = L
         return _lib
 
