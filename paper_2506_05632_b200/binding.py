@@ -9,6 +9,7 @@ import threading
 import warnings
 
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
@@ -707,6 +708,14 @@ def _fast():
     return _calls
 
 
+def _no_tangent(*tensors):
+    """The operators have no forward-mode derivative: a result without the tangent would be a wrong one."""
+    if getattr(forward_ad, "_current_level", 0) >= 0:  # within torch.autograd.forward_ad.dual_level()
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None:
+                raise GlsError("there is no forward-mode derivative: the call takes no tensor with a tangent")
+
+
 def _done(r):
     """The compiled module's answer: results, or a status code."""
     if r.__class__ is int:
@@ -827,6 +836,7 @@ def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=N
     Returns dict(logprobs, lse [B,K,J], entropy [B,K,J], top_ids and top_logprobs [B,K,J,top]); entropy
     only if wanted, the alternatives only for top > 0.  Given `out`, its tensors are written (an
     'lse_tail' among them too).  No autograd: see token_logprobs."""
+    _no_tangent(logits)
     if out is None and inv_temp_per_draft is None:
         r = (_calls or _fast()).token_logprobs(logits, tokens, top, inv_temp, want_entropy, status)
         if r is not None:
@@ -848,6 +858,7 @@ def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0
     """gls_emitted_logprobs: the target rows [B,K,J,V] of a verification with the tokens [B,J] and
     accept flags [B,K,L] it returned -> token_logprobs' dict over [B,J], zeros (alternatives -1) at and
     beyond tau."""
+    _no_tangent(target_logits)
     if out is None:
         r = (_calls or _fast()).emitted_logprobs(target_logits, tokens, accept, top, inv_temp, flags, want_entropy, status)
         if r is not None:
@@ -871,6 +882,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
                             grad_logits=None):
     """gls_token_logprobs_backward: the gradient with respect to the logits, [B,K,J,V] in their type,
     from token_logprobs' inputs and outputs and the gradients of its outputs (each may be None)."""
+    _no_tangent(logits, lse, entropy, lse_tail, grad_logprobs, grad_lse, grad_entropy, grad_top_logprobs)
     if grad_logits is None and inv_temp_per_draft is None:
         r = (_calls or _fast()).token_logprobs_backward(logits, tokens, lse, entropy, lse_tail, top_ids, grad_logprobs,
                                                         grad_lse, grad_entropy, grad_top_logprobs, inv_temp)
@@ -921,6 +933,7 @@ def _matrix(t, name):
 def embed_tokens_raw(table, tokens, scale=1.0, status=None, out=None):
     """gls_embed_tokens: scale * table[tokens] for table [V,D] and int32 tokens of any shape ->
     [*tokens.shape, D]; a token below 0 gives zeros.  No autograd: see embed_tokens."""
+    _no_tangent(table)
     if out is None:
         r = (_calls or _fast()).embed_tokens(table, tokens, scale, status)
         if r is not None:
@@ -955,6 +968,7 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
     """gls_embed_tokens_backward: grad_out [*tokens.shape, D] -> the gradient of the table, [V,D] in
     grad_out's type unless grad_table (the same type, or float32) is given.  accumulate: added to
     grad_table, whose other rows are not touched."""
+    _no_tangent(grad_out, grad_table)
     if grad_table is None and workspace is None and not accumulate:
         r = (_calls or _fast()).embed_tokens_backward(grad_out, tokens, V, scale, status)
         if r is not None:
