@@ -857,8 +857,10 @@ def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0
                      status=None, out=None):
     """gls_emitted_logprobs: the target rows [B,K,J,V] of a verification with the tokens [B,J] and
     accept flags [B,K,L] it returned -> token_logprobs' dict over [B,J], zeros (alternatives -1) at and
-    beyond tau."""
+    beyond tau.  Not differentiable: logits that require a gradient are refused where one is recorded."""
     _no_tangent(target_logits)
+    if isinstance(target_logits, torch.Tensor) and target_logits.requires_grad and torch.is_grad_enabled():
+        raise GlsError("emitted_logprobs has no gradient: give it detached logits or call under torch.no_grad()")
     if out is None:
         r = (_calls or _fast()).emitted_logprobs(target_logits, tokens, accept, top, inv_temp, flags, want_entropy, status)
         if r is not None:

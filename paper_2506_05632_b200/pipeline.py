@@ -58,7 +58,7 @@ class StepBuffers:
 def spec_step(draft_logits, target_logits, buf, inv_temp=1.0, seed=0, seq_base=0, pos_base=0,
               spec=4, rounds=10, fused=False):
     """draft_logits [B,K,L,V], target_logits [B,K,L+1,V] on the device -> buf.out (device), and
-    buf.answers and buf.inputs where the buffers have them.
+    buf.answers and buf.inputs where the buffers have them.  No result carries a gradient.
     fused: one gls_draft_verify call instead of a draft call followed by a verify call."""
     kw = dict(inv_temp=inv_temp, seed=seed, seq_base=seq_base, pos_base=pos_base, spec=spec,
               rounds=rounds, workspace=buf.workspace, status=buf.status)
@@ -71,7 +71,7 @@ def spec_step(draft_logits, target_logits, buf, inv_temp=1.0, seed=0, seq_base=0
                                  out_scores=buf.draft_scores, **kw)
         binding.target_sample_verify(target_logits, buf.draft_tokens, out=buf.out, **kw)
     if buf.answers is not None:
-        binding.emitted_logprobs(target_logits, buf.out["tokens"], buf.out["accept"], top=buf.top,
+        binding.emitted_logprobs(target_logits.detach(), buf.out["tokens"], buf.out["accept"], top=buf.top,
                                  inv_temp=inv_temp, status=buf.status, out=buf.answers)
     if buf.inputs is not None:
         binding.embed_tokens_raw(buf.table, buf.out["tokens"], scale=buf.table_scale, status=buf.status,

@@ -34,3 +34,29 @@ def test_tangents_are_refused(call, requires_grad):
         with pytest.raises(gls.GlsError) as e:  # the level alone changes nothing: these have no tangent
             call(lambda t: t)
         assert "forward-mode" not in str(e.value)
+
+
+def test_emitted_logprobs_of_logits_that_require_a_gradient():
+    """They would come back without a history and drop out of a loss."""
+    x = X.clone().requires_grad_()
+    args = TOK[:, 0], torch.zeros(1, 2, 2, dtype=torch.uint8)
+    with pytest.raises(gls.GlsError, match="no gradient"):
+        gls.emitted_logprobs(x, *args)
+    for y, grad in ((x.detach(), True), (x, False)):  # on the way to the kernel, which there is not here
+        with torch.set_grad_enabled(grad), pytest.raises(gls.GlsError, match="device tensors"):
+            gls.emitted_logprobs(y, *args)
+
+
+@pytest.mark.gpu
+def test_a_step_on_logits_that_require_a_gradient(gls):
+    """The serving step reports on them all the same: its results carry no gradient."""
+    from paper_2506_05632_b200 import pipeline
+
+    t = torch.randn((3, 2, 3, 600), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    out = []
+    for x in (t, t.clone().requires_grad_()):
+        buf = pipeline.StepBuffers(3, 2, 2, 600, top=4)
+        pipeline.spec_step(x[:, :, :2], x, buf, seed=3)
+        out.append(buf.answers)
+    for n in out[0]:
+        assert torch.equal(out[0][n], out[1][n]) and not out[1][n].requires_grad
