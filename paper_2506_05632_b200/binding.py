@@ -10,6 +10,7 @@ import warnings
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.graph import increment_version
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
@@ -304,6 +305,12 @@ def _workspace(workspace, need, device):
     return workspace
 
 
+def _wrote(*given):
+    """Counts what a call wrote into tensors that its caller gave as a change of them, as torch's own in-place
+    operations do: a backward pass that saved one (the tokens of a lookup, say) then refuses it."""
+    increment_version([t for t in given if t is not None])
+
+
 def draft_sample(logits, inv_temp=1.0, inv_temp_per_draft=None, seed=0, seq_base=0, seq_ids=None,
                  pos_base=0, spec=4, rounds=10, noise_flags=0, want_scores=True, workspace=None,
                  status=None, out_tokens=None, out_scores=None):
@@ -313,6 +320,7 @@ def draft_sample(logits, inv_temp=1.0, inv_temp_per_draft=None, seed=0, seq_base
     dev = logits.device
     rows = _rows(logits, 3)
     nz = _noise(seed, seq_base, seq_ids, pos_base, spec, rounds, noise_flags)
+    given = out_tokens, out_scores
     if out_tokens is None:
         out_tokens = torch.empty((B, K, J), dtype=torch.int32, device=dev)
     if out_scores is None and want_scores:
@@ -326,6 +334,7 @@ def draft_sample(logits, inv_temp=1.0, inv_temp_per_draft=None, seed=0, seq_base
                               C.cast(itk, C.c_void_p) if itk is not None else None, C.byref(nz),
                               _ptr(out_tokens), _ptr(out_scores), workspace.data_ptr(),
                               workspace.numel(), _ptr(status), _stream()))
+    _wrote(*given)
     return out_tokens, out_scores
 
 
@@ -352,6 +361,7 @@ def draft_sample_static(logits, out_tokens, out_scores=None, inv_temp=1.0, inv_t
                                      C.cast(itk, C.c_void_p) if itk is not None else None,
                                      C.byref(nz), _ptr(out_tokens), _ptr(out_scores), _ptr(status),
                                      _stream()))
+    _wrote(out_tokens, out_scores)
     return out_tokens, out_scores
 
 
@@ -451,6 +461,7 @@ def draft_sample_topm(logits, M, inv_temp=1.0, inv_temp_per_draft=None, seed=0, 
                                    C.cast(itk, C.c_void_p) if itk is not None else None,
                                    C.byref(nz), _ptr(out_tokens), _ptr(out_scores),
                                    workspace.data_ptr(), workspace.numel(), _ptr(status), _stream()))
+    _wrote(workspace)  # views of it were returned
     return out_tokens, out_scores, _topm_lists(workspace, B, K, J, M)
 
 
@@ -479,6 +490,7 @@ def target_sample_verify_topm(logits, draft_tokens, M, inv_temp=1.0, flags=0, se
         _ptr(draft_tokens) if Ld > 0 else None, C.byref(nz), int(flags), _ptr(out["tokens"]),
         _ptr(out["tau"]), _ptr(out["accept"]) if Ld > 0 else None, _ptr(out.get("scores")),
         workspace.data_ptr(), workspace.numel(), _ptr(status), _stream()))
+    _wrote(workspace)
     return out
 
 
@@ -498,6 +510,7 @@ def target_sample_verify(logits, draft_tokens, inv_temp=1.0, flags=0, seed=0, se
         if draft_tokens.dtype != torch.int32 or not draft_tokens.is_contiguous():
             raise GlsError("draft_tokens must be contiguous int32")
         assert tuple(draft_tokens.shape) == (B, K, Ld)
+    given = out
     if out is None:
         out = dict(tokens=torch.empty((B, J), dtype=torch.int32, device=dev),
                    tau=torch.empty((B,), dtype=torch.int32, device=dev),
@@ -511,6 +524,8 @@ def target_sample_verify(logits, draft_tokens, inv_temp=1.0, flags=0, seed=0, se
         C.byref(nz), int(flags), _ptr(out["tokens"]), _ptr(out["tau"]),
         _ptr(out["accept"]) if Ld > 0 else None, _ptr(out.get("scores")), workspace.data_ptr(),
         workspace.numel(), _ptr(status), _stream()))
+    if given is not None:
+        _wrote(*given.values())
     return out
 
 
@@ -531,6 +546,7 @@ def copy_rows_to_device(dst, src, stream=None):
     st = stream.cuda_stream if stream is not None else _stream()
     _check(lib.gls_copy_rows_to_device(dst.data_ptr(), max(dst.stride(0), row) * es, src.data_ptr(),
                                        max(src.stride(0), row) * es, row * es, n, st))
+    _wrote(dst)
 
 
 def verify_walk(target_logits, L, flags=0, spec=4):
@@ -583,6 +599,7 @@ def draft_verify(draft_logits, target_logits, inv_temp=1.0, inv_temp_per_draft=N
     dev = draft_logits.device
     drows, trows = _rows(draft_logits, 3), _rows(target_logits, 3)
     nz = _noise(seed, seq_base, seq_ids, pos_base, spec, rounds, noise_flags)
+    given = out_draft_tokens, out_draft_scores, *(() if out is None else out.values())
     if out_draft_tokens is None:
         out_draft_tokens = torch.empty((B, K, L), dtype=torch.int32, device=dev)
     if out_draft_scores is None and want_scores:
@@ -604,6 +621,7 @@ def draft_verify(draft_logits, target_logits, inv_temp=1.0, inv_temp_per_draft=N
         _ptr(out_draft_tokens), _ptr(out_draft_scores), _ptr(out["tokens"]), _ptr(out["tau"]),
         _ptr(out["accept"]), _ptr(out.get("scores")), workspace.data_ptr(), workspace.numel(),
         _ptr(status), _stream()))
+    _wrote(*given)
     return out_draft_tokens, out_draft_scores, out
 
 
@@ -629,6 +647,7 @@ def compress_select(enc_logw, dec_logw=None, bins=None, K=None, seed=0, seq_base
             raise GlsError("bins must be contiguous uint8")
         bsb = 0 if bins.dim() == 1 else N
     nz = _noise(seed, seq_base, seq_ids, pos_base, spec, rounds, noise_flags)
+    given = out
     if out is None:
         out = dict(enc_index=torch.empty((B,), dtype=torch.int32, device=dev),
                    message=torch.empty((B,), dtype=torch.uint8, device=dev),
@@ -643,6 +662,8 @@ def compress_select(enc_logw, dec_logw=None, bins=None, K=None, seed=0, seq_base
         C.byref(nz), _ptr(out["enc_index"]), _ptr(out["message"]), _ptr(out["dec_index"]),
         _ptr(out["match"]), _ptr(out.get("scores")), workspace.data_ptr(), workspace.numel(),
         _ptr(status), _stream()))
+    if given is not None:
+        _wrote(*given.values())
     return out
 
 
@@ -670,6 +691,7 @@ def compress_gaussian(candidates, source, side_info, bins=None, s2_eta=0.5, s2_z
             raise GlsError("bins must be contiguous uint8")
         bsb = 0 if bins.dim() == 1 else N
     nz = _noise(seed, seq_base, seq_ids, pos_base, spec, rounds, noise_flags)
+    given = out
     if out is None:
         out = dict(enc_index=torch.empty((B,), dtype=torch.int32, device=dev),
                    message=torch.empty((B,), dtype=torch.uint8, device=dev),
@@ -686,6 +708,8 @@ def compress_gaussian(candidates, source, side_info, bins=None, s2_eta=0.5, s2_z
         _ptr(out["message"]), _ptr(out["dec_index"]), _ptr(out["match"]), _ptr(out.get("scores")),
         _ptr(out.get("recon")), _ptr(out.get("sqerr")), workspace.data_ptr(), workspace.numel(),
         _ptr(status), _stream()))
+    if given is not None:
+        _wrote(*given.values())
     return out
 
 
@@ -850,6 +874,7 @@ def token_logprobs_raw(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=N
     keep, itk = _temps(inv_temp_per_draft, K)
     _run(dev, _ready().gls_token_logprobs, rows, B, K, J, V, float(inv_temp), itk, tp, G, M, lp, lse, tail, ent, ids, tlp,
          _vec(status, "status", (1,), _I32, dev))
+    _wrote(*out.values())
     return out
 
 
@@ -875,6 +900,7 @@ def emitted_logprobs(target_logits, tokens, accept, top=0, inv_temp=1.0, flags=0
     out, lp, lse, _, ent, ids, tlp = _score_out(out, target_logits, lead, lead, M, want_entropy, dev)
     _run(dev, _ready().gls_emitted_logprobs, rows, B, K, L, V, float(inv_temp), tp, ap, int(flags), M, lp, lse, ent, ids, tlp,
          _vec(status, "status", (1,), _I32, dev))
+    _wrote(*out.values())
     return out
 
 
@@ -915,6 +941,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
          _vec(grad_logprobs, "grad_logprobs", given, _F32T, dev), _vec(grad_lse, "grad_lse", lead, _F32T, dev),
          _vec(grad_entropy, "grad_entropy", lead, _F32T, dev),
          _vec(grad_top_logprobs, "grad_top_logprobs", top, _F32T, dev), _rows4(grad_logits, "grad_logits"))
+    _wrote(grad_logits)
     return grad_logits
 
 
@@ -958,6 +985,7 @@ def embed_tokens_raw(table, tokens, scale=1.0, status=None, out=None):
         _, ostride = _matrix(flat, "out")
     _run(dev, _ready().gls_embed_tokens, table.data_ptr(), dt, stride, V, D, tp, N, float(scale), out.data_ptr(), ostride,
          _vec(status, "status", (1,), _I32, dev))
+    _wrote(out)
     return out
 
 
@@ -996,4 +1024,5 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
     keep, ws, nbytes = _space(workspace, embed_tokens_backward_workspace_bytes(N, V, D), grad_out)
     _run(dev, _ready().gls_embed_tokens_backward, flat.data_ptr(), dt, stride, tp, N, V, D, float(scale), grad_table.data_ptr(),
          gdt, gstride, EMBED_ACCUMULATE if accumulate else 0, ws, nbytes, _vec(status, "status", (1,), _I32, dev))
+    _wrote(grad_table)
     return grad_table

@@ -100,7 +100,9 @@ class GraphedStep:
 
     def replay(self):
         self.graph.replay()
-        return self.buf.out
+        b = self.buf
+        binding._wrote(b.draft_tokens, b.draft_scores, b.inputs, *b.out.values(), *(b.answers or {}).values())
+        return b.out
 
 
 class HostStepper:
