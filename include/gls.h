@@ -525,6 +525,8 @@ int gls_token_logprobs_backward(const gls_rows_t* logits, int B, int K, int J, i
  *   Rows may start at any element and have any size.  They are read in aligned 16-byte words, which may
  *   hold elements beside or between the rows (not used), but nothing in front of the table's first
  *   element or behind its last.  Nothing but the N rows is written.
+ *   No row of out may share memory with one of the table, V of them; columns of one buffer may be the one
+ *   and the other if their rows are equally far apart (GLS_ERR_INVALID_ARG otherwise).
  */
 int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t V, int64_t D,
                      const int32_t* tokens, int64_t N, float scale, void* out, int64_t out_stride,
@@ -538,7 +540,7 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
  * read nor written.
  *
  *   grad_out [N,D] of type `dtype`; grad_table [V,D] of type `grad_dtype`: the same, or fp32 for
- *   bf16 grad_out; strides, sizes and alignment as above
+ *   bf16 grad_out; strides, sizes, alignment and sharing of memory as above
  *   workspace  gls_embed_tokens_backward_workspace_bytes(N, V, D) bytes, 16-byte aligned; its
  *              contents on entry are ignored (may be NULL when N = 0)
  * N < 2^30.

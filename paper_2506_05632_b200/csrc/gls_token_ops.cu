@@ -31,6 +31,21 @@ static int sm_count() {
   return n;
 }
 
+// Whether two sets of rows share memory: n rows of `len` bytes from p, `pitch` bytes apart, and m of `mlen` from
+// q.  Rows of one pitch may lie side by side (columns of one buffer); where the pitches differ, sets whose
+// stretches of memory meet are taken to share some.
+static bool rows_meet(const void* p, int64_t n, int64_t pitch, int64_t len, const void* q, int64_t m, int64_t mpitch,
+                      int64_t mlen) {
+  typedef __int128 wide;  // a stride may be anything
+  if (n == 1) pitch = mpitch;
+  if (m == 1) mpitch = pitch;
+  const wide a = (wide)(uintptr_t)p, b = (wide)(uintptr_t)q;
+  if (a + (n - 1) * (wide)pitch + len <= b || b + (m - 1) * (wide)mpitch + mlen <= a) return false;
+  if (pitch != mpitch || (n == 1 && m == 1)) return true;
+  const wide r = ((b - a) % pitch + pitch) % pitch;  // a row of q begins r behind one of p
+  return r < len || r + mlen > pitch;
+}
+
 static size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 static bool score_sizes_ok(int B, int K, int J, int64_t V) {
@@ -277,6 +292,8 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
   if (!table || !tokens || !out || (V > 1 && table_stride < D) || (N > 1 && out_stride < D)) return GLS_ERR_INVALID_ARG;
   const int es = dtype == GLS_F32 ? 4 : 2;
   if ((uintptr_t)table % es || (uintptr_t)out % es) return GLS_ERR_MISALIGNED;
+  // the table is read while the rows are written
+  if (rows_meet(table, V, table_stride * es, D * es, out, N, out_stride * es, D * es)) return GLS_ERR_INVALID_ARG;
   EmbedArgs A;
   A.table = (const char*)table;
   A.table_stride = table_stride;
@@ -467,6 +484,9 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
   const EmbedGradPlan P = embed_grad_plan(N, V, D);
   if (!workspace || workspace_bytes < P.total) return GLS_ERR_WORKSPACE;
   if ((uintptr_t)workspace % 16) return GLS_ERR_MISALIGNED;
+  // zeros are written before the gradient's rows are read
+  if (rows_meet(grad_out, N, grad_out_stride * es, D * es, grad_table, V, grad_table_stride * eso, D * eso))
+    return GLS_ERR_INVALID_ARG;
   char* ws = (char*)workspace;
   const bool vec = D % kEgCols == 0 && grad_out_stride * es % 16 == 0 && grad_table_stride * eso % 16 == 0 &&
                    (uintptr_t)grad_out % 16 == 0 && (uintptr_t)grad_table % 16 == 0;
