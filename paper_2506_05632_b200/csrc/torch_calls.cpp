@@ -67,6 +67,11 @@ int64_t integer(PyObject* o) {
   }
   return v;
 }
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw python_error();
+  return v == 1;
+}
 int dtype_code(const at::Tensor& t) {
   if (t.scalar_type() == at::kFloat) return GLS_F32;
   if (t.scalar_type() == at::kBFloat16) return GLS_BF16;
@@ -171,7 +176,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const double inv_temp = number(a[3]);
   const int64_t G = t.dim() == 4 ? t.size(3) : 1;
   if (G < 0 || G > GLS_MAX_GIVEN || lead[1] > GLS_MAX_K) throw Decline();
-  const bool entropy = PyObject_IsTrue(a[4]) == 1;
+  const bool entropy = truth(a[4]);
   std::optional<NoGil> free_others(std::in_place);
   ScoreOut o(t.sizes(), lead, M, entropy, dev);
   const int rc = g_logprobs(&rows, (int)lead[0], (int)lead[1], (int)lead[2], x.size(3), (float)inv_temp, nullptr, tokens,
@@ -197,7 +202,7 @@ PyObject* emitted_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const uint8_t* accept = L > 0 ? data<uint8_t>(tensor(a[2]), at::kByte, shape, dev) : nullptr;
   uint32_t* status = status_word(a[7], dev);
   const double inv_temp = number(a[4]);
-  const bool entropy = PyObject_IsTrue(a[6]) == 1;
+  const bool entropy = truth(a[6]);
   std::optional<NoGil> free_others(std::in_place);
   ScoreOut o(lead, lead, M, entropy, dev);
   const int rc = g_emitted(&rows, (int)B, (int)K, (int)L, x.size(3), (float)inv_temp, tokens, accept, (uint32_t)flags,
