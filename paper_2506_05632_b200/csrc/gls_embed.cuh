@@ -32,6 +32,16 @@ __device__ __forceinline__ uint4 ld_global16(const void* p) {
   asm volatile("ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
+// What an earlier launch of the same call has written.  The launches overlap (see zero_share), so a grid may
+// have started before these writes; the read-only path (__ldg) is for data that stays as it is while a grid
+// lives and is not for them, a plain load behind griddepcontrol.wait sees them.
+template <class T>
+__device__ __forceinline__ T ld_made(const T* p) {
+  static_assert(sizeof(T) == 4, "a word");
+  uint32_t v;
+  asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return (T)v;
+}
 template <int DT>
 __device__ __forceinline__ uint32_t scale_word(uint32_t w, float s) {
   if (DT == kF32) return __float_as_uint(__uint_as_float(w) * s);
@@ -348,12 +358,12 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, lo
       while (n > 0) {
         const int part = (n + (int)blockDim.x) / ((int)blockDim.x + 1);  // 1 .. n
         const int at = (int)(threadIdx.x + 1) * part - 1;                // the last of this thread's part
-        const int below = __syncthreads_count(at < n && __ldg(Z.keys + lo + at) < first);
+        const int below = __syncthreads_count(at < n && ld_made(Z.keys + lo + at) < first);
         lo += below * part;
         n = min(n - below * part, part - 1);
       }
       for (int i = lo + threadIdx.x; i < Z.N; i += blockDim.x) {
-        const long long r = (long long)__ldg(Z.keys + i) - first;
+        const long long r = (long long)ld_made(Z.keys + i) - first;
         if (r >= last - first) break;
         atomicOr(&here[r >> 5], 1u << (r & 31));
       }
@@ -365,7 +375,7 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, lo
     // Rows without gaps between them: each warp writes its rows' runs, whatever a row's size and alignment.
     const long long part = (last - first + warps - 1) / warps, base = look ? first : 0ll, row = Z.D * Z.es;
     const long long a = first + (threadIdx.x >> 5) * part, b = min(last, a + part);
-    auto bits = [&](long long v) { return look ? here[(v - base) >> 5] : __ldg(Z.touched + (v >> 5)); };
+    auto bits = [&](long long v) { return look ? here[(v - base) >> 5] : ld_made(Z.touched + (v >> 5)); };
     for (long long v = a; v < b;) {
       const int at = (int)((v - base) & 31);
       const uint32_t w = bits(v) >> at;
@@ -394,7 +404,7 @@ __device__ __forceinline__ void zero_rows(const ZeroArgs& Z, long long first, lo
   if (mine >= side) return;
   for (long long v = first + mine; v < last; v += side) {
     const long long b = look ? v - first : v;
-    if (((look ? here[b >> 5] : __ldg(Z.touched + (b >> 5))) >> (b & 31)) & 1u) continue;
+    if (((look ? here[b >> 5] : ld_made(Z.touched + (b >> 5))) >> (b & 31)) & 1u) continue;
     char* const row = Z.out + v * Z.out_stride * Z.es;
     const long long off = (long long)((uintptr_t)row & 15);
     for (long long o = c0 * 16 - off; o < len; o += 16ll * blockDim.x) {
@@ -884,8 +894,8 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
   const int n = min(A.per_range, A.N - i0);
   for (int i = threadIdx.x; i < n + 2; i += blockDim.x) {  // sk[0]: the key before the range, sk[n + 1]: behind it
     const int at = i0 + i - 1;
-    sk[i] = at >= 0 && at < A.N ? __ldg(A.key + at) : -1;
-    if (i >= 1 && i <= n) sp[i - 1] = __ldg(A.pos + at);
+    sk[i] = at >= 0 && at < A.N ? ld_made(A.key + at) : -1;
+    if (i >= 1 && i <= n) sp[i - 1] = ld_made(A.pos + at);
   }
   __syncthreads();
   if (slab == 0 && sk[n] < A.V && sk[n] == sk[n + 1] && sk[0] != sk[n]) {
@@ -894,7 +904,7 @@ __global__ void __launch_bounds__(kEgThreads) embed_grad_kernel(const __grid_con
     for (int t0 = 0; t0 <= kEgMany; t0 += blockDim.x) {
       const int t = t0 + threadIdx.x;
       const long long at = (long long)i0 + (long long)(1 + t) * A.per_range;
-      go += __syncthreads_count(t <= kEgMany && at < A.N && __ldg(A.key + at) == sk[n]);
+      go += __syncthreads_count(t <= kEgMany && at < A.N && ld_made(A.key + at) == sk[n]);
     }
     if (threadIdx.x == 0) {
       const int many = go > kEgMany ? 1 : 0;
@@ -978,7 +988,7 @@ __global__ void __launch_bounds__(kEgThreads, 4) embed_join_kernel(const __grid_
     if (many) {
       for (;;) {
         const long long at = ((long long)h.x + 1 + go + threadIdx.x) * A.per_range;
-        const int more = __syncthreads_count(at < A.N && __ldg(A.key + at) == h.y);
+        const int more = __syncthreads_count(at < A.N && ld_made(A.key + at) == h.y);
         go += more;
         if (more < kEgThreads) break;
       }
