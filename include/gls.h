@@ -449,7 +449,11 @@ int gls_compress_select(const gls_rows_t* enc_logw, const gls_rows_t* dec_logw, 
  *     lse = ln sum_i e^(z_i);  log probability of token t = z_t - lse;  p_i = e^(z_i - lse)
  *     entropy = -sum_i p_i ln p_i   (nats)
  *     alternatives: the M largest logits in descending order, ties to the lower index
- * The row is read once.
+ * The row is read once, except that parts of it are read again for the alternatives: the groups of 16 tokens
+ * that reach a bound on the M-th; a short row with more than 24 alternatives per 2048 bf16 or 1024 fp32
+ * tokens, whole; and where more tokens reach the bound than the call's buffers hold (equal logits, or large
+ * ones side by side, as in a vocabulary ordered by frequency), the row several times.  Rows with +inf or
+ * logits beyond 1e30 in size are summed again.  Results do not depend on any of it, time does.
  *
  *   logits            [B,K,J,V] rows (fp32 or bf16, any alignment of their first elements)
  *   inv_temp, inv_temp_per_draft_host  as in gls_draft_sample, each within [1e-20, 1e20]
@@ -514,7 +518,8 @@ int gls_token_logprobs_backward(const gls_rows_t* logits, int B, int K, int J, i
                                 const gls_rows_t* grad_logits, void* stream);
 
 /*
- * Rows of a table by token, scaled: out[n,:] = scale * table[tokens[n],:], rounded once.  The
+ * Rows of a table by token, scaled: out[n,:] = scale * table[tokens[n],:]; the product is rounded to fp32
+ * and, for bf16, from there to bf16; a scale of 1 copies.  The
  * inputs of the next draft position from the tokens that a call above returned, or the candidates
  * that gls_compress_select's decoders chose (W_k = U_{X^(k)}, Sec. 5.1).  A token below 0 (behind a
  * sequence's last token, a decoder without a candidate) gives a row of zeros, and so does one that
@@ -534,7 +539,9 @@ int gls_embed_tokens(const void* table, int dtype, int64_t table_stride, int64_t
 
 /*
  * Its gradient: grad_table[v,:] = scale * sum over n with tokens[n] == v of grad_out[n,:].  The
- * tokens are sorted and every sum runs in the order of n in fp32, so equal calls return equal bits.
+ * tokens are sorted; a token's rows are added up in fp32 in the order of n within ranges of 8 to 64 sorted
+ * positions, and the ranges' sums in an order that N, V, D and the tokens fix, so equal calls return equal
+ * bits.  The sum times scale is rounded to fp32 and from there to the table's type.
  * Tokens outside [0, V) add nothing.  Rows of tokens that do not occur are written as zeros;
  * with GLS_EMBED_ACCUMULATE the sums are added to what grad_table holds and those rows are neither
  * read nor written.

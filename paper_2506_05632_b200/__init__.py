@@ -13,8 +13,8 @@ kernels of csrc/.  There is no CPU fallback: if libgls.so cannot be loaded the c
     emitted_logprobs(logits, tokens, accept)  the same for the tokens a verification emitted
     embed_tokens(table, tokens, ...)          rows of a table by token, scaled
 
-The last group's token_logprobs and embed_tokens are differentiable (autograd.py); their gradients
-are token_logprobs_backward and embed_tokens_backward.
+The last group's token_logprobs and embed_tokens are differentiable in reverse mode (autograd.py); their
+gradients are token_logprobs_backward and embed_tokens_backward.  emitted_logprobs has none.
 """
 from .autograd import embed_tokens, token_logprobs  # noqa: F401
 from .binding import (  # noqa: F401

@@ -5,7 +5,8 @@
 //
 // The gradient sorts the tokens (stable, so that equal tokens stay in the order of n), cuts the
 // sorted positions into ranges of a fixed length and sums each range's rows in order; what a token
-// has in more than one range is joined by a last kernel, again in order.  The result does not
+// has in more than one range is joined by a last kernel: in order for up to 32 ranges more, beyond that by
+// eight warps, each every eighth range in order, whose sums are then added in turn.  The result does not
 // depend on how the blocks are scheduled, and a token that fills half the batch costs no more than
 // many different ones.
 #pragma once

@@ -304,10 +304,15 @@ __device__ __forceinline__ uint32_t warp_kth(const uint32_t (&code)[N], int k) {
 // too many), rounded down to bf16: two instructions a step.  At the end the M-th largest of a few
 // maxima over entries (distinct tokens) bounds the M-th largest logit T from below; entries that
 // reach T are listed, their tokens read once more, and those that reach T ranked.  About a tenth more
-// than M tokens get that far, so what this costs does not depend on the row's length or order.  (Testing groups
+// than M tokens get that far where large logits lie anywhere in the row.  (Testing groups
 // against a running threshold in the sweep and examining them in batches took 11 thousand
 // instructions a row of 152064 tokens and M = 20, four tenths of what the sums take.)
-// Rows of which more tokens reach T than the buffers hold (equal logits) go through a radix select.
+// Where large logits lie side by side, the entries hide all but one of each 64 (32) of them and T is far
+// below the M-th largest; in the cluster kernel, whose bound is the smallest of its warps', even more so.
+// Rows of which more tokens reach T than the buffers hold, these or rows of equal logits, go through a radix
+// select, which reads the whole row for each of its passes.  Rows in the order of 2 ln(rank) with noise of 1,
+// beside the same shuffled: one of 152064, M = 5, 39 us and 10; 224 of 128256, M = 20, 125 and 21; 8192 of
+// 152064, M = 20, 454 and 423, M = 50, 7.1 ms and 0.45, M = 256, 10.1 and 0.74.
 // ------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t top_entry_bits(float x, std::integral_constant<int, kBF16>) {
   return __float_as_uint(x) >> 16;
