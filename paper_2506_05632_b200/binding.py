@@ -909,7 +909,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, lse_tail=None, to
                             grad_top_logprobs=None, inv_temp=1.0, inv_temp_per_draft=None,
                             grad_logits=None):
     """gls_token_logprobs_backward: the gradient with respect to the logits, [B,K,J,V] in their type,
-    from token_logprobs' inputs and outputs and the gradients of its outputs (each may be None)."""
+    from token_logprobs' inputs and outputs and the gradients of its outputs (each may be None).  No autograd."""
     _no_tangent(logits, lse, entropy, lse_tail, grad_logprobs, grad_lse, grad_entropy, grad_top_logprobs)
     if grad_logits is None and inv_temp_per_draft is None:
         r = (_calls or _fast()).token_logprobs_backward(logits, tokens, lse, entropy, lse_tail, top_ids, grad_logprobs,
@@ -997,7 +997,7 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
                           workspace=None, status=None):
     """gls_embed_tokens_backward: grad_out [*tokens.shape, D] -> the gradient of the table, [V,D] in
     grad_out's type unless grad_table (the same type, or float32) is given.  accumulate: added to
-    grad_table, whose other rows are not touched."""
+    grad_table, whose other rows are not touched.  No autograd."""
     _no_tangent(grad_out, grad_table)
     if grad_table is None and workspace is None and not accumulate:
         r = (_calls or _fast()).embed_tokens_backward(grad_out, tokens, V, scale, status)
