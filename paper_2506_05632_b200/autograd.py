@@ -67,9 +67,9 @@ def token_logprobs(logits, tokens, top=0, inv_temp=1.0, inv_temp_per_draft=None,
     Returns dict(logprobs, lse, entropy, top_ids, top_logprobs), the entropy only if wanted and the
     alternatives only for top > 0; see gls_token_logprobs in include/gls.h.  Differentiable in the
     logits (in reverse mode, once; not during a graph capture, and not into given outputs)."""
-    binding._no_tangent(logits)
     if not (logits.requires_grad and torch.is_grad_enabled()):
         return binding.token_logprobs_raw(logits, tokens, top, inv_temp, inv_temp_per_draft, want_entropy, status, out)
+    binding._no_tangent(logits)
     kw = dict(inv_temp=inv_temp, inv_temp_per_draft=inv_temp_per_draft, want_entropy=want_entropy,
               status=status)
     if out is not None:
@@ -97,9 +97,9 @@ def embed_tokens(table, tokens, scale=1.0, status=None, out=None):
     """scale * table[tokens]: table [V,D], int32 tokens of any shape -> [*tokens.shape, D]; a token
     below 0 gives zeros; see gls_embed_tokens in include/gls.h.  Differentiable in the table (in reverse
     mode, once; not during a graph capture, and not into a given output)."""
-    binding._no_tangent(table)
     if not (table.requires_grad and torch.is_grad_enabled()):
         return binding.embed_tokens_raw(table, tokens, scale, status, out)
+    binding._no_tangent(table)
     if out is not None:
         raise binding.GlsError("a given output can not carry a gradient: call under torch.no_grad()")
     return _EmbedTokens.apply(table, tokens, float(scale), status)
