@@ -97,6 +97,7 @@ typedef enum {
 /* bits OR-ed into *device_status by the kernels */
 #define GLS_DEV_EMPTY_SUPPORT 1u /* some row had no finite logit: its token is -1 */
 #define GLS_DEV_BAD_TOKEN 2u     /* a token given to the calls below was not smaller than V */
+#define GLS_DEV_BAD_SETTING 4u   /* a row's sampling setting or uniform number was out of range: its token is -1 */
 
 typedef enum { GLS_F32 = 0, GLS_BF16 = 1 } gls_dtype_t;
 
@@ -558,6 +559,100 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
                               int64_t N, int64_t V, int64_t D, float scale, void* grad_table, int grad_dtype,
                               int64_t grad_table_stride, uint32_t flags, void* workspace,
                               size_t workspace_bytes, uint32_t* device_status, void* stream);
+
+/*
+ * One token per row by temperature, top-k, top-p and min-p from a given uniform number: independent
+ * sampling beside the coupled races above (no counterpart in the paper).  Over the row's finite logits (-inf,
+ * NaN and +inf are masked, as in the races) w_i = e^((l_i - max l) inv_temp); in the order of falling
+ * logits, ties to the lower index,
+ *     top_k  keeps the first top_k tokens (below 1 or not below V: all of them);
+ *     top_p  of these the shortest start whose mass reaches top_p times theirs (the token of rank r stays
+ *            if the mass in front of it is below that; 1 and above: all of them);
+ *     min_p  of these the tokens with (l_i - max l) inv_temp >= ln(min_p) (0: all of them);
+ * the first token of the order always stays.  Drawn is the first token BY INDEX whose cumulative mass among the
+ * kept ones exceeds u times their total (u = 1: the last kept one); its log probability is among the
+ * kept ones.  inv_temp = +inf is the limit of low temperature: the first token of the order, log probability 0.
+ * What is decided is decided by sums of 64-bit exponentials (the border of top_p among codes of several
+ * values by integer multiples of 2^-(62 - log2 V) of the largest weight); equal calls return equal tokens.
+ *
+ *   logits         [B,K,J,V] rows (fp32 or bf16, any alignment of their first elements)
+ *   uniforms       fp32 [B,K,J], each within [0, 1]
+ *   out_tokens     int32 [B,K,J]
+ *   out_logprobs   NULL or fp32 [B,K,J]
+ * A setting is one value for all rows, or where its pointer is set an array on the device, with a stride
+ * in elements per sequence, draft and position (0 broadcasts).  One value for all is checked by the host (inv_temp
+ * as in gls_token_logprobs, or +inf; top_p > 0; 0 <= min_p <= 1); a row whose own setting is out of range, or
+ * whose uniform number is, gets token -1, log probability 0 and GLS_DEV_BAD_SETTING; a row without a finite
+ * logit the same and GLS_DEV_EMPTY_SUPPORT.  No workspace is needed.
+ */
+typedef struct {
+  float inv_temp;
+  int32_t top_k;
+  float top_p;
+  float min_p;
+  const float* inv_temp_rows; /* NULL or device pointers */
+  const int32_t* top_k_rows;
+  const float* top_p_rows;
+  const float* min_p_rows;
+  int64_t inv_temp_stride[3]; /* b, k, j */
+  int64_t top_k_stride[3];
+  int64_t top_p_stride[3];
+  int64_t min_p_stride[3];
+} gls_sampling_t;
+int gls_sample_tokens(const gls_rows_t* logits, int B, int K, int J, int64_t V, const gls_sampling_t* settings,
+                      const float* uniforms, int32_t* out_tokens, float* out_logprobs, uint32_t* device_status,
+                      void* stream);
+
+/*
+ * A table of V rows of D columns at 4 bits, the head or the embedding of a drafter whose weights are held so:
+ *     element (v, d) = scale[v, d / group] * (code[v, d] - zero[v, d / group])
+ *   codes     two a byte, the even column in the low four bits; rows code_stride bytes apart, a multiple of 16 that
+ *             holds ceil(D / 32) * 16 bytes, which are read (codes beyond D are not used); 16-byte aligned
+ *   scales    [V, ceil(D / group)] of type scale_dtype (fp32 or bf16), scale_stride elements apart
+ *   zeros     uint8 of the same shape, zero_stride apart, of which the low four bits count; NULL: 8
+ *   group     32, 64 or 128 columns; D <= 32768
+ */
+typedef struct {
+  uint8_t* codes;
+  int64_t code_stride;
+  void* scales;
+  int32_t scale_dtype;
+  int64_t scale_stride;
+  uint8_t* zeros;
+  int64_t zero_stride;
+  int64_t V, D;
+  int32_t group;
+} gls_int4_table_t;
+
+/*
+ * Weights -> table, to the nearest code.  Per group, with lo = min(0, min w) and hi = max(0, max w):
+ *     with zeros:    scale = (hi - lo) / 15, zero = -lo / scale, code = w / scale + zero
+ *     without:       scale = max |w| / 7, code = w / scale + 8
+ * each quotient rounded to fp32, the scale from there to its type, zero and w / scale to integers (ties to
+ * even), codes and zeros held to 0 .. 15.  A group of zeros gets scale 0 and the codes of zero; one with a weight
+ * that is not finite, or whose scale is beyond its type, the scale NaN.  Codes beyond D within a byte are 0.
+ *   weights [V,D] of type dtype, rows contiguous, weight_stride elements apart; table: written
+ */
+int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, const gls_int4_table_t* table,
+                       void* stream);
+
+/*
+ * Logits of hidden states: out[n,v] = sum over d of x[n,d] * element(v, d), the products of a group summed in
+ * fp32 and multiplied by its scale in fp32, the sum rounded once to the output's type.  bf16 x goes in as it is, fp32 x
+ * in three parts that hold all of its 24 bits.  Eight rows of x are taken per pass over the table (fewer
+ * where D is large), so this is for the few rows of a decoding step.
+ *   x [N,D], out [N,V] of types x_dtype, out_dtype (fp32 or bf16), rows contiguous, strides in elements
+ *   of at least D and V; N <= 65535, N = 0 is legal.  An out in the memory of x or of the table is refused.
+ */
+int gls_head_logits(const void* x, int x_dtype, int64_t x_stride, int64_t N, const gls_int4_table_t* table,
+                    void* out, int out_dtype, int64_t out_stride, void* stream);
+
+/*
+ * Rows of the table by token, scaled: out[n,:] = scale * element(tokens[n], :), rounded to fp32 after each product
+ * and from there to the output's type.  Tokens outside the table as in gls_embed_tokens.
+ */
+int gls_embed_tokens_int4(const gls_int4_table_t* table, const int32_t* tokens, int64_t N, float scale, void* out,
+                          int out_dtype, int64_t out_stride, uint32_t* device_status, void* stream);
 
 #ifdef __cplusplus
 }

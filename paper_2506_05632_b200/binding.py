@@ -7,6 +7,7 @@ import subprocess
 import sysconfig
 import threading
 import warnings
+from typing import NamedTuple, Optional
 
 import torch
 from torch.autograd import forward_ad
@@ -26,7 +27,7 @@ VERIFY_ALL_ROWS, VERIFY_ACTIVE_ROWS = 4, 8  # how the dense verify call walks Al
 VERIFY_FIRST_PHASE, VERIFY_REST = 16, 32   # the walk in phases as two calls (rows fetched on demand)
 VERIFY_THREE_PHASES = 64                   # positions 1 and 2 as a phase of their own
 NOISE_SHARED_ACROSS_K = 1
-DEV_EMPTY_SUPPORT, DEV_BAD_TOKEN = 1, 2
+DEV_EMPTY_SUPPORT, DEV_BAD_TOKEN, DEV_BAD_SETTING = 1, 2, 4
 EMBED_ACCUMULATE = 1
 MAX_GIVEN = 64  # tokens per row of token_logprobs
 F32, BF16 = 0, 1
@@ -133,6 +134,19 @@ class _SparseRows(C.Structure):
                 ("stride_k", C.c_int64), ("stride_j", C.c_int64), ("M", C.c_int32)]
 
 
+class _Sampling(C.Structure):
+    _fields_ = [("inv_temp", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("inv_temp_rows", C.c_void_p), ("top_k_rows", C.c_void_p), ("top_p_rows", C.c_void_p),
+                ("min_p_rows", C.c_void_p), ("inv_temp_stride", C.c_int64 * 3), ("top_k_stride", C.c_int64 * 3),
+                ("top_p_stride", C.c_int64 * 3), ("min_p_stride", C.c_int64 * 3)]
+
+
+class _Int4(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("code_stride", C.c_int64), ("scales", C.c_void_p),
+                ("scale_dtype", C.c_int32), ("scale_stride", C.c_int64), ("zeros", C.c_void_p),
+                ("zero_stride", C.c_int64), ("V", C.c_int64), ("D", C.c_int64), ("group", C.c_int32)]
+
+
 class _Noise(C.Structure):
     _fields_ = [("seed", C.c_uint64), ("seq_base", C.c_uint32), ("seq_ids", C.c_void_p),
                 ("pos_base", C.c_uint32), ("noise_spec", C.c_uint32), ("rounds", C.c_uint32),
@@ -234,6 +248,18 @@ def load():
         L.gls_embed_tokens_backward.argtypes = [
             C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_float,
             C.c_void_p, C.c_int, C.c_int64, C.c_uint32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.gls_sample_tokens.restype = C.c_int
+        L.gls_sample_tokens.argtypes = [
+            C.POINTER(_Rows), C.c_int, C.c_int, C.c_int, C.c_int64, C.POINTER(_Sampling), C.c_void_p, C.c_void_p,
+            C.c_void_p, C.c_void_p, C.c_void_p]
+        L.gls_quantize_table.restype = C.c_int
+        L.gls_quantize_table.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.POINTER(_Int4), C.c_void_p]
+        L.gls_head_logits.restype = C.c_int
+        L.gls_head_logits.argtypes = [
+            C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.POINTER(_Int4), C.c_void_p, C.c_int, C.c_int64, C.c_void_p]
+        L.gls_embed_tokens_int4.restype = C.c_int
+        L.gls_embed_tokens_int4.argtypes = [
+            C.POINTER(_Int4), C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p]
         _calls = _load_calls(L)
         _lib = L
         return _lib
@@ -1026,3 +1052,166 @@ def embed_tokens_backward(grad_out, tokens, V, scale=1.0, grad_table=None, accum
          gdt, gstride, EMBED_ACCUMULATE if accumulate else 0, ws, nbytes, _vec(status, "status", (1,), _I32, dev))
     _wrote(grad_table)
     return grad_table
+
+
+# ---- independent sampling, and a drafter's vocabulary ends at 4 bits -------------------------------
+def _no_gradient(name, *tensors):
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and t.requires_grad:
+                raise GlsError("%s has no gradient: give it detached tensors or call under torch.no_grad()" % name)
+
+
+def _setting(s, name, value, dtype, lead, dev):
+    """Puts one sampling setting, a number or a tensor [B], [B,K] or [B,K,J] (sizes of 1 broadcast), into s."""
+    if not isinstance(value, torch.Tensor):
+        setattr(s, name, int(value) if dtype is _I32 else float(value))
+        return
+    n = value.dim()
+    if value.dtype is not dtype or value.get_device() != dev or not 1 <= n <= 3 or any(
+            a != b and a != 1 for a, b in zip(value.shape, lead)):
+        raise GlsError("%s must be a number or a %s tensor of shape [B], [B,K] or [B,K,J] on the logits' device" % (name, dtype))
+    setattr(s, name + "_rows", value.data_ptr())
+    st = [value.stride(i) if i < n and value.shape[i] > 1 else 0 for i in range(3)]
+    setattr(s, name + "_stride", (C.c_int64 * 3)(*st))
+
+
+def sample_tokens(logits, uniforms, inv_temp=1.0, top_k=0, top_p=1.0, min_p=0.0, want_logprobs=True, status=None,
+                  out=None):
+    """gls_sample_tokens: logits [B,K,J,V] and uniforms fp32 [B,K,J] -> dict(tokens int32 [B,K,J], logprobs fp32
+    [B,K,J] if wanted), independently per row.
+
+    Each setting is a number or a tensor with a value per sequence [B], or [B,K], or [B,K,J].  inv_temp = inf
+    takes the most likely token, top_k < 1 and top_p = 1 and min_p = 0 do not restrict.  Given `out`, its
+    tensors are written (log probabilities where it has them).  Not differentiable (see token_logprobs)."""
+    _no_tangent(logits)
+    _no_gradient("sample_tokens", logits)
+    dev = _device(logits, "logits")
+    rows = _rows4(logits, "logits")
+    B, K, J, V = logits.shape
+    lead = (B, K, J)
+    s = _Sampling()
+    _setting(s, "inv_temp", inv_temp, _F32T, lead, dev)
+    _setting(s, "top_k", top_k, _I32, lead, dev)
+    _setting(s, "top_p", top_p, _F32T, lead, dev)
+    _setting(s, "min_p", min_p, _F32T, lead, dev)
+    up = _vec(uniforms, "uniforms", lead, _F32T, dev)
+    if out is None:
+        out = {"tokens": torch.empty(lead, dtype=_I32, device=logits.device)}
+        if want_logprobs:
+            out["logprobs"] = torch.empty(lead, dtype=_F32T, device=logits.device)
+    _run(dev, _ready().gls_sample_tokens, rows, B, K, J, V, s, up, _vec(out["tokens"], "out['tokens']", lead, _I32, dev),
+         _vec(out.get("logprobs"), "out['logprobs']", lead, _F32T, dev), _vec(status, "status", (1,), _I32, dev))
+    _wrote(*out.values())
+    return out
+
+
+class Int4Table(NamedTuple):
+    """A table [V,dim] at 4 bits: codes uint8 [V, at least ceil(dim / 32) * 16], the even column in a byte's low half,
+    scales [V, ceil(dim / group)] fp32 or bf16, zeros uint8 of the same shape or None (8).  See gls_int4_table_t."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    zeros: Optional[torch.Tensor]
+    dim: int
+    group: int
+
+
+def _int4(table):
+    """(gls_int4_table_t, device index, V) of an Int4Table."""
+    codes, scales, zeros, D, group = table
+    dev = _device(codes, "codes")
+    V, G = codes.shape[0], -(-D // group) if group > 0 else 0
+    if codes.dtype is not _U8 or codes.dim() != 2 or (codes.stride(1) != 1 and codes.shape[1] > 1) or codes.shape[1] < -(-D // 32) * 16:
+        raise GlsError("codes must be uint8 [V, ceil(dim / 32) * 16] with contiguous rows")
+    for t, name in ((scales, "scales"), (zeros, "zeros")):
+        if t is not None and (t.shape != (V, G) or t.get_device() != dev or (t.stride(1) != 1 and G > 1)):
+            raise GlsError("%s must be [V, ceil(dim / group)] with contiguous rows on the codes' device" % name)
+    if zeros is not None and zeros.dtype is not _U8:
+        raise GlsError("zeros must be uint8")
+    if scales.dtype is not _F32T and scales.dtype is not _BF16T:
+        raise GlsError("scales must be float32 or bfloat16")
+    return _Int4(codes.data_ptr(), codes.stride(0), scales.data_ptr(), F32 if scales.dtype is _F32T else BF16, scales.stride(0),
+                 None if zeros is None else zeros.data_ptr(), 0 if zeros is None else zeros.stride(0), V, D, group), dev, V
+
+
+def quantize_table(weights, group=128, zeros=True, scale_dtype=torch.bfloat16, out=None):
+    """gls_quantize_table: weights [V,D] fp32 or bf16 -> Int4Table with a scale (and a zero) per `group` columns.
+
+    Given `out`, an Int4Table of these sizes, its tensors are written.  Not differentiable."""
+    _no_tangent(weights)
+    _no_gradient("quantize_table", weights)
+    dev = _device(weights, "weights")
+    dt, stride = _matrix(weights, "weights")
+    V, D = weights.shape
+    if out is None:
+        if group not in (32, 64, 128):
+            raise GlsError("group must be 32, 64 or 128")
+        if scale_dtype is not _F32T and scale_dtype is not _BF16T:
+            raise GlsError("scale_dtype must be float32 or bfloat16")
+        new, G = dict(device=weights.device), -(-D // group)
+        out = Int4Table(torch.empty((V, -(-D // 32) * 16), dtype=_U8, **new), torch.empty((V, G), dtype=scale_dtype, **new),
+                        torch.empty((V, G), dtype=_U8, **new) if zeros else None, D, group)
+    t, tdev, tv = _int4(out)
+    if (tv, out.dim, tdev) != (V, D, dev):
+        raise GlsError("out must have the weights' sizes and device")
+    _run(dev, _ready().gls_quantize_table, weights.data_ptr(), dt, stride, t)
+    _wrote(out.codes, out.scales, out.zeros)
+    return out
+
+
+def head_logits(x, table, dtype=None, out=None):
+    """gls_head_logits: x [...,D] fp32 or bf16 times the rows of an Int4Table [V,D] -> logits [...,V] of type `dtype`
+    (x's unless given), accumulated in fp32.  Not differentiable."""
+    _no_tangent(x, table.scales)
+    _no_gradient("head_logits", x, table.scales)
+    dev = _device(x, "x")
+    t, tdev, V = _int4(table)
+    lead = x.shape[:-1]
+    if x.dim() < 1 or x.shape[-1] != table.dim or tdev != dev:
+        raise GlsError("x must be [..., dim] on the table's device")
+    N = lead.numel()
+    try:
+        flat = x.view(N, table.dim)
+    except RuntimeError:
+        flat = x.reshape(N, table.dim)
+    if N > 1 and flat.stride(0) < table.dim:  # an expanded tensor
+        flat = flat.contiguous()
+    dt, stride = _matrix(flat, "x")
+    if out is None:
+        out = torch.empty(lead + (V,), dtype=x.dtype if dtype is None else dtype, device=x.device)
+        ostride = V
+        odt = _matrix(out.view(N, V), "dtype")[0]
+    else:
+        if out.shape != lead + (V,) or out.get_device() != dev or (dtype is not None and out.dtype is not dtype):
+            raise GlsError("out must have shape [..., V] and be on x's device")
+        try:
+            odt, ostride = _matrix(out.view(N, V), "out")
+        except RuntimeError as e:
+            raise e if isinstance(e, GlsError) else GlsError("out's rows must be a constant stride apart") from None
+    _run(dev, _ready().gls_head_logits, flat.data_ptr(), dt, stride, N, t, out.data_ptr(), odt, ostride)
+    _wrote(out)
+    return out
+
+
+def embed_tokens_int4(table, tokens, scale=1.0, dtype=torch.bfloat16, status=None, out=None):
+    """gls_embed_tokens_int4: scale * the rows of an Int4Table [V,D] that int32 tokens of any shape name ->
+    [*tokens.shape, D] of type `dtype`; a token below 0 gives zeros.  Not differentiable."""
+    _no_tangent(table.scales)
+    _no_gradient("embed_tokens_int4", table.scales)
+    t, dev, _ = _int4(table)
+    D, lead = table.dim, tokens.shape
+    tp = _vec(tokens, "tokens", lead, _I32, dev)
+    N = tokens.numel()
+    if out is None:
+        out = torch.empty(lead + (D,), dtype=dtype, device=tokens.device)
+    elif out.shape != lead + (D,) or out.get_device() != dev:
+        raise GlsError("out must have shape [*tokens.shape, dim] and be on the table's device")
+    try:
+        flat = out.view(N, D)  # rows a constant stride apart
+    except RuntimeError:
+        raise GlsError("out's rows must be a constant stride apart") from None
+    odt, ostride = _matrix(flat, "out")
+    _run(dev, _ready().gls_embed_tokens_int4, t, tp, N, float(scale), out.data_ptr(), odt, ostride,
+         _vec(status, "status", (1,), _I32, dev))
+    _wrote(out)
+    return out

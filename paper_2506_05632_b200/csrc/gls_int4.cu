@@ -1,0 +1,163 @@
+// gls_int4.cu -- C ABI of 4-bit tables (see include/gls.h): made from weights, read by token, multiplied with
+// hidden states.
+#include <cmath>
+
+#include "../../include/gls.h"
+#include "gls_host.cuh"
+#include "gls_int4.cuh"
+
+namespace gls {
+
+static bool float_type(int dtype) { return dtype == GLS_F32 || dtype == GLS_BF16; }
+
+static int table_of(const gls_int4_table_t* t, Int4Table* out) {
+  if (!t || !t->codes || !t->scales || t->V <= 0 || t->V >= (1LL << 31) - 65536 || t->D <= 0) return GLS_ERR_INVALID_ARG;
+  if (t->group != 32 && t->group != 64 && t->group != 128) return GLS_ERR_UNSUPPORTED;
+  if (!float_type(t->scale_dtype) || t->D > 32768) return GLS_ERR_UNSUPPORTED;
+  const int64_t G = (t->D + t->group - 1) / t->group;
+  if (t->V > 1 && (t->code_stride < (t->D + 31) / 32 * 16 || t->scale_stride < G || (t->zeros && t->zero_stride < G)))
+    return GLS_ERR_INVALID_ARG;
+  if ((uintptr_t)t->codes % 16 || (t->V > 1 && t->code_stride % 16) || (uintptr_t)t->scales % (t->scale_dtype == GLS_F32 ? 4 : 2))
+    return GLS_ERR_MISALIGNED;
+  out->codes = t->codes;
+  out->code_stride = t->code_stride;
+  out->scales = t->scales;
+  out->scale_stride = t->scale_stride;
+  out->zeros = t->zeros;
+  out->zero_stride = t->zero_stride;
+  out->V = t->V;
+  out->D = t->D;
+  out->G = (int)G;
+  out->log_group = t->group == 32 ? 5 : t->group == 64 ? 6 : 7;
+  out->scale_bf16 = t->scale_dtype == GLS_BF16;
+  return GLS_OK;
+}
+
+// whether rows of `len` bytes written from p lie in the table's memory
+static bool meets_table(const void* p, int64_t n, int64_t pitch, int64_t len, const Int4Table& T) {
+  const int64_t ss = T.scale_bf16 ? 2 : 4;
+  return rows_meet(p, n, pitch, len, T.codes, T.V, T.code_stride, (T.D + 1) / 2) ||
+         rows_meet(p, n, pitch, len, T.scales, T.V, T.scale_stride * ss, T.G * ss) ||
+         (T.zeros && rows_meet(p, n, pitch, len, T.zeros, T.V, T.zero_stride, T.G));
+}
+
+// threads per row, a power of two that leaves few idle and holds whole groups; CTAs for that many rows
+static int lanes_for(long long units, int least) {
+  int n = least;
+  while (n < units && n < kInt4Threads) n *= 2;
+  return n;
+}
+static unsigned ctas_for(long long rows, int lanes) {
+  const long long per = kInt4Threads / lanes, n = (rows + per - 1) / per, cap = (long long)sm_count() * 32;
+  return (unsigned)(n < cap ? n : cap);
+}
+
+template <int GPC, int PARTS>
+static cudaError_t launch_head(HeadArgs& A, cudaStream_t st) {
+  const size_t per_col = (size_t)PARTS * A.chunks * 256, room = 216 * 1024, red = 16 * 128 * 4;
+  long long cols = (long long)(room / per_col);
+  if (cols > 8) cols = 8;
+  if (cols > A.N) cols = A.N;
+  A.cols = (int)cols;
+  const size_t smem = per_col * cols + red;
+  const cudaError_t err = cudaFuncSetAttribute(head_kernel<GPC, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (err != cudaSuccess) return err;
+  A.team = A.chunks >= 16 ? 8 : A.chunks >= 8 ? 4 : A.chunks >= 4 ? 2 : 1;
+  const long long teams = kHeadThreads / 32 / A.team, want = (A.tiles + teams - 1) / teams, most = sm_count();
+  dim3 grid((unsigned)(want < most ? want : most), (unsigned)((A.N + cols - 1) / cols));
+  head_kernel<GPC, PARTS><<<grid, kHeadThreads, smem, st>>>(A);
+  return cudaGetLastError();
+}
+
+template <int PARTS>
+static cudaError_t launch_head_for(HeadArgs& A, cudaStream_t st) {
+  switch (A.T.log_group) {
+    case 5: return launch_head<4, PARTS>(A, st);
+    case 6: return launch_head<2, PARTS>(A, st);
+    default: return launch_head<1, PARTS>(A, st);
+  }
+}
+
+}  // namespace gls
+
+extern "C" {
+
+int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, const gls_int4_table_t* table, void* stream) {
+  using namespace gls;
+  QuantizeArgs A;
+  const int rc = table_of(table, &A.T);
+  if (rc != GLS_OK) return rc;
+  if (!weights || (table->V > 1 && weight_stride < table->D)) return GLS_ERR_INVALID_ARG;
+  if (!float_type(dtype)) return GLS_ERR_UNSUPPORTED;
+  const int es = dtype == GLS_F32 ? 4 : 2;
+  if ((uintptr_t)weights % es) return GLS_ERR_MISALIGNED;
+  if (meets_table(weights, table->V, table->V > 1 ? weight_stride * es : table->D * es, table->D * es, A.T)) return GLS_ERR_INVALID_ARG;
+  A.w = weights;
+  A.stride = weight_stride;
+  A.vec = (uintptr_t)weights % 16 == 0 && (table->V == 1 || weight_stride * es % 16 == 0);
+  A.lanes = lanes_for((long long)A.T.G << (A.T.log_group - 3), 1 << (A.T.log_group - 3));
+  const unsigned grid = ctas_for(A.T.V, A.lanes);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == GLS_F32) quantize_kernel<kF32><<<grid, kInt4Threads, 0, st>>>(A);
+  else quantize_kernel<kBF16><<<grid, kInt4Threads, 0, st>>>(A);
+  return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
+
+int gls_head_logits(const void* x, int x_dtype, int64_t x_stride, int64_t N, const gls_int4_table_t* table, void* out,
+                    int out_dtype, int64_t out_stride, void* stream) {
+  using namespace gls;
+  HeadArgs A;
+  const int rc = table_of(table, &A.T);
+  if (rc != GLS_OK) return rc;
+  if (N < 0 || N > 65535) return GLS_ERR_INVALID_ARG;
+  if (!float_type(x_dtype) || !float_type(out_dtype)) return GLS_ERR_UNSUPPORTED;
+  if (N == 0) return GLS_OK;
+  if (!x || !out || (N > 1 && (x_stride < table->D || out_stride < table->V))) return GLS_ERR_INVALID_ARG;
+  if ((uintptr_t)x % (x_dtype == GLS_F32 ? 4 : 2) || (uintptr_t)out % (out_dtype == GLS_F32 ? 4 : 2)) return GLS_ERR_MISALIGNED;
+  const int xs = x_dtype == GLS_F32 ? 4 : 2, os = out_dtype == GLS_F32 ? 4 : 2;
+  if (meets_table(out, N, N > 1 ? out_stride * os : table->V * os, table->V * os, A.T) ||
+      rows_meet(out, N, N > 1 ? out_stride * os : table->V * os, table->V * os, x, N, N > 1 ? x_stride * xs : table->D * xs, table->D * xs))
+    return GLS_ERR_INVALID_ARG;
+  A.x = (const char*)x;
+  A.x_stride = x_stride;
+  A.N = (int)N;
+  A.out = (char*)out;
+  A.out_stride = out_stride;
+  A.out_bf16 = out_dtype == GLS_BF16;
+  A.chunks = (int)((A.T.D + 127) / 128);
+  A.tiles = (A.T.V + 15) / 16;
+  const cudaError_t err = x_dtype == GLS_BF16 ? launch_head_for<1>(A, (cudaStream_t)stream) : launch_head_for<3>(A, (cudaStream_t)stream);
+  return err == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
+
+int gls_embed_tokens_int4(const gls_int4_table_t* table, const int32_t* tokens, int64_t N, float scale, void* out,
+                          int out_dtype, int64_t out_stride, uint32_t* device_status, void* stream) {
+  using namespace gls;
+  EmbedInt4Args A;
+  const int rc = table_of(table, &A.T);
+  if (rc != GLS_OK) return rc;
+  if (N < 0 || N >= (1LL << 31) - 65536 || !std::isfinite(scale)) return GLS_ERR_INVALID_ARG;
+  if (!float_type(out_dtype)) return GLS_ERR_UNSUPPORTED;
+  if (N == 0) return GLS_OK;
+  if (!tokens || !out || (N > 1 && out_stride < table->D)) return GLS_ERR_INVALID_ARG;
+  const int es = out_dtype == GLS_F32 ? 4 : 2;
+  if ((uintptr_t)out % es) return GLS_ERR_MISALIGNED;
+  const int64_t pitch = N > 1 ? out_stride * es : table->D * es;
+  if (meets_table(out, N, pitch, table->D * es, A.T) || rows_meet(out, N, pitch, table->D * es, tokens, 1, N * 4, N * 4))
+    return GLS_ERR_INVALID_ARG;
+  A.tokens = tokens;
+  A.N = N;
+  A.scale = scale;
+  A.out = (char*)out;
+  A.out_stride = out_stride;
+  A.vec = (uintptr_t)out % 16 == 0 && (N == 1 || out_stride * es % 16 == 0);
+  A.status = device_status;
+  A.lanes = lanes_for((A.T.D + 7) / 8, 1);
+  const unsigned grid = ctas_for(N, A.lanes);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (out_dtype == GLS_F32) embed_int4_kernel<kF32><<<grid, kInt4Threads, 0, st>>>(A);
+  else embed_int4_kernel<kBF16><<<grid, kInt4Threads, 0, st>>>(A);
+  return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
+
+}  // extern "C"

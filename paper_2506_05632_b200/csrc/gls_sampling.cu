@@ -1,0 +1,68 @@
+// gls_sampling.cu -- C ABI of independent sampling by temperature, top-k, top-p and min-p (see include/gls.h).
+#include <cmath>
+
+#include "../../include/gls.h"
+#include "gls_host.cuh"
+#include "gls_sample.cuh"
+
+namespace gls {
+
+static_assert(kSampleBadSetting == GLS_DEV_BAD_SETTING, "header");
+
+static SampleSetting setting(const void* rows, const int64_t* stride, float value, int ivalue) {
+  SampleSetting s;
+  s.rows = rows;
+  s.sb = stride[0], s.sk = stride[1], s.sj = stride[2];
+  s.value = value;
+  s.ivalue = ivalue;
+  return s;
+}
+
+template <int DT, int THREADS>
+static void launch_sample(SampleArgs& A, long long rows, cudaStream_t st) {
+  // as few positions per chunk as leave the row no more chunks than there is room for
+  A.shift = 0;
+  while ((((long long)A.V + 15 + (256LL << A.shift) - 1) >> (8 + A.shift)) > SampleShared<THREADS>::kChunks) ++A.shift;
+  sample_kernel<DT, THREADS><<<(unsigned)rows, THREADS, 0, st>>>(A);
+}
+
+}  // namespace gls
+
+extern "C" int gls_sample_tokens(const gls_rows_t* logits, int B, int K, int J, int64_t V, const gls_sampling_t* s,
+                                 const float* uniforms, int32_t* out_tokens, float* out_logprobs, uint32_t* device_status,
+                                 void* stream) {
+  using namespace gls;
+  if (B <= 0 || K <= 0 || K > GLS_MAX_K || J <= 0 || V <= 0 || V >= (1LL << 31) - 65536 ||
+      (long long)B * K * J >= (1LL << 31) / 64 || !logits || !logits->data || !s || !uniforms || !out_tokens)
+    return GLS_ERR_INVALID_ARG;
+  if (logits->dtype != GLS_F32 && logits->dtype != GLS_BF16) return GLS_ERR_UNSUPPORTED;
+  if ((uintptr_t)logits->data % (logits->dtype == GLS_F32 ? 4 : 2)) return GLS_ERR_MISALIGNED;
+  if (!s->inv_temp_rows) {
+    if (!(s->inv_temp > 0.f)) return GLS_ERR_INVALID_ARG;
+    if (s->inv_temp < 1e-20f || (s->inv_temp > 1e20f && !std::isinf(s->inv_temp))) return GLS_ERR_UNSUPPORTED;
+  }
+  if (!s->top_p_rows && !(s->top_p > 0.f)) return GLS_ERR_INVALID_ARG;
+  if (!s->min_p_rows && !(s->min_p >= 0.f && s->min_p <= 1.f)) return GLS_ERR_INVALID_ARG;
+  SampleArgs A;
+  A.data = logits->data;
+  A.sb = logits->stride_b, A.sk = logits->stride_k, A.sj = logits->stride_j;
+  A.K = K, A.J = J, A.V = (int)V;
+  A.inv_temp = setting(s->inv_temp_rows, s->inv_temp_stride, s->inv_temp, 0);
+  A.top_k = setting(s->top_k_rows, s->top_k_stride, 0.f, s->top_k);
+  A.top_p = setting(s->top_p_rows, s->top_p_stride, s->top_p, 0);
+  A.min_p = setting(s->min_p_rows, s->min_p_stride, s->min_p, 0);
+  A.u = uniforms;
+  A.tokens = out_tokens;
+  A.logprobs = out_logprobs;
+  A.status = device_status;
+  const long long rows = (long long)B * K * J;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (V <= 8192) {
+    if (logits->dtype == GLS_F32) launch_sample<kF32, 128>(A, rows, st);
+    else launch_sample<kBF16, 128>(A, rows, st);
+  } else {
+    if (logits->dtype == GLS_F32) launch_sample<kF32, 512>(A, rows, st);
+    else launch_sample<kBF16, 512>(A, rows, st);
+  }
+  return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+}
