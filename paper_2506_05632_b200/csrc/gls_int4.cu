@@ -52,30 +52,45 @@ static unsigned ctas_for(long long rows, int lanes) {
   return (unsigned)(n < cap ? n : cap);
 }
 
-template <int GPC, int PARTS>
+template <int GPC, int PARTS, int NT, int ST>
 static cudaError_t launch_head(HeadArgs& A, cudaStream_t st) {
-  const size_t per_col = (size_t)PARTS * A.chunks * 256, room = 216 * 1024, red = 16 * 128 * 4;
-  long long cols = (long long)(room / per_col);
-  if (cols > 8) cols = 8;
-  if (cols > A.N) cols = A.N;
-  A.cols = (int)cols;
-  const size_t smem = per_col * cols + red;
-  const cudaError_t err = cudaFuncSetAttribute(head_kernel<GPC, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const size_t smem = (size_t)PARTS * A.chunks * 256 * A.cols + 16 * 128 * 4 * NT + 16;
+  const cudaError_t err = cudaFuncSetAttribute(head_kernel<GPC, PARTS, NT, ST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (err != cudaSuccess) return err;
   A.team = A.chunks >= 16 ? 8 : A.chunks >= 8 ? 4 : A.chunks >= 4 ? 2 : 1;
   const long long teams = kHeadThreads / 32 / A.team, want = (A.tiles + teams - 1) / teams, most = sm_count();
-  dim3 grid((unsigned)(want < most ? want : most), (unsigned)((A.N + cols - 1) / cols));
-  head_kernel<GPC, PARTS><<<grid, kHeadThreads, smem, st>>>(A);
+  dim3 grid((unsigned)(want < most ? want : most), (unsigned)((A.N + A.cols - 1) / A.cols));
+  head_kernel<GPC, PARTS, NT, ST><<<grid, kHeadThreads, smem, st>>>(A);
   return cudaGetLastError();
+}
+
+template <int GPC, int PARTS, int NT>
+static cudaError_t launch_head_scales(HeadArgs& A, cudaStream_t st) {
+  const Int4Table& T = A.T;
+  const int ss = T.scale_bf16 ? 2 : 4;
+  const bool vec = T.G % GPC == 0 && (uintptr_t)T.scales % (GPC * ss) == 0 && (T.V == 1 || T.scale_stride % GPC == 0) &&
+                   (!T.zeros || ((uintptr_t)T.zeros % GPC == 0 && (T.V == 1 || T.zero_stride % GPC == 0)));
+  if (!vec) return launch_head<GPC, PARTS, NT, kScalesAny>(A, st);
+  return T.scale_bf16 ? launch_head<GPC, PARTS, NT, kScalesBF16>(A, st) : launch_head<GPC, PARTS, NT, kScalesF32>(A, st);
+}
+
+template <int PARTS, int NT>
+static cudaError_t launch_head_groups(HeadArgs& A, cudaStream_t st) {
+  switch (A.T.log_group) {
+    case 5: return launch_head_scales<4, PARTS, NT>(A, st);
+    case 6: return launch_head_scales<2, PARTS, NT>(A, st);
+    default: return launch_head_scales<1, PARTS, NT>(A, st);
+  }
 }
 
 template <int PARTS>
 static cudaError_t launch_head_for(HeadArgs& A, cudaStream_t st) {
-  switch (A.T.log_group) {
-    case 5: return launch_head<4, PARTS>(A, st);
-    case 6: return launch_head<2, PARTS>(A, st);
-    default: return launch_head<1, PARTS>(A, st);
-  }
+  const long long fit = 204 * 1024 / ((long long)PARTS * A.chunks * 256);  // hidden states that shared memory holds
+  const long long most = PARTS == 1 ? 16 : 8, cols = fit < most ? fit : most;
+  A.cols = (int)(cols < A.N ? cols : A.N);
+  if constexpr (PARTS == 1)
+    if (A.cols > 8) return launch_head_groups<1, 2>(A, st);
+  return launch_head_groups<PARTS, 1>(A, st);
 }
 
 }  // namespace gls

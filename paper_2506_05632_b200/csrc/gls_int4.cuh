@@ -236,7 +236,7 @@ struct HeadArgs {
 constexpr int kHeadThreads = 512;
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -278,25 +278,39 @@ __device__ __forceinline__ void team_sync(int team, int threads) {  // barrier 0
   else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(threads) : "memory");
 }
 
-template <int GPC>  // groups per chunk of 128 columns
+// How a chunk's scales come: as one aligned vector per row of that type, or one by one.
+enum : int { kScalesF32 = 0, kScalesBF16 = 1, kScalesAny = 2 };
+
+template <int GPC, int ST>  // groups per chunk of 128 columns
 struct HeadChunk {
+  static constexpr int kWords = ST == kScalesBF16 ? (GPC + 1) / 2 : GPC;  // raw scales per row
   uint4 code[2];      // 32 codes of rows gid and gid + 8
-  float scale[2][GPC];
-  uint32_t zero[2][GPC];
+  uint32_t scale[2][kWords];
+  uint32_t zero[2];   // a byte per group
+  __device__ __forceinline__ float step(int r, int g) const {
+    if constexpr (ST == kScalesBF16) return __uint_as_float(g & 1 ? scale[r][g >> 1] & 0xffff0000u : scale[r][g >> 1] << 16);
+    else return __uint_as_float(scale[r][g]);
+  }
+  // 128 + zero twice, in bf16
+  __device__ __forceinline__ uint32_t zero_pair(int r, int g) const {
+    return __byte_perm(zero[r] & 0x0f0f0f0fu, 0x43u, 0x4040u | (uint32_t)g * 0x0101u);
+  }
 };
 
-template <int GPC, int PARTS>
+template <int GPC, int PARTS, int NT, int ST>
 __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A) {
   extern __shared__ __align__(16) uint4 head_shared[];
-  constexpr int kAhead = GPC == 4 ? 3 : 4;
+  constexpr int kAhead = GPC == 4 && ST != kScalesBF16 ? 2 : GPC > 1 || NT > 1 ? 3 : 4;  // what registers hold
+  typedef HeadChunk<GPC, ST> Chunk;
   const Int4Table& T = A.T;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
   const int n0 = blockIdx.y * A.cols, cols = min(A.cols, A.N - n0);
   const int plane = A.chunks * 4 * cols * 4;  // 16-byte units per part
-  uint4* const xs = head_shared;
-  float* const red = (float*)(head_shared + (size_t)PARTS * A.chunks * 16 * A.cols);  // [16 warps][8][16]
+  float* const red = (float*)head_shared;     // [16 warps][8 NT][16]
+  uint4* const xs = head_shared + 16 * 32 * NT;  // a unit of zeros, then the hidden states
 
   // hidden states -> shared memory: unit (chunk, j, n, t) holds 8 columns as pairs (k, k + 4)
+  if (threadIdx.x == 0) xs[0] = make_uint4(0u, 0u, 0u, 0u);
   for (int i = threadIdx.x; i < plane; i += kHeadThreads) {
     const int t = i & 3, n = (i >> 2) % cols, cj = (i >> 2) / cols, j = cj & 3, c = cj >> 2;
     const long long d = (long long)c * 128 + (GPC == 1 ? t * 32 + j * 8 : j * 32 + t * 8);
@@ -314,7 +328,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A)
       uint32_t h[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[e] = PARTS == 1 ? __float_as_uint(v[e]) >> 16 : take_bf16(v[e]);
-      xs[(size_t)part * plane + i] = make_uint4(h[0] | h[4] << 16, h[1] | h[5] << 16, h[2] | h[6] << 16, h[3] | h[7] << 16);
+      xs[1 + (size_t)part * plane + i] = make_uint4(h[0] | h[4] << 16, h[1] | h[5] << 16, h[2] | h[6] << 16, h[3] | h[7] << 16);
     }
   }
   __syncthreads();
@@ -322,60 +336,118 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A)
   const int teams = kHeadThreads / 32 / A.team, my_team = warp / A.team, in_team = warp % A.team;
   const int rounds = (A.chunks + A.team - 1) / A.team;
   const long long first = (long long)blockIdx.x * teams + my_team, stride = (long long)gridDim.x * teams;
-  const long long mine = first < A.tiles ? (A.tiles - first + stride - 1) / stride : 0;
-  const long long steps = mine * rounds;
-  const long long row_bytes = (T.D + 31) / 32 * 16;
+  const int mine = (int)(first < A.tiles ? (A.tiles - first + stride - 1) / stride : 0);
+  const int steps = mine * rounds;
+  const int row_bytes = (int)((T.D + 31) / 32 * 16);
 
-  // what the next request reads
+  // What the next request reads: rows of a tile, chunk l_chunk of them.
   long long l_tile = first;
-  int l_round = 0;
-  auto request = [&](HeadChunk<GPC>& h, bool any) {
-    const int c = l_round * A.team + in_team;
-    const long long at = (long long)c * 64 + tig * 16;
-    const bool in = any && c < A.chunks;
+  int l_chunk = in_team;
+  const uint8_t* l_code[2];
+  const char* l_scale[2];
+  const uint8_t* l_zero[2];
+  const int ss = ST == kScalesAny ? (T.scale_bf16 ? 2 : 4) : ST == kScalesBF16 ? 2 : 4;
+  auto aim = [&]() {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       long long v = l_tile * 16 + gid + 8 * r;
-      if (v >= T.V) v = T.V - 1;
-      h.code[r] = in && at < row_bytes ? ld_stream16(T.codes + v * T.code_stride + at) : make_uint4(0u, 0u, 0u, 0u);
+      if (v >= T.V) v = T.V - 1;  // read again, not stored
+      l_code[r] = T.codes + v * T.code_stride + tig * 16;
+      l_scale[r] = (const char*)T.scales + v * T.scale_stride * ss;
+      l_zero[r] = T.zeros + v * T.zero_stride;
+    }
+  };
+  aim();
+  auto request = [&](Chunk& h, bool any) {
+    if (any) {
+      const bool in = l_chunk * 64 + tig * 16 < row_bytes;
+      const bool some = l_chunk < A.chunks;
 #pragma unroll
-      for (int g = 0; g < GPC; ++g) {
-        const int gg = c * GPC + g;
-        h.scale[r][g] = in && gg < T.G ? int4_scale(T, v, gg) : 0.f;
-        h.zero[r][g] = in && gg < T.G ? int4_zero(T, v, gg) : 8u;
+      for (int r = 0; r < 2; ++r) {
+        h.code[r] = make_uint4(0u, 0u, 0u, 0u);
+        if (in) h.code[r] = ld_stream16(l_code[r] + l_chunk * 64);
+        if constexpr (ST == kScalesAny) {
+#pragma unroll
+          for (int g = 0; g < GPC; ++g) {
+            const int gg = l_chunk * GPC + g;
+            h.scale[r][g] = 0u;
+            if (gg < T.G)
+              h.scale[r][g] = T.scale_bf16 ? (uint32_t)__ldg((const unsigned short*)l_scale[r] + gg) << 16 : __ldg((const uint32_t*)l_scale[r] + gg);
+          }
+        } else if (some) {
+          const char* p = l_scale[r] + l_chunk * (GPC * ss);
+          if constexpr (Chunk::kWords == 4) {
+            const uint4 q = __ldg((const uint4*)p);
+            h.scale[r][0] = q.x, h.scale[r][1] = q.y, h.scale[r][2] = q.z, h.scale[r][3] = q.w;
+          } else if constexpr (Chunk::kWords == 2) {
+            const uint2 q = __ldg((const uint2*)p);
+            h.scale[r][0] = q.x, h.scale[r][1] = q.y;
+          } else if constexpr (ST == kScalesBF16 && GPC == 1) {
+            h.scale[r][0] = __ldg((const unsigned short*)p);
+          } else {
+            h.scale[r][0] = __ldg((const uint32_t*)p);
+          }
+        }
+        h.zero[r] = 0x08080808u;
+        if (T.zeros) {
+          if constexpr (ST == kScalesAny) {
+            h.zero[r] = 0u;
+#pragma unroll
+            for (int g = 0; g < GPC; ++g)
+              if (l_chunk * GPC + g < T.G) h.zero[r] |= (uint32_t)__ldg(l_zero[r] + l_chunk * GPC + g) << (8 * g);
+          } else if (some) {
+            const uint8_t* p = l_zero[r] + l_chunk * GPC;
+            h.zero[r] = GPC == 4 ? __ldg((const uint32_t*)p) : GPC == 2 ? (uint32_t)__ldg((const unsigned short*)p) : (uint32_t)__ldg(p);
+          }
+        }
       }
     }
-    if (++l_round == rounds) l_round = 0, l_tile += stride;
+    l_chunk += A.team;
+    if (l_chunk >= rounds * A.team) {
+      l_chunk = in_team;
+      l_tile += stride;
+      aim();
+    }
   };
 
-  HeadChunk<GPC> ring[kAhead];
+  // where the hidden states of the lane's columns lie: bytes from xs, and from one j to the next
+  uint32_t x_at[NT], x_step[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const bool there = gid + 8 * nt < cols;
+    x_at[nt] = there ? (uint32_t)__cvta_generic_to_shared(xs) + 16u + ((gid + 8 * nt) * 4 + tig) * 16u : (uint32_t)__cvta_generic_to_shared(xs);
+    x_step[nt] = there ? (uint32_t)cols * 64u : 0u;
+  }
+
+  Chunk ring[kAhead];
 #pragma unroll
   for (int q = 0; q < kAhead; ++q) request(ring[q], q < steps);
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  float acc[NT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
   long long tile = first;
-  int round = 0;
-  for (long long s0 = 0; s0 < steps; s0 += kAhead) {
+  int c = in_team;
+  for (int s0 = 0; s0 < steps; s0 += kAhead) {
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
       if (s0 + q >= steps) break;
-      HeadChunk<GPC> h = ring[q];
+      const Chunk h = ring[q];
       request(ring[q], s0 + q + kAhead < steps);
-      const int c = round * A.team + in_team;
       if (c < A.chunks) {
         uint32_t w[2][4] = {{h.code[0].x, h.code[0].y, h.code[0].z, h.code[0].w}, {h.code[1].x, h.code[1].y, h.code[1].z, h.code[1].w}};
         if (GPC > 1) quad_transpose(w[0]), quad_transpose(w[1]);
-        const uint4* xc = xs + (size_t)c * 16 * cols + gid * 4 + tig;
+        uint32_t xa[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) xa[nt] = x_at[nt] + (uint32_t)c * 4u * x_step[nt];
 #pragma unroll
         for (int g = 0; g < GPC; ++g) {
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          const uint32_t z0 = (0x4300u | h.zero[0][g]) * 0x10001u, z1 = (0x4300u | h.zero[1][g]) * 0x10001u;
+          float sum[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) sum[nt][0] = sum[nt][1] = sum[nt][2] = sum[nt][3] = 0.f;
+          const uint32_t z0 = h.zero_pair(0, g), z1 = h.zero_pair(1, g);
 #pragma unroll
           for (int jj = 0; jj < 4 / GPC; ++jj) {
             const int j = g * (4 / GPC) + jj;
-            uint4 b[PARTS];
-#pragma unroll
-            for (int part = 0; part < PARTS; ++part)
-              b[part] = gid < cols ? xc[(size_t)part * plane + j * 4 * cols] : make_uint4(0u, 0u, 0u, 0u);
             uint32_t p0[4], p1[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -384,30 +456,45 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A)
             }
             const uint32_t a0[4] = {p0[0], p1[0], p0[1], p1[1]}, a1[4] = {p0[2], p1[2], p0[3], p1[3]};
 #pragma unroll
-            for (int part = 0; part < PARTS; ++part) {
-              mma_bf16(sum, a0, b[part].x, b[part].y);
-              mma_bf16(sum, a1, b[part].z, b[part].w);
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+              for (int part = 0; part < PARTS; ++part) {
+                uint4 b;
+                const uint32_t at = xa[nt] + (x_step[nt] ? (uint32_t)part * (uint32_t)plane * 16u : 0u);
+                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(at));
+                mma_bf16(sum[nt], a0, b.x, b.y);
+                mma_bf16(sum[nt], a1, b.z, b.w);
+              }
+              xa[nt] += x_step[nt];
             }
           }
-          acc[0] += h.scale[0][g] * sum[0];
-          acc[1] += h.scale[0][g] * sum[1];
-          acc[2] += h.scale[1][g] * sum[2];
-          acc[3] += h.scale[1][g] * sum[3];
+          const float s0v = h.step(0, g), s1v = h.step(1, g);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            acc[nt][0] += s0v * sum[nt][0];
+            acc[nt][1] += s0v * sum[nt][1];
+            acc[nt][2] += s1v * sum[nt][2];
+            acc[nt][3] += s1v * sum[nt][3];
+          }
         }
       }
-      if (++round == rounds) {
+      c += A.team;
+      if (c >= rounds * A.team) {
         // the team's sums: [warp][column][row]
-        float* mine_at = red + warp * 128;
-        mine_at[(2 * tig) * 16 + gid] = acc[0];
-        mine_at[(2 * tig + 1) * 16 + gid] = acc[1];
-        mine_at[(2 * tig) * 16 + gid + 8] = acc[2];
-        mine_at[(2 * tig + 1) * 16 + gid + 8] = acc[3];
+        constexpr int kPer = 128 * NT;
+        float* mine_at = red + warp * kPer;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float* q_at = mine_at + (8 * nt + 2 * tig) * 16 + gid;
+          q_at[0] = acc[nt][0], q_at[16] = acc[nt][1], q_at[8] = acc[nt][2], q_at[24] = acc[nt][3];
+          acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
+        }
         const int threads = A.team * 32;
         team_sync(my_team, threads);
-        const float* team_at = red + my_team * A.team * 128;
+        const float* team_at = red + my_team * A.team * kPer;
         for (int i = in_team * 32 + lane; i < 16 * cols; i += threads) {
           float y = 0.f;
-          for (int k = 0; k < A.team; ++k) y += team_at[k * 128 + i];
+          for (int k = 0; k < A.team; ++k) y += team_at[k * kPer + i];
           const long long v = tile * 16 + (i & 15);
           if (v < T.V) {
             const long long at = (long long)(n0 + (i >> 4)) * A.out_stride + v;
@@ -416,8 +503,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A)
           }
         }
         team_sync(my_team, threads);
-        acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-        round = 0;
+        c = in_team;
         tile += stride;
       }
     }
