@@ -52,26 +52,28 @@ static unsigned ctas_for(long long rows, int lanes) {
   return (unsigned)(n < cap ? n : cap);
 }
 
-template <int GPC, int PARTS, int NT, int ST>
-static cudaError_t launch_head(HeadArgs& A, cudaStream_t st) {
-  const size_t smem = (size_t)PARTS * A.chunks * 256 * A.cols + 16 * 128 * 4 * NT + 16;
-  const cudaError_t err = cudaFuncSetAttribute(head_kernel<GPC, PARTS, NT, ST>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+static cudaError_t launch_head(void (*kernel)(HeadArgs), int parts, int nt, HeadArgs& A, cudaStream_t st) {
+  const int steps = (A.chunks + 1) / 2;
+  const size_t smem = (size_t)parts * steps * 512 * A.cols + 16 * 128 * 4 * nt + 16;
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (err != cudaSuccess) return err;
-  A.team = A.chunks >= 16 ? 8 : A.chunks >= 8 ? 4 : A.chunks >= 4 ? 2 : 1;
+  A.team = steps >= 16 ? 8 : steps >= 8 ? 4 : steps >= 4 ? 2 : 1;
   const long long teams = kHeadThreads / 32 / A.team, want = (A.tiles + teams - 1) / teams, most = sm_count();
   dim3 grid((unsigned)(want < most ? want : most), (unsigned)((A.N + A.cols - 1) / A.cols));
-  head_kernel<GPC, PARTS, NT, ST><<<grid, kHeadThreads, smem, st>>>(A);
+  kernel<<<grid, kHeadThreads, smem, st>>>(A);
   return cudaGetLastError();
 }
 
 template <int GPC, int PARTS, int NT>
 static cudaError_t launch_head_scales(HeadArgs& A, cudaStream_t st) {
   const Int4Table& T = A.T;
-  const int ss = T.scale_bf16 ? 2 : 4;
-  const bool vec = T.G % GPC == 0 && (uintptr_t)T.scales % (GPC * ss) == 0 && (T.V == 1 || T.scale_stride % GPC == 0) &&
-                   (!T.zeros || ((uintptr_t)T.zeros % GPC == 0 && (T.V == 1 || T.zero_stride % GPC == 0)));
-  if (!vec) return launch_head<GPC, PARTS, NT, kScalesAny>(A, st);
-  return T.scale_bf16 ? launch_head<GPC, PARTS, NT, kScalesBF16>(A, st) : launch_head<GPC, PARTS, NT, kScalesF32>(A, st);
+  const int ss = T.scale_bf16 ? 2 : 4, per = 2 * GPC, align = per * ss < 16 ? per * ss : 16;
+  const bool vec = T.G % per == 0 && (uintptr_t)T.scales % align == 0 && (T.V == 1 || T.scale_stride * ss % align == 0) &&
+                   (!T.zeros || ((uintptr_t)T.zeros % per == 0 && (T.V == 1 || T.zero_stride % per == 0)));
+  return launch_head(!vec           ? head_kernel<GPC, PARTS, NT, kScalesAny>
+                     : T.scale_bf16 ? head_kernel<GPC, PARTS, NT, kScalesBF16>
+                                    : head_kernel<GPC, PARTS, NT, kScalesF32>,
+                     PARTS, NT, A, st);
 }
 
 template <int PARTS, int NT>
@@ -85,9 +87,10 @@ static cudaError_t launch_head_groups(HeadArgs& A, cudaStream_t st) {
 
 template <int PARTS>
 static cudaError_t launch_head_for(HeadArgs& A, cudaStream_t st) {
-  const long long fit = 204 * 1024 / ((long long)PARTS * A.chunks * 256);  // hidden states that shared memory holds
+  const long long fit = 204 * 1024 / ((long long)PARTS * ((A.chunks + 1) / 2) * 512);  // hidden states that shared memory holds
   const long long most = PARTS == 1 ? 16 : 8, cols = fit < most ? fit : most;
   A.cols = (int)(cols < A.N ? cols : A.N);
+  if (A.cols <= 2) return launch_head(A.T.scale_bf16 ? head_few_kernel<PARTS, kScalesBF16> : head_few_kernel<PARTS, kScalesF32>, PARTS, 1, A, st);
   if constexpr (PARTS == 1)
     if (A.cols > 8) return launch_head_groups<1, 2>(A, st);
   return launch_head_groups<PARTS, 1>(A, st);

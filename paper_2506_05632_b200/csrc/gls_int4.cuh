@@ -278,47 +278,88 @@ __device__ __forceinline__ void team_sync(int team, int threads) {  // barrier 0
   else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(threads) : "memory");
 }
 
-// How a chunk's scales come: as one aligned vector per row of that type, or one by one.
+// How the scales come: as one aligned vector per row and step of that type, or one by one.
 enum : int { kScalesF32 = 0, kScalesBF16 = 1, kScalesAny = 2 };
 
-template <int GPC, int ST>  // groups per chunk of 128 columns
-struct HeadChunk {
-  static constexpr int kWords = ST == kScalesBF16 ? (GPC + 1) / 2 : GPC;  // raw scales per row
-  uint4 code[2];      // 32 codes of rows gid and gid + 8
+template <int BYTES>
+__device__ __forceinline__ void load_words(uint32_t* w, const char* p) {
+  if constexpr (BYTES == 1) {
+    w[0] = __ldg((const uint8_t*)p);
+  } else if constexpr (BYTES == 2) {
+    w[0] = __ldg((const unsigned short*)p);
+  } else if constexpr (BYTES == 4) {
+    w[0] = __ldg((const uint32_t*)p);
+  } else if constexpr (BYTES == 8) {
+    const uint2 q = __ldg((const uint2*)p);
+    w[0] = q.x, w[1] = q.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < BYTES / 16; ++i) {
+      const uint4 q = __ldg((const uint4*)p + i);
+      w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+    }
+  }
+}
+
+// A step: 256 columns of 16 rows.  Lane (gid, tig) has columns 32 tig .. 32 tig + 31 of each half for rows gid, gid + 8.
+template <int GPC, int ST>  // groups per 128 columns
+struct HeadStep {
+  static constexpr int kGroups = 2 * GPC;
+  static constexpr int kWords = ST == kScalesBF16 ? GPC : kGroups;  // raw scales per row
+  uint4 code[2][2];  // [row][half]
   uint32_t scale[2][kWords];
-  uint32_t zero[2];   // a byte per group
+  uint32_t zero[2][(kGroups + 3) / 4];  // a byte per group
   __device__ __forceinline__ float step(int r, int g) const {
     if constexpr (ST == kScalesBF16) return __uint_as_float(g & 1 ? scale[r][g >> 1] & 0xffff0000u : scale[r][g >> 1] << 16);
     else return __uint_as_float(scale[r][g]);
   }
-  // 128 + zero twice, in bf16
+  // 128 + zero twice, in bf16; the low four bits of a zero count
   __device__ __forceinline__ uint32_t zero_pair(int r, int g) const {
-    return __byte_perm(zero[r] & 0x0f0f0f0fu, 0x43u, 0x4040u | (uint32_t)g * 0x0101u);
+    return __byte_perm(zero[r][g >> 2] & 0x0f0f0f0fu, 0x43u, 0x4040u | (uint32_t)(g & 3) * 0x0101u);
   }
 };
 
-template <int GPC, int PARTS, int NT, int ST>
-__global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A) {
-  extern __shared__ __align__(16) uint4 head_shared[];
-  constexpr int kAhead = GPC == 4 && ST != kScalesBF16 ? 2 : GPC > 1 || NT > 1 ? 3 : 4;  // what registers hold
-  typedef HeadChunk<GPC, ST> Chunk;
-  const Int4Table& T = A.T;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
-  const int n0 = blockIdx.y * A.cols, cols = min(A.cols, A.N - n0);
-  const int plane = A.chunks * 4 * cols * 4;  // 16-byte units per part
-  float* const red = (float*)head_shared;     // [16 warps][8 NT][16]
-  uint4* const xs = head_shared + 16 * 32 * NT;  // a unit of zeros, then the hidden states
+// Position of a warp in its CTA's share of the table: teams of warps take tiles of 16 rows, a warp every team-th step of
+// them, and its requests run some steps ahead of its products, across tiles.
+struct HeadWalk {
+  int in_team, team, rounds, steps_per_row;
+  long long first, stride;
+  int steps;
+  __device__ __forceinline__ HeadWalk(const HeadArgs& A, int teams, int my_team, int warp_in_team) {
+    in_team = warp_in_team;
+    team = A.team;
+    steps_per_row = (A.chunks + 1) >> 1;
+    rounds = (steps_per_row + team - 1) / team;
+    first = (long long)blockIdx.x * teams + my_team;
+    stride = (long long)gridDim.x * teams;
+    steps = (int)(first < A.tiles ? (A.tiles - first + stride - 1) / stride : 0) * rounds;
+  }
+};
 
-  // hidden states -> shared memory: unit (chunk, j, n, t) holds 8 columns as pairs (k, k + 4)
-  if (threadIdx.x == 0) xs[0] = make_uint4(0u, 0u, 0u, 0u);
-  for (int i = threadIdx.x; i < plane; i += kHeadThreads) {
+// A 4-column pair of codes as bf16 differences to their zero
+__device__ __forceinline__ void int4_pairs(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = sub_bf16x2(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u, z);
+}
+
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 b;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(at));
+  return b;
+}
+
+// Hidden states -> shared memory in parts of bf16: unit (chunk, j, n, t) holds 8 columns as pairs (k, k + 4); QUAD: those
+// of a lane's own 32 columns, otherwise those that the exchanged words of a quad are of.
+template <int PARTS, bool QUAD>
+__device__ __forceinline__ void stage_hidden(const HeadArgs& A, uint4* xs, int n0, int cols, int units, int plane) {
+  for (int i = threadIdx.x; i < units; i += kHeadThreads) {
     const int t = i & 3, n = (i >> 2) % cols, cj = (i >> 2) / cols, j = cj & 3, c = cj >> 2;
-    const long long d = (long long)c * 128 + (GPC == 1 ? t * 32 + j * 8 : j * 32 + t * 8);
+    const long long d = (long long)c * 128 + (QUAD ? t * 32 + j * 8 : j * 32 + t * 8);
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[e] = 0.f;
-      if (d + e < T.D) {
+      if (d + e < A.T.D) {
         const long long at = (long long)(n0 + n) * A.x_stride + d + e;
         v[e] = PARTS == 1 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)A.x + at) << 16) : __ldg((const float*)A.x + at);
       }
@@ -328,183 +369,319 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A)
       uint32_t h[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[e] = PARTS == 1 ? __float_as_uint(v[e]) >> 16 : take_bf16(v[e]);
-      xs[1 + (size_t)part * plane + i] = make_uint4(h[0] | h[4] << 16, h[1] | h[5] << 16, h[2] | h[6] << 16, h[3] | h[7] << 16);
+      xs[(size_t)part * plane + i] = make_uint4(h[0] | h[4] << 16, h[1] | h[5] << 16, h[2] | h[6] << 16, h[3] | h[7] << 16);
     }
   }
+}
+
+// The sums that a team's warps left in `red` [warp][column][row], added up and stored.
+template <int NT>
+__device__ __forceinline__ void head_store(const HeadArgs& A, const float* team_at, int thread, int threads, int n0, int cols, long long tile) {
+  for (int i = thread; i < 16 * cols; i += threads) {
+    float y = 0.f;
+    for (int k = 0; k < A.team; ++k) y += team_at[k * 128 * NT + i];
+    const long long v = tile * 16 + (i & 15);
+    if (v < A.T.V) {
+      const long long at = (long long)(n0 + (i >> 4)) * A.out_stride + v;
+      if (A.out_bf16) ((unsigned short*)A.out)[at] = (unsigned short)bf16_bits(y);
+      else ((float*)A.out)[at] = y;
+    }
+  }
+}
+
+template <int GPC, int PARTS, int NT, int ST>
+__global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A) {
+  extern __shared__ __align__(16) uint4 head_shared[];
+  typedef HeadStep<GPC, ST> Step;
+  constexpr int kAhead = GPC == 4 || (GPC == 2 && ST != kScalesBF16) ? 1 : 2;  // what registers hold
+  const Int4Table& T = A.T;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
+  const int n0 = blockIdx.y * A.cols, cols = min(A.cols, A.N - n0);
+  const int chunks2 = (A.chunks + 1) & ~1;
+  const int plane = chunks2 * 16 * cols;      // 16-byte units per part
+  float* const red = (float*)head_shared;     // [16 warps][8 NT][16]
+  uint4* const xs = head_shared + 16 * 32 * NT;  // a unit of zeros, then the hidden states
+  if (threadIdx.x == 0) xs[0] = make_uint4(0u, 0u, 0u, 0u);
+  stage_hidden<PARTS, GPC == 1>(A, xs + 1, n0, cols, plane, plane);
   __syncthreads();
 
-  const int teams = kHeadThreads / 32 / A.team, my_team = warp / A.team, in_team = warp % A.team;
-  const int rounds = (A.chunks + A.team - 1) / A.team;
-  const long long first = (long long)blockIdx.x * teams + my_team, stride = (long long)gridDim.x * teams;
-  const int mine = (int)(first < A.tiles ? (A.tiles - first + stride - 1) / stride : 0);
-  const int steps = mine * rounds;
-  const int row_bytes = (int)((T.D + 31) / 32 * 16);
+  const int teams = kHeadThreads / 32 / A.team, my_team = warp / A.team;
+  const HeadWalk W(A, teams, my_team, warp % A.team);
+  const int row_last = (int)((T.D + 31) / 32 * 16) - 16;
 
-  // What the next request reads: rows of a tile, chunk l_chunk of them.
-  long long l_tile = first;
-  int l_chunk = in_team;
+  // What the next request reads: step l_step of the rows at l_code.  Codes and scales behind a row's end
+  // are replaced by its last ones: the hidden states there are zeros.
+  long long l_tile = W.first;
+  int l_step = W.in_team;
   const uint8_t* l_code[2];
   const char* l_scale[2];
   const uint8_t* l_zero[2];
-  const int ss = ST == kScalesAny ? (T.scale_bf16 ? 2 : 4) : ST == kScalesBF16 ? 2 : 4;
+  constexpr int ss = ST == kScalesBF16 ? 2 : 4;
+  const int ss_any = T.scale_bf16 ? 2 : 4;
   auto aim = [&]() {
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       long long v = l_tile * 16 + gid + 8 * r;
       if (v >= T.V) v = T.V - 1;  // read again, not stored
-      l_code[r] = T.codes + v * T.code_stride + tig * 16;
+      l_code[r] = T.codes + v * T.code_stride;
+      l_scale[r] = (const char*)T.scales + v * T.scale_stride * (ST == kScalesAny ? ss_any : ss);
+      l_zero[r] = T.zeros + v * T.zero_stride;
+    }
+  };
+  aim();
+  auto request = [&](Step& h) {
+    const int at0 = min(l_step * 128 + tig * 16, row_last), at1 = min(l_step * 128 + tig * 16 + 64, row_last);
+    const int s = min(l_step, W.steps_per_row - 1);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      h.code[r][0] = ld_stream16(l_code[r] + at0);
+      h.code[r][1] = ld_stream16(l_code[r] + at1);
+      if constexpr (ST == kScalesAny) {
+#pragma unroll
+        for (int g = 0; g < Step::kGroups; ++g) {
+          const int gg = min(s * Step::kGroups + g, T.G - 1);
+          h.scale[r][g] = T.scale_bf16 ? (uint32_t)__ldg((const unsigned short*)l_scale[r] + gg) << 16 : __ldg((const uint32_t*)l_scale[r] + gg);
+        }
+      } else {
+        load_words<Step::kGroups * ss>(h.scale[r], l_scale[r] + s * (Step::kGroups * ss));
+      }
+      if (T.zeros) {
+        if constexpr (ST == kScalesAny) {
+#pragma unroll
+          for (int i = 0; i < (Step::kGroups + 3) / 4; ++i) h.zero[r][i] = 0u;
+#pragma unroll
+          for (int g = 0; g < Step::kGroups; ++g)
+            h.zero[r][g >> 2] |= (uint32_t)__ldg(l_zero[r] + min(s * Step::kGroups + g, T.G - 1)) << (8 * (g & 3));
+        } else {
+          load_words<Step::kGroups>(h.zero[r], (const char*)l_zero[r] + s * Step::kGroups);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < (Step::kGroups + 3) / 4; ++i) h.zero[r][i] = 0x08080808u;
+      }
+    }
+    l_step += W.team;
+    if (l_step >= W.rounds * W.team) {
+      l_step = W.in_team;
+      l_tile += W.stride;
+      aim();
+    }
+  };
+
+  // where the hidden states of the lane's columns lie: bytes, and from one j to the next
+  uint32_t x_at[NT], x_step[NT], x_part[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const bool there = gid + 8 * nt < cols;
+    x_at[nt] = (uint32_t)__cvta_generic_to_shared(xs) + (there ? 16u + ((gid + 8 * nt) * 4 + tig) * 16u : 0u);
+    x_step[nt] = there ? (uint32_t)cols * 64u : 0u;
+    x_part[nt] = there ? (uint32_t)plane * 16u : 0u;
+  }
+
+  Step ring[kAhead];
+#pragma unroll
+  for (int q = 0; q < kAhead; ++q)
+    if (q < W.steps) request(ring[q]);
+  float acc[NT][4];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
+  long long tile = W.first;
+  int s = W.in_team;
+  for (int s0 = 0; s0 < W.steps; s0 += kAhead) {
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) {
+      if (s0 + q >= W.steps) break;
+      Step& h = ring[q];
+      if (s < W.steps_per_row) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t w[2][4];
+#pragma unroll
+          for (int r = 0; r < 2; ++r) w[r][0] = h.code[r][half].x, w[r][1] = h.code[r][half].y, w[r][2] = h.code[r][half].z, w[r][3] = h.code[r][half].w;
+          if (GPC > 1) quad_transpose(w[0]), quad_transpose(w[1]);
+          uint32_t xa[NT];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) xa[nt] = x_at[nt] + (uint32_t)(2 * s + half) * 4u * x_step[nt];
+#pragma unroll
+          for (int gl = 0; gl < GPC; ++gl) {
+            const int g = half * GPC + gl;
+            float sum[NT][4];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) sum[nt][0] = sum[nt][1] = sum[nt][2] = sum[nt][3] = 0.f;
+            const uint32_t z0 = h.zero_pair(0, g), z1 = h.zero_pair(1, g);
+#pragma unroll
+            for (int jj = 0; jj < 4 / GPC; ++jj) {
+              const int j = gl * (4 / GPC) + jj;
+              uint32_t p0[4], p1[4];
+              int4_pairs(w[0][j], z0, p0);
+              int4_pairs(w[1][j], z1, p1);
+              const uint32_t a0[4] = {p0[0], p1[0], p0[1], p1[1]}, a1[4] = {p0[2], p1[2], p0[3], p1[3]};
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                  const uint4 b = lds16(xa[nt] + (uint32_t)part * x_part[nt]);
+                  mma_bf16(sum[nt], a0, b.x, b.y);
+                  mma_bf16(sum[nt], a1, b.z, b.w);
+                }
+                xa[nt] += x_step[nt];
+              }
+            }
+            const float s0v = h.step(0, g), s1v = h.step(1, g);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              acc[nt][0] += s0v * sum[nt][0];
+              acc[nt][1] += s0v * sum[nt][1];
+              acc[nt][2] += s1v * sum[nt][2];
+              acc[nt][3] += s1v * sum[nt][3];
+            }
+          }
+        }
+      }
+      if (s0 + q + kAhead < W.steps) request(h);
+      s += W.team;
+      if (s >= W.rounds * W.team) {
+        float* q_at = red + warp * 128 * NT + 2 * tig * 16 + gid;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          q_at[128 * nt] = acc[nt][0], q_at[128 * nt + 16] = acc[nt][1];
+          q_at[128 * nt + 8] = acc[nt][2], q_at[128 * nt + 24] = acc[nt][3];
+          acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
+        }
+        team_sync(my_team, W.team * 32);
+        head_store<NT>(A, red + my_team * W.team * 128 * NT, W.in_team * 32 + lane, W.team * 32, n0, cols, tile);
+        team_sync(my_team, W.team * 32);
+        s = W.in_team;
+        tile += W.stride;
+      }
+    }
+  }
+}
+
+// The same for one or two hidden states.  The instruction's eight columns then are two hidden states times the four
+// lanes of a quad: column 2 t + n holds hidden state n where the k belong to lane t and zeros elsewhere, so that the sums of
+// lanes t come apart.  Each is of 32 neighbouring columns, hence of one group, whatever the groups' size, and lane t
+// holds it: it multiplies it by its own scale, no words are exchanged, and scales need no alignment.
+template <int PARTS, int ST>
+__global__ void __launch_bounds__(kHeadThreads, 1) head_few_kernel(const HeadArgs A) {
+  extern __shared__ __align__(16) uint4 head_shared[];
+  constexpr int kAhead = 2;
+  const Int4Table& T = A.T;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
+  const int n0 = blockIdx.y * A.cols, cols = min(A.cols, A.N - n0);
+  const int chunks2 = (A.chunks + 1) & ~1;
+  const int plane = chunks2 * 16 * cols;
+  float* const red = (float*)head_shared;
+  uint4* const xs = head_shared + 16 * 32;
+  if (threadIdx.x == 0) xs[0] = make_uint4(0u, 0u, 0u, 0u);
+  stage_hidden<PARTS, true>(A, xs + 1, n0, cols, plane, plane);
+  __syncthreads();
+
+  const int teams = kHeadThreads / 32 / A.team, my_team = warp / A.team;
+  const HeadWalk W(A, teams, my_team, warp % A.team);
+  const int row_last = (int)((T.D + 31) / 32 * 16) - 16;
+  struct Step {
+    uint4 code[2][2];
+    uint32_t scale[2][2], zero[2][2];
+  };
+  long long l_tile = W.first;
+  int l_step = W.in_team;
+  const uint8_t* l_code[2];
+  const char* l_scale[2];
+  const uint8_t* l_zero[2];
+  constexpr int ss = ST == kScalesBF16 ? 2 : 4;
+  auto aim = [&]() {
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      long long v = l_tile * 16 + gid + 8 * r;
+      if (v >= T.V) v = T.V - 1;
+      l_code[r] = T.codes + v * T.code_stride;
       l_scale[r] = (const char*)T.scales + v * T.scale_stride * ss;
       l_zero[r] = T.zeros + v * T.zero_stride;
     }
   };
   aim();
-  auto request = [&](Chunk& h, bool any) {
-    if (any) {
-      const bool in = l_chunk * 64 + tig * 16 < row_bytes;
-      const bool some = l_chunk < A.chunks;
+  auto request = [&](Step& h) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int at = min(l_step * 128 + half * 64 + tig * 16, row_last), g = at >> (T.log_group - 1);
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        h.code[r] = make_uint4(0u, 0u, 0u, 0u);
-        if (in) h.code[r] = ld_stream16(l_code[r] + l_chunk * 64);
-        if constexpr (ST == kScalesAny) {
-#pragma unroll
-          for (int g = 0; g < GPC; ++g) {
-            const int gg = l_chunk * GPC + g;
-            h.scale[r][g] = 0u;
-            if (gg < T.G)
-              h.scale[r][g] = T.scale_bf16 ? (uint32_t)__ldg((const unsigned short*)l_scale[r] + gg) << 16 : __ldg((const uint32_t*)l_scale[r] + gg);
-          }
-        } else if (some) {
-          const char* p = l_scale[r] + l_chunk * (GPC * ss);
-          if constexpr (Chunk::kWords == 4) {
-            const uint4 q = __ldg((const uint4*)p);
-            h.scale[r][0] = q.x, h.scale[r][1] = q.y, h.scale[r][2] = q.z, h.scale[r][3] = q.w;
-          } else if constexpr (Chunk::kWords == 2) {
-            const uint2 q = __ldg((const uint2*)p);
-            h.scale[r][0] = q.x, h.scale[r][1] = q.y;
-          } else if constexpr (ST == kScalesBF16 && GPC == 1) {
-            h.scale[r][0] = __ldg((const unsigned short*)p);
-          } else {
-            h.scale[r][0] = __ldg((const uint32_t*)p);
-          }
-        }
-        h.zero[r] = 0x08080808u;
-        if (T.zeros) {
-          if constexpr (ST == kScalesAny) {
-            h.zero[r] = 0u;
-#pragma unroll
-            for (int g = 0; g < GPC; ++g)
-              if (l_chunk * GPC + g < T.G) h.zero[r] |= (uint32_t)__ldg(l_zero[r] + l_chunk * GPC + g) << (8 * g);
-          } else if (some) {
-            const uint8_t* p = l_zero[r] + l_chunk * GPC;
-            h.zero[r] = GPC == 4 ? __ldg((const uint32_t*)p) : GPC == 2 ? (uint32_t)__ldg((const unsigned short*)p) : (uint32_t)__ldg(p);
-          }
-        }
+        h.code[r][half] = ld_stream16(l_code[r] + at);
+        load_words<ss>(&h.scale[r][half], l_scale[r] + g * ss);
+        h.zero[r][half] = 8u;
+        if (T.zeros) h.zero[r][half] = __ldg(l_zero[r] + g);
       }
     }
-    l_chunk += A.team;
-    if (l_chunk >= rounds * A.team) {
-      l_chunk = in_team;
-      l_tile += stride;
+    l_step += W.team;
+    if (l_step >= W.rounds * W.team) {
+      l_step = W.in_team;
+      l_tile += W.stride;
       aim();
     }
   };
+  const bool there = tig == gid >> 1 && (gid & 1) < cols;
+  const uint32_t x_at = (uint32_t)__cvta_generic_to_shared(xs) + (there ? 16u + ((gid & 1) * 4 + tig) * 16u : 0u);
+  const uint32_t x_step = there ? (uint32_t)cols * 64u : 0u, x_part = there ? (uint32_t)plane * 16u : 0u;
 
-  // where the hidden states of the lane's columns lie: bytes from xs, and from one j to the next
-  uint32_t x_at[NT], x_step[NT];
+  Step ring[kAhead];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const bool there = gid + 8 * nt < cols;
-    x_at[nt] = there ? (uint32_t)__cvta_generic_to_shared(xs) + 16u + ((gid + 8 * nt) * 4 + tig) * 16u : (uint32_t)__cvta_generic_to_shared(xs);
-    x_step[nt] = there ? (uint32_t)cols * 64u : 0u;
-  }
-
-  Chunk ring[kAhead];
-#pragma unroll
-  for (int q = 0; q < kAhead; ++q) request(ring[q], q < steps);
-  float acc[NT][4];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
-  long long tile = first;
-  int c = in_team;
-  for (int s0 = 0; s0 < steps; s0 += kAhead) {
+  for (int q = 0; q < kAhead; ++q)
+    if (q < W.steps) request(ring[q]);
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  long long tile = W.first;
+  int s = W.in_team;
+  for (int s0 = 0; s0 < W.steps; s0 += kAhead) {
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
-      if (s0 + q >= steps) break;
-      const Chunk h = ring[q];
-      request(ring[q], s0 + q + kAhead < steps);
-      if (c < A.chunks) {
-        uint32_t w[2][4] = {{h.code[0].x, h.code[0].y, h.code[0].z, h.code[0].w}, {h.code[1].x, h.code[1].y, h.code[1].z, h.code[1].w}};
-        if (GPC > 1) quad_transpose(w[0]), quad_transpose(w[1]);
-        uint32_t xa[NT];
+      if (s0 + q >= W.steps) break;
+      Step& h = ring[q];
+      if (s < W.steps_per_row) {
+        uint32_t xa = x_at + (uint32_t)s * 8u * x_step;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) xa[nt] = x_at[nt] + (uint32_t)c * 4u * x_step[nt];
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t w[2][4] = {{h.code[0][half].x, h.code[0][half].y, h.code[0][half].z, h.code[0][half].w},
+                                    {h.code[1][half].x, h.code[1][half].y, h.code[1][half].z, h.code[1][half].w}};
+          const uint32_t z0 = ((h.zero[0][half] & 15u) | 0x4300u) * 0x10001u, z1 = ((h.zero[1][half] & 15u) | 0x4300u) * 0x10001u;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int g = 0; g < GPC; ++g) {
-          float sum[NT][4];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) sum[nt][0] = sum[nt][1] = sum[nt][2] = sum[nt][3] = 0.f;
-          const uint32_t z0 = h.zero_pair(0, g), z1 = h.zero_pair(1, g);
-#pragma unroll
-          for (int jj = 0; jj < 4 / GPC; ++jj) {
-            const int j = g * (4 / GPC) + jj;
+          for (int j = 0; j < 4; ++j) {
             uint32_t p0[4], p1[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              p0[i] = sub_bf16x2(((w[0][j] >> (4 * i)) & 0x000f000fu) | 0x43004300u, z0);
-              p1[i] = sub_bf16x2(((w[1][j] >> (4 * i)) & 0x000f000fu) | 0x43004300u, z1);
-            }
+            int4_pairs(w[0][j], z0, p0);
+            int4_pairs(w[1][j], z1, p1);
             const uint32_t a0[4] = {p0[0], p1[0], p0[1], p1[1]}, a1[4] = {p0[2], p1[2], p0[3], p1[3]};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-              for (int part = 0; part < PARTS; ++part) {
-                uint4 b;
-                const uint32_t at = xa[nt] + (x_step[nt] ? (uint32_t)part * (uint32_t)plane * 16u : 0u);
-                asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(at));
-                mma_bf16(sum[nt], a0, b.x, b.y);
-                mma_bf16(sum[nt], a1, b.z, b.w);
-              }
-              xa[nt] += x_step[nt];
+            for (int part = 0; part < PARTS; ++part) {
+              const uint4 b = lds16(xa + (uint32_t)part * x_part);
+              mma_bf16(sum, a0, b.x, b.y);
+              mma_bf16(sum, a1, b.z, b.w);
             }
+            xa += x_step;
           }
-          const float s0v = h.step(0, g), s1v = h.step(1, g);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            acc[nt][0] += s0v * sum[nt][0];
-            acc[nt][1] += s0v * sum[nt][1];
-            acc[nt][2] += s1v * sum[nt][2];
-            acc[nt][3] += s1v * sum[nt][3];
-          }
+          const float s0v = __uint_as_float(ST == kScalesBF16 ? h.scale[0][half] << 16 : h.scale[0][half]);
+          const float s1v = __uint_as_float(ST == kScalesBF16 ? h.scale[1][half] << 16 : h.scale[1][half]);
+          acc[0] += s0v * sum[0], acc[1] += s0v * sum[1];
+          acc[2] += s1v * sum[2], acc[3] += s1v * sum[3];
         }
       }
-      c += A.team;
-      if (c >= rounds * A.team) {
-        // the team's sums: [warp][column][row]
-        constexpr int kPer = 128 * NT;
-        float* mine_at = red + warp * kPer;
+      if (s0 + q + kAhead < W.steps) request(h);
+      s += W.team;
+      if (s >= W.rounds * W.team) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float* q_at = mine_at + (8 * nt + 2 * tig) * 16 + gid;
-          q_at[0] = acc[nt][0], q_at[16] = acc[nt][1], q_at[8] = acc[nt][2], q_at[24] = acc[nt][3];
-          acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
+        for (int i = 0; i < 4; ++i) {
+          acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 1);
+          acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 2);
         }
-        const int threads = A.team * 32;
-        team_sync(my_team, threads);
-        const float* team_at = red + my_team * A.team * kPer;
-        for (int i = in_team * 32 + lane; i < 16 * cols; i += threads) {
-          float y = 0.f;
-          for (int k = 0; k < A.team; ++k) y += team_at[k * kPer + i];
-          const long long v = tile * 16 + (i & 15);
-          if (v < T.V) {
-            const long long at = (long long)(n0 + (i >> 4)) * A.out_stride + v;
-            if (A.out_bf16) ((unsigned short*)A.out)[at] = (unsigned short)bf16_bits(y);
-            else ((float*)A.out)[at] = y;
-          }
+        if (tig == 0) {
+          float* q_at = red + warp * 128 + gid;
+          q_at[0] = acc[0], q_at[16] = acc[1], q_at[8] = acc[2], q_at[24] = acc[3];
         }
-        team_sync(my_team, threads);
-        c = in_team;
-        tile += stride;
+        acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+        team_sync(my_team, W.team * 32);
+        head_store<1>(A, red + my_team * W.team * 128, W.in_team * 32 + lane, W.team * 32, n0, cols, tile);
+        team_sync(my_team, W.team * 32);
+        s = W.in_team;
+        tile += W.stride;
       }
     }
   }
