@@ -52,48 +52,65 @@ static unsigned ctas_for(long long rows, int lanes) {
   return (unsigned)(n < cap ? n : cap);
 }
 
-static cudaError_t launch_head(void (*kernel)(HeadArgs), int parts, int nt, HeadArgs& A, cudaStream_t st) {
-  const int steps = (A.chunks + 1) / 2;
-  const size_t smem = (size_t)parts * steps * 512 * A.cols + 16 * 128 * 4 * nt + 16;
-  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (err != cudaSuccess) return err;
-  A.team = steps >= 16 ? 8 : steps >= 8 ? 4 : steps >= 4 ? 2 : 1;
-  const long long teams = kHeadThreads / 32 / A.team, want = (A.tiles + teams - 1) / teams, most = sm_count();
-  dim3 grid((unsigned)(want < most ? want : most), (unsigned)((A.N + A.cols - 1) / A.cols));
-  kernel<<<grid, kHeadThreads, smem, st>>>(A);
-  return cudaGetLastError();
-}
-
-template <int GPC, int PARTS, int NT>
-static cudaError_t launch_head_scales(HeadArgs& A, cudaStream_t st) {
-  const Int4Table& T = A.T;
-  const int ss = T.scale_bf16 ? 2 : 4, per = 2 * GPC, align = per * ss < 16 ? per * ss : 16;
-  const bool vec = T.G % per == 0 && (uintptr_t)T.scales % align == 0 && (T.V == 1 || T.scale_stride * ss % align == 0) &&
-                   (!T.zeros || ((uintptr_t)T.zeros % per == 0 && (T.V == 1 || T.zero_stride % per == 0)));
-  return launch_head(!vec           ? head_kernel<GPC, PARTS, NT, kScalesAny>
-                     : T.scale_bf16 ? head_kernel<GPC, PARTS, NT, kScalesBF16>
-                                    : head_kernel<GPC, PARTS, NT, kScalesF32>,
-                     PARTS, NT, A, st);
-}
-
-template <int PARTS, int NT>
-static cudaError_t launch_head_groups(HeadArgs& A, cudaStream_t st) {
-  switch (A.T.log_group) {
-    case 5: return launch_head_scales<4, PARTS, NT>(A, st);
-    case 6: return launch_head_scales<2, PARTS, NT>(A, st);
-    default: return launch_head_scales<1, PARTS, NT>(A, st);
+// The codes as bytes [V][ceil(D / 32) * 16], copied in boxes of 16 rows by 64.
+static bool codes_map(const Int4Table& T, CUtensorMap* map) {
+  typedef decltype(&cuTensorMapEncodeTiled) Encode;
+  static std::atomic<Encode> found{nullptr};
+  Encode encode = found.load(std::memory_order_relaxed);
+  if (!encode) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess || !p) {
+      (void)cudaGetLastError();
+      return false;
+    }
+    encode = (Encode)p;
+    found.store(encode, std::memory_order_relaxed);
   }
+  const cuuint64_t row = (cuuint64_t)((T.D + 31) / 32 * 16), dims[2] = {row, (cuuint64_t)T.V};
+  const cuuint64_t stride[1] = {T.V > 1 ? (cuuint64_t)T.code_stride : row};
+  const cuuint32_t box[2] = {64, 16}, step[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, T.codes, dims, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr int kHeadUnit = 2;  // chunks of 128 columns per unit
+
+template <int GPC, int PARTS>
+static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
+  const long long per_col = (long long)PARTS * ((A.chunks + kHeadUnit - 1) / kHeadUnit) * kHeadUnit * 256, most = 227 * 1024;
+  int warps = kHeadWarps;
+  long long cols;
+  while ((cols = (most - HeadLayout::fixed(GPC, kHeadUnit, warps)) / per_col) < 1) warps /= 2;  // D <= 32768: two have room
+  if (cols > 8) cols = 8;
+  if (cols > A.N) cols = A.N;
+  A.cols = (int)cols;
+  const Int4Table& T = A.T;
+  // a lane's scales are half a unit's
+  const int ss = T.scale_bf16 ? 2 : 4, per = GPC * kHeadUnit / 2, align = per * ss < 16 ? per * ss : 16;
+  A.vec = (uintptr_t)T.scales % align == 0 && (T.V == 1 || T.scale_stride * ss % align == 0) &&
+          (!T.zeros || ((uintptr_t)T.zeros % per == 0 && (T.V == 1 || T.zero_stride % per == 0)));
+  void (*const kernel)(HeadArgs, CUtensorMap) = cols == 1   ? head_kernel<GPC, PARTS, 1, kHeadUnit>
+                                   : cols == 2 ? head_kernel<GPC, PARTS, 2, kHeadUnit>
+                                               : head_kernel<GPC, PARTS, 0, kHeadUnit>;
+  const int smem = (int)(HeadLayout::fixed(GPC, kHeadUnit, warps) + per_col * cols);
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err != cudaSuccess) return err;
+  dim3 grid((unsigned)(A.tiles < sm_count() ? A.tiles : sm_count()), (unsigned)((A.N + cols - 1) / cols));
+  kernel<<<grid, 32 * warps, smem, st>>>(A, codes);
+  return cudaGetLastError();
 }
 
 template <int PARTS>
 static cudaError_t launch_head_for(HeadArgs& A, cudaStream_t st) {
-  const long long fit = 204 * 1024 / ((long long)PARTS * ((A.chunks + 1) / 2) * 512);  // hidden states that shared memory holds
-  const long long most = PARTS == 1 ? 16 : 8, cols = fit < most ? fit : most;
-  A.cols = (int)(cols < A.N ? cols : A.N);
-  if (A.cols <= 2) return launch_head(A.T.scale_bf16 ? head_few_kernel<PARTS, kScalesBF16> : head_few_kernel<PARTS, kScalesF32>, PARTS, 1, A, st);
-  if constexpr (PARTS == 1)
-    if (A.cols > 8) return launch_head_groups<1, 2>(A, st);
-  return launch_head_groups<PARTS, 1>(A, st);
+  CUtensorMap codes;
+  if (!codes_map(A.T, &codes)) return cudaErrorInvalidValue;
+  switch (A.T.log_group) {
+    case 5: return launch_head<4, PARTS>(A, codes, st);
+    case 6: return launch_head<2, PARTS>(A, codes, st);
+    default: return launch_head<1, PARTS>(A, codes, st);
+  }
 }
 
 }  // namespace gls

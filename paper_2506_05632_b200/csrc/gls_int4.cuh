@@ -3,6 +3,8 @@
 // made from weights, read back by token, and multiplied with hidden states (the logits of a 4-bit head).
 // Two codes a byte, the even column in the low half; a row's codes start on a 16-byte boundary.
 #pragma once
+#include <cuda.h>
+
 #include "gls_kernels.cuh"
 
 namespace gls {
@@ -207,17 +209,24 @@ __global__ void __launch_bounds__(kInt4Threads) embed_int4_kernel(const EmbedInt
 // Logits of hidden states: out[n,v] = sum_d x[n,d] * element(v, d).
 //
 // The product is mma.sync m16n8k16 with 16 table rows as the one operand and up to 8 hidden states as the other: for so
-// few columns the codes' way into the registers, not the tensor pipe, is what costs, and there A comes straight from the
-// lanes that loaded and converted it.  A code becomes bf16 without a conversion: 0x4300 | code is 128 + code, and
+// few columns the codes' way into the registers, not the tensor pipe, is what costs, and there the operand comes straight
+// from the lanes that converted it.  A code becomes bf16 without a conversion: 0x4300 | code is 128 + code, and
 // (128 + code) - (128 + zero) is exact.  Which column of a sum goes to which k of an instruction is free as long as both
-// operands agree, so a lane's 16 loaded bytes (32 columns) feed the instructions in the order in which masks and
-// shifts give them, and the hidden states lie in shared memory in that order.  With groups of 128
-// a chunk of 128 columns has one step per row; with smaller groups the lanes of a quad exchange their words, so that an
-// instruction's columns are of one group.  A group's sum is multiplied by its step in fp32.
-// fp32 hidden states are split into three bf16 parts (8 bits each, exactly), each with its own product.
+// operands agree, so a lane's 16 bytes (32 columns) feed the instructions in the order in which masks and
+// shifts give them, and the hidden states lie in shared memory in that order.  A group's sum is multiplied by its
+// scale in fp32.  fp32 hidden states are split into three bf16 parts (8 bits each, exactly), each with its own product.
 //
-// A team of warps takes 16 rows, a warp every team-th chunk of 128 columns (1 KB of codes, the next three already
-// requested); the team's sums meet in shared memory.
+// One or two hidden states (FEW): the instruction's eight columns are two hidden states times the four lanes of a
+// quad: column 2 t + n holds hidden state n where the k belong to lane t and zeros elsewhere, so that the sums of
+// lanes t come apart.  Each is of 32 neighbouring columns, hence of one group, whatever the groups' size, and lane t holds it.
+// More: with groups of 128 a chunk of 128 columns has one scale per row; with smaller ones the lanes of
+// a quad exchange their words first, so that an instruction's columns are of one group.
+//
+// A CTA has a range of tiles of 16 rows, cut into units of UC chunks of 128 columns; each warp takes a run of
+// units of equal length, whatever the tiles, and streams them through a ring of its own: a tensor copy of 64 bytes of 16
+// rows per chunk, which leaves what a warp reads at once side by side.  (Bulk copies row by row take one lane after
+// the other: 262 instead of 130 instructions per chunk.)  The scales and zeros of a unit are requested when its codes are and stored
+// beside them as pairs (fp32 scale, bf16 zero twice).  A tile that two or more warps share is added up at the end.
 // ------------------------------------------------------------------------------------------
 struct HeadArgs {
   Int4Table T;
@@ -228,22 +237,38 @@ struct HeadArgs {
   long long out_stride;
   int out_bf16;
   int cols;            // hidden states per CTA row of the grid
-  int team;            // warps per 16 rows: 1, 2, 4, 8, 16
   int chunks;          // of 128 columns
+  int vec;             // a lane's scales and zeros of a unit are aligned vectors
   long long tiles;     // of 16 rows
 };
 
-constexpr int kHeadThreads = 512;
+constexpr int kHeadWarps = 16;  // at most: fewer where the hidden states leave no room for their rings
+constexpr int kHeadStages = 2;
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t sub_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
+}
+// Eight codes as bf16 differences to their zero, columns k and k + 4 as pairs.  Mask and magic in one instruction (written
+// as & and | they are two: 22 instead of 14 integer instructions per two words).
+__device__ __forceinline__ void int4_pairs(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, 0x000f000f, 0x43004300, 0xea;" : "=r"(d) : "r"(w >> (4 * i)));
+    p[i] = sub_bf16x2(d, z);
+  }
 }
 // words of a quad's lanes exchanged: afterwards w[j] of lane t is what w[t] of lane j was
 __device__ __forceinline__ void quad_transpose(uint32_t (&w)[4]) {
@@ -272,14 +297,41 @@ __device__ __forceinline__ uint32_t take_bf16(float& x) {
   x = __fsub_rn(x, __uint_as_float(b & 0xffff0000u));
   return b >> 16;
 }
-
-__device__ __forceinline__ void team_sync(int team, int threads) {  // barrier 0 is the whole CTA's
-  if (threads == 32) __syncwarp();
-  else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(threads) : "memory");
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+  uint4 b;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(at));
+  return b;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+  uint2 b;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(b.x), "=r"(b.y) : "r"(at));
+  return b;
 }
 
-// How the scales come: as one aligned vector per row and step of that type, or one by one.
-enum : int { kScalesF32 = 0, kScalesBF16 = 1, kScalesAny = 2 };
+__device__ __forceinline__ void barrier_init(uint32_t at, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(at), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t at, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(at), "r"(bytes) : "memory");
+}
+// false if the phase did not end within a limit that no copy reaches
+__device__ __forceinline__ bool barrier_wait(uint32_t at, uint32_t parity) {
+  for (int i = 0; i < (1 << 22); ++i) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done)
+                 : "r"(at), "r"(parity)
+                 : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+// 64 bytes of 16 rows, from byte x of row y on; what lies outside the table comes as zeros
+__device__ __forceinline__ void copy_codes(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t barrier) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to),
+               "l"(map), "r"(x), "r"(y), "r"(barrier)
+               : "memory");
+}
 
 template <int BYTES>
 __device__ __forceinline__ void load_words(uint32_t* w, const char* p) {
@@ -301,65 +353,132 @@ __device__ __forceinline__ void load_words(uint32_t* w, const char* p) {
   }
 }
 
-// A step: 256 columns of 16 rows.  Lane (gid, tig) has columns 32 tig .. 32 tig + 31 of each half for rows gid, gid + 8.
-template <int GPC, int ST>  // groups per 128 columns
-struct HeadStep {
-  static constexpr int kGroups = 2 * GPC;
-  static constexpr int kWords = ST == kScalesBF16 ? GPC : kGroups;  // raw scales per row
-  uint4 code[2][2];  // [row][half]
-  uint32_t scale[2][kWords];
-  uint32_t zero[2][(kGroups + 3) / 4];  // a byte per group
-  __device__ __forceinline__ float step(int r, int g) const {
-    if constexpr (ST == kScalesBF16) return __uint_as_float(g & 1 ? scale[r][g >> 1] & 0xffff0000u : scale[r][g >> 1] << 16);
-    else return __uint_as_float(scale[r][g]);
-  }
-  // 128 + zero twice, in bf16; the low four bits of a zero count
-  __device__ __forceinline__ uint32_t zero_pair(int r, int g) const {
-    return __byte_perm(zero[r][g >> 2] & 0x0f0f0f0fu, 0x43u, 0x4040u | (uint32_t)(g & 3) * 0x0101u);
+// Shared memory of a head kernel: partial sums, per warp the ring and its barriers, zeros as far as a chunk of hidden
+// states reaches, the hidden states.
+struct HeadLayout {
+  static constexpr int kRed = 2 * 128 * 4;  // per warp: two tiles of 8 columns
+  static constexpr int kZeros = 2048;
+  static __host__ __device__ constexpr int stage(int gpc, int uc) { return 1024 * uc + 16 * gpc * uc * 8; }
+  static __host__ __device__ constexpr int fixed(int gpc, int uc, int warps) {
+    return warps * (kRed + kHeadStages * (stage(gpc, uc) + 8)) + kZeros;
   }
 };
 
-// Position of a warp in its CTA's share of the table: teams of warps take tiles of 16 rows, a warp every team-th step of
-// them, and its requests run some steps ahead of its products, across tiles.
-struct HeadWalk {
-  int in_team, team, rounds, steps_per_row;
-  long long first, stride;
-  int steps;
-  __device__ __forceinline__ HeadWalk(const HeadArgs& A, int teams, int my_team, int warp_in_team) {
-    in_team = warp_in_team;
-    team = A.team;
-    steps_per_row = (A.chunks + 1) >> 1;
-    rounds = (steps_per_row + team - 1) / team;
-    first = (long long)blockIdx.x * teams + my_team;
-    stride = (long long)gridDim.x * teams;
-    steps = (int)(first < A.tiles ? (A.tiles - first + stride - 1) / stride : 0) * rounds;
-  }
-};
+// Groups' scales and zeros of a unit on their way: lane (row = lane / 2, half = lane % 2) has those of half a unit.
+template <int GPC, int UC>
+struct HeadScales {
+  static constexpr int kMine = GPC * UC / 2;
+  uint32_t scale[kMine], zero[(kMine + 3) / 4];
 
-// A 4-column pair of codes as bf16 differences to their zero
-__device__ __forceinline__ void int4_pairs(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
+  __device__ __forceinline__ void load(const HeadArgs& A, long long v, int unit) {
+    const Int4Table& T = A.T;
+    const int g0 = unit * GPC * UC + (threadIdx.x & 1) * kMine;
+    if (v >= T.V) v = T.V - 1;
+    const char* s = (const char*)T.scales + (v * T.scale_stride + g0) * (T.scale_bf16 ? 2 : 4);
+    if (A.vec && g0 + kMine <= T.G) {
+      if (T.scale_bf16) load_words<kMine * 2>(scale, s);
+      else load_words<kMine * 4>(scale, s);
+      if (T.zeros) load_words<kMine>(zero, (const char*)T.zeros + v * T.zero_stride + g0);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) p[i] = sub_bf16x2(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u, z);
-}
+      for (int i = 0; i < (kMine + 3) / 4; ++i) zero[i] = 0u;
+      if (T.scale_bf16) {
+#pragma unroll
+        for (int i = 0; i < (kMine + 1) / 2; ++i) scale[i] = 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const bool in = g0 + i < T.G;
+        if (T.scale_bf16) {
+          if (in) scale[i >> 1] |= (uint32_t)__ldg((const unsigned short*)s + i) << (16 * (i & 1));
+        } else {
+          scale[i] = in ? __ldg((const uint32_t*)s + i) : 0u;
+        }
+        if (in && T.zeros) zero[i >> 2] |= (uint32_t)__ldg(T.zeros + v * T.zero_stride + g0 + i) << (8 * (i & 3));
+      }
+    }
+  }
+  // -> shared memory: [row][group of the unit] {fp32 scale, bf16 128 + zero twice}; the low four bits of a zero count
+  __device__ __forceinline__ void store(const HeadArgs& A, uint32_t at) const {
+    uint32_t out[2 * kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      out[2 * i] = !A.T.scale_bf16 ? scale[i] : i & 1 ? scale[i >> 1] & 0xffff0000u : scale[i >> 1] << 16;
+      const uint32_t z = A.T.zeros ? zero[i >> 2] & 0x0f0f0f0fu : 0x08080808u;
+      out[2 * i + 1] = __byte_perm(z, 0x43u, 0x4040u | (uint32_t)(i & 3) * 0x0101u);
+    }
+    at += threadIdx.x % 32 * (kMine * 8);
+    if constexpr (kMine == 1) {
+      asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(out[0]), "r"(out[1]) : "memory");
+    } else {
+#pragma unroll
+      for (int i = 0; i < kMine / 2; ++i)
+        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at + 16 * i), "r"(out[4 * i]), "r"(out[4 * i + 1]),
+                     "r"(out[4 * i + 2]), "r"(out[4 * i + 3])
+                     : "memory");
+    }
+  }
+};
 
-__device__ __forceinline__ uint4 lds16(uint32_t at) {
-  uint4 b;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(at));
-  return b;
-}
+// FEW: 1 or 2, the hidden states at most; 0: up to 8
+template <int GPC, int PARTS, int FEW, int UC>
+__global__ void __launch_bounds__(32 * kHeadWarps, 1) head_kernel(const HeadArgs A, const __grid_constant__ CUtensorMap codes) {
+  extern __shared__ __align__(1024) char head_shared[];
+  constexpr bool kQuad = FEW || GPC == 1;  // a lane's words stay its own
+  constexpr int kStage = HeadLayout::stage(GPC, UC);
+  const Int4Table& T = A.T;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
+  const int n0 = blockIdx.y * A.cols, cols = min(A.cols, A.N - n0);
+  const int width = FEW ? FEW : cols;  // columns that the hidden states' layout has
+  const uint32_t base = (uint32_t)__cvta_generic_to_shared(head_shared);
+  const int warps = blockDim.x >> 5;
+  float* const red = (float*)head_shared;  // [warp][2][8][16]
+  const uint32_t ring = base + warps * HeadLayout::kRed + warp * (kHeadStages * kStage);
+  const int bars_at = warps * (HeadLayout::kRed + kHeadStages * kStage), zeros_at = bars_at + warps * kHeadStages * 8;
+  const uint32_t bars = base + bars_at + warp * (kHeadStages * 8);
+  const int chunks_up = (A.chunks + UC - 1) / UC * UC;
+  const int plane = chunks_up * 16 * width;  // 16-byte units per part
 
-// Hidden states -> shared memory in parts of bf16: unit (chunk, j, n, t) holds 8 columns as pairs (k, k + 4); QUAD: those
-// of a lane's own 32 columns, otherwise those that the exchanged words of a quad are of.
-template <int PARTS, bool QUAD>
-__device__ __forceinline__ void stage_hidden(const HeadArgs& A, uint4* xs, int n0, int cols, int units, int plane) {
-  for (int i = threadIdx.x; i < units; i += kHeadThreads) {
-    const int t = i & 3, n = (i >> 2) % cols, cj = (i >> 2) / cols, j = cj & 3, c = cj >> 2;
-    const long long d = (long long)c * 128 + (QUAD ? t * 32 + j * 8 : j * 32 + t * 8);
+  const long long units_per_row = (A.chunks + UC - 1) / UC;
+  const long long t0 = A.tiles * blockIdx.x / gridDim.x, t1 = A.tiles * (blockIdx.x + 1) / gridDim.x;
+  const long long all = (t1 - t0) * units_per_row;
+  const int first = (int)(all * warp / warps), last = (int)(all * (warp + 1) / warps);
+  const int upr = (int)units_per_row;
+
+  // requests run kHeadStages units ahead of the products
+  long long l_tile = t0 + first / upr;
+  int l_unit = first % upr;
+  HeadScales<GPC, UC> scales[kHeadStages];
+  auto request = [&](int stage) {
+    const uint32_t bar = bars + stage * 8;
+    if (lane == 0) {
+      barrier_expect(bar, UC * 1024);
+#pragma unroll
+      for (int c = 0; c < UC; ++c)
+        copy_codes(ring + stage * kStage + c * 1024, &codes, (l_unit * UC + c) * 64, (int)(l_tile * 16), bar);
+    }
+    scales[stage].load(A, l_tile * 16 + (lane >> 1), l_unit);
+    if (++l_unit == upr) l_unit = 0, ++l_tile;
+  };
+  if (lane < kHeadStages) barrier_init(bars + lane * 8, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncwarp();
+#pragma unroll
+  for (int q = 0; q < kHeadStages; ++q)
+    if (first + q < last) request(q);
+
+  // hidden states -> shared memory in parts of bf16: unit (chunk, j, n, t) holds 8 columns as pairs (k, k + 4), of a lane's
+  // own 32 columns, or of those that a quad's lanes have after exchanging their words
+  uint4* const xs = (uint4*)(head_shared + zeros_at);
+  for (int i = threadIdx.x; i < HeadLayout::kZeros / 16; i += blockDim.x) xs[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = threadIdx.x; i < plane; i += blockDim.x) {
+    const int t = i & 3, n = (i >> 2) % width, cj = (i >> 2) / width, j = cj & 3, c = cj >> 2;
+    const long long d = (long long)c * 128 + (kQuad ? t * 32 + j * 8 : j * 32 + t * 8);
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       v[e] = 0.f;
-      if (d + e < A.T.D) {
+      if (d + e < T.D && n < cols) {
         const long long at = (long long)(n0 + n) * A.x_stride + d + e;
         v[e] = PARTS == 1 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)A.x + at) << 16) : __ldg((const float*)A.x + at);
       }
@@ -369,320 +488,117 @@ __device__ __forceinline__ void stage_hidden(const HeadArgs& A, uint4* xs, int n
       uint32_t h[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) h[e] = PARTS == 1 ? __float_as_uint(v[e]) >> 16 : take_bf16(v[e]);
-      xs[(size_t)part * plane + i] = make_uint4(h[0] | h[4] << 16, h[1] | h[5] << 16, h[2] | h[6] << 16, h[3] | h[7] << 16);
+      xs[HeadLayout::kZeros / 16 + (size_t)part * plane + i] = make_uint4(h[0] | h[4] << 16, h[1] | h[5] << 16, h[2] | h[6] << 16, h[3] | h[7] << 16);
     }
   }
-}
-
-// The sums that a team's warps left in `red` [warp][column][row], added up and stored.
-template <int NT>
-__device__ __forceinline__ void head_store(const HeadArgs& A, const float* team_at, int thread, int threads, int n0, int cols, long long tile) {
-  for (int i = thread; i < 16 * cols; i += threads) {
-    float y = 0.f;
-    for (int k = 0; k < A.team; ++k) y += team_at[k * 128 * NT + i];
-    const long long v = tile * 16 + (i & 15);
-    if (v < A.T.V) {
-      const long long at = (long long)(n0 + (i >> 4)) * A.out_stride + v;
-      if (A.out_bf16) ((unsigned short*)A.out)[at] = (unsigned short)bf16_bits(y);
-      else ((float*)A.out)[at] = y;
-    }
-  }
-}
-
-template <int GPC, int PARTS, int NT, int ST>
-__global__ void __launch_bounds__(kHeadThreads, 1) head_kernel(const HeadArgs A) {
-  extern __shared__ __align__(16) uint4 head_shared[];
-  typedef HeadStep<GPC, ST> Step;
-  constexpr int kAhead = GPC == 4 || (GPC == 2 && ST != kScalesBF16) ? 1 : 2;  // what registers hold
-  const Int4Table& T = A.T;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
-  const int n0 = blockIdx.y * A.cols, cols = min(A.cols, A.N - n0);
-  const int chunks2 = (A.chunks + 1) & ~1;
-  const int plane = chunks2 * 16 * cols;      // 16-byte units per part
-  float* const red = (float*)head_shared;     // [16 warps][8 NT][16]
-  uint4* const xs = head_shared + 16 * 32 * NT;  // a unit of zeros, then the hidden states
-  if (threadIdx.x == 0) xs[0] = make_uint4(0u, 0u, 0u, 0u);
-  stage_hidden<PARTS, GPC == 1>(A, xs + 1, n0, cols, plane, plane);
   __syncthreads();
 
-  const int teams = kHeadThreads / 32 / A.team, my_team = warp / A.team;
-  const HeadWalk W(A, teams, my_team, warp % A.team);
-  const int row_last = (int)((T.D + 31) / 32 * 16) - 16;
+  // where the hidden states of the lane's columns lie, bytes from one chunk to the next and from one part to the next;
+  // lanes without one read zeros
+  const uint32_t x_j = (uint32_t)width * 64u;
+  const bool there = FEW ? tig == gid >> 1 && (gid & 1) < FEW : gid < cols;
+  const uint32_t x_at = base + zeros_at + (there ? HeadLayout::kZeros + ((FEW ? gid & 1 : gid) * 4 + tig) * 16 : 0);
+  const uint32_t x_chunk = there ? 4u * x_j : 0u, x_part = there ? (uint32_t)plane * 16u : 0u;
 
-  // What the next request reads: step l_step of the rows at l_code.  Codes and scales behind a row's end
-  // are replaced by its last ones: the hidden states there are zeros.
-  long long l_tile = W.first;
-  int l_step = W.in_team;
-  const uint8_t* l_code[2];
-  const char* l_scale[2];
-  const uint8_t* l_zero[2];
-  constexpr int ss = ST == kScalesBF16 ? 2 : 4;
-  const int ss_any = T.scale_bf16 ? 2 : 4;
-  auto aim = [&]() {
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      long long v = l_tile * 16 + gid + 8 * r;
-      if (v >= T.V) v = T.V - 1;  // read again, not stored
-      l_code[r] = T.codes + v * T.code_stride;
-      l_scale[r] = (const char*)T.scales + v * T.scale_stride * (ST == kScalesAny ? ss_any : ss);
-      l_zero[r] = T.zeros + v * T.zero_stride;
-    }
-  };
-  aim();
-  auto request = [&](Step& h) {
-    const int at0 = min(l_step * 128 + tig * 16, row_last), at1 = min(l_step * 128 + tig * 16 + 64, row_last);
-    const int s = min(l_step, W.steps_per_row - 1);
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      h.code[r][0] = ld_stream16(l_code[r] + at0);
-      h.code[r][1] = ld_stream16(l_code[r] + at1);
-      if constexpr (ST == kScalesAny) {
-#pragma unroll
-        for (int g = 0; g < Step::kGroups; ++g) {
-          const int gg = min(s * Step::kGroups + g, T.G - 1);
-          h.scale[r][g] = T.scale_bf16 ? (uint32_t)__ldg((const unsigned short*)l_scale[r] + gg) << 16 : __ldg((const uint32_t*)l_scale[r] + gg);
-        }
-      } else {
-        load_words<Step::kGroups * ss>(h.scale[r], l_scale[r] + s * (Step::kGroups * ss));
-      }
-      if (T.zeros) {
-        if constexpr (ST == kScalesAny) {
-#pragma unroll
-          for (int i = 0; i < (Step::kGroups + 3) / 4; ++i) h.zero[r][i] = 0u;
-#pragma unroll
-          for (int g = 0; g < Step::kGroups; ++g)
-            h.zero[r][g >> 2] |= (uint32_t)__ldg(l_zero[r] + min(s * Step::kGroups + g, T.G - 1)) << (8 * (g & 3));
-        } else {
-          load_words<Step::kGroups>(h.zero[r], (const char*)l_zero[r] + s * Step::kGroups);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < (Step::kGroups + 3) / 4; ++i) h.zero[r][i] = 0x08080808u;
-      }
-    }
-    l_step += W.team;
-    if (l_step >= W.rounds * W.team) {
-      l_step = W.in_team;
-      l_tile += W.stride;
-      aim();
-    }
-  };
-
-  // where the hidden states of the lane's columns lie: bytes, and from one j to the next
-  uint32_t x_at[NT], x_step[NT], x_part[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const bool there = gid + 8 * nt < cols;
-    x_at[nt] = (uint32_t)__cvta_generic_to_shared(xs) + (there ? 16u + ((gid + 8 * nt) * 4 + tig) * 16u : 0u);
-    x_step[nt] = there ? (uint32_t)cols * 64u : 0u;
-    x_part[nt] = there ? (uint32_t)plane * 16u : 0u;
-  }
-
-  Step ring[kAhead];
-#pragma unroll
-  for (int q = 0; q < kAhead; ++q)
-    if (q < W.steps) request(ring[q]);
-  float acc[NT][4];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
-  long long tile = W.first;
-  int s = W.in_team;
-  for (int s0 = 0; s0 < W.steps; s0 += kAhead) {
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      if (s0 + q >= W.steps) break;
-      Step& h = ring[q];
-      if (s < W.steps_per_row) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t w[2][4];
-#pragma unroll
-          for (int r = 0; r < 2; ++r) w[r][0] = h.code[r][half].x, w[r][1] = h.code[r][half].y, w[r][2] = h.code[r][half].z, w[r][3] = h.code[r][half].w;
-          if (GPC > 1) quad_transpose(w[0]), quad_transpose(w[1]);
-          uint32_t xa[NT];
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) xa[nt] = x_at[nt] + (uint32_t)(2 * s + half) * 4u * x_step[nt];
-#pragma unroll
-          for (int gl = 0; gl < GPC; ++gl) {
-            const int g = half * GPC + gl;
-            float sum[NT][4];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) sum[nt][0] = sum[nt][1] = sum[nt][2] = sum[nt][3] = 0.f;
-            const uint32_t z0 = h.zero_pair(0, g), z1 = h.zero_pair(1, g);
-#pragma unroll
-            for (int jj = 0; jj < 4 / GPC; ++jj) {
-              const int j = gl * (4 / GPC) + jj;
-              uint32_t p0[4], p1[4];
-              int4_pairs(w[0][j], z0, p0);
-              int4_pairs(w[1][j], z1, p1);
-              const uint32_t a0[4] = {p0[0], p1[0], p0[1], p1[1]}, a1[4] = {p0[2], p1[2], p0[3], p1[3]};
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-                for (int part = 0; part < PARTS; ++part) {
-                  const uint4 b = lds16(xa[nt] + (uint32_t)part * x_part[nt]);
-                  mma_bf16(sum[nt], a0, b.x, b.y);
-                  mma_bf16(sum[nt], a1, b.z, b.w);
-                }
-                xa[nt] += x_step[nt];
-              }
-            }
-            const float s0v = h.step(0, g), s1v = h.step(1, g);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              acc[nt][0] += s0v * sum[nt][0];
-              acc[nt][1] += s0v * sum[nt][1];
-              acc[nt][2] += s1v * sum[nt][2];
-              acc[nt][3] += s1v * sum[nt][3];
-            }
-          }
-        }
-      }
-      if (s0 + q + kAhead < W.steps) request(h);
-      s += W.team;
-      if (s >= W.rounds * W.team) {
-        float* q_at = red + warp * 128 * NT + 2 * tig * 16 + gid;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          q_at[128 * nt] = acc[nt][0], q_at[128 * nt + 16] = acc[nt][1];
-          q_at[128 * nt + 8] = acc[nt][2], q_at[128 * nt + 24] = acc[nt][3];
-          acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
-        }
-        team_sync(my_team, W.team * 32);
-        head_store<NT>(A, red + my_team * W.team * 128 * NT, W.in_team * 32 + lane, W.team * 32, n0, cols, tile);
-        team_sync(my_team, W.team * 32);
-        s = W.in_team;
-        tile += W.stride;
-      }
-    }
-  }
-}
-
-// The same for one or two hidden states.  The instruction's eight columns then are two hidden states times the four
-// lanes of a quad: column 2 t + n holds hidden state n where the k belong to lane t and zeros elsewhere, so that the sums of
-// lanes t come apart.  Each is of 32 neighbouring columns, hence of one group, whatever the groups' size, and lane t
-// holds it: it multiplies it by its own scale, no words are exchanged, and scales need no alignment.
-template <int PARTS, int ST>
-__global__ void __launch_bounds__(kHeadThreads, 1) head_few_kernel(const HeadArgs A) {
-  extern __shared__ __align__(16) uint4 head_shared[];
-  constexpr int kAhead = 2;
-  const Int4Table& T = A.T;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
-  const int n0 = blockIdx.y * A.cols, cols = min(A.cols, A.N - n0);
-  const int chunks2 = (A.chunks + 1) & ~1;
-  const int plane = chunks2 * 16 * cols;
-  float* const red = (float*)head_shared;
-  uint4* const xs = head_shared + 16 * 32;
-  if (threadIdx.x == 0) xs[0] = make_uint4(0u, 0u, 0u, 0u);
-  stage_hidden<PARTS, true>(A, xs + 1, n0, cols, plane, plane);
-  __syncthreads();
-
-  const int teams = kHeadThreads / 32 / A.team, my_team = warp / A.team;
-  const HeadWalk W(A, teams, my_team, warp % A.team);
-  const int row_last = (int)((T.D + 31) / 32 * 16) - 16;
-  struct Step {
-    uint4 code[2][2];
-    uint32_t scale[2][2], zero[2][2];
-  };
-  long long l_tile = W.first;
-  int l_step = W.in_team;
-  const uint8_t* l_code[2];
-  const char* l_scale[2];
-  const uint8_t* l_zero[2];
-  constexpr int ss = ST == kScalesBF16 ? 2 : 4;
-  auto aim = [&]() {
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      long long v = l_tile * 16 + gid + 8 * r;
-      if (v >= T.V) v = T.V - 1;
-      l_code[r] = T.codes + v * T.code_stride;
-      l_scale[r] = (const char*)T.scales + v * T.scale_stride * ss;
-      l_zero[r] = T.zeros + v * T.zero_stride;
-    }
-  };
-  aim();
-  auto request = [&](Step& h) {
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int at = min(l_step * 128 + half * 64 + tig * 16, row_last), g = at >> (T.log_group - 1);
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        h.code[r][half] = ld_stream16(l_code[r] + at);
-        load_words<ss>(&h.scale[r][half], l_scale[r] + g * ss);
-        h.zero[r][half] = 8u;
-        if (T.zeros) h.zero[r][half] = __ldg(l_zero[r] + g);
-      }
-    }
-    l_step += W.team;
-    if (l_step >= W.rounds * W.team) {
-      l_step = W.in_team;
-      l_tile += W.stride;
-      aim();
-    }
-  };
-  const bool there = tig == gid >> 1 && (gid & 1) < cols;
-  const uint32_t x_at = (uint32_t)__cvta_generic_to_shared(xs) + (there ? 16u + ((gid & 1) * 4 + tig) * 16u : 0u);
-  const uint32_t x_step = there ? (uint32_t)cols * 64u : 0u, x_part = there ? (uint32_t)plane * 16u : 0u;
-
-  Step ring[kAhead];
-#pragma unroll
-  for (int q = 0; q < kAhead; ++q)
-    if (q < W.steps) request(ring[q]);
   float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  long long tile = W.first;
-  int s = W.in_team;
-  for (int s0 = 0; s0 < W.steps; s0 += kAhead) {
+  auto put = [&](int i, long long tile, float y) {
+    const long long v = tile * 16 + (i & 15);
+    if (v >= T.V) return;
+    const long long at = (long long)(n0 + (i >> 4)) * A.out_stride + v;
+    if (A.out_bf16) ((unsigned short*)A.out)[at] = (unsigned short)bf16_bits(y);
+    else ((float*)A.out)[at] = y;
+  };
+  long long tile = t0 + first / upr;
+  int unit = first % upr, phase = 0;
+  bool whole = unit == 0, lost = false;  // whole: all of the tile so far is this warp's
+  for (int u0 = first; u0 < last; u0 += kHeadStages, phase ^= 1) {
 #pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      if (s0 + q >= W.steps) break;
-      Step& h = ring[q];
-      if (s < W.steps_per_row) {
-        uint32_t xa = x_at + (uint32_t)s * 8u * x_step;
+    for (int q = 0; q < kHeadStages; ++q) {
+      if (u0 + q >= last) break;
+      const uint32_t stage_at = ring + q * kStage, scale_at = stage_at + UC * 1024;
+      scales[q].store(A, scale_at);
+      lost |= !barrier_wait(bars + q * 8, phase);
+      __syncwarp();
+      const uint32_t code_at = stage_at + lane * 16;
+      const uint32_t sc_at = scale_at + (gid * GPC * UC + (FEW ? tig * GPC >> 2 : 0)) * 8;
+      uint32_t xa = x_at + (uint32_t)(unit * UC) * x_chunk;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t w[2][4] = {{h.code[0][half].x, h.code[0][half].y, h.code[0][half].z, h.code[0][half].w},
-                                    {h.code[1][half].x, h.code[1][half].y, h.code[1][half].z, h.code[1][half].w}};
-          const uint32_t z0 = ((h.zero[0][half] & 15u) | 0x4300u) * 0x10001u, z1 = ((h.zero[1][half] & 15u) | 0x4300u) * 0x10001u;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < UC; ++c) {
+        const uint4 c0 = lds16(code_at + c * 1024), c1 = lds16(code_at + c * 1024 + 512);
+        uint32_t w[2][4] = {{c0.x, c0.y, c0.z, c0.w}, {c1.x, c1.y, c1.z, c1.w}};
+        if (!kQuad) quad_transpose(w[0]), quad_transpose(w[1]);
+        constexpr int kSets = FEW ? 1 : GPC;  // sums of one scale each
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+        for (int g = 0; g < kSets; ++g) {
+          const uint2 s0 = lds8(sc_at + (c * GPC + g) * 8), s1 = lds8(sc_at + (8 * GPC * UC + c * GPC + g) * 8);
+          float sum[2][4];  // two chains of products
+#pragma unroll
+          for (int jj = 0; jj < 4 / kSets; ++jj) {
+            const int j = g * (4 / kSets) + jj;
             uint32_t p0[4], p1[4];
-            int4_pairs(w[0][j], z0, p0);
-            int4_pairs(w[1][j], z1, p1);
+            int4_pairs(w[0][j], s0.y, p0);
+            int4_pairs(w[1][j], s1.y, p1);
             const uint32_t a0[4] = {p0[0], p1[0], p0[1], p1[1]}, a1[4] = {p0[2], p1[2], p0[3], p1[3]};
 #pragma unroll
             for (int part = 0; part < PARTS; ++part) {
-              const uint4 b = lds16(xa + (uint32_t)part * x_part);
-              mma_bf16(sum, a0, b.x, b.y);
-              mma_bf16(sum, a1, b.z, b.w);
+              const uint4 b = lds16(xa + (uint32_t)j * x_j + (uint32_t)part * x_part);
+              if (jj == 0 && part == 0) {
+                mma_bf16_first(sum[0], a0, b.x, b.y);
+                mma_bf16_first(sum[1], a1, b.z, b.w);
+              } else {
+                mma_bf16(sum[0], a0, b.x, b.y);
+                mma_bf16(sum[1], a1, b.z, b.w);
+              }
             }
-            xa += x_step;
           }
-          const float s0v = __uint_as_float(ST == kScalesBF16 ? h.scale[0][half] << 16 : h.scale[0][half]);
-          const float s1v = __uint_as_float(ST == kScalesBF16 ? h.scale[1][half] << 16 : h.scale[1][half]);
-          acc[0] += s0v * sum[0], acc[1] += s0v * sum[1];
-          acc[2] += s1v * sum[2], acc[3] += s1v * sum[3];
+          const float f0 = __uint_as_float(s0.x), f1 = __uint_as_float(s1.x);
+          acc[0] += f0 * (sum[0][0] + sum[1][0]);
+          acc[1] += f0 * (sum[0][1] + sum[1][1]);
+          acc[2] += f1 * (sum[0][2] + sum[1][2]);
+          acc[3] += f1 * (sum[0][3] + sum[1][3]);
         }
+        xa += x_chunk;
       }
-      if (s0 + q + kAhead < W.steps) request(h);
-      s += W.team;
-      if (s >= W.rounds * W.team) {
+      __syncwarp();  // the stage has been read
+      if (u0 + q + kHeadStages < last) request(q);
+      const bool row_end = ++unit == upr;
+      if (row_end || u0 + q + 1 == last) {
+        // the sums of the tile, or of the warp's part of it: [column][row].  The first slot keeps the end of a tile that
+        // an earlier warp began, the second one whole tiles on their way and at last a part without the tile's end.
+        float* const slot = red + (warp * 2 + (row_end && !whole ? 0 : 1)) * 128;
+        if (FEW) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 1);
-          acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 2);
+          for (int i = 0; i < 4; ++i) {
+            acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 1);
+            acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 2);
+          }
         }
-        if (tig == 0) {
-          float* q_at = red + warp * 128 + gid;
-          q_at[0] = acc[0], q_at[16] = acc[1], q_at[8] = acc[2], q_at[24] = acc[3];
+        const float bad = lost ? __uint_as_float(0x7fc00000u) : 0.f;
+        if (!FEW || tig == 0) {
+          float* at = slot + (FEW ? 0 : 2 * tig) * 16 + gid;
+          at[0] = acc[0] + bad, at[16] = acc[1] + bad, at[8] = acc[2] + bad, at[24] = acc[3] + bad;
         }
         acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-        team_sync(my_team, W.team * 32);
-        head_store<1>(A, red + my_team * W.team * 128, W.in_team * 32 + lane, W.team * 32, n0, cols, tile);
-        team_sync(my_team, W.team * 32);
-        s = W.in_team;
-        tile += W.stride;
+        if (row_end && whole) {
+          __syncwarp();
+          for (int i = lane; i < 16 * cols; i += 32) put(i, tile, slot[i]);
+          __syncwarp();
+        }
+        if (row_end) unit = 0, whole = true, ++tile;
       }
+    }
+  }
+  __syncthreads();
+  // a tile that this warp began and others went on with: parts in order
+  const int begun = last / upr * upr, end = begun + upr;
+  if (first < last && last % upr != 0 && begun >= first) {
+    int parts = warp + 1;  // warps up to the one that has the tile's end
+    while ((int)(all * (parts + 1) / warps) < end) ++parts;
+    for (int i = lane; i < 16 * cols; i += 32) {
+      float y = red[(warp * 2 + 1) * 128 + i];
+      for (int w = warp + 1; w <= parts; ++w)
+        if (all * w / warps < all * (w + 1) / warps) y += red[(w * 2 + (w < parts ? 1 : 0)) * 128 + i];
+      put(i, t0 + last / upr, y);
     }
   }
 }
