@@ -52,6 +52,9 @@ static unsigned ctas_for(long long rows, int lanes) {
   return (unsigned)(n < cap ? n : cap);
 }
 
+// shared memory per hidden state
+static long long head_column_bytes(int parts, int chunks, int uc) { return (long long)parts * ((chunks + uc - 1) / uc) * uc * 256; }
+
 // The codes as bytes [V][ceil(D / 32) * 16], copied in boxes of 16 rows by 64.
 static bool codes_map(const Int4Table& T, CUtensorMap* map) {
   typedef decltype(&cuTensorMapEncodeTiled) Encode;
@@ -75,31 +78,36 @@ static bool codes_map(const Int4Table& T, CUtensorMap* map) {
                 CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int kHeadUnit = 2;  // chunks of 128 columns per unit
-
-template <int GPC, int PARTS>
-static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
-  const long long per_col = (long long)PARTS * ((A.chunks + kHeadUnit - 1) / kHeadUnit) * kHeadUnit * 256, most = 227 * 1024;
-  int warps = kHeadWarps;
-  long long cols;
-  while ((cols = (most - HeadLayout::fixed(GPC, kHeadUnit, warps)) / per_col) < 1) warps /= 2;  // D <= 32768: two have room
-  if (cols > 8) cols = 8;
-  if (cols > A.N) cols = A.N;
-  A.cols = (int)cols;
+template <int GPC, int PARTS, int UC>
+static cudaError_t launch_head_unit(HeadArgs& A, const CUtensorMap& codes, int cols, int warps, cudaStream_t st) {
+  A.cols = cols;
   const Int4Table& T = A.T;
   // a lane's scales are half a unit's
-  const int ss = T.scale_bf16 ? 2 : 4, per = GPC * kHeadUnit / 2, align = per * ss < 16 ? per * ss : 16;
+  const int ss = T.scale_bf16 ? 2 : 4, per = GPC * UC / 2, align = per * ss < 16 ? per * ss : 16;
   A.vec = (uintptr_t)T.scales % align == 0 && (T.V == 1 || T.scale_stride * ss % align == 0) &&
           (!T.zeros || ((uintptr_t)T.zeros % per == 0 && (T.V == 1 || T.zero_stride % per == 0)));
-  void (*const kernel)(HeadArgs, CUtensorMap) = cols == 1   ? head_kernel<GPC, PARTS, 1, kHeadUnit>
-                                   : cols == 2 ? head_kernel<GPC, PARTS, 2, kHeadUnit>
-                                               : head_kernel<GPC, PARTS, 0, kHeadUnit>;
-  const int smem = (int)(HeadLayout::fixed(GPC, kHeadUnit, warps) + per_col * cols);
+  void (*const kernel)(HeadArgs, CUtensorMap) = cols == 1   ? head_kernel<GPC, PARTS, 1, UC>
+                                                : cols == 2 ? head_kernel<GPC, PARTS, 2, UC>
+                                                            : head_kernel<GPC, PARTS, 0, UC>;
+  const int smem = (int)(HeadLayout::fixed(GPC, UC, warps) + head_column_bytes(PARTS, A.chunks, UC) * cols);
   const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (err != cudaSuccess) return err;
   dim3 grid((unsigned)(A.tiles < sm_count() ? A.tiles : sm_count()), (unsigned)((A.N + cols - 1) / cols));
   kernel<<<grid, 32 * warps, smem, st>>>(A, codes);
   return cudaGetLastError();
+}
+
+// As many hidden states per pass as shared memory holds, up to 8; units of four chunks (half the work per unit beside the
+// products) where that takes none of them away and a row has that many chunks, otherwise of two.
+template <int GPC, int PARTS>
+static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
+  const long long most = 227 * 1024, want = A.N < 8 ? A.N : 8;
+  if (A.chunks >= 4 && (most - HeadLayout::fixed(GPC, 4, kHeadWarps)) / head_column_bytes(PARTS, A.chunks, 4) >= want)
+    return launch_head_unit<GPC, PARTS, 4>(A, codes, (int)want, kHeadWarps, st);
+  int warps = kHeadWarps;
+  long long cols;
+  while ((cols = (most - HeadLayout::fixed(GPC, 2, warps)) / head_column_bytes(PARTS, A.chunks, 2)) < 1) warps /= 2;  // D <= 32768: two have room
+  return launch_head_unit<GPC, PARTS, 2>(A, codes, (int)(cols < want ? cols : want), warps, st);
 }
 
 template <int PARTS>

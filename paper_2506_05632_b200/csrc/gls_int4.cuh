@@ -5,6 +5,7 @@
 #pragma once
 #include <cuda.h>
 
+#include "gls_async.cuh"
 #include "gls_kernels.cuh"
 
 namespace gls {
@@ -308,24 +309,6 @@ __device__ __forceinline__ uint2 lds8(uint32_t at) {
   return b;
 }
 
-__device__ __forceinline__ void barrier_init(uint32_t at, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(at), "r"(count) : "memory");
-}
-__device__ __forceinline__ void barrier_expect(uint32_t at, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(at), "r"(bytes) : "memory");
-}
-// false if the phase did not end within a limit that no copy reaches
-__device__ __forceinline__ bool barrier_wait(uint32_t at, uint32_t parity) {
-  for (int i = 0; i < (1 << 22); ++i) {
-    uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(done)
-                 : "r"(at), "r"(parity)
-                 : "memory");
-    if (done) return true;
-  }
-  return false;
-}
 // 64 bytes of 16 rows, from byte x of row y on; what lies outside the table comes as zeros
 __device__ __forceinline__ void copy_codes(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t barrier) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to),

@@ -8,18 +8,20 @@
 // so it is described by the least kept logit and how many tokens of that logit stay (the lowest indices).
 // The token is the first by INDEX whose cumulative kept mass exceeds u times the total.
 //
-// A CTA takes a row.  The row is read once from HBM; per chunk of 256 tokens (more in very long rows) the sweep
-// keeps the largest logit and, where a total over the row is needed, the chunk's sum relative to it.  Everything
-// later reads only the chunks whose largest logit reaches a bound, out of L2 (the rows in flight fit there):
+// A CTA takes a row (a cluster of them sweeps it where there are few rows; the first one does the rest).  The row is read
+// once from HBM; per chunk of 256 tokens (more in very long rows) the sweep keeps the largest logit and, where a total
+// over the row is needed, per four chunks the sum relative to their largest.  Everything later reads only the chunks
+// whose largest logit reaches a bound, out of L2 (the rows in flight fit there):
 //     bound    top-k: the k-th largest chunk maximum; top-p: V e^-c = (1 - p) total leaves no more than 1 - p
 //              below max - c; min-p: itself
 //     select   the least kept logit, by counting (and, for top-p, weighing) the tokens above the bound per bin of
 //              their ordered codes and refining the bin the border falls into
 //     sums     the kept tokens' mass per chunk, in 64 bits; the chunk that u falls into; the token inside it
 // Decisions are those of exact arithmetic but for 64-bit rounding: sums that decide something are 64-bit sums of
-// 64-bit exponentials (or integers of 2^-(62 - log2 V)).  The sweep's fp32 sums decide only where their error bound
-// leaves no doubt; otherwise the row is summed again in 64 bits.
+// exponentials good to 2e-13 (or integers of 2^-(62 - log2 V)).  The sweep's fp32 sums decide only where their error
+// bound leaves no doubt; otherwise the row is summed again in 64 bits.
 #pragma once
+#include "gls_async.cuh"
 #include "gls_kernels.cuh"
 
 namespace gls {
@@ -67,6 +69,23 @@ __device__ __forceinline__ T warp_scan(T x) {  // inclusive
   return x;
 }
 
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t cluster_ctas() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+// stores to the first CTA of the cluster
+__device__ __forceinline__ void store_first(const float* at, float x) {
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(at), d;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(d) : "r"(a));
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(d), "f"(x) : "memory");
+}
+
 // A row in positions counted from the 16-byte boundary at or below its start: token i is position i + mis.
 template <int DT>
 struct SampleRow {
@@ -83,6 +102,10 @@ struct SampleRow {
     if (p >= mis && p + 8 <= end) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) r.v[i] = __ldg((const uint4*)(base + p * ES) + i);
+    } else if (p >= end) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) r.v[i] = DT == kBF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                                                          : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
     } else {
       uint32_t w[8];
 #pragma unroll
@@ -102,8 +125,7 @@ struct SampleRow {
     }
     return r;
   }
-  // masked logits (NaN, infinities) become -inf, -0 becomes +0
-  static __device__ __forceinline__ void unpack(const Raw& r, float (&a)[8]) {
+  static __device__ __forceinline__ void widen(const Raw& r, float (&a)[8]) {
     if constexpr (DT == kBF16) {
       const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
 #pragma unroll
@@ -115,6 +137,23 @@ struct SampleRow {
         a[4 * i + 2] = __uint_as_float(r.v[i].z), a[4 * i + 3] = __uint_as_float(r.v[i].w);
       }
     }
+  }
+  // the largest logit, +0 for -0; NaN counts as nothing (-inf)
+  static __device__ __forceinline__ float largest(const Raw& r) {
+    float m;
+    if constexpr (DT == kBF16) {
+      const uint32_t w = max_bf16x2(max_bf16x2(r.v[0].x, r.v[0].y), max_bf16x2(r.v[0].z, r.v[0].w));
+      m = fmaxf(bf16_lo(w), bf16_hi(w));
+    } else {
+      float a[8];
+      widen(r, a);
+      m = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7])));
+    }
+    return fmaxf(m, -CUDART_INF_F) + 0.f;
+  }
+  // masked logits (NaN, infinities) become -inf, -0 becomes +0
+  static __device__ __forceinline__ void unpack(const Raw& r, float (&a)[8]) {
+    widen(r, a);
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = fabsf(a[i]) <= 3.402823466e38f ? a[i] + 0.f : -CUDART_INF_F;
   }
@@ -129,22 +168,36 @@ struct SampleRow {
   static constexpr uint32_t kLowest = DT == kBF16 ? 0x80u : 0x800000u;  // code of the lowest finite value
 };
 
-template <int THREADS>
+constexpr int kSampleChunks = 1024;
+
+// Shared memory: what the search needs lies where the sweep's rings were.
+template <int DT, int THREADS>
 struct SampleShared {
-  static constexpr int kChunks = 2 * THREADS;
-  double psum[kChunks];                     // mass per chunk
-  unsigned long long mass[kSampleBins];     // per bin, in units of 2^-frac
+  static constexpr int kStages = DT == kBF16 ? 3 : 2;
+  static constexpr int kStage = DT == kBF16 ? 2048 : 4096;  // 1024 tokens
+  union {
+    struct {
+      union {
+        double psum[kSampleChunks];            // mass per chunk
+        unsigned long long mass[kSampleBins];  // per bin, in units of 2^-frac
+      };
+      uint32_t count[kSampleBins];  // per bin, or per chunk
+    };
+    char ring[THREADS / 32][kStages][kStage];
+  };
   double wred[32];
-  float cmax[kChunks], csum[kChunks];       // largest logit, sum relative to it
-  uint32_t count[kSampleBins];
+  double exp16[16];             // 2^(i / 16)
+  uint64_t barriers[THREADS / 32][kStages];
+  float cmax[kSampleChunks];    // largest logit of a chunk
+  float csum[kSampleChunks / 4];  // sum relative to the largest logit of four chunks
   uint32_t ired[32];
-  uint16_t list[kChunks];                   // chunks to look at
+  uint16_t list[kSampleChunks];  // chunks to look at
   int n_list;
   // results of a search
   int found;
   uint32_t at;
   uint32_t nabove, nat;
-  double mabove, mat;
+  double mabove;
   long long pos;
 };
 
@@ -172,22 +225,41 @@ struct Sampler {
   typedef SampleRow<DT> Row;
   typedef typename Row::Raw Raw;
   static constexpr int kWarps = THREADS / 32;
-  static constexpr int kAhead = 4;
-  static constexpr int kPer = kSampleBins / THREADS;  // bins per thread in a scan
+  static constexpr int kAhead = DT == kBF16 ? 4 : 2;
+  static constexpr int kPer = kSampleBins / THREADS;     // bins per thread in a scan
+  static constexpr int kPerC = kSampleChunks / THREADS;  // chunks
 
-  SampleShared<THREADS>& sh;
+  typedef SampleShared<DT, THREADS> Shared;
+  Shared& sh;
   Row row;
   int nch, shift, frac;
-  double it;
-  float top;  // the largest logit
+  double it, it2;  // inverse temperature, the same to base 2
+  float top;       // the largest logit
 
-  __device__ __forceinline__ double weight(float x) const { return exp(((double)x - (double)top) * it); }
+  // e^((x - top) it) to 2e-13: 2^n 2^(i / 16) 2^r with |r| <= 1 / 32, the last by its series (eleven operations in 64 bits;
+  // exp() takes about three times as many)
+  __device__ __forceinline__ double weight(float x) const {
+    const double t = ((double)x - (double)top) * it2;
+    const double magic = 6755399441055744.0 / 16.0;  // 1.5 * 2^48: sixteenths in the lowest bits
+    const double big = t + magic;
+    const int n = __double2loint(big);
+    const double r = t - (big - magic);
+    double y = 1.3333558146428443e-3;  // ln2^5 / 5!
+    y = fma(y, r, 9.6181291076284772e-3);
+    y = fma(y, r, 5.5504108664821580e-2);
+    y = fma(y, r, 2.4022650695910071e-1);
+    y = fma(y, r, 6.9314718055994531e-1);
+    y = fma(y, r, 1.0);
+    y *= sh.exp16[n & 15];
+    const int hi = __double2hiint(y) + ((n >> 4) << 20);
+    return t > -1000.0 ? __hiloint2double(hi, __double2loint(y)) : 0.0;
+  }
 
-  // f(chunk, first position of the lane, logits) over all chunks (LISTED: over sh.list), a warp per chunk
-  template <bool LISTED, class Begin, class F, class End>
+  // f(chunk, first position of the lane, logits) over the chunks of sh.list, a warp per chunk
+  template <class Begin, class F, class End>
   __device__ __forceinline__ void for_chunks(Begin&& begin, F&& f, End&& fin) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int n = LISTED ? sh.n_list : nch;
+    const int n = sh.n_list;
     if (shift == 0) {
       for (int i0 = warp; i0 < n; i0 += kWarps * kAhead) {
         Raw r[kAhead];
@@ -195,7 +267,7 @@ struct Sampler {
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
           const int i = i0 + q * kWarps;
-          c[q] = i < n ? (LISTED ? (int)sh.list[i] : i) : -1;
+          c[q] = i < n ? (int)sh.list[i] : -1;
           if (c[q] >= 0) r[q] = row.load((long long)c[q] * 256 + lane * 8);
         }
 #pragma unroll
@@ -211,7 +283,7 @@ struct Sampler {
       return;
     }
     for (int i = warp; i < n; i += kWarps) {
-      const int c = LISTED ? (int)sh.list[i] : i;
+      const int c = (int)sh.list[i];
       begin(c);
       for (long long p = ((long long)c << (8 + shift)) + lane * 8, e = (long long)(c + 1) << (8 + shift); p < e; p += 256) {
         float a[8];
@@ -232,33 +304,104 @@ struct Sampler {
     __syncthreads();
   }
 
-  // Largest logit (and, SUM, the sum of 2^((l - largest) c2)) of each chunk.
+  // Largest logit of each chunk and, SUM, per four chunks the sum of 2^((l - their largest) c2), into the shared memory
+  // of the cluster's first CTA.  A warp takes every so many-th four chunks; those that lie within the row come
+  // through a ring, two or three sets ahead.
   template <bool SUM>
   __device__ __forceinline__ void sweep(float c2) {
-    float m = 0.f, s = 0.f;
-    for_chunks<false>([&](int) { m = -CUDART_INF_F, s = 0.f; },
-                      [&](int, long long, const float (&a)[8]) {
-                        const float mx = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7])));
-                        const float nm = fmaxf(m, redux_max(mx));
-                        if (SUM && nm > -CUDART_INF_F) {
-                          float t = 0.f;
+    constexpr int kStages = Shared::kStages;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rank = (int)cluster_rank(), ranks = (int)cluster_ctas();
+    const int sets = (nch + 3) >> 2, stride = kWarps * ranks, first = warp * ranks + rank;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp]), bars = (uint32_t)__cvta_generic_to_shared(sh.barriers[warp]);
+    auto inside = [&](int g) { return shift == 0 && g * 1024LL >= row.mis && g * 1024LL + 1024 <= row.end; };
+    auto request = [&](int g, int stage) {
+      if (lane == 0 && g < sets && inside(g)) {
+        barrier_expect(bars + stage * 8, Shared::kStage);
+        copy_bulk(ring + stage * Shared::kStage, row.base + (long long)g * Shared::kStage, Shared::kStage, bars + stage * 8);
+      }
+    };
+    if (lane < kStages) barrier_init(bars + lane * 8, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncwarp();
 #pragma unroll
-                          for (int i = 0; i < 8; ++i) t += ex2_approx((a[i] - nm) * c2);
-                          s = s * (m > -CUDART_INF_F ? ex2_approx((m - nm) * c2) : 0.f) + t;
-                        }
-                        m = nm;
-                      },
-                      [&](int c) {
-                        if (SUM) {
+    for (int i = 0; i < kStages; ++i) request(first + i * stride, i);
+    uint32_t phases = 0u;
+    int stage = 0;
+    for (int g = first; g < sets; g += stride) {
+      float m[4], s = 0.f;
+      bool odd = true;  // to be looked at token by token
+      if (inside(g)) {
+        odd = !barrier_wait(bars + stage * 8, phases >> stage & 1u);
+        phases ^= 1u << stage;
+        __syncwarp();
+        Raw r[4];
 #pragma unroll
-                          for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                        }
-                        if ((threadIdx.x & 31) == 0) {
-                          sh.cmax[c] = m;
-                          if (SUM) sh.csum[c] = s;
-                        }
-                      });
-    __syncthreads();
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int i = 0; i < Row::kVec; ++i)  // which lane has which token of a chunk does not matter here
+            r[q].v[i] = *(const uint4*)(sh.ring[warp][stage] + (q * Row::kVec + i) * 512 + lane * 16);
+        __syncwarp();
+        request(g + kStages * stride, stage);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) m[q] = redux_max(Row::largest(r[q]));
+        const float mm = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+        odd |= !(mm < CUDART_INF_F);
+        if (SUM && mm > -CUDART_INF_F) {
+          float t[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float a[8];
+            Row::widen(r[q], a);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = ex2_approx((a[i] - mm) * c2);
+            t[q] = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
+          }
+          s = (t[0] + t[1]) + (t[2] + t[3]);
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+          odd |= !(s < CUDART_INF_F);  // a NaN among the logits
+        }
+      } else {
+        request(g + kStages * stride, stage);
+      }
+      if (odd) s = sweep_carefully<SUM>(g, c2, m);
+      if (lane < 4) {
+        const float mine = lane == 0 ? m[0] : lane == 1 ? m[1] : lane == 2 ? m[2] : m[3];
+        store_first(&sh.cmax[4 * g + lane], mine);
+        if (SUM && lane == 0) store_first(&sh.csum[g], s);
+      }
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+  }
+  // The same with masked logits taken out one by one, for chunks of any size.
+  template <bool SUM>
+  __device__ __noinline__ float sweep_carefully(int g, float c2, float (&m)[4]) {
+    const int lane = threadIdx.x & 31;
+    float mm = -CUDART_INF_F, s = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      m[q] = -CUDART_INF_F;
+      for (long long p = ((long long)(4 * g + q) << (8 + shift)) + lane * 8, e = (long long)(4 * g + q + 1) << (8 + shift); p < e; p += 256) {
+        float a[8];
+        Row::unpack(row.load(p), a);
+        const float b = redux_max(fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7]))));
+        m[q] = fmaxf(m[q], b);
+        const float nm = fmaxf(mm, b);
+        if (SUM && nm > -CUDART_INF_F) {
+          float t = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) t += ex2_approx((a[i] - nm) * c2);
+          s = s * (mm > -CUDART_INF_F ? ex2_approx((mm - nm) * c2) : 0.f) + t;
+        }
+        mm = nm;
+      }
+    }
+    if (SUM) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    }
+    return s;
   }
 
   // Tokens with codes in [lo, lo + span) per bin of 2^sh codes; MASS: their weights too.
@@ -270,15 +413,24 @@ struct Sampler {
     }
     __syncthreads();
     const double unit = (double)(1ull << frac);
-    for_chunks<true>([](int) {},
+    for_chunks([](int) {},
                      [&](int, long long, const float (&a)[8]) {
+                       uint32_t d[8];
+                       bool any = false;
 #pragma unroll
-                       for (int i = 0; i < 8; ++i) {
-                         const uint32_t d = Row::key(a[i]) - lo;
-                         if (d < span) {
-                           atomicAdd(&sh.count[d >> sft], 1u);
-                           if (MASS) atomicAdd(&sh.mass[d >> sft], (unsigned long long)(weight(a[i]) * unit + 0.5));
-                         }
+                       for (int i = 0; i < 8; ++i) any |= (d[i] = Row::key(a[i]) - lo) < span;
+                       if (!__any_sync(0xffffffffu, any)) return;
+#pragma unroll
+                       for (int h = 0; h < 8; h += 4) {
+                         double w[4];
+#pragma unroll
+                         for (int i = 0; i < 4; ++i) w[i] = MASS ? weight(a[h + i]) * unit + 0.5 : 0.0;
+#pragma unroll
+                         for (int i = 0; i < 4; ++i)
+                           if (d[h + i] < span) {
+                             atomicAdd(&sh.count[d[h + i] >> sft], 1u);
+                             if (MASS) atomicAdd(&sh.mass[d[h + i] >> sft], (unsigned long long)w[i]);
+                           }
                        }
                      },
                      [](int) {});
@@ -290,8 +442,8 @@ struct Sampler {
   }
 
   // Code of the k-th largest chunk maximum (at least k tokens reach it); 0 where there are fewer chunks with one.
-  __device__ uint32_t kth_chunk(uint32_t k) {
-    constexpr int kEach = SampleShared<THREADS>::kChunks / 32;
+  __device__ __noinline__ uint32_t kth_chunk(uint32_t k) {
+    constexpr int kEach = kSampleChunks / 32;
     if (threadIdx.x < 32) {
       uint32_t code[kEach];
 #pragma unroll
@@ -317,7 +469,7 @@ struct Sampler {
 
   // The code of the k-th token of the order among codes >= lo, how many tokens of it stay, and how many have it;
   // false where fewer than k tokens are that large.
-  __device__ bool kth(uint32_t lo, uint32_t k, uint32_t* code, uint32_t* take, uint32_t* equal) {
+  __device__ __noinline__ bool kth(uint32_t lo, uint32_t k, uint32_t* code, uint32_t* take, uint32_t* equal) {
     uint32_t span = Row::key(top) - lo + 1u;
     for (;;) {
       const int sft = bin_shift(span);
@@ -370,7 +522,7 @@ struct Sampler {
   // Least kept code under top-p among the codes >= lo (of those at lo, `drop` do not belong to the set).
   // Goal: share times the set's own mass, or somewhere between goal_lo and goal_hi.
   // 1: found; 0: the set does not reach the goal, all of it stays; -1: the interval leaves it open.
-  __device__ int nucleus(uint32_t lo, uint32_t drop, bool own_total, double share, double goal_lo, double goal_hi,
+  __device__ __noinline__ int nucleus(uint32_t lo, uint32_t drop, bool own_total, double share, double goal_lo, double goal_hi,
                          uint32_t* code, uint32_t* take, uint32_t* equal) {
     uint32_t span = Row::key(top) - lo + 1u;
     const uint32_t first = lo;
@@ -452,26 +604,36 @@ struct Sampler {
   }
 
   // Position behind the `take`-th token (by index) of this code; sh.list holds the chunks that may have some.
-  __device__ long long equal_end(uint32_t code, uint32_t take) {
-    uint32_t* cnt = (uint32_t*)sh.csum;  // the sweep's sums are not needed any more
-    for (int c = threadIdx.x; c < SampleShared<THREADS>::kChunks; c += THREADS) cnt[c] = 0u;
+  __device__ __noinline__ long long equal_end(uint32_t code, uint32_t take) {
+    uint32_t* cnt = sh.count;
+    for (int c = threadIdx.x; c < kSampleChunks; c += THREADS) cnt[c] = 0u;
     __syncthreads();
     uint32_t n = 0u;
-    for_chunks<true>([&](int) { n = 0u; },
-                     [&](int, long long, const float (&a)[8]) {
+    for_chunks([&](int) { n = 0u; },
+               [&](int, long long, const float (&a)[8]) {
 #pragma unroll
-                       for (int i = 0; i < 8; ++i) n += Row::key(a[i]) == code ? 1u : 0u;
-                     },
-                     [&](int c) {
-                       n = __reduce_add_sync(0xffffffffu, n);
-                       if ((threadIdx.x & 31) == 0) cnt[c] = n;
-                     });
+                 for (int i = 0; i < 8; ++i) n += Row::key(a[i]) == code ? 1u : 0u;
+               },
+               [&](int c) {
+                 n = __reduce_add_sync(0xffffffffu, n);
+                 if ((threadIdx.x & 31) == 0) cnt[c] = n;
+               });
     __syncthreads();
-    const uint32_t x0 = cnt[2 * threadIdx.x], x1 = cnt[2 * threadIdx.x + 1];
-    uint32_t total;
-    const uint32_t before = block_scan<THREADS>(x0 + x1, sh.ired, &total);
-    if (before < take && take <= before + x0) sh.at = 2 * threadIdx.x, sh.nabove = before;
-    if (before + x0 < take && take <= before + x0 + x1) sh.at = 2 * threadIdx.x + 1, sh.nabove = before + x0;
+    uint32_t mine = 0u, total;
+#pragma unroll
+    for (int i = 0; i < kPerC; ++i) mine += cnt[threadIdx.x * kPerC + i];
+    uint32_t before = block_scan<THREADS>(mine, sh.ired, &total);
+    if (before < take && take <= before + mine) {
+      for (int i = 0; i < kPerC; ++i) {
+        const uint32_t x = cnt[threadIdx.x * kPerC + i];
+        if (take <= before + x) {
+          sh.at = threadIdx.x * kPerC + i;
+          sh.nabove = before;
+          break;
+        }
+        before += x;
+      }
+    }
     __syncthreads();
     if (threadIdx.x < 32) {
       const int lane = threadIdx.x, c = (int)sh.at;
@@ -508,16 +670,32 @@ struct Sampler {
     }
   };
 
+  // The kept ones' mass among a lane's eight tokens.  Weights are computed four at a time whether kept or not (their
+  // operations depend on each other, 20 us a row of 150000 tokens; behind a branch each 100), or for no lane.
+  __device__ __forceinline__ double kept_mass(const Kept& kept, const float (&a)[8], long long p) const {
+    bool in[8], any = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) any |= in[i] = kept(a[i], p + i);
+    double s = 0.0;
+    if (!__any_sync(0xffffffffu, any)) return s;
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      double w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = weight(a[h + i]);
+      s += ((in[h] ? w[0] : 0.0) + (in[h + 1] ? w[1] : 0.0)) + ((in[h + 2] ? w[2] : 0.0) + (in[h + 3] ? w[3] : 0.0));
+    }
+    return s;
+  }
+
   // 64-bit mass of the kept tokens of the listed chunks -> sh.psum, 0 elsewhere
-  __device__ void exact_sums(const Kept& kept) {
-    for (int c = threadIdx.x; c < SampleShared<THREADS>::kChunks; c += THREADS) sh.psum[c] = 0.0;
+  __device__ __noinline__ void exact_sums(const Kept& kept) {
+    for (int c = threadIdx.x; c < kSampleChunks; c += THREADS) sh.psum[c] = 0.0;
     __syncthreads();
     double s = 0.0;
-    for_chunks<true>([&](int) { s = 0.0; },
+    for_chunks([&](int) { s = 0.0; },
                      [&](int, long long p, const float (&a)[8]) {
-#pragma unroll
-                       for (int i = 0; i < 8; ++i)
-                         if (kept(a[i], p + i)) s += weight(a[i]);
+                       s += kept_mass(kept, a, p);
                      },
                      [&](int c) {
                        s = warp_sum(s);
@@ -526,32 +704,42 @@ struct Sampler {
     __syncthreads();
   }
   __device__ double total_mass() {
-    double total;
-    block_scan<THREADS>(sh.psum[2 * threadIdx.x] + sh.psum[2 * threadIdx.x + 1], sh.wred, &total);
+    double mine = 0.0, total;
+#pragma unroll
+    for (int i = 0; i < kPerC; ++i) mine += sh.psum[threadIdx.x * kPerC + i];
+    block_scan<THREADS>(mine, sh.wred, &total);
     return total;
   }
 
-  // The token that u falls to by sh.psum.  slack: relative error of those sums; false where it leaves the token open.
-  __device__ bool locate(const Kept& kept, double u, double slack, long long* pos, double* total_out) {
-    const double x0 = sh.psum[2 * threadIdx.x], x1 = sh.psum[2 * threadIdx.x + 1];
-    double total;
-    const double before = block_scan<THREADS>(x0 + x1, sh.wred, &total);
+  // The token that u falls to by sh.psum, whose entries hold 2^size positions each.  slack: relative error of those sums;
+  // false where it leaves the token open.
+  __device__ __noinline__ bool locate(const Kept& kept, double u, int size, double slack, long long* pos, double* total_out) {
+    double mine = 0.0, total;
+#pragma unroll
+    for (int i = 0; i < kPerC; ++i) mine += sh.psum[threadIdx.x * kPerC + i];
+    double before = block_scan<THREADS>(mine, sh.wred, &total);
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
     if (x > most) x = most;
     if (threadIdx.x == 0) sh.found = 0, sh.pos = -1;
     __syncthreads();
     // the pieces' borders are rounded sums: where none holds x, the last chunk with mass does
-    const bool in0 = x0 > 0.0 && before <= x && x < before + x0, in1 = x1 > 0.0 && before + x0 <= x && x < before + (x0 + x1);
-    if (in0 || in1) {
-      sh.at = 2 * threadIdx.x + (in0 ? 0 : 1);
-      sh.mabove = in0 ? before : before + x0;
-      sh.found = 1;
+    if (mine > 0.0 && before <= x && x < before + mine) {
+      for (int i = 0; i < kPerC; ++i) {
+        const double y = sh.psum[threadIdx.x * kPerC + i];
+        if (y > 0.0) {
+          sh.at = threadIdx.x * kPerC + i;
+          sh.mabove = before;
+          sh.found = 1;
+          if (x < before + y) break;
+        }
+        before += y;
+      }
     }
     __syncthreads();
     if (!sh.found && threadIdx.x == 0) {
       double b = 0.0;
-      for (int c = 0; c < nch; ++c)
+      for (int c = 0; c < kSampleChunks; ++c)
         if (sh.psum[c] > 0.0 && (b <= x || !sh.found)) {
           sh.at = (uint32_t)c;
           sh.mabove = b;
@@ -567,7 +755,7 @@ struct Sampler {
       const double margin = slack * total;
       long long last = -1;  // last kept position so far
       bool sure = true, done = false;
-      for (long long p0 = c << (8 + shift), e = (c + 1) << (8 + shift); p0 < e && !done; p0 += 256) {
+      for (long long p0 = c << size, e = (c + 1) << size; p0 < e && !done; p0 += 256) {
         const long long p = p0 + lane * 8;
         float a[8];
         Row::unpack(row.load(p), a);
@@ -575,7 +763,8 @@ struct Sampler {
         int mlast = -1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          w[i] = kept(a[i], p + i) ? weight(a[i]) : 0.0;
+          w[i] = weight(a[i]);
+          if (!kept(a[i], p + i)) w[i] = 0.0;
           mine += w[i];
           if (w[i] > 0.0) mlast = i;
         }
@@ -622,11 +811,12 @@ __device__ __forceinline__ float sample_setting(const SampleSetting& s, long lon
 }
 
 template <int DT, int THREADS>
-__global__ void __launch_bounds__(THREADS) sample_kernel(const SampleArgs A) {
+__global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const SampleArgs A) {
   typedef SampleRow<DT> Row;
-  __shared__ SampleShared<THREADS> sh;
+  extern __shared__ __align__(128) char sample_shared[];
+  SampleShared<DT, THREADS>& sh = *(SampleShared<DT, THREADS>*)sample_shared;
   Sampler<DT, THREADS> S{sh};
-  const long long r = blockIdx.x;
+  const long long r = blockIdx.x / cluster_ctas();
   const int j = (int)(r % A.J), k = (int)(r / A.J % A.K);
   const long long b = r / A.J / A.K;
   float itf = sample_setting(A.inv_temp, b, k, j), p = sample_setting(A.top_p, b, k, j), mp = sample_setting(A.min_p, b, k, j);
@@ -634,7 +824,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const SampleArgs A) {
   const float u = __ldg(A.u + r);
   const bool greedy = itf == CUDART_INF_F;
   if (!((itf >= 1e-20f && itf <= 1e20f) || greedy) || !(p > 0.f) || !(mp >= 0.f && mp <= 1.f) || !(u >= 0.f && u <= 1.f)) {
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && cluster_rank() == 0) {
       A.tokens[r] = -1;
       if (A.logprobs) A.logprobs[r] = 0.f;
       if (A.status) atomicOr(A.status, kSampleBadSetting);
@@ -651,11 +841,23 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const SampleArgs A) {
   S.nch = (int)((S.row.end + (256LL << A.shift) - 1) >> (8 + A.shift));
   S.frac = 62 - (32 - __clz(A.V));
   S.it = (double)itf;
+  S.it2 = S.it * 1.4426950408889634;
+  if (threadIdx.x < 16) sh.exp16[threadIdx.x] = exp2((double)threadIdx.x * 0.0625);
   const bool use_k = kk > 0 && kk < A.V, use_p = p < 1.f;
   const bool need_sum = !use_k && (use_p || mp == 0.f);
   const float c2 = itf * kLog2e;
+  if (cluster_ctas() > 1) {  // the first CTA's shared memory is written by the others
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+  }
   if (need_sum) S.template sweep<true>(c2);
   else S.template sweep<false>(c2);
+  if (cluster_ctas() > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (cluster_rank() != 0) return;
+  }
+  __syncthreads();
   float m = -CUDART_INF_F;
   for (int c = threadIdx.x; c < S.nch; c += THREADS) m = fmaxf(m, sh.cmax[c]);
   m = redux_max(m);
@@ -673,17 +875,23 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const SampleArgs A) {
   }
   S.top = m;
   typename Sampler<DT, THREADS>::Kept kept{Row::kLowest, S.row.end};
-  // Relative error of a chunk's sum: exponentials 2^-22; their arguments 3 roundings, weighted by the terms themselves
-  // |t| is log2(chunk) + 1.5 on the mean; a chain of 2^shift + 13 additions.  One more step for what follows in 64 bits.
-  const double eps = 2.5e-7 + 1.3e-7 * (9.5 + A.shift) + 6e-8 * (14.0 + (double)(1 << A.shift));
+  // Relative error of a sum of four chunks: exponentials 2^-22; their arguments 3 roundings, where |t|, weighted by the terms
+  // themselves, is log2(tokens) + 1.5 on the mean; 10 additions one after another, or 2^(2 + shift) more in long chunks.
+  const double eps = 2.5e-7 + 1.3e-7 * (11.5 + A.shift) + 6e-8 * (12.0 + (A.shift ? (double)(4 << A.shift) : 4.0));
   double total = 0.0;
   long long pos = -1;
   bool done = false;
   if (need_sum) {
-    for (int c = threadIdx.x; c < SampleShared<THREADS>::kChunks; c += THREADS)
-      sh.psum[c] = c < S.nch && sh.cmax[c] > -CUDART_INF_F ? (double)sh.csum[c] * S.weight(sh.cmax[c]) : 0.0;
+    for (int g = threadIdx.x; g < kSampleChunks; g += THREADS) {
+      double y = 0.0;
+      if (4 * g < S.nch) {
+        const float mm = fmaxf(fmaxf(sh.cmax[4 * g], sh.cmax[4 * g + 1]), fmaxf(sh.cmax[4 * g + 2], sh.cmax[4 * g + 3]));
+        if (mm > -CUDART_INF_F) y = (double)sh.csum[g] * S.weight(mm);
+      }
+      sh.psum[g] = y;
+    }
     __syncthreads();
-    if (!use_p) done = S.locate(kept, (double)u, 2.2 * eps, &pos, &total);
+    if (!use_p) done = S.locate(kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
   }
   if (!done) {
     // the least code that min-p keeps
@@ -751,7 +959,7 @@ __global__ void __launch_bounds__(THREADS) sample_kernel(const SampleArgs A) {
     kept.end = S.row.end;
     if (take < equal) kept.end = S.equal_end(kept.code, take);
     S.exact_sums(kept);
-    S.locate(kept, (double)u, 0.0, &pos, &total);
+    S.locate(kept, (double)u, 8 + A.shift, 0.0, &pos, &total);
   }
   if (threadIdx.x == 0) {
     if (pos < S.row.mis) pos = S.row.mis - 1;  // not reached: the largest logit is always kept

@@ -19,11 +19,35 @@ static SampleSetting setting(const void* rows, const int64_t* stride, float valu
 }
 
 template <int DT, int THREADS>
-static void launch_sample(SampleArgs& A, long long rows, cudaStream_t st) {
+static cudaError_t launch_sample(SampleArgs& A, long long rows, int ctas, cudaStream_t st) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)ctas;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(rows * ctas));
+  cfg.blockDim = dim3(THREADS);
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = ctas > 1 ? 1 : 0;
+  cfg.dynamicSmemBytes = sizeof(SampleShared<DT, THREADS>);
+  const cudaError_t err = cudaFuncSetAttribute(sample_kernel<DT, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+  if (err != cudaSuccess) return err;
+  return cudaLaunchKernelEx(&cfg, sample_kernel<DT, THREADS>, A);
+}
+
+template <int DT>
+static cudaError_t launch_sample_rows(SampleArgs& A, long long rows, cudaStream_t st) {
   // as few positions per chunk as leave the row no more chunks than there is room for
   A.shift = 0;
-  while ((((long long)A.V + 15 + (256LL << A.shift) - 1) >> (8 + A.shift)) > SampleShared<THREADS>::kChunks) ++A.shift;
-  sample_kernel<DT, THREADS><<<(unsigned)rows, THREADS, 0, st>>>(A);
+  while ((((long long)A.V + 7 + (256LL << A.shift) - 1) >> (8 + A.shift)) > kSampleChunks) ++A.shift;
+  // few rows: several CTAs sweep one, so that most SMs have a share of it
+  const int sms = sm_count();
+  if (A.V <= 8192) return launch_sample<DT, 128>(A, rows, 1, st);
+  if (rows * 2 > sms) return rows * 2 > 4 * sms ? launch_sample<DT, 256>(A, rows, 1, st) : launch_sample<DT, 512>(A, rows, 1, st);
+  int ctas = 2;
+  while (ctas < 8 && rows * ctas * 2 <= sms && A.V > 8192 * ctas) ctas *= 2;
+  return launch_sample<DT, 512>(A, rows, ctas, st);
 }
 
 }  // namespace gls
@@ -57,12 +81,6 @@ extern "C" int gls_sample_tokens(const gls_rows_t* logits, int B, int K, int J, 
   A.status = device_status;
   const long long rows = (long long)B * K * J;
   cudaStream_t st = (cudaStream_t)stream;
-  if (V <= 8192) {
-    if (logits->dtype == GLS_F32) launch_sample<kF32, 128>(A, rows, st);
-    else launch_sample<kBF16, 128>(A, rows, st);
-  } else {
-    if (logits->dtype == GLS_F32) launch_sample<kF32, 512>(A, rows, st);
-    else launch_sample<kBF16, 512>(A, rows, st);
-  }
-  return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
+  const cudaError_t err = logits->dtype == GLS_F32 ? launch_sample_rows<kF32>(A, rows, st) : launch_sample_rows<kBF16>(A, rows, st);
+  return err == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
 }
