@@ -95,13 +95,13 @@ struct SampleRow {
     uint4 v[kVec];
   };
   const char* base;
-  long long mis, end;
+  uint32_t mis, end;
 
-  __device__ __forceinline__ Raw load(long long p) const {
+  __device__ __forceinline__ Raw load(uint32_t p) const {
     Raw r;
     if (p >= mis && p + 8 <= end) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) r.v[i] = __ldg((const uint4*)(base + p * ES) + i);
+      for (int i = 0; i < kVec; ++i) r.v[i] = __ldg((const uint4*)(base + (long long)p * ES) + i);
     } else if (p >= end) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) r.v[i] = DT == kBF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
@@ -169,6 +169,7 @@ struct SampleRow {
 };
 
 constexpr int kSampleChunks = 1024;
+constexpr int kSampleList = 2048;
 
 // Shared memory: what the search needs lies where the sweep's rings were.
 template <int DT, int THREADS>
@@ -182,11 +183,12 @@ struct SampleShared {
         unsigned long long mass[kSampleBins];  // per bin, in units of 2^-frac
       };
       uint32_t count[kSampleBins];  // per bin, or per chunk
+      uint32_t key[kSampleList], place[kSampleList];  // codes and positions of listed tokens, in order of position
     };
     char ring[THREADS / 32][kStages][kStage];
   };
   double wred[32];
-  double exp16[16];             // 2^(i / 16)
+  double exp64[64];             // 2^(i / 64)
   uint64_t barriers[THREADS / 32][kStages];
   float cmax[kSampleChunks];    // largest logit of a chunk
   float csum[kSampleChunks / 4];  // sum relative to the largest logit of four chunks
@@ -198,7 +200,7 @@ struct SampleShared {
   uint32_t at;
   uint32_t nabove, nat;
   double mabove;
-  long long pos;
+  uint32_t pos;
 };
 
 // exclusive prefix of x over the block; *total: the sum over all
@@ -221,6 +223,9 @@ __device__ __forceinline__ T block_scan(T x, T* red, T* total) {
 }
 
 template <int DT, int THREADS>
+struct SampleCalls;
+
+template <int DT, int THREADS>
 struct Sampler {
   typedef SampleRow<DT> Row;
   typedef typename Row::Raw Raw;
@@ -230,36 +235,52 @@ struct Sampler {
   static constexpr int kPerC = kSampleChunks / THREADS;  // chunks
 
   typedef SampleShared<DT, THREADS> Shared;
-  Shared& sh;
+  // (found anew in each function, so that the compiler sees that it is shared memory)
+  static __device__ __forceinline__ Shared& shared() {
+    extern __shared__ __align__(128) char sample_shared[];
+    return *(Shared*)sample_shared;
+  }
   Row row;
   int nch, shift, frac;
+  int listed;      // tokens in shared().key, or -1
   double it, it2;  // inverse temperature, the same to base 2
+  double c;        // exponent of a logit x: (x - base) it2 - c, where one of base and c is 0
+  float base;
   float top;       // the largest logit
+  float least;     // below it weights are 0
 
-  // e^((x - top) it) to 2e-13: 2^n 2^(i / 16) 2^r with |r| <= 1 / 32, the last by its series (eleven operations in 64 bits;
-  // exp() takes about three times as many)
-  __device__ __forceinline__ double weight(float x) const {
-    const double t = ((double)x - (double)top) * it2;
-    const double magic = 6755399441055744.0 / 16.0;  // 1.5 * 2^48: sixteenths in the lowest bits
+  __device__ __forceinline__ void set_top(float m) {
+    top = m;
+    c = (double)m * it2;
+    base = 0.f;
+    // c is rounded, by the same for all weights; where that is too much the difference comes first (logits that far
+    // from 0 and different from the largest have no weight)
+    if (!(fabs(c) < 1073741824.0)) base = m, c = 0.0;
+    least = (float)((double)m - 1000.0 / it2);
+    if (!(least >= -3.402823466e38f)) least = -3.402823466e38f;
+  }
+  // 2^((x - top) it2) to 1e-13 for x >= least: 2^n 2^(i / 64) 2^r with |r| <= 1 / 128, the last by its series (nine
+  // operations in 64 bits and a conversion; exp() takes about three times as many)
+  __device__ __forceinline__ double weight_of(float x) const {
+    const double t = fma((double)(x - base), it2, -c);
+    const double magic = 6755399441055744.0 / 64.0;  // 1.5 * 2^46: 64ths in the lowest bits
     const double big = t + magic;
     const int n = __double2loint(big);
     const double r = t - (big - magic);
-    double y = 1.3333558146428443e-3;  // ln2^5 / 5!
-    y = fma(y, r, 9.6181291076284772e-3);
-    y = fma(y, r, 5.5504108664821580e-2);
-    y = fma(y, r, 2.4022650695910071e-1);
-    y = fma(y, r, 6.9314718055994531e-1);
-    y = fma(y, r, 1.0);
-    y *= sh.exp16[n & 15];
-    const int hi = __double2hiint(y) + ((n >> 4) << 20);
-    return t > -1000.0 ? __hiloint2double(hi, __double2loint(y)) : 0.0;
+    double q = 9.6181291076284772e-3;  // ln2^4 / 4!
+    q = fma(q, r, 5.5504108664821580e-2);
+    q = fma(q, r, 2.4022650695910071e-1);
+    q = fma(q, r, 6.9314718055994531e-1);
+    const double e = shared().exp64[n & 63], y = fma(e * r, q, e);
+    return __hiloint2double(__double2hiint(y) + ((n >> 6) << 20), __double2loint(y));
   }
+  __device__ __forceinline__ double weight(float x) const { return x >= least ? weight_of(x) : 0.0; }
 
-  // f(chunk, first position of the lane, logits) over the chunks of sh.list, a warp per chunk
+  // f(chunk, first position of the lane, logits) over the chunks of shared().list, a warp per chunk
   template <class Begin, class F, class End>
   __device__ __forceinline__ void for_chunks(Begin&& begin, F&& f, End&& fin) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int n = sh.n_list;
+    const int n = shared().n_list;
     if (shift == 0) {
       for (int i0 = warp; i0 < n; i0 += kWarps * kAhead) {
         Raw r[kAhead];
@@ -267,8 +288,8 @@ struct Sampler {
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
           const int i = i0 + q * kWarps;
-          c[q] = i < n ? (int)sh.list[i] : -1;
-          if (c[q] >= 0) r[q] = row.load((long long)c[q] * 256 + lane * 8);
+          c[q] = i < n ? (int)shared().list[i] : -1;
+          if (c[q] >= 0) r[q] = row.load((uint32_t)c[q] * 256u + lane * 8);
         }
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
@@ -276,17 +297,18 @@ struct Sampler {
           float a[8];
           Row::unpack(r[q], a);
           begin(c[q]);
-          f(c[q], (long long)c[q] * 256 + lane * 8, a);
+          f(c[q], (uint32_t)c[q] * 256u + lane * 8, a);
           fin(c[q]);
         }
       }
       return;
     }
     for (int i = warp; i < n; i += kWarps) {
-      const int c = (int)sh.list[i];
+      const int c = (int)shared().list[i];
       begin(c);
-      for (long long p = ((long long)c << (8 + shift)) + lane * 8, e = (long long)(c + 1) << (8 + shift); p < e; p += 256) {
+      for (int i = 0; i < 1 << shift; ++i) {
         float a[8];
+        const uint32_t p = ((uint32_t)c << (8 + shift)) + (uint32_t)i * 256u + lane * 8;
         Row::unpack(row.load(p), a);
         f(c, p, a);
       }
@@ -294,13 +316,73 @@ struct Sampler {
     }
   }
 
-  // chunks whose largest logit reaches `bound` -> sh.list
+  // chunks whose largest logit reaches `bound` -> shared().list, in order
   __device__ __forceinline__ void make_list(float bound) {
+    uint32_t in = 0u, total;
+#pragma unroll
+    for (int i = 0; i < kPerC; ++i) {
+      const int c = (int)threadIdx.x * kPerC + i;
+      if (c < nch && shared().cmax[c] >= bound) in |= 1u << i;
+    }
+    uint32_t at = block_scan<THREADS>((uint32_t)__popc(in), shared().ired, &total);
+#pragma unroll
+    for (int i = 0; i < kPerC; ++i)
+      if (in >> i & 1u) shared().list[at++] = (uint16_t)(threadIdx.x * kPerC + i);
+    if (threadIdx.x == 0) shared().n_list = (int)total;
     __syncthreads();
-    if (threadIdx.x == 0) sh.n_list = 0;
+  }
+
+  // The tokens with logits of `bound` and above -> shared().key and shared().place, in order of position; shared().list holds their chunks.
+  // Sets `listed`; no more than there is room for, otherwise -1.
+  __device__ __forceinline__ void gather(float bound) {
+    uint32_t* const cnt = shared().count;  // per entry of the list
+    uint32_t n = 0u;
+    for (int i = threadIdx.x; i < kSampleChunks; i += THREADS) cnt[i] = 0u;
     __syncthreads();
-    for (int c = threadIdx.x; c < nch; c += THREADS)
-      if (sh.cmax[c] >= bound) sh.list[atomicAdd(&sh.n_list, 1)] = (uint16_t)c;
+    auto hits_of = [&](const float (&a)[8]) {
+      uint32_t h = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h |= (a[i] >= bound ? 1u : 0u) << i;
+      return h;
+    };
+    const int lane = threadIdx.x & 31;
+    for_chunks([&](int) { n = 0u; }, [&](int, uint32_t, const float (&a)[8]) { n += __popc(hits_of(a)); },
+               [&](int c) {
+                 n = __reduce_add_sync(0xffffffffu, n);
+                 if (lane == 0) cnt[c] = n;
+               });
+    __syncthreads();
+    uint32_t mine[kPerC], sum = 0u, total;
+#pragma unroll
+    for (int i = 0; i < kPerC; ++i) sum += mine[i] = cnt[threadIdx.x * kPerC + i];
+    uint32_t at = block_scan<THREADS>(sum, shared().ired, &total);
+    if (total > (uint32_t)kSampleList) {
+      listed = -1;
+      __syncthreads();
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < kPerC; ++i) {
+      cnt[threadIdx.x * kPerC + i] = at;
+      at += mine[i];
+    }
+    __syncthreads();
+    for_chunks([&](int c) { n = cnt[c]; },
+               [&](int, uint32_t p, const float (&a)[8]) {
+                 const uint32_t h = hits_of(a);
+                 if (!__any_sync(0xffffffffu, h != 0u)) return;
+                 const uint32_t k = __popc(h), incl = warp_scan(k);
+                 uint32_t to = n + incl - k;
+#pragma unroll
+                 for (int i = 0; i < 8; ++i)
+                   if (h >> i & 1u) {
+                     shared().key[to] = Row::key(a[i]);
+                     shared().place[to++] = p + i;
+                   }
+                 n += __shfl_sync(0xffffffffu, incl, 31);
+               },
+               [](int) {});
+    listed = (int)total;
     __syncthreads();
   }
 
@@ -313,7 +395,7 @@ struct Sampler {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int rank = (int)cluster_rank(), ranks = (int)cluster_ctas();
     const int sets = (nch + 3) >> 2, stride = kWarps * ranks, first = warp * ranks + rank;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(sh.ring[warp]), bars = (uint32_t)__cvta_generic_to_shared(sh.barriers[warp]);
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(shared().ring[warp]), bars = (uint32_t)__cvta_generic_to_shared(shared().barriers[warp]);
     auto inside = [&](int g) { return shift == 0 && g * 1024LL >= row.mis && g * 1024LL + 1024 <= row.end; };
     auto request = [&](int g, int stage) {
       if (lane == 0 && g < sets && inside(g)) {
@@ -340,7 +422,7 @@ struct Sampler {
         for (int q = 0; q < 4; ++q)
 #pragma unroll
           for (int i = 0; i < Row::kVec; ++i)  // which lane has which token of a chunk does not matter here
-            r[q].v[i] = *(const uint4*)(sh.ring[warp][stage] + (q * Row::kVec + i) * 512 + lane * 16);
+            r[q].v[i] = *(const uint4*)(shared().ring[warp][stage] + (q * Row::kVec + i) * 512 + lane * 16);
         __syncwarp();
         request(g + kStages * stride, stage);
 #pragma unroll
@@ -365,26 +447,31 @@ struct Sampler {
       } else {
         request(g + kStages * stride, stage);
       }
-      if (odd) s = sweep_carefully<SUM>(g, c2, m);
+      if (odd) {
+        float4 q;
+        s = SampleCalls<DT, THREADS>::sweep_carefully(*this, g, c2, SUM, &q);
+        m[0] = q.x, m[1] = q.y, m[2] = q.z, m[3] = q.w;
+      }
       if (lane < 4) {
         const float mine = lane == 0 ? m[0] : lane == 1 ? m[1] : lane == 2 ? m[2] : m[3];
-        store_first(&sh.cmax[4 * g + lane], mine);
-        if (SUM && lane == 0) store_first(&sh.csum[g], s);
+        store_first(&shared().cmax[4 * g + lane], mine);
+        if (SUM && lane == 0) store_first(&shared().csum[g], s);
       }
       stage = stage + 1 == kStages ? 0 : stage + 1;
     }
   }
   // The same with masked logits taken out one by one, for chunks of any size.
   template <bool SUM>
-  __device__ __noinline__ float sweep_carefully(int g, float c2, float (&m)[4]) {
+  __device__ __forceinline__ float sweep_carefully(int g, float c2, float (&m)[4]) {
     const int lane = threadIdx.x & 31;
     float mm = -CUDART_INF_F, s = 0.f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       m[q] = -CUDART_INF_F;
-      for (long long p = ((long long)(4 * g + q) << (8 + shift)) + lane * 8, e = (long long)(4 * g + q + 1) << (8 + shift); p < e; p += 256) {
+      if (4 * g + q >= nch) continue;
+      for (int k = 0; k < 1 << shift; ++k) {
         float a[8];
-        Row::unpack(row.load(p), a);
+        Row::unpack(row.load(((uint32_t)(4 * g + q) << (8 + shift)) + (uint32_t)k * 256u + lane * 8), a);
         const float b = redux_max(fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(a[4], a[5]), fmaxf(a[6], a[7]))));
         m[q] = fmaxf(m[q], b);
         const float nm = fmaxf(mm, b);
@@ -404,36 +491,49 @@ struct Sampler {
     return s;
   }
 
-  // Tokens with codes in [lo, lo + span) per bin of 2^sh codes; MASS: their weights too.
+  // Tokens with codes in [lo, lo + span) per bin of 2^sft codes, of the listed tokens or of the listed chunks; MASS: their
+  // weights too.
   template <bool MASS>
   __device__ __forceinline__ void histogram(uint32_t lo, uint32_t span, int sft) {
     for (int i = threadIdx.x; i < kSampleBins; i += THREADS) {
-      sh.count[i] = 0u;
-      if (MASS) sh.mass[i] = 0ull;
+      shared().count[i] = 0u;
+      if (MASS) shared().mass[i] = 0ull;
     }
     __syncthreads();
     const double unit = (double)(1ull << frac);
-    for_chunks([](int) {},
-                     [&](int, long long, const float (&a)[8]) {
-                       uint32_t d[8];
-                       bool any = false;
+    if (listed >= 0) {
+      for (int i = threadIdx.x; i < listed; i += THREADS) {
+        const uint32_t d = shared().key[i] - lo;
+        if (d < span) {
+          atomicAdd(&shared().count[d >> sft], 1u);
+          if (MASS) atomicAdd(&shared().mass[d >> sft], (unsigned long long)(weight(Row::value(shared().key[i])) * unit + 0.5));
+        }
+      }
+    } else {
+      const float from = Row::value(lo);
+      for_chunks([](int) {},
+                 [&](int, uint32_t, const float (&a)[8]) {
+                   bool any = false;
 #pragma unroll
-                       for (int i = 0; i < 8; ++i) any |= (d[i] = Row::key(a[i]) - lo) < span;
-                       if (!__any_sync(0xffffffffu, any)) return;
+                   for (int i = 0; i < 8; ++i) any |= a[i] >= from;
+                   if (!__any_sync(0xffffffffu, any)) return;
 #pragma unroll
-                       for (int h = 0; h < 8; h += 4) {
-                         double w[4];
+                   for (int h = 0; h < 8; h += 4) {
+                     double w[4];
 #pragma unroll
-                         for (int i = 0; i < 4; ++i) w[i] = MASS ? weight(a[h + i]) * unit + 0.5 : 0.0;
+                     for (int i = 0; i < 4; ++i) w[i] = MASS ? weight(a[h + i]) * unit + 0.5 : 0.0;
 #pragma unroll
-                         for (int i = 0; i < 4; ++i)
-                           if (d[h + i] < span) {
-                             atomicAdd(&sh.count[d[h + i] >> sft], 1u);
-                             if (MASS) atomicAdd(&sh.mass[d[h + i] >> sft], (unsigned long long)w[i]);
-                           }
+                     for (int i = 0; i < 4; ++i) {
+                       const uint32_t d = Row::key(a[h + i]) - lo;
+                       if (d < span) {
+                         atomicAdd(&shared().count[d >> sft], 1u);
+                         if (MASS) atomicAdd(&shared().mass[d >> sft], (unsigned long long)w[i]);
                        }
-                     },
-                     [](int) {});
+                     }
+                   }
+                 },
+                 [](int) {});
+    }
     __syncthreads();
   }
   static __device__ __forceinline__ int bin_shift(uint32_t span) {
@@ -442,14 +542,14 @@ struct Sampler {
   }
 
   // Code of the k-th largest chunk maximum (at least k tokens reach it); 0 where there are fewer chunks with one.
-  __device__ __noinline__ uint32_t kth_chunk(uint32_t k) {
+  __device__ __forceinline__ uint32_t kth_chunk(uint32_t k) {
     constexpr int kEach = kSampleChunks / 32;
     if (threadIdx.x < 32) {
       uint32_t code[kEach];
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int c = i * 32 + (int)threadIdx.x;
-        code[i] = c < nch ? Row::key(sh.cmax[c]) : 0u;
+        code[i] = c < nch ? Row::key(shared().cmax[c]) : 0u;
       }
       uint32_t best = 0u;
       for (int bit = DT == kBF16 ? 15 : 31; bit >= 0; --bit) {
@@ -459,46 +559,46 @@ struct Sampler {
         for (int i = 0; i < kEach; ++i) n += code[i] >= cand ? 1u : 0u;
         if (__reduce_add_sync(0xffffffffu, n) >= k) best = cand;
       }
-      if (threadIdx.x == 0) sh.at = best;
+      if (threadIdx.x == 0) shared().at = best;
     }
     __syncthreads();
-    const uint32_t best = sh.at;
+    const uint32_t best = shared().at;
     __syncthreads();
     return best;
   }
 
   // The code of the k-th token of the order among codes >= lo, how many tokens of it stay, and how many have it;
   // false where fewer than k tokens are that large.
-  __device__ __noinline__ bool kth(uint32_t lo, uint32_t k, uint32_t* code, uint32_t* take, uint32_t* equal) {
+  __device__ __forceinline__ bool kth(uint32_t lo, uint32_t k, uint32_t* code, uint32_t* take, uint32_t* equal) {
     uint32_t span = Row::key(top) - lo + 1u;
     for (;;) {
       const int sft = bin_shift(span);
       histogram<false>(lo, span, sft);
       uint32_t mine = 0u, total;
 #pragma unroll
-      for (int j = 0; j < kPer; ++j) mine += sh.count[kSampleBins - 1 - ((int)threadIdx.x * kPer + j)];
-      uint32_t before = block_scan<THREADS>(mine, sh.ired, &total);
+      for (int j = 0; j < kPer; ++j) mine += shared().count[kSampleBins - 1 - ((int)threadIdx.x * kPer + j)];
+      uint32_t before = block_scan<THREADS>(mine, shared().ired, &total);
       if (total < k) return false;
       if (before < k && k <= before + mine) {
         for (int j = 0; j < kPer; ++j) {
           const int bin = kSampleBins - 1 - ((int)threadIdx.x * kPer + j);
-          const uint32_t n = sh.count[bin];
+          const uint32_t n = shared().count[bin];
           if (k <= before + n) {
-            sh.at = (uint32_t)bin;
-            sh.nabove = before;
-            sh.nat = n;
+            shared().at = (uint32_t)bin;
+            shared().nabove = before;
+            shared().nat = n;
             break;
           }
           before += n;
         }
       }
       __syncthreads();
-      const uint32_t bin = sh.at;
-      k -= sh.nabove;
+      const uint32_t bin = shared().at;
+      k -= shared().nabove;
       if (sft == 0) {
         *code = lo + bin;
         *take = k;
-        *equal = sh.nat;
+        *equal = shared().nat;
         __syncthreads();
         return true;
       }
@@ -522,7 +622,7 @@ struct Sampler {
   // Least kept code under top-p among the codes >= lo (of those at lo, `drop` do not belong to the set).
   // Goal: share times the set's own mass, or somewhere between goal_lo and goal_hi.
   // 1: found; 0: the set does not reach the goal, all of it stays; -1: the interval leaves it open.
-  __device__ __noinline__ int nucleus(uint32_t lo, uint32_t drop, bool own_total, double share, double goal_lo, double goal_hi,
+  __device__ __forceinline__ int nucleus(uint32_t lo, uint32_t drop, bool own_total, double share, double goal_lo, double goal_hi,
                          uint32_t* code, uint32_t* take, uint32_t* equal) {
     uint32_t span = Row::key(top) - lo + 1u;
     const uint32_t first = lo;
@@ -537,20 +637,20 @@ struct Sampler {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) {
         const int bin = kSampleBins - 1 - ((int)threadIdx.x * kPer + j);
-        uint32_t n = sh.count[bin];
+        uint32_t n = shared().count[bin];
         const bool lowest = bin == 0 && lo == first && drop > 0u;
         m[j] = 0.0;
         if (sft == 0) {
           if (lowest) n -= drop;
           if (n) m[j] = (double)n * weight(Row::value(lo + (uint32_t)bin));
         } else {
-          if (n) m[j] = (double)sh.mass[bin] * per_unit;
+          if (n) m[j] = (double)shared().mass[bin] * per_unit;
           if (lowest) m[j] -= (double)drop * weight(Row::value(lo));
         }
         mine += m[j];
       }
-      if (threadIdx.x == 0) sh.found = 0;
-      double before = above + block_scan<THREADS>(mine, sh.wred, &total);
+      if (threadIdx.x == 0) shared().found = 0;
+      double before = above + block_scan<THREADS>(mine, shared().wred, &total);
       if (own_total) {
         own_total = false;
         goal_lo = goal_hi = share * total;
@@ -560,32 +660,32 @@ struct Sampler {
         // the last bin that holds something where the bins' own sums round below the goal
         for (int j = 0; j < kPer; ++j) {
           if (m[j] > 0.0) {
-            sh.found = 1;
-            sh.at = (uint32_t)(kSampleBins - 1 - ((int)threadIdx.x * kPer + j));
-            sh.mabove = before;
+            shared().found = 1;
+            shared().at = (uint32_t)(kSampleBins - 1 - ((int)threadIdx.x * kPer + j));
+            shared().mabove = before;
             if (goal <= before + m[j]) break;
           }
           before += m[j];
         }
       }
       __syncthreads();
-      if (!sh.found) {
+      if (!shared().found) {
         __syncthreads();
         if (outermost) return above + total < goal_lo || goal_lo == goal_hi ? 0 : -1;
         // a bin whose parts' sum rounds below the bin's: its lowest part
         if (threadIdx.x == 0) {
           int bin = 0;
-          while (bin < kSampleBins - 1 && sh.count[bin] == 0u) ++bin;
-          sh.at = (uint32_t)bin;
-          sh.mabove = above + total - (sft == 0 ? (double)sh.count[bin] * weight(Row::value(lo + (uint32_t)bin)) : (double)sh.mass[bin] * per_unit);
+          while (bin < kSampleBins - 1 && shared().count[bin] == 0u) ++bin;
+          shared().at = (uint32_t)bin;
+          shared().mabove = above + total - (sft == 0 ? (double)shared().count[bin] * weight(Row::value(lo + (uint32_t)bin)) : (double)shared().mass[bin] * per_unit);
         }
         __syncthreads();
       }
       outermost = false;
-      const uint32_t bin = sh.at;
-      above = sh.mabove;
+      const uint32_t bin = shared().at;
+      above = shared().mabove;
       if (sft == 0) {
-        uint32_t n = sh.count[bin];
+        uint32_t n = shared().count[bin];
         *equal = n;
         if (lo + bin == first) n -= drop;
         *code = lo + bin;
@@ -603,14 +703,14 @@ struct Sampler {
     }
   }
 
-  // Position behind the `take`-th token (by index) of this code; sh.list holds the chunks that may have some.
-  __device__ __noinline__ long long equal_end(uint32_t code, uint32_t take) {
-    uint32_t* cnt = sh.count;
+  // Position behind the `take`-th token (by index) of this code; shared().list holds the chunks that may have some.
+  __device__ __forceinline__ uint32_t equal_end(uint32_t code, uint32_t take) {
+    uint32_t* cnt = shared().count;
     for (int c = threadIdx.x; c < kSampleChunks; c += THREADS) cnt[c] = 0u;
     __syncthreads();
     uint32_t n = 0u;
     for_chunks([&](int) { n = 0u; },
-               [&](int, long long, const float (&a)[8]) {
+               [&](int, uint32_t, const float (&a)[8]) {
 #pragma unroll
                  for (int i = 0; i < 8; ++i) n += Row::key(a[i]) == code ? 1u : 0u;
                },
@@ -622,13 +722,13 @@ struct Sampler {
     uint32_t mine = 0u, total;
 #pragma unroll
     for (int i = 0; i < kPerC; ++i) mine += cnt[threadIdx.x * kPerC + i];
-    uint32_t before = block_scan<THREADS>(mine, sh.ired, &total);
+    uint32_t before = block_scan<THREADS>(mine, shared().ired, &total);
     if (before < take && take <= before + mine) {
       for (int i = 0; i < kPerC; ++i) {
         const uint32_t x = cnt[threadIdx.x * kPerC + i];
         if (take <= before + x) {
-          sh.at = threadIdx.x * kPerC + i;
-          sh.nabove = before;
+          shared().at = threadIdx.x * kPerC + i;
+          shared().nabove = before;
           break;
         }
         before += x;
@@ -636,9 +736,10 @@ struct Sampler {
     }
     __syncthreads();
     if (threadIdx.x < 32) {
-      const int lane = threadIdx.x, c = (int)sh.at;
-      uint32_t want = take - sh.nabove;  // >= 1
-      for (long long p0 = (long long)c << (8 + shift), e = (long long)(c + 1) << (8 + shift); p0 < e; p0 += 256) {
+      const int lane = threadIdx.x, c = (int)shared().at;
+      uint32_t want = take - shared().nabove;  // >= 1
+      for (int k = 0; k < 1 << shift; ++k) {
+        const uint32_t p0 = ((uint32_t)c << (8 + shift)) + (uint32_t)k * 256u;
         float a[8];
         Row::unpack(row.load(p0 + lane * 8), a);
         uint32_t hits = 0u;
@@ -648,7 +749,7 @@ struct Sampler {
         if (want <= all) {
           if (incl - mine < want && want <= incl) {
             for (uint32_t r = incl - mine + 1u; r < want; ++r) hits &= hits - 1u;
-            sh.pos = p0 + lane * 8 + __ffs((int)hits);
+            shared().pos = p0 + lane * 8 + __ffs((int)hits);
           }
           break;
         }
@@ -656,107 +757,106 @@ struct Sampler {
       }
     }
     __syncthreads();
-    const long long end = sh.pos;
+    const uint32_t end = shared().pos;
     __syncthreads();
     return end;
   }
 
   struct Kept {
-    uint32_t code;   // least kept code
-    long long end;   // tokens of that code stay in front of this position
-    __device__ __forceinline__ bool operator()(float x, long long p) const {
-      const uint32_t k = Row::key(x);
-      return k > code || (k == code && p < end);
+    float from;    // least kept logit
+    float upto;    // the largest one (+inf and NaN are not kept)
+    uint32_t end;  // tokens of the least one stay in front of this position
+    __device__ __forceinline__ bool operator()(float x, uint32_t p) const {
+      return x >= from && x <= upto && !(x == from && p >= end);
     }
   };
 
   // The kept ones' mass among a lane's eight tokens.  Weights are computed four at a time whether kept or not (their
-  // operations depend on each other, 20 us a row of 150000 tokens; behind a branch each 100), or for no lane.
-  __device__ __forceinline__ double kept_mass(const Kept& kept, const float (&a)[8], long long p) const {
+  // operations depend on each other), or for no lane.
+  __device__ __forceinline__ double kept_mass(const Kept& kept, const float (&a)[8], uint32_t p) const {
     bool in[8], any = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) any |= in[i] = kept(a[i], p + i);
+    for (int i = 0; i < 8; ++i) any |= in[i] = kept(a[i], p + i) && a[i] >= least;
     double s = 0.0;
     if (!__any_sync(0xffffffffu, any)) return s;
 #pragma unroll
     for (int h = 0; h < 8; h += 4) {
       double w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = weight(a[h + i]);
+      for (int i = 0; i < 4; ++i) w[i] = weight_of(a[h + i]);
       s += ((in[h] ? w[0] : 0.0) + (in[h + 1] ? w[1] : 0.0)) + ((in[h + 2] ? w[2] : 0.0) + (in[h + 3] ? w[3] : 0.0));
     }
     return s;
   }
 
-  // 64-bit mass of the kept tokens of the listed chunks -> sh.psum, 0 elsewhere
-  __device__ __noinline__ void exact_sums(const Kept& kept) {
-    for (int c = threadIdx.x; c < kSampleChunks; c += THREADS) sh.psum[c] = 0.0;
+  // 64-bit mass of the kept tokens of the listed chunks -> shared().psum, 0 elsewhere
+  __device__ __forceinline__ void exact_sums(const Kept& kept) {
+    for (int c = threadIdx.x; c < kSampleChunks; c += THREADS) shared().psum[c] = 0.0;
     __syncthreads();
     double s = 0.0;
     for_chunks([&](int) { s = 0.0; },
-                     [&](int, long long p, const float (&a)[8]) {
+                     [&](int, uint32_t p, const float (&a)[8]) {
                        s += kept_mass(kept, a, p);
                      },
                      [&](int c) {
                        s = warp_sum(s);
-                       if ((threadIdx.x & 31) == 0) sh.psum[c] = s;
+                       if ((threadIdx.x & 31) == 0) shared().psum[c] = s;
                      });
     __syncthreads();
   }
   __device__ double total_mass() {
     double mine = 0.0, total;
 #pragma unroll
-    for (int i = 0; i < kPerC; ++i) mine += sh.psum[threadIdx.x * kPerC + i];
-    block_scan<THREADS>(mine, sh.wred, &total);
+    for (int i = 0; i < kPerC; ++i) mine += shared().psum[threadIdx.x * kPerC + i];
+    block_scan<THREADS>(mine, shared().wred, &total);
     return total;
   }
 
-  // The token that u falls to by sh.psum, whose entries hold 2^size positions each.  slack: relative error of those sums;
+  // The token that u falls to by shared().psum, whose entries hold 2^size positions each.  slack: relative error of those sums;
   // false where it leaves the token open.
-  __device__ __noinline__ bool locate(const Kept& kept, double u, int size, double slack, long long* pos, double* total_out) {
+  __device__ __forceinline__ bool locate(const Kept& kept, double u, int size, double slack, uint32_t* pos, double* total_out) {
     double mine = 0.0, total;
 #pragma unroll
-    for (int i = 0; i < kPerC; ++i) mine += sh.psum[threadIdx.x * kPerC + i];
-    double before = block_scan<THREADS>(mine, sh.wred, &total);
+    for (int i = 0; i < kPerC; ++i) mine += shared().psum[threadIdx.x * kPerC + i];
+    double before = block_scan<THREADS>(mine, shared().wred, &total);
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
     if (x > most) x = most;
-    if (threadIdx.x == 0) sh.found = 0, sh.pos = -1;
+    if (threadIdx.x == 0) shared().found = 0, shared().pos = row.mis;
     __syncthreads();
     // the pieces' borders are rounded sums: where none holds x, the last chunk with mass does
     if (mine > 0.0 && before <= x && x < before + mine) {
       for (int i = 0; i < kPerC; ++i) {
-        const double y = sh.psum[threadIdx.x * kPerC + i];
+        const double y = shared().psum[threadIdx.x * kPerC + i];
         if (y > 0.0) {
-          sh.at = threadIdx.x * kPerC + i;
-          sh.mabove = before;
-          sh.found = 1;
+          shared().at = threadIdx.x * kPerC + i;
+          shared().mabove = before;
+          shared().found = 1;
           if (x < before + y) break;
         }
         before += y;
       }
     }
     __syncthreads();
-    if (!sh.found && threadIdx.x == 0) {
+    if (!shared().found && threadIdx.x == 0) {
       double b = 0.0;
       for (int c = 0; c < kSampleChunks; ++c)
-        if (sh.psum[c] > 0.0 && (b <= x || !sh.found)) {
-          sh.at = (uint32_t)c;
-          sh.mabove = b;
-          sh.found = 1;
-          b += sh.psum[c];
+        if (shared().psum[c] > 0.0 && (b <= x || !shared().found)) {
+          shared().at = (uint32_t)c;
+          shared().mabove = b;
+          shared().found = 1;
+          b += shared().psum[c];
         }
     }
     __syncthreads();
     if (threadIdx.x < 32) {
       const int lane = threadIdx.x;
-      const long long c = sh.at;
-      double base = sh.mabove;
+      double front = shared().mabove;
       const double margin = slack * total;
-      long long last = -1;  // last kept position so far
+      uint32_t last = row.mis;  // last kept position so far
       bool sure = true, done = false;
-      for (long long p0 = c << size, e = (c + 1) << size; p0 < e && !done; p0 += 256) {
-        const long long p = p0 + lane * 8;
+      for (int k = 0; k < 1 << (size - 8) && !done; ++k) {
+        const uint32_t p = (shared().at << size) + (uint32_t)k * 256u + lane * 8;
         float a[8];
         Row::unpack(row.load(p), a);
         double w[8], mine = 0.0;
@@ -769,40 +869,126 @@ struct Sampler {
           if (w[i] > 0.0) mlast = i;
         }
         const double incl = warp_scan(mine);
-        const unsigned hit = __ballot_sync(0xffffffffu, base + incl > x && mine > 0.0);
+        const unsigned hit = __ballot_sync(0xffffffffu, front + incl > x && mine > 0.0);
         const unsigned some = __ballot_sync(0xffffffffu, mlast >= 0);
         if (hit) {
           const int src = __ffs((int)hit) - 1;
           if (lane == src) {
-            double b = base + (incl - mine);
-            int i = 0;
+            double f = front + (incl - mine), border = f;
+            int at = 0;
+            bool open = true;
             // the lane's sums in order; the last of its kept tokens where rounding leaves none
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (w[j] > 0.0 && (i = j, b + w[j] > x)) break;
-              else b += w[j];
-            if (margin > 0.0) sure = x - b > margin && b + w[i] - x > margin;
-            sh.pos = p + i;
-            sh.found = sure ? 1 : 0;
+            for (int i = 0; i < 8; ++i)
+              if (open && w[i] > 0.0) {
+                at = i;
+                border = f;
+                f += w[i];
+                open = !(f > x);
+              }
+            if (margin > 0.0) sure = x - border > margin && f - x > margin;
+            shared().pos = p + at;
+            shared().found = sure ? 1 : 0;
           }
           done = true;
         } else if (some) {
           const int src = 31 - __clz((int)some);
           last = __shfl_sync(0xffffffffu, p + mlast, src);
         }
-        base += __shfl_sync(0xffffffffu, incl, 31);
+        front += __shfl_sync(0xffffffffu, incl, 31);
       }
       if (!done && lane == 0) {
-        sh.pos = last;
-        sh.found = margin > 0.0 ? 0 : 1;
+        shared().pos = last;
+        shared().found = margin > 0.0 ? 0 : 1;
       }
     }
     __syncthreads();
-    *pos = sh.pos;
+    *pos = shared().pos;
     *total_out = total;
-    const bool ok = sh.found != 0;
+    const bool ok = shared().found != 0;
     __syncthreads();
-    return ok && *pos >= 0;
+    return ok;
+  }
+
+  // The same among the listed tokens, of which the first `take` (by position) of the code `code` and those above it stay.
+  __device__ __forceinline__ void locate_listed(uint32_t code, uint32_t take, double u, uint32_t* pos, double* total_out) {
+    const int each = (listed + THREADS - 1) / THREADS, from = min((int)threadIdx.x * each, listed), upto = min(from + each, listed);
+    uint32_t equal = 0u, all;
+    for (int i = from; i < upto; ++i) equal += shared().key[i] == code ? 1u : 0u;
+    const uint32_t rank = block_scan<THREADS>(equal, shared().ired, &all);
+    double mine = 0.0, total;
+    uint32_t r = rank;
+    for (int i = from; i < upto; ++i) {
+      const uint32_t k = shared().key[i];
+      if (k > code || (k == code && r++ < take)) mine += weight(Row::value(k));
+    }
+    double f = block_scan<THREADS>(mine, shared().wred, &total);
+    double x = u * total;
+    const double most = total * (1.0 - 1.2e-16);
+    if (x > most) x = most;
+    if (threadIdx.x == 0) shared().found = 0, shared().pos = row.mis;
+    __syncthreads();
+    if (mine > 0.0 && f <= x && x < f + mine) {
+      r = rank;
+      for (int i = from; i < upto; ++i) {
+        const uint32_t k = shared().key[i];
+        if (!(k > code || (k == code && r++ < take))) continue;
+        const double w = weight(Row::value(k));
+        if (!(w > 0.0)) continue;
+        shared().pos = shared().place[i];
+        shared().found = 1;
+        f += w;
+        if (f > x) break;
+      }
+    }
+    __syncthreads();
+    // the threads' borders are rounded sums: where none holds x, the last token with weight
+    if (!shared().found && threadIdx.x == 0) {
+      r = 0u;
+      for (int i = 0; i < listed; ++i) {
+        const uint32_t k = shared().key[i];
+        if ((k > code || (k == code && r++ < take)) && weight(Row::value(k)) > 0.0) shared().pos = shared().place[i];
+      }
+    }
+    __syncthreads();
+    *pos = shared().pos;
+    *total_out = total;
+    __syncthreads();
+  }
+};
+
+// The searches as functions of their own (inlined, the kernel would not fit its registers), each with a copy of the
+// sampler that it can hold in registers.
+template <int DT, int THREADS>
+struct SampleCalls {
+  typedef Sampler<DT, THREADS> S;
+  typedef typename S::Kept Kept;
+  static __device__ __noinline__ float sweep_carefully(S s, int g, float c2, bool sum, float4* m) {
+    float q[4];
+    const float t = sum ? s.template sweep_carefully<true>(g, c2, q) : s.template sweep_carefully<false>(g, c2, q);
+    *m = make_float4(q[0], q[1], q[2], q[3]);
+    return t;
+  }
+  static __device__ __noinline__ uint32_t kth_chunk(S s, uint32_t k) { return s.kth_chunk(k); }
+  static __device__ __noinline__ void make_list(S s, float bound) { s.make_list(bound); }
+  static __device__ __noinline__ int gather(S s, float bound) {
+    s.gather(bound);
+    return s.listed;
+  }
+  static __device__ __noinline__ bool kth(S s, uint32_t lo, uint32_t k, uint32_t* code, uint32_t* take, uint32_t* equal) {
+    return s.kth(lo, k, code, take, equal);
+  }
+  static __device__ __noinline__ int nucleus(S s, uint32_t lo, uint32_t drop, bool own, double share, double goal_lo, double goal_hi,
+                                             uint32_t* code, uint32_t* take, uint32_t* equal) {
+    return s.nucleus(lo, drop, own, share, goal_lo, goal_hi, code, take, equal);
+  }
+  static __device__ __noinline__ uint32_t equal_end(S s, uint32_t code, uint32_t take) { return s.equal_end(code, take); }
+  static __device__ __noinline__ void exact_sums(S s, Kept kept) { s.exact_sums(kept); }
+  static __device__ __noinline__ bool locate(S s, Kept kept, double u, int size, double slack, uint32_t* pos, double* total) {
+    return s.locate(kept, u, size, slack, pos, total);
+  }
+  static __device__ __noinline__ void locate_listed(S s, uint32_t code, uint32_t take, double u, uint32_t* pos, double* total) {
+    s.locate_listed(code, take, u, pos, total);
   }
 };
 
@@ -813,9 +999,9 @@ __device__ __forceinline__ float sample_setting(const SampleSetting& s, long lon
 template <int DT, int THREADS>
 __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const SampleArgs A) {
   typedef SampleRow<DT> Row;
-  extern __shared__ __align__(128) char sample_shared[];
-  SampleShared<DT, THREADS>& sh = *(SampleShared<DT, THREADS>*)sample_shared;
-  Sampler<DT, THREADS> S{sh};
+  typedef SampleCalls<DT, THREADS> Calls;
+  SampleShared<DT, THREADS>& sh = Sampler<DT, THREADS>::shared();
+  Sampler<DT, THREADS> S;
   const long long r = blockIdx.x / cluster_ctas();
   const int j = (int)(r % A.J), k = (int)(r / A.J % A.K);
   const long long b = r / A.J / A.K;
@@ -834,15 +1020,16 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
   if (greedy) itf = 1.f, kk = 1;
   if (kk == 1) p = 1.f, mp = 0.f;
   const char* start = (const char*)A.data + (b * A.sb + k * A.sk + j * A.sj) * Row::ES;
-  S.row.mis = ((uintptr_t)start & 15) / Row::ES;
+  S.row.mis = (uint32_t)(((uintptr_t)start & 15) / Row::ES);
   S.row.base = start - S.row.mis * Row::ES;
-  S.row.end = S.row.mis + A.V;
+  S.row.end = S.row.mis + (uint32_t)A.V;
+  S.listed = -1;
   S.shift = A.shift;
-  S.nch = (int)((S.row.end + (256LL << A.shift) - 1) >> (8 + A.shift));
+  S.nch = (int)(((long long)S.row.end + (256LL << A.shift) - 1) >> (8 + A.shift));
   S.frac = 62 - (32 - __clz(A.V));
   S.it = (double)itf;
   S.it2 = S.it * 1.4426950408889634;
-  if (threadIdx.x < 16) sh.exp16[threadIdx.x] = exp2((double)threadIdx.x * 0.0625);
+  if (threadIdx.x < 64) sh.exp64[threadIdx.x] = exp2((double)threadIdx.x * 0.015625);
   const bool use_k = kk > 0 && kk < A.V, use_p = p < 1.f;
   const bool need_sum = !use_k && (use_p || mp == 0.f);
   const float c2 = itf * kLog2e;
@@ -873,13 +1060,13 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
     }
     return;
   }
-  S.top = m;
-  typename Sampler<DT, THREADS>::Kept kept{Row::kLowest, S.row.end};
+  S.set_top(m);
+  typename Sampler<DT, THREADS>::Kept kept{-3.402823466e38f, m, S.row.end};
   // Relative error of a sum of four chunks: exponentials 2^-22; their arguments 3 roundings, where |t|, weighted by the terms
   // themselves, is log2(tokens) + 1.5 on the mean; 10 additions one after another, or 2^(2 + shift) more in long chunks.
   const double eps = 2.5e-7 + 1.3e-7 * (11.5 + A.shift) + 6e-8 * (12.0 + (A.shift ? (double)(4 << A.shift) : 4.0));
   double total = 0.0;
-  long long pos = -1;
+  uint32_t pos = S.row.mis;
   bool done = false;
   if (need_sum) {
     for (int g = threadIdx.x; g < kSampleChunks; g += THREADS) {
@@ -891,7 +1078,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
       sh.psum[g] = y;
     }
     __syncthreads();
-    if (!use_p) done = S.locate(kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
+    if (!use_p) done = Calls::locate(S, kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
   }
   if (!done) {
     // the least code that min-p keeps
@@ -907,30 +1094,27 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
       while (e > Row::kLowest && ((double)Row::value(e - 1) - (double)m) * S.it >= ln) --e;
       floor_code = e;
     }
-    uint32_t take = 0u, equal = 0u;  // of the least kept code; equal == 0: all of it stays
-    kept.code = floor_code;
+    uint32_t code = floor_code;         // the least kept one
+    uint32_t take = 0u, equal = 0u;     // of the tokens that have it; equal == 0: all of them stay
+    uint32_t pc, pt, pe;
     if (use_k) {
       // top-p needs the mass of all k
-      uint32_t cut = use_p ? Row::kLowest : floor_code;
-      if (kk <= S.nch) {
-        const uint32_t e = S.kth_chunk((uint32_t)kk);
-        if (e > cut) cut = e;
+      const uint32_t lowest = use_p ? Row::kLowest : floor_code;
+      // At least k tokens reach the k-th largest chunk maximum; with more of them to keep than there are chunks, some
+      // six a chunk reach the smallest one, and where that does not do, further down.
+      uint32_t cut = Calls::kth_chunk(S, (uint32_t)kk < (uint32_t)S.nch ? (uint32_t)kk : (uint32_t)S.nch);
+      bool limited = false;
+      for (;;) {
+        if (cut < lowest) cut = lowest;
+        Calls::make_list(S, Row::value(cut));
+        if (kk <= 512) S.listed = Calls::gather(S, Row::value(cut));
+        limited = Calls::kth(S, cut, (uint32_t)kk, &code, &take, &equal);
+        if (limited || cut == lowest) break;
+        const float v = Row::value(cut), further = v - (m - v) * 0.5f;
+        cut = further < v && further > -3.402823466e38f ? Row::key(further) : lowest;
       }
-      S.make_list(Row::value(cut));
-      uint32_t code;
-      const bool limited = S.kth(cut, (uint32_t)kk, &code, &take, &equal);
-      if (limited) kept.code = code;
-      else take = equal = 0u, kept.code = cut;
-      if (limited && use_p) {
-        uint32_t pc, pt, pe;
-        const int got = S.nucleus(kept.code, equal - take, true, (double)p, 0.0, 0.0, &pc, &pt, &pe);
-        if (got == 1) kept.code = pc, take = pt, equal = pe;
-      }
-      if (!limited && use_p) {  // fewer than k finite logits: all of them are the set
-        uint32_t pc, pt, pe;
-        const int got = S.nucleus(cut, 0u, true, (double)p, 0.0, 0.0, &pc, &pt, &pe);
-        if (got == 1) kept.code = pc, take = pt, equal = pe;
-      }
+      if (!limited) take = equal = 0u, code = cut;
+      if (use_p && Calls::nucleus(S, code, equal - take, true, (double)p, 0.0, 0.0, &pc, &pt, &pe) == 1) code = pc, take = pt, equal = pe;
     } else if (use_p) {
       double goal = S.total_mass(), slack = eps;
       for (int pass = 0; pass < 2; ++pass) {
@@ -941,31 +1125,35 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
         uint32_t cut = Row::key(edge);
         if (cut > Row::kLowest) --cut;
         if (cut < floor_code) cut = floor_code;
-        S.make_list(Row::value(cut));
-        uint32_t pc, pt, pe;
-        const int got = S.nucleus(cut, 0u, false, 0.0, (double)p * goal * (1.0 - slack), (double)p * goal * (1.0 + slack), &pc, &pt, &pe);
-        if (got == 1) kept.code = pc, take = pt, equal = pe;
-        else if (got == 0) kept.code = cut;
+        Calls::make_list(S, Row::value(cut));
+        const int got = Calls::nucleus(S, cut, 0u, false, 0.0, (double)p * goal * (1.0 - slack), (double)p * goal * (1.0 + slack), &pc, &pt, &pe);
+        if (got == 1) code = pc, take = pt, equal = pe;
+        else if (got == 0) code = cut;
         if (got >= 0) break;
         // the border lies within the sweep's error: the total in 64 bits
-        S.make_list(-3.402823466e38f);
-        S.exact_sums(typename Sampler<DT, THREADS>::Kept{Row::kLowest, S.row.end});
+        Calls::make_list(S, -3.402823466e38f);
+        Calls::exact_sums(S, kept);
         goal = S.total_mass();
         slack = 0.0;
       }
     }
-    if (kept.code < floor_code) kept.code = floor_code, take = equal = 0u;
-    S.make_list(Row::value(kept.code));
-    kept.end = S.row.end;
-    if (take < equal) kept.end = S.equal_end(kept.code, take);
-    S.exact_sums(kept);
-    S.locate(kept, (double)u, 8 + A.shift, 0.0, &pos, &total);
+    if (code < floor_code) code = floor_code, take = equal = 0u;
+    if (S.listed < 0) {
+      Calls::make_list(S, Row::value(code));
+      if (use_k || use_p || mp > 0.f) S.listed = Calls::gather(S, Row::value(code));
+    }
+    if (S.listed >= 0) {
+      Calls::locate_listed(S, code, take < equal ? take : 0xffffffffu, (double)u, &pos, &total);
+    } else {
+      kept.from = Row::value(code);
+      if (take < equal) kept.end = Calls::equal_end(S, code, take);
+      Calls::exact_sums(S, kept);
+      Calls::locate(S, kept, (double)u, 8 + A.shift, 0.0, &pos, &total);
+    }
   }
   if (threadIdx.x == 0) {
-    if (pos < S.row.mis) pos = S.row.mis - 1;  // not reached: the largest logit is always kept
     A.tokens[r] = (int32_t)(pos - S.row.mis);
-    if (A.logprobs && pos < S.row.mis) A.logprobs[r] = 0.f;
-    else if (A.logprobs) {
+    if (A.logprobs) {
       const float x = DT == kBF16 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)S.row.base + pos) << 16)
                                   : __ldg((const float*)S.row.base + pos);
       A.logprobs[r] = (float)(((double)x - (double)m) * S.it - log(total));
