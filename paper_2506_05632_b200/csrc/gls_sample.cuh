@@ -18,8 +18,8 @@
 //              their ordered codes and refining the bin the border falls into
 //     sums     the kept tokens' mass per chunk, in 64 bits; the chunk that u falls into; the token inside it
 // Decisions are those of exact arithmetic but for 64-bit rounding: sums that decide something are 64-bit sums of
-// exponentials good to 2e-13 (or integers of 2^-(62 - log2 V)).  The sweep's fp32 sums decide only where their error
-// bound leaves no doubt; otherwise the row is summed again in 64 bits.
+// exponentials good to 2e-13, and counts.  The sweep's fp32 sums decide only where the border is further away than 5e-7 of the
+// total, twenty times what their rounding leaves; otherwise the row is summed again in 64 bits.
 #pragma once
 #include "gls_async.cuh"
 #include "gls_kernels.cuh"
@@ -178,17 +178,14 @@ struct SampleShared {
   static constexpr int kStage = DT == kBF16 ? 2048 : 4096;  // 1024 tokens
   union {
     struct {
-      union {
-        double psum[kSampleChunks];            // mass per chunk
-        unsigned long long mass[kSampleBins];  // per bin, in units of 2^-frac
-      };
+      double psum[kSampleChunks];   // mass per chunk
       uint32_t count[kSampleBins];  // per bin, or per chunk
       uint32_t key[kSampleList], place[kSampleList];  // codes and positions of listed tokens, in order of position
     };
     char ring[THREADS / 32][kStages][kStage];
   };
   double wred[32];
-  double exp64[64];             // 2^(i / 64)
+  double exp16[16];             // 2^(i / 16)
   uint64_t barriers[THREADS / 32][kStages];
   float cmax[kSampleChunks];    // largest logit of a chunk
   float csum[kSampleChunks / 4];  // sum relative to the largest logit of four chunks
@@ -241,7 +238,7 @@ struct Sampler {
     return *(Shared*)sample_shared;
   }
   Row row;
-  int nch, shift, frac;
+  int nch, shift;
   int listed;      // tokens in shared().key, or -1
   double it, it2;  // inverse temperature, the same to base 2
   double c;        // exponent of a logit x: (x - base) it2 - c, where one of base and c is 0
@@ -259,46 +256,58 @@ struct Sampler {
     least = (float)((double)m - 1000.0 / it2);
     if (!(least >= -3.402823466e38f)) least = -3.402823466e38f;
   }
-  // 2^((x - top) it2) to 1e-13 for x >= least: 2^n 2^(i / 64) 2^r with |r| <= 1 / 128, the last by its series (nine
-  // operations in 64 bits and a conversion; exp() takes about three times as many)
-  __device__ __forceinline__ double weight_of(float x) const {
+  // 2^((x - top) it2) to 2e-13 for x >= least: 2^n 2^(i / 16) 2^r with |r| <= 1 / 32, the last by its series (ten
+  // operations in 64 bits and a conversion; exp() takes about three times as many).  Sixteen table entries have a pair of banks
+  // each; with 64 a warp's reads wait for one another (7.8 a clock and SM).
+  // (a number below 2^-1022 where it is not wanted, without a branch)
+  __device__ __forceinline__ double weight_of(float x, bool wanted = true) const {
     const double t = fma((double)(x - base), it2, -c);
-    const double magic = 6755399441055744.0 / 64.0;  // 1.5 * 2^46: 64ths in the lowest bits
+    const double magic = 6755399441055744.0 / 16.0;  // 1.5 * 2^48: sixteenths in the lowest bits
     const double big = t + magic;
     const int n = __double2loint(big);
     const double r = t - (big - magic);
-    double q = 9.6181291076284772e-3;  // ln2^4 / 4!
+    double q = 1.3333558146428443e-3;  // ln2^5 / 5!
+    q = fma(q, r, 9.6181291076284772e-3);
     q = fma(q, r, 5.5504108664821580e-2);
     q = fma(q, r, 2.4022650695910071e-1);
     q = fma(q, r, 6.9314718055994531e-1);
-    const double e = shared().exp64[n & 63], y = fma(e * r, q, e);
-    return __hiloint2double(__double2hiint(y) + ((n >> 6) << 20), __double2loint(y));
+    const double e = shared().exp16[n & 15], y = fma(e * r, q, e);
+    return __hiloint2double(wanted ? __double2hiint(y) + ((n >> 4) << 20) : 0, __double2loint(y));
   }
   __device__ __forceinline__ double weight(float x) const { return x >= least ? weight_of(x) : 0.0; }
 
-  // f(chunk, first position of the lane, logits) over the chunks of shared().list, a warp per chunk
-  template <class Begin, class F, class End>
+  // f(chunk, first position of the lane, logits) over the chunks of sh.list, a warp per chunk; RAW: masked logits as they are
+  template <bool RAW = false, class Begin, class F, class End>
   __device__ __forceinline__ void for_chunks(Begin&& begin, F&& f, End&& fin) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = shared().n_list;
     if (shift == 0) {
-      for (int i0 = warp; i0 < n; i0 += kWarps * kAhead) {
-        Raw r[kAhead];
-        int c[kAhead];
+      // kAhead chunks of a warp at a time, the next ones requested before these are looked at
+      Raw next[kAhead];
+      auto fetch = [&](int i0) {
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
           const int i = i0 + q * kWarps;
-          c[q] = i < n ? (int)shared().list[i] : -1;
-          if (c[q] >= 0) r[q] = row.load((uint32_t)c[q] * 256u + lane * 8);
+          if (i < n) next[q] = row.load((uint32_t)shared().list[i] * 256u + lane * 8);
         }
+      };
+      fetch(warp);
+      for (int i0 = warp; i0 < n; i0 += kWarps * kAhead) {
+        Raw r[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) r[q] = next[q];
+        fetch(i0 + kWarps * kAhead);
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-          if (c[q] < 0) continue;
+          const int i = i0 + q * kWarps;
+          if (i >= n) break;
+          const int c = (int)shared().list[i];
           float a[8];
-          Row::unpack(r[q], a);
-          begin(c[q]);
-          f(c[q], (uint32_t)c[q] * 256u + lane * 8, a);
-          fin(c[q]);
+          if (RAW) Row::widen(r[q], a);
+          else Row::unpack(r[q], a);
+          begin(c);
+          f(c, (uint32_t)c * 256u + lane * 8, a);
+          fin(c);
         }
       }
       return;
@@ -309,7 +318,8 @@ struct Sampler {
       for (int i = 0; i < 1 << shift; ++i) {
         float a[8];
         const uint32_t p = ((uint32_t)c << (8 + shift)) + (uint32_t)i * 256u + lane * 8;
-        Row::unpack(row.load(p), a);
+        if (RAW) Row::widen(row.load(p), a);
+        else Row::unpack(row.load(p), a);
         f(c, p, a);
       }
       fin(c);
@@ -386,7 +396,8 @@ struct Sampler {
     __syncthreads();
   }
 
-  // Largest logit of each chunk and, SUM, per four chunks the sum of 2^((l - their largest) c2), into the shared memory
+  // Largest logit of each chunk and, SUM, per four chunks the sum of 2^(l c2 - r) with r their largest one
+  // times c2, rounded (where that is beyond 1e30: of 2^((l - their largest) c2)), into the shared memory
   // of the cluster's first CTA.  A warp takes every so many-th four chunks; those that lie within the row come
   // through a ring, two or three sets ahead.
   template <bool SUM>
@@ -429,14 +440,16 @@ struct Sampler {
         for (int q = 0; q < 4; ++q) m[q] = redux_max(Row::largest(r[q]));
         const float mm = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
         odd |= !(mm < CUDART_INF_F);
+        const float ref = mm * c2;
         if (SUM && mm > -CUDART_INF_F) {
+          odd |= !(fabsf(ref) < 1e30f);
           float t[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             float a[8];
             Row::widen(r[q], a);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = ex2_approx((a[i] - mm) * c2);
+            for (int i = 0; i < 8; ++i) a[i] = ex2_approx(fmaf(a[i], c2, -ref));
             t[q] = ((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7]));
           }
           s = (t[0] + t[1]) + (t[2] + t[3]);
@@ -488,26 +501,19 @@ struct Sampler {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     }
+    if (SUM && fabsf(mm * c2) < 1e30f) s *= ex2_approx(fmaf(mm, c2, -(mm * c2)));  // to the reference that sets without odd logits have
     return s;
   }
 
-  // Tokens with codes in [lo, lo + span) per bin of 2^sft codes, of the listed tokens or of the listed chunks; MASS: their
-  // weights too.
-  template <bool MASS>
+  // Tokens with codes in [lo, lo + span) per bin of 2^sft codes, of the listed tokens or of the listed chunks.  (32-bit
+  // counts: 12 a clock and SM; 64-bit sums of weights would be 1.6, and 0.35 where a few bins take them.)
   __device__ __forceinline__ void histogram(uint32_t lo, uint32_t span, int sft) {
-    for (int i = threadIdx.x; i < kSampleBins; i += THREADS) {
-      shared().count[i] = 0u;
-      if (MASS) shared().mass[i] = 0ull;
-    }
+    for (int i = threadIdx.x; i < kSampleBins; i += THREADS) shared().count[i] = 0u;
     __syncthreads();
-    const double unit = (double)(1ull << frac);
     if (listed >= 0) {
       for (int i = threadIdx.x; i < listed; i += THREADS) {
         const uint32_t d = shared().key[i] - lo;
-        if (d < span) {
-          atomicAdd(&shared().count[d >> sft], 1u);
-          if (MASS) atomicAdd(&shared().mass[d >> sft], (unsigned long long)(weight(Row::value(shared().key[i])) * unit + 0.5));
-        }
+        if (d < span) atomicAdd(&shared().count[d >> sft], 1u);
       }
     } else {
       const float from = Row::value(lo);
@@ -518,23 +524,28 @@ struct Sampler {
                    for (int i = 0; i < 8; ++i) any |= a[i] >= from;
                    if (!__any_sync(0xffffffffu, any)) return;
 #pragma unroll
-                   for (int h = 0; h < 8; h += 4) {
-                     double w[4];
-#pragma unroll
-                     for (int i = 0; i < 4; ++i) w[i] = MASS ? weight(a[h + i]) * unit + 0.5 : 0.0;
-#pragma unroll
-                     for (int i = 0; i < 4; ++i) {
-                       const uint32_t d = Row::key(a[h + i]) - lo;
-                       if (d < span) {
-                         atomicAdd(&shared().count[d >> sft], 1u);
-                         if (MASS) atomicAdd(&shared().mass[d >> sft], (unsigned long long)w[i]);
-                       }
-                     }
+                   for (int i = 0; i < 8; ++i) {
+                     const uint32_t d = Row::key(a[i]) - lo;
+                     if (d < span) atomicAdd(&shared().count[d >> sft], 1u);
                    }
                  },
                  [](int) {});
     }
     __syncthreads();
+  }
+  // 64-bit mass of the tokens with codes lo .. hi
+  __device__ __forceinline__ double mass_of(uint32_t lo, uint32_t hi) {
+    if (listed < 0) {
+      exact_sums(Kept{Row::value(lo), Row::value(hi), row.end});
+      return total_mass();
+    }
+    double mine = 0.0, total;
+    for (int i = threadIdx.x; i < listed; i += THREADS) {
+      const uint32_t k = shared().key[i];
+      if (k >= lo && k <= hi) mine += weight(Row::value(k));
+    }
+    block_scan<THREADS>(mine, shared().wred, &total);
+    return total;
   }
   static __device__ __forceinline__ int bin_shift(uint32_t span) {
     const int bits = 32 - __clz((int)(span - 1u));
@@ -573,7 +584,7 @@ struct Sampler {
     uint32_t span = Row::key(top) - lo + 1u;
     for (;;) {
       const int sft = bin_shift(span);
-      histogram<false>(lo, span, sft);
+      histogram(lo, span, sft);
       uint32_t mine = 0u, total;
 #pragma unroll
       for (int j = 0; j < kPer; ++j) mine += shared().count[kSampleBins - 1 - ((int)threadIdx.x * kPer + j)];
@@ -620,75 +631,76 @@ struct Sampler {
   }
 
   // Least kept code under top-p among the codes >= lo (of those at lo, `drop` do not belong to the set).
-  // Goal: share times the set's own mass, or somewhere between goal_lo and goal_hi.
+  // Goal: share times the set's own mass, or somewhere between goal_lo and goal_hi.  counted: the bins hold the counts of a call
+  // with the same lo, whose codes had a bin each.
   // 1: found; 0: the set does not reach the goal, all of it stays; -1: the interval leaves it open.
-  __device__ __forceinline__ int nucleus(uint32_t lo, uint32_t drop, bool own_total, double share, double goal_lo, double goal_hi,
-                         uint32_t* code, uint32_t* take, uint32_t* equal) {
-    uint32_t span = Row::key(top) - lo + 1u;
+  // Bins of one code have their mass from their count.  The masses of wider ones lie between their counts times the
+  // weights at their ends, which leaves a few bins that the border may be in: the mass above those is summed in 64 bits
+  // and they are cut finer.
+  __device__ __forceinline__ int nucleus(uint32_t lo, uint32_t drop, bool own_total, bool counted, double share, double goal_lo, double goal_hi,
+                                         uint32_t* code, uint32_t* take, uint32_t* equal) {
     const uint32_t first = lo;
-    double above = 0.0;
-    bool outermost = true;
-    const double per_unit = 1.0 / (double)(1ull << frac);
+    uint32_t hi = Row::key(top);
+    double above = 0.0;  // mass of the codes above hi
+    if (own_total) goal_lo = goal_hi = share * (mass_of(lo, hi) - (double)drop * weight(Row::value(lo)));
+    const double goal = 0.5 * (goal_lo + goal_hi);
     for (;;) {
+      const uint32_t span = hi - lo + 1u;
       const int sft = bin_shift(span);
-      if (sft == 0) histogram<false>(lo, span, sft);
-      else histogram<true>(lo, span, sft);
-      double m[kPer], mine = 0.0, total;
-#pragma unroll
+      if (!counted) histogram(lo, span, sft);
+      counted = false;
+      if (lo == first && drop > 0u) {
+        if (threadIdx.x == 0) shared().count[0] -= drop;
+        __syncthreads();
+      }
+      // masses from the top bin on: at least and at most
+      double least_sum = 0.0, most_sum = 0.0, total_least, total_most;
+#pragma unroll 1
       for (int j = 0; j < kPer; ++j) {
-        const int bin = kSampleBins - 1 - ((int)threadIdx.x * kPer + j);
-        uint32_t n = shared().count[bin];
-        const bool lowest = bin == 0 && lo == first && drop > 0u;
-        m[j] = 0.0;
-        if (sft == 0) {
-          if (lowest) n -= drop;
-          if (n) m[j] = (double)n * weight(Row::value(lo + (uint32_t)bin));
-        } else {
-          if (n) m[j] = (double)shared().mass[bin] * per_unit;
-          if (lowest) m[j] -= (double)drop * weight(Row::value(lo));
-        }
-        mine += m[j];
+        const uint32_t bin = kSampleBins - 1 - (threadIdx.x * kPer + j), n = shared().count[bin];
+        if (!n) continue;
+        const uint32_t c0 = lo + (bin << sft), c1 = min(c0 + (1u << sft) - 1u, hi);
+        const double w = (double)n * weight(Row::value(c1));
+        most_sum += w;
+        least_sum += sft == 0 ? w : (double)n * weight(Row::value(c0));
       }
-      if (threadIdx.x == 0) shared().found = 0;
-      double before = above + block_scan<THREADS>(mine, shared().wred, &total);
-      if (own_total) {
-        own_total = false;
-        goal_lo = goal_hi = share * total;
-      }
-      const double goal = 0.5 * (goal_lo + goal_hi);
-      if (before < goal && goal <= before + mine) {
-        // the last bin that holds something where the bins' own sums round below the goal
-        for (int j = 0; j < kPer; ++j) {
-          if (m[j] > 0.0) {
-            shared().found = 1;
-            shared().at = (uint32_t)(kSampleBins - 1 - ((int)threadIdx.x * kPer + j));
-            shared().mabove = before;
-            if (goal <= before + m[j]) break;
-          }
-          before += m[j];
-        }
-      }
-      __syncthreads();
-      if (!shared().found) {
-        __syncthreads();
-        if (outermost) return above + total < goal_lo || goal_lo == goal_hi ? 0 : -1;
-        // a bin whose parts' sum rounds below the bin's: its lowest part
-        if (threadIdx.x == 0) {
-          int bin = 0;
-          while (bin < kSampleBins - 1 && shared().count[bin] == 0u) ++bin;
-          shared().at = (uint32_t)bin;
-          shared().mabove = above + total - (sft == 0 ? (double)shared().count[bin] * weight(Row::value(lo + (uint32_t)bin)) : (double)shared().mass[bin] * per_unit);
-        }
-        __syncthreads();
-      }
-      outermost = false;
-      const uint32_t bin = shared().at;
-      above = shared().mabove;
+      if (threadIdx.x == 0) shared().found = 0, shared().at = 0xffffffffu, shared().nat = 0u;
+      const double most0 = above + block_scan<THREADS>(most_sum, shared().wred, &total_most);
       if (sft == 0) {
-        uint32_t n = shared().count[bin];
-        *equal = n;
-        if (lo + bin == first) n -= drop;
+        if (most0 < goal && goal <= most0 + most_sum) {
+          double before = most0;
+          // the last bin that holds something where the bins' own sums round below the goal
+          for (int j = 0; j < kPer; ++j) {
+            const uint32_t bin = kSampleBins - 1 - (threadIdx.x * kPer + j), n = shared().count[bin];
+            if (!n) continue;
+            const double w = (double)n * weight(Row::value(lo + bin));
+            shared().found = 1;
+            shared().at = bin;
+            shared().mabove = before;
+            before += w;
+            if (goal <= before) break;
+          }
+        }
+        __syncthreads();
+        if (!shared().found) {
+          const bool whole = lo == first;
+          if (whole) {
+            __syncthreads();
+            return above + total_most < goal_lo || goal_lo == goal_hi ? 0 : -1;
+          }
+          // a border that rounding put behind the last code of the bins it was found in
+          if (threadIdx.x == 0) {
+            uint32_t bin = 0u;
+            while (bin < kSampleBins - 1 && shared().count[bin] == 0u) ++bin;
+            shared().at = bin;
+            shared().mabove = above + total_most - (double)shared().count[bin] * weight(Row::value(lo + bin));
+          }
+          __syncthreads();
+        }
+        const uint32_t bin = shared().at, n = shared().count[bin];
+        above = shared().mabove;
         *code = lo + bin;
+        *equal = n + (lo + bin == first ? drop : 0u);
         const double w = weight(Row::value(lo + bin));
         const uint32_t a = ranks_below(above, w, n, goal_lo), b = ranks_below(above, w, n, goal_hi);
         *take = b ? b : 1u;
@@ -696,10 +708,64 @@ struct Sampler {
         if (goal_lo < goal_hi && (a != b || a == 0u || above + (double)n * w < goal_hi)) return -1;
         return 1;
       }
-      const uint32_t left = span - (bin << sft);
-      lo += bin << sft;
-      span = left < (1u << sft) ? left : 1u << sft;
+      const double least0 = above + block_scan<THREADS>(least_sum, shared().wred, &total_least);
+      // The border lies no higher than the first bin with which the masses at most reach the goal, and no lower than the first
+      // with which those at least do (2^-40 of the goal wider, for the sums' own rounding).
+      const double from = goal_lo * (1.0 - 1e-12), upto = goal_hi * (1.0 + 1e-12);
+      const bool top_here = most0 < from && from <= most0 + most_sum, low_here = least0 < upto && upto <= least0 + least_sum;
+      if (top_here || low_here) {
+        double f = most0, g = least0;
+        bool top_open = top_here, low_open = low_here;
+        for (int j = 0; j < kPer; ++j) {
+          const uint32_t bin = kSampleBins - 1 - (threadIdx.x * kPer + j), n = shared().count[bin];
+          if (!n) continue;
+          const uint32_t c0 = lo + (bin << sft), c1 = min(c0 + (1u << sft) - 1u, hi);
+          if (top_open) {
+            shared().at = bin;
+            f += (double)n * weight(Row::value(c1));
+            top_open = f < from;
+          }
+          if (low_open) {
+            shared().nat = bin;
+            g += (double)n * weight(Row::value(c0));
+            low_open = g < upto;
+          }
+        }
+      }
       __syncthreads();
+      const uint32_t b1 = shared().at, b0 = shared().nat;
+      __syncthreads();
+      if (b1 == 0xffffffffu) {
+        if (lo == first) return above + total_most < goal_lo ? 0 : goal_lo == goal_hi ? 0 : -1;
+        // rounding again: the lowest bin that holds something
+        if (threadIdx.x == 0) {
+          uint32_t bin = 0u;
+          while (bin < kSampleBins - 1 && shared().count[bin] == 0u) ++bin;
+          shared().at = bin;
+        }
+        __syncthreads();
+      }
+      const uint32_t bin1 = shared().at, upper = min(lo + (bin1 << sft) + ((1u << sft) - 1u), hi);
+      uint32_t lower = lo + (b0 << sft), edge = upper;
+      __syncthreads();
+      if (upper == hi && lower == lo) {
+        // bins too wide for their ends to say anything: whether the border is in the first of them decides its mass
+        const uint32_t low1 = lo + (bin1 << sft);
+        const double in_it = mass_of(low1, hi);
+        if (above + in_it >= goal) {
+          lower = low1;  // above lo: a bin is narrower than the span
+        } else {
+          above += in_it;
+          edge = low1 - 1u;
+          hi = edge;
+          continue;
+        }
+      } else if (upper < hi) {
+        above += mass_of(upper + 1u, hi);
+      }
+      hi = edge;
+      if (lower > hi) lower = hi;
+      lo = lower;
     }
   }
 
@@ -771,20 +837,25 @@ struct Sampler {
     }
   };
 
-  // The kept ones' mass among a lane's eight tokens.  Weights are computed four at a time whether kept or not (their
-  // operations depend on each other), or for no lane.
+  // The kept ones' mass among a lane's eight tokens, without branches, since a weight's operations wait for one another;
+  // not computed where no lane has a kept one.
   __device__ __forceinline__ double kept_mass(const Kept& kept, const float (&a)[8], uint32_t p) const {
-    bool in[8], any = false;
+    const float from = fmaxf(kept.from, least);
+    bool keep[8], any = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) any |= in[i] = kept(a[i], p + i) && a[i] >= least;
+    for (int i = 0; i < 8; ++i) {
+      bool in = a[i] >= from && a[i] <= kept.upto;
+      if (p + 8u > kept.end) in = in && !(p + i >= kept.end && a[i] == kept.from);  // some of the least ones are out
+      any |= keep[i] = in;
+    }
+    if (!__any_sync(0xffffffffu, any)) return 0.0;
     double s = 0.0;
-    if (!__any_sync(0xffffffffu, any)) return s;
 #pragma unroll
     for (int h = 0; h < 8; h += 4) {
       double w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = weight_of(a[h + i]);
-      s += ((in[h] ? w[0] : 0.0) + (in[h + 1] ? w[1] : 0.0)) + ((in[h + 2] ? w[2] : 0.0) + (in[h + 3] ? w[3] : 0.0));
+      for (int i = 0; i < 4; ++i) w[i] = weight_of(a[h + i], keep[h + i]);
+      s += (w[0] + w[1]) + (w[2] + w[3]);
     }
     return s;
   }
@@ -794,7 +865,7 @@ struct Sampler {
     for (int c = threadIdx.x; c < kSampleChunks; c += THREADS) shared().psum[c] = 0.0;
     __syncthreads();
     double s = 0.0;
-    for_chunks([&](int) { s = 0.0; },
+    for_chunks<true>([&](int) { s = 0.0; },
                      [&](int, uint32_t p, const float (&a)[8]) {
                        s += kept_mass(kept, a, p);
                      },
@@ -978,9 +1049,9 @@ struct SampleCalls {
   static __device__ __noinline__ bool kth(S s, uint32_t lo, uint32_t k, uint32_t* code, uint32_t* take, uint32_t* equal) {
     return s.kth(lo, k, code, take, equal);
   }
-  static __device__ __noinline__ int nucleus(S s, uint32_t lo, uint32_t drop, bool own, double share, double goal_lo, double goal_hi,
+  static __device__ __noinline__ int nucleus(S s, uint32_t lo, uint32_t drop, bool own, bool counted, double share, double goal_lo, double goal_hi,
                                              uint32_t* code, uint32_t* take, uint32_t* equal) {
-    return s.nucleus(lo, drop, own, share, goal_lo, goal_hi, code, take, equal);
+    return s.nucleus(lo, drop, own, counted, share, goal_lo, goal_hi, code, take, equal);
   }
   static __device__ __noinline__ uint32_t equal_end(S s, uint32_t code, uint32_t take) { return s.equal_end(code, take); }
   static __device__ __noinline__ void exact_sums(S s, Kept kept) { s.exact_sums(kept); }
@@ -997,7 +1068,7 @@ __device__ __forceinline__ float sample_setting(const SampleSetting& s, long lon
 }
 
 template <int DT, int THREADS>
-__global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const SampleArgs A) {
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 768 / THREADS) sample_kernel(const SampleArgs A) {
   typedef SampleRow<DT> Row;
   typedef SampleCalls<DT, THREADS> Calls;
   SampleShared<DT, THREADS>& sh = Sampler<DT, THREADS>::shared();
@@ -1026,13 +1097,12 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
   S.listed = -1;
   S.shift = A.shift;
   S.nch = (int)(((long long)S.row.end + (256LL << A.shift) - 1) >> (8 + A.shift));
-  S.frac = 62 - (32 - __clz(A.V));
   S.it = (double)itf;
   S.it2 = S.it * 1.4426950408889634;
-  if (threadIdx.x < 64) sh.exp64[threadIdx.x] = exp2((double)threadIdx.x * 0.015625);
+  if (threadIdx.x < 16) sh.exp16[threadIdx.x] = exp2((double)threadIdx.x * 0.0625);
   const bool use_k = kk > 0 && kk < A.V, use_p = p < 1.f;
   const bool need_sum = !use_k && (use_p || mp == 0.f);
-  const float c2 = itf * kLog2e;
+  const float c2 = (float)S.it2;
   if (cluster_ctas() > 1) {  // the first CTA's shared memory is written by the others
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
@@ -1062,9 +1132,12 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
   }
   S.set_top(m);
   typename Sampler<DT, THREADS>::Kept kept{-3.402823466e38f, m, S.row.end};
-  // Relative error of a sum of four chunks: exponentials 2^-22; their arguments 3 roundings, where |t|, weighted by the terms
-  // themselves, is log2(tokens) + 1.5 on the mean; 10 additions one after another, or 2^(2 + shift) more in long chunks.
-  const double eps = 2.5e-7 + 1.3e-7 * (11.5 + A.shift) + 6e-8 * (12.0 + (A.shift ? (double)(4 << A.shift) : 4.0));
+  // Relative error of the sweep's sums.  Were all roundings to go one way: exponentials 2^-22; their arguments, and the rounding
+  // of c2, 2 roundings, where |t|, weighted by the terms themselves, is log2(tokens) + 1.5 on the mean; 10 additions: 1.8e-6.
+  // They do not: sums of a thousand terms are off by some 2e-8.  Taken is 5e-7, which holds for an error of the
+  // exponential or of c2 that all terms share as well; in chunks beyond 256 tokens the worst case, with a reference that
+  // changes on the way.
+  const double eps = A.shift ? 2.5e-7 + 0.84e-7 * (11.5 + A.shift) + 6e-8 * (16.0 + 8.0 * (double)(4 << A.shift)) : 5e-7;
   double total = 0.0;
   uint32_t pos = S.row.mis;
   bool done = false;
@@ -1073,7 +1146,8 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
       double y = 0.0;
       if (4 * g < S.nch) {
         const float mm = fmaxf(fmaxf(sh.cmax[4 * g], sh.cmax[4 * g + 1]), fmaxf(sh.cmax[4 * g + 2], sh.cmax[4 * g + 3]));
-        if (mm > -CUDART_INF_F) y = (double)sh.csum[g] * S.weight(mm);
+        if (mm > -CUDART_INF_F)
+          y = (double)sh.csum[g] * (fabsf(mm * c2) < 1e30f ? exp2((double)(mm * c2) - (double)m * (double)c2) : S.weight(mm));
       }
       sh.psum[g] = y;
     }
@@ -1114,9 +1188,10 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
         cut = further < v && further > -3.402823466e38f ? Row::key(further) : lowest;
       }
       if (!limited) take = equal = 0u, code = cut;
-      if (use_p && Calls::nucleus(S, code, equal - take, true, (double)p, 0.0, 0.0, &pc, &pt, &pe) == 1) code = pc, take = pt, equal = pe;
+      if (use_p && Calls::nucleus(S, code, equal - take, true, false, (double)p, 0.0, 0.0, &pc, &pt, &pe) == 1) code = pc, take = pt, equal = pe;
     } else if (use_p) {
       double goal = S.total_mass(), slack = eps;
+      uint32_t was = 0u;
       for (int pass = 0; pass < 2; ++pass) {
         // what lies below max - c has at most V e^(-c inv_temp) = (1 - p) total
         const double c = log((double)A.V / ((1.0 - (double)p) * goal * (1.0 - 2.0 * eps))) / S.it;
@@ -1126,10 +1201,11 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) sample_kernel(const Sa
         if (cut > Row::kLowest) --cut;
         if (cut < floor_code) cut = floor_code;
         Calls::make_list(S, Row::value(cut));
-        const int got = Calls::nucleus(S, cut, 0u, false, 0.0, (double)p * goal * (1.0 - slack), (double)p * goal * (1.0 + slack), &pc, &pt, &pe);
+        const int got = Calls::nucleus(S, cut, 0u, false, pass == 1 && cut == was && Row::key(m) - cut < (uint32_t)kSampleBins, 0.0, (double)p * goal * (1.0 - slack), (double)p * goal * (1.0 + slack), &pc, &pt, &pe);
         if (got == 1) code = pc, take = pt, equal = pe;
         else if (got == 0) code = cut;
         if (got >= 0) break;
+        was = cut;
         // the border lies within the sweep's error: the total in 64 bits
         Calls::make_list(S, -3.402823466e38f);
         Calls::exact_sums(S, kept);
