@@ -138,7 +138,7 @@ int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, co
   A.w = weights;
   A.stride = weight_stride;
   A.vec = (uintptr_t)weights % 16 == 0 && (table->V == 1 || weight_stride * es % 16 == 0);
-  A.lanes = lanes_for((long long)A.T.G << (A.T.log_group - 3), 1 << (A.T.log_group - 3));
+  A.lanes = lanes_for((long long)A.T.G << (A.T.log_group - 4), 1 << (A.T.log_group - 4));
   const unsigned grid = ctas_for(A.T.V, A.lanes);
   cudaStream_t st = (cudaStream_t)stream;
   if (dtype == GLS_F32) quantize_kernel<kF32><<<grid, kInt4Threads, 0, st>>>(A);
@@ -195,7 +195,7 @@ int gls_embed_tokens_int4(const gls_int4_table_t* table, const int32_t* tokens, 
   A.out_stride = out_stride;
   A.vec = (uintptr_t)out % 16 == 0 && (N == 1 || out_stride * es % 16 == 0);
   A.status = device_status;
-  A.lanes = lanes_for((A.T.D + 7) / 8, 1);
+  A.lanes = lanes_for((A.T.D + 15) / 16, 1);
   const unsigned grid = ctas_for(N, A.lanes);
   cudaStream_t st = (cudaStream_t)stream;
   if (out_dtype == GLS_F32) embed_int4_kernel<kF32><<<grid, kInt4Threads, 0, st>>>(A);

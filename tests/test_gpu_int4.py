@@ -233,3 +233,19 @@ def test_refusals(gls):
     for bad in (w.half(), w.T, w[0], w.cpu(), w.clone().requires_grad_()):
         with pytest.raises(E):
             gls.quantize_table(bad)
+
+
+def test_quantize_quotients_of_all_sizes(gls):
+    """Quotients next to half way between two codes, for steps of every mantissa: equal to those of a division."""
+    g = _gen(77)
+    step = (1.0 + torch.rand((4000, 1), generator=g, device="cuda")) * 2.0 ** torch.randint(-60, 60, (4000, 1), generator=g, device="cuda").float()
+    k = torch.randint(-7, 7, (4000, 64), generator=g, device="cuda") + 0.5
+    w = k * step * (1.0 + torch.randint(-3, 4, (4000, 64), generator=g, device="cuda") * 2.0 ** -23)
+    w[:, 0] = 7.0 * step[:, 0]
+    for zeros in (False, True):
+        for x in (w, w.to(BF16)):
+            for sd in (F32, BF16):
+                t = gls.quantize_table(x, group=64, zeros=zeros, scale_dtype=sd)
+                q, s, z = ref.quantize(x, 64, zeros, sd)
+                codes, tz = ref.unpack(t)
+                assert torch.equal(t.scales.double(), s) and torch.equal(tz, z) and torch.equal(codes, q), (zeros, x.dtype, sd)
