@@ -117,9 +117,10 @@ def _load_calls(L):
         calls = importlib.util.module_from_spec(spec)
         calls.entry_points(*(C.cast(getattr(L, "gls_" + n), C.c_void_p).value for n in (
             "token_logprobs", "emitted_logprobs", "token_logprobs_backward", "embed_tokens",
-            "embed_tokens_backward_workspace_bytes", "embed_tokens_backward")))
+            "embed_tokens_backward_workspace_bytes", "embed_tokens_backward", "sample_tokens", "head_logits",
+            "embed_tokens_int4")))
         return calls
-    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+    except (ImportError, OSError, TypeError, subprocess.CalledProcessError) as e:  # TypeError: made from older sources
         _without_calls(e)
         return _GeneralWay()
 
@@ -1086,6 +1087,10 @@ def sample_tokens(logits, uniforms, inv_temp=1.0, top_k=0, top_p=1.0, min_p=0.0,
     tensors are written (log probabilities where it has them).  Not differentiable (see token_logprobs)."""
     _no_tangent(logits)
     _no_gradient("sample_tokens", logits)
+    if out is None:
+        r = (_calls or _fast()).sample_tokens(logits, uniforms, inv_temp, top_k, top_p, min_p, want_logprobs, status)
+        if r is not None:
+            return _done(r)
     dev = _device(logits, "logits")
     rows = _rows4(logits, "logits")
     B, K, J, V = logits.shape
@@ -1104,6 +1109,9 @@ def sample_tokens(logits, uniforms, inv_temp=1.0, top_k=0, top_p=1.0, min_p=0.0,
          _vec(out.get("logprobs"), "out['logprobs']", lead, _F32T, dev), _vec(status, "status", (1,), _I32, dev))
     _wrote(*out.values())
     return out
+
+
+_TYPE_CODE = {_F32T: F32, _BF16T: BF16}
 
 
 class Int4Table(NamedTuple):
@@ -1164,6 +1172,10 @@ def head_logits(x, table, dtype=None, out=None):
     (x's unless given), accumulated in fp32.  Not differentiable."""
     _no_tangent(x, table.scales)
     _no_gradient("head_logits", x, table.scales)
+    if out is None and (dtype is None or dtype in _TYPE_CODE):
+        r = (_calls or _fast()).head_logits(x, *table, -1 if dtype is None else _TYPE_CODE[dtype])
+        if r is not None:
+            return _done(r)
     dev = _device(x, "x")
     t, tdev, V = _int4(table)
     lead = x.shape[:-1]
@@ -1198,6 +1210,10 @@ def embed_tokens_int4(table, tokens, scale=1.0, dtype=torch.bfloat16, status=Non
     [*tokens.shape, D] of type `dtype`; a token below 0 gives zeros.  Not differentiable."""
     _no_tangent(table.scales)
     _no_gradient("embed_tokens_int4", table.scales)
+    if out is None and dtype in _TYPE_CODE:
+        r = (_calls or _fast()).embed_tokens_int4(*table, tokens, scale, _TYPE_CODE[dtype], status)
+        if r is not None:
+            return _done(r)
     t, dev, _ = _int4(table)
     D, lead = table.dim, tokens.shape
     tp = _vec(tokens, "tokens", lead, _I32, dev)

@@ -15,6 +15,7 @@
 
 #include <climits>
 #include <optional>
+#include <type_traits>
 
 #include "../../include/gls.h"
 
@@ -26,6 +27,9 @@ decltype(&gls_token_logprobs_backward) g_logprobs_backward = nullptr;
 decltype(&gls_embed_tokens) g_embed = nullptr;
 decltype(&gls_embed_tokens_backward_workspace_bytes) g_embed_backward_bytes = nullptr;
 decltype(&gls_embed_tokens_backward) g_embed_backward = nullptr;
+decltype(&gls_sample_tokens) g_sample = nullptr;
+decltype(&gls_head_logits) g_head = nullptr;
+decltype(&gls_embed_tokens_int4) g_embed_int4 = nullptr;
 
 constexpr int64_t kMaxTop = 256;  // the library's largest `top`
 
@@ -305,14 +309,147 @@ PyObject* embed_tokens_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   CALL_END
 }
 
-// entry_points(addresses of the six entry points, in the order of the variables above)
-PyObject* entry_points(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* p[6];
-  if (n != 6) {
-    PyErr_SetString(PyExc_TypeError, "six addresses");
+// One sampling setting: a number, or a tensor [B], [B,K] or [B,K,J] whose sizes of 1 broadcast.
+template <class T>
+const T* setting(PyObject* o, at::ScalarType type, at::IntArrayRef lead, c10::Device dev, T* value, int64_t* stride) {
+  if (!THPVariable_Check(o)) {
+    if constexpr (std::is_integral_v<T>) {
+      const int64_t v = integer(o);
+      if (v < INT_MIN || v > INT_MAX) throw Decline();
+      *value = (T)v;
+    } else {
+      *value = (T)number(o);
+    }
     return nullptr;
   }
-  for (int i = 0; i < 6; ++i) {
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.scalar_type() != type || t.device() != dev || t.layout() != at::kStrided || t.dim() < 1 || t.dim() > 3) throw Decline();
+  for (int i = 0; i < t.dim(); ++i) {
+    if (t.size(i) != lead[i] && t.size(i) != 1) throw Decline();
+    stride[i] = t.size(i) > 1 ? t.stride(i) : 0;
+  }
+  return (const T*)t.data_ptr();
+}
+
+// sample_tokens(logits, uniforms, inv_temp, top_k, top_p, min_p, want_logprobs, status)
+PyObject* sample_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN(8)
+  const at::Tensor& x = tensor(a[0]);
+  const c10::Device dev = here(x);
+  const gls_rows_t rows = rows_of(x);
+  const at::IntArrayRef lead = x.sizes().slice(0, 3);
+  if (lead[1] > GLS_MAX_K) throw Decline();
+  const float* u = data<float>(tensor(a[1]), at::kFloat, lead, dev);
+  gls_sampling_t s = {};
+  s.inv_temp_rows = setting(a[2], at::kFloat, lead, dev, &s.inv_temp, s.inv_temp_stride);
+  s.top_k_rows = setting(a[3], at::kInt, lead, dev, &s.top_k, s.top_k_stride);
+  s.top_p_rows = setting(a[4], at::kFloat, lead, dev, &s.top_p, s.top_p_stride);
+  s.min_p_rows = setting(a[5], at::kFloat, lead, dev, &s.min_p, s.min_p_stride);
+  const bool want = truth(a[6]);
+  uint32_t* status = status_word(a[7], dev);
+  std::optional<NoGil> free_others(std::in_place);
+  const at::Tensor tokens = make(lead, at::kInt, dev);
+  at::Tensor lp;
+  if (want) lp = make(lead, at::kFloat, dev);
+  const int rc = g_sample(&rows, (int)lead[0], (int)lead[1], (int)lead[2], x.size(3), &s, u, (int32_t*)tokens.data_ptr(),
+                          want ? (float*)lp.data_ptr() : nullptr, status, stream());
+  free_others.reset();
+  if (rc) return PyLong_FromLong(rc);
+  PyObject* d = PyDict_New();
+  if (!d) throw python_error();
+  put(d, "tokens", tokens);
+  if (want) put(d, "logprobs", lp);
+  return d;
+  CALL_END
+}
+
+// The table that codes, scales, zeros, columns and group make.
+gls_int4_table_t table_of(PyObject* const* a, c10::Device dev) {
+  const at::Tensor& codes = tensor(a[0]);
+  const at::Tensor& scales = tensor(a[1]);
+  const at::Tensor zeros = tensor_or_none(a[2]);
+  gls_int4_table_t t;
+  t.D = integer(a[3]);
+  const int64_t group = integer(a[4]);
+  if (group != 32 && group != 64 && group != 128) throw Decline();
+  t.group = (int32_t)group;
+  const int64_t G = (t.D + group - 1) / group;
+  if (t.D <= 0 || codes.scalar_type() != at::kByte || codes.device() != dev || codes.layout() != at::kStrided ||
+      codes.dim() != 2 || codes.stride(1) != 1 || codes.size(1) < (t.D + 31) / 32 * 16)
+    throw Decline();
+  t.V = codes.size(0);
+  auto fits = [&](const at::Tensor& s) {
+    return s.device() == dev && s.layout() == at::kStrided && s.dim() == 2 && s.size(0) == t.V && s.size(1) == G &&
+           (s.stride(1) == 1 || G == 1);
+  };
+  if (!fits(scales) || (zeros.defined() && (!fits(zeros) || zeros.scalar_type() != at::kByte))) throw Decline();
+  t.codes = (uint8_t*)codes.data_ptr();
+  t.code_stride = codes.stride(0);
+  t.scales = scales.data_ptr();
+  t.scale_dtype = dtype_code(scales);
+  t.scale_stride = scales.stride(0);
+  t.zeros = zeros.defined() ? (uint8_t*)zeros.data_ptr() : nullptr;
+  t.zero_stride = zeros.defined() ? zeros.stride(0) : 0;
+  return t;
+}
+at::ScalarType type_of(int64_t code) {
+  if (code == GLS_F32) return at::kFloat;
+  if (code == GLS_BF16) return at::kBFloat16;
+  throw Decline();
+}
+
+// head_logits(x, codes, scales, zeros, dim, group, type of the logits, -1 for x's)
+PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN(7)
+  const at::Tensor& x = tensor(a[0]);
+  const c10::Device dev = here(x);
+  const int dt = dtype_code(x);
+  const gls_int4_table_t t = table_of(a + 1, dev);
+  const int64_t code = integer(a[6]);
+  if (x.dim() < 1 || x.size(x.dim() - 1) != t.D || !x.is_contiguous()) throw Decline();
+  const at::ScalarType type = type_of(code < 0 ? dt : code);
+  c10::SmallVector<int64_t, 5> shape(x.sizes().begin(), x.sizes().end());
+  shape.back() = t.V;
+  std::optional<NoGil> free_others(std::in_place);
+  const at::Tensor out = make(shape, type, dev);
+  const int rc = g_head(x.data_ptr(), dt, t.D, x.numel() / t.D, &t, out.data_ptr(), type == at::kFloat ? GLS_F32 : GLS_BF16, t.V,
+                        stream());
+  free_others.reset();
+  if (rc) return PyLong_FromLong(rc);
+  return THPVariable_Wrap(out);
+  CALL_END
+}
+
+// embed_tokens_int4(codes, scales, zeros, dim, group, tokens, scale, type, status)
+PyObject* embed_tokens_int4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  CALL_BEGIN(9)
+  const at::Tensor& k = tensor(a[5]);
+  const c10::Device dev = here(k);
+  const gls_int4_table_t t = table_of(a, dev);
+  const int32_t* tokens = data<int32_t>(k, at::kInt, k.sizes(), dev);
+  const double scale = number(a[6]);
+  const at::ScalarType type = type_of(integer(a[7]));
+  uint32_t* status = status_word(a[8], dev);
+  c10::SmallVector<int64_t, 5> shape(k.sizes().begin(), k.sizes().end());
+  shape.push_back(t.D);
+  std::optional<NoGil> free_others(std::in_place);
+  const at::Tensor out = make(shape, type, dev);
+  const int rc = g_embed_int4(&t, tokens, k.numel(), (float)scale, out.data_ptr(), type == at::kFloat ? GLS_F32 : GLS_BF16, t.D,
+                              status, stream());
+  free_others.reset();
+  if (rc) return PyLong_FromLong(rc);
+  return THPVariable_Wrap(out);
+  CALL_END
+}
+
+// entry_points(addresses of the nine entry points, in the order of the variables above)
+PyObject* entry_points(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  void* p[9];
+  if (n != 9) {
+    PyErr_SetString(PyExc_TypeError, "nine addresses");
+    return nullptr;
+  }
+  for (int i = 0; i < 9; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
@@ -325,6 +462,9 @@ PyObject* entry_points(PyObject*, PyObject* const* a, Py_ssize_t n) {
   g_embed = (decltype(g_embed))p[3];
   g_embed_backward_bytes = (decltype(g_embed_backward_bytes))p[4];
   g_embed_backward = (decltype(g_embed_backward))p[5];
+  g_sample = (decltype(g_sample))p[6];
+  g_head = (decltype(g_head))p[7];
+  g_embed_int4 = (decltype(g_embed_int4))p[8];
   Py_RETURN_NONE;
 }
 
@@ -335,6 +475,9 @@ PyMethodDef g_methods[] = {
     {"token_logprobs_backward", (PyCFunction)(void (*)(void))token_logprobs_backward, METH_FASTCALL, nullptr},
     {"embed_tokens", (PyCFunction)(void (*)(void))embed_tokens, METH_FASTCALL, nullptr},
     {"embed_tokens_backward", (PyCFunction)(void (*)(void))embed_tokens_backward, METH_FASTCALL, nullptr},
+    {"sample_tokens", (PyCFunction)(void (*)(void))sample_tokens, METH_FASTCALL, nullptr},
+    {"head_logits", (PyCFunction)(void (*)(void))head_logits, METH_FASTCALL, nullptr},
+    {"embed_tokens_int4", (PyCFunction)(void (*)(void))embed_tokens_int4, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "gls_torch_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

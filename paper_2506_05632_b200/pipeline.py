@@ -4,7 +4,9 @@
 are on the GPU: draft-side sampling (Algorithm 2, draft loop) followed by target-side sampling and
 verification (Algorithm 2, second half), and where the buffers ask for it what a serving loop needs of
 the emitted tokens next: their log probabilities with entropy and alternatives, and their rows of an
-embedding table, the inputs of the next step.  `HostStepper` is the same step for logits that live in
+embedding table, the inputs of the next step.  `draft_position` is what a drafter calls per position between
+its hidden states and its next inputs: the logits of its 4-bit head, the tokens (by the races, or independent
+ones), their rows of the embedding.  `HostStepper` is the same step for logits that live in
 (pinned) host memory: it streams sequence chunks to the device through two staging buffers so
 that the copy of chunk n+1 overlaps the sweep of chunk n, and returns the results to the host.
 Only copies, launches and bookkeeping happen here; all arithmetic is in the CUDA library.
@@ -77,6 +79,58 @@ def spec_step(draft_logits, target_logits, buf, inv_temp=1.0, seed=0, seq_base=0
         binding.embed_tokens_raw(buf.table, buf.out["tokens"], scale=buf.table_scale, status=buf.status,
                                  out=buf.inputs)
     return buf.out
+
+
+class DraftBuffers:
+    """Preallocated outputs of `draft_position` for B sequences of K drafts with L positions.
+
+    head: the drafter's head, an Int4Table [V,D].  embedding: None, or the table the next inputs come from, an
+    Int4Table [V,E] or a plain one; `inputs` [B,K,E] then holds embed_scale * its rows of the tokens drawn last."""
+
+    def __init__(self, B, K, L, head, embedding=None, logits_dtype=torch.bfloat16, inputs_dtype=torch.bfloat16,
+                 embed_scale=1.0, device="cuda"):
+        V = head.codes.shape[0]
+        self.shape = (B, K, L, V)
+        self.head, self.embedding, self.embed_scale = head, embedding, embed_scale
+        self.logits = torch.empty((B, K, 1, V), dtype=logits_dtype, device=device)
+        self.tokens = torch.empty((B, K, 1), dtype=torch.int32, device=device)
+        self.scores = torch.empty((B, K, 1), dtype=torch.float32, device=device)
+        self.draft_tokens = torch.empty((B, K, L), dtype=torch.int32, device=device)
+        self.draft_scores = torch.empty((B, K, L), dtype=torch.float32, device=device)
+        self.inputs = None
+        if isinstance(embedding, binding.Int4Table):
+            self.inputs = torch.empty((B, K, embedding.dim), dtype=inputs_dtype, device=device)
+        elif embedding is not None:
+            self.inputs = torch.empty((B, K, embedding.shape[1]), dtype=embedding.dtype, device=device)
+        self.workspace = torch.empty(binding.workspace_bytes(B, K, 1, V), dtype=torch.uint8, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+
+
+def draft_position(hidden, j, buf, inv_temp=1.0, seed=0, seq_base=0, pos_base=0, uniforms=None, **settings):
+    """One position of a drafter between its last hidden states and its next inputs: hidden [B,K,D] on the
+    device -> buf.logits, the tokens of position j in buf.draft_tokens[:, :, j] (scores beside them) and buf.inputs.
+
+    The tokens are those of the races (draft_sample at position pos_base + j), which a verification of the same
+    seed couples with; or, given uniforms [B,K,1], independent ones of sample_tokens, whose top_k, top_p and min_p
+    `settings` are and whose log probabilities take the scores' place.  No result carries a gradient."""
+    if not 0 <= j < buf.shape[2]:
+        raise binding.GlsError("position %d of %d" % (j, buf.shape[2]))
+    binding.head_logits(hidden.detach(), buf.head, out=buf.logits[:, :, 0])
+    if uniforms is None:
+        if settings:
+            raise binding.GlsError("the races take no %s" % ", ".join(sorted(settings)))
+        binding.draft_sample(buf.logits, inv_temp=inv_temp, seed=seed, seq_base=seq_base, pos_base=pos_base + j,
+                             workspace=buf.workspace, status=buf.status, out_tokens=buf.tokens, out_scores=buf.scores)
+    else:
+        binding.sample_tokens(buf.logits, uniforms, inv_temp=inv_temp, status=buf.status,
+                              out=dict(tokens=buf.tokens, logprobs=buf.scores), **settings)
+    buf.draft_tokens[:, :, j] = buf.tokens[:, :, 0]
+    buf.draft_scores[:, :, j] = buf.scores[:, :, 0]
+    if isinstance(buf.embedding, binding.Int4Table):
+        binding.embed_tokens_int4(buf.embedding, buf.tokens[:, :, 0], scale=buf.embed_scale, status=buf.status, out=buf.inputs)
+    elif buf.embedding is not None:
+        binding.embed_tokens_raw(buf.embedding, buf.tokens[:, :, 0], scale=buf.embed_scale, status=buf.status, out=buf.inputs)
+    return buf.inputs
 
 
 class GraphedStep:
