@@ -12,7 +12,7 @@ __device__ __forceinline__ void barrier_expect(uint32_t at, uint32_t bytes) {
 }
 // false if the phase did not end within a limit that no copy reaches
 __device__ __forceinline__ bool barrier_wait(uint32_t at, uint32_t parity) {
-  for (int i = 0; i < (1 << 22); ++i) {
+  for (int i = 0; i < (1 << 20); ++i) {
     uint32_t done;
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(done)

@@ -4,7 +4,7 @@
 
 #include "../../include/gls.h"
 #include "gls_host.cuh"
-#include "gls_int4.cuh"
+#include "gls_head_wide.cuh"
 
 namespace gls {
 
@@ -55,8 +55,8 @@ static unsigned ctas_for(long long rows, int lanes) {
 // shared memory per hidden state
 static long long head_column_bytes(int parts, int chunks, int uc) { return (long long)parts * ((chunks + uc - 1) / uc) * uc * 256; }
 
-// The codes as bytes [V][ceil(D / 32) * 16], copied in boxes of 16 rows by 64.
-static bool codes_map(const Int4Table& T, CUtensorMap* map) {
+// The codes as bytes [V][ceil(D / 32) * 16], copied in boxes of `rows` rows by 64.
+static bool codes_map(const Int4Table& T, int rows, CUtensorMapSwizzle swizzle, CUtensorMap* map) {
   typedef decltype(&cuTensorMapEncodeTiled) Encode;
   static std::atomic<Encode> found{nullptr};
   Encode encode = found.load(std::memory_order_relaxed);
@@ -73,9 +73,9 @@ static bool codes_map(const Int4Table& T, CUtensorMap* map) {
   }
   const cuuint64_t row = (cuuint64_t)((T.D + 31) / 32 * 16), dims[2] = {row, (cuuint64_t)T.V};
   const cuuint64_t stride[1] = {T.V > 1 ? (cuuint64_t)T.code_stride : row};
-  const cuuint32_t box[2] = {64, 16}, step[2] = {1, 1};
+  const cuuint32_t box[2] = {64, (cuuint32_t)rows}, step[2] = {1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, T.codes, dims, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int GPC, int PARTS, int UC>
@@ -110,14 +110,39 @@ static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream
   return launch_head_unit<GPC, PARTS, 2>(A, codes, (int)(cols < want ? cols : want), warps, st);
 }
 
+template <int NB, int GPC, int PARTS>
+static cudaError_t launch_wide(const HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
+  const int smem = WideShared::total(NB, PARTS);
+  const cudaError_t err = cudaFuncSetAttribute(head_wide_kernel<NB, GPC, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err != cudaSuccess) return err;
+  const long long pairs = (A.T.V + 2 * kWideRows - 1) / (2 * kWideRows), most = sm_count();
+  dim3 grid((unsigned)(pairs < most ? pairs : most), (unsigned)((A.N + 16 * NB - 1) / (16 * NB)));
+  head_wide_kernel<NB, GPC, PARTS><<<grid, kWideThreads, smem, st>>>(A, codes);
+  return cudaGetLastError();
+}
+
+template <int GPC, int PARTS>
+static cudaError_t launch_wide_for(const HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
+  // passes of equal size: 16 .. 64 hidden states
+  const int passes = (A.N + 63) / 64, nb = (A.N + 16 * passes - 1) / (16 * passes);
+  switch (nb) {
+    case 1: return launch_wide<1, GPC, PARTS>(A, codes, st);
+    case 2: return launch_wide<2, GPC, PARTS>(A, codes, st);
+    case 3: return launch_wide<3, GPC, PARTS>(A, codes, st);
+    default: return launch_wide<4, GPC, PARTS>(A, codes, st);
+  }
+}
+
 template <int PARTS>
 static cudaError_t launch_head_for(HeadArgs& A, cudaStream_t st) {
   CUtensorMap codes;
-  if (!codes_map(A.T, &codes)) return cudaErrorInvalidValue;
+  // more than one pass of the kernel for few hidden states takes longer than one of the other
+  const bool wide = A.N > 8;
+  if (!codes_map(A.T, wide ? kWideRows : 16, wide ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, &codes)) return cudaErrorInvalidValue;
   switch (A.T.log_group) {
-    case 5: return launch_head<4, PARTS>(A, codes, st);
-    case 6: return launch_head<2, PARTS>(A, codes, st);
-    default: return launch_head<1, PARTS>(A, codes, st);
+    case 5: return wide ? launch_wide_for<4, PARTS>(A, codes, st) : launch_head<4, PARTS>(A, codes, st);
+    case 6: return wide ? launch_wide_for<2, PARTS>(A, codes, st) : launch_head<2, PARTS>(A, codes, st);
+    default: return wide ? launch_wide_for<1, PARTS>(A, codes, st) : launch_head<1, PARTS>(A, codes, st);
   }
 }
 
@@ -163,6 +188,7 @@ int gls_head_logits(const void* x, int x_dtype, int64_t x_stride, int64_t N, con
     return GLS_ERR_INVALID_ARG;
   A.x = (const char*)x;
   A.x_stride = x_stride;
+  A.x_vec = (uintptr_t)x % 16 == 0 && (N == 1 || x_stride * xs % 16 == 0);
   A.N = (int)N;
   A.out = (char*)out;
   A.out_stride = out_stride;

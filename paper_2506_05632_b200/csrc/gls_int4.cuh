@@ -259,6 +259,7 @@ struct HeadArgs {
   int cols;            // hidden states per CTA row of the grid
   int chunks;          // of 128 columns
   int vec;             // a lane's scales and zeros of a unit are aligned vectors
+  int x_vec;           // 8 columns of a hidden state are aligned 16-byte words
   long long tiles;     // of 16 rows
 };
 
