@@ -27,7 +27,7 @@ from .binding import (  # noqa: F401
     DEV_BAD_SETTING, DEV_BAD_TOKEN, DEV_EMPTY_SUPPORT, MAX_GIVEN, GlsError, Int4Table,
     build, copy_rows_to_device, debug_bounds, compress_gaussian, compress_gaussian_workspace_bytes, compress_select, draft_sample, draft_sample_sparse, draft_sample_static,
     draft_sample_topm, draft_verify, draft_verify_workspace_bytes, lib_path, load,
-    embed_tokens_backward, embed_tokens_backward_workspace_bytes, embed_tokens_int4, emitted_logprobs, head_logits,
+    embed_tokens_backward, embed_tokens_backward_workspace_bytes, embed_tokens_int4, emitted_logprobs, head_logits, head_logits_workspace_bytes,
     quantize_table, sample_tokens,
     static_scratch_bytes, status_string, target_sample_verify, target_sample_verify_sparse,
     target_sample_verify_topm, token_logprobs_backward, topm_workspace_bytes, verify_phases, verify_walk, version, workspace_bytes)

@@ -118,7 +118,7 @@ def _load_calls(L):
         calls.entry_points(*(C.cast(getattr(L, "gls_" + n), C.c_void_p).value for n in (
             "token_logprobs", "emitted_logprobs", "token_logprobs_backward", "embed_tokens",
             "embed_tokens_backward_workspace_bytes", "embed_tokens_backward", "sample_tokens", "head_logits",
-            "embed_tokens_int4")))
+            "head_logits_workspace_bytes", "embed_tokens_int4")))
         return calls
     except (ImportError, OSError, TypeError, subprocess.CalledProcessError) as e:  # TypeError: made from older sources
         _without_calls(e)
@@ -257,7 +257,10 @@ def load():
         L.gls_quantize_table.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.POINTER(_Int4), C.c_void_p]
         L.gls_head_logits.restype = C.c_int
         L.gls_head_logits.argtypes = [
-            C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.POINTER(_Int4), C.c_void_p, C.c_int, C.c_int64, C.c_void_p]
+            C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.POINTER(_Int4), C.c_void_p, C.c_int, C.c_int64, C.c_void_p,
+            C.c_size_t, C.c_void_p]
+        L.gls_head_logits_workspace_bytes.restype = C.c_size_t
+        L.gls_head_logits_workspace_bytes.argtypes = [C.c_int64, C.c_int64, C.c_int]
         L.gls_embed_tokens_int4.restype = C.c_int
         L.gls_embed_tokens_int4.argtypes = [
             C.POINTER(_Int4), C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_void_p]
@@ -1167,12 +1170,16 @@ def quantize_table(weights, group=128, zeros=True, scale_dtype=torch.bfloat16, o
     return out
 
 
-def head_logits(x, table, dtype=None, out=None):
+def head_logits_workspace_bytes(N, D, dtype):
+    return int(_ready().gls_head_logits_workspace_bytes(int(N), int(D), _TYPE_CODE[dtype]))
+
+
+def head_logits(x, table, dtype=None, workspace=None, out=None):
     """gls_head_logits: x [...,D] fp32 or bf16 times the rows of an Int4Table [V,D] -> logits [...,V] of type `dtype`
     (x's unless given), accumulated in fp32.  Not differentiable."""
     _no_tangent(x, table.scales)
     _no_gradient("head_logits", x, table.scales)
-    if out is None and (dtype is None or dtype in _TYPE_CODE):
+    if out is None and workspace is None and (dtype is None or dtype in _TYPE_CODE):
         r = (_calls or _fast()).head_logits(x, *table, -1 if dtype is None else _TYPE_CODE[dtype])
         if r is not None:
             return _done(r)
@@ -1200,7 +1207,8 @@ def head_logits(x, table, dtype=None, out=None):
             odt, ostride = _matrix(out.view(N, V), "out")
         except RuntimeError as e:
             raise e if isinstance(e, GlsError) else GlsError("out's rows must be a constant stride apart") from None
-    _run(dev, _ready().gls_head_logits, flat.data_ptr(), dt, stride, N, t, out.data_ptr(), odt, ostride)
+    keep, ws, nbytes = _space(workspace, int(_ready().gls_head_logits_workspace_bytes(N, table.dim, dt)), x)
+    _run(dev, _ready().gls_head_logits, flat.data_ptr(), dt, stride, N, t, out.data_ptr(), odt, ostride, ws, nbytes)
     _wrote(out)
     return out
 

@@ -10,9 +10,10 @@
 // per group bind the kernel.
 //
 // A CTA has two warpgroups of that kind, each with 128 rows, which share the hidden states' tiles, and a third one: a
-// thread that requests the codes (tensor copies), a thread that issues the products, two warps that bring the hidden states
-// (from L2, reordered and, fp32 ones, split into three bf16 parts).  Everything is double buffered: while a group's product
-// runs, its warpgroup converts the next group.
+// thread that requests the codes, one that requests the hidden states (both by tensor copies), one that issues the
+// products.  Everything is double buffered: while a group's product runs, its warpgroup converts the next group.  The hidden
+// states are put in order (and fp32 ones split into three bf16 parts) by a small kernel before: two warps of
+// each CTA that did so on the way took 1130 us where the copies take a fraction of it.
 #pragma once
 #include "gls_int4.cuh"
 
@@ -64,9 +65,40 @@ __device__ __forceinline__ uint64_t tensor_tile(uint32_t at) {
   return (uint64_t)(at >> 4 & 0x3fffu) | 1ull << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
+// Hidden states -> [pass][part][kN][chunks * 128] bf16, zeros beyond N and D, within 8 columns in the order 0 4 1 5 2 6 3 7.
+template <int PARTS>
+__global__ void __launch_bounds__(256) head_order_kernel(const HeadArgs A, int kn, int passes, uint4* to) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  const int words = A.chunks * 16;
+  const long long all = (long long)passes * kn * words;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+    const int word = (int)(i % words);
+    const long long n = i / words, d = (long long)word * 8;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = 0.f;
+      if (n < A.N && d + e < A.T.D) {
+        const long long at = n * A.x_stride + d + e;
+        v[e] = PARTS == 1 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)A.x + at) << 16) : __ldg((const float*)A.x + at);
+      }
+    }
+    const long long pass = n / kn, row = n % kn;
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+      uint32_t h[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = PARTS == 1 ? __float_as_uint(v[e]) >> 16 : take_bf16(v[e]);
+      to[((pass * PARTS + part) * kn + row) * words + word] =
+          make_uint4(h[0] | h[4] << 16, h[1] | h[5] << 16, h[2] | h[6] << 16, h[3] | h[7] << 16);
+    }
+  }
+}
+
 // NB: 16 hidden states each; GPC: groups per 128 columns
 template <int NB, int GPC, int PARTS>
-__global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadArgs A, const __grid_constant__ CUtensorMap codes) {
+__global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadArgs A, const __grid_constant__ CUtensorMap codes,
+                                                                   const __grid_constant__ CUtensorMap hidden) {
   extern __shared__ __align__(1024) char wide_shared[];
   constexpr int kN = 16 * NB, kXStages = WideShared::x_stages(PARTS), kXStage = WideShared::x_stage(NB, PARTS);
   constexpr int kSteps = 8 / GPC;   // products of 16 columns per group
@@ -91,7 +123,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
       for (int s = 0; s < kWideCodeStages; ++s) barrier_init(code_full(w, s), 1), barrier_init(code_free(w, s), 4);
       for (int s = 0; s < 2; ++s) barrier_init(a_full(w, s), 4), barrier_init(d_full(w, s), 1);
     }
-    for (int s = 0; s < kXStages; ++s) barrier_init(x_full(s), 2), barrier_init(x_free(s), 1);
+    for (int s = 0; s < kXStages; ++s) barrier_init(x_full(s), 1), barrier_init(x_free(s), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) {
@@ -209,7 +241,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
             if (chunk >= kWideCodeStages) wait(code_free(w, s), (uint32_t)(chunk / kWideCodeStages - 1) & 1u);
             if (lost) continue;
             barrier_expect(code_full(w, s), 8192);
-            copy_codes(base + WideShared::kCodes + (w * kWideCodeStages + s) * 8192, &codes, c * 64, (int)((tile * 2 + w) * kWideRows), code_full(w, s));
+            copy_box(base + WideShared::kCodes + (w * kWideCodeStages + s) * 8192, &codes, c * 64, (int)((tile * 2 + w) * kWideRows), code_full(w, s));
           }
         }
       }
@@ -250,55 +282,28 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
         }
       }
     }
-  } else {
-    // ---- the hidden states: 16-byte words (8 columns in the order of the codes' pairs) of a chunk's two panels
-    const int t = threadIdx.x - 320;  // 64 threads
-    long long chunk = 0;
-    for (int i = 0; i < mine; ++i) {
-      for (int c = 0; c < A.chunks; ++c, ++chunk) {
-        const int xs = (int)(chunk % kXStages);
-        if (chunk >= kXStages) wait(x_free(xs), (uint32_t)(chunk / kXStages - 1) & 1u);
-        const uint32_t to = base + WideShared::kX + xs * kXStage;
-#pragma unroll 4
-        for (int u = t; u < kN * 16; u += 64) {
-          const int n = u >> 4, word = u & 15;
-          const long long d = (long long)c * 128 + word * 8;
-          float v[8];
-          const char* p = A.x + ((long long)(n0 + n) * A.x_stride + d) * (PARTS == 1 ? 2 : 4);
-          uint32_t h[8];
-          const bool all = n < cols && d + 8 <= T.D;
-          if (PARTS == 1 && all && A.x_vec) {
-            const uint4 q = __ldg((const uint4*)p);
-            const uint32_t x[4] = {q.x, q.y, q.z, q.w};
+  } else if (warp == 10) {
+    // ---- the hidden states
+    if (lane == 0) {
+      asm volatile("griddepcontrol.wait;" ::: "memory");  // the kernel that puts them in order
+      long long chunk = 0;
+      for (int i = 0; i < mine; ++i) {
+        for (int c = 0; c < A.chunks; ++c, ++chunk) {
+          const int xs = (int)(chunk % kXStages);
+          if (chunk >= kXStages) wait(x_free(xs), (uint32_t)(chunk / kXStages - 1) & 1u);
+          if (lost) continue;
+          barrier_expect(x_full(xs), (uint32_t)kXStage);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[2 * e] = x[e] & 0xffffu, h[2 * e + 1] = x[e] >> 16;
-          } else {
+          for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              v[e] = 0.f;
-              if (n < cols && d + e < T.D) {
-                if (PARTS == 1) v[e] = __uint_as_float((uint32_t)__ldg((const unsigned short*)p + e) << 16);
-                else v[e] = __ldg((const float*)p + e);
-              }
-              h[e] = __float_as_uint(v[e]) >> 16;
-            }
-          }
-#pragma unroll
-          for (int part = 0; part < PARTS; ++part) {
-            if (PARTS > 1) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) h[e] = take_bf16(v[e]);
-            }
-            const uint32_t at = to + (part * 2 + (word >> 3)) * (kN * 128) + n * 128 + (((word & 7) ^ (n & 7)) << 4);
-            asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(h[0] | h[4] << 16), "r"(h[1] | h[5] << 16),
-                         "r"(h[2] | h[6] << 16), "r"(h[3] | h[7] << 16)
-                         : "memory");
-          }
+            for (int panel = 0; panel < 2; ++panel)
+              copy_box(base + WideShared::kX + xs * kXStage + (part * 2 + panel) * (kN * 128), &hidden, c * 128 + panel * 64,
+                         ((int)blockIdx.y * PARTS + part) * kN, x_full(xs));
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) barrier_arrive(x_full(xs));
       }
+      if (lost)
+        for (int xs = 0; xs < kXStages; ++xs)
+          for (uint32_t parity = 0; parity < 2; ++parity) (void)barrier_wait(x_full(xs), parity);
     }
   }
   __syncwarp();

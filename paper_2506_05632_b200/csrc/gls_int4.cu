@@ -55,8 +55,9 @@ static unsigned ctas_for(long long rows, int lanes) {
 // shared memory per hidden state
 static long long head_column_bytes(int parts, int chunks, int uc) { return (long long)parts * ((chunks + uc - 1) / uc) * uc * 256; }
 
-// The codes as bytes [V][ceil(D / 32) * 16], copied in boxes of `rows` rows by 64.
-static bool codes_map(const Int4Table& T, int rows, CUtensorMapSwizzle swizzle, CUtensorMap* map) {
+// A map of rows x columns, copied in boxes of `rows` rows by `cols` columns.
+static bool box_map(CUtensorMapDataType type, void* data, long long columns, long long rows, long long pitch_bytes, int box_columns,
+                    int box_rows, CUtensorMapSwizzle swizzle, CUtensorMap* map) {
   typedef decltype(&cuTensorMapEncodeTiled) Encode;
   static std::atomic<Encode> found{nullptr};
   Encode encode = found.load(std::memory_order_relaxed);
@@ -71,11 +72,15 @@ static bool codes_map(const Int4Table& T, int rows, CUtensorMapSwizzle swizzle, 
     encode = (Encode)p;
     found.store(encode, std::memory_order_relaxed);
   }
-  const cuuint64_t row = (cuuint64_t)((T.D + 31) / 32 * 16), dims[2] = {row, (cuuint64_t)T.V};
-  const cuuint64_t stride[1] = {T.V > 1 ? (cuuint64_t)T.code_stride : row};
-  const cuuint32_t box[2] = {64, (cuuint32_t)rows}, step[2] = {1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, T.codes, dims, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t dims[2] = {(cuuint64_t)columns, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)pitch_bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)box_columns, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  return encode(map, type, 2, data, dims, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The codes as bytes [V][ceil(D / 32) * 16]
+static bool codes_map(const Int4Table& T, int rows, CUtensorMapSwizzle swizzle, CUtensorMap* map) {
+  const long long row = (T.D + 31) / 32 * 16;
+  return box_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, T.codes, row, T.V, T.V > 1 ? T.code_stride : row, 64, rows, swizzle, map);
 }
 
 template <int GPC, int PARTS, int UC>
@@ -110,39 +115,61 @@ static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream
   return launch_head_unit<GPC, PARTS, 2>(A, codes, (int)(cols < want ? cols : want), warps, st);
 }
 
+// How many hidden states take the kernel for many of them, and how: passes of equal size, 16 .. 64 at a time.
+constexpr int kHeadFew = 8;
+struct WidePlan {
+  int passes, nb;  // nb: 16 hidden states each per pass
+  explicit WidePlan(long long N) : passes((int)((N + 63) / 64)), nb((int)((N + 16 * passes - 1) / (16 * passes))) {}
+  size_t bytes(int parts, long long D) const { return (size_t)passes * parts * nb * 16 * (size_t)((D + 127) / 128) * 256; }
+};
+
 template <int NB, int GPC, int PARTS>
-static cudaError_t launch_wide(const HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
+static cudaError_t launch_wide(const HeadArgs& A, const CUtensorMap& codes, int passes, void* workspace, cudaStream_t st) {
+  CUtensorMap hidden;
+  const long long columns = A.chunks * 128;
+  if (!box_map(CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, workspace, columns, (long long)passes * PARTS * 16 * NB, columns * 2, 64, 16 * NB,
+               CU_TENSOR_MAP_SWIZZLE_128B, &hidden))
+    return cudaErrorInvalidValue;
   const int smem = WideShared::total(NB, PARTS);
-  const cudaError_t err = cudaFuncSetAttribute(head_wide_kernel<NB, GPC, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  cudaError_t err = cudaFuncSetAttribute(head_wide_kernel<NB, GPC, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (err != cudaSuccess) return err;
-  const long long pairs = (A.T.V + 2 * kWideRows - 1) / (2 * kWideRows), most = sm_count();
-  dim3 grid((unsigned)(pairs < most ? pairs : most), (unsigned)((A.N + 16 * NB - 1) / (16 * NB)));
-  head_wide_kernel<NB, GPC, PARTS><<<grid, kWideThreads, smem, st>>>(A, codes);
-  return cudaGetLastError();
+  const long long pairs = (A.T.V + 2 * kWideRows - 1) / (2 * kWideRows), most = sm_count(), words = (long long)passes * 16 * NB * A.chunks * 16;
+  head_order_kernel<PARTS><<<(unsigned)(words < 256 * most ? (words + 255) / 256 : most), 256, 0, st>>>(A, 16 * NB, passes, (uint4*)workspace);
+  err = cudaGetLastError();
+  if (err != cudaSuccess) return err;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(pairs < most ? pairs : most), (unsigned)passes);
+  cfg.blockDim = dim3(kWideThreads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, head_wide_kernel<NB, GPC, PARTS>, A, codes, hidden);
 }
 
 template <int GPC, int PARTS>
-static cudaError_t launch_wide_for(const HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
-  // passes of equal size: 16 .. 64 hidden states
-  const int passes = (A.N + 63) / 64, nb = (A.N + 16 * passes - 1) / (16 * passes);
-  switch (nb) {
-    case 1: return launch_wide<1, GPC, PARTS>(A, codes, st);
-    case 2: return launch_wide<2, GPC, PARTS>(A, codes, st);
-    case 3: return launch_wide<3, GPC, PARTS>(A, codes, st);
-    default: return launch_wide<4, GPC, PARTS>(A, codes, st);
+static cudaError_t launch_wide_for(const HeadArgs& A, const CUtensorMap& codes, void* workspace, cudaStream_t st) {
+  const WidePlan P(A.N);
+  switch (P.nb) {
+    case 1: return launch_wide<1, GPC, PARTS>(A, codes, P.passes, workspace, st);
+    case 2: return launch_wide<2, GPC, PARTS>(A, codes, P.passes, workspace, st);
+    case 3: return launch_wide<3, GPC, PARTS>(A, codes, P.passes, workspace, st);
+    default: return launch_wide<4, GPC, PARTS>(A, codes, P.passes, workspace, st);
   }
 }
 
 template <int PARTS>
-static cudaError_t launch_head_for(HeadArgs& A, cudaStream_t st) {
+static cudaError_t launch_head_for(HeadArgs& A, void* workspace, cudaStream_t st) {
   CUtensorMap codes;
-  // more than one pass of the kernel for few hidden states takes longer than one of the other
-  const bool wide = A.N > 8;
+  const bool wide = A.N > kHeadFew;
   if (!codes_map(A.T, wide ? kWideRows : 16, wide ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, &codes)) return cudaErrorInvalidValue;
   switch (A.T.log_group) {
-    case 5: return wide ? launch_wide_for<4, PARTS>(A, codes, st) : launch_head<4, PARTS>(A, codes, st);
-    case 6: return wide ? launch_wide_for<2, PARTS>(A, codes, st) : launch_head<2, PARTS>(A, codes, st);
-    default: return wide ? launch_wide_for<1, PARTS>(A, codes, st) : launch_head<1, PARTS>(A, codes, st);
+    case 5: return wide ? launch_wide_for<4, PARTS>(A, codes, workspace, st) : launch_head<4, PARTS>(A, codes, st);
+    case 6: return wide ? launch_wide_for<2, PARTS>(A, codes, workspace, st) : launch_head<2, PARTS>(A, codes, st);
+    default: return wide ? launch_wide_for<1, PARTS>(A, codes, workspace, st) : launch_head<1, PARTS>(A, codes, st);
   }
 }
 
@@ -171,8 +198,13 @@ int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, co
   return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
 }
 
+size_t gls_head_logits_workspace_bytes(int64_t N, int64_t D, int x_dtype) {
+  if (N <= gls::kHeadFew || N > 65535 || D <= 0 || D > 32768 || !gls::float_type(x_dtype)) return 0;
+  return gls::WidePlan(N).bytes(x_dtype == GLS_BF16 ? 1 : 3, D);
+}
+
 int gls_head_logits(const void* x, int x_dtype, int64_t x_stride, int64_t N, const gls_int4_table_t* table, void* out,
-                    int out_dtype, int64_t out_stride, void* stream) {
+                    int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream) {
   using namespace gls;
   HeadArgs A;
   const int rc = table_of(table, &A.T);
@@ -188,14 +220,20 @@ int gls_head_logits(const void* x, int x_dtype, int64_t x_stride, int64_t N, con
     return GLS_ERR_INVALID_ARG;
   A.x = (const char*)x;
   A.x_stride = x_stride;
-  A.x_vec = (uintptr_t)x % 16 == 0 && (N == 1 || x_stride * xs % 16 == 0);
   A.N = (int)N;
   A.out = (char*)out;
   A.out_stride = out_stride;
   A.out_bf16 = out_dtype == GLS_BF16;
+  const size_t need = gls_head_logits_workspace_bytes(N, A.T.D, x_dtype);
+  if (need) {
+    if (!workspace || workspace_bytes < need) return GLS_ERR_WORKSPACE;
+    if ((uintptr_t)workspace % 16) return GLS_ERR_MISALIGNED;
+    if (rows_meet(out, N, N > 1 ? out_stride * os : table->V * os, table->V * os, workspace, 1, need, need)) return GLS_ERR_INVALID_ARG;
+  }
   A.chunks = (int)((A.T.D + 127) / 128);
   A.tiles = (A.T.V + 15) / 16;
-  const cudaError_t err = x_dtype == GLS_BF16 ? launch_head_for<1>(A, (cudaStream_t)stream) : launch_head_for<3>(A, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t err = x_dtype == GLS_BF16 ? launch_head_for<1>(A, workspace, st) : launch_head_for<3>(A, workspace, st);
   return err == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
 }
 

@@ -259,7 +259,6 @@ struct HeadArgs {
   int cols;            // hidden states per CTA row of the grid
   int chunks;          // of 128 columns
   int vec;             // a lane's scales and zeros of a unit are aligned vectors
-  int x_vec;           // 8 columns of a hidden state are aligned 16-byte words
   long long tiles;     // of 16 rows
 };
 
@@ -329,8 +328,8 @@ __device__ __forceinline__ uint2 lds8(uint32_t at) {
   return b;
 }
 
-// 64 bytes of 16 rows, from byte x of row y on; what lies outside the table comes as zeros
-__device__ __forceinline__ void copy_codes(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t barrier) {
+// A map's box, from column x of row y on; what lies outside comes as zeros
+__device__ __forceinline__ void copy_box(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t barrier) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to),
                "l"(map), "r"(x), "r"(y), "r"(barrier)
                : "memory");
@@ -458,7 +457,7 @@ __global__ void __launch_bounds__(32 * kHeadWarps, 1) head_kernel(const HeadArgs
       barrier_expect(bar, UC * 1024);
 #pragma unroll
       for (int c = 0; c < UC; ++c)
-        copy_codes(ring + stage * kStage + c * 1024, &codes, (l_unit * UC + c) * 64, (int)(l_tile * 16), bar);
+        copy_box(ring + stage * kStage + c * 1024, &codes, (l_unit * UC + c) * 64, (int)(l_tile * 16), bar);
     }
     scales[stage].load(A, l_tile * 16 + (lane >> 1), l_unit);
     if (++l_unit == upr) l_unit = 0, ++l_tile;

@@ -29,6 +29,7 @@ decltype(&gls_embed_tokens_backward_workspace_bytes) g_embed_backward_bytes = nu
 decltype(&gls_embed_tokens_backward) g_embed_backward = nullptr;
 decltype(&gls_sample_tokens) g_sample = nullptr;
 decltype(&gls_head_logits) g_head = nullptr;
+decltype(&gls_head_logits_workspace_bytes) g_head_bytes = nullptr;
 decltype(&gls_embed_tokens_int4) g_embed_int4 = nullptr;
 
 constexpr int64_t kMaxTop = 256;  // the library's largest `top`
@@ -412,8 +413,12 @@ PyObject* head_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
   shape.back() = t.V;
   std::optional<NoGil> free_others(std::in_place);
   const at::Tensor out = make(shape, type, dev);
-  const int rc = g_head(x.data_ptr(), dt, t.D, x.numel() / t.D, &t, out.data_ptr(), type == at::kFloat ? GLS_F32 : GLS_BF16, t.V,
-                        stream());
+  const int64_t N = x.numel() / t.D;
+  const size_t need = g_head_bytes(N, t.D, dt);
+  at::Tensor space;
+  if (need) space = make({(int64_t)need}, at::kByte, dev);
+  const int rc = g_head(x.data_ptr(), dt, t.D, N, &t, out.data_ptr(), type == at::kFloat ? GLS_F32 : GLS_BF16, t.V,
+                        need ? space.data_ptr() : nullptr, need, stream());
   free_others.reset();
   if (rc) return PyLong_FromLong(rc);
   return THPVariable_Wrap(out);
@@ -442,14 +447,14 @@ PyObject* embed_tokens_int4(PyObject*, PyObject* const* a, Py_ssize_t n) {
   CALL_END
 }
 
-// entry_points(addresses of the nine entry points, in the order of the variables above)
+// entry_points(addresses of the ten entry points, in the order of the variables above)
 PyObject* entry_points(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* p[9];
-  if (n != 9) {
-    PyErr_SetString(PyExc_TypeError, "nine addresses");
+  void* p[10];
+  if (n != 10) {
+    PyErr_SetString(PyExc_TypeError, "ten addresses");
     return nullptr;
   }
-  for (int i = 0; i < 9; ++i) {
+  for (int i = 0; i < 10; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
@@ -464,7 +469,8 @@ PyObject* entry_points(PyObject*, PyObject* const* a, Py_ssize_t n) {
   g_embed_backward = (decltype(g_embed_backward))p[5];
   g_sample = (decltype(g_sample))p[6];
   g_head = (decltype(g_head))p[7];
-  g_embed_int4 = (decltype(g_embed_int4))p[8];
+  g_head_bytes = (decltype(g_head_bytes))p[8];
+  g_embed_int4 = (decltype(g_embed_int4))p[9];
   Py_RETURN_NONE;
 }
 

@@ -102,7 +102,9 @@ class DraftBuffers:
             self.inputs = torch.empty((B, K, embedding.dim), dtype=inputs_dtype, device=device)
         elif embedding is not None:
             self.inputs = torch.empty((B, K, embedding.shape[1]), dtype=embedding.dtype, device=device)
-        self.workspace = torch.empty(binding.workspace_bytes(B, K, 1, V), dtype=torch.uint8, device=device)
+        # the head's use of it ends before the races' begins
+        need = max(binding.workspace_bytes(B, K, 1, V), binding.head_logits_workspace_bytes(B * K, head.dim, torch.float32))
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
 
 
@@ -115,7 +117,7 @@ def draft_position(hidden, j, buf, inv_temp=1.0, seed=0, seq_base=0, pos_base=0,
     `settings` are and whose log probabilities take the scores' place.  No result carries a gradient."""
     if not 0 <= j < buf.shape[2]:
         raise binding.GlsError("position %d of %d" % (j, buf.shape[2]))
-    binding.head_logits(hidden.detach(), buf.head, out=buf.logits[:, :, 0])
+    binding.head_logits(hidden.detach(), buf.head, workspace=buf.workspace, out=buf.logits[:, :, 0])
     if uniforms is None:
         if settings:
             raise binding.GlsError("the races take no %s" % ", ".join(sorted(settings)))

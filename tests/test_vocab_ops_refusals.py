@@ -11,7 +11,7 @@ from paper_2506_05632_b200 import binding
 
 pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="made-up pointers: only where no kernel can start")
 
-OK, INVALID, UNSUPPORTED, MISALIGNED = 0, 1, 2, 3
+OK, INVALID, UNSUPPORTED, MISALIGNED, WORKSPACE = 0, 1, 2, 3, 4
 P = 0x10000000  # an aligned address
 INF, NAN = float("inf"), float("nan")
 
@@ -58,15 +58,16 @@ BAD_TABLES = [
 @pytest.mark.parametrize("kw,status", BAD_TABLES)
 def test_bad_tables(kw, status):
     L, t = gls.load(), _table(**kw)
-    assert L.gls_head_logits(5 * P, 1, 128, 3, C.byref(t), 6 * P, 1, 50, None) == status
+    assert L.gls_head_logits(5 * P, 1, 128, 3, C.byref(t), 6 * P, 1, 50, None, 0, None) == status
     assert L.gls_quantize_table(5 * P, 1, 128, C.byref(t), None) == status
     assert L.gls_embed_tokens_int4(C.byref(t), 7 * P, 3, 1.0, 6 * P, 1, 128, None, None) == status
 
 
 def _head(**kw):
-    a = dict(x=5 * P, xd=1, xs=128, N=3, out=6 * P, od=1, os=50, t=_table())
+    a = dict(x=5 * P, xd=1, xs=128, N=3, out=6 * P, od=1, os=50, t=_table(), ws=None, n=0)
     a.update(kw)
-    return gls.load().gls_head_logits(a["x"], a["xd"], a["xs"], a["N"], C.byref(a["t"]) if a["t"] else None, a["out"], a["od"], a["os"], None)
+    return gls.load().gls_head_logits(a["x"], a["xd"], a["xs"], a["N"], C.byref(a["t"]) if a["t"] else None, a["out"], a["od"], a["os"], a["ws"], a["n"],
+                                      None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -74,7 +75,8 @@ def _head(**kw):
     (dict(xs=127), INVALID), (dict(os=49), INVALID), (dict(xd=2), UNSUPPORTED), (dict(od=-1), UNSUPPORTED),
     (dict(x=5 * P + 1), MISALIGNED), (dict(out=6 * P + 2, od=0), MISALIGNED), (dict(out=5 * P), INVALID), (dict(out=5 * P + 256), INVALID),
     (dict(out=P + 64), INVALID), (dict(out=2 * P - 100), INVALID), (dict(out=3 * P), INVALID), (dict(N=0), OK),
-    (dict(N=0, x=None, out=None), OK),
+    (dict(N=0, x=None, out=None), OK), (dict(N=9), WORKSPACE), (dict(N=9, ws=8 * P, n=100), WORKSPACE),
+    (dict(N=9, ws=8 * P + 8, n=1 << 20), MISALIGNED), (dict(N=9, ws=6 * P + 64, n=1 << 20), INVALID),
 ])
 def test_head_refusals(kw, status):
     assert _head(**kw) == status
@@ -119,3 +121,10 @@ def test_host_tensors_are_refused():
                  lambda: gls.quantize_table(torch.zeros(4, 8, requires_grad=True))):
         with pytest.raises(gls.GlsError, match="no gradient"):
             call()
+
+
+def test_workspace_sizes():
+    f = gls.head_logits_workspace_bytes
+    assert f(8, 4096, torch.bfloat16) == 0 and f(9, 4096, torch.bfloat16) == 16 * 4096 * 2
+    assert f(64, 4000, torch.float32) == 3 * 64 * 4096 * 2 and f(65, 100, torch.bfloat16) == 2 * 48 * 128 * 2
+    assert f(9, 32769, torch.bfloat16) == 0 and f(9, 0, torch.bfloat16) == 0
