@@ -7,30 +7,40 @@
 // The products of one group of columns end up in an accumulator of their own, which the same thread reads back, multiplies
 // by the group's scale and adds to its 64 sums in fp32: the scale never meets a rounding to fewer bits.  The tensor pipe
 // takes 8 instructions of 128 x 64 x 16 per 128 columns; the conversion, 11 operations per 8 codes, and the 64 multiply-adds
-// per group bind the kernel.
+// per row and group, and what they wait for, bind the kernel.
 //
-// A CTA has two warpgroups of that kind, each with 128 rows, which share the hidden states' tiles, and a third one: a
-// thread that requests the codes, one that requests the hidden states (both by tensor copies), one that issues the
-// products.  Everything is double buffered: while a group's product runs, its warpgroup converts the next group.  The hidden
-// states are put in order (and fp32 ones split into three bf16 parts) by a small kernel before: two warps of
-// each CTA that did so on the way took 1130 us where the copies take a fraction of it.
+// A CTA has two tiles of 128 rows at a time, which share the hidden states' tiles, and two warpgroups for each.  A
+// warpgroup takes every other group of columns of its tile: while one waits for its group's products the other converts
+// the next group (one warpgroup a tile, or two that share each group, wait most of the time: 251 us for 64 hidden states,
+// 152064 x 4096).  At the tile's end the two exchange halves of their sums.  Two more warps serve them: a thread that requests
+// codes and hidden states (tensor copies), one that issues the products.  The hidden states are put in order (and
+// fp32 ones split into three bf16 parts) by a small kernel before.
 #pragma once
 #include "gls_int4.cuh"
 
 namespace gls {
 
-constexpr int kWideThreads = 384, kWideCodeStages = 4, kWideRows = 128;
+constexpr int kWideThreads = 576, kWideCodeStages = 4, kWideRows = 128;
 
 struct WideShared {
   // offsets in bytes; tiles on 1024-byte boundaries
-  static constexpr int kCodes = 0;                                                     // [warpgroup][stage][128 rows][64]
+  static constexpr int kCodes = 0;                                                     // [tile][stage][128 rows][64]
   static constexpr int kX = 2 * kWideCodeStages * 8192;
   static __host__ __device__ constexpr int x_stage(int nb, int parts) { return parts * 2 * nb * 16 * 128; }  // [part][panel][row][128]
   static __host__ __device__ constexpr int x_stages(int parts) { return parts == 1 ? 4 : 2; }
   static __host__ __device__ constexpr int barriers(int nb, int parts) { return kX + x_stages(parts) * x_stage(nb, parts); }
-  static __host__ __device__ constexpr int total(int nb, int parts) { return 1024 + barriers(nb, parts) + 264; }  // the first kilobyte: up to a boundary
+  // scales and zeros of eight groups [8][512 threads] 8 bytes; at a tile's end, among the places of
+  // the tile's own threads, sums on their way [16][128] from either side
+  static __host__ __device__ constexpr int scales(int nb, int parts) { return barriers(nb, parts) + 512; }
+  static __host__ __device__ constexpr int total(int nb, int parts) { return 1024 + scales(nb, parts) + 32768; }  // the first kilobyte: up to a boundary
 };
 
+// one lane of a warp whose lanes are together: what it issues then has operands that the compiler knows to be the warp's
+__device__ __forceinline__ bool elected() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0u;
+}
 __device__ __forceinline__ void barrier_arrive(uint32_t at) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(at) : "memory");
 }
@@ -101,10 +111,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
                                                                    const __grid_constant__ CUtensorMap hidden) {
   extern __shared__ __align__(1024) char wide_shared[];
   constexpr int kN = 16 * NB, kXStages = WideShared::x_stages(PARTS), kXStage = WideShared::x_stage(NB, PARTS);
+  constexpr int kHalf = kN / 2;
   constexpr int kSteps = 8 / GPC;   // products of 16 columns per group
   constexpr int kWords = 16 / GPC;  // words of 8 codes per group and row
   const Int4Table& T = A.T;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, wg = warp >> 2;  // warpgroup 2 serves the other two
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, pair = warp >> 3, side = warp >> 2 & 1;  // a tile's warpgroups
   const uint32_t base = ((uint32_t)__cvta_generic_to_shared(wide_shared) + 1023u) & ~1023u;
   const uint32_t bars = base + WideShared::barriers(NB, PARTS);
   auto code_full = [&](int w, int s) { return bars + (w * kWideCodeStages + s) * 8; };
@@ -120,13 +131,13 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
   if (threadIdx.x == 0) {
     lost = 0;
     for (int w = 0; w < 2; ++w) {
-      for (int s = 0; s < kWideCodeStages; ++s) barrier_init(code_full(w, s), 1), barrier_init(code_free(w, s), 4);
+      for (int s = 0; s < kWideCodeStages; ++s) barrier_init(code_full(w, s), 1), barrier_init(code_free(w, s), GPC == 1 ? 4 : 8);
       for (int s = 0; s < 2; ++s) barrier_init(a_full(w, s), 4), barrier_init(d_full(w, s), 1);
     }
     for (int s = 0; s < kXStages; ++s) barrier_init(x_full(s), 1), barrier_init(x_free(s), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 9) {
+  if (warp == 17) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(tensor_at) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
@@ -145,165 +156,223 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
   const int mine = (int)((pairs - blockIdx.x + gridDim.x - 1) / gridDim.x);
   const int groups = T.G;  // per row; the last chunk may have fewer than GPC
 
-  if (wg < 2) {
-    // ---- a row per thread: codes -> first operand; accumulators -> sums
-    const int w4 = warp & 3;
+  if (pair < 2) {
+    // ---- a row per thread, every other group: codes -> first operand; accumulators -> sums
+    const int w4 = warp & 3, row = w4 * 32 + lane;
     const uint32_t lanes = (uint32_t)(w4 * 32) << 16;
-    const uint32_t a_at = tm + lanes + wg * 128, d_at = tm + lanes + 256 + wg * 128;  // two buffers of 64 columns each
-    const int row = w4 * 32 + lane;
-    long long unit = 0;   // groups so far
-    long long chunk = 0;  // chunks so far
+    const uint32_t a_at = tm + lanes + pair * 128 + side * 64, d_at = tm + lanes + 256 + pair * 128 + side * 64;
+    const uint32_t slot = base + WideShared::scales(NB, PARTS) + threadIdx.x * 8;  // scales: each thread its own copy
+    long long chunk = 0;  // so far, of all tiles
+    uint32_t used = 0u;   // how often the buffers were
     for (int i = 0; i < mine; ++i) {
-      const long long tile = blockIdx.x + (long long)i * gridDim.x, v = (tile * 2 + wg) * kWideRows + row;
+      const long long tile = blockIdx.x + (long long)i * gridDim.x, v = (tile * 2 + pair) * kWideRows + row;
       const long long vr = v < T.V ? v : T.V - 1;
       const char* const sp = (const char*)T.scales + vr * T.scale_stride * (T.scale_bf16 ? 2 : 4);
       const uint8_t* const zp = T.zeros ? T.zeros + vr * T.zero_stride : nullptr;
-      auto scale_of = [&](int g) {
-        return T.scale_bf16 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)sp + g) << 16) : __ldg((const float*)sp + g);
+      // Scales and zeros of eight groups at a time: a warp's read of 32 rows is 32 lines, whatever it takes of them.
+      uint32_t raw[8], zraw[2];
+      auto load_block = [&](int g0) {
+        zraw[0] = zraw[1] = 0x08080808u;
+        if (A.vec && g0 + 8 <= groups) {
+          if (T.scale_bf16) load_words<16>(raw, sp + g0 * 2);
+          else load_words<32>(raw, sp + g0 * 4);
+          if (zp) load_words<8>(zraw, (const char*)zp + g0);
+        } else {
+          if (zp) zraw[0] = zraw[1] = 0u;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool in = g0 + j < groups;
+            if (T.scale_bf16) {
+              const uint32_t h = in ? (uint32_t)__ldg((const unsigned short*)sp + g0 + j) : 0u;
+              if (j & 1) raw[j >> 1] |= h << 16;
+              else raw[j >> 1] = h;
+            } else {
+              raw[j] = in ? __ldg((const uint32_t*)sp + g0 + j) : 0u;
+            }
+            if (zp && in) zraw[j >> 2] |= (uint32_t)__ldg(zp + g0 + j) << (8 * (j & 3));
+          }
+        }
       };
-      auto zero_of = [&](int g) { return zp ? (uint32_t)__ldg(zp + g) & 15u : 8u; };
+      auto store_block = [&]() {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t f = !T.scale_bf16 ? raw[j] : j & 1 ? raw[j >> 1] & 0xffff0000u : raw[j >> 1] << 16;
+          const uint32_t z = __byte_perm(zraw[j >> 2] & 0x0f0f0f0fu, 0x43u, 0x4040u | (uint32_t)(j & 3) * 0x0101u);
+          asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(slot + j * 4096), "r"(f), "r"(z) : "memory");
+        }
+      };
+      load_block(0);
       float acc[kN];
 #pragma unroll
       for (int n = 0; n < kN; ++n) acc[n] = 0.f;
-      float scale = 0.f, next_scale = scale_of(0);
-      uint32_t next_zero = zero_of(0);
-      auto add_up = [&](long long u, float s) {  // the sums of group u, times its scale
-        wait(d_full(wg, (int)(u & 1)), (uint32_t)(u >> 1) & 1u);
+      for (int c = 0; c < A.chunks; ++c, ++chunk) {
+        if (GPC == 1 && (c & 1) != side) continue;
+        const int stage = (int)(chunk % kWideCodeStages);
+        wait(code_full(pair, stage), (uint32_t)(chunk / kWideCodeStages) & 1u);
         __syncwarp();
-        tensor_after();
-        constexpr int kAt = NB % 2 ? 1 : 2;  // sets of 16 read at a time
+        const uint32_t at = base + WideShared::kCodes + (pair * kWideCodeStages + stage) * 8192 + row * 64;
 #pragma unroll
-        for (int h = 0; h < NB; h += kAt) {
-          uint32_t d[16 * kAt];
+        for (int sub = GPC == 1 ? 0 : side; sub < GPC; sub += 2) {
+          const int g = c * GPC + sub;
+          if (g < groups) {
+            if ((g & 7) == side) store_block();
+            const uint2 sz = lds8(slot + (g & 7) * 4096);
+            if ((g & 7) == side + 2 && g - side + 6 < groups) load_block(g - side + 6);
 #pragma unroll
-          for (int j = 0; j < kAt; ++j) tensor_load16(d_at + (uint32_t)(u & 1) * 64 + (h + j) * 16, d + 16 * j);
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            for (int q = 0; q < kWords / 4; ++q) {
+              const int word = sub * (kWords / 4) + q;  // of 16 bytes
+              const uint4 k4 = lds16(at + ((word ^ (row >> 1 & 3)) << 4));
+              const uint32_t w[4] = {k4.x, k4.y, k4.z, k4.w};
+              uint32_t p[16];
 #pragma unroll
-          for (int n = 0; n < 16 * kAt; ++n) acc[h * 16 + n] = fmaf(s, __uint_as_float(d[n]), acc[h * 16 + n]);
-        }
-        tensor_before();
-      };
-      for (int g = 0; g < groups; ++g, ++unit) {
-        const int sub = g & (GPC - 1), stage = (int)(chunk % kWideCodeStages);
-        const float last_scale = scale;
-        scale = next_scale;
-        const uint32_t z = (0x4300u | next_zero) * 0x10001u;
-        if (g + 1 < groups) next_scale = scale_of(g + 1), next_zero = zero_of(g + 1);
-        if (sub == 0) wait(code_full(wg, stage), (uint32_t)(chunk / kWideCodeStages) & 1u);
-        __syncwarp();
-        const uint32_t at = base + WideShared::kCodes + (wg * kWideCodeStages + stage) * 8192 + row * 64;
+              for (int j = 0; j < 4; ++j) {
+                uint32_t t[4];
+                int4_pairs(w[j], sz.y, t);
 #pragma unroll
-        for (int q = 0; q < kWords / 4; ++q) {
-          const int word = sub * (kWords / 4) + q;  // of 16 bytes
-          const uint4 c = lds16(at + ((word ^ (row >> 1 & 3)) << 4));
-          const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-          uint32_t p[16];
+                for (int k = 0; k < 4; ++k) p[4 * j + k] = t[k];
+              }
+              tensor_store16(a_at + q * 16, p);
+            }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+            tensor_before();
+            __syncwarp();
+            if (lane == 0) {
+              barrier_arrive(a_full(pair, side));
+              if (GPC == 1 || sub + 2 >= GPC) barrier_arrive(code_free(pair, stage));
+            }
+            // the group's sums, times its scale
+            const float s = __uint_as_float(sz.x);
+            wait(d_full(pair, side), used & 1u);
+            ++used;
+            __syncwarp();
+            tensor_after();
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t t[4];
-            int4_pairs(w[j], z, t);
+            for (int h = 0; h < NB; ++h) {
+              uint32_t d[16];
+              tensor_load16(d_at + h * 16, d);
+              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-            for (int k = 0; k < 4; ++k) p[4 * j + k] = t[k];
+              for (int n = 0; n < 16; ++n) acc[h * 16 + n] = fmaf(s, __uint_as_float(d[n]), acc[h * 16 + n]);
+            }
+            tensor_before();
+          } else if (lane == 0 && (GPC == 1 || sub + 2 >= GPC)) {
+            barrier_arrive(code_free(pair, stage));
           }
-          tensor_store16(a_at + (uint32_t)(unit & 1) * 64 + q * 16, p);
         }
-        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-        tensor_before();
-        __syncwarp();
-        if (lane == 0) {
-          barrier_arrive(a_full(wg, (int)(unit & 1)));
-          if (sub == GPC - 1 || g == groups - 1) barrier_arrive(code_free(wg, stage));
-        }
-        if (sub == GPC - 1 || g == groups - 1) ++chunk;
-        if (g > 0) add_up(unit - 1, last_scale);
       }
-      add_up(unit - 1, scale);
+      // The tile's other warpgroup has the other groups' sums: each sends the half that it does not store, through the
+      // scales' place, up to 16 hidden states at a time.
+      const uint32_t out_box = base + WideShared::scales(NB, PARTS) + side * 16384 + pair * 2048 + row * 4;
+      const uint32_t in_box = side ? out_box - 16384 : out_box + 16384;
+      constexpr int kAt = kHalf < 16 ? kHalf : 16;
+      auto pair_sync = [&]() { asm volatile("bar.sync %0, 256;" ::"r"(1 + pair) : "memory"); };
+      pair_sync();
+#pragma unroll
+      for (int from = 0; from < kHalf; from += kAt) {
+#pragma unroll
+        for (int n = 0; n < kAt; ++n)
+          if (from + n < kHalf)
+            asm volatile("st.shared.f32 [%0], %1;" ::"r"(out_box + (n >> 2) * 4096 + (n & 3) * 512), "f"(side ? acc[from + n] : acc[kHalf + from + n]) : "memory");
+        pair_sync();
+#pragma unroll
+        for (int n = 0; n < kAt; ++n)
+          if (from + n < kHalf) {
+            float y;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(in_box + (n >> 2) * 4096 + (n & 3) * 512) : "memory");
+            // the first warpgroup's sum is the first term on both sides
+            if (side) acc[kHalf + from + n] = y + acc[kHalf + from + n];
+            else acc[from + n] += y;
+          }
+        pair_sync();
+      }
       const float bad = lost ? __uint_as_float(0x7fc00000u) : 0.f;
       if (v < T.V) {
 #pragma unroll
-        for (int n = 0; n < kN; ++n)
-          if (n < cols) {
-            const long long o = (long long)(n0 + n) * A.out_stride + v;
-            if (A.out_bf16) ((unsigned short*)A.out)[o] = (unsigned short)bf16_bits(acc[n] + bad);
-            else ((float*)A.out)[o] = acc[n] + bad;
-          }
-      }
-    }
-  } else if (warp == 8) {
-    // ---- codes of both warpgroups
-    if (lane == 0) {
-      long long chunk = 0;
-      for (int i = 0; i < mine; ++i) {
-        const long long tile = blockIdx.x + (long long)i * gridDim.x;
-        for (int c = 0; c < A.chunks; ++c, ++chunk) {
-          const int s = (int)(chunk % kWideCodeStages);
-          for (int w = 0; w < 2; ++w) {
-            if (chunk >= kWideCodeStages) wait(code_free(w, s), (uint32_t)(chunk / kWideCodeStages - 1) & 1u);
-            if (lost) continue;
-            barrier_expect(code_full(w, s), 8192);
-            copy_box(base + WideShared::kCodes + (w * kWideCodeStages + s) * 8192, &codes, c * 64, (int)((tile * 2 + w) * kWideRows), code_full(w, s));
+        for (int n = 0; n < kHalf; ++n) {
+          const int col = side * kHalf + n;
+          const float y = (side ? acc[kHalf + n] : acc[n]) + bad;
+          if (col < cols) {
+            const long long o = (long long)(n0 + col) * A.out_stride + v;
+            if (A.out_bf16) ((unsigned short*)A.out)[o] = (unsigned short)bf16_bits(y);
+            else ((float*)A.out)[o] = y;
           }
         }
       }
-      // nothing of its own is under way when the CTA ends: the warpgroups have waited for every copy, unless a wait ran out
-      if (lost)
-        for (int w = 0; w < 2; ++w)
-          for (int s = 0; s < kWideCodeStages; ++s)
-            for (uint32_t parity = 0; parity < 2; ++parity) (void)barrier_wait(code_full(w, s), parity);
     }
-  } else if (warp == 9) {
-    // ---- the products
-    if (lane == 0) {
-      constexpr uint32_t kind = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kWideRows >> 4) << 24;
-      long long unit = 0, chunk = 0;
-      for (int i = 0; i < mine; ++i) {
-        for (int c = 0; c < A.chunks; ++c, ++chunk) {
-          const int xs = (int)(chunk % kXStages);
-          wait(x_full(xs), (uint32_t)(chunk / kXStages) & 1u);
-          for (int sub = 0; sub < GPC && c * GPC + sub < groups; ++sub, ++unit) {
-            const int b = (int)(unit & 1);
-            for (int w = 0; w < 2; ++w) {
-              wait(a_full(w, b), (uint32_t)(unit >> 1) & 1u);
-              tensor_after();
-              if (!lost) {
-#pragma unroll
-                for (int part = 0; part < PARTS; ++part)
-#pragma unroll
-                  for (int k = 0; k < kSteps; ++k) {
-                    const int kk = sub * kSteps + k;  // of eight; four to a panel
-                    const uint32_t x = base + WideShared::kX + xs * kXStage + (part * 2 + (kk >> 2)) * (kN * 128) + (kk & 3) * 32;
-                    tensor_product(tm + 256 + w * 128 + b * 64, tm + w * 128 + b * 64 + k * 8, tensor_tile(x), kind, part + k > 0);
-                  }
-              }
-              tensor_commit(d_full(w, b));
-            }
-          }
-          tensor_commit(x_free(xs));
-        }
-      }
-    }
-  } else if (warp == 10) {
-    // ---- the hidden states
-    if (lane == 0) {
-      asm volatile("griddepcontrol.wait;" ::: "memory");  // the kernel that puts them in order
-      long long chunk = 0;
-      for (int i = 0; i < mine; ++i) {
-        for (int c = 0; c < A.chunks; ++c, ++chunk) {
-          const int xs = (int)(chunk % kXStages);
-          if (chunk >= kXStages) wait(x_free(xs), (uint32_t)(chunk / kXStages - 1) & 1u);
-          if (lost) continue;
+  } else if (warp == 16) {
+    // ---- hidden states, and codes of both tiles
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the kernel that puts the hidden states in order
+    uint32_t chunk = 0;
+    for (int i = 0; i < mine; ++i) {
+      const long long tile = blockIdx.x + (long long)i * gridDim.x;
+      for (int c = 0; c < A.chunks; ++c, ++chunk) {
+        const int s = (int)(chunk % kWideCodeStages), xs = (int)(chunk % kXStages);
+        if (chunk >= kXStages) wait(x_free(xs), (chunk / kXStages - 1) & 1u);
+        __syncwarp();
+        if (!lost && elected()) {
           barrier_expect(x_full(xs), (uint32_t)kXStage);
 #pragma unroll
           for (int part = 0; part < PARTS; ++part)
 #pragma unroll
             for (int panel = 0; panel < 2; ++panel)
               copy_box(base + WideShared::kX + xs * kXStage + (part * 2 + panel) * (kN * 128), &hidden, c * 128 + panel * 64,
-                         ((int)blockIdx.y * PARTS + part) * kN, x_full(xs));
+                       ((int)blockIdx.y * PARTS + part) * kN, x_full(xs));
+        }
+        for (int w = 0; w < 2; ++w) {
+          if (chunk >= kWideCodeStages) wait(code_free(w, s), (chunk / kWideCodeStages - 1) & 1u);
+          __syncwarp();
+          if (!lost && elected()) {
+            barrier_expect(code_full(w, s), 8192);
+            copy_box(base + WideShared::kCodes + (w * kWideCodeStages + s) * 8192, &codes, c * 64, (int)((tile * 2 + w) * kWideRows), code_full(w, s));
+          }
         }
       }
-      if (lost)
-        for (int xs = 0; xs < kXStages; ++xs)
-          for (uint32_t parity = 0; parity < 2; ++parity) (void)barrier_wait(x_full(xs), parity);
+    }
+    // nothing of its own is under way when the CTA ends: the others have waited for every copy, unless a wait ran out
+    if (lost) {
+      for (uint32_t parity = 0; parity < 2; ++parity) {
+        for (int s = 0; s < kWideCodeStages; ++s) (void)barrier_wait(code_full(0, s), parity), (void)barrier_wait(code_full(1, s), parity);
+        for (int xs = 0; xs < kXStages; ++xs) (void)barrier_wait(x_full(xs), parity);
+      }
+    }
+  } else {
+    // ---- the products
+    constexpr uint32_t kind = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kWideRows >> 4) << 24;
+    uint32_t chunk = 0, used[2] = {0u, 0u};  // how often the buffers of either side were
+    for (int i = 0; i < mine; ++i) {
+      for (int c = 0; c < A.chunks; ++c, ++chunk) {
+        const int xs = (int)(chunk % kXStages);
+        wait(x_full(xs), (chunk / kXStages) & 1u);
+        const uint64_t x_tile = tensor_tile(base + WideShared::kX + xs * kXStage);
+#pragma unroll
+        for (int sub = 0; sub < GPC; ++sub) {
+          if (c * GPC + sub >= groups) break;
+          const int b = GPC == 1 ? c & 1 : sub & 1;
+          const uint32_t phase = (b ? used[1] : used[0]) & 1u;
+          if (b) ++used[1];
+          else ++used[0];
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            wait(a_full(w, b), phase);
+            __syncwarp();
+            tensor_after();
+            if (elected()) {
+              if (!lost) {
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                  for (int k = 0; k < kSteps; ++k) {
+                    const int kk = sub * kSteps + k;  // of eight; four to a panel
+                    tensor_product(tm + 256 + w * 128 + b * 64, tm + w * 128 + b * 64 + k * 8,
+                                   x_tile + (uint64_t)(((part * 2 + (kk >> 2)) * (kN * 128) + (kk & 3) * 32) >> 4), kind, part + k > 0);
+                  }
+              }
+              tensor_commit(d_full(w, b));
+            }
+          }
+        }
+        if (elected()) tensor_commit(x_free(xs));
+      }
     }
   }
   __syncwarp();
@@ -311,7 +380,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
   __syncthreads();
   tensor_after();
   __syncwarp();
-  if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
+  if (warp == 17) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tm) : "memory");
 }
 
 }  // namespace gls

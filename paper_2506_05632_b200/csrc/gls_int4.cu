@@ -151,8 +151,12 @@ static cudaError_t launch_wide(const HeadArgs& A, const CUtensorMap& codes, int 
 }
 
 template <int GPC, int PARTS>
-static cudaError_t launch_wide_for(const HeadArgs& A, const CUtensorMap& codes, void* workspace, cudaStream_t st) {
+static cudaError_t launch_wide_for(HeadArgs& A, const CUtensorMap& codes, void* workspace, cudaStream_t st) {
   const WidePlan P(A.N);
+  const Int4Table& T = A.T;
+  // a thread's scales are those of eight groups
+  A.vec = (uintptr_t)T.scales % 16 == 0 && (T.V == 1 || T.scale_stride * (T.scale_bf16 ? 2 : 4) % 16 == 0) &&
+          (!T.zeros || ((uintptr_t)T.zeros % 8 == 0 && (T.V == 1 || T.zero_stride % 8 == 0)));
   switch (P.nb) {
     case 1: return launch_wide<1, GPC, PARTS>(A, codes, P.passes, workspace, st);
     case 2: return launch_wide<2, GPC, PARTS>(A, codes, P.passes, workspace, st);
