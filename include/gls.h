@@ -639,11 +639,11 @@ int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, co
 /*
  * Logits of hidden states: out[n,v] = sum over d of x[n,d] * element(v, d), the products of a group summed in
  * fp32 and multiplied by its scale in fp32, the sum rounded once to the output's type.  bf16 x goes in as it is, fp32 x
- * in three parts that hold all of its 24 bits.  Up to 8 rows of x take one kernel and no workspace (several passes over the
- * table where D is so large that shared memory holds fewer), more another one, 64 of them per pass.
+ * in three parts that hold all of its 24 bits.  Up to 8 rows of x take one kernel and no workspace (fewer where D is so
+ * large that shared memory does not hold them), more another one, 64 of them per pass over the table.
  *   x [N,D], out [N,V] of types x_dtype, out_dtype (fp32 or bf16), rows contiguous, strides in elements
  *   of at least D and V; N <= 65535, N = 0 is legal.  An out in the memory of x or of the table is refused.
- *   workspace  gls_head_logits_workspace_bytes(N, D, x_dtype) bytes (0 for N <= 8), 16-byte aligned; its contents on entry
+ *   workspace  gls_head_logits_workspace_bytes(N, D, x_dtype) bytes (0 for few rows), 16-byte aligned; its contents on entry
  *              are ignored
  * Scales are finite or NaN.
  */

@@ -4,6 +4,12 @@
 
 namespace gls {
 
+// one lane of a warp whose lanes are together: what it issues then has operands that the compiler knows to be the warp's
+__device__ __forceinline__ bool elected() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0u;
+}
 __device__ __forceinline__ void barrier_init(uint32_t at, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(at), "r"(count) : "memory");
 }

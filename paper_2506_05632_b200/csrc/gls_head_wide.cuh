@@ -12,15 +12,15 @@
 // A CTA has two tiles of 128 rows at a time, which share the hidden states' tiles, and two warpgroups for each.  A
 // warpgroup takes every other group of columns of its tile: while one waits for its group's products the other converts
 // the next group (one warpgroup a tile, or two that share each group, wait most of the time: 251 us for 64 hidden states,
-// 152064 x 4096).  At the tile's end the two exchange halves of their sums.  Two more warps serve them: a thread that requests
-// codes and hidden states (tensor copies), one that issues the products.  The hidden states are put in order (and
+// 152064 x 4096).  At the tile's end the two exchange halves of their sums.  Three more warps serve them: one that requests codes
+// and hidden states (tensor copies), one for either tile that issues the products.  The hidden states are put in order (and
 // fp32 ones split into three bf16 parts) by a small kernel before.
 #pragma once
 #include "gls_int4.cuh"
 
 namespace gls {
 
-constexpr int kWideThreads = 576, kWideCodeStages = 4, kWideRows = 128;
+constexpr int kWideThreads = 640, kWideCodeStages = 4, kWideRows = 128;
 
 struct WideShared {
   // offsets in bytes; tiles on 1024-byte boundaries
@@ -35,12 +35,6 @@ struct WideShared {
   static __host__ __device__ constexpr int total(int nb, int parts) { return 1024 + scales(nb, parts) + 32768; }  // the first kilobyte: up to a boundary
 };
 
-// one lane of a warp whose lanes are together: what it issues then has operands that the compiler knows to be the warp's
-__device__ __forceinline__ bool elected() {
-  uint32_t one;
-  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(one));
-  return one != 0u;
-}
 __device__ __forceinline__ void barrier_arrive(uint32_t at) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(at) : "memory");
 }
@@ -134,7 +128,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
       for (int s = 0; s < kWideCodeStages; ++s) barrier_init(code_full(w, s), 1), barrier_init(code_free(w, s), GPC == 1 ? 4 : 8);
       for (int s = 0; s < 2; ++s) barrier_init(a_full(w, s), 4), barrier_init(d_full(w, s), 1);
     }
-    for (int s = 0; s < kXStages; ++s) barrier_init(x_full(s), 1), barrier_init(x_free(s), 1);
+    for (int s = 0; s < kXStages; ++s) barrier_init(x_full(s), 1), barrier_init(x_free(s), 2);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 17) {
@@ -335,8 +329,9 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
         for (int xs = 0; xs < kXStages; ++xs) (void)barrier_wait(x_full(xs), parity);
       }
     }
-  } else {
-    // ---- the products
+  } else if (warp < 19) {
+    // ---- the products of a tile
+    const int w = warp - 17;
     constexpr uint32_t kind = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kWideRows >> 4) << 24;
     uint32_t chunk = 0, used[2] = {0u, 0u};  // how often the buffers of either side were
     for (int i = 0; i < mine; ++i) {
@@ -351,24 +346,21 @@ __global__ void __launch_bounds__(kWideThreads, 1) head_wide_kernel(const HeadAr
           const uint32_t phase = (b ? used[1] : used[0]) & 1u;
           if (b) ++used[1];
           else ++used[0];
+          wait(a_full(w, b), phase);
+          __syncwarp();
+          tensor_after();
+          if (elected()) {
+            if (!lost) {
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
-            wait(a_full(w, b), phase);
-            __syncwarp();
-            tensor_after();
-            if (elected()) {
-              if (!lost) {
+              for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-                for (int part = 0; part < PARTS; ++part)
-#pragma unroll
-                  for (int k = 0; k < kSteps; ++k) {
-                    const int kk = sub * kSteps + k;  // of eight; four to a panel
-                    tensor_product(tm + 256 + w * 128 + b * 64, tm + w * 128 + b * 64 + k * 8,
-                                   x_tile + (uint64_t)(((part * 2 + (kk >> 2)) * (kN * 128) + (kk & 3) * 32) >> 4), kind, part + k > 0);
-                  }
-              }
-              tensor_commit(d_full(w, b));
+                for (int k = 0; k < kSteps; ++k) {
+                  const int kk = sub * kSteps + k;  // of eight; four to a panel
+                  tensor_product(tm + 256 + w * 128 + b * 64, tm + w * 128 + b * 64 + k * 8,
+                                 x_tile + (uint64_t)(((part * 2 + (kk >> 2)) * (kN * 128) + (kk & 3) * 32) >> 4), kind, part + k > 0);
+                }
             }
+            tensor_commit(d_full(w, b));
           }
         }
         if (elected()) tensor_commit(x_free(xs));

@@ -115,8 +115,14 @@ static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream
   return launch_head_unit<GPC, PARTS, 2>(A, codes, (int)(cols < want ? cols : want), warps, st);
 }
 
-// How many hidden states take the kernel for many of them, and how: passes of equal size, 16 .. 64 at a time.
-constexpr int kHeadFew = 8;
+// Whether N hidden states take the kernel for many of them: beyond 8, or where shared memory holds so few that the other one
+// would take more than two passes over the table (152064 x 4096, groups of 128, 1 .. 8 bf16 hidden states by
+// the other one 78 .. 100 us, 9 .. 64 by this one 147 .. 190; 8 fp32 ones 233 in two passes and 209).
+static bool head_is_wide(long long N, int parts, long long D) {
+  const int chunks = (int)((D + 127) / 128);
+  return N > 8 || N * head_column_bytes(parts, chunks, 2) > 2 * (227 * 1024 - HeadLayout::fixed(4, 2, kHeadWarps));
+}
+// How: passes of equal size, 16 .. 64 hidden states at a time.
 struct WidePlan {
   int passes, nb;  // nb: 16 hidden states each per pass
   explicit WidePlan(long long N) : passes((int)((N + 63) / 64)), nb((int)((N + 16 * passes - 1) / (16 * passes))) {}
@@ -168,7 +174,7 @@ static cudaError_t launch_wide_for(HeadArgs& A, const CUtensorMap& codes, void* 
 template <int PARTS>
 static cudaError_t launch_head_for(HeadArgs& A, void* workspace, cudaStream_t st) {
   CUtensorMap codes;
-  const bool wide = A.N > kHeadFew;
+  const bool wide = head_is_wide(A.N, PARTS, A.T.D);
   if (!codes_map(A.T, wide ? kWideRows : 16, wide ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE, &codes)) return cudaErrorInvalidValue;
   switch (A.T.log_group) {
     case 5: return wide ? launch_wide_for<4, PARTS>(A, codes, workspace, st) : launch_head<4, PARTS>(A, codes, st);
@@ -203,8 +209,9 @@ int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, co
 }
 
 size_t gls_head_logits_workspace_bytes(int64_t N, int64_t D, int x_dtype) {
-  if (N <= gls::kHeadFew || N > 65535 || D <= 0 || D > 32768 || !gls::float_type(x_dtype)) return 0;
-  return gls::WidePlan(N).bytes(x_dtype == GLS_BF16 ? 1 : 3, D);
+  if (N <= 0 || N > 65535 || D <= 0 || D > 32768 || !gls::float_type(x_dtype)) return 0;
+  const int parts = x_dtype == GLS_BF16 ? 1 : 3;
+  return gls::head_is_wide(N, parts, D) ? gls::WidePlan(N).bytes(parts, D) : 0;
 }
 
 int gls_head_logits(const void* x, int x_dtype, int64_t x_stride, int64_t N, const gls_int4_table_t* table, void* out,

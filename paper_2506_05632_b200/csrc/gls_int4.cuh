@@ -453,7 +453,7 @@ __global__ void __launch_bounds__(32 * kHeadWarps, 1) head_kernel(const HeadArgs
   HeadScales<GPC, UC> scales[kHeadStages];
   auto request = [&](int stage) {
     const uint32_t bar = bars + stage * 8;
-    if (lane == 0) {
+    if (elected()) {
       barrier_expect(bar, UC * 1024);
 #pragma unroll
       for (int c = 0; c < UC; ++c)

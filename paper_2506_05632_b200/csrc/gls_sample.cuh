@@ -409,7 +409,7 @@ struct Sampler {
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(shared().ring[warp]), bars = (uint32_t)__cvta_generic_to_shared(shared().barriers[warp]);
     auto inside = [&](int g) { return shift == 0 && g * 1024LL >= row.mis && g * 1024LL + 1024 <= row.end; };
     auto request = [&](int g, int stage) {
-      if (lane == 0 && g < sets && inside(g)) {
+      if (g < sets && inside(g) && elected()) {
         barrier_expect(bars + stage * 8, Shared::kStage);
         copy_bulk(ring + stage * Shared::kStage, row.base + (long long)g * Shared::kStage, Shared::kStage, bars + stage * 8);
       }

@@ -132,6 +132,32 @@ def test_head_of_the_widest_rows(gls, xt):
     ref.check_logits(gls.head_logits(x, t, dtype=F32), x, t)
 
 
+@pytest.mark.parametrize("xt", [F32, BF16])
+def test_head_of_many_hidden_states(gls, xt):
+    for V, D, N, group in ((300, 130, 65, 128), (257, 1000, 130, 64), (5000, 96, 200, 32), (128, 8192, 24, 32), (1, 5, 9, 128),
+                           (40000, 160, 40, 64), (130, 128, 64, 128)):
+        for zeros in (False, True):
+            t = _table(gls, V, D, group, zeros, [F32, BF16][N % 2], V + N)
+            x = torch.randn((N, D), generator=_gen(N), device="cuda").to(xt)
+            room = torch.full((N, V + 5), 3.0, device="cuda")
+            gls.head_logits(x, t, out=room[:, 2:V + 2])
+            ref.check_logits(room[:, 2:V + 2], x, t, str((V, D, N, group, zeros)))
+            assert bool((room[:, :2] == 3).all()) and bool((room[:, V + 2:] == 3).all())
+
+
+def test_head_workspace(gls):
+    """A given workspace is used whatever it holds; one that is too small is refused; hidden states that lie anywhere."""
+    t = _table(gls, 700, 333, 32, True, BF16, 21)
+    store = torch.randn((20, 400), generator=_gen(21), device="cuda").to(BF16)
+    n = gls.head_logits_workspace_bytes(20, 333, BF16)
+    ws = torch.full((n + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+    for off in (0, 1, 7):
+        x = store[:, off:off + 333]
+        ref.check_logits(gls.head_logits(x, t, workspace=ws), x, t)
+    with pytest.raises(gls.GlsError):
+        gls.head_logits(x, t, workspace=ws[:n - 16])
+
+
 def test_head_of_large_vocabularies(gls):
     for V, D, N, group in ((50257, 1000, 3, 32), (128256, 256, 8, 128), (32000, 1024, 1, 64), (20000, 2048, 33, 128)):
         t = _table(gls, V, D, group, True, BF16, V)
