@@ -174,7 +174,7 @@ constexpr int kSampleList = 2048;
 // Shared memory: what the search needs lies where the sweep's rings were.
 template <int DT, int THREADS>
 struct SampleShared {
-  static constexpr int kStages = DT == kBF16 ? 3 : 2;
+  static constexpr int kStages = 2;
   static constexpr int kStage = DT == kBF16 ? 2048 : 4096;  // 1024 tokens
   union {
     struct {
@@ -349,14 +349,15 @@ struct Sampler {
     uint32_t n = 0u;
     for (int i = threadIdx.x; i < kSampleChunks; i += THREADS) cnt[i] = 0u;
     __syncthreads();
+    const float upto = top;  // +inf and NaN are masked
     auto hits_of = [&](const float (&a)[8]) {
       uint32_t h = 0u;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h |= (a[i] >= bound ? 1u : 0u) << i;
+      for (int i = 0; i < 8; ++i) h |= (a[i] >= bound && a[i] <= upto ? 1u : 0u) << i;
       return h;
     };
     const int lane = threadIdx.x & 31;
-    for_chunks([&](int) { n = 0u; }, [&](int, uint32_t, const float (&a)[8]) { n += __popc(hits_of(a)); },
+    for_chunks<true>([&](int) { n = 0u; }, [&](int, uint32_t, const float (&a)[8]) { n += __popc(hits_of(a)); },
                [&](int c) {
                  n = __reduce_add_sync(0xffffffffu, n);
                  if (lane == 0) cnt[c] = n;
@@ -377,7 +378,7 @@ struct Sampler {
       at += mine[i];
     }
     __syncthreads();
-    for_chunks([&](int c) { n = cnt[c]; },
+    for_chunks<true>([&](int c) { n = cnt[c]; },
                [&](int, uint32_t p, const float (&a)[8]) {
                  const uint32_t h = hits_of(a);
                  if (!__any_sync(0xffffffffu, h != 0u)) return;
@@ -386,7 +387,7 @@ struct Sampler {
 #pragma unroll
                  for (int i = 0; i < 8; ++i)
                    if (h >> i & 1u) {
-                     shared().key[to] = Row::key(a[i]);
+                     shared().key[to] = Row::key(a[i] + 0.f);
                      shared().place[to++] = p + i;
                    }
                  n += __shfl_sync(0xffffffffu, incl, 31);
@@ -399,7 +400,7 @@ struct Sampler {
   // Largest logit of each chunk and, SUM, per four chunks the sum of 2^(l c2 - r) with r their largest one
   // times c2, rounded (where that is beyond 1e30: of 2^((l - their largest) c2)), into the shared memory
   // of the cluster's first CTA.  A warp takes every so many-th four chunks; those that lie within the row come
-  // through a ring, two or three sets ahead.
+  // through a ring, two sets ahead.
   template <bool SUM>
   __device__ __forceinline__ void sweep(float c2) {
     constexpr int kStages = Shared::kStages;
@@ -516,18 +517,15 @@ struct Sampler {
         if (d < span) atomicAdd(&shared().count[d >> sft], 1u);
       }
     } else {
-      const float from = Row::value(lo);
-      for_chunks([](int) {},
+      const float from = Row::value(lo), upto = top;
+      for_chunks<true>([](int) {},
                  [&](int, uint32_t, const float (&a)[8]) {
-                   bool any = false;
 #pragma unroll
-                   for (int i = 0; i < 8; ++i) any |= a[i] >= from;
-                   if (!__any_sync(0xffffffffu, any)) return;
-#pragma unroll
-                   for (int i = 0; i < 8; ++i) {
-                     const uint32_t d = Row::key(a[i]) - lo;
-                     if (d < span) atomicAdd(&shared().count[d >> sft], 1u);
-                   }
+                   for (int i = 0; i < 8; ++i)
+                     if (a[i] >= from && a[i] <= upto) {
+                       const uint32_t d = Row::key(a[i] + 0.f) - lo;
+                       if (d < span) atomicAdd(&shared().count[d >> sft], 1u);
+                     }
                  },
                  [](int) {});
     }
@@ -775,10 +773,11 @@ struct Sampler {
     for (int c = threadIdx.x; c < kSampleChunks; c += THREADS) cnt[c] = 0u;
     __syncthreads();
     uint32_t n = 0u;
-    for_chunks([&](int) { n = 0u; },
+    const float value = Row::value(code);
+    for_chunks<true>([&](int) { n = 0u; },
                [&](int, uint32_t, const float (&a)[8]) {
 #pragma unroll
-                 for (int i = 0; i < 8; ++i) n += Row::key(a[i]) == code ? 1u : 0u;
+                 for (int i = 0; i < 8; ++i) n += a[i] == value ? 1u : 0u;
                },
                [&](int c) {
                  n = __reduce_add_sync(0xffffffffu, n);
@@ -1068,7 +1067,7 @@ __device__ __forceinline__ float sample_setting(const SampleSetting& s, long lon
 }
 
 template <int DT, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 768 / THREADS) sample_kernel(const SampleArgs A) {
+__global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) sample_kernel(const SampleArgs A) {
   typedef SampleRow<DT> Row;
   typedef SampleCalls<DT, THREADS> Calls;
   SampleShared<DT, THREADS>& sh = Sampler<DT, THREADS>::shared();
@@ -1174,14 +1173,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 768 / THREADS) s
     if (use_k) {
       // top-p needs the mass of all k
       const uint32_t lowest = use_p ? Row::kLowest : floor_code;
-      // At least k tokens reach the k-th largest chunk maximum; with more of them to keep than there are chunks, some
-      // six a chunk reach the smallest one, and where that does not do, further down.
-      uint32_t cut = Calls::kth_chunk(S, (uint32_t)kk < (uint32_t)S.nch ? (uint32_t)kk : (uint32_t)S.nch);
+      // At least k tokens reach the k-th largest chunk maximum.  With more of them to keep than there are chunks, a
+      // smaller one is taken that about 1.5 k tokens reach if they lie anywhere; where fewer than k do, one goes further down.
+      const int nth = kk <= S.nch ? kk : max(1, min(S.nch, (int)((float)S.nch * (1.f - __expf(-1.5f * (float)kk / (float)S.nch)))));
+      uint32_t cut = Calls::kth_chunk(S, (uint32_t)nth);
       bool limited = false;
       for (;;) {
         if (cut < lowest) cut = lowest;
         Calls::make_list(S, Row::value(cut));
-        if (kk <= 512) S.listed = Calls::gather(S, Row::value(cut));
+        if (kk <= kSampleList / 3 * 2) S.listed = Calls::gather(S, Row::value(cut));
         limited = Calls::kth(S, cut, (uint32_t)kk, &code, &take, &equal);
         if (limited || cut == lowest) break;
         const float v = Row::value(cut), further = v - (m - v) * 0.5f;
