@@ -344,12 +344,11 @@ struct Sampler {
 
   // The tokens with logits of `bound` and above -> shared().key and shared().place, in order of position; shared().list holds their chunks.
   // Sets `listed`; no more than there is room for, otherwise -1.
-  __device__ __forceinline__ void gather(float bound) {
+  __device__ __forceinline__ void gather(float bound, float upto) {
     uint32_t* const cnt = shared().count;  // per entry of the list
     uint32_t n = 0u;
     for (int i = threadIdx.x; i < kSampleChunks; i += THREADS) cnt[i] = 0u;
     __syncthreads();
-    const float upto = top;  // +inf and NaN are masked
     auto hits_of = [&](const float (&a)[8]) {
       uint32_t h = 0u;
 #pragma unroll
@@ -634,7 +633,7 @@ struct Sampler {
   // 1: found; 0: the set does not reach the goal, all of it stays; -1: the interval leaves it open.
   // Bins of one code have their mass from their count.  The masses of wider ones lie between their counts times the
   // weights at their ends, which leaves a few bins that the border may be in: the mass above those is summed in 64 bits
-  // and they are cut finer.
+  // and they are cut finer, among their own tokens only as soon as there is room for these.
   __device__ __forceinline__ int nucleus(uint32_t lo, uint32_t drop, bool own_total, bool counted, double share, double goal_lo, double goal_hi,
                                          uint32_t* code, uint32_t* take, uint32_t* equal) {
     const uint32_t first = lo;
@@ -760,6 +759,17 @@ struct Sampler {
         }
       } else if (upper < hi) {
         above += mass_of(upper + 1u, hi);
+      }
+      // few tokens left: they alone are looked at from here on
+      if (listed < 0) {
+        uint32_t mine = 0u, left;
+#pragma unroll 1
+        for (int j = 0; j < kPer; ++j) {
+          const uint32_t bin = kSampleBins - 1 - (threadIdx.x * kPer + j);
+          if (bin >= b0 && bin <= bin1) mine += shared().count[bin];
+        }
+        block_scan<THREADS>(mine, shared().ired, &left);
+        if (left <= (uint32_t)kSampleList) listed = SampleCalls<DT, THREADS>::gather(*this, Row::value(max(lower, first)), Row::value(edge));
       }
       hi = edge;
       if (lower > hi) lower = hi;
@@ -1041,8 +1051,8 @@ struct SampleCalls {
   }
   static __device__ __noinline__ uint32_t kth_chunk(S s, uint32_t k) { return s.kth_chunk(k); }
   static __device__ __noinline__ void make_list(S s, float bound) { s.make_list(bound); }
-  static __device__ __noinline__ int gather(S s, float bound) {
-    s.gather(bound);
+  static __device__ __noinline__ int gather(S s, float bound, float upto) {
+    s.gather(bound, upto);
     return s.listed;
   }
   static __device__ __noinline__ bool kth(S s, uint32_t lo, uint32_t k, uint32_t* code, uint32_t* take, uint32_t* equal) {
@@ -1181,7 +1191,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       for (;;) {
         if (cut < lowest) cut = lowest;
         Calls::make_list(S, Row::value(cut));
-        if (kk <= kSampleList / 3 * 2) S.listed = Calls::gather(S, Row::value(cut));
+        if (kk <= kSampleList / 3 * 2) S.listed = Calls::gather(S, Row::value(cut), m);  // +inf and NaN are masked
         limited = Calls::kth(S, cut, (uint32_t)kk, &code, &take, &equal);
         if (limited || cut == lowest) break;
         const float v = Row::value(cut), further = v - (m - v) * 0.5f;
@@ -1216,7 +1226,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     if (code < floor_code) code = floor_code, take = equal = 0u;
     if (S.listed < 0) {
       Calls::make_list(S, Row::value(code));
-      if (use_k || use_p || mp > 0.f) S.listed = Calls::gather(S, Row::value(code));
+      if (use_k || use_p || mp > 0.f) S.listed = Calls::gather(S, Row::value(code), m);
     }
     if (S.listed >= 0) {
       Calls::locate_listed(S, code, take < equal ? take : 0xffffffffu, (double)u, &pos, &total);
