@@ -76,7 +76,7 @@ def build(force=False, verbose=False, debug_bounds=False):
     if force or not os.path.exists(_LIB) or os.path.getmtime(_LIB) < max(os.path.getmtime(s) for s in srcs):
         cus = [s for s in srcs if s.endswith(".cu")]
         tmp = _LIB + ".tmp%d" % os.getpid()
-        cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+        cmd = ["nvcc", "--threads", "4", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
                "-shared", "-Xcompiler", "-fPIC", "-o", tmp] + cus
         if debug_bounds or os.environ.get("GLS_DEBUG_BOUNDS") == "1":
             cmd.insert(1, "-DGLS_DEBUG_BOUNDS")  # range checks of the kernels' own indices
