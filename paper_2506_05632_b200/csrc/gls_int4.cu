@@ -199,12 +199,13 @@ int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, co
   if (meets_table(weights, table->V, table->V > 1 ? weight_stride * es : table->D * es, table->D * es, A.T)) return GLS_ERR_INVALID_ARG;
   A.w = weights;
   A.stride = weight_stride;
-  A.vec = (uintptr_t)weights % 16 == 0 && (table->V == 1 || weight_stride * es % 16 == 0);
+  const bool vec = (uintptr_t)weights % 16 == 0 && (table->V == 1 || weight_stride * es % 16 == 0);
   A.lanes = lanes_for((long long)A.T.G << (A.T.log_group - 4), 1 << (A.T.log_group - 4));
   const unsigned grid = ctas_for(A.T.V, A.lanes);
   cudaStream_t st = (cudaStream_t)stream;
-  if (dtype == GLS_F32) quantize_kernel<kF32><<<grid, kInt4Threads, 0, st>>>(A);
-  else quantize_kernel<kBF16><<<grid, kInt4Threads, 0, st>>>(A);
+  void (*const kernel)(QuantizeArgs) = dtype == GLS_F32 ? (vec ? quantize_kernel<kF32, true> : quantize_kernel<kF32, false>)
+                                                        : (vec ? quantize_kernel<kBF16, true> : quantize_kernel<kBF16, false>);
+  kernel<<<grid, kInt4Threads, 0, st>>>(A);
   return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
 }
 
@@ -268,13 +269,17 @@ int gls_embed_tokens_int4(const gls_int4_table_t* table, const int32_t* tokens, 
   A.scale = scale;
   A.out = (char*)out;
   A.out_stride = out_stride;
-  A.vec = (uintptr_t)out % 16 == 0 && (N == 1 || out_stride * es % 16 == 0);
+  // fp32 rows go through shared memory even where they are aligned: a thread's 16 columns are four words there, and a warp's
+  // store of every fourth word takes longer (128256 x 4096: 578 us, 434 through shared memory; bf16 260 and 402)
+  const bool vec = out_dtype == GLS_BF16 && (uintptr_t)out % 16 == 0 && (N == 1 || out_stride * es % 16 == 0);
   A.status = device_status;
   A.lanes = lanes_for((A.T.D + 15) / 16, 1);
   const unsigned grid = ctas_for(N, A.lanes);
   cudaStream_t st = (cudaStream_t)stream;
-  if (out_dtype == GLS_F32) embed_int4_kernel<kF32><<<grid, kInt4Threads, 0, st>>>(A);
-  else embed_int4_kernel<kBF16><<<grid, kInt4Threads, 0, st>>>(A);
+  void (*const kernel)(EmbedInt4Args) = out_dtype == GLS_F32 ? embed_int4_kernel<kF32, false>
+                                        : vec                ? embed_int4_kernel<kBF16, true>
+                                                             : embed_int4_kernel<kBF16, false>;
+  kernel<<<grid, kInt4Threads, 0, st>>>(A);
   return cudaGetLastError() == cudaSuccess ? GLS_OK : GLS_ERR_CUDA;
 }
 

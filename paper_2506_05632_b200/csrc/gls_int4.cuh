@@ -34,6 +34,8 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return d;
 }
 constexpr int kInt4Threads = 256;
+// place of a row's column among those that a warp's lanes exchange through shared memory: 16 to a lane, 17 apart
+__device__ __forceinline__ int swap_at(int column) { return (column >> 4) * 17 + (column & 15); }
 
 // ------------------------------------------------------------------------------------------
 // Weights -> table.  A group's 32 .. 128 columns lie in 2 .. 8 neighbouring lanes, 16 columns each; the extremes meet
@@ -48,17 +50,19 @@ struct QuantizeArgs {
   const void* w;
   long long stride;  // elements
   Int4Table T;
-  int vec;           // 1: 16 columns of a row are aligned 16-byte words
   int lanes;         // threads per row, a power of two
 };
 
-template <int DT>
+template <int DT, bool VEC>  // VEC: 16 columns of a row are aligned 16-byte words
 __global__ void __launch_bounds__(kInt4Threads) quantize_kernel(const QuantizeArgs A) {
   constexpr int ES = DT == kBF16 ? 2 : 4, kCols = 16;
   const Int4Table& T = A.T;
   const int per_group = 1 << (T.log_group - 4);  // lanes
   const int units = T.G * per_group, D = (int)T.D;
   const int at = threadIdx.x & (A.lanes - 1), rows = kInt4Threads / A.lanes;
+  const int L = min(A.lanes, 32), l = threadIdx.x & (L - 1);  // lanes side by side in a row
+  __shared__ float turns[VEC ? 1 : kInt4Threads * 17];
+  float* const turn = turns + (VEC ? 0 : (threadIdx.x - l) * 17);
   const int bytes = (D + 1) >> 1;
   for (long long v0 = (long long)blockIdx.x * rows; v0 < T.V; v0 += (long long)gridDim.x * rows) {
     const long long v = v0 + threadIdx.x / A.lanes;
@@ -69,7 +73,7 @@ __global__ void __launch_bounds__(kInt4Threads) quantize_kernel(const QuantizeAr
       const int n = !live || d >= D ? 0 : min(D - d, kCols);
       float x[kCols];
       const char* p = row + (long long)d * ES;
-      if (A.vec && n == kCols) {
+      if (VEC && n == kCols) {
 #pragma unroll
         for (int i = 0; i < kCols * ES / 16; ++i) {
           const uint4 q = ld_stream16(p + 16 * i);
@@ -80,13 +84,26 @@ __global__ void __launch_bounds__(kInt4Threads) quantize_kernel(const QuantizeAr
             else x[4 * i + j] = __uint_as_float(w[j]);
           }
         }
-      } else {
+      } else if (VEC) {
 #pragma unroll
         for (int i = 0; i < kCols; ++i) {
           x[i] = 0.f;
           if (i < n)
             x[i] = DT == kBF16 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)p + i) << 16) : __ldg((const float*)p + i);
         }
+      } else {  // columns by neighbouring lanes, 16 each out of shared memory
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) {
+          const int col = (unit - l) * kCols + i * L + l;
+          float y = 0.f;
+          if (v < T.V && col < D)
+            y = DT == kBF16 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)row + col) << 16) : __ldg((const float*)row + col);
+          turn[swap_at(i * L + l)] = y;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) x[i] = turn[swap_at(l * kCols + i)];
       }
       float lo = 0.f, hi = 0.f, odd = 0.f;
 #pragma unroll
@@ -156,33 +173,36 @@ struct EmbedInt4Args {
   float scale;
   char* out;
   long long out_stride;  // elements
-  int vec, lanes;
+  int lanes;             // threads per row, a power of two
   uint32_t* status;
 };
 
-template <int DT>
+template <int DT, bool VEC>  // VEC: 16 columns of a row of the output are aligned 16-byte words
 __global__ void __launch_bounds__(kInt4Threads) embed_int4_kernel(const EmbedInt4Args A) {
   constexpr int ES = DT == kBF16 ? 2 : 4;
   const Int4Table& T = A.T;
   const int units = (int)((T.D + 15) >> 4), D = (int)T.D;
   const int at = threadIdx.x & (A.lanes - 1), rows = kInt4Threads / A.lanes;
+  const int L = min(A.lanes, 32), l = threadIdx.x & (L - 1);  // lanes side by side in a row
+  __shared__ float turns[VEC ? 1 : kInt4Threads * 17];
+  float* const turn = turns + (VEC ? 0 : (threadIdx.x - l) * 17);
   const long long step = (long long)gridDim.x * rows;
   long long n = (long long)blockIdx.x * rows + threadIdx.x / A.lanes;
   int next = n < A.N ? __ldg(A.tokens + n) : -1;
-  for (; n < A.N; n += step) {
+  for (long long n0 = (long long)blockIdx.x * rows; n0 < A.N; n0 += step, n += step) {  // the same for every lane
     const int t = next;
     if (n + step < A.N) next = __ldg(A.tokens + n + step);
-    const bool live = t >= 0 && t < T.V;
-    if (t >= T.V && at == 0 && A.status) atomicOr(A.status, 2u);
+    const bool row_there = n < A.N, live = row_there && t >= 0 && t < T.V;
+    if (row_there && t >= T.V && at == 0 && A.status) atomicOr(A.status, 2u);
     const long long v = live ? t : 0;
     const uint8_t* const codes = T.codes + v * T.code_stride;
     const char* const scales = (const char*)T.scales + v * T.scale_stride * (T.scale_bf16 ? 2 : 4);
     const uint8_t* const zeros = T.zeros + (T.zeros ? v * T.zero_stride : 0);
     char* const row = A.out + n * A.out_stride * ES;
-    for (int unit = at; unit < units; unit += A.lanes) {
-      const int d = unit * 16;
+    for (int first = 0; first < units; first += A.lanes) {
+      const int unit = first + at, d = unit * 16;
       float y[16];
-      if (live) {
+      if (live && unit < units) {
         const uint2 w = __ldg((const uint2*)(codes + unit * 8));  // a row's codes fill 16-byte words
         const int g = unit >> (T.log_group - 4);
         const float s = T.scale_bf16 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)scales + g) << 16) : __ldg((const float*)scales + g);
@@ -203,23 +223,40 @@ __global__ void __launch_bounds__(kInt4Threads) embed_int4_kernel(const EmbedInt
         for (int i = 0; i < 16; ++i) y[i] = 0.f;
       }
       char* const q = row + (long long)d * ES;
-      if (A.vec && d + 16 <= D) {
-        if constexpr (DT == kBF16) {
+      if (VEC) {
+        if (!row_there || unit >= units) continue;
+        if (d + 16 <= D) {
+          if constexpr (DT == kBF16) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            ((uint4*)q)[h] = make_uint4(bf16_pair(y[8 * h], y[8 * h + 1]), bf16_pair(y[8 * h + 2], y[8 * h + 3]),
-                                        bf16_pair(y[8 * h + 4], y[8 * h + 5]), bf16_pair(y[8 * h + 6], y[8 * h + 7]));
+            for (int h = 0; h < 2; ++h)
+              ((uint4*)q)[h] = make_uint4(bf16_pair(y[8 * h], y[8 * h + 1]), bf16_pair(y[8 * h + 2], y[8 * h + 3]),
+                                          bf16_pair(y[8 * h + 4], y[8 * h + 5]), bf16_pair(y[8 * h + 6], y[8 * h + 7]));
+          } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h) ((float4*)q)[h] = make_float4(y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]);
+          }
         } else {
 #pragma unroll
-          for (int h = 0; h < 4; ++h) ((float4*)q)[h] = make_float4(y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]);
+          for (int i = 0; i < 16; ++i)
+            if (d + i < D) {
+              if constexpr (DT == kBF16) ((unsigned short*)q)[i] = (unsigned short)bf16_bits(y[i]);
+              else ((float*)q)[i] = y[i];
+            }
         }
-      } else {
+      } else {  // out of shared memory, columns by neighbouring lanes
+        __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (d + i < D) {
-            if constexpr (DT == kBF16) ((unsigned short*)q)[i] = (unsigned short)bf16_bits(y[i]);
-            else ((float*)q)[i] = y[i];
+        for (int i = 0; i < 16; ++i) turn[swap_at(l * 16 + i)] = y[i];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int col = (unit - l) * 16 + i * L + l;
+          const float x = turn[swap_at(i * L + l)];
+          if (row_there && col < D) {
+            if constexpr (DT == kBF16) ((unsigned short*)row)[col] = (unsigned short)bf16_bits(x);
+            else ((float*)row)[col] = x;
           }
+        }
       }
     }
   }
