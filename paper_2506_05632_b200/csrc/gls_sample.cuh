@@ -990,6 +990,48 @@ struct Sampler {
     return ok;
   }
 
+  // All of it for no more listed tokens than threads, which are at least the first `k` of the order or all of it: a thread has
+  // one, finds its place in the order by comparing it with the others, and top-p's border and the token that u falls to
+  // are scans over the threads.
+  __device__ __forceinline__ void pick(uint32_t k, bool use_p, double share, uint32_t floor_code, double u, uint32_t* pos, double* total_out) {
+    const int i = threadIdx.x;
+    const bool have = i < listed;
+    const uint32_t mine = have ? shared().key[i] : 0u;
+    uint32_t rank = 0u;
+    for (int j = 0; j < listed; ++j) {
+      const uint32_t other = shared().key[j];
+      rank += other > mine || (other == mine && j < i) ? 1u : 0u;
+    }
+    const double w = have ? weight(Row::value(mine)) : 0.0;
+    double total;
+    if (use_p) {
+      shared().psum[i] = 0.0;
+      __syncthreads();
+      if (have && rank < k) shared().psum[rank] = w;
+      __syncthreads();
+      const double x = shared().psum[i], front = block_scan<THREADS>(x, shared().wred, &total);
+      const uint32_t stay = (uint32_t)__syncthreads_count((uint32_t)i < k && i < listed && front < share * total);
+      if (stay < k) k = stay ? stay : 1u;
+    }
+    const bool kept = have && (rank < k && mine >= floor_code || rank == 0u);
+    const double y = kept ? w : 0.0, f = block_scan<THREADS>(y, shared().wred, &total);
+    double x = u * total;
+    const double most = total * (1.0 - 1.2e-16);
+    if (x > most) x = most;
+    if (i == 0) shared().found = 0, shared().at = 0u;
+    __syncthreads();
+    if (y > 0.0) {
+      atomicMax(&shared().at, (uint32_t)i);  // the last one with weight, for borders that rounding leaves without x
+      if (f <= x && x < f + y) {
+        shared().pos = shared().place[i];
+        shared().found = 1;
+      }
+    }
+    __syncthreads();
+    *pos = shared().found ? shared().pos : shared().place[shared().at];
+    *total_out = total;
+  }
+
   // The same among the listed tokens, of which the first `take` (by position) of the code `code` and those above it stay.
   __device__ __forceinline__ void locate_listed(uint32_t code, uint32_t take, double u, uint32_t* pos, double* total_out) {
     const int each = (listed + THREADS - 1) / THREADS, from = min((int)threadIdx.x * each, listed), upto = min(from + each, listed);
@@ -1066,6 +1108,10 @@ struct SampleCalls {
   static __device__ __noinline__ void exact_sums(S s, Kept kept) { s.exact_sums(kept); }
   static __device__ __noinline__ bool locate(S s, Kept kept, double u, int size, double slack, uint32_t* pos, double* total) {
     return s.locate(kept, u, size, slack, pos, total);
+  }
+  static __device__ __noinline__ void pick(S s, uint32_t k, bool use_p, double share, uint32_t floor_code, double u, uint32_t* pos,
+                                           double* total) {
+    s.pick(k, use_p, share, floor_code, u, pos, total);
   }
   static __device__ __noinline__ void locate_listed(S s, uint32_t code, uint32_t take, double u, uint32_t* pos, double* total) {
     s.locate_listed(code, take, u, pos, total);
@@ -1192,13 +1238,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
         if (cut < lowest) cut = lowest;
         Calls::make_list(S, Row::value(cut));
         if (kk <= kSampleList / 3 * 2) S.listed = Calls::gather(S, Row::value(cut), m);  // +inf and NaN are masked
+        if (S.listed >= 0 && S.listed <= THREADS && (S.listed >= kk || cut == lowest)) {
+          Calls::pick(S, (uint32_t)kk, use_p, (double)p, floor_code, (double)u, &pos, &total);
+          done = true;
+          break;
+        }
         limited = Calls::kth(S, cut, (uint32_t)kk, &code, &take, &equal);
         if (limited || cut == lowest) break;
         const float v = Row::value(cut), further = v - (m - v) * 0.5f;
         cut = further < v && further > -3.402823466e38f ? Row::key(further) : lowest;
       }
       if (!limited) take = equal = 0u, code = cut;
-      if (use_p && Calls::nucleus(S, code, equal - take, true, false, (double)p, 0.0, 0.0, &pc, &pt, &pe) == 1) code = pc, take = pt, equal = pe;
+      if (!done && use_p && Calls::nucleus(S, code, equal - take, true, false, (double)p, 0.0, 0.0, &pc, &pt, &pe) == 1) code = pc, take = pt, equal = pe;
     } else if (use_p) {
       double goal = S.total_mass(), slack = eps;
       uint32_t was = 0u;
@@ -1224,11 +1275,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       }
     }
     if (code < floor_code) code = floor_code, take = equal = 0u;
-    if (S.listed < 0) {
+    if (!done && S.listed < 0) {
       Calls::make_list(S, Row::value(code));
       if (use_k || use_p || mp > 0.f) S.listed = Calls::gather(S, Row::value(code), m);
     }
-    if (S.listed >= 0) {
+    if (done) {
+    } else if (S.listed >= 0) {
       Calls::locate_listed(S, code, take < equal ? take : 0xffffffffu, (double)u, &pos, &total);
     } else {
       kept.from = Row::value(code);
