@@ -622,9 +622,15 @@ struct Sampler {
     if (!(front < goal)) return 0u;
     const double q = (goal - front) / w;
     uint32_t r = q >= (double)n ? n : (uint32_t)q;
-    while (r > 0u && !(front + (double)(r - 1u) * w < goal)) --r;
-    while (r < n && front + (double)r * w < goal) ++r;
-    return r;
+    // off by its rounding; by more than one where many such weights are less than a step of the sum: by halving
+    if ((r == 0u || front + (double)(r - 1u) * w < goal) && (r == n || !(front + (double)r * w < goal))) return r;
+    uint32_t lo = 0u, hi = n;
+    while (lo < hi) {
+      const uint32_t c = lo + (hi - lo) / 2u;
+      if (front + (double)c * w < goal) lo = c + 1u;
+      else hi = c;
+    }
+    return lo;
   }
 
   // Least kept code under top-p among the codes >= lo (of those at lo, `drop` do not belong to the set).
@@ -1216,11 +1222,21 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       const double ln = log((double)mp);
       float edge = (float)((double)m + ln / S.it);
       if (!(edge >= -3.402823466e38f)) edge = -3.402823466e38f;
-      uint32_t e = Row::key(edge);
       const uint32_t hi = Row::key(m);
-      if (e > hi) e = hi;
-      while (e < hi && !(((double)Row::value(e) - (double)m) * S.it >= ln)) ++e;
-      while (e > Row::kLowest && ((double)Row::value(e - 1) - (double)m) * S.it >= ln) --e;
+      uint32_t e = min(Row::key(edge), hi);
+      const auto keeps = [&](uint32_t c) { return ((double)Row::value(c) - (double)m) * S.it >= ln; };
+      // The edge is off by its rounding, most often by no code or one.  Around zero codes lie far closer than the
+      // 64-bit difference tells apart (a million of them for ordinary settings): there by halving.
+      if (!keeps(e)) e = min(e + 1u, hi);
+      if ((e < hi && !keeps(e)) || (e > Row::kLowest && keeps(e - 1u))) {
+        uint32_t below = Row::kLowest;
+        e = hi;  // always kept
+        while (below < e) {
+          const uint32_t c = below + (e - below) / 2u;
+          if (keeps(c)) e = c;
+          else below = c + 1u;
+        }
+      }
       floor_code = e;
     }
     uint32_t code = floor_code;         // the least kept one
@@ -1279,10 +1295,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       Calls::make_list(S, Row::value(code));
       if (use_k || use_p || mp > 0.f) S.listed = Calls::gather(S, Row::value(code), m);
     }
-    if (done) {
-    } else if (S.listed >= 0) {
+    if (!done && S.listed >= 0) {
       Calls::locate_listed(S, code, take < equal ? take : 0xffffffffu, (double)u, &pos, &total);
-    } else {
+    } else if (!done) {
       kept.from = Row::value(code);
       if (take < equal) kept.end = Calls::equal_end(S, code, take);
       Calls::exact_sums(S, kept);

@@ -222,3 +222,14 @@ def test_refusals(gls):
             gls.sample_tokens(**a)
     with torch.no_grad():
         gls.sample_tokens(x.clone().requires_grad_(), u)
+
+
+@pytest.mark.parametrize("most,inv_temp,min_p", [(3.3137195, 0.10763583, 0.7), (3.4443467, 0.103553735, 0.7), (2.37963, 0.9676231, 0.1),
+                                                 (2.776235, 0.82939124, 0.1)])
+def test_border_of_min_p_around_zero(gls, most, inv_temp, min_p):
+    """ln(min_p) / inv_temp + the largest logit is zero but for 1e-15: the 64-bit difference holds up to a million
+    neighbouring codes for equal.  Logits around it, and far smaller than that difference's step."""
+    x = torch.tensor([most, 0.0, 1e-30, -1e-30, 1e-14, -1e-14, 1e-8, -1e-8, -2.4424904e-15, 1e-45, -1.0, most / 2] * 3, device="cuda")
+    x = x.view(1, 1, 1, 36).expand(1, 1, 64, 36).contiguous()
+    u = ((torch.arange(64, device="cuda") + 0.5) / 64).view(1, 1, 64)
+    _check(gls, x, u, inv_temp=ref.f32(inv_temp), min_p=ref.f32(min_p))
