@@ -240,7 +240,10 @@ int gls_head_logits(const void* x, int x_dtype, int64_t x_stride, int64_t N, con
   if (need) {
     if (!workspace || workspace_bytes < need) return GLS_ERR_WORKSPACE;
     if ((uintptr_t)workspace % 16) return GLS_ERR_MISALIGNED;
-    if (rows_meet(out, N, N > 1 ? out_stride * os : table->V * os, table->V * os, workspace, 1, need, need)) return GLS_ERR_INVALID_ARG;
+    if (rows_meet(out, N, N > 1 ? out_stride * os : table->V * os, table->V * os, workspace, 1, need, need) ||
+        rows_meet(x, N, N > 1 ? x_stride * xs : table->D * xs, table->D * xs, workspace, 1, need, need) ||
+        meets_table(workspace, 1, need, need, A.T))
+      return GLS_ERR_INVALID_ARG;
   }
   A.chunks = (int)((A.T.D + 127) / 128);
   A.tiles = (A.T.V + 15) / 16;

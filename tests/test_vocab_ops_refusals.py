@@ -128,3 +128,9 @@ def test_workspace_sizes():
     assert f(8, 4096, torch.bfloat16) == 0 and f(9, 4096, torch.bfloat16) == 16 * 4096 * 2
     assert f(64, 4000, torch.float32) == 3 * 64 * 4096 * 2 and f(65, 100, torch.bfloat16) == 2 * 48 * 128 * 2
     assert f(9, 32769, torch.bfloat16) == 0 and f(9, 0, torch.bfloat16) == 0
+
+
+@pytest.mark.parametrize("ws", [5 * P, 5 * P + 1024, P, 2 * P, 3 * P])
+def test_workspace_that_meets_an_input(ws):
+    """Hidden states and the table are read after the workspace has been written."""
+    assert _head(N=9, ws=ws, n=1 << 20) == INVALID
