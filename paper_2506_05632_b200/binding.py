@@ -1069,7 +1069,12 @@ def _no_gradient(name, *tensors):
 def _setting(s, name, value, dtype, lead, dev):
     """Puts one sampling setting, a number or a tensor [B], [B,K] or [B,K,J] (sizes of 1 broadcast), into s."""
     if not isinstance(value, torch.Tensor):
-        setattr(s, name, int(value) if dtype is _I32 else float(value))
+        if dtype is not _I32:
+            setattr(s, name, float(value))
+        elif value != value or value in (float("inf"), -float("inf")) or int(value) != value:
+            raise GlsError("%s must be a whole number" % name)
+        else:
+            setattr(s, name, max(-1, min(int(value), 2 ** 31 - 1)))  # neither end restricts
         return
     n = value.dim()
     if value.dtype is not dtype or value.get_device() != dev or not 1 <= n <= 3 or any(

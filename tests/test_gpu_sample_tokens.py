@@ -233,3 +233,10 @@ def test_border_of_min_p_around_zero(gls, most, inv_temp, min_p):
     x = x.view(1, 1, 1, 36).expand(1, 1, 64, 36).contiguous()
     u = ((torch.arange(64, device="cuda") + 0.5) / 64).view(1, 1, 64)
     _check(gls, x, u, inv_temp=ref.f32(inv_temp), min_p=ref.f32(min_p))
+
+
+def test_top_k_beyond_32_bits(gls):
+    x, u = _logits((2, 1, 8, 500), torch.float32, 31), torch.rand((2, 1, 8), generator=_gen(32), device="cuda")
+    want = gls.sample_tokens(x, u)
+    for k in (2 ** 31, 2 ** 40 + 5, -2 ** 40 + 5):
+        assert torch.equal(gls.sample_tokens(x, u, top_k=k)["tokens"], want["tokens"])

@@ -134,3 +134,17 @@ def test_workspace_sizes():
 def test_workspace_that_meets_an_input(ws):
     """Hidden states and the table are read after the workspace has been written."""
     assert _head(N=9, ws=ws, n=1 << 20) == INVALID
+
+
+@pytest.mark.parametrize("k,value", [(5, 5), (0, 0), (-7, -1), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1), (2 ** 40 + 5, 2 ** 31 - 1),
+                                     (-2 ** 40 + 5, -1), (7.0, 7), (True, 1)])
+def test_top_k_beyond_32_bits(k, value):
+    s = binding._Sampling()
+    binding._setting(s, "top_k", k, torch.int32, (1, 1, 1), 0)
+    assert s.top_k == value
+
+
+@pytest.mark.parametrize("k", [0.5, 50.9, NAN, INF])
+def test_top_k_that_is_no_whole_number(k):
+    with pytest.raises(gls.GlsError, match="whole number"):
+        binding._setting(binding._Sampling(), "top_k", k, torch.int32, (1, 1, 1), 0)
