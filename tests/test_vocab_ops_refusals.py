@@ -148,3 +148,9 @@ def test_top_k_beyond_32_bits(k, value):
 def test_top_k_that_is_no_whole_number(k):
     with pytest.raises(gls.GlsError, match="whole number"):
         binding._setting(binding._Sampling(), "top_k", k, torch.int32, (1, 1, 1), 0)
+
+
+@pytest.mark.parametrize("name", ["inv_temp", "top_p", "min_p"])
+def test_settings_that_want_a_gradient(name):
+    with pytest.raises(gls.GlsError, match="no gradient"):
+        gls.sample_tokens(torch.zeros(1, 1, 1, 8), torch.zeros(1, 1, 1), **{name: torch.ones(1, requires_grad=True)})
