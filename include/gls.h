@@ -572,8 +572,8 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
  * the first token of the order always stays.  Drawn is the first token BY INDEX whose cumulative mass among the
  * kept ones exceeds u times their total (u = 1: the last kept one); its log probability is among the
  * kept ones.  inv_temp = +inf is the limit of low temperature: the first token of the order, log probability 0.
- * What is decided is decided by sums of 64-bit exponentials (the border of top_p among codes of several
- * values by integer multiples of 2^-(62 - log2 V) of the largest weight); equal calls return equal tokens.
+ * What is decided is decided by counts and by 64-bit sums of 64-bit exponentials; fp32 sums decide only where the border is
+ * further than 5e-7 of the total away.  Equal calls return equal tokens.
  *
  *   logits         [B,K,J,V] rows (fp32 or bf16, any alignment of their first elements)
  *   uniforms       fp32 [B,K,J], each within [0, 1]

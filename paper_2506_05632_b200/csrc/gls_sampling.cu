@@ -36,6 +36,13 @@ static cudaError_t launch_sample(SampleArgs& A, long long rows, int ctas, cudaSt
   return cudaLaunchKernelEx(&cfg, sample_kernel<DT, THREADS>, A);
 }
 
+// whether a row may need a total over all its tokens: neither all rows have a top-k, nor all a min-p without a top-p
+static bool may_sum(const SampleArgs& A) {
+  const bool top_k = !A.top_k.rows && A.top_k.ivalue > 0 && A.top_k.ivalue < A.V, greedy = !A.inv_temp.rows && std::isinf(A.inv_temp.value);
+  const bool min_p = !A.min_p.rows && A.min_p.value > 0.f && !A.top_p.rows && A.top_p.value >= 1.f;
+  return !top_k && !greedy && !min_p;
+}
+
 template <int DT>
 static cudaError_t launch_sample_rows(SampleArgs& A, long long rows, cudaStream_t st) {
   // as few positions per chunk as leave the row no more chunks than there is room for
@@ -44,9 +51,13 @@ static cudaError_t launch_sample_rows(SampleArgs& A, long long rows, cudaStream_
   // few rows: several CTAs sweep one, so that most SMs have a share of it
   const int sms = sm_count();
   if (A.V <= 8192) return launch_sample<DT, 128>(A, rows, 1, st);
-  // many rows: small CTAs hide one another's waits; up to four an SM: large ones, so that a row that takes long is done sooner
-  // (512 rows of 128256 with settings of their own 177 us, by small ones 236)
-  if (rows * 2 > sms) return rows > 4 * sms ? launch_sample<DT, 256>(A, rows, 1, st) : launch_sample<DT, 512>(A, rows, 1, st);
+  // More rows than SMs: four small CTAs an SM hide one another's waits, a large one is done sooner with a row that has to be
+  // summed in 64 bits.  128256 bf16 tokens, the same rows, small / large: top-k 50 and top-p 0.9, 200 rows 33 / 40 us,
+  // 592 59 / 88, 888 90 / 126; min-p 0.05, 592 46 / 63; top-k 1000 alone 592 170 / 185, but 296 115 / 90; where rows may be
+  // summed, settings of their own, 200 rows 192-220 / 110-129, 512 222-236 / 139-193, 888 262-319 / 225-241, 2048 409-435 /
+  // 436-470; nothing restricted, 592 115-132 / 81-113, 888 135 / 123-141, 2048 195-200 / 240-262.
+  if (rows * 2 > sms)
+    return rows > (may_sum(A) ? 4 : 1) * (long long)sms ? launch_sample<DT, 256>(A, rows, 1, st) : launch_sample<DT, 512>(A, rows, 1, st);
   int ctas = 2;
   while (ctas < 8 && rows * ctas * 2 <= sms && A.V > 8192 * ctas) ctas *= 2;
   return launch_sample<DT, 512>(A, rows, ctas, st);

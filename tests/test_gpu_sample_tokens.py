@@ -240,3 +240,13 @@ def test_top_k_beyond_32_bits(gls):
     want = gls.sample_tokens(x, u)
     for k in (2 ** 31, 2 ** 40 + 5, -2 ** 40 + 5):
         assert torch.equal(gls.sample_tokens(x, u, top_k=k)["tokens"], want["tokens"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_more_rows_than_multiprocessors(gls, dtype):
+    """Rows of more than 8192 tokens by each size of CTA: between one and four a multiprocessor the settings choose."""
+    for rows in (200, 700):
+        x, u = _logits((rows, 1, 1, 9001), dtype, 41), torch.rand((rows, 1, 1), generator=_gen(42), device="cuda")
+        for kw in (dict(), dict(top_k=50, top_p=0.9), dict(min_p=0.05), dict(top_p=0.9), dict(top_p=0.9, min_p=0.05), dict(inv_temp=INF),
+                   dict(top_k=torch.full((rows,), 50, dtype=torch.int32, device="cuda"))):
+            _check(gls, x, u, what=(rows, kw.keys()), **kw)
