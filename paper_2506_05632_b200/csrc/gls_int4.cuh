@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kInt4Threads) embed_int4_kernel(const EmbedInt
 // A CTA has a range of tiles of 16 rows, cut into units of UC chunks of 128 columns; each warp takes a run of
 // units of equal length, whatever the tiles, and streams them through a ring of its own: a tensor copy of 64 bytes of 16
 // rows per chunk, which leaves what a warp reads at once side by side.  (Bulk copies row by row take one lane after
-// the other: 262 instead of 130 instructions per chunk.)  The scales and zeros of a unit are requested when its codes are and stored
+// the other: 262 instead of 150 instructions per chunk.)  The scales and zeros of a unit are requested when its codes are and stored
 // beside them as pairs (fp32 scale, bf16 zero twice).  A tile that two or more warps share is added up at the end.
 // ------------------------------------------------------------------------------------------
 struct HeadArgs {
