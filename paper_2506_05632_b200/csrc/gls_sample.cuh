@@ -1201,7 +1201,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
   const double eps = A.shift ? 2.5e-7 + 0.84e-7 * (11.5 + A.shift) + 6e-8 * (16.0 + 8.0 * (double)(4 << A.shift)) : 5e-7;
   double total = 0.0;
   uint32_t pos = S.row.mis;
-  bool done = false;
+  bool done = false, swept = false;
   if (need_sum) {
     for (int g = threadIdx.x; g < kSampleChunks; g += THREADS) {
       double y = 0.0;
@@ -1213,7 +1213,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       sh.psum[g] = y;
     }
     __syncthreads();
-    if (!use_p) done = Calls::locate(S, kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
+    if (!use_p) done = swept = Calls::locate(S, kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
   }
   if (!done) {
     // the least code that min-p keeps
@@ -1309,7 +1309,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     if (A.logprobs) {
       const float x = DT == kBF16 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)S.row.base + pos) << 16)
                                   : __ldg((const float*)S.row.base + pos);
-      A.logprobs[r] = (float)(((double)x - (double)m) * S.it - log(total));
+      // Sums of the sweep are relative to the row's largest logit, 64-bit ones to weights in which that one's is not quite 1
+      // (2e-15): over its own weight a token that is kept alone has log probability 0, and none has more.
+      const double w = swept ? 0.0 : S.weight(x);
+      A.logprobs[r] = fminf((float)(w > 0.0 ? log(w / total) : ((double)x - (double)m) * S.it - log(total)), 0.f);
     }
   }
 }

@@ -250,3 +250,16 @@ def test_more_rows_than_multiprocessors(gls, dtype):
         for kw in (dict(), dict(top_k=50, top_p=0.9), dict(min_p=0.05), dict(top_p=0.9), dict(top_p=0.9, min_p=0.05), dict(inv_temp=INF),
                    dict(top_k=torch.full((rows,), 50, dtype=torch.int32, device="cuda"))):
             _check(gls, x, u, what=(rows, kw.keys()), **kw)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1909, 37903])
+def test_a_token_kept_alone_has_log_probability_zero(gls, V, dtype):
+    x, u = _logits((24, 2, 1, V), dtype, 51, spread=4.0), torch.rand((24, 2, 1), generator=_gen(52), device="cuda")
+    per_row = torch.ones(24, dtype=torch.int32, device="cuda")
+    for kw in (dict(top_k=1), dict(top_k=1, top_p=0.9, min_p=0.02, inv_temp=2.0), dict(inv_temp=INF), dict(top_k=per_row, inv_temp=0.8),
+               dict(top_p=1e-6, inv_temp=1.25)):
+        lp = gls.sample_tokens(x, u, **kw)["logprobs"]
+        assert torch.equal(lp, torch.zeros_like(lp)), (kw.keys(), float(lp.min()), float(lp.max()))
+    for kw in (dict(), dict(top_k=50), dict(top_p=0.9), dict(inv_temp=20.0), dict(min_p=0.05, inv_temp=20.0)):
+        assert bool((gls.sample_tokens(x, u, **kw)["logprobs"] <= 0).all()), kw
