@@ -253,8 +253,8 @@ struct Sampler {
     // c is rounded, by the same for all weights; where that is too much the difference comes first (logits that far
     // from 0 and different from the largest have no weight)
     if (!(fabs(c) < 1073741824.0)) base = m, c = 0.0;
-    least = (float)((double)m - 1000.0 / it2);
-    if (!(least >= -3.402823466e38f)) least = -3.402823466e38f;
+    // rounded up: at low temperatures a step of fp32 is many exponents, and weight_of's range ends at 2^-1022
+    least = __double2float_ru((double)m - 1000.0 / it2);
   }
   // 2^((x - top) it2) to 2e-13 for x >= least: 2^n 2^(i / 16) 2^r with |r| <= 1 / 32, the last by its series (ten
   // operations in 64 bits and a conversion; exp() takes about three times as many).  Sixteen table entries have a pair of banks
