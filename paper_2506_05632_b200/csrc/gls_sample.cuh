@@ -241,31 +241,27 @@ struct Sampler {
   int nch, shift;
   int listed;      // tokens in shared().key, or -1
   double it, it2;  // inverse temperature, the same to base 2
-  double c;        // exponent of a logit x: (x - base) it2 - c, where one of base and c is 0
-  float base;
+  double top64;    // the largest logit; exponent of a logit x: (x - top64) it2
   float top;       // the largest logit
   float least;     // below it weights are 0
 
   __device__ __forceinline__ void set_top(float m) {
     top = m;
-    c = (double)m * it2;
-    base = 0.f;
-    // c is rounded, by the same for all weights; where that is too much the difference comes first (logits that far
-    // from 0 and different from the largest have no weight)
-    if (!(fabs(c) < 1073741824.0)) base = m, c = 0.0;
+    top64 = (double)m;
     // rounded up: at low temperatures a step of fp32 is many exponents, and weight_of's range ends at 2^-1022
-    least = __double2float_ru((double)m - 1000.0 / it2);
+    least = __double2float_ru(top64 - 1000.0 / it2);
   }
   // 2^((x - top) it2) to 2e-13 for x >= least: 2^n 2^(i / 16) 2^r with |r| <= 1 / 32, the last by its series (ten
-  // operations in 64 bits and a conversion; exp() takes about three times as many).  Sixteen table entries have a pair of banks
+  // operations in 64 bits and a conversion; exp() takes about three times as many).  The largest logit's is 1, so that sums and
+  // shares of equal ones are exact.  Sixteen table entries have a pair of banks
   // each; with 64 a warp's reads wait for one another (7.8 a clock and SM).
   // (a number below 2^-1022 where it is not wanted, without a branch)
   __device__ __forceinline__ double weight_of(float x, bool wanted = true) const {
-    const double t = fma((double)(x - base), it2, -c);
+    const double d = (double)x - top64;
     const double magic = 6755399441055744.0 / 16.0;  // 1.5 * 2^48: sixteenths in the lowest bits
-    const double big = t + magic;
+    const double big = fma(d, it2, magic);
     const int n = __double2loint(big);
-    const double r = t - (big - magic);
+    const double r = fma(d, it2, magic - big);
     double q = 1.3333558146428443e-3;  // ln2^5 / 5!
     q = fma(q, r, 9.6181291076284772e-3);
     q = fma(q, r, 5.5504108664821580e-2);
@@ -1201,7 +1197,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
   const double eps = A.shift ? 2.5e-7 + 0.84e-7 * (11.5 + A.shift) + 6e-8 * (16.0 + 8.0 * (double)(4 << A.shift)) : 5e-7;
   double total = 0.0;
   uint32_t pos = S.row.mis;
-  bool done = false, swept = false;
+  bool done = false;
   if (need_sum) {
     for (int g = threadIdx.x; g < kSampleChunks; g += THREADS) {
       double y = 0.0;
@@ -1213,7 +1209,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       sh.psum[g] = y;
     }
     __syncthreads();
-    if (!use_p) done = swept = Calls::locate(S, kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
+    if (!use_p) done = Calls::locate(S, kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
   }
   if (!done) {
     // the least code that min-p keeps
@@ -1309,10 +1305,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
     if (A.logprobs) {
       const float x = DT == kBF16 ? __uint_as_float((uint32_t)__ldg((const unsigned short*)S.row.base + pos) << 16)
                                   : __ldg((const float*)S.row.base + pos);
-      // Sums of the sweep are relative to the row's largest logit, 64-bit ones to weights in which that one's is not quite 1
-      // (2e-15): over its own weight a token that is kept alone has log probability 0, and none has more.
-      const double w = swept ? 0.0 : S.weight(x);
-      A.logprobs[r] = fminf((float)(w > 0.0 ? log(w / total) : ((double)x - (double)m) * S.it - log(total)), 0.f);
+      // none is positive: a total of the sweep may be below 1 by its rounding
+      A.logprobs[r] = fminf((float)(((double)x - (double)m) * S.it - log(total)), 0.f);
     }
   }
 }
