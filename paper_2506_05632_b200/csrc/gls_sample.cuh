@@ -392,8 +392,13 @@ struct Sampler {
     __syncthreads();
   }
 
+  // Whether a set's sum is relative to ref, its largest logit times c2, rounded: the rounding stays in the exponents of all its
+  // terms, half of one at most up to 2^24.  Beyond it (126 at 2^31: every term 0 or infinite) the largest logit is taken off
+  // before the product.
+  static __device__ __forceinline__ bool by_product(float ref) { return fabsf(ref) < 16777216.f; }
+
   // Largest logit of each chunk and, SUM, per four chunks the sum of 2^(l c2 - r) with r their largest one
-  // times c2, rounded (where that is beyond 1e30: of 2^((l - their largest) c2)), into the shared memory
+  // times c2, rounded (where by_product does not hold: of 2^((l - their largest) c2)), into the shared memory
   // of the cluster's first CTA.  A warp takes every so many-th four chunks; those that lie within the row come
   // through a ring, two sets ahead.
   template <bool SUM>
@@ -438,7 +443,7 @@ struct Sampler {
         odd |= !(mm < CUDART_INF_F);
         const float ref = mm * c2;
         if (SUM && mm > -CUDART_INF_F) {
-          odd |= !(fabsf(ref) < 1e30f);
+          odd |= !by_product(ref);
           float t[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -497,7 +502,7 @@ struct Sampler {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     }
-    if (SUM && fabsf(mm * c2) < 1e30f) s *= ex2_approx(fmaf(mm, c2, -(mm * c2)));  // to the reference that sets without odd logits have
+    if (SUM && by_product(mm * c2)) s *= ex2_approx(fmaf(mm, c2, -(mm * c2)));  // to the reference that sets without odd logits have
     return s;
   }
 
@@ -895,12 +900,14 @@ struct Sampler {
   }
 
   // The token that u falls to by shared().psum, whose entries hold 2^size positions each.  slack: relative error of those sums;
-  // false where it leaves the token open.
+  // false where it leaves the token open, or where there is no mass.
   __device__ __forceinline__ bool locate(const Kept& kept, double u, int size, double slack, uint32_t* pos, double* total_out) {
     double mine = 0.0, total;
 #pragma unroll
     for (int i = 0; i < kPerC; ++i) mine += shared().psum[threadIdx.x * kPerC + i];
     double before = block_scan<THREADS>(mine, shared().wred, &total);
+    *total_out = total;
+    if (!(total > 0.0 && total < CUDART_INF)) return false;  // no entry to look into
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
     if (x > most) x = most;
@@ -986,7 +993,6 @@ struct Sampler {
     }
     __syncthreads();
     *pos = shared().pos;
-    *total_out = total;
     const bool ok = shared().found != 0;
     __syncthreads();
     return ok;
@@ -1204,7 +1210,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       if (4 * g < S.nch) {
         const float mm = fmaxf(fmaxf(sh.cmax[4 * g], sh.cmax[4 * g + 1]), fmaxf(sh.cmax[4 * g + 2], sh.cmax[4 * g + 3]));
         if (mm > -CUDART_INF_F)
-          y = (double)sh.csum[g] * (fabsf(mm * c2) < 1e30f ? exp2((double)(mm * c2) - (double)m * (double)c2) : S.weight(mm));
+          y = (double)sh.csum[g] * (S.by_product(mm * c2) ? exp2((double)(mm * c2) - (double)m * (double)c2) : S.weight(mm));
       }
       sh.psum[g] = y;
     }
