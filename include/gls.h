@@ -573,7 +573,10 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
  * kept ones exceeds u times their total (u = 1: the last kept one); its log probability is among the
  * kept ones.  inv_temp = +inf is the limit of low temperature: the first token of the order, log probability 0.
  * What is decided is decided by counts and by 64-bit sums of 64-bit exponentials; fp32 sums decide only where the border is
- * further than 5e-7 of the total away.  Equal calls return equal tokens.
+ * further away than their error can move it.  Log probabilities are rounded to fp32 from 64 bits where top_k, top_p or min_p
+ * restricts the row.  Where none does, their total is a sum in fp32 that is off by at most 1.3e-6 of itself (1.3e-7 more for each
+ * doubling of V beyond 2^18), for a token that has more than half of it at most 1.3e-6 of what the others have.  Equal
+ * calls return equal tokens.
  *
  *   logits         [B,K,J,V] rows (fp32 or bf16, any alignment of their first elements)
  *   uniforms       fp32 [B,K,J], each within [0, 1]

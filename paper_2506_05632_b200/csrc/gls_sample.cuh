@@ -18,8 +18,8 @@
 //              their ordered codes and refining the bin the border falls into
 //     sums     the kept tokens' mass per chunk, in 64 bits; the chunk that u falls into; the token inside it
 // Decisions are those of exact arithmetic but for 64-bit rounding: sums that decide something are 64-bit sums of
-// exponentials good to 2e-13, and counts.  The sweep's fp32 sums decide only where the border is further away than 5e-7 of the
-// total, twenty times what their rounding leaves; otherwise the row is summed again in 64 bits.
+// exponentials good to 2e-13, and counts.  The sweep's fp32 sums decide only where the border is further away than they can be
+// off at all (1.3e-6 of what they hold); otherwise the row is summed again in 64 bits.
 #pragma once
 #include "gls_async.cuh"
 #include "gls_kernels.cuh"
@@ -478,7 +478,8 @@ struct Sampler {
   template <bool SUM>
   __device__ __forceinline__ float sweep_carefully(int g, float c2, float (&m)[4]) {
     const int lane = threadIdx.x & 31;
-    float mm = -CUDART_INF_F, s = 0.f;
+    float mm = -CUDART_INF_F;
+    double s = 0.0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       m[q] = -CUDART_INF_F;
@@ -490,20 +491,17 @@ struct Sampler {
         m[q] = fmaxf(m[q], b);
         const float nm = fmaxf(mm, b);
         if (SUM && nm > -CUDART_INF_F) {
-          float t = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) t += ex2_approx((a[i] - nm) * c2);
-          s = s * (mm > -CUDART_INF_F ? ex2_approx((mm - nm) * c2) : 0.f) + t;
+          for (int i = 0; i < 8; ++i) a[i] = ex2_approx((a[i] - nm) * c2);
+          if (nm > mm) s *= mm > -CUDART_INF_F ? exp2(((double)mm - (double)nm) * (double)c2) : 0.0;
+          s += (double)(((a[0] + a[1]) + (a[2] + a[3])) + ((a[4] + a[5]) + (a[6] + a[7])));
         }
         mm = nm;
       }
     }
-    if (SUM) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    }
-    if (SUM && by_product(mm * c2)) s *= ex2_approx(fmaf(mm, c2, -(mm * c2)));  // to the reference that sets without odd logits have
-    return s;
+    if (SUM) s = warp_sum(s);
+    if (SUM && by_product(mm * c2)) s *= exp2((double)mm * (double)c2 - (double)(mm * c2));  // to the reference that sets without odd logits have
+    return (float)s;
   }
 
   // Tokens with codes in [lo, lo + span) per bin of 2^sft codes, of the listed tokens or of the listed chunks.  (32-bit
@@ -900,13 +898,14 @@ struct Sampler {
   }
 
   // The token that u falls to by shared().psum, whose entries hold 2^size positions each.  slack: relative error of those sums;
-  // false where it leaves the token open, or where there is no mass.
+  // false where it leaves the token open, or where there is no mass.  The entry that u falls into is looked at in 64 bits.
+  // With sums S = M (1 + e) and P in front of that entry, u total - P is off by u times the errors from the entry on minus (1 - u)
+  // times those in front of it: by slack ((1 - u) P + u (total - P)) at most.
   __device__ __forceinline__ bool locate(const Kept& kept, double u, int size, double slack, uint32_t* pos, double* total_out) {
     double mine = 0.0, total;
 #pragma unroll
     for (int i = 0; i < kPerC; ++i) mine += shared().psum[threadIdx.x * kPerC + i];
     double before = block_scan<THREADS>(mine, shared().wred, &total);
-    *total_out = total;
     if (!(total > 0.0 && total < CUDART_INF)) return false;  // no entry to look into
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
@@ -940,11 +939,13 @@ struct Sampler {
     __syncthreads();
     if (threadIdx.x < 32) {
       const int lane = threadIdx.x;
-      double front = shared().mabove;
-      const double margin = slack * total;
+      const double first = shared().mabove;
+      const double margin = slack > 0.0 ? slack * ((1.0 - u) * first + u * (total - first)) + 1e-12 * total : 0.0;
+      double front = first;
       uint32_t last = row.mis;  // last kept position so far
-      bool sure = true, done = false;
-      for (int k = 0; k < 1 << (size - 8) && !done; ++k) {
+      bool sure = true, done = false, likely = false;
+      const int parts = 1 << (size - 8);
+      for (int k = 0; k < parts && (!done || likely); ++k) {
         const uint32_t p = (shared().at << size) + (uint32_t)k * 256u + lane * 8;
         float a[8];
         Row::unpack(row.load(p), a);
@@ -960,8 +961,9 @@ struct Sampler {
         const double incl = warp_scan(mine);
         const unsigned hit = __ballot_sync(0xffffffffu, front + incl > x && mine > 0.0);
         const unsigned some = __ballot_sync(0xffffffffu, mlast >= 0);
-        if (hit) {
+        if (!done && hit) {
           const int src = __ffs((int)hit) - 1;
+          bool half = false;
           if (lane == src) {
             double f = front + (incl - mine), border = f;
             int at = 0;
@@ -978,8 +980,10 @@ struct Sampler {
             if (margin > 0.0) sure = x - border > margin && f - x > margin;
             shared().pos = p + at;
             shared().found = sure ? 1 : 0;
+            half = slack > 0.0 && f - border > 0.5 * total;
           }
           done = true;
+          likely = __any_sync(0xffffffffu, half);
         } else if (some) {
           const int src = 31 - __clz((int)some);
           last = __shfl_sync(0xffffffffu, p + mlast, src);
@@ -988,10 +992,14 @@ struct Sampler {
       }
       if (!done && lane == 0) {
         shared().pos = last;
-        shared().found = margin > 0.0 ? 0 : 1;
+        shared().found = slack > 0.0 ? 0 : 1;
       }
+      // for a token that has more than half of it the total has the entry's own mass in 64 bits: its log probability is near 0, and off
+      // by a share of what others hold
+      if (lane == 0) shared().mabove = likely ? total - shared().psum[shared().at] + (front - first) : total;
     }
     __syncthreads();
+    *total_out = shared().mabove;
     *pos = shared().pos;
     const bool ok = shared().found != 0;
     __syncthreads();
@@ -1195,12 +1203,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
   }
   S.set_top(m);
   typename Sampler<DT, THREADS>::Kept kept{-3.402823466e38f, m, S.row.end};
-  // Relative error of the sweep's sums.  Were all roundings to go one way: exponentials 2^-22; their arguments, and the rounding
-  // of c2, 2 roundings, where |t|, weighted by the terms themselves, is log2(tokens) + 1.5 on the mean; 10 additions: 1.8e-6.
-  // They do not: sums of a thousand terms are off by some 2e-8.  Taken is 5e-7, which holds for an error of the
-  // exponential or of c2 that all terms share as well; in chunks beyond 256 tokens the worst case, with a reference that
-  // changes on the way.
-  const double eps = A.shift ? 2.5e-7 + 0.84e-7 * (11.5 + A.shift) + 6e-8 * (16.0 + 8.0 * (double)(4 << A.shift)) : 5e-7;
+  // Relative error of the sweep's sums, were all roundings to go one way: exponentials 1.5e-7 (measured for every argument). Their
+  // exponents t, 2^-24 |t| per rounding: two, the difference's and c2's own (the sets' references are set off against one another in
+  // 64 bits), where |t|, weighted by the terms of 1024, is 6.4 at most on the mean (one term of 1, 1023 of 2^-7.85) and 0.5
+  // more by the reference's rounding.  Ten additions, 2^-24 each.  Rows with many equal logits come near it: one token above
+  // 152063 equal ones is off by 5e-7 by c2 alone where their sums are taken relative to the row's.  Odd sets and chunks beyond 256
+  // tokens have three roundings per exponent, a mean that grows by one per doubling, and 64-bit additions.
+  const double eps = 1.5e-7 + 5.97e-8 * (19.3 + 2.1 * A.shift);
   double total = 0.0;
   uint32_t pos = S.row.mis;
   bool done = false;
@@ -1210,12 +1219,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       if (4 * g < S.nch) {
         const float mm = fmaxf(fmaxf(sh.cmax[4 * g], sh.cmax[4 * g + 1]), fmaxf(sh.cmax[4 * g + 2], sh.cmax[4 * g + 3]));
         if (mm > -CUDART_INF_F)
-          y = (double)sh.csum[g] * (S.by_product(mm * c2) ? exp2((double)(mm * c2) - (double)m * (double)c2) : S.weight(mm));
+          y = (double)sh.csum[g] * exp2(((double)mm - (double)m) * S.it2 + (S.by_product(mm * c2) ? (double)(mm * c2) - (double)mm * (double)c2 : 0.0));
       }
       sh.psum[g] = y;
     }
     __syncthreads();
-    if (!use_p) done = Calls::locate(S, kept, (double)u, 10 + A.shift, 2.2 * eps, &pos, &total);
+    if (!use_p) done = Calls::locate(S, kept, (double)u, 10 + A.shift, 1.01 * eps, &pos, &total);
   }
   if (!done) {
     // the least code that min-p keeps
