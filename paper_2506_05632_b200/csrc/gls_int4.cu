@@ -52,6 +52,8 @@ static unsigned ctas_for(long long rows, int lanes) {
   return (unsigned)(n < cap ? n : cap);
 }
 
+constexpr int kHeadShared = 227 * 1024;  // at most per CTA
+
 // shared memory per hidden state
 static long long head_column_bytes(int parts, int chunks, int uc) { return (long long)parts * ((chunks + uc - 1) / uc) * uc * 256; }
 
@@ -95,7 +97,8 @@ static cudaError_t launch_head_unit(HeadArgs& A, const CUtensorMap& codes, int c
                                                 : cols == 2 ? head_kernel<GPC, PARTS, 2, UC>
                                                             : head_kernel<GPC, PARTS, 0, UC>;
   const int smem = (int)(HeadLayout::fixed(GPC, UC, warps) + head_column_bytes(PARTS, A.chunks, UC) * cols);
-  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  // the same for every call: another thread's may come between this and the launch
+  const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadShared);
   if (err != cudaSuccess) return err;
   dim3 grid((unsigned)(A.tiles < sm_count() ? A.tiles : sm_count()), (unsigned)((A.N + cols - 1) / cols));
   kernel<<<grid, 32 * warps, smem, st>>>(A, codes);
@@ -106,7 +109,7 @@ static cudaError_t launch_head_unit(HeadArgs& A, const CUtensorMap& codes, int c
 // products) where that takes none of them away and a row has that many chunks, otherwise of two.
 template <int GPC, int PARTS>
 static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream_t st) {
-  const long long most = 227 * 1024, want = A.N < 8 ? A.N : 8;
+  const long long most = kHeadShared, want = A.N < 8 ? A.N : 8;
   if (A.chunks >= 4 && (most - HeadLayout::fixed(GPC, 4, kHeadWarps)) / head_column_bytes(PARTS, A.chunks, 4) >= want)
     return launch_head_unit<GPC, PARTS, 4>(A, codes, (int)want, kHeadWarps, st);
   int warps = kHeadWarps;
@@ -120,7 +123,7 @@ static cudaError_t launch_head(HeadArgs& A, const CUtensorMap& codes, cudaStream
 // the other one 78 .. 100 us, 9 .. 64 by this one 147 .. 190; 8 fp32 ones 233 in two passes and 209).
 static bool head_is_wide(long long N, int parts, long long D) {
   const int chunks = (int)((D + 127) / 128);
-  return N > 8 || N * head_column_bytes(parts, chunks, 2) > 2 * (227 * 1024 - HeadLayout::fixed(4, 2, kHeadWarps));
+  return N > 8 || N * head_column_bytes(parts, chunks, 2) > 2 * (kHeadShared - HeadLayout::fixed(4, 2, kHeadWarps));
 }
 // How: passes of equal size, 16 .. 64 hidden states at a time.
 struct WidePlan {
