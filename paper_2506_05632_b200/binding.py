@@ -1,6 +1,7 @@
 """ctypes binding of libgls.so (C ABI in include/gls.h).  Argument marshalling only."""
 import ctypes as C
 import importlib.util
+import math
 import os
 import shutil
 import subprocess
@@ -1070,7 +1071,12 @@ def _setting(s, name, value, dtype, lead, dev):
     """Puts one sampling setting, a number or a tensor [B], [B,K] or [B,K,J] (sizes of 1 broadcast), into s."""
     if not isinstance(value, torch.Tensor):
         if dtype is not _I32:
-            setattr(s, name, float(value))
+            try:
+                setattr(s, name, float(value))
+            except OverflowError:
+                raise GlsError("%s is beyond fp32's range" % name) from None
+            if name == "inv_temp" and math.isinf(s.inv_temp) and not math.isinf(value):  # infinity is a setting of its own
+                raise GlsError("inv_temp is beyond fp32's range")
         elif value != value or value in (float("inf"), -float("inf")) or int(value) != value:
             raise GlsError("%s must be a whole number" % name)
         else:

@@ -14,6 +14,7 @@
 #include <c10/cuda/CUDAStream.h>
 
 #include <climits>
+#include <cmath>
 #include <optional>
 #include <type_traits>
 
@@ -319,7 +320,9 @@ const T* setting(PyObject* o, at::ScalarType type, at::IntArrayRef lead, c10::De
       if (v < INT_MIN || v > INT_MAX) throw Decline();
       *value = (T)v;
     } else {
-      *value = (T)number(o);
+      const double v = number(o);
+      *value = (T)v;
+      if (std::isinf(*value) && !std::isinf(v)) throw Decline();  // beyond fp32
     }
     return nullptr;
   }
