@@ -50,14 +50,28 @@ static cudaError_t launch_sample_rows(SampleArgs& A, long long rows, cudaStream_
   while ((((long long)A.V + 7 + (256LL << A.shift) - 1) >> (8 + A.shift)) > kSampleChunks) ++A.shift;
   // few rows: several CTAs sweep one, so that most SMs have a share of it
   const int sms = sm_count();
-  if (A.V <= 8192) return launch_sample<DT, 128>(A, rows, 1, st);
-  // More rows than SMs: four small CTAs an SM hide one another's waits, a large one is done sooner with a row that has to be
-  // summed in 64 bits.  128256 bf16 tokens, the same rows, small / large: top-k 50 and top-p 0.9, 200 rows 33 / 40 us,
-  // 592 59 / 88, 888 90 / 126; min-p 0.05, 592 46 / 63; top-k 1000 alone 592 170 / 185, but 296 115 / 90; where rows may be
-  // summed, settings of their own, 200 rows 192-220 / 110-129, 512 222-236 / 139-193, 888 262-319 / 225-241, 2048 409-435 /
-  // 436-470; nothing restricted, 592 115-132 / 81-113, 888 135 / 123-141, 2048 195-200 / 240-262.
-  if (rows * 2 > sms)
-    return rows > (may_sum(A) ? 4 : 1) * (long long)sms ? launch_sample<DT, 256>(A, rows, 1, st) : launch_sample<DT, 512>(A, rows, 1, st);
+  // One CTA a row: four small ones an SM hide one another's waits, a large one is done sooner with a row that has to be summed in 64
+  // bits or has many tokens to choose among.  Rows without such work take the small one beyond one row an SM, others once the rest of
+  // the grid hides theirs, the later the longer they are: beyond one row an SM per 48 KB of a row where nothing restricts them, per
+  // 32 KB with top-p or a large top-k, per 16 KB with settings of their own.  bf16 rows of 32000 / 152064 tokens, small : large, us:
+  // min-p 0.05, 200 rows 19 : 24 / 30 : 34, 1184 42 : 80 / 96 : 129; nothing, 200 rows 18 : 24 / 73 : 56, 592 38 : 48 / 136 : 108,
+  // 1776 76 : 144 / 213 : 252; p = 0.9, 200 rows 68 : 66 / 223 : 130, 592 73 : 110 / 303 : 249, 1776 199 : 313 / 622 : 670; top-k
+  // 1000, 200 rows 86 : 88 / 110 : 100, 592 115 : 172 / 194 : 207 (fp32 128256: 395 : 222); settings of their own, 296 rows
+  // 110 : 92 / 282 : 175, 592 120 : 134 / 356 : 260, 2368 378 : 422 / 644 : 622.
+  const bool sums = may_sum(A), many = !A.top_k.rows && A.top_k.ivalue > 256 && A.top_k.ivalue < A.V;
+  const bool own = A.inv_temp.rows || A.top_k.rows || A.top_p.rows || A.min_p.rows;
+  const bool top_p = A.top_p.rows || A.top_p.value < 1.f;
+  if (A.V <= 8192) {
+    // A few KB a row: eight CTAs of 128 threads an SM once four of 256 leave rows waiting, where there is little to do for one.
+    // bf16 rows of 1000 / 8192 tokens, 128 : 256 threads: nothing, 592 rows 18 : 17 / 21 : 19, 740 18 : 25 / 23 : 25; top-k 1, 740 rows
+    // 18 : 28 / 18 : 26; p = 0.9, 888 rows 55 : 50 / 66 : 56; settings of their own, 740 rows 64 : 68 / 97 : 84.
+    return rows > 4LL * sms && !many && !(sums && (own || top_p)) ? launch_sample<DT, 128>(A, rows, 1, st) : launch_sample<DT, 256>(A, rows, 1, st);
+  }
+  if (rows * 2 > sms) {
+    const long long bytes = (long long)A.V * SampleRow<DT>::ES, unit = many ? 32768 : own ? 16384 : top_p ? 32768 : 49152;
+    const bool large = rows <= sms || ((sums || many) && rows * unit <= bytes * sms);
+    return large ? launch_sample<DT, 512>(A, rows, 1, st) : launch_sample<DT, 256>(A, rows, 1, st);
+  }
   int ctas = 2;
   while (ctas < 8 && rows * ctas * 2 <= sms && A.V > 8192 * ctas) ctas *= 2;
   return launch_sample<DT, 512>(A, rows, ctas, st);
