@@ -177,8 +177,9 @@ struct EmbedInt4Args {
   uint32_t* status;
 };
 
-template <int DT, bool VEC>  // VEC: 16 columns of a row of the output are aligned 16-byte words
+template <int DT, bool VEC>  // VEC: 16 columns of a row of the output are aligned 16-byte words (of bf16)
 __global__ void __launch_bounds__(kInt4Threads) embed_int4_kernel(const EmbedInt4Args A) {
+  static_assert(!VEC || DT == kBF16, "fp32 rows go through shared memory");
   constexpr int ES = DT == kBF16 ? 2 : 4;
   const Int4Table& T = A.T;
   const int units = (int)((T.D + 15) >> 4), D = (int)T.D;
@@ -226,22 +227,14 @@ __global__ void __launch_bounds__(kInt4Threads) embed_int4_kernel(const EmbedInt
       if (VEC) {
         if (!row_there || unit >= units) continue;
         if (d + 16 <= D) {
-          if constexpr (DT == kBF16) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              ((uint4*)q)[h] = make_uint4(bf16_pair(y[8 * h], y[8 * h + 1]), bf16_pair(y[8 * h + 2], y[8 * h + 3]),
-                                          bf16_pair(y[8 * h + 4], y[8 * h + 5]), bf16_pair(y[8 * h + 6], y[8 * h + 7]));
-          } else {
-#pragma unroll
-            for (int h = 0; h < 4; ++h) ((float4*)q)[h] = make_float4(y[4 * h], y[4 * h + 1], y[4 * h + 2], y[4 * h + 3]);
-          }
+          for (int h = 0; h < 2; ++h)
+            ((uint4*)q)[h] = make_uint4(bf16_pair(y[8 * h], y[8 * h + 1]), bf16_pair(y[8 * h + 2], y[8 * h + 3]),
+                                        bf16_pair(y[8 * h + 4], y[8 * h + 5]), bf16_pair(y[8 * h + 6], y[8 * h + 7]));
         } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (d + i < D) {
-              if constexpr (DT == kBF16) ((unsigned short*)q)[i] = (unsigned short)bf16_bits(y[i]);
-              else ((float*)q)[i] = y[i];
-            }
+            if (d + i < D) ((unsigned short*)q)[i] = (unsigned short)bf16_bits(y[i]);
         }
       } else {  // out of shared memory, columns by neighbouring lanes
         __syncwarp();
