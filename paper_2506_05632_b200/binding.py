@@ -1099,7 +1099,7 @@ def sample_tokens(logits, uniforms, inv_temp=1.0, top_k=0, top_p=1.0, min_p=0.0,
     Each setting is a number or a tensor with a value per sequence [B], or [B,K], or [B,K,J].  inv_temp = inf
     takes the most likely token, top_k < 1 and top_p = 1 and min_p = 0 do not restrict.  Given `out`, its
     tensors are written (log probabilities where it has them).  Not differentiable (see token_logprobs)."""
-    _no_tangent(logits)
+    _no_tangent(logits, inv_temp, top_p, min_p)
     _no_gradient("sample_tokens", logits, inv_temp, top_p, min_p)
     if out is None:
         r = (_calls or _fast()).sample_tokens(logits, uniforms, inv_temp, top_k, top_p, min_p, want_logprobs, status)

@@ -21,6 +21,14 @@ def test_numbers_that_are_taken():
         assert getattr(s, name) == want
 
 
+@pytest.mark.parametrize("name", ["inv_temp", "top_p", "min_p"])
+def test_a_setting_with_a_tangent(name):
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(torch.ones(1), torch.ones(1))
+        with pytest.raises(gls.GlsError, match="forward-mode"):
+            gls.sample_tokens(torch.zeros(1, 1, 1, 8), torch.zeros(1, 1, 1), **{name: dual})
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("value", [1e39, 1e300, 10 ** 50, 10 ** 400], ids=["1e39", "1e300", "10^50", "10^400"])
 def test_calls_with_it(gls, monkeypatch, value):
