@@ -1261,7 +1261,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       const int nth = kk <= S.nch ? kk : max(1, min(S.nch, (int)((float)S.nch * (1.f - __expf(-1.5f * (float)kk / (float)S.nch)))));
       uint32_t cut = Calls::kth_chunk(S, (uint32_t)nth);
       bool limited = false;
-      for (;;) {
+      for (int tries = 0;; ++tries) {
         if (cut < lowest) cut = lowest;
         Calls::make_list(S, Row::value(cut));
         if (kk <= kSampleList / 3 * 2) S.listed = Calls::gather(S, Row::value(cut), m);  // +inf and NaN are masked
@@ -1272,8 +1272,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
         }
         limited = Calls::kth(S, cut, (uint32_t)kk, &code, &take, &equal);
         if (limited || cut == lowest) break;
+        // Further down by half of the way so far, by a code at least (below 0 a bf16 code holds what lies less than a step below its
+        // value); after eight times to the end, which rows with fewer than k tokens come to.
         const float v = Row::value(cut), further = v - (m - v) * 0.5f;
-        cut = further < v && further > -3.402823466e38f ? Row::key(further) : lowest;
+        cut = tries < 8 && further > -3.402823466e38f ? min(Row::key(further), cut - 1u) : lowest;
       }
       if (!limited) take = equal = 0u, code = cut;
       if (!done && use_p && Calls::nucleus(S, code, equal - take, true, false, (double)p, 0.0, 0.0, &pc, &pt, &pe) == 1) code = pc, take = pt, equal = pe;
