@@ -570,7 +570,7 @@ int gls_embed_tokens_backward(const void* grad_out, int dtype, int64_t grad_out_
  *            if the mass in front of it is below that; 1 and above: all of them);
  *     min_p  of these the tokens with (l_i - max l) inv_temp >= ln(min_p) (0: all of them);
  * the first token of the order always stays.  Drawn is the first token BY INDEX whose cumulative mass among the
- * kept ones exceeds u times their total (u = 1: the last kept one); its log probability is among the
+ * kept ones exceeds u times their total (u = 0: the first kept one, u = 1: the last; weights below 2^-1000 are 0); its log probability is among the
  * kept ones.  inv_temp = +inf is the limit of low temperature: the first token of the order, log probability 0.
  * What is decided is decided by counts and by 64-bit sums of 64-bit exponentials; fp32 sums decide only where the border is
  * further away than their error can move it.  Log probabilities are rounded to fp32 from 64 bits where top_k, top_p or min_p

@@ -1034,11 +1034,13 @@ struct Sampler {
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
     if (x > most) x = most;
-    if (i == 0) shared().found = 0, shared().at = 0u;
+    if (i == 0) shared().found = 0, shared().at = u == 0.0 ? 0xffffffffu : 0u;
     __syncthreads();
     if (y > 0.0) {
-      atomicMax(&shared().at, (uint32_t)i);  // the last one with weight, for borders that rounding leaves without x
-      if (f <= x && x < f + y) {
+      // the last one with weight, for borders that rounding leaves without x and for u = 1; for u = 0 the first
+      if (u == 0.0) atomicMin(&shared().at, (uint32_t)i);
+      else atomicMax(&shared().at, (uint32_t)i);
+      if (u > 0.0 && u < 1.0 && f <= x && x < f + y) {
         shared().pos = shared().place[i];
         shared().found = 1;
       }
@@ -1066,7 +1068,7 @@ struct Sampler {
     if (x > most) x = most;
     if (threadIdx.x == 0) shared().found = 0, shared().pos = row.mis;
     __syncthreads();
-    if (mine > 0.0 && f <= x && x < f + mine) {
+    if (u > 0.0 && u < 1.0 && mine > 0.0 && f <= x && x < f + mine) {
       r = rank;
       for (int i = from; i < upto; ++i) {
         const uint32_t k = shared().key[i];
@@ -1080,12 +1082,14 @@ struct Sampler {
       }
     }
     __syncthreads();
-    // the threads' borders are rounded sums: where none holds x, the last token with weight
+    // the threads' borders are rounded sums: where none holds x, and for u = 1, the last token with weight; for u = 0 the first
     if (!shared().found && threadIdx.x == 0) {
       r = 0u;
       for (int i = 0; i < listed; ++i) {
         const uint32_t k = shared().key[i];
-        if ((k > code || (k == code && r++ < take)) && weight(Row::value(k)) > 0.0) shared().pos = shared().place[i];
+        if (!(k > code || (k == code && r++ < take)) || !(weight(Row::value(k)) > 0.0)) continue;
+        shared().pos = shared().place[i];
+        if (u == 0.0) break;
       }
     }
     __syncthreads();
@@ -1224,7 +1228,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       sh.psum[g] = y;
     }
     __syncthreads();
-    if (!use_p) done = Calls::locate(S, kept, (double)u, 10 + A.shift, 1.01 * eps, &pos, &total);
+    // (the ends of the unit interval have tokens whose weights no sum may round away)
+    if (!use_p && u > 0.f && u < 1.f) done = Calls::locate(S, kept, (double)u, 10 + A.shift, 1.01 * eps, &pos, &total);
   }
   if (!done) {
     // the least code that min-p keeps
@@ -1315,6 +1320,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 512 ? 1 : 1024 / THREADS) 
       if (take < equal) kept.end = Calls::equal_end(S, code, take);
       Calls::exact_sums(S, kept);
       Calls::locate(S, kept, (double)u, 8 + A.shift, 0.0, &pos, &total);
+      if (!(u > 0.f && u < 1.f)) {  // the first or the last one that has a weight, by their number: weights of 1
+        double number;
+        S.it2 = 0.0;
+        Calls::exact_sums(S, kept);
+        Calls::locate(S, kept, (double)u, 8 + A.shift, 0.0, &pos, &number);
+      }
     }
   }
   if (threadIdx.x == 0) {
