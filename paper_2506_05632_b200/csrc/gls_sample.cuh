@@ -200,11 +200,18 @@ struct SampleShared {
   uint32_t pos;
 };
 
-// exclusive prefix of x over the block; *total: the sum over all
+// the value of the lane in front, 0 in the first: from an inclusive scan what lies in front, with nothing taken off again (which
+// would leave a small sum in front of a large term the rounding of the latter)
+template <class T>
+__device__ __forceinline__ T lane_before(T incl) {
+  const T y = __shfl_up_sync(0xffffffffu, incl, 1);
+  return threadIdx.x & 31 ? y : (T)0;
+}
+// Exclusive prefix of x over the block; *total: the sum over all; *end: where the next thread begins, to the bit.
 template <int THREADS, class T>
-__device__ __forceinline__ T block_scan(T x, T* red, T* total) {
+__device__ __forceinline__ T block_scan(T x, T* red, T* total, T* end = nullptr) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const T incl = warp_scan(x);
+  const T incl = warp_scan(x), front = lane_before(incl);
   __syncthreads();  // earlier readers of red are done
   if (lane == 31) red[warp] = incl;
   __syncthreads();
@@ -216,7 +223,8 @@ __device__ __forceinline__ T block_scan(T x, T* red, T* total) {
     all += y;
   }
   *total = all;
-  return before + (incl - x);
+  if (end) *end = before + incl;
+  return before + front;
 }
 
 template <int DT, int THREADS>
@@ -902,39 +910,25 @@ struct Sampler {
   // With sums S = M (1 + e) and P in front of that entry, u total - P is off by u times the errors from the entry on minus (1 - u)
   // times those in front of it: by slack ((1 - u) P + u (total - P)) at most.
   __device__ __forceinline__ bool locate(const Kept& kept, double u, int size, double slack, uint32_t* pos, double* total_out) {
-    double mine = 0.0, total;
+    double mine = 0.0, total, end;
 #pragma unroll
     for (int i = 0; i < kPerC; ++i) mine += shared().psum[threadIdx.x * kPerC + i];
-    double before = block_scan<THREADS>(mine, shared().wred, &total);
+    if (threadIdx.x == 0) shared().at = 0u, shared().mabove = 0.0;
+    double before = block_scan<THREADS>(mine, shared().wred, &total, &end);
     if (!(total > 0.0 && total < CUDART_INF)) return false;  // no entry to look into
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
     if (x > most) x = most;
-    if (threadIdx.x == 0) shared().found = 0, shared().pos = row.mis;
-    __syncthreads();
-    // the pieces' borders are rounded sums: where none holds x, the last chunk with mass does
-    if (mine > 0.0 && before <= x && x < before + mine) {
+        if (before <= x && x < end) {
       for (int i = 0; i < kPerC; ++i) {
         const double y = shared().psum[threadIdx.x * kPerC + i];
         if (y > 0.0) {
           shared().at = threadIdx.x * kPerC + i;
           shared().mabove = before;
-          shared().found = 1;
           if (x < before + y) break;
         }
         before += y;
       }
-    }
-    __syncthreads();
-    if (!shared().found && threadIdx.x == 0) {
-      double b = 0.0;
-      for (int c = 0; c < kSampleChunks; ++c)
-        if (shared().psum[c] > 0.0 && (b <= x || !shared().found)) {
-          shared().at = (uint32_t)c;
-          shared().mabove = b;
-          shared().found = 1;
-          b += shared().psum[c];
-        }
     }
     __syncthreads();
     if (threadIdx.x < 32) {
@@ -958,14 +952,14 @@ struct Sampler {
           mine += w[i];
           if (w[i] > 0.0) mlast = i;
         }
-        const double incl = warp_scan(mine);
+        const double incl = warp_scan(mine), ahead = lane_before(incl);
         const unsigned hit = __ballot_sync(0xffffffffu, front + incl > x && mine > 0.0);
         const unsigned some = __ballot_sync(0xffffffffu, mlast >= 0);
         if (!done && hit) {
           const int src = __ffs((int)hit) - 1;
           bool half = false;
           if (lane == src) {
-            double f = front + (incl - mine), border = f;
+            double f = front + ahead, border = f;
             int at = 0;
             bool open = true;
             // the lane's sums in order; the last of its kept tokens where rounding leaves none
@@ -1030,17 +1024,18 @@ struct Sampler {
       if (stay < k) k = stay ? stay : 1u;
     }
     const bool kept = have && (rank < k && mine >= floor_code || rank == 0u);
-    const double y = kept ? w : 0.0, f = block_scan<THREADS>(y, shared().wred, &total);
+    double end;
+    const double y = kept ? w : 0.0, f = block_scan<THREADS>(y, shared().wred, &total, &end);
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
     if (x > most) x = most;
     if (i == 0) shared().found = 0, shared().at = u == 0.0 ? 0xffffffffu : 0u;
     __syncthreads();
     if (y > 0.0) {
-      // the last one with weight, for borders that rounding leaves without x and for u = 1; for u = 0 the first
+      // for u = 1 the last one with weight, for u = 0 the first
       if (u == 0.0) atomicMin(&shared().at, (uint32_t)i);
       else atomicMax(&shared().at, (uint32_t)i);
-      if (u > 0.0 && u < 1.0 && f <= x && x < f + y) {
+      if (u > 0.0 && u < 1.0 && f <= x && x < end) {
         shared().pos = shared().place[i];
         shared().found = 1;
       }
@@ -1056,19 +1051,18 @@ struct Sampler {
     uint32_t equal = 0u, all;
     for (int i = from; i < upto; ++i) equal += shared().key[i] == code ? 1u : 0u;
     const uint32_t rank = block_scan<THREADS>(equal, shared().ired, &all);
-    double mine = 0.0, total;
+    double mine = 0.0, total, end;
     uint32_t r = rank;
     for (int i = from; i < upto; ++i) {
       const uint32_t k = shared().key[i];
       if (k > code || (k == code && r++ < take)) mine += weight(Row::value(k));
     }
-    double f = block_scan<THREADS>(mine, shared().wred, &total);
+    if (threadIdx.x == 0) shared().pos = row.mis;
+    double f = block_scan<THREADS>(mine, shared().wred, &total, &end);
     double x = u * total;
     const double most = total * (1.0 - 1.2e-16);
     if (x > most) x = most;
-    if (threadIdx.x == 0) shared().found = 0, shared().pos = row.mis;
-    __syncthreads();
-    if (u > 0.0 && u < 1.0 && mine > 0.0 && f <= x && x < f + mine) {
+    if (u > 0.0 && u < 1.0 && f <= x && x < end) {
       r = rank;
       for (int i = from; i < upto; ++i) {
         const uint32_t k = shared().key[i];
@@ -1076,14 +1070,13 @@ struct Sampler {
         const double w = weight(Row::value(k));
         if (!(w > 0.0)) continue;
         shared().pos = shared().place[i];
-        shared().found = 1;
         f += w;
         if (f > x) break;
       }
     }
     __syncthreads();
-    // the threads' borders are rounded sums: where none holds x, and for u = 1, the last token with weight; for u = 0 the first
-    if (!shared().found && threadIdx.x == 0) {
+    // for u = 1 the last token with weight, for u = 0 the first
+    if (!(u > 0.0 && u < 1.0) && threadIdx.x == 0) {
       r = 0u;
       for (int i = 0; i < listed; ++i) {
         const uint32_t k = shared().key[i];
