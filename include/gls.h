@@ -631,9 +631,9 @@ typedef struct {
  * Weights -> table, to the nearest code.  Per group, with lo = min(0, min w) and hi = max(0, max w):
  *     with zeros:    scale = (hi - lo) / 15, zero = -lo / scale, code = w / scale + zero
  *     without:       scale = max |w| / 7, code = w / scale + 8
- * each quotient rounded to fp32, the scale from there to its type, zero and w / scale to integers (ties to
+ * hi - lo and each quotient rounded to fp32, the scale from there to its type, zero and w / scale to integers (ties to
  * even), codes and zeros held to 0 .. 15.  A group of zeros gets scale 0 and the codes of zero; one with a weight
- * that is not finite, or whose scale is beyond its type, the scale NaN.  Codes beyond D within a byte are 0.
+ * that is not finite, or whose scale is beyond its type or hi - lo beyond fp32, the scale NaN.  Codes beyond D within a byte are 0.
  *   weights [V,D] of type dtype, rows contiguous, weight_stride elements apart; table: written
  */
 int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, const gls_int4_table_t* table,
@@ -641,7 +641,8 @@ int gls_quantize_table(const void* weights, int dtype, int64_t weight_stride, co
 
 /*
  * Logits of hidden states: out[n,v] = sum over d of x[n,d] * element(v, d), the products of a group summed in
- * fp32 and multiplied by its scale in fp32, the sum rounded once to the output's type.  bf16 x goes in as it is, fp32 x
+ * fp32 and multiplied by its scale in fp32, the sum rounded once to the output's type.  The tensor cores' additions cut
+ * below 24 bits instead of rounding: fp32 logits of 32000 x 1024 are off by up to 2.3e-7 of the largest.  bf16 x goes in as it is, fp32 x
  * in three parts that hold all of its 24 bits.  Up to 8 rows of x take one kernel and no workspace (fewer where D is so
  * large that shared memory does not hold them), more another one, 64 of them per pass over the table.
  *   x [N,D], out [N,V] of types x_dtype, out_dtype (fp32 or bf16), rows contiguous, strides in elements

@@ -42,9 +42,11 @@ __device__ __forceinline__ int swap_at(int column) { return (column >> 4) * 17 +
 // by shuffles, so the weights are read once and nothing but the table is written.
 // Roundings: the step to fp32 and to its type, the quotient weight / step to fp32, that to an integer
 // (ties to even).  A group with a weight that is not finite gets the step NaN, codes and zero 0.
-// The quotients are the reciprocal's product corrected by its remainder (Markstein's theorem: with the reciprocal rounded to
-// nearest, q + (x - q step) / step is the quotient rounded to nearest), three operations instead of a division each
-// (128256 x 4096 bf16: 855 us with divisions).
+// The quotients are the reciprocal's product q corrected by its remainder, q + (x - q step) / step: three operations instead of a
+// division each (128256 x 4096 bf16: 855 us with divisions).  Markstein's theorem gives the quotient rounded to nearest where
+// q is off by less than a step of fp32, which in one pair of sixty it is not.  What is wanted are integers, and
+// those hang on the quotients next to half steps: for every mantissa of the step and the five weights
+// around each half step (671 million pairs, on the host) the corrected quotient is the division's.
 // ------------------------------------------------------------------------------------------
 struct QuantizeArgs {
   const void* w;
